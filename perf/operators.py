@@ -11,6 +11,7 @@ import torch
 own = False
 
 TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+GATES = {"none": 0, "channel": 1, "row": 2, "full": 3}         # CORAL_GATE_*
 NO_TOKEN = 0x7FFFFFFF          # id of a candidate that does not exist (fewer active tokens than candidates)
 EPS = 1e-5
 
@@ -300,7 +301,7 @@ def _own_logits(s):
 def _own_norm(s):
     from paper_2502_16880_b200 import lmhead
     lmhead.coral_lmhead_block_norm(s["block"], s["resid"], s["w_pre"], EPS, s["stream"], s["hidden"], w_post=s["w_post"],
-                                   gate=s["g"], alpha=s["alpha"])
+                                   gate=s["g"], gate_mode=GATES[s["gate"]], alpha=s["alpha"])
     return dict(stream=s["stream"], hidden=s["hidden"])
 
 
@@ -308,7 +309,8 @@ def _own_norm_backward(s):
     from paper_2502_16880_b200 import lmhead
     lmhead.coral_lmhead_block_norm_backward(
         s["block"], s["resid"], s["w_pre"], EPS, s["d_stream"], s["d_hidden"], s["workspace"], s["d_block"], s["d_resid"],
-        s["d_w_pre"], w_post=s["w_post"], gate=s["g"], alpha=s["alpha"], d_w_post=s["d_w_post"], d_gate=s["d_g"])
+        s["d_w_pre"], w_post=s["w_post"], gate=s["g"], gate_mode=GATES[s["gate"]], alpha=s["alpha"],
+        out_dw_post=s["d_w_post"], out_dgate=s["d_g"])
     out = dict(d_resid=s["d_resid"], d_w_pre=s["d_w_pre"], d_block=s["d_block"])
     if s["post"]:
         out["d_w_post"] = s["d_w_post"]
