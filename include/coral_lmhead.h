@@ -390,6 +390,58 @@ int coral_tree_expand(const float *parent_scores_dev, const int32_t *cand_ids_de
                       int n_seq, int nodes, int k_tokens, int K, int32_t *out_parent_dev, int32_t *out_token_dev,
                       float *out_score_dev, void *stream);
 
+/* Element types of the operators around the draft step (block norm, 4-bit products, logits). */
+#define CORAL_TYPE_F32 0
+#define CORAL_TYPE_BF16 1
+#define CORAL_TYPE_F16 2
+
+/*
+ * Block norm: what makes the hidden rows that coral_lmhead_draft reads (the paper's drafter ends in the target model's
+ * kind of decoder block and norm; Section 2.2).  For every row of M, all sums in fp32, one rounding per output:
+ *   b = w_post ? x / sqrt(mean(x^2) + eps) * w_post : x      norm after the block
+ *   y = alpha * r + gate * b                                  gated, scaled residual
+ *   h = y / sqrt(mean(y^2) + eps) * w_pre                     norm before the next block, or before the head
+ * h is computed from y before its rounding.  gate_mode says how the gate is shared.
+ *   x, r [M x H] of `type`; r NULL: no residual (y = gate * b).  w_post, w_pre [H] of `type`; w_post NULL: no norm after
+ *   the block; w_pre NULL: no h (out_h must then be NULL).  gate of `type`: [H], [M] or [M x H] by gate_mode.
+ *   out_y, out_h [M x H] of `type`; out_y may be NULL when out_h is not.  An output may be the very buffer of x, r or a
+ *   full gate (not one that overlaps it in part).
+ * M >= 1; H a multiple of 8 and H * element size <= 32768; all pointers 16-byte aligned (a row gate: to its element);
+ * eps >= 0; else CORAL_ERR_INVALID.  A row of zeros with eps = 0 gives NaN, as the formula does.
+ * Asynchronous on `stream`, one launch, no scratch memory.
+ */
+#define CORAL_GATE_NONE 0
+#define CORAL_GATE_CHANNEL 1       /* gate [H] */
+#define CORAL_GATE_ROW 2           /* gate [M] */
+#define CORAL_GATE_FULL 3          /* gate [M x H] */
+
+typedef struct coral_lmhead_norm_args {
+    uint32_t struct_size;          /* sizeof(coral_lmhead_norm_args) */
+    int32_t type, M, H, gate_mode;
+    float alpha, eps;
+    const void *x_dev, *r_dev, *gate_dev, *w_post_dev, *w_pre_dev;
+    void *out_y_dev, *out_h_dev;             /* coral_lmhead_block_norm */
+    const void *dy_dev, *dh_dev;             /* coral_lmhead_block_norm_backward: gradients of y and h, [M x H] of `type` */
+    void *out_dx_dev, *out_dr_dev, *out_dgate_dev;
+    float *out_dw_pre_dev, *out_dw_post_dev;
+} coral_lmhead_norm_args;
+
+int coral_lmhead_block_norm(const coral_lmhead_norm_args *args, void *stream);
+
+/*
+ * Gradient of the block norm (training the drafter through it).  Reads x, r, gate, w_post, w_pre as above and dy, dh;
+ * either of the two may be NULL (no gradient comes that way; dh must be NULL when w_pre is, one of the two is needed).
+ *   out_dx [M x H] of `type` (required); out_dr [M x H] of `type`, NULL when r is or when not wanted;
+ *   out_dgate: fp32 [H] for a channel gate, fp32 [M] for a row gate, [M x H] of `type` for a full gate; may be NULL;
+ *   out_dw_pre, out_dw_post: fp32 [H]; may be NULL.
+ * Sums over rows are in fp32 in an order that depends on M, H and the device only: the same call gives the same bits.
+ * out_dx and out_dr may each be the buffer of x, r, dy or dh.  workspace_dev: 256-byte aligned, at least
+ * coral_lmhead_block_norm_backward_bytes(M, H) bytes of the current device; it holds nothing between calls, and two
+ * calls that may overlap on the GPU need one each.  Asynchronous on `stream`.
+ */
+int coral_lmhead_block_norm_backward_bytes(int M, int H, size_t *bytes);
+int coral_lmhead_block_norm_backward(const coral_lmhead_norm_args *args, void *workspace_dev, void *stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char *coral_lmhead_error_string(int code);
 

@@ -10,7 +10,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcoral_lmhead.so")
 LIB_CHECKED = os.path.join(PKG, "libcoral_lmhead_checked.so")   # same sources with -DCORAL_CHECK_BOUNDS
-SOURCES = [os.path.join(CSRC, "coral_lmhead.cu")]
+SOURCES = [os.path.join(CSRC, "coral_lmhead.cu"), os.path.join(CSRC, "coral_operators.cu")]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

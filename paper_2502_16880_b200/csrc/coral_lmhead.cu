@@ -14,6 +14,7 @@
 #include "copy_probe.cuh"
 #include "tc_probe.cuh"
 #include "csra.cuh"
+#include "launch.cuh"
 #include "merge.cuh"
 #include "route.cuh"
 #include "tree.cuh"
@@ -252,24 +253,7 @@ CallView make_view(const coral_lmhead_s* h, const void* hidden, int M, int kg, i
     return c;
 }
 
-// Launch with the programmatic-serialisation attribute: the kernel may begin while the previous kernel of
-// the stream is still running and synchronises with it through pdl_wait().
-template <typename... KArgs, typename... Args>
-cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
-}
-
-// The same for a kernel that runs as clusters of two CTAs.
+// launch_pdl for a kernel that runs as clusters of two CTAs.
 template <typename... KArgs, typename... Args>
 cudaError_t launch_pdl_pairs(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
     cudaLaunchConfig_t cfg{};

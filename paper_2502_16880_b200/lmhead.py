@@ -28,6 +28,8 @@ CORAL_ERR_TOO_LARGE = -7
 CORAL_ERR_NONFINITE = -8
 CORAL_ROUTE_STATIC_MAX_ROWS = 64
 CORAL_OUTPUT_JOINT, CORAL_OUTPUT_FACTORISED, CORAL_OUTPUT_FACTORISED_RENORM = 0, 1, 2
+CORAL_TYPE_F32, CORAL_TYPE_BF16, CORAL_TYPE_F16 = 0, 1, 2
+CORAL_GATE_NONE, CORAL_GATE_CHANNEL, CORAL_GATE_ROW, CORAL_GATE_FULL = 0, 1, 2, 3
 CORAL_PATH_AUTO, CORAL_PATH_STREAM, CORAL_PATH_TCGEN05, CORAL_PATH_SIMT_PLAIN, CORAL_PATH_ADAPTIVE = 0, 1, 2, 3, 4
 
 
@@ -42,6 +44,14 @@ class coral_lmhead_stats(ctypes.Structure):
                 ("k_tokens", ctypes.c_int32), ("groups_touched", ctypes.c_int32),
                 ("kernel_launches", ctypes.c_int32), ("weight_bytes", ctypes.c_int64),
                 ("algorithmic_bytes", ctypes.c_int64)]
+
+
+class coral_lmhead_norm_args(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("type", ctypes.c_int32), ("M", ctypes.c_int32), ("H", ctypes.c_int32),
+                ("gate_mode", ctypes.c_int32), ("alpha", ctypes.c_float), ("eps", ctypes.c_float)] + [
+        (n, ctypes.c_void_p) for n in ("x_dev", "r_dev", "gate_dev", "w_post_dev", "w_pre_dev", "out_y_dev", "out_h_dev",
+                                       "dy_dev", "dh_dev", "out_dx_dev", "out_dr_dev", "out_dgate_dev", "out_dw_pre_dev",
+                                       "out_dw_post_dev")]
 
 
 _lib = None
@@ -75,6 +85,9 @@ _SIGNATURES = {
     "coral_lmhead_last_stats": (_i, [_vp, ctypes.POINTER(coral_lmhead_stats), _vp]),
     "coral_lmhead_route_static": (_i, [_vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp]),
     "coral_tree_expand": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp]),
+    "coral_lmhead_block_norm": (_i, [ctypes.POINTER(coral_lmhead_norm_args), _vp]),
+    "coral_lmhead_block_norm_backward_bytes": (_i, [_i, _i, ctypes.POINTER(ctypes.c_size_t)]),
+    "coral_lmhead_block_norm_backward": (_i, [ctypes.POINTER(coral_lmhead_norm_args), _vp, _vp]),
     "coral_lmhead_error_string": (ctypes.c_char_p, [_i]),
     "coral_lmhead_destroy": (_i, [_vp]),
 }
@@ -343,6 +356,92 @@ def coral_tree_expand(parent_scores, cand_ids, cand_logprobs, K, out_parent, out
         _dev_ptr(parent_scores, torch.float32, False), _dev_ptr(cand_ids, torch.int32), _dev_ptr(cand_logprobs, torch.float32),
         n_seq, nodes, k_tokens, int(K), _dev_ptr(out_parent, torch.int32, False), _dev_ptr(out_token, torch.int32, False),
         _dev_ptr(out_score, torch.float32, False), _stream_ptr(stream)), "coral_tree_expand")
+
+
+_TYPES = {torch.float32: CORAL_TYPE_F32, torch.bfloat16: CORAL_TYPE_BF16, torch.float16: CORAL_TYPE_F16}
+
+
+def _type_of(t) -> int:
+    if t.dtype not in _TYPES:
+        raise ValueError(f"expected float32, bfloat16 or float16, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _op_ptr(name, t, dtype, shape, device):
+    """Pointer of an operator's tensor (None stays None) after checking type, shape, contiguity and device: the library
+    launches on the current device and reads and writes as many elements as the other arguments say."""
+    if t is None:
+        return None
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous CUDA tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: expected dtype {dtype}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _op_device(t, name):
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current CUDA device")
+    return t.device
+
+
+def _norm_args(x, r, w_pre, eps, w_post, gate, gate_mode, alpha):
+    dev = _op_device(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be [M, H]")
+    M, H = x.shape
+    t = x.dtype
+    shape = {CORAL_GATE_CHANNEL: (H,), CORAL_GATE_ROW: (M,), CORAL_GATE_FULL: (M, H)}.get(int(gate_mode))
+    return coral_lmhead_norm_args(
+        struct_size=ctypes.sizeof(coral_lmhead_norm_args), type=_type_of(x), M=M, H=H, gate_mode=int(gate_mode),
+        alpha=float(alpha), eps=float(eps), x_dev=_op_ptr("x", x, t, (M, H), dev), r_dev=_op_ptr("r", r, t, (M, H), dev),
+        gate_dev=_op_ptr("gate", gate, t, shape, dev), w_post_dev=_op_ptr("w_post", w_post, t, (H,), dev),
+        w_pre_dev=_op_ptr("w_pre", w_pre, t, (H,), dev)), dev
+
+
+def coral_lmhead_block_norm(x, r, w_pre, eps, out_y, out_h, w_post=None, gate=None, gate_mode=CORAL_GATE_NONE, alpha=1.0,
+                            stream=None):
+    """y = alpha r + gate b with b = x, or its norm times w_post; h = the norm of y times w_pre.  x, r, out_y, out_h:
+    [M, H]; gate: [H], [M] or [M, H] by gate_mode (CORAL_GATE_*).  r, w_pre with out_h, or out_y may be None."""
+    a, dev = _norm_args(x, r, w_pre, eps, w_post, gate, gate_mode, alpha)
+    a.out_y_dev = _op_ptr("out_y", out_y, x.dtype, x.shape, dev)
+    a.out_h_dev = _op_ptr("out_h", out_h, x.dtype, x.shape, dev)
+    _check(load_library().coral_lmhead_block_norm(ctypes.byref(a), _stream_ptr(stream)), "coral_lmhead_block_norm")
+
+
+def coral_lmhead_block_norm_backward_bytes(M: int, H: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load_library().coral_lmhead_block_norm_backward_bytes(int(M), int(H), ctypes.byref(b)),
+           "coral_lmhead_block_norm_backward_bytes")
+    return int(b.value)
+
+
+def coral_lmhead_block_norm_backward(x, r, w_pre, eps, dy, dh, workspace, out_dx, out_dr=None, out_dw_pre=None, w_post=None,
+                                     gate=None, gate_mode=CORAL_GATE_NONE, alpha=1.0, out_dw_post=None, out_dgate=None,
+                                     stream=None):
+    """Gradient of coral_lmhead_block_norm.  dy, dh: gradients of y and h (one may be None); out_dx, out_dr like x;
+    out_dw_pre, out_dw_post: fp32 [H]; out_dgate: fp32 [H] or [M], or like x for a full gate; workspace: CUDA uint8
+    tensor of coral_lmhead_block_norm_backward_bytes(M, H)."""
+    a, dev = _norm_args(x, r, w_pre, eps, w_post, gate, gate_mode, alpha)
+    M, H = x.shape
+    t, f = x.dtype, torch.float32
+    a.dy_dev = _op_ptr("dy", dy, t, (M, H), dev)
+    a.dh_dev = _op_ptr("dh", dh, t, (M, H), dev)
+    a.out_dx_dev = _op_ptr("out_dx", out_dx, t, (M, H), dev)
+    a.out_dr_dev = _op_ptr("out_dr", out_dr, t, (M, H), dev)
+    a.out_dw_pre_dev = _op_ptr("out_dw_pre", out_dw_pre, f, (H,), dev)
+    a.out_dw_post_dev = _op_ptr("out_dw_post", out_dw_post, f, (H,), dev)
+    full = int(gate_mode) == CORAL_GATE_FULL
+    a.out_dgate_dev = _op_ptr("out_dgate", out_dgate, t if full else f, None if gate is None else gate.shape, dev)
+    if workspace.numel() * workspace.element_size() < coral_lmhead_block_norm_backward_bytes(M, H):
+        raise ValueError("workspace is smaller than coral_lmhead_block_norm_backward_bytes(M, H)")
+    _check(load_library().coral_lmhead_block_norm_backward(
+        ctypes.byref(a), _op_ptr("workspace", workspace, torch.uint8, None, dev), _stream_ptr(stream)),
+        "coral_lmhead_block_norm_backward")
 
 
 def coral_lmhead_destroy(handle) -> None:
