@@ -442,6 +442,83 @@ int coral_lmhead_block_norm(const coral_lmhead_norm_args *args, void *stream);
 int coral_lmhead_block_norm_backward_bytes(int M, int H, size_t *bytes);
 int coral_lmhead_block_norm_backward(const coral_lmhead_norm_args *args, void *workspace_dev, void *stream);
 
+/*
+ * Products with 4-bit weights and group scales, for few rows: the dense head over the whole vocabulary (the logits that
+ * verify a draft; Section 1 has the target model verify in one pass) and the drafter's projections, which are bound by their
+ * weight bytes as the draft head is:
+ *   out[m][n] = sum_g scale[n][g] * sum_{k in group g} (q[n][k] - zero[n][g]) * x[m][k]
+ * The sum inside a group is over exact operands (an integer and an activation) with fp32 accumulation; the scale multiplies
+ * that fp32 sum; groups add up in fp32; one rounding to the output type.
+ *
+ * coral_lmhead_q4_config: N outputs, K inputs (a multiple of group, at most 65536), group 32, 64 or 128 columns,
+ *   scale_type CORAL_TYPE_BF16 or CORAL_TYPE_F16, has_zeros 0 (zero = 8 everywhere) or 1.
+ * coral_lmhead_q4_packed_bytes: size of the packed copy.
+ * coral_lmhead_q4_pack: Wq_dev [N x K/2] bytes, column 2j in the low and 2j + 1 in the high four bits of byte j, 16-byte
+ *   aligned; scales_dev [N x K/group]; zeros_dev [N x K/group] bytes, 0..127, or NULL.  Writes packed_dev (256-byte aligned,
+ *   owned by the caller; the inputs may be freed once the call has run on `stream`).
+ * coral_lmhead_q4_linear: x_dev [M x K] of x_type (bf16 or fp16), 16-byte aligned; out_dev [M x N] of out_type (fp32, bf16 or
+ *   fp16).  M >= 1; the weights are read once per pass over the rows.  A call holds nothing between calls, so any number may
+ *   run at once on one packed copy.
+ * Asynchronous on `stream`; no allocation.  CORAL_ERR_INVALID for a bad configuration, NULL or misaligned pointers, M < 1.
+ */
+typedef struct coral_lmhead_q4_config {
+    uint32_t struct_size;          /* sizeof(coral_lmhead_q4_config) */
+    int32_t N, K, group, scale_type, has_zeros;
+} coral_lmhead_q4_config;
+
+int coral_lmhead_q4_packed_bytes(const coral_lmhead_q4_config *cfg, size_t *bytes);
+int coral_lmhead_q4_pack(const coral_lmhead_q4_config *cfg, const void *Wq_dev, const void *scales_dev, const void *zeros_dev,
+                         void *packed_dev, void *stream);
+int coral_lmhead_q4_linear(const coral_lmhead_q4_config *cfg, const void *packed_dev, const void *x_dev, int x_type, int M,
+                           void *out_dev, int out_type, void *stream);
+
+/*
+ * Penalties for repeated tokens, biases and grammar masks on dense logits, with the candidates of the result in the same
+ * pass (what coral_lmhead_draft gives for the grouped head, for logits [M x V] that exist already: those of
+ * coral_lmhead_q4_linear or of the target model; out_ids / out_logprobs are what coral_tree_expand takes).  Rows may be tree
+ * nodes: row m belongs to sequence row_seq[m] and has, besides that sequence's tokens, the draft tokens on its own path.
+ * For token x, with n = its occurrences in the sequence's output and in the row's path, each step one fp32 operation:
+ *   l1 = x in prompt, output or path ? (l > 0 ? l / repetition : l * repetition) : l
+ *   l2 = n > 0 ? l1 - frequency * n - presence : l1          (the product rounded, then two subtractions from the left)
+ *   l3 = x in the bias list ? l2 + bias : l2                  (of several entries for one token the last one counts)
+ *   out = allowed by the row's mask ? l3 : -inf
+ * ids: the k_tokens largest out (descending, equal -> lower id), logprobs: out - lse, lse: log-sum-exp of the row's out, all
+ * of the fp32 values.  A value of -inf or NaN is no candidate; candidates that do not exist have id 0x7fffffff and
+ * log-probability -inf.  A row that allows nothing has lse -inf; a row with an allowed NaN or +inf has lse NaN.
+ *
+ * logits_dev [M rows of V, ld_logits apart] of `type`.  Optional parts (NULL = absent):
+ *   row_seq [M]: sequence of a row, negative or >= n_seq: a row without lists and penalties.  NULL: row m is sequence m
+ *     (n_seq >= M; n_seq = 0: no sequence at all).
+ *   prompt_tokens, output_tokens (int32) with offsets (int64 [n_seq + 1], in elements) and the number of list elements in
+ *     *_total: offsets are clamped to it.  Tokens outside [0, V) are passed over, so a list may be padded with -1.
+ *   path_tokens [M x path_len] int32, entries outside [0, V) passed over.
+ *   repetition (> 0), frequency, presence: fp32 [n_seq].
+ *   bias_tokens, bias_values, bias_offsets, bias_total: lists like the prompt's, with one fp32 value an entry.
+ *   mask_words: int32 words [n_masks x ceil(V / 32)], bit x % 32 of word x / 32 allows token x; mask_rows [M]: mask of a row,
+ *     negative: everything is allowed, >= n_masks: nothing is.  NULL: row m has mask m.
+ *   out_logits [M rows of V, ld_out apart] of `type`, rounded once; may be the logits themselves (same row distance; no other
+ *     overlap).  Columns from V on are not touched.
+ *   out_ids, out_logprobs [M x k_tokens], k_tokens 0..32 (0: both NULL); out_lse [M].  At least one output is needed.
+ * Values of a masked token, NaN and infinities too, have no influence.  Asynchronous on `stream`, one launch, no scratch
+ * memory, no atomics on floats: the same call gives the same bits.
+ */
+typedef struct coral_lmhead_logits_args {
+    uint32_t struct_size;          /* sizeof(coral_lmhead_logits_args) */
+    int32_t type, M, V, n_seq, path_len, n_masks, k_tokens;
+    int64_t ld_logits, ld_out, prompt_total, output_total, bias_total;
+    const void *logits_dev;
+    void *out_logits_dev;
+    const int32_t *row_seq_dev, *prompt_tokens_dev, *output_tokens_dev, *path_tokens_dev, *bias_tokens_dev;
+    const int64_t *prompt_offsets_dev, *output_offsets_dev, *bias_offsets_dev;
+    const float *repetition_dev, *frequency_dev, *presence_dev, *bias_values_dev;
+    const uint32_t *mask_words_dev;
+    const int32_t *mask_rows_dev;
+    int32_t *out_ids_dev;
+    float *out_logprobs_dev, *out_lse_dev;
+} coral_lmhead_logits_args;
+
+int coral_lmhead_logits_process(const coral_lmhead_logits_args *args, void *stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char *coral_lmhead_error_string(int code);
 

@@ -5,6 +5,8 @@
 
 #include "block_norm.cuh"
 #include "launch.cuh"
+#include "logits.cuh"
+#include "q4.cuh"
 
 using namespace coral;
 
@@ -114,9 +116,223 @@ int launch_norm_type(int type, const NormArgs& k, const NormPlan& p, bool backwa
     return launch_norm_nv<float>(k, p, backward, st);
 }
 
+// ---- products with 4-bit weights -----------------------------------------------------------------------------
+constexpr int kQ4MaxK = 65536;
+constexpr size_t kQ4MaxSmem = 227 * 1024;
+
+bool q4_config_ok(const coral_lmhead_q4_config* c) {
+    if (!c || c->struct_size != sizeof(*c)) return false;
+    if (c->group != 32 && c->group != 64 && c->group != 128) return false;
+    if (c->N < 1 || c->K < c->group || c->K > kQ4MaxK || c->K % c->group != 0) return false;
+    if (c->scale_type != CORAL_TYPE_BF16 && c->scale_type != CORAL_TYPE_F16) return false;
+    return c->has_zeros == 0 || c->has_zeros == 1;
+}
+
+struct Q4Layout {
+    int KB, T;
+    size_t weights, scales;                      // bytes of the two parts; the scales follow the weights
+};
+
+Q4Layout q4_layout(const coral_lmhead_q4_config& c) {
+    Q4Layout L;
+    L.KB = (c.K + 127) / 128;
+    L.T = (c.N - 1) / 16 + 1;
+    const size_t blocks = (size_t)L.T * L.KB;
+    L.weights = blocks * 1024;
+    L.scales = blocks * 16 * (128 / c.group) * (c.has_zeros ? 4 : 2);
+    return L;
+}
+
+// How many warps share a tile's columns: the split whose busiest warp has the fewest column blocks to read (ties: the
+// smaller split, which joins fewer parts).
+int q4_split(int T, int KB, int sms) {
+    int best = 1;
+    long long best_cost = -1;
+    for (int s = 1; s <= kQ4Warps; s *= 2) {
+        const long long teams = (long long)sms * (kQ4Warps / s);
+        const long long cost = ((T + teams - 1) / teams) * ((KB + s - 1) / s);
+        if (best_cost < 0 || cost < best_cost) { best = s; best_cost = cost; }
+    }
+    return best;
+}
+
+template <typename TX, int NT, int PER, bool ZEROS>
+int launch_q4(const Q4View& q, const void* x, int M, void* out, int out_type, int sms, cudaStream_t st) {
+    const int split = q4_split(q.T, q.KB, sms);
+    const long long units = (long long)q.T * split;              // warps that have a tile to work on
+    int warps = kQ4Warps;
+    while (warps > split && warps > 4 && units < (long long)sms * warps) warps /= 2;
+    const long long teams = warps / split;
+    const long long blocks = (q.T + teams - 1) / teams;
+    const size_t smem = (size_t)M * (q.KB * 256 + 64) + (size_t)2 * warps * 16 * 8 * NT * sizeof(float);
+    auto kernel = q4_rows_kernel<TX, NT, PER, ZEROS>;
+    if (!allow_smem(kernel, smem)) return CORAL_ERR_CUDA;
+    kernel<<<(int)(blocks < sms ? blocks : sms), warps * 32, smem, st>>>(q, static_cast<const TX*>(x), M, out, out_type, split);
+    return cudaGetLastError() == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+}
+
+template <typename TX, int NT, int PER>
+int launch_q4_zeros(const Q4View& q, bool zeros, const void* x, int M, void* out, int out_type, int sms, cudaStream_t st) {
+    return zeros ? launch_q4<TX, NT, PER, true>(q, x, M, out, out_type, sms, st)
+                 : launch_q4<TX, NT, PER, false>(q, x, M, out, out_type, sms, st);
+}
+
+template <typename TX, int NT>
+int launch_q4_group(const Q4View& q, int group, bool zeros, const void* x, int M, void* out, int out_type, int sms, cudaStream_t st) {
+    if (group == 128) return launch_q4_zeros<TX, NT, 1>(q, zeros, x, M, out, out_type, sms, st);
+    if (group == 64) return launch_q4_zeros<TX, NT, 2>(q, zeros, x, M, out, out_type, sms, st);
+    return launch_q4_zeros<TX, NT, 4>(q, zeros, x, M, out, out_type, sms, st);
+}
+
+template <typename TX>
+int launch_q4_rows(const Q4View& q, int group, bool zeros, const void* x, int M, void* out, int out_type, int sms, cudaStream_t st) {
+    return M <= 8 ? launch_q4_group<TX, 1>(q, group, zeros, x, M, out, out_type, sms, st)
+                  : launch_q4_group<TX, 2>(q, group, zeros, x, M, out, out_type, sms, st);
+}
+
+// ---- logits ----------------------------------------------------------------------------------------------------
+constexpr int kLogitsMaxV = 1 << 30;
+constexpr int kLogitsFewRows = 8;                // up to here a row takes the largest cluster: latency counts, SMs are free
+
+bool logits_args_ok(const coral_lmhead_logits_args* a) {
+    if (!a || a->struct_size != sizeof(*a)) return false;
+    if (a->type != CORAL_TYPE_F32 && a->type != CORAL_TYPE_BF16 && a->type != CORAL_TYPE_F16) return false;
+    if (!a->logits_dev || a->M < 1 || a->V < 1 || a->V > kLogitsMaxV || a->n_seq < 0) return false;
+    if (a->ld_logits < a->V || (a->out_logits_dev && a->ld_out < a->V)) return false;
+    if (a->out_logits_dev == a->logits_dev && a->ld_out != a->ld_logits) return false;
+    if (!a->row_seq_dev && a->n_seq != 0 && a->n_seq < a->M) return false;     // row m is sequence m
+    if (a->k_tokens < 0 || a->k_tokens > CORAL_MAX_K_TOKENS || a->k_tokens > a->V) return false;
+    if (a->k_tokens > 0 ? !a->out_ids_dev || !a->out_logprobs_dev : a->out_ids_dev || a->out_logprobs_dev) return false;
+    if (!a->out_logits_dev && !a->out_lse_dev && a->k_tokens == 0) return false;
+    if ((a->prompt_tokens_dev != nullptr) != (a->prompt_offsets_dev != nullptr) || a->prompt_total < 0 || a->prompt_total > 0x7fffffff) return false;
+    if ((a->output_tokens_dev != nullptr) != (a->output_offsets_dev != nullptr) || a->output_total < 0 || a->output_total > 0x7fffffff) return false;
+    if ((a->bias_tokens_dev != nullptr) != (a->bias_offsets_dev != nullptr) ||
+        (a->bias_tokens_dev != nullptr) != (a->bias_values_dev != nullptr) || a->bias_total < 0 || a->bias_total > 0x7fffffff)
+        return false;
+    if (a->path_len < 0 || (a->path_tokens_dev != nullptr) != (a->path_len > 0)) return false;
+    if (a->mask_words_dev ? a->n_masks < 1 : a->mask_rows_dev != nullptr) return false;
+    if (a->mask_words_dev && !a->mask_rows_dev && a->n_masks < a->M) return false;
+    const size_t e = elem_size(a->type);
+    if (!aligned(a->logits_dev, e) || !aligned(a->out_logits_dev, e)) return false;
+    for (const void* p : {(const void*)a->row_seq_dev, (const void*)a->prompt_tokens_dev, (const void*)a->output_tokens_dev,
+                          (const void*)a->path_tokens_dev, (const void*)a->bias_tokens_dev, (const void*)a->bias_values_dev,
+                          (const void*)a->repetition_dev, (const void*)a->frequency_dev, (const void*)a->presence_dev,
+                          (const void*)a->mask_words_dev, (const void*)a->mask_rows_dev, (const void*)a->out_ids_dev,
+                          (const void*)a->out_logprobs_dev, (const void*)a->out_lse_dev})
+        if (!aligned(p, 4)) return false;
+    return aligned(a->prompt_offsets_dev, 8) && aligned(a->output_offsets_dev, 8) && aligned(a->bias_offsets_dev, 8);
+}
+
+template <typename T>
+int launch_logits(const LogitsArgs& k, cudaStream_t st) {
+    const size_t smem = (size_t)kLogitsChunk * 4 * ((k.prompt || k.output || k.path ? 1 : 0) + (k.bias_tokens ? 1 : 0));
+    const int most = k.M <= kLogitsFewRows ? kLogitsMaxCluster : kLogitsMaxCluster / 2;
+    const int chunks = (k.V - 1) / kLogitsChunk + 1;
+    int C = 1;
+    while (C < chunks && C < most) C *= 2;
+    auto kernel = logits_kernel<T>;
+    if (!allow_smem(kernel, smem)) return CORAL_ERR_CUDA;
+    if (C > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return CORAL_ERR_CUDA;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)k.M * C);
+    cfg.blockDim = dim3(kLogitsThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = C;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, k, C) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+}
+
 }  // namespace
 
 extern "C" {
+
+int coral_lmhead_logits_process(const coral_lmhead_logits_args* a, void* stream) {
+    if (!logits_args_ok(a)) return CORAL_ERR_INVALID;
+    if (a->M > 0x7fffffff / kLogitsMaxCluster) return CORAL_ERR_TOO_LARGE;
+    LogitsArgs k{};
+    k.logits = a->logits_dev; k.out = a->out_logits_dev;
+    k.ld_in = a->ld_logits; k.ld_out = a->ld_out;
+    k.M = a->M; k.V = a->V; k.n_seq = a->n_seq; k.path_len = a->path_len; k.n_masks = a->n_masks;
+    k.mask_words = (a->V + 31) / 32; k.k = a->k_tokens;
+    k.row_seq = a->row_seq_dev;
+    // lists and penalties belong to sequences; without a penalty the token lists change nothing
+    if (a->n_seq > 0 && (a->repetition_dev || a->frequency_dev || a->presence_dev)) {
+        k.prompt = a->prompt_tokens_dev; k.prompt_off = reinterpret_cast<const long long*>(a->prompt_offsets_dev); k.prompt_total = a->prompt_total;
+        k.output = a->output_tokens_dev; k.output_off = reinterpret_cast<const long long*>(a->output_offsets_dev); k.output_total = a->output_total;
+        k.path = a->path_tokens_dev;
+        k.rep = a->repetition_dev; k.freq = a->frequency_dev; k.pres = a->presence_dev;
+    }
+    if (a->n_seq > 0) {
+        k.bias_tokens = a->bias_tokens_dev; k.bias_off = reinterpret_cast<const long long*>(a->bias_offsets_dev); k.bias_total = a->bias_total;
+        k.bias_values = a->bias_values_dev;
+    }
+    k.mask = a->mask_words_dev; k.mask_rows = a->mask_rows_dev;
+    k.out_ids = a->out_ids_dev; k.out_logprobs = a->out_logprobs_dev; k.out_lse = a->out_lse_dev;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (a->type == CORAL_TYPE_BF16) return launch_logits<__nv_bfloat16>(k, st);
+    if (a->type == CORAL_TYPE_F16) return launch_logits<__half>(k, st);
+    return launch_logits<float>(k, st);
+}
+
+int coral_lmhead_q4_packed_bytes(const coral_lmhead_q4_config* cfg, size_t* bytes) {
+    if (!q4_config_ok(cfg) || !bytes) return CORAL_ERR_INVALID;
+    const Q4Layout L = q4_layout(*cfg);
+    *bytes = L.weights + L.scales;
+    return CORAL_OK;
+}
+
+int coral_lmhead_q4_pack(const coral_lmhead_q4_config* cfg, const void* Wq_dev, const void* scales_dev, const void* zeros_dev,
+                         void* packed_dev, void* stream) {
+    if (!q4_config_ok(cfg) || !Wq_dev || !scales_dev || !packed_dev || (zeros_dev != nullptr) != (cfg->has_zeros != 0))
+        return CORAL_ERR_INVALID;
+    if (!aligned(Wq_dev, 16) || !aligned(scales_dev, 2) || !aligned(packed_dev, 256)) return CORAL_ERR_INVALID;
+    const Q4Layout L = q4_layout(*cfg);
+    const size_t pieces = L.weights / 16;
+    const size_t blocks = (pieces + 255) / 256;
+    if (blocks > 0x7fffffffu) return CORAL_ERR_TOO_LARGE;
+    q4_pack_kernel<<<(unsigned)blocks, 256, 0, static_cast<cudaStream_t>(stream)>>>(
+        static_cast<const unsigned char*>(Wq_dev), static_cast<const uint16_t*>(scales_dev),
+        static_cast<const unsigned char*>(zeros_dev), cfg->N, cfg->K, L.KB, cfg->group, static_cast<uint4*>(packed_dev),
+        static_cast<unsigned char*>(packed_dev) + L.weights, pieces);
+    return cudaGetLastError() == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+}
+
+int coral_lmhead_q4_linear(const coral_lmhead_q4_config* cfg, const void* packed_dev, const void* x_dev, int x_type, int M,
+                           void* out_dev, int out_type, void* stream) {
+    if (!q4_config_ok(cfg) || !packed_dev || !x_dev || !out_dev || M < 1) return CORAL_ERR_INVALID;
+    if (x_type != CORAL_TYPE_BF16 && x_type != CORAL_TYPE_F16) return CORAL_ERR_INVALID;
+    if (out_type != CORAL_TYPE_F32 && out_type != CORAL_TYPE_BF16 && out_type != CORAL_TYPE_F16) return CORAL_ERR_INVALID;
+    if (!aligned(packed_dev, 256) || !aligned(x_dev, 16) || !aligned(out_dev, elem_size(out_type))) return CORAL_ERR_INVALID;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int sms = 0;
+    if (!device_sms(&sms)) return CORAL_ERR_CUDA;
+    const Q4Layout L = q4_layout(*cfg);
+    Q4View q{};
+    q.w = static_cast<const uint4*>(packed_dev);
+    q.sz = static_cast<const unsigned char*>(packed_dev) + L.weights;
+    q.N = cfg->N; q.K = cfg->K; q.KB = L.KB; q.T = L.T;
+    q.scale_half = cfg->scale_type == CORAL_TYPE_F16;
+    // rows of x that fit shared memory beside the two buffers of partial sums
+    const size_t fixed = (size_t)2 * kQ4Warps * 16 * kQ4PassRows * sizeof(float);
+    int rows = (int)((kQ4MaxSmem - fixed) / (L.KB * 256 + 64));
+    rows = rows > kQ4PassRows ? kQ4PassRows : rows;
+    for (int m = 0; m < M; m += rows) {
+        const int n = M - m < rows ? M - m : rows;
+        const void* x = static_cast<const unsigned char*>(x_dev) + (size_t)m * cfg->K * 2;
+        void* o = static_cast<unsigned char*>(out_dev) + (size_t)m * cfg->N * elem_size(out_type);
+        const int rc = x_type == CORAL_TYPE_BF16
+                           ? launch_q4_rows<__nv_bfloat16>(q, cfg->group, cfg->has_zeros != 0, x, n, o, out_type, sms, st)
+                           : launch_q4_rows<__half>(q, cfg->group, cfg->has_zeros != 0, x, n, o, out_type, sms, st);
+        if (rc != CORAL_OK) return rc;
+    }
+    return CORAL_OK;
+}
 
 int coral_lmhead_block_norm(const coral_lmhead_norm_args* a, void* stream) {
     if (!norm_args_ok(a) || (!a->out_y_dev && !a->out_h_dev)) return CORAL_ERR_INVALID;

@@ -54,6 +54,22 @@ class coral_lmhead_norm_args(ctypes.Structure):
                                        "out_dw_post_dev")]
 
 
+class coral_lmhead_q4_config(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("N", ctypes.c_int32), ("K", ctypes.c_int32), ("group", ctypes.c_int32),
+                ("scale_type", ctypes.c_int32), ("has_zeros", ctypes.c_int32)]
+
+
+class coral_lmhead_logits_args(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [
+        (n, ctypes.c_int32) for n in ("type", "M", "V", "n_seq", "path_len", "n_masks", "k_tokens")] + [
+        (n, ctypes.c_int64) for n in ("ld_logits", "ld_out", "prompt_total", "output_total", "bias_total")] + [
+        (n, ctypes.c_void_p) for n in (
+            "logits_dev", "out_logits_dev", "row_seq_dev", "prompt_tokens_dev", "output_tokens_dev", "path_tokens_dev",
+            "bias_tokens_dev", "prompt_offsets_dev", "output_offsets_dev", "bias_offsets_dev", "repetition_dev",
+            "frequency_dev", "presence_dev", "bias_values_dev", "mask_words_dev", "mask_rows_dev", "out_ids_dev",
+            "out_logprobs_dev", "out_lse_dev")]
+
+
 _lib = None
 _vp, _i = ctypes.c_void_p, ctypes.c_int
 
@@ -88,6 +104,10 @@ _SIGNATURES = {
     "coral_lmhead_block_norm": (_i, [ctypes.POINTER(coral_lmhead_norm_args), _vp]),
     "coral_lmhead_block_norm_backward_bytes": (_i, [_i, _i, ctypes.POINTER(ctypes.c_size_t)]),
     "coral_lmhead_block_norm_backward": (_i, [ctypes.POINTER(coral_lmhead_norm_args), _vp, _vp]),
+    "coral_lmhead_q4_packed_bytes": (_i, [ctypes.POINTER(coral_lmhead_q4_config), ctypes.POINTER(ctypes.c_size_t)]),
+    "coral_lmhead_q4_pack": (_i, [ctypes.POINTER(coral_lmhead_q4_config), _vp, _vp, _vp, _vp, _vp]),
+    "coral_lmhead_q4_linear": (_i, [ctypes.POINTER(coral_lmhead_q4_config), _vp, _vp, _i, _i, _vp, _i, _vp]),
+    "coral_lmhead_logits_process": (_i, [ctypes.POINTER(coral_lmhead_logits_args), _vp]),
     "coral_lmhead_error_string": (ctypes.c_char_p, [_i]),
     "coral_lmhead_destroy": (_i, [_vp]),
 }
@@ -444,6 +464,107 @@ def coral_lmhead_block_norm_backward(x, r, w_pre, eps, dy, dh, workspace, out_dx
         "coral_lmhead_block_norm_backward")
 
 
+def make_q4_config(N, K, group, scale_dtype, has_zeros) -> coral_lmhead_q4_config:
+    return coral_lmhead_q4_config(ctypes.sizeof(coral_lmhead_q4_config), int(N), int(K), int(group), _TYPES[scale_dtype],
+                                  int(bool(has_zeros)))
+
+
+def coral_lmhead_q4_packed_bytes(cfg: coral_lmhead_q4_config) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load_library().coral_lmhead_q4_packed_bytes(ctypes.byref(cfg), ctypes.byref(b)), "coral_lmhead_q4_packed_bytes")
+    return int(b.value)
+
+
+def coral_lmhead_q4_pack(cfg, Wq, scales, zeros, packed, stream=None) -> None:
+    """Wq: CUDA uint8 [N, K / 2], low four bits first; scales: bf16 or fp16 [N, K / group]; zeros: uint8 like scales, or
+    None (8 everywhere); packed: CUDA uint8 tensor of coral_lmhead_q4_packed_bytes(cfg)."""
+    dev = _op_device(Wq, "Wq")
+    g = (cfg.N, cfg.K // cfg.group)
+    sdt = torch.bfloat16 if cfg.scale_type == CORAL_TYPE_BF16 else torch.float16
+    if packed.numel() < coral_lmhead_q4_packed_bytes(cfg):
+        raise ValueError("packed is smaller than coral_lmhead_q4_packed_bytes(cfg)")
+    _check(load_library().coral_lmhead_q4_pack(
+        ctypes.byref(cfg), _op_ptr("Wq", Wq, torch.uint8, (cfg.N, cfg.K // 2), dev), _op_ptr("scales", scales, sdt, g, dev),
+        _op_ptr("zeros", zeros, torch.uint8, g, dev), _op_ptr("packed", packed, torch.uint8, None, dev), _stream_ptr(stream)),
+        "coral_lmhead_q4_pack")
+
+
+def coral_lmhead_q4_linear(cfg, packed, x, out, stream=None) -> None:
+    """out [M, N] (fp32, bf16 or fp16) = x [M, K] (bf16 or fp16) times the packed weights' transpose."""
+    dev = _op_device(x, "x")
+    M = x.shape[0]
+    _check(load_library().coral_lmhead_q4_linear(
+        ctypes.byref(cfg), _op_ptr("packed", packed, torch.uint8, None, dev), _op_ptr("x", x, x.dtype, (M, cfg.K), dev),
+        _type_of(x), M, _op_ptr("out", out, out.dtype, (M, cfg.N), dev), _type_of(out), _stream_ptr(stream)),
+        "coral_lmhead_q4_linear")
+
+
+def _rows_ptr(name, t, dtype, shape, device):
+    """Pointer and row distance of a matrix whose rows may lie apart (a slice of padded rows)."""
+    if t is None:
+        return None, 0
+    M, V = shape
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if t.dtype != dtype or tuple(t.shape) != (M, V):
+        raise ValueError(f"{name}: expected {dtype} {(M, V)}, got {t.dtype} {tuple(t.shape)}")
+    ld = t.stride(0) if M > 1 else V
+    if (V > 1 and t.stride(1) != 1) or ld < V:
+        raise ValueError(f"{name}: the elements of a row must be contiguous and rows must not overlap")
+    return t.data_ptr(), ld
+
+
+def coral_lmhead_logits_process(logits, *, row_seq=None, prompt_tokens=None, prompt_offsets=None, output_tokens=None,
+                                output_offsets=None, path_tokens=None, repetition=None, frequency=None, presence=None,
+                                bias_tokens=None, bias_values=None, bias_offsets=None, mask_words=None, mask_rows=None,
+                                out_logits=None, out_ids=None, out_logprobs=None, out_lse=None, stream=None) -> None:
+    """Penalties, biases and masks on logits [M, V] (rows may lie apart), and the candidates of the result.  Lists are flat
+    int32 with int64 offsets [n_seq + 1]; path_tokens int32 [M, path_len]; repetition, frequency, presence fp32 [n_seq];
+    mask_words int32 [n_masks, ceil(V / 32)]; out_ids int32 and out_logprobs fp32 [M, k_tokens]; out_lse fp32 [M]."""
+    dev = _op_device(logits, "logits")
+    if logits.dim() != 2:
+        raise ValueError("logits must be [M, V]")
+    M, V = logits.shape
+    i32, i64, f32 = torch.int32, torch.int64, torch.float32
+    n_seq = None
+    for t, more in ((repetition, 0), (frequency, 0), (presence, 0), (prompt_offsets, 1), (output_offsets, 1), (bias_offsets, 1)):
+        if t is not None:
+            n = t.numel() - more
+            if n_seq is not None and n != n_seq:
+                raise ValueError("the sequences' lists and penalties differ in number")
+            n_seq = n
+    n_seq = n_seq or 0                               # no lists and no penalties: no sequences
+    path_len = path_tokens.shape[1] if path_tokens is not None else 0
+    n_masks = mask_words.shape[0] if mask_words is not None else 0
+    k = out_ids.shape[1] if out_ids is not None else 0
+    a = coral_lmhead_logits_args(
+        struct_size=ctypes.sizeof(coral_lmhead_logits_args), type=_type_of(logits), M=M, V=V, n_seq=n_seq, path_len=path_len,
+        n_masks=n_masks, k_tokens=k, row_seq_dev=_op_ptr("row_seq", row_seq, i32, (M,), dev),
+        path_tokens_dev=_op_ptr("path_tokens", path_tokens, i32, (M, path_len), dev) if path_len else None,
+        repetition_dev=_op_ptr("repetition", repetition, f32, (n_seq,), dev),
+        frequency_dev=_op_ptr("frequency", frequency, f32, (n_seq,), dev),
+        presence_dev=_op_ptr("presence", presence, f32, (n_seq,), dev),
+        mask_words_dev=_op_ptr("mask_words", mask_words, i32, (n_masks, (V + 31) // 32), dev),
+        mask_rows_dev=_op_ptr("mask_rows", mask_rows, i32, (M,), dev), out_ids_dev=_op_ptr("out_ids", out_ids, i32, (M, k), dev),
+        out_logprobs_dev=_op_ptr("out_logprobs", out_logprobs, f32, (M, k), dev), out_lse_dev=_op_ptr("out_lse", out_lse, f32, (M,), dev))
+    a.logits_dev, a.ld_logits = _rows_ptr("logits", logits, logits.dtype, (M, V), dev)
+    a.out_logits_dev, a.ld_out = _rows_ptr("out_logits", out_logits, logits.dtype, (M, V), dev)
+    for name, tokens, offsets in (("prompt", prompt_tokens, prompt_offsets), ("output", output_tokens, output_offsets),
+                                  ("bias", bias_tokens, bias_offsets)):
+        if tokens is None and offsets is None:
+            continue
+        if tokens is None or offsets is None:
+            raise ValueError(f"{name}_tokens and {name}_offsets go together")
+        if tokens.numel() == 0:                      # every list is empty
+            continue
+        setattr(a, f"{name}_tokens_dev", _op_ptr(f"{name}_tokens", tokens, i32, (tokens.numel(),), dev))
+        setattr(a, f"{name}_offsets_dev", _op_ptr(f"{name}_offsets", offsets, i64, (n_seq + 1,), dev))
+        setattr(a, f"{name}_total", tokens.numel())
+        if name == "bias":
+            a.bias_values_dev = _op_ptr("bias_values", bias_values, f32, (tokens.numel(),), dev)
+    _check(load_library().coral_lmhead_logits_process(ctypes.byref(a), _stream_ptr(stream)), "coral_lmhead_logits_process")
+
+
 def coral_lmhead_destroy(handle) -> None:
     _check(load_library().coral_lmhead_destroy(handle), "coral_lmhead_destroy")
 
@@ -503,3 +624,24 @@ class LMHead:
             self.close()
         except Exception:
             pass
+
+
+class Q4Linear:
+    """Owns the packed copy of one 4-bit weight matrix: Wq uint8 [N, K / 2], scales [N, K / group] (bf16 or fp16), zeros
+    uint8 like scales or None.  The inputs may be freed after construction."""
+
+    def __init__(self, Wq, scales, zeros=None):
+        N, K = Wq.shape[0], 2 * Wq.shape[1]
+        if scales.dim() != 2 or scales.shape[1] < 1 or K % scales.shape[1]:
+            raise ValueError("scales must be [N, K / group]")
+        if scales.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("scales must be bfloat16 or float16")
+        self.cfg = make_q4_config(N, K, K // scales.shape[1], scales.dtype, zeros is not None)
+        self.packed = torch.empty(coral_lmhead_q4_packed_bytes(self.cfg), dtype=torch.uint8, device=Wq.device)
+        coral_lmhead_q4_pack(self.cfg, Wq, scales, zeros, self.packed)
+
+    def forward(self, x, out=None, out_dtype=torch.float32, stream=None):
+        if out is None:
+            out = torch.empty((x.shape[0], self.cfg.N), dtype=out_dtype, device=x.device)
+        coral_lmhead_q4_linear(self.cfg, self.packed, x, out, stream)
+        return out

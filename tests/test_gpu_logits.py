@@ -1,0 +1,264 @@
+"""GPU parity of the logits step.  Processed logits and candidate ids are the oracle's float32 steps bit for bit.
+
+Tolerance of the log-sum-exp.  u = 2^-24.  A thread adds 16 exponentials a chunk, a warp 5, a block 16 and a cluster 16 partial
+sums, each rescaled once; an exponential is off by 2 ulp and its argument, at most 40 where it still counts, by one rounding:
+the sum is off by at most (16 * passes + 37 + 6 + 40) u relative, which is what the logarithm is off by absolutely; adding the
+maximum and subtracting from a logit round once each.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators_oracle as oor
+from paper_2502_16880_b200 import lmhead
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def _csr(lists, dtype=torch.int32):
+    off = torch.tensor(np.concatenate([[0], np.cumsum([len(x) for x in lists])]), dtype=torch.int64)
+    flat = torch.tensor([t for x in lists for t in x], dtype=dtype)
+    return flat, off
+
+
+def _cuda(t):
+    return None if t is None else t.cuda()
+
+
+def _run(logits, k, write=True, n_seq=0, row_seq=None, prompt=None, output=None, path=None, rep=None, freq=None, pres=None, bias=None,
+         mask=None, mask_rows=None, logits_dev=None, out=None, stream=None):
+    """logits: CPU tensor; lists: python lists per sequence; bias: lists of (token, value).  Returns numpy results."""
+    M, V = logits.shape
+    kw = {}
+    if prompt is not None:
+        kw["prompt_tokens"], kw["prompt_offsets"] = map(_cuda, _csr(prompt))
+    if output is not None:
+        kw["output_tokens"], kw["output_offsets"] = map(_cuda, _csr(output))
+    if bias is not None:
+        kw["bias_tokens"], kw["bias_offsets"] = map(_cuda, _csr([[t for t, _ in b] for b in bias]))
+        kw["bias_values"] = torch.tensor([v for b in bias for _, v in b], dtype=torch.float32).cuda()
+    f = lambda v: None if v is None else torch.tensor(v, dtype=torch.float32).cuda()
+    x = logits.cuda() if logits_dev is None else logits_dev
+    out = torch.empty(M, V, dtype=logits.dtype, device="cuda") if write and out is None else out
+    ids = torch.empty(M, k, dtype=torch.int32, device="cuda") if k else None
+    lps = torch.empty(M, k, dtype=torch.float32, device="cuda") if k else None
+    lse = torch.empty(M, dtype=torch.float32, device="cuda")
+    kw.update(row_seq=_cuda(row_seq), path_tokens=_cuda(path), repetition=f(rep), frequency=f(freq), presence=f(pres),
+              mask_words=_cuda(mask), mask_rows=_cuda(mask_rows), out_logits=out, out_ids=ids, out_logprobs=lps, out_lse=lse)
+    lmhead.coral_lmhead_logits_process(x, stream=stream, **kw)
+    torch.cuda.synchronize()
+    return dict(out=out, ids=None if ids is None else ids.cpu().numpy(), lps=None if lps is None else lps.cpu().numpy(), lse=lse.cpu().numpy())
+
+
+def _check(got, logits, k, rows=None, n_seq=0, row_seq=None, prompt=None, output=None, path=None, rep=None, freq=None, pres=None,
+           bias=None, mask=None, mask_rows=None):
+    M, V = logits.shape
+    for m in range(M) if rows is None else rows:
+        s = m if row_seq is None else int(row_seq[m])
+        known = 0 <= s < n_seq
+        of = lambda a, d: a[s] if a is not None and known else d
+        mr = (m if mask_rows is None else int(mask_rows[m])) if mask is not None else -1
+        nothing = mask is not None and mr >= mask.shape[0]
+        v, ids, lps, lse = oor.logits_row(
+            logits[m].float().numpy(), V, k, of(prompt, ()), of(output, ()), path[m].tolist() if path is not None and known else (),
+            of(rep, None), of(freq, None), of(pres, None), of(bias, ()), mask[mr].numpy() if mr >= 0 and not nothing else None, nothing)
+        if got["out"] is not None:
+            want = torch.from_numpy(v).to(logits.dtype)
+            assert torch.equal(torch.nan_to_num(got["out"][m].cpu(), nan=123.0), torch.nan_to_num(want, nan=123.0)), m
+        tol = (16 * (V // 8192 // 8 + 1) + 83) * U
+        if np.isfinite(lse):
+            assert abs(got["lse"][m] - lse) <= tol + U * abs(lse), (m, got["lse"][m], lse)
+        else:
+            assert np.array_equal(got["lse"][m], np.float32(lse), equal_nan=True), m
+        if k:
+            assert np.array_equal(got["ids"][m], ids), (m, got["ids"][m], ids)
+            a, b = got["lps"][m], lps
+            fin = np.isfinite(b)
+            assert np.array_equal(np.isnan(a), np.isnan(b)) and np.all(a[np.isneginf(b)] == -np.inf)
+            assert np.all(np.abs(a[fin] - b[fin]) <= tol + U * (abs(lse) + np.abs(b[fin])))
+
+
+def _random(seed, M, V, t, n_seq, plen, olen, path_len, n_bias, std=2.5):
+    rng = np.random.default_rng(seed)
+    g = torch.Generator().manual_seed(seed)
+    logits = (torch.randn(M, V, generator=g) * std).to(t)
+    tok = lambda n: (rng.random(n) ** 3 * V).astype(int).tolist()
+    d = dict(n_seq=n_seq, row_seq=torch.tensor(rng.integers(0, n_seq, M), dtype=torch.int32),
+             prompt=[tok(max(0, plen - 5 * s)) for s in range(n_seq)], output=[tok(max(0, olen - 3 * s)) for s in range(n_seq)],
+             rep=(1 + rng.random(n_seq)).astype(np.float32).tolist(), freq=rng.random(n_seq).astype(np.float32).tolist(),
+             pres=rng.random(n_seq).astype(np.float32).tolist())
+    if path_len:
+        d["path"] = torch.tensor(rng.integers(-V, V, (M, path_len)), dtype=torch.int32)
+    if n_bias:
+        d["bias"] = [[(t, float(np.float32(b))) for t, b in zip(tok(n_bias), rng.normal(size=n_bias) * 3)] for _ in range(n_seq)]
+    W = (V + 31) // 32
+    d["mask"] = torch.tensor(rng.integers(-2 ** 31, 2 ** 31, (M, W)), dtype=torch.int32)
+    d["mask_rows"] = torch.tensor(rng.integers(-1, M, M), dtype=torch.int32)
+    return logits, d
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("M,V,k", [(1, 1, 1), (3, 31, 5), (2, 1000, 10), (5, 4001, 32), (9, 8192, 10), (4, 8193, 7), (10, 32000, 10),
+                                   (3, 70001, 32), (2, 152064, 10), (12, 140003, 1)])
+def test_random_rows(M, V, k, t):
+    logits, d = _random(M * 1000 + V, M, V, t, 3, 300, 200, 4, 40)
+    _check(_run(logits, k, **d), logits, k, **d)
+    plain = {}
+    _check(_run(logits, k, **plain), logits, k, **plain)                     # nothing to apply: log-softmax and candidates
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_parts_alone(t):
+    logits, d = _random(5, 6, 9001, t, 2, 100, 50, 3, 20)
+    seqs = dict(n_seq=2, row_seq=d["row_seq"])
+    for names in (["prompt", "rep"], ["output", "freq"], ["output", "pres"], ["path", "freq", "pres"], ["path", "rep"], ["bias"]):
+        kw = dict(seqs, **{n: d[n] for n in names})
+        _check(_run(logits, 10, **kw), logits, 10, **kw)
+    kw = dict(mask=d["mask"], mask_rows=d["mask_rows"])
+    _check(_run(logits, 10, **kw), logits, 10, **kw)
+    kw = dict(mask=d["mask"])
+    _check(_run(logits, 10, **kw), logits, 10, **kw)
+    _check(_run(logits, 0, **kw), logits, 0, **kw)                           # no candidates wanted
+    got = _run(logits, 10, write=False, **kw)                                # ... or no logits
+    _check(got, logits, 10, **kw)
+
+
+def test_rows_without_sequence_or_mask():
+    logits, d = _random(6, 8, 500, torch.float32, 3, 50, 50, 2, 10)
+    d["row_seq"] = torch.tensor([0, -1, 1, 3, 2, 1000, -2 ** 31, 2 ** 31 - 1], dtype=torch.int32)
+    d["mask_rows"] = torch.tensor([0, -1, 8, 7, 100, -5, 3, 2 ** 31 - 1], dtype=torch.int32)
+    _check(_run(logits, 5, **d), logits, 5, **d)
+
+
+@pytest.mark.parametrize("V", [40, 5000, 20000, 100000])
+def test_ties_and_piles(V):
+    """Equal logits (the lower id wins), values that pile up just under the best ones, sorted rows, few distinct values."""
+    rows = [torch.zeros(V), torch.arange(V).float(), -torch.arange(V).float(), (torch.arange(V) % 7).float(),
+            torch.full((V,), -3.0e38), torch.where(torch.arange(V) % 5 == 0, 1.0, 0.999), torch.full((V,), -float("inf"))]
+    rows[6][V // 2] = -7.5
+    blocky = torch.zeros(V)
+    blocky[:min(V, 2048)] = 5 + torch.rand(min(V, 2048), generator=torch.Generator().manual_seed(0))
+    one_lane = torch.full((V,), -9.0)                                        # the best values all lie with few threads
+    one_lane[::2048] = torch.arange(len(one_lane[::2048])).float()
+    logits = torch.stack(rows + [blocky, one_lane, torch.full((V,), float("-0.0"))])
+    logits[-1, 1::2] = 0.0                                                    # -0 and +0 are equal
+    for t in TYPES:
+        x = logits.to(t)
+        for k in (1, 10, 32):
+            _check(_run(x, k), x, k)
+
+
+def test_empty_rows_and_non_finite_values():
+    V, W = 9000, (9000 + 31) // 32
+    g = torch.Generator().manual_seed(1)
+    logits = torch.randn(8, V, generator=g)
+    mask = torch.zeros(8, W, dtype=torch.int32)
+    mask[1, 280] = 1 << 5                                                     # one token
+    mask[2, 0] = 0b1011
+    mask[3:] = -1
+    mask[5, 3] = 0
+    logits[0, 5] = float("nan")                                               # masked: no influence
+    logits[1, :] = float("inf")
+    logits[1, 280 * 32 + 5] = 1.25
+    logits[3, 77] = float("nan")                                              # allowed
+    logits[4, 99] = float("inf")
+    logits[5, 96:128] = torch.tensor([float("inf"), float("nan")] * 16)       # masked
+    logits[6, :] = -float("inf")
+    logits[7, :] = torch.finfo(torch.float32).min
+    got = _run(logits, 10, mask=mask)
+    _check(got, logits, 10, mask=mask)
+    assert np.all(got["ids"][0] == oor.NO_TOKEN) and got["lse"][0] == -np.inf and np.all(got["lps"][0] == -np.inf)
+    assert got["ids"][1][0] == 280 * 32 + 5 and got["lps"][1][0] == 0.0 and got["ids"][1][1] == oor.NO_TOKEN
+    for t in (torch.bfloat16, torch.float16):
+        x = torch.nan_to_num(logits, nan=0.0, posinf=float("inf"), neginf=-float("inf")).to(t)
+        _check(_run(x, 10, mask=mask), x, 10, mask=mask)
+
+
+def test_long_lists_repeats_and_bad_entries():
+    """Histories far longer than a block, one token thousands of times, padding and tokens past the vocabulary, two biases for
+    one token, offsets that leave the list."""
+    V, rng = 30011, np.random.default_rng(3)
+    logits = torch.randn(4, V, generator=torch.Generator().manual_seed(2))
+    out = [[7] * 5000 + rng.integers(0, V, 30000).tolist(), [], [-1, V, V + 1, 2 ** 31 - 1, -2 ** 31, 3, 3], [V - 1, 0]]
+    prompt = [[], rng.integers(0, V, 40000).tolist(), [5, -1], [0]]
+    bias = [[(7, 1.0), (7, 2.0), (8, -1.0), (7, 3.5)], [], [(-1, 9.0), (V, 9.0), (3, 0.5)], [(0, float("inf"))]]
+    d = dict(n_seq=4, prompt=prompt, output=out, bias=bias, rep=[1.3, 2.0, 0.5, 1.0], freq=[0.01, 0.5, -0.25, 0.1], pres=[0.5, 0.1, 0.2, 0.3])
+    _check(_run(logits, 10, **d), logits, 10, **d)
+    flat, off = _csr(out)
+    bad = off.clone()
+    bad[0], bad[4] = -50, 10 ** 15                                            # clamped to the list
+    ids = [torch.empty(4, 10, dtype=torch.int32, device="cuda") for _ in range(2)]
+    lps = torch.empty(4, 10, device="cuda")
+    for o, i in zip((off, bad), ids):
+        lmhead.coral_lmhead_logits_process(logits.cuda(), output_tokens=flat.cuda(), output_offsets=o.cuda(),
+                                           frequency=torch.tensor(d["freq"]).cuda(), out_ids=i, out_logprobs=lps)
+    assert torch.equal(*ids)
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_row_distance_alignment_in_place(t):
+    """Rows that lie apart and start on any address, outputs aligned otherwise, the columns behind a row left as they were."""
+    V, M = 12345, 5
+    logits, d = _random(9, M, V, t, 2, 60, 60, 2, 9)
+    for off, ld, ooff, old in [(1, V + 3, 0, V), (3, V + 8, 3, V + 8), (0, V + 1, 5, V + 2), (7, 16384, 2, 12352)]:
+        buf = torch.full((off + ld * M + 8,), 3.0, dtype=t, device="cuda")
+        obuf = torch.full((ooff + old * M + 8,), 4.0, dtype=t, device="cuda")
+        x = buf[off:off + ld * M].view(M, ld)[:, :V]
+        o = obuf[ooff:ooff + old * M].view(M, old)[:, :V]
+        x.copy_(logits)
+        _check(_run(logits, 10, logits_dev=x, out=o, **d), logits, 10, **d)
+        touched = torch.zeros_like(obuf, dtype=torch.bool)
+        touched[ooff:ooff + old * M].view(M, old)[:, :V] = True
+        assert torch.all(obuf[~touched] == 4.0)
+        _check(_run(logits, 10, logits_dev=x, out=x, **d), logits, 10, **d)   # in place
+        inside = torch.zeros_like(buf, dtype=torch.bool)
+        inside[off:off + ld * M].view(M, ld)[:, :V] = True
+        assert torch.all(buf[~inside] == 3.0)
+
+
+def test_many_rows_repeat_stream_and_graph():
+    M, V = 700, 20000
+    logits, d = _random(10, M, V, torch.bfloat16, 16, 400, 300, 6, 10)
+    a = _run(logits, 10, **d)
+    _check(a, logits, 10, rows=range(0, M, 53), **d)
+    st = torch.cuda.Stream()
+    b = _run(logits, 10, stream=st, **d)
+    for n in ("ids", "lps", "lse"):
+        assert np.array_equal(a[n], b[n]), n
+    assert torch.equal(a["out"], b["out"])
+    x = logits.cuda()
+    ids, lps, lse = torch.empty(M, 10, dtype=torch.int32, device="cuda"), torch.empty(M, 10, device="cuda"), torch.empty(M, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        lmhead.coral_lmhead_logits_process(x, out_ids=ids, out_logprobs=lps, out_lse=lse)
+    x.copy_(logits.flip(0))
+    for _ in range(2):
+        g.replay()
+    torch.cuda.synchronize()
+    want = _run(logits.flip(0), 10)
+    assert np.array_equal(ids.cpu().numpy(), want["ids"]) and np.array_equal(lps.cpu().numpy(), want["lps"])
+
+
+def test_binding_refuses_wrong_tensors():
+    x = torch.zeros(4, 64, device="cuda")
+    ids, lps = torch.empty(4, 5, dtype=torch.int32, device="cuda"), torch.empty(4, 5, device="cuda")
+    call = lmhead.coral_lmhead_logits_process
+    one = torch.ones(4, device="cuda")
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")
+    i64 = lambda *s: torch.zeros(*s, dtype=torch.int64, device="cuda")
+    for bad in [dict(out_logprobs=None), dict(out_logprobs=lps[:, :4].contiguous()), dict(repetition=torch.ones(3, device="cuda")),
+                dict(repetition=one, frequency=torch.ones(5, device="cuda")), dict(prompt_tokens=i32(7)), dict(prompt_offsets=i64(5)),
+                dict(prompt_tokens=i32(7), prompt_offsets=i32(5)), dict(mask_words=i32(4, 1)), dict(mask_words=i32(3, 2)),
+                dict(bias_tokens=i32(3), bias_offsets=i64(5)), dict(bias_tokens=i32(3), bias_offsets=i64(5), bias_values=torch.ones(2, device="cuda")),
+                dict(path_tokens=i32(3, 2), repetition=one), dict(row_seq=i64(4)), dict(mask_rows=i32(4)), dict(out_lse=torch.empty(3, device="cuda")),
+                dict(out_logits=torch.empty(4, 64, device="cuda").half()), dict(out_logits=torch.empty(64, 4, device="cuda").t())]:
+        kw = dict(out_ids=ids, out_logprobs=lps)
+        kw.update(bad)
+        with pytest.raises((ValueError, lmhead.CoralError)):
+            call(x, **kw)
+    with pytest.raises(ValueError):
+        call(torch.zeros(64, 4, device="cuda").t(), out_ids=ids, out_logprobs=lps)
+    with pytest.raises(lmhead.CoralError):
+        call(x, out_ids=torch.empty(4, 33, dtype=torch.int32, device="cuda"), out_logprobs=torch.empty(4, 33, device="cuda"))

@@ -1,0 +1,141 @@
+"""GPU parity of the product with 4-bit weights against the float64 oracle.
+
+Tolerance.  u = 2^-24.  Integers and activations are exact operands; one MMA step adds 16 products and the running sum, each
+kept to at least 24 bits below the largest of them, so a step is off by at most 17 u of the sizes it adds and a group of g
+columns by 17 g / 16 u; the groups add K / g roundings, the split of the columns at most 16 more and the scale's product 1.
+Then one rounding to the output type.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators_oracle as oor
+from paper_2502_16880_b200 import lmhead
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def _make(seed, M, N, K, group, zeros, xt, st):
+    g = torch.Generator().manual_seed(seed)
+    Wq = torch.randint(0, 256, (N, K // 2), generator=g, dtype=torch.uint8)
+    scales = ((0.5 + torch.rand(N, K // group, generator=g)) * 0.01).to(st)
+    z = torch.randint(0, 16, (N, K // group), generator=g, dtype=torch.uint8) if zeros else None
+    return Wq, scales, z, torch.randn(M, K, generator=g).to(xt)
+
+
+def _linear(Wq, scales, z):
+    return lmhead.Q4Linear(Wq.cuda(), scales.cuda(), None if z is None else z.cuda())
+
+
+def _check(got, Wq, scales, z, x, group):
+    want, size = oor.q4_linear(Wq.numpy(), scales.double().numpy(), None if z is None else z.numpy(), x.double().numpy())
+    K = x.shape[1]
+    tol = (17 * group / 16 + K / group + 17) * U * size
+    tol = tol + torch.finfo(got.dtype).eps / 2 * (np.abs(want) + tol) + (2.0 ** -25 if got.dtype == torch.float16 else 0)
+    off = np.abs(got.double().cpu().numpy() - want)
+    assert np.all(off <= tol), float(np.max(off / tol))
+
+
+@pytest.mark.parametrize("xt", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_types_groups_and_row_counts(xt, group, zeros):
+    for i, (M, N, K) in enumerate([(1, 1, group), (2, 17, 3 * group), (8, 500, 1024), (9, 129, 5 * 128), (16, 4001, 256), (61, 48, 384),
+                                   (150, 33, 7 * group)]):
+        st = [torch.bfloat16, torch.float16][i % 2]
+        Wq, s, z, x = _make(i * 7 + group, M, N, K, group, zeros, xt, st)
+        lin = _linear(Wq, s, z)
+        for ot in (torch.float32, xt) if i else (torch.float32, torch.bfloat16, torch.float16):
+            _check(lin.forward(x.cuda(), out_dtype=ot), Wq, s, z, x, group)
+
+
+@pytest.mark.parametrize("M", [1, 2, 7, 8, 13, 16, 17, 31, 33, 60, 64, 65])
+def test_wide_products(M):
+    """Column splits over many warps, several passes over the rows, more tiles than the device holds at once."""
+    for N, K, group in [(3000, 4096, 128), (40000, 512, 64), (100, 8192, 32)]:
+        Wq, s, z, x = _make(M, M, N, K, group, M % 2 == 0, torch.bfloat16, torch.bfloat16)
+        _check(_linear(Wq, s, z).forward(x.cuda()), Wq, s, z, x, group)
+
+
+def test_longest_columns():
+    for M, K in [(1, 65536), (3, 28672), (10, 14336)]:
+        Wq, s, z, x = _make(K, M, 40, K, 128, True, torch.float16, torch.float16)
+        _check(_linear(Wq, s, z).forward(x.cuda()), Wq, s, z, x, 128)
+
+
+@pytest.mark.parametrize("xt", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("M", [1, 8, 16, 24, 60])
+def test_whole_numbers_are_exact(M, xt):
+    """Small integers and scales that are powers of two: every sum is exact, so a wrong or missing term shows."""
+    g = torch.Generator().manual_seed(M)
+    N, K, group = 300, 1152, 32
+    Wq = torch.randint(0, 256, (N, K // 2), generator=g, dtype=torch.uint8)
+    s = (2.0 ** torch.randint(-2, 3, (N, K // group), generator=g).float()).to(xt)
+    z = torch.randint(0, 128, (N, K // group), generator=g, dtype=torch.uint8)
+    x = torch.randint(-4, 5, (M, K), generator=g).to(xt)
+    got = _linear(Wq, s, z).forward(x.cuda())
+    want, _ = oor.q4_linear(Wq.numpy(), s.double().numpy(), z.numpy(), x.double().numpy())
+    assert np.array_equal(got.double().cpu().numpy(), want)
+    # one column at a time lands where it belongs
+    for col in (0, 1, 5, 37, K - 1):
+        e = torch.zeros(M, K, dtype=xt)
+        e[M - 1, col] = 1
+        got = _linear(Wq, s, z).forward(e.cuda()).double().cpu().numpy()
+        want, _ = oor.q4_linear(Wq.numpy(), s.double().numpy(), z.numpy(), e.double().numpy())
+        assert np.array_equal(got, want), col
+
+
+def test_a_bad_row_stays_in_its_row():
+    Wq, s, z, x = _make(3, 20, 200, 256, 64, True, torch.bfloat16, torch.bfloat16)
+    clean = _linear(Wq, s, z).forward(x.cuda())
+    x[11, 7] = float("nan")
+    x[2, 9] = float("inf")
+    got = _linear(Wq, s, z).forward(x.cuda())
+    assert torch.all(torch.isnan(got[11])) and not torch.any(torch.isfinite(got[2]))
+    keep = [m for m in range(20) if m not in (2, 11)]
+    assert torch.equal(got[keep], clean[keep])
+
+
+def test_repeat_streams_graph_and_neighbours():
+    Wq, s, z, x = _make(4, 24, 1003, 512, 128, False, torch.bfloat16, torch.float16)
+    lin, x = _linear(Wq, s, z), x.cuda()
+    first = lin.forward(x)
+    assert torch.equal(first, lin.forward(x))
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    outs = [torch.empty_like(first) for _ in streams]
+    torch.cuda.synchronize()
+    for st, o in zip(streams, outs):                        # the same packed copy on several streams at once
+        lin.forward(x, out=o, stream=st)
+    torch.cuda.synchronize()
+    for o in outs:
+        assert torch.equal(o, first)
+    big = torch.full((26, 1003), 5.0, device="cuda")
+    lin.forward(x, out=big[1:25])                            # rows before and behind stay as they were
+    assert torch.equal(big[1:25], first) and torch.all(big[0] == 5) and torch.all(big[25] == 5)
+    out = torch.empty_like(first)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        lin.forward(x, out=out)
+    x.mul_(-2)
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, first * -2)                      # a power of two scales every sum exactly
+
+
+def test_binding_refuses_wrong_tensors():
+    Wq, s, z, x = _make(5, 4, 64, 256, 64, True, torch.bfloat16, torch.bfloat16)
+    lin = _linear(Wq, s, z)
+    x = x.cuda()
+    for bad in [x.float(), x[:, :128].contiguous(), x.cpu(), x.t()]:
+        with pytest.raises((ValueError, lmhead.CoralError)):
+            lin.forward(bad, out=torch.empty(4, 64, device="cuda"))
+    for out in [torch.empty(4, 63, device="cuda"), torch.empty(3, 64, device="cuda"), torch.empty(4, 64, device="cuda", dtype=torch.int32)]:
+        with pytest.raises((ValueError, lmhead.CoralError)):
+            lin.forward(x, out=out)
+    with pytest.raises((ValueError, lmhead.CoralError)):     # a group of 16 columns
+        lmhead.Q4Linear(Wq.cuda(), torch.ones(64, 16, dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(ValueError):
+        lmhead.Q4Linear(Wq.cuda(), s.float().cuda())
+    with pytest.raises(ValueError):
+        lmhead.Q4Linear(Wq.cuda(), s.cuda(), z[:, :2].contiguous().cuda())
