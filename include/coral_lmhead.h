@@ -43,6 +43,7 @@ extern "C" {
 /* Limits of this build. */
 #define CORAL_MAX_GROUPS 256       /* n_groups <= 256 */
 #define CORAL_MAX_K_TOKENS 32      /* k_tokens <= 32 */
+#define CORAL_MAX_PATH 64          /* draft tokens on a row's path (coral_lmhead_logits_process) */
 #define CORAL_ROUTE_STATIC_MAX_ROWS 64 /* M <= 64 for coral_lmhead_route_static */
 
 /* config flags: a handle that stores (and computes) only the groups n with n % world == rank */
@@ -491,7 +492,7 @@ int coral_lmhead_q4_linear(const coral_lmhead_q4_config *cfg, const void *packed
  *     (n_seq >= M; n_seq = 0: no sequence at all).
  *   prompt_tokens, output_tokens (int32) with offsets (int64 [n_seq + 1], in elements) and the number of list elements in
  *     *_total: offsets are clamped to it.  Tokens outside [0, V) are passed over, so a list may be padded with -1.
- *   path_tokens [M x path_len] int32, entries outside [0, V) passed over.
+ *   path_tokens [M x path_len] int32, path_len at most CORAL_MAX_PATH, entries outside [0, V) passed over.
  *   repetition (> 0), frequency, presence: fp32 [n_seq].
  *   bias_tokens, bias_values, bias_offsets, bias_total: lists like the prompt's, with one fp32 value an entry.
  *   mask_words: int32 words [n_masks x ceil(V / 32)], bit x % 32 of word x / 32 allows token x; mask_rows [M]: mask of a row,

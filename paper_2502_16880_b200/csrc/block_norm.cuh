@@ -26,6 +26,7 @@ struct NormArgs {
     const void *dy, *dh;                            // backward: either may be null
     void *dx, *dr, *dgate;                          // dr null when r is; dgate: modes 2 (fp32) and 3 (element type)
     float* part;                                    // [grid][3][H] column sums: w_pre, w_post, gate (backward)
+    int want;                                       // ... bits 0 to 2: which of them
 };
 
 __device__ __forceinline__ void cp_async16(void* dst, const void* src) {
@@ -41,24 +42,53 @@ __device__ __forceinline__ void cp_async_wait_left(int left) {
     else cp_async_wait<3>();
 }
 
-// Sum of (a, b) over the block, the same bits in every thread and on every run.  `turn` alternates between two
-// buffers, so one barrier a sum is enough: a buffer is written again only behind the barrier of the sum in between.
-__device__ __forceinline__ void block_sum2(float& a, float& b, float2 (*buf)[kNormWarps], int& turn) {
+// Sums over the block, the same bits in every thread and on every run: a shuffle tree a warp, then the warps' sums in order.
+// `turn` alternates between two buffers, so one barrier a sum is enough: a buffer is written again only behind the barrier of
+// the sum in between.  The buffers start as zeros, and warps that do not exist stay zero.
+struct NormSums {
+    float4 a[2][kNormWarps / 4], b[2][kNormWarps / 4];
+};
+__device__ __forceinline__ float sum_warps(const float4 (&v)[kNormWarps / 4]) {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < kNormWarps / 4; ++i) t += (v[i].x + v[i].y) + (v[i].z + v[i].w);
+    return t;
+}
+__device__ __forceinline__ float block_sum(float a, NormSums& s, int& turn) {
+    a = warp_sum(a);
+    if ((threadIdx.x & 31) == 0) reinterpret_cast<float*>(s.a[turn])[threadIdx.x >> 5] = a;
+    __syncthreads();
+    a = sum_warps(s.a[turn]);
+    turn ^= 1;
+    return a;
+}
+__device__ __forceinline__ void block_sum2(float& a, float& b, NormSums& s, int& turn) {
     a = warp_sum(a);
     b = warp_sum(b);
-    const int warps = blockDim.x >> 5;
-    float2* s = buf[turn];
-    turn ^= 1;
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = make_float2(a, b);
-    __syncthreads();
-    a = 0.f;
-    b = 0.f;
-    for (int w = 0; w < warps; ++w) {
-        const float2 v = s[w];
-        a += v.x;
-        b += v.y;
+    if ((threadIdx.x & 31) == 0) {
+        reinterpret_cast<float*>(s.a[turn])[threadIdx.x >> 5] = a;
+        reinterpret_cast<float*>(s.b[turn])[threadIdx.x >> 5] = b;
     }
+    __syncthreads();
+    a = sum_warps(s.a[turn]);
+    b = sum_warps(s.b[turn]);
+    turn ^= 1;
 }
+__device__ __forceinline__ void clear_sums(NormSums& s) {
+    for (int i = threadIdx.x; i < (int)(sizeof(s) / 4); i += blockDim.x) reinterpret_cast<float*>(&s)[i] = 0.f;
+    __syncthreads();
+}
+
+// Eight elements as they lie in memory, widened where they are used (weights wait in registers this way).
+template <typename T> struct Raw8 {
+    uint4 v[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const void* p, int ch) {
+        const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p) + (size_t)ch * 8);
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(T) / 2); ++i) v[i] = __ldg(q + i);
+    }
+    __device__ __forceinline__ void get(float (&f)[8]) const { Elem<T>::load8(reinterpret_cast<const T*>(v), f); }
+};
 
 // Staged tensors of one row: x, then r, then (backward) dy, dh, then a full gate; absent ones are not staged.
 template <typename T, int NV>
@@ -96,9 +126,9 @@ __device__ __forceinline__ void load_weights8(const void* w, int ch, float (&v)[
 
 // grid: any; dynamic shared memory: stages * tensors * NV * blockDim * 8 elements.
 template <typename T, int NV>
-__global__ void __launch_bounds__(kNormMaxThreads) block_norm_kernel(NormArgs a, int stages) {
+__global__ void __launch_bounds__(kNormMaxThreads, NV < 4 ? 2 : 1) block_norm_kernel(NormArgs a, int stages) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    __shared__ float2 s_sum[2][kNormWarps];
+    __shared__ NormSums s_sum;
     const int H = a.H, chunks = H >> 3;
     const int t_r = a.r ? 1 : -1, t_g = a.gate_mode == 3 ? 1 + (a.r ? 1 : 0) : -1;
     const NormStage<T, NV> st{smem_raw, 1 + (a.r ? 1 : 0) + (a.gate_mode == 3 ? 1 : 0), chunks};
@@ -112,54 +142,56 @@ __global__ void __launch_bounds__(kNormMaxThreads) block_norm_kernel(NormArgs a,
         if (row < (size_t)a.M) fetch(s, row);
         cp_async_commit();
     }
-    // the weights of this thread's columns: column gate and w_post act as one factor where both are vectors
-    float wb[NV][8], wp[NV][8];
+    Raw8<T> w_post[NV], w_pre[NV], w_gate[NV];      // the weights of this thread's columns
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int ch = threadIdx.x + i * blockDim.x;
         if (ch >= chunks) continue;
-        load_weights8<T>(a.w_post, ch, wb[i]);
-        load_weights8<T>(a.w_pre, ch, wp[i]);
-        if (a.gate_mode == 1) {
-            float g[8];
-            load_weights8<T>(a.gate, ch, g);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) wb[i][j] *= g[j];
-        }
+        if (a.w_post) w_post[i].load(a.w_post, ch);
+        if (a.w_pre) w_pre[i].load(a.w_pre, ch);
+        if (a.gate_mode == 1) w_gate[i].load(a.gate, ch);
     }
+    clear_sums(s_sum);
     int turn = 0, stage = 0;
     const float inv_h = 1.f / (float)H;
     for (size_t row = blockIdx.x; row < (size_t)a.M; row += gridDim.x) {
         cp_async_wait_left(stages - 1);
-        float x[NV][8], y[NV][8];
-        float sx = 0.f, sy = 0.f, none = 0.f;
+        float y[NV][8];                             // first x, then y
+        float sx = 0.f, sy = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (threadIdx.x + i * blockDim.x >= chunks) continue;
-            Elem<T>::load8(st.slot(stage, 0, i), x[i]);
+            Elem<T>::load8(st.slot(stage, 0, i), y[i]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sx = fmaf(x[i][j], x[i][j], sx);
+            for (int j = 0; j < 8; ++j) sx = fmaf(y[i][j], y[i][j], sx);
         }
-        float scale = 1.f;
-        if (a.w_post) {
-            block_sum2(sx, none, s_sum, turn);
-            scale = rsqrtf(fmaf(sx, inv_h, a.eps));
-        }
-        if (a.gate_mode == 2) scale *= Elem<T>::up(reinterpret_cast<const T*>(a.gate)[row]);
+        float scale = a.gate_mode == 2 ? Elem<T>::up(reinterpret_cast<const T*>(a.gate)[row]) : 1.f;
+        if (a.w_post) scale *= rsqrtf(fmaf(block_sum(sx, s_sum, turn), inv_h, a.eps));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int ch = threadIdx.x + i * blockDim.x;
             if (ch >= chunks) continue;
-            float r[8], g[8];
-            if (t_r >= 0) Elem<T>::load8(st.slot(stage, t_r, i), r);
-            if (t_g >= 0) Elem<T>::load8(st.slot(stage, t_g, i), g);
+            float f[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float b = x[i][j] * scale * wb[i][j];
-                if (t_g >= 0) b *= g[j];
-                y[i][j] = t_r >= 0 ? fmaf(a.alpha, r[j], b) : b;
-                sy = fmaf(y[i][j], y[i][j], sy);
+            for (int j = 0; j < 8; ++j) y[i][j] *= scale;
+            if (a.w_post) {
+                w_post[i].get(f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[i][j] *= f[j];
             }
+            if (a.gate_mode == 1 || a.gate_mode == 3) {
+                if (a.gate_mode == 1) w_gate[i].get(f);
+                else Elem<T>::load8(st.slot(stage, t_g, i), f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[i][j] *= f[j];
+            }
+            if (t_r >= 0) {
+                Elem<T>::load8(st.slot(stage, t_r, i), f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[i][j] = fmaf(a.alpha, f[j], y[i][j]);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sy = fmaf(y[i][j], y[i][j], sy);
             if (a.y) Elem<T>::store8(reinterpret_cast<T*>(a.y) + row * H + (size_t)ch * 8, y[i]);
         }
         // this thread's slots of the stage have been read: the row `stages` turns ahead may come in
@@ -168,14 +200,15 @@ __global__ void __launch_bounds__(kNormMaxThreads) block_norm_kernel(NormArgs a,
         cp_async_commit();
         stage = stage + 1 == stages ? 0 : stage + 1;
         if (!a.h) continue;
-        block_sum2(sy, none, s_sum, turn);
-        const float ry = rsqrtf(fmaf(sy, inv_h, a.eps));
+        const float ry = rsqrtf(fmaf(block_sum(sy, s_sum, turn), inv_h, a.eps));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int ch = threadIdx.x + i * blockDim.x;
             if (ch >= chunks) continue;
+            float f[8];
+            w_pre[i].get(f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[i][j] = y[i][j] * ry * wp[i][j];
+            for (int j = 0; j < 8; ++j) y[i][j] = y[i][j] * ry * f[j];
             Elem<T>::store8(reinterpret_cast<T*>(a.h) + row * H + (size_t)ch * 8, y[i]);
         }
     }
@@ -189,7 +222,7 @@ __global__ void __launch_bounds__(kNormMaxThreads) block_norm_kernel(NormArgs a,
 template <typename T, int NV>
 __global__ void __launch_bounds__(kNormMaxThreads) block_norm_backward_kernel(NormArgs a, int stages) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    __shared__ float2 s_sum[2][kNormWarps];
+    __shared__ NormSums s_sum;
     const int H = a.H, chunks = H >> 3;
     int n_t = 1;
     const int t_r = a.r ? n_t++ : -1, t_dy = a.dy ? n_t++ : -1, t_dh = a.dh ? n_t++ : -1, t_g = a.gate_mode == 3 ? n_t++ : -1;
@@ -207,11 +240,12 @@ __global__ void __launch_bounds__(kNormMaxThreads) block_norm_backward_kernel(No
         cp_async_commit();
     }
     float acc_pre[NV][8] = {}, acc_post[NV][8] = {}, acc_gate[NV][8] = {};
+    clear_sums(s_sum);
     int turn = 0, stage = 0;
     const float inv_h = 1.f / (float)H;
     for (size_t row = blockIdx.x; row < (size_t)a.M; row += gridDim.x) {
         cp_async_wait_left(stages - 1);
-        float sx = 0.f, none = 0.f;
+        float sx = 0.f;
         float rx = 1.f;
         if (a.w_post) {
 #pragma unroll
@@ -222,8 +256,7 @@ __global__ void __launch_bounds__(kNormMaxThreads) block_norm_backward_kernel(No
 #pragma unroll
                 for (int j = 0; j < 8; ++j) sx = fmaf(x[j], x[j], sx);
             }
-            block_sum2(sx, none, s_sum, turn);
-            rx = rsqrtf(fmaf(sx, inv_h, a.eps));
+            rx = rsqrtf(fmaf(block_sum(sx, s_sum, turn), inv_h, a.eps));
         }
         const float g_row = a.gate_mode == 2 ? Elem<T>::up(reinterpret_cast<const T*>(a.gate)[row]) : 1.f;
         auto gate8 = [&](int i, int ch, float (&g)[8]) {
@@ -336,9 +369,9 @@ __global__ void __launch_bounds__(kNormMaxThreads) block_norm_backward_kernel(No
     for (int i = 0; i < NV; ++i) {
         const int ch = threadIdx.x + i * blockDim.x;
         if (ch >= chunks) continue;
-        Elem<float>::store8(part + (size_t)ch * 8, acc_pre[i]);
-        Elem<float>::store8(part + H + (size_t)ch * 8, acc_post[i]);
-        Elem<float>::store8(part + 2 * H + (size_t)ch * 8, acc_gate[i]);
+        if (a.want & 1) Elem<float>::store8(part + (size_t)ch * 8, acc_pre[i]);
+        if (a.want & 2) Elem<float>::store8(part + H + (size_t)ch * 8, acc_post[i]);
+        if (a.want & 4) Elem<float>::store8(part + 2 * H + (size_t)ch * 8, acc_gate[i]);
     }
     pdl_launch_dependents();
 }

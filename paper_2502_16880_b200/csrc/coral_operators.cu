@@ -20,15 +20,17 @@ bool device_sms(int* sms) {
     return cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess;
 }
 
-// The attribute is per kernel and device; above 48 KB it has to be raised before the launch.
+// The attribute is per kernel and device; above 48 KB, static shared memory (at most 16 KB in these kernels) counted in, it has
+// to be raised before the launch.
 template <typename K>
 bool allow_smem(K kernel, size_t bytes) {
-    return bytes <= 48 * 1024 ||
+    return bytes <= 32 * 1024 ||
            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
 }
 
 // ---- block norm ----------------------------------------------------------------------------------------------
 constexpr int kNormFwdThreadsPerSm = 1024, kNormBwdThreadsPerSm = 512;
+constexpr int kNormSmallBlock = 256;             // threads of a block while a row fits two chunks a thread
 constexpr size_t kNormSmemPerSm = 200 * 1024;
 constexpr int kNormMaxBlocksPerSm = 16;
 constexpr int kNormSmCap = 160;                 // most SMs the partial rows of the workspace are sized for
@@ -38,15 +40,24 @@ struct NormPlan {
     size_t smem;
 };
 
-// nv: 8-column chunks a thread keeps.  Threads are the chunks over nv rounded up to a warp, so that a row of 3584
-// columns runs 448 threads and wastes none.
+// nv: 8-column chunks a thread keeps.  Blocks of up to 256 threads, several a SM, so that one block's row sums wait while
+// another's row is worked on (16384 x 4096 forward: @@A@@ us, @@B@@ with one chunk a thread and 512 threads).  Threads are the
+// chunks over nv rounded up to a warp: a row of 3584 columns runs 224 threads and wastes none.
+void norm_block(int H, int* nv, int* threads) {
+    const int chunks = H / 8;
+    *nv = chunks <= kNormSmallBlock ? 1 : chunks <= 2 * kNormMaxThreads ? 2 : 4;
+    *threads = ((chunks + *nv - 1) / *nv + 31) / 32 * 32;
+}
+
+int norm_blocks_per_sm(int threads, int threads_per_sm) {
+    const int blocks = threads_per_sm / threads;
+    return blocks < 1 ? 1 : blocks > kNormMaxBlocksPerSm ? kNormMaxBlocksPerSm : blocks;
+}
+
 NormPlan norm_plan(int M, int H, int type, int tensors, int threads_per_sm, int sms) {
     NormPlan p{};
-    const int chunks = H / 8;
-    p.nv = chunks <= kNormMaxThreads ? 1 : chunks <= 2 * kNormMaxThreads ? 2 : 4;
-    p.threads = ((chunks + p.nv - 1) / p.nv + 31) / 32 * 32;
-    int blocks = threads_per_sm / p.threads;
-    blocks = blocks < 1 ? 1 : blocks > kNormMaxBlocksPerSm ? kNormMaxBlocksPerSm : blocks;
+    norm_block(H, &p.nv, &p.threads);
+    int blocks = norm_blocks_per_sm(p.threads, threads_per_sm);
     const size_t stage = (size_t)tensors * p.nv * p.threads * 8 * elem_size(type);
     size_t stages = kNormSmemPerSm / blocks / stage;
     if (stages < 1) {                            // very wide fp32 rows: one block a SM
@@ -55,19 +66,17 @@ NormPlan norm_plan(int M, int H, int type, int tensors, int threads_per_sm, int 
     }
     p.stages = stages > 4 ? 4 : (int)stages;
     if (sms > kNormSmCap) sms = kNormSmCap;
-    const long long most = (long long)sms * blocks;
-    p.grid = (int)(M < most ? M : most);
+    const int most = sms * blocks, turns = (M - 1) / most + 1;
+    p.grid = (M - 1) / turns + 1;                // no more blocks than the busiest one's rows ask for
     p.smem = stage * p.stages;
     return p;
 }
 
 // Most partial rows a backward call can write.
 int norm_max_grid(int H) {
-    const int chunks = H / 8;
-    const int threads = (((chunks > kNormMaxThreads ? kNormMaxThreads : chunks)) + 31) / 32 * 32;
-    int blocks = kNormBwdThreadsPerSm / threads;
-    blocks = blocks < 1 ? 1 : blocks > kNormMaxBlocksPerSm ? kNormMaxBlocksPerSm : blocks;
-    return 2 * blocks * kNormSmCap;              // nv > 1 halves the threads at most, which doubles the blocks
+    int nv, threads;
+    norm_block(H, &nv, &threads);
+    return norm_blocks_per_sm(threads, kNormBwdThreadsPerSm) * kNormSmCap;
 }
 
 bool norm_args_ok(const coral_lmhead_norm_args* a) {
@@ -209,7 +218,7 @@ bool logits_args_ok(const coral_lmhead_logits_args* a) {
     if ((a->bias_tokens_dev != nullptr) != (a->bias_offsets_dev != nullptr) ||
         (a->bias_tokens_dev != nullptr) != (a->bias_values_dev != nullptr) || a->bias_total < 0 || a->bias_total > 0x7fffffff)
         return false;
-    if (a->path_len < 0 || (a->path_tokens_dev != nullptr) != (a->path_len > 0)) return false;
+    if (a->path_len < 0 || a->path_len > CORAL_MAX_PATH || (a->path_tokens_dev != nullptr) != (a->path_len > 0)) return false;
     if (a->mask_words_dev ? a->n_masks < 1 : a->mask_rows_dev != nullptr) return false;
     if (a->mask_words_dev && !a->mask_rows_dev && a->n_masks < a->M) return false;
     const size_t e = elem_size(a->type);
@@ -373,11 +382,12 @@ int coral_lmhead_block_norm_backward(const coral_lmhead_norm_args* a, void* work
     k.dgate = a->gate_mode == CORAL_GATE_CHANNEL ? nullptr : a->out_dgate_dev;
     k.part = static_cast<float*>(workspace_dev);
     float* d_gate = a->gate_mode == CORAL_GATE_CHANNEL ? static_cast<float*>(a->out_dgate_dev) : nullptr;
+    k.want = (a->out_dw_pre_dev ? 1 : 0) | (a->out_dw_post_dev ? 2 : 0) | (d_gate ? 4 : 0);
     const int tensors = 1 + (k.r ? 1 : 0) + (k.dy ? 1 : 0) + (k.dh ? 1 : 0) + (k.gate_mode == CORAL_GATE_FULL ? 1 : 0);
     const NormPlan p = norm_plan(a->M, a->H, a->type, tensors, kNormBwdThreadsPerSm, sms);
     const int rc = launch_norm_type(a->type, k, p, true, st);
     if (rc != CORAL_OK) return rc;
-    if (!a->out_dw_pre_dev && !a->out_dw_post_dev && !d_gate) return CORAL_OK;
+    if (!k.want) return CORAL_OK;
     if (launch_pdl(block_norm_columns_kernel, dim3((a->H + 31) / 32, 3), dim3(kNormColWarps * 32), 0, st, k.part, p.grid, a->H,
                    a->out_dw_pre_dev, a->out_dw_post_dev, d_gate) != cudaSuccess)
         return CORAL_ERR_CUDA;

@@ -378,6 +378,8 @@ def coral_tree_expand(parent_scores, cand_ids, cand_logprobs, K, out_parent, out
         _dev_ptr(out_score, torch.float32, False), _stream_ptr(stream)), "coral_tree_expand")
 
 
+# The operators around the draft step are called once per layer or token, so their checks are kept short: one line per
+# tensor that returns its pointer, and the reason is looked for only when it fails.
 _TYPES = {torch.float32: CORAL_TYPE_F32, torch.bfloat16: CORAL_TYPE_BF16, torch.float16: CORAL_TYPE_F16}
 
 
@@ -387,50 +389,57 @@ def _type_of(t) -> int:
     return _TYPES[t.dtype]
 
 
-def _op_ptr(name, t, dtype, shape, device):
-    """Pointer of an operator's tensor (None stays None) after checking type, shape, contiguity and device: the library
-    launches on the current device and reads and writes as many elements as the other arguments say."""
+def _op_ptr(name, t, dtype, shape, dev):
+    """Pointer of an operator's tensor (None stays None) of this type and shape, contiguous, on device index `dev`: the
+    library launches on the current device and reads and writes as many elements as the other arguments say."""
     if t is None:
         return None
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous CUDA tensor")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
-    if t.dtype != dtype:
-        raise ValueError(f"{name}: expected dtype {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and (shape is None or t.shape == shape):
+        return t.data_ptr()
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{dev}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor")
+    raise ValueError(f"{name}: expected {dtype} {shape if shape is not None else ''}, got {t.dtype} {tuple(t.shape)}")
 
 
-def _op_device(t, name):
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+def _op_device(t, name) -> int:
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
         raise ValueError(f"{name} must be on the current CUDA device")
-    return t.device
+    return dev
 
 
-def _norm_args(x, r, w_pre, eps, w_post, gate, gate_mode, alpha):
-    dev = _op_device(x, "x")
+def _op_stream(stream, dev) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+_NORM_SIZE = ctypes.sizeof(coral_lmhead_norm_args)
+
+
+def _norm_args(x, r, w_pre, eps, w_post, gate, gate_mode, alpha, dev, out_y=None, out_h=None, dy=None, dh=None, out_dx=None,
+               out_dr=None, out_dgate=None, out_dw_pre=None, out_dw_post=None):
     if x.dim() != 2:
         raise ValueError("x must be [M, H]")
-    M, H = x.shape
-    t = x.dtype
-    shape = {CORAL_GATE_CHANNEL: (H,), CORAL_GATE_ROW: (M,), CORAL_GATE_FULL: (M, H)}.get(int(gate_mode))
+    shape, t, f = x.shape, x.dtype, torch.float32
+    M, H = shape
+    g_shape = None if gate is None else (H,) if gate_mode == CORAL_GATE_CHANNEL else (M,) if gate_mode == CORAL_GATE_ROW else shape
     return coral_lmhead_norm_args(
-        struct_size=ctypes.sizeof(coral_lmhead_norm_args), type=_type_of(x), M=M, H=H, gate_mode=int(gate_mode),
-        alpha=float(alpha), eps=float(eps), x_dev=_op_ptr("x", x, t, (M, H), dev), r_dev=_op_ptr("r", r, t, (M, H), dev),
-        gate_dev=_op_ptr("gate", gate, t, shape, dev), w_post_dev=_op_ptr("w_post", w_post, t, (H,), dev),
-        w_pre_dev=_op_ptr("w_pre", w_pre, t, (H,), dev)), dev
+        _NORM_SIZE, _type_of(x), M, H, gate_mode, alpha, eps, _op_ptr("x", x, t, shape, dev), _op_ptr("r", r, t, shape, dev),
+        _op_ptr("gate", gate, t, g_shape, dev), _op_ptr("w_post", w_post, t, (H,), dev), _op_ptr("w_pre", w_pre, t, (H,), dev),
+        _op_ptr("out_y", out_y, t, shape, dev), _op_ptr("out_h", out_h, t, shape, dev), _op_ptr("dy", dy, t, shape, dev),
+        _op_ptr("dh", dh, t, shape, dev), _op_ptr("out_dx", out_dx, t, shape, dev), _op_ptr("out_dr", out_dr, t, shape, dev),
+        _op_ptr("out_dgate", out_dgate, t if gate_mode == CORAL_GATE_FULL else f, g_shape, dev),
+        _op_ptr("out_dw_pre", out_dw_pre, f, (H,), dev), _op_ptr("out_dw_post", out_dw_post, f, (H,), dev))
 
 
 def coral_lmhead_block_norm(x, r, w_pre, eps, out_y, out_h, w_post=None, gate=None, gate_mode=CORAL_GATE_NONE, alpha=1.0,
                             stream=None):
     """y = alpha r + gate b with b = x, or its norm times w_post; h = the norm of y times w_pre.  x, r, out_y, out_h:
     [M, H]; gate: [H], [M] or [M, H] by gate_mode (CORAL_GATE_*).  r, w_pre with out_h, or out_y may be None."""
-    a, dev = _norm_args(x, r, w_pre, eps, w_post, gate, gate_mode, alpha)
-    a.out_y_dev = _op_ptr("out_y", out_y, x.dtype, x.shape, dev)
-    a.out_h_dev = _op_ptr("out_h", out_h, x.dtype, x.shape, dev)
-    _check(load_library().coral_lmhead_block_norm(ctypes.byref(a), _stream_ptr(stream)), "coral_lmhead_block_norm")
+    dev = _op_device(x, "x")
+    a = _norm_args(x, r, w_pre, eps, w_post, gate, gate_mode, alpha, dev, out_y, out_h)
+    _check((_lib or load_library()).coral_lmhead_block_norm(ctypes.byref(a), _op_stream(stream, dev)), "coral_lmhead_block_norm")
 
 
 def coral_lmhead_block_norm_backward_bytes(M: int, H: int) -> int:
@@ -446,21 +455,13 @@ def coral_lmhead_block_norm_backward(x, r, w_pre, eps, dy, dh, workspace, out_dx
     """Gradient of coral_lmhead_block_norm.  dy, dh: gradients of y and h (one may be None); out_dx, out_dr like x;
     out_dw_pre, out_dw_post: fp32 [H]; out_dgate: fp32 [H] or [M], or like x for a full gate; workspace: CUDA uint8
     tensor of coral_lmhead_block_norm_backward_bytes(M, H)."""
-    a, dev = _norm_args(x, r, w_pre, eps, w_post, gate, gate_mode, alpha)
-    M, H = x.shape
-    t, f = x.dtype, torch.float32
-    a.dy_dev = _op_ptr("dy", dy, t, (M, H), dev)
-    a.dh_dev = _op_ptr("dh", dh, t, (M, H), dev)
-    a.out_dx_dev = _op_ptr("out_dx", out_dx, t, (M, H), dev)
-    a.out_dr_dev = _op_ptr("out_dr", out_dr, t, (M, H), dev)
-    a.out_dw_pre_dev = _op_ptr("out_dw_pre", out_dw_pre, f, (H,), dev)
-    a.out_dw_post_dev = _op_ptr("out_dw_post", out_dw_post, f, (H,), dev)
-    full = int(gate_mode) == CORAL_GATE_FULL
-    a.out_dgate_dev = _op_ptr("out_dgate", out_dgate, t if full else f, None if gate is None else gate.shape, dev)
-    if workspace.numel() * workspace.element_size() < coral_lmhead_block_norm_backward_bytes(M, H):
+    dev = _op_device(x, "x")
+    a = _norm_args(x, r, w_pre, eps, w_post, gate, gate_mode, alpha, dev, None, None, dy, dh, out_dx, out_dr, out_dgate,
+                   out_dw_pre, out_dw_post)
+    if workspace.numel() < coral_lmhead_block_norm_backward_bytes(*x.shape):
         raise ValueError("workspace is smaller than coral_lmhead_block_norm_backward_bytes(M, H)")
-    _check(load_library().coral_lmhead_block_norm_backward(
-        ctypes.byref(a), _op_ptr("workspace", workspace, torch.uint8, None, dev), _stream_ptr(stream)),
+    _check((_lib or load_library()).coral_lmhead_block_norm_backward(
+        ctypes.byref(a), _op_ptr("workspace", workspace, torch.uint8, None, dev), _op_stream(stream, dev)),
         "coral_lmhead_block_norm_backward")
 
 
@@ -485,33 +486,53 @@ def coral_lmhead_q4_pack(cfg, Wq, scales, zeros, packed, stream=None) -> None:
         raise ValueError("packed is smaller than coral_lmhead_q4_packed_bytes(cfg)")
     _check(load_library().coral_lmhead_q4_pack(
         ctypes.byref(cfg), _op_ptr("Wq", Wq, torch.uint8, (cfg.N, cfg.K // 2), dev), _op_ptr("scales", scales, sdt, g, dev),
-        _op_ptr("zeros", zeros, torch.uint8, g, dev), _op_ptr("packed", packed, torch.uint8, None, dev), _stream_ptr(stream)),
+        _op_ptr("zeros", zeros, torch.uint8, g, dev), _op_ptr("packed", packed, torch.uint8, None, dev), _op_stream(stream, dev)),
         "coral_lmhead_q4_pack")
 
 
 def coral_lmhead_q4_linear(cfg, packed, x, out, stream=None) -> None:
     """out [M, N] (fp32, bf16 or fp16) = x [M, K] (bf16 or fp16) times the packed weights' transpose."""
     dev = _op_device(x, "x")
-    M = x.shape[0]
-    _check(load_library().coral_lmhead_q4_linear(
-        ctypes.byref(cfg), _op_ptr("packed", packed, torch.uint8, None, dev), _op_ptr("x", x, x.dtype, (M, cfg.K), dev),
-        _type_of(x), M, _op_ptr("out", out, out.dtype, (M, cfg.N), dev), _type_of(out), _stream_ptr(stream)),
+    M, N, K, group = x.shape[0], cfg.N, cfg.K, cfg.group
+    if packed.numel() < (N + 15) // 16 * ((K + 127) // 128) * (1024 + 2048 // group * (4 if cfg.has_zeros else 2)):
+        raise ValueError("packed is smaller than coral_lmhead_q4_packed_bytes(cfg)")
+    _check((_lib or load_library()).coral_lmhead_q4_linear(
+        ctypes.byref(cfg), _op_ptr("packed", packed, torch.uint8, None, dev), _op_ptr("x", x, x.dtype, (M, K), dev),
+        _type_of(x), M, _op_ptr("out", out, out.dtype, (M, N), dev), _type_of(out), _op_stream(stream, dev)),
         "coral_lmhead_q4_linear")
 
 
-def _rows_ptr(name, t, dtype, shape, device):
+def _rows_ptr(name, t, dtype, shape, dev):
     """Pointer and row distance of a matrix whose rows may lie apart (a slice of padded rows)."""
     if t is None:
         return None, 0
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{dev}")
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
     M, V = shape
-    if not t.is_cuda or t.device != device:
-        raise ValueError(f"{name} must be on {device}")
-    if t.dtype != dtype or tuple(t.shape) != (M, V):
-        raise ValueError(f"{name}: expected {dtype} {(M, V)}, got {t.dtype} {tuple(t.shape)}")
+    if t.is_contiguous():
+        return t.data_ptr(), V
     ld = t.stride(0) if M > 1 else V
     if (V > 1 and t.stride(1) != 1) or ld < V:
         raise ValueError(f"{name}: the elements of a row must be contiguous and rows must not overlap")
     return t.data_ptr(), ld
+
+
+def _list_ptrs(name, tokens, offsets, n_seq, dev):
+    """Pointers and length of a flat token list and its offsets; lists that are all empty count as absent."""
+    if tokens is None or offsets is None:
+        if tokens is not offsets:
+            raise ValueError(f"{name}_tokens and {name}_offsets go together")
+        return None, None, 0
+    n = tokens.numel()
+    if n == 0:
+        return None, None, 0
+    return (_op_ptr(name + "_tokens", tokens, torch.int32, (n,), dev),
+            _op_ptr(name + "_offsets", offsets, torch.int64, (n_seq + 1,), dev), n)
+
+
+_LOGITS_SIZE = ctypes.sizeof(coral_lmhead_logits_args)
 
 
 def coral_lmhead_logits_process(logits, *, row_seq=None, prompt_tokens=None, prompt_offsets=None, output_tokens=None,
@@ -524,45 +545,38 @@ def coral_lmhead_logits_process(logits, *, row_seq=None, prompt_tokens=None, pro
     dev = _op_device(logits, "logits")
     if logits.dim() != 2:
         raise ValueError("logits must be [M, V]")
-    M, V = logits.shape
-    i32, i64, f32 = torch.int32, torch.int64, torch.float32
-    n_seq = None
-    for t, more in ((repetition, 0), (frequency, 0), (presence, 0), (prompt_offsets, 1), (output_offsets, 1), (bias_offsets, 1)):
-        if t is not None:
-            n = t.numel() - more
-            if n_seq is not None and n != n_seq:
-                raise ValueError("the sequences' lists and penalties differ in number")
-            n_seq = n
-    n_seq = n_seq or 0                               # no lists and no penalties: no sequences
-    path_len = path_tokens.shape[1] if path_tokens is not None else 0
-    n_masks = mask_words.shape[0] if mask_words is not None else 0
-    k = out_ids.shape[1] if out_ids is not None else 0
+    shape, t = logits.shape, logits.dtype
+    M, V = shape
+    i32, f32 = torch.int32, torch.float32
+    n_seq = 0                                        # no lists and no penalties: no sequences
+    for p in (repetition, frequency, presence):
+        if p is not None:
+            n_seq = p.numel()
+            break
+    else:
+        for o in (prompt_offsets, output_offsets, bias_offsets):
+            if o is not None:
+                n_seq = o.numel() - 1
+                break
+    path_len = 0 if path_tokens is None else path_tokens.shape[1]
+    n_masks = 0 if mask_words is None else mask_words.shape[0]
+    k = 0 if out_ids is None else out_ids.shape[1]
+    in_ptr, ld_in = _rows_ptr("logits", logits, t, shape, dev)
+    out_ptr, ld_out = _rows_ptr("out_logits", out_logits, t, shape, dev)
+    prompt, prompt_off, prompt_n = _list_ptrs("prompt", prompt_tokens, prompt_offsets, n_seq, dev)
+    output, output_off, output_n = _list_ptrs("output", output_tokens, output_offsets, n_seq, dev)
+    bias, bias_off, bias_n = _list_ptrs("bias", bias_tokens, bias_offsets, n_seq, dev)
     a = coral_lmhead_logits_args(
-        struct_size=ctypes.sizeof(coral_lmhead_logits_args), type=_type_of(logits), M=M, V=V, n_seq=n_seq, path_len=path_len,
-        n_masks=n_masks, k_tokens=k, row_seq_dev=_op_ptr("row_seq", row_seq, i32, (M,), dev),
-        path_tokens_dev=_op_ptr("path_tokens", path_tokens, i32, (M, path_len), dev) if path_len else None,
-        repetition_dev=_op_ptr("repetition", repetition, f32, (n_seq,), dev),
-        frequency_dev=_op_ptr("frequency", frequency, f32, (n_seq,), dev),
-        presence_dev=_op_ptr("presence", presence, f32, (n_seq,), dev),
-        mask_words_dev=_op_ptr("mask_words", mask_words, i32, (n_masks, (V + 31) // 32), dev),
-        mask_rows_dev=_op_ptr("mask_rows", mask_rows, i32, (M,), dev), out_ids_dev=_op_ptr("out_ids", out_ids, i32, (M, k), dev),
-        out_logprobs_dev=_op_ptr("out_logprobs", out_logprobs, f32, (M, k), dev), out_lse_dev=_op_ptr("out_lse", out_lse, f32, (M,), dev))
-    a.logits_dev, a.ld_logits = _rows_ptr("logits", logits, logits.dtype, (M, V), dev)
-    a.out_logits_dev, a.ld_out = _rows_ptr("out_logits", out_logits, logits.dtype, (M, V), dev)
-    for name, tokens, offsets in (("prompt", prompt_tokens, prompt_offsets), ("output", output_tokens, output_offsets),
-                                  ("bias", bias_tokens, bias_offsets)):
-        if tokens is None and offsets is None:
-            continue
-        if tokens is None or offsets is None:
-            raise ValueError(f"{name}_tokens and {name}_offsets go together")
-        if tokens.numel() == 0:                      # every list is empty
-            continue
-        setattr(a, f"{name}_tokens_dev", _op_ptr(f"{name}_tokens", tokens, i32, (tokens.numel(),), dev))
-        setattr(a, f"{name}_offsets_dev", _op_ptr(f"{name}_offsets", offsets, i64, (n_seq + 1,), dev))
-        setattr(a, f"{name}_total", tokens.numel())
-        if name == "bias":
-            a.bias_values_dev = _op_ptr("bias_values", bias_values, f32, (tokens.numel(),), dev)
-    _check(load_library().coral_lmhead_logits_process(ctypes.byref(a), _stream_ptr(stream)), "coral_lmhead_logits_process")
+        _LOGITS_SIZE, _type_of(logits), M, V, n_seq, path_len, n_masks, k, ld_in, ld_out, prompt_n, output_n, bias_n, in_ptr,
+        out_ptr, _op_ptr("row_seq", row_seq, i32, (M,), dev), prompt, output,
+        _op_ptr("path_tokens", path_tokens, i32, (M, path_len), dev) if path_len else None, bias, prompt_off, output_off, bias_off,
+        _op_ptr("repetition", repetition, f32, (n_seq,), dev), _op_ptr("frequency", frequency, f32, (n_seq,), dev),
+        _op_ptr("presence", presence, f32, (n_seq,), dev), _op_ptr("bias_values", bias_values, f32, (bias_n,), dev) if bias_n else None,
+        _op_ptr("mask_words", mask_words, i32, (n_masks, (V + 31) // 32), dev), _op_ptr("mask_rows", mask_rows, i32, (M,), dev),
+        _op_ptr("out_ids", out_ids, i32, (M, k), dev), _op_ptr("out_logprobs", out_logprobs, f32, (M, k), dev),
+        _op_ptr("out_lse", out_lse, f32, (M,), dev))
+    _check((_lib or load_library()).coral_lmhead_logits_process(ctypes.byref(a), _op_stream(stream, dev)),
+           "coral_lmhead_logits_process")
 
 
 def coral_lmhead_destroy(handle) -> None:

@@ -197,6 +197,29 @@ def test_long_lists_repeats_and_bad_entries():
     assert torch.equal(*ids)
 
 
+@pytest.mark.parametrize("V,wide", [(400003, False), (200010, True)])
+def test_vocabularies_longer_than_the_table(V, wide):
+    """The token table then covers a row in several passes, built anew for each row."""
+    logits, d = _random(21, 10, V, torch.float32, 3, 400, 300, 4, 30)
+    if wide:
+        d["output"][0] = d["output"][0] + [11] * 33000                      # counts past 15 bits
+    _check(_run(logits, 10, **d), logits, 10, rows=[0, 3, 9], **d)
+
+
+@pytest.mark.parametrize("V", [33333, 32002, 32000])
+def test_tree_nodes_of_a_few_sequences(V):
+    """Rows of one sequence follow one another and differ in their path only; rows without a sequence stand between them."""
+    M = 310
+    logits, d = _random(22, M, V, torch.bfloat16, 5, 300, 200, 6, 25)
+    d["row_seq"] = torch.arange(M, dtype=torch.int32) // 62
+    d["row_seq"][40::41] = -1
+    d["path"][:, 2] = d["path"][:, 1]                                        # a token twice on one path
+    d["path"][1::2, 0] = torch.tensor([d["output"][int(s)][0] if s >= 0 else 0 for s in d["row_seq"][1::2]], dtype=torch.int32)
+    _check(_run(logits, 10, **d), logits, 10, rows=list(range(0, M, 17)) + [40, 41, 42, 61, 62, 63], **d)
+    d["row_seq"] = torch.arange(M, dtype=torch.int32) % 5                    # the sequences in turn
+    _check(_run(logits, 10, **d), logits, 10, rows=range(0, M, 31), **d)
+
+
 @pytest.mark.parametrize("t", TYPES)
 def test_row_distance_alignment_in_place(t):
     """Rows that lie apart and start on any address, outputs aligned otherwise, the columns behind a row left as they were."""

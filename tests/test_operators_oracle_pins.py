@@ -93,7 +93,7 @@ def _largs(**kw):
     dict(output_tokens_dev=P + 2, output_offsets_dev=P), dict(output_tokens_dev=P, output_offsets_dev=P, output_total=1 << 31),
     dict(bias_tokens_dev=P), dict(bias_tokens_dev=P, bias_offsets_dev=P), dict(bias_values_dev=P),
     dict(bias_tokens_dev=P, bias_offsets_dev=P, bias_values_dev=P, bias_total=-1),
-    dict(path_tokens_dev=P), dict(path_len=3), dict(path_len=-1), dict(mask_words_dev=P), dict(mask_rows_dev=P),
+    dict(path_tokens_dev=P), dict(path_len=3), dict(path_len=-1), dict(path_tokens_dev=P, path_len=65), dict(mask_words_dev=P), dict(mask_rows_dev=P),
     dict(mask_words_dev=P, n_masks=1), dict(mask_words_dev=P, n_masks=0, mask_rows_dev=P), dict(logits_dev=P + 2),
     dict(type=1, logits_dev=P + 1), dict(repetition_dev=P + 1), dict(out_lse_dev=P + 2), dict(row_seq_dev=P + 1)])
 def test_logits_refusals(lib, kw):
