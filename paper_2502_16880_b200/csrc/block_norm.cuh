@@ -87,7 +87,7 @@ template <typename T> struct Raw8 {
 #pragma unroll
         for (int i = 0; i < (int)(sizeof(T) / 2); ++i) v[i] = __ldg(q + i);
     }
-    __device__ __forceinline__ void get(float (&f)[8]) const { Elem<T>::load8(reinterpret_cast<const T*>(v), f); }
+    __device__ __forceinline__ V8 get() const { return load8v(reinterpret_cast<const T*>(v)); }
 };
 
 // Staged tensors of one row: x, then r, then (backward) dy, dh, then a full gate; absent ones are not staged.
@@ -114,15 +114,6 @@ struct NormStage {
         }
     }
 };
-
-template <typename T>
-__device__ __forceinline__ void load_weights8(const void* w, int ch, float (&v)[8]) {
-    if (w) Elem<T>::load8(reinterpret_cast<const T*>(w) + (size_t)ch * 8, v);
-    else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 1.f;
-    }
-}
 
 // grid: any; dynamic shared memory: stages * tensors * NV * blockDim * 8 elements.
 template <typename T, int NV>
@@ -156,43 +147,30 @@ __global__ void __launch_bounds__(kNormMaxThreads, NV < 4 ? 2 : 1) block_norm_ke
     const float inv_h = 1.f / (float)H;
     for (size_t row = blockIdx.x; row < (size_t)a.M; row += gridDim.x) {
         cp_async_wait_left(stages - 1);
-        float y[NV][8];                             // first x, then y
-        float sx = 0.f, sy = 0.f;
+        V8 y[NV];                                   // first x, then y
+        float scale = a.gate_mode == 2 ? Elem<T>::up(reinterpret_cast<const T*>(a.gate)[row]) : 1.f;
+        unsigned long long sx = 0, sy = 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (threadIdx.x + i * blockDim.x >= chunks) continue;
-            Elem<T>::load8(st.slot(stage, 0, i), y[i]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sx = fmaf(y[i][j], y[i][j], sx);
+            y[i] = load8v(st.slot(stage, 0, i));
+            sx = dot8v(y[i], y[i], sx);
         }
-        float scale = a.gate_mode == 2 ? Elem<T>::up(reinterpret_cast<const T*>(a.gate)[row]) : 1.f;
-        if (a.w_post) scale *= rsqrtf(fmaf(block_sum(sx, s_sum, turn), inv_h, a.eps));
+        if (a.w_post) {
+            const float2 s = halves(sx);
+            scale *= rsqrtf(fmaf(block_sum(s.x + s.y, s_sum, turn), inv_h, a.eps));
+        }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int ch = threadIdx.x + i * blockDim.x;
             if (ch >= chunks) continue;
-            float f[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[i][j] *= scale;
-            if (a.w_post) {
-                w_post[i].get(f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[i][j] *= f[j];
-            }
-            if (a.gate_mode == 1 || a.gate_mode == 3) {
-                if (a.gate_mode == 1) w_gate[i].get(f);
-                else Elem<T>::load8(st.slot(stage, t_g, i), f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[i][j] *= f[j];
-            }
-            if (t_r >= 0) {
-                Elem<T>::load8(st.slot(stage, t_r, i), f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[i][j] = fmaf(a.alpha, f[j], y[i][j]);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sy = fmaf(y[i][j], y[i][j], sy);
-            if (a.y) Elem<T>::store8(reinterpret_cast<T*>(a.y) + row * H + (size_t)ch * 8, y[i]);
+            if (a.w_post || a.gate_mode == 2) y[i] = y[i] * splat8(scale);
+            if (a.w_post) y[i] = y[i] * w_post[i].get();
+            if (a.gate_mode == 1) y[i] = y[i] * w_gate[i].get();
+            if (a.gate_mode == 3) y[i] = y[i] * load8v(st.slot(stage, t_g, i));
+            if (t_r >= 0) y[i] = fma8(splat8(a.alpha), load8v(st.slot(stage, t_r, i)), y[i]);
+            sy = dot8v(y[i], y[i], sy);
+            if (a.y) store8v(reinterpret_cast<T*>(a.y) + row * H + (size_t)ch * 8, y[i]);
         }
         // this thread's slots of the stage have been read: the row `stages` turns ahead may come in
         const size_t next = row + (size_t)stages * gridDim.x;
@@ -200,16 +178,13 @@ __global__ void __launch_bounds__(kNormMaxThreads, NV < 4 ? 2 : 1) block_norm_ke
         cp_async_commit();
         stage = stage + 1 == stages ? 0 : stage + 1;
         if (!a.h) continue;
-        const float ry = rsqrtf(fmaf(block_sum(sy, s_sum, turn), inv_h, a.eps));
+        const float2 s = halves(sy);
+        const V8 ry = splat8(rsqrtf(fmaf(block_sum(s.x + s.y, s_sum, turn), inv_h, a.eps)));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int ch = threadIdx.x + i * blockDim.x;
             if (ch >= chunks) continue;
-            float f[8];
-            w_pre[i].get(f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[i][j] = y[i][j] * ry * f[j];
-            Elem<T>::store8(reinterpret_cast<T*>(a.h) + row * H + (size_t)ch * 8, y[i]);
+            store8v(reinterpret_cast<T*>(a.h) + row * H + (size_t)ch * 8, y[i] * ry * w_pre[i].get());
         }
     }
 }
@@ -239,129 +214,101 @@ __global__ void __launch_bounds__(kNormMaxThreads) block_norm_backward_kernel(No
         if (row < (size_t)a.M) fetch(s, row);
         cp_async_commit();
     }
-    float acc_pre[NV][8] = {}, acc_post[NV][8] = {}, acc_gate[NV][8] = {};
+    V8 acc_pre[NV] = {}, acc_post[NV] = {}, acc_gate[NV] = {};
+    // weights come from L1 wherever they are used: the column sums take the registers
+    auto weights = [&](const void* w, int i) {
+        Raw8<T> r;
+        r.load(w, threadIdx.x + i * blockDim.x);
+        return r.get();
+    };
     clear_sums(s_sum);
     int turn = 0, stage = 0;
     const float inv_h = 1.f / (float)H;
     for (size_t row = blockIdx.x; row < (size_t)a.M; row += gridDim.x) {
         cp_async_wait_left(stages - 1);
-        float sx = 0.f;
         float rx = 1.f;
         if (a.w_post) {
+            unsigned long long sx = 0;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 if (threadIdx.x + i * blockDim.x >= chunks) continue;
-                float x[8];
-                Elem<T>::load8(st.slot(stage, 0, i), x);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sx = fmaf(x[j], x[j], sx);
+                const V8 x = load8v(st.slot(stage, 0, i));
+                sx = dot8v(x, x, sx);
             }
-            rx = rsqrtf(fmaf(block_sum(sx, s_sum, turn), inv_h, a.eps));
+            const float2 s = halves(sx);
+            rx = rsqrtf(fmaf(block_sum(s.x + s.y, s_sum, turn), inv_h, a.eps));
         }
         const float g_row = a.gate_mode == 2 ? Elem<T>::up(reinterpret_cast<const T*>(a.gate)[row]) : 1.f;
-        auto gate8 = [&](int i, int ch, float (&g)[8]) {
-            if (a.gate_mode == 3) Elem<T>::load8(st.slot(stage, t_g, i), g);
-            else if (a.gate_mode == 1) load_weights8<T>(a.gate, ch, g);
-            else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) g[j] = g_row;
-            }
+        // v times the gate
+        auto gated = [&](const V8& v, int i) {
+            if (a.gate_mode == 1) return v * weights(a.gate, i);
+            if (a.gate_mode == 2) return v * splat8(g_row);
+            if (a.gate_mode == 3) return v * load8v(st.slot(stage, t_g, i));
+            return v;
         };
-        float y[NV][8], b[NV][8];
-        float sy = 0.f, sd = 0.f;                   // sum y^2, sum dh w_pre y
+        V8 y[NV], b[NV];
+        unsigned long long sy = 0, sd = 0;          // sum y^2, sum dh w_pre y
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int ch = threadIdx.x + i * blockDim.x;
-            if (ch >= chunks) continue;
-            float x[8], r[8], g[8], w[8], dh[8];
-            Elem<T>::load8(st.slot(stage, 0, i), x);
-            if (t_r >= 0) Elem<T>::load8(st.slot(stage, t_r, i), r);
-            gate8(i, ch, g);
-            load_weights8<T>(a.w_post, ch, w);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                b[i][j] = x[j] * rx * w[j];
-                y[i][j] = t_r >= 0 ? fmaf(a.alpha, r[j], g[j] * b[i][j]) : g[j] * b[i][j];
-            }
+            if (threadIdx.x + i * blockDim.x >= chunks) continue;
+            b[i] = load8v(st.slot(stage, 0, i));
+            if (a.w_post) b[i] = b[i] * splat8(rx) * weights(a.w_post, i);
+            y[i] = gated(b[i], i);
+            if (t_r >= 0) y[i] = fma8(splat8(a.alpha), load8v(st.slot(stage, t_r, i)), y[i]);
             if (t_dh >= 0) {
-                Elem<T>::load8(st.slot(stage, t_dh, i), dh);
-                load_weights8<T>(a.w_pre, ch, w);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    sy = fmaf(y[i][j], y[i][j], sy);
-                    sd = fmaf(dh[j] * w[j], y[i][j], sd);
-                }
+                sy = dot8v(y[i], y[i], sy);
+                sd = dot8v(load8v(st.slot(stage, t_dh, i)) * weights(a.w_pre, i), y[i], sd);
             }
         }
         float ry = 0.f, mean = 0.f;                 // mean of dh w_pre yh, times ry
         if (t_dh >= 0) {
-            block_sum2(sy, sd, s_sum, turn);
-            ry = rsqrtf(fmaf(sy, inv_h, a.eps));
-            mean = sd * ry * inv_h;
+            const float2 u = halves(sy), v = halves(sd);
+            float s0 = u.x + u.y, s1 = v.x + v.y;
+            block_sum2(s0, s1, s_sum, turn);
+            ry = rsqrtf(fmaf(s0, inv_h, a.eps));
+            mean = s1 * ry * inv_h;
         }
-        float sb = 0.f, sg = 0.f;                   // sum db w_post x, sum dY b
+        unsigned long long sb = 0, sg = 0;          // sum db w_post x, sum dY b
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int ch = threadIdx.x + i * blockDim.x;
             if (ch >= chunks) continue;
-            float d[8] = {}, w[8], g[8];
-            if (t_dy >= 0) Elem<T>::load8(st.slot(stage, t_dy, i), d);
+            V8 d = {};
+            if (t_dy >= 0) d = load8v(st.slot(stage, t_dy, i));
             if (t_dh >= 0) {
-                float dh[8];
-                Elem<T>::load8(st.slot(stage, t_dh, i), dh);
-                load_weights8<T>(a.w_pre, ch, w);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float yh = y[i][j] * ry;
-                    acc_pre[i][j] = fmaf(dh[j], yh, acc_pre[i][j]);
-                    d[j] = fmaf(ry, fmaf(-yh, mean, dh[j] * w[j]), d[j]);
-                }
+                const V8 dh = load8v(st.slot(stage, t_dh, i)), yh = y[i] * splat8(ry);
+                acc_pre[i] = fma8(dh, yh, acc_pre[i]);
+                d = fma8(splat8(ry), fma8(yh, splat8(-mean), dh * weights(a.w_pre, i)), d);
             }
-            if (a.dr) {
-                float o[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = a.alpha * d[j];
-                Elem<T>::store8(reinterpret_cast<T*>(a.dr) + row * H + (size_t)ch * 8, o);
-            }
-            gate8(i, ch, g);
-            if (a.gate_mode == 3 && a.dgate) {
-                float o[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = d[j] * b[i][j];
-                Elem<T>::store8(reinterpret_cast<T*>(a.dgate) + row * H + (size_t)ch * 8, o);
-            }
-            float x[8];
-            Elem<T>::load8(st.slot(stage, 0, i), x);
-            load_weights8<T>(a.w_post, ch, w);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float db = g[j] * d[j];
-                sg = fmaf(d[j], b[i][j], sg);
-                acc_gate[i][j] = fmaf(d[j], b[i][j], acc_gate[i][j]);
-                acc_post[i][j] = fmaf(db, x[j] * rx, acc_post[i][j]);
-                y[i][j] = db * w[j];                // from here on: db w_post
-                sb = fmaf(y[i][j], x[j], sb);
-                b[i][j] = x[j];                     // ... and x
-            }
+            if (a.dr) store8v(reinterpret_cast<T*>(a.dr) + row * H + (size_t)ch * 8, d * splat8(a.alpha));
+            if (a.gate_mode == 1) acc_gate[i] = fma8(d, b[i], acc_gate[i]);
+            else if (a.gate_mode == 2) sg = dot8v(d, b[i], sg);
+            else if (a.gate_mode == 3 && a.dgate) store8v(reinterpret_cast<T*>(a.dgate) + row * H + (size_t)ch * 8, d * b[i]);
+            y[i] = gated(d, i);                     // from here on: db, times w_post if there is one
+            if (a.w_post) {
+                const V8 x = load8v(st.slot(stage, 0, i));
+                acc_post[i] = fma8(y[i], x * splat8(rx), acc_post[i]);
+                y[i] = y[i] * weights(a.w_post, i);
+                sb = dot8v(y[i], x, sb);
+                b[i] = x;                           // ... and x
+            } else store8v(reinterpret_cast<T*>(a.dx) + row * H + (size_t)ch * 8, y[i]);
         }
         const size_t next = row + (size_t)stages * gridDim.x;
         if (next < (size_t)a.M) fetch(stage, next);
         cp_async_commit();
         stage = stage + 1 == stages ? 0 : stage + 1;
-        float back = 0.f;                           // mean of db w_post xh, times rx
-        if (a.w_post || a.gate_mode == 2) {
-            block_sum2(sb, sg, s_sum, turn);
-            if (a.w_post) back = sb * rx * rx * inv_h;
-            if (a.gate_mode == 2 && a.dgate && threadIdx.x == 0) reinterpret_cast<float*>(a.dgate)[row] = sg;
-        }
+        if (!a.w_post && a.gate_mode != 2) continue;
+        const float2 u = halves(sb), v = halves(sg);
+        float s0 = u.x + u.y, s1 = v.x + v.y;
+        block_sum2(s0, s1, s_sum, turn);
+        if (a.gate_mode == 2 && a.dgate && threadIdx.x == 0) reinterpret_cast<float*>(a.dgate)[row] = s1;
+        if (!a.w_post) continue;
+        const V8 back = splat8(-s0 * rx * rx * inv_h);          // minus the mean of db w_post xh, times rx
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int ch = threadIdx.x + i * blockDim.x;
             if (ch >= chunks) continue;
-            float o[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = rx * fmaf(-b[i][j], back, y[i][j]);
-            Elem<T>::store8(reinterpret_cast<T*>(a.dx) + row * H + (size_t)ch * 8, o);
+            store8v(reinterpret_cast<T*>(a.dx) + row * H + (size_t)ch * 8, splat8(rx) * fma8(b[i], back, y[i]));
         }
     }
     float* part = a.part + (size_t)blockIdx.x * 3 * H;
@@ -369,9 +316,9 @@ __global__ void __launch_bounds__(kNormMaxThreads) block_norm_backward_kernel(No
     for (int i = 0; i < NV; ++i) {
         const int ch = threadIdx.x + i * blockDim.x;
         if (ch >= chunks) continue;
-        if (a.want & 1) Elem<float>::store8(part + (size_t)ch * 8, acc_pre[i]);
-        if (a.want & 2) Elem<float>::store8(part + H + (size_t)ch * 8, acc_post[i]);
-        if (a.want & 4) Elem<float>::store8(part + 2 * H + (size_t)ch * 8, acc_gate[i]);
+        if (a.want & 1) store8v(part + (size_t)ch * 8, acc_pre[i]);
+        if (a.want & 2) store8v(part + H + (size_t)ch * 8, acc_post[i]);
+        if (a.want & 4) store8v(part + 2 * H + (size_t)ch * 8, acc_gate[i]);
     }
     pdl_launch_dependents();
 }

