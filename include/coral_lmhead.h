@@ -448,8 +448,9 @@ int coral_lmhead_block_norm_backward(const coral_lmhead_norm_args *args, void *w
  * verify a draft; Section 1 has the target model verify in one pass) and the drafter's projections, which are bound by their
  * weight bytes as the draft head is:
  *   out[m][n] = sum_g scale[n][g] * sum_{k in group g} (q[n][k] - zero[n][g]) * x[m][k]
- * The sum inside a group is over exact operands (an integer and an activation) with fp32 accumulation; the scale multiplies
- * that fp32 sum; groups add up in fp32; one rounding to the output type.
+ * The sum inside a group is over exact operands (an integer and an activation; an activation under 2^-25 of its row's largest
+ * is rounded at 2^-40 of that) with fp32 accumulation; the scale multiplies that fp32 sum; groups add up in fp32; one rounding
+ * to the output type.  A row that holds an infinity or a NaN gives no finite outputs; other rows are not touched by it.
  *
  * coral_lmhead_q4_config: N outputs, K inputs (a multiple of group, at most 65536), group 32, 64 or 128 columns,
  *   scale_type CORAL_TYPE_BF16 or CORAL_TYPE_F16, has_zeros 0 (zero = 8 everywhere) or 1.
@@ -457,10 +458,15 @@ int coral_lmhead_block_norm_backward(const coral_lmhead_norm_args *args, void *w
  * coral_lmhead_q4_pack: Wq_dev [N x K/2] bytes, column 2j in the low and 2j + 1 in the high four bits of byte j, 16-byte
  *   aligned; scales_dev [N x K/group]; zeros_dev [N x K/group] bytes, 0..127, or NULL.  Writes packed_dev (256-byte aligned,
  *   owned by the caller; the inputs may be freed once the call has run on `stream`).
+ * coral_lmhead_q4_workspace_bytes: scratch a call of M rows needs (0 for the fewest rows).
  * coral_lmhead_q4_linear: x_dev [M x K] of x_type (bf16 or fp16), 16-byte aligned; out_dev [M x N] of out_type (fp32, bf16 or
- *   fp16).  M >= 1; the weights are read once per pass over the rows.  A call holds nothing between calls, so any number may
- *   run at once on one packed copy.
- * Asynchronous on `stream`; no allocation.  CORAL_ERR_INVALID for a bad configuration, NULL or misaligned pointers, M < 1.
+ *   fp16).  M >= 1; the weights are read once per pass of 64 rows (of 16 for what is left, if that is no more).
+ *   workspace_dev: 256-byte aligned, at least that size (NULL if 0), holds nothing between calls; calls that may overlap on
+ *   the GPU need one each, the packed copy they can share.
+ * coral_lmhead_q4_status: synchronises `stream` and returns the status word of the last call that used the workspace (0 or
+ *   CORAL_ERR_TIMEOUT; 0 for NULL).
+ * Asynchronous on `stream` but for the last; no allocation.  CORAL_ERR_INVALID for a bad configuration, NULL or misaligned
+ * pointers, M < 1.
  */
 typedef struct coral_lmhead_q4_config {
     uint32_t struct_size;          /* sizeof(coral_lmhead_q4_config) */
@@ -470,8 +476,10 @@ typedef struct coral_lmhead_q4_config {
 int coral_lmhead_q4_packed_bytes(const coral_lmhead_q4_config *cfg, size_t *bytes);
 int coral_lmhead_q4_pack(const coral_lmhead_q4_config *cfg, const void *Wq_dev, const void *scales_dev, const void *zeros_dev,
                          void *packed_dev, void *stream);
+int coral_lmhead_q4_workspace_bytes(const coral_lmhead_q4_config *cfg, int M, size_t *bytes);
 int coral_lmhead_q4_linear(const coral_lmhead_q4_config *cfg, const void *packed_dev, const void *x_dev, int x_type, int M,
-                           void *out_dev, int out_type, void *stream);
+                           void *out_dev, int out_type, void *workspace_dev, void *stream);
+int coral_lmhead_q4_status(const void *workspace_dev, void *stream);
 
 /*
  * Penalties for repeated tokens, biases and grammar masks on dense logits, with the candidates of the result in the same

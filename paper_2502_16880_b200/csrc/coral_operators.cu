@@ -7,6 +7,7 @@
 #include "launch.cuh"
 #include "logits.cuh"
 #include "q4.cuh"
+#include "q4_tc.cuh"
 
 using namespace coral;
 
@@ -165,38 +166,111 @@ int q4_split(int T, int KB, int sms) {
     return best;
 }
 
-template <typename TX, int NT, int PER, bool ZEROS>
-int launch_q4(const Q4View& q, const void* x, int M, void* out, int out_type, int sms, cudaStream_t st) {
+// The passes over the rows of a call: up to 64 rows each on the tensor cores while more than 16 are left (two thirds of the time
+// of two passes of 16 at 17 rows, a fifth of four at 60: @@TC@@), then up to 16 on the warps' MMA, fewer where very long rows do
+// not fit shared memory.  Rows that a block would spend long on scaling are laid out first, in the caller's workspace.
+constexpr int kQ4StageUnits = 1024;              // 8-column pieces that a block of the product scales itself
+
+struct Q4Pass {
+    int first, rows, slab_rows;                  // slab_rows: 32 or 64 on the tensor cores, else 0
+    bool staged;
+    size_t at, back_bytes, sum_bytes, bytes;     // its part of the workspace
+};
+
+int q4_row_limit(int KB, int per) {
+    const size_t row = (size_t)KB * 256 + 64, red = (size_t)2 * kQ4Warps * 16 * 8 * sizeof(float);
+    auto fit = [&](int nt) {
+        const size_t fixed = nt * red + (size_t)KB * per * 8 * nt * sizeof(float) + 1024;
+        const size_t n = fixed < kQ4MaxSmem ? (kQ4MaxSmem - fixed) / row : 0;
+        return n < (size_t)8 * nt ? (int)n : 8 * nt;
+    };
+    const int one = fit(1), two = fit(2);
+    return two > one ? two : one;
+}
+
+// Pass `i` of a call, in order; false behind the last.  `at` is where the workspace part of the next pass starts.
+bool q4_next_pass(const coral_lmhead_q4_config& c, int KB, int M, int* first, size_t* at, Q4Pass* p) {
+    const int left = M - *first, per = 128 / c.group;
+    if (left < 1) return false;
+    *p = Q4Pass{};
+    p->first = *first;
+    auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+    if (left > kQ4PassRows) {
+        p->rows = left < kQ4TcMaxRows ? left : kQ4TcMaxRows;
+        p->slab_rows = p->rows <= 32 ? 32 : 64;
+        p->staged = true;
+        p->back_bytes = up(p->slab_rows * 4);
+        p->bytes = p->back_bytes + up((size_t)((c.K + 63) / 64) * p->slab_rows * 128);
+    } else {
+        const int limit = q4_row_limit(KB, per);
+        p->rows = left < limit ? left : limit;
+        p->staged = p->rows * KB * 16 > kQ4StageUnits;
+        if (p->staged) {
+            p->back_bytes = up(p->rows * 4);
+            p->sum_bytes = up((size_t)p->rows * KB * per * 4);
+            p->bytes = p->back_bytes + p->sum_bytes + up((size_t)p->rows * KB * 256);
+        }
+    }
+    if (p->bytes && *at == 0) *at = 256;         // the status word comes first
+    p->at = *at;
+    *at += p->bytes;
+    *first += p->rows;
+    return true;
+}
+
+template <typename TX, int PER, bool ZEROS>
+int launch_q4_pass(const Q4View& q, const Q4Pass& p, const void* x_all, void* out_all, int out_type, unsigned char* ws, bool first,
+                   int sms, cudaStream_t st) {
+    const TX* x = static_cast<const TX*>(x_all) + (size_t)p.first * q.K;
+    void* out = static_cast<unsigned char*>(out_all) + (size_t)p.first * q.N * elem_size(out_type);
+    Q4Staged s{};
+    if (p.staged) {
+        s.status = first ? reinterpret_cast<int*>(ws) : nullptr;
+        s.back = reinterpret_cast<float*>(ws + p.at);
+        s.sums = reinterpret_cast<float*>(ws + p.at + p.back_bytes);
+        s.x = reinterpret_cast<uint4*>(ws + p.at + p.back_bytes + p.sum_bytes);
+        q4_stage_kernel<TX, PER><<<p.slab_rows ? p.slab_rows : p.rows, 256, 0, st>>>(x, p.rows, q.K, q.KB, p.slab_rows, s);
+        if (cudaGetLastError() != cudaSuccess) return CORAL_ERR_CUDA;
+    }
+    if (p.slab_rows) {
+        const int grid = q.T < sms ? q.T : sms;
+        DeviceState* state = reinterpret_cast<DeviceState*>(ws);
+        auto run = [&](auto kernel, size_t smem) {
+            return allow_smem(kernel, smem) && launch_pdl(kernel, dim3(grid), dim3(kQ4TcThreads), smem, st, q, s, p.rows, out, out_type,
+                                                          state) == cudaSuccess;
+        };
+        const bool ok = p.slab_rows == 32 ? run(q4_tc_kernel<32, PER, ZEROS>, q4_tc_smem_bytes<32>())
+                                          : run(q4_tc_kernel<64, PER, ZEROS>, q4_tc_smem_bytes<64>());
+        return ok ? CORAL_OK : CORAL_ERR_CUDA;
+    }
     const int split = q4_split(q.T, q.KB, sms);
     const long long units = (long long)q.T * split;              // warps that have a tile to work on
     int warps = kQ4Warps;
     while (warps > split && warps > 4 && units < (long long)sms * warps) warps /= 2;
-    const long long teams = warps / split;
-    const long long blocks = (q.T + teams - 1) / teams;
-    const size_t smem = (size_t)M * (q.KB * 256 + 64) + (size_t)2 * warps * 16 * 8 * NT * sizeof(float);
-    auto kernel = q4_rows_kernel<TX, NT, PER, ZEROS>;
-    if (!allow_smem(kernel, smem)) return CORAL_ERR_CUDA;
-    kernel<<<(int)(blocks < sms ? blocks : sms), warps * 32, smem, st>>>(q, static_cast<const TX*>(x), M, out, out_type, split);
-    return cudaGetLastError() == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+    const long long teams = warps / split, blocks = (q.T + teams - 1) / teams;
+    const int nt = p.rows <= 8 ? 1 : 2;
+    const size_t smem = (size_t)p.rows * (q.KB * 256 + 64) + (size_t)q.KB * PER * 8 * nt * sizeof(float) +
+                        (size_t)2 * warps * 16 * 8 * nt * sizeof(float);
+    auto run = [&](auto kernel) {
+        return allow_smem(kernel, smem) && launch_pdl(kernel, dim3((unsigned)(blocks < sms ? blocks : sms)), dim3(warps * 32), smem, st, q, x,
+                                                      s, p.rows, out, out_type, split) == cudaSuccess;
+    };
+    return (nt == 1 ? run(q4_rows_kernel<TX, 1, PER, ZEROS>) : run(q4_rows_kernel<TX, 2, PER, ZEROS>)) ? CORAL_OK : CORAL_ERR_CUDA;
 }
 
-template <typename TX, int NT, int PER>
-int launch_q4_zeros(const Q4View& q, bool zeros, const void* x, int M, void* out, int out_type, int sms, cudaStream_t st) {
-    return zeros ? launch_q4<TX, NT, PER, true>(q, x, M, out, out_type, sms, st)
-                 : launch_q4<TX, NT, PER, false>(q, x, M, out, out_type, sms, st);
-}
-
-template <typename TX, int NT>
-int launch_q4_group(const Q4View& q, int group, bool zeros, const void* x, int M, void* out, int out_type, int sms, cudaStream_t st) {
-    if (group == 128) return launch_q4_zeros<TX, NT, 1>(q, zeros, x, M, out, out_type, sms, st);
-    if (group == 64) return launch_q4_zeros<TX, NT, 2>(q, zeros, x, M, out, out_type, sms, st);
-    return launch_q4_zeros<TX, NT, 4>(q, zeros, x, M, out, out_type, sms, st);
+template <typename TX, int PER>
+int launch_q4_zeros(const coral_lmhead_q4_config& c, const Q4View& q, const Q4Pass& p, const void* x, void* out, int out_type,
+                    unsigned char* ws, bool first, int sms, cudaStream_t st) {
+    return c.has_zeros ? launch_q4_pass<TX, PER, true>(q, p, x, out, out_type, ws, first, sms, st)
+                       : launch_q4_pass<TX, PER, false>(q, p, x, out, out_type, ws, first, sms, st);
 }
 
 template <typename TX>
-int launch_q4_rows(const Q4View& q, int group, bool zeros, const void* x, int M, void* out, int out_type, int sms, cudaStream_t st) {
-    return M <= 8 ? launch_q4_group<TX, 1>(q, group, zeros, x, M, out, out_type, sms, st)
-                  : launch_q4_group<TX, 2>(q, group, zeros, x, M, out, out_type, sms, st);
+int launch_q4(const coral_lmhead_q4_config& c, const Q4View& q, const Q4Pass& p, const void* x, void* out, int out_type,
+              unsigned char* ws, bool first, int sms, cudaStream_t st) {
+    if (c.group == 128) return launch_q4_zeros<TX, 1>(c, q, p, x, out, out_type, ws, first, sms, st);
+    if (c.group == 64) return launch_q4_zeros<TX, 2>(c, q, p, x, out, out_type, ws, first, sms, st);
+    return launch_q4_zeros<TX, 4>(c, q, p, x, out, out_type, ws, first, sms, st);
 }
 
 // ---- logits ----------------------------------------------------------------------------------------------------
@@ -312,12 +386,26 @@ int coral_lmhead_q4_pack(const coral_lmhead_q4_config* cfg, const void* Wq_dev, 
     return cudaGetLastError() == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
 }
 
+int coral_lmhead_q4_workspace_bytes(const coral_lmhead_q4_config* cfg, int M, size_t* bytes) {
+    if (!q4_config_ok(cfg) || !bytes || M < 1) return CORAL_ERR_INVALID;
+    const int KB = q4_layout(*cfg).KB;
+    int first = 0;
+    size_t at = 0;
+    for (Q4Pass p; q4_next_pass(*cfg, KB, M, &first, &at, &p);) {}
+    *bytes = at;
+    return CORAL_OK;
+}
+
 int coral_lmhead_q4_linear(const coral_lmhead_q4_config* cfg, const void* packed_dev, const void* x_dev, int x_type, int M,
-                           void* out_dev, int out_type, void* stream) {
+                           void* out_dev, int out_type, void* workspace_dev, void* stream) {
     if (!q4_config_ok(cfg) || !packed_dev || !x_dev || !out_dev || M < 1) return CORAL_ERR_INVALID;
     if (x_type != CORAL_TYPE_BF16 && x_type != CORAL_TYPE_F16) return CORAL_ERR_INVALID;
     if (out_type != CORAL_TYPE_F32 && out_type != CORAL_TYPE_BF16 && out_type != CORAL_TYPE_F16) return CORAL_ERR_INVALID;
-    if (!aligned(packed_dev, 256) || !aligned(x_dev, 16) || !aligned(out_dev, elem_size(out_type))) return CORAL_ERR_INVALID;
+    if (!aligned(packed_dev, 256) || !aligned(x_dev, 16) || !aligned(out_dev, elem_size(out_type)) || !aligned(workspace_dev, 256))
+        return CORAL_ERR_INVALID;
+    size_t bytes = 0;
+    coral_lmhead_q4_workspace_bytes(cfg, M, &bytes);
+    if (bytes && !workspace_dev) return CORAL_ERR_INVALID;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int sms = 0;
     if (!device_sms(&sms)) return CORAL_ERR_CUDA;
@@ -327,20 +415,25 @@ int coral_lmhead_q4_linear(const coral_lmhead_q4_config* cfg, const void* packed
     q.sz = static_cast<const unsigned char*>(packed_dev) + L.weights;
     q.N = cfg->N; q.K = cfg->K; q.KB = L.KB; q.T = L.T;
     q.scale_half = cfg->scale_type == CORAL_TYPE_F16;
-    // rows of x that fit shared memory beside the two buffers of partial sums
-    const size_t fixed = (size_t)2 * kQ4Warps * 16 * kQ4PassRows * sizeof(float);
-    int rows = (int)((kQ4MaxSmem - fixed) / (L.KB * 256 + 64));
-    rows = rows > kQ4PassRows ? kQ4PassRows : rows;
-    for (int m = 0; m < M; m += rows) {
-        const int n = M - m < rows ? M - m : rows;
-        const void* x = static_cast<const unsigned char*>(x_dev) + (size_t)m * cfg->K * 2;
-        void* o = static_cast<unsigned char*>(out_dev) + (size_t)m * cfg->N * elem_size(out_type);
-        const int rc = x_type == CORAL_TYPE_BF16
-                           ? launch_q4_rows<__nv_bfloat16>(q, cfg->group, cfg->has_zeros != 0, x, n, o, out_type, sms, st)
-                           : launch_q4_rows<__half>(q, cfg->group, cfg->has_zeros != 0, x, n, o, out_type, sms, st);
+    unsigned char* ws = static_cast<unsigned char*>(workspace_dev);
+    int first = 0;
+    size_t at = 0;
+    bool fresh = true;
+    for (Q4Pass p; q4_next_pass(*cfg, L.KB, M, &first, &at, &p);) {
+        const int rc = x_type == CORAL_TYPE_BF16 ? launch_q4<__nv_bfloat16>(*cfg, q, p, x_dev, out_dev, out_type, ws, fresh && p.staged, sms, st)
+                                                 : launch_q4<__half>(*cfg, q, p, x_dev, out_dev, out_type, ws, fresh && p.staged, sms, st);
         if (rc != CORAL_OK) return rc;
+        if (p.staged) fresh = false;
     }
     return CORAL_OK;
+}
+
+int coral_lmhead_q4_status(const void* workspace_dev, void* stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int status = CORAL_OK;
+    if (workspace_dev && cudaMemcpyAsync(&status, workspace_dev, sizeof status, cudaMemcpyDeviceToHost, st) != cudaSuccess) return CORAL_ERR_CUDA;
+    if (cudaStreamSynchronize(st) != cudaSuccess) return CORAL_ERR_CUDA;
+    return status;
 }
 
 int coral_lmhead_block_norm(const coral_lmhead_norm_args* a, void* stream) {

@@ -21,6 +21,7 @@
 // owns the contiguous run [b*per, (b+1)*per), so all CTAs stream the same bytes.
 #pragma once
 #include "common.cuh"
+#include "mbarrier.cuh"
 
 namespace coral {
 
@@ -33,8 +34,6 @@ constexpr int kStreamSegTab = 64;               // capacity of the per-CTA segme
 constexpr int kStreamPassRows = 16;             // hidden rows per pass (two n-tiles of 8)
 constexpr int kStreamMaxH = 4096;               // 16 k-blocks of 32 columns per warp
 constexpr int kStreamMaxM = 128;                // beyond this the pass count makes the path pointless
-constexpr int kStreamSpin = 1 << 20;            // bound of every mbarrier wait
-constexpr int kStreamSpinAfterAbort = 1 << 8;
 
 struct StreamGeom {
     int grid;         // CTAs launched
@@ -56,48 +55,6 @@ struct StreamPartials {
     float* pval;      // [...][k_tokens]
     int32_t* pid;
 };
-
-// ---- mbarrier / bulk-copy primitives (shared::cta addresses as 32-bit) ----
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-// Bounded wait.  On expiry the device status word is set, the CTA-wide abort
-// flag raised, and the caller carries on (all indices stay in bounds; results
-// of the call are then meaningless and the status says so).  After an abort
-// later waits give up quickly so the kernel still ends promptly.
-__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, DeviceState* st) {
-    const int limit = *abort_flag ? kStreamSpinAfterAbort : kStreamSpin;
-    for (int i = 0; i < limit; ++i)
-        if (mbar_try_wait(bar, parity)) return;
-    *abort_flag = 1;
-    set_status(st, -5);
-}
-__device__ __forceinline__ void bulk_g2s_hint(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint64_t policy) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
-                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar), "l"(policy) : "memory");
-}
-__device__ __forceinline__ void bulk_g2s(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
-
 
 __device__ __forceinline__ uint4 lds128(uint32_t addr) {
     uint4 v;

@@ -1,7 +1,11 @@
 // Products of few rows with 4-bit weights and group scales (the dense head and the drafter's projections):
 //   out[m][n] = sum_g s[n][g] * sum_{k in group g} (q[n][k] - z[n][g]) * x[m][k]
-// The sums inside a group run over exact operands: q - z is a small integer, exact in bf16 and fp16, so a warp MMA of
-// integers and activations accumulates in fp32 with no rounded weight, and the scale multiplies the group's fp32 sum.
+// The sums inside a group run over exact operands on the warp's fp16 MMA with fp32 accumulation, no weight is ever rounded:
+// four bits under a mask are a subnormal fp16 number, q 2^-24, so a word becomes operands with five instructions (q under the
+// upper mask is 16 times that, which the activations of those columns make good).  What the group's sum then has too much,
+// zero point times the sum of the activations, is taken off in fp32 before the scale multiplies it.  Activations come as fp16
+// numbers too: a row is scaled by a power of two that brings its largest value to 2^14..2^15, so bf16 rows fit as well and a
+// value is exact unless it is 2^-25 times smaller than the row's largest (and then off by 2^-40 of that at most).
 // Few rows are bound by the weight bytes, so a weight is read once, straight into registers in the order the MMA wants
 // (the packed layout below), with several kilobytes a warp in flight.
 //
@@ -11,6 +15,7 @@
 // shift and mask, and the activations are staged in that order.  A group of 32 columns is one word a lane, so every group
 // size that is a multiple of 32 ends on a word.  Scales (and zero points) follow: [tile][block][16 rows][128 / group].
 #pragma once
+#include "block_norm.cuh"                        // cp.async helpers
 #include "element.cuh"
 
 namespace coral {
@@ -66,33 +71,39 @@ __global__ void q4_pack_kernel(const unsigned char* __restrict__ Wq, const uint1
     }
 }
 
-template <typename T> struct Q4Num;
-template <> struct Q4Num<__nv_bfloat16> {
-    static constexpr uint32_t kMagic = 0x43004300u;     // 128 + q, q < 128, is exact
-    static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t z) {
-        uint32_t d;
-        asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(z));
-        return d;
-    }
-    static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    }
-};
-template <> struct Q4Num<__half> {
-    static constexpr uint32_t kMagic = 0x64006400u;     // 1024 + q
-    static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t z) {
-        uint32_t d;
-        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(z));
-        return d;
-    }
-    static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    }
-};
+__device__ __forceinline__ void q4_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// A word's eight weights as four MMA operands: (0,4), 16 (1,5), (2,6), 16 (3,7), in units of 2^-24.
+__device__ __forceinline__ void q4_spread(uint32_t w, uint32_t (&v)[4]) {
+    v[0] = w & 0x000f000fu;
+    v[1] = w & 0x00f000f0u;
+    w >>= 8;
+    v[2] = w & 0x000f000fu;
+    v[3] = w & 0x00f000f0u;
+}
+
+// The power of two that brings the largest absolute value (as bits) to 2^14..2^15; 1 for a row that is not finite.
+__device__ __forceinline__ int q4_exponent(uint32_t max_bits) {
+    if (max_bits >= 0x7f800000u) return 0;
+    const int e = 14 - ((int)(max_bits >> 23) - 127);
+    return e > 100 ? 100 : e < -100 ? -100 : e;
+}
+__device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// Eight scaled activations in the order of q4_spread.
+__device__ __forceinline__ uint4 q4_operand(const float (&f)[8]) {
+    uint4 v;
+    const __half2 h[4] = {__floats2half2_rn(f[0], f[4]), __floats2half2_rn(f[1] * 0.0625f, f[5] * 0.0625f),
+                          __floats2half2_rn(f[2], f[6]), __floats2half2_rn(f[3] * 0.0625f, f[7] * 0.0625f)};
+    v.x = *reinterpret_cast<const uint32_t*>(&h[0]);
+    v.y = *reinterpret_cast<const uint32_t*>(&h[1]);
+    v.z = *reinterpret_cast<const uint32_t*>(&h[2]);
+    v.w = *reinterpret_cast<const uint32_t*>(&h[3]);
+    return v;
+}
 
 // Raw scale entries of one row's block: PER = 128 / group of them, 2 or 4 bytes each, one load.
 template <int PER, bool ZEROS> struct Q4Scales {
@@ -114,23 +125,76 @@ template <int PER, bool ZEROS> struct Q4Scales {
         const uint32_t u = ZEROS ? v[g] & 0xffffu : (v[g >> 1] >> (16 * (g & 1))) & 0xffffu;
         return half ? __half2float(__ushort_as_half((unsigned short)u)) : __uint_as_float(u << 16);
     }
-    __device__ __forceinline__ uint32_t zero(int g) const {            // the zero point in both halves
-        if (!ZEROS) return 0x00080008u;
-        return __byte_perm(v[g], 0, 0x3232);
-    }
+    __device__ __forceinline__ float zero(int g) const { return ZEROS ? (float)(v[g] >> 16) : 8.f; }
 };
 
+// ---- activations ---------------------------------------------------------------------------------------------
+// More than a few rows are scaled and laid out once, by a kernel of their own (a block a row), instead of by every block of the
+// product.  Two layouts: rows (for q4_rows_kernel, with the group sums) and slabs (for the tensor-core kernel: 64 columns of
+// `slab_rows` rows, 128 bytes a row, 16-byte chunks of row r swapped by r % 8 as the 128-byte swizzle has them).
+struct Q4Staged {
+    int* status;                                   // the call's status word, cleared here, or null
+    uint4* x;                                      // rows: [M][KB * 16]; slabs: [ceil(K / 64)][slab_rows][8]
+    float* sums;                                   // rows: [M][KB * PER]
+    float* back;                                   // what undoes a row's scale and the weights' 2^-24
+};
+
+template <typename TX, int PER>
+__global__ void __launch_bounds__(256) q4_stage_kernel(const TX* __restrict__ x, int M, int K, int KB, int slab_rows, Q4Staged st) {
+    __shared__ uint32_t s_max[8];
+    pdl_launch_dependents();
+    const int m = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (st.status && m == 0 && threadIdx.x == 0) *st.status = 0;
+    const int chunks = slab_rows ? (K + 63) / 64 * 8 : KB * 16;
+    const TX* row = x + (size_t)m * K;             // rows from M on are zeros
+    uint32_t top = 0;
+    for (int ch = threadIdx.x; ch * 8 < K && m < M; ch += 256) {
+        float f[8];
+        Elem<TX>::load8(row + ch * 8, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) s_max[warp] = top;
+    __syncthreads();
+    top = s_max[0];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) top = max(top, s_max[w]);
+    const int e2 = q4_exponent(top);
+    const float scale = exp2_int(e2);
+    if (threadIdx.x == 0) st.back[m] = exp2_int(24 - e2);
+    for (int c0 = 0; c0 < chunks; c0 += 256) {
+        const int ch = c0 + threadIdx.x;
+        float f[8] = {}, sum = 0.f;
+        if (ch * 8 < K && m < M) Elem<TX>::load8(row + ch * 8, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { f[e] *= scale; sum += f[e]; }
+        if (slab_rows) {
+            if (ch < chunks) st.x[((size_t)(ch >> 3) * slab_rows + m) * 8 + ((ch & 7) ^ (m & 7))] = q4_operand(f);
+            continue;
+        }
+        if (ch < chunks) st.x[(size_t)m * chunks + ch] = q4_operand(f);
+#pragma unroll
+        for (int o = 1; o < 16 / PER; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (ch < chunks && (ch & (16 / PER - 1)) == 0) st.sums[(size_t)m * KB * PER + ch / (16 / PER)] = sum * 0x1p-24f;
+    }
+}
+
 // grid: any number of blocks of `warps` warps; `split` warps (a power of two dividing warps) share a tile's columns.
-// dynamic shared memory: M rows of x (KB * 256 + 64 bytes each), then 2 * warps * 16 * 8 NT floats.
+// dynamic shared memory: M rows of x (KB * 256 + 64 bytes each), group sums [KB * PER][8 NT], then 2 * warps * 16 * 8 NT floats.
 // Rows of x are padded to 64 bytes past a multiple of 128, so the eight rows of a quarter warp's 16-byte loads fall on
-// different banks.
+// different banks.  x is read from `st` if it has been laid out there, else each block scales and lays out the few rows itself.
 template <typename TX, int NT, int PER, bool ZEROS>
-__global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const TX* __restrict__ x, int M, void* __restrict__ out, int out_type, int split) {
+__global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const TX* __restrict__ x, Q4Staged st, int M, void* __restrict__ out, int out_type, int split) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
+    constexpr int kCols = 8 * NT;
+    __shared__ uint32_t s_max[kCols];
+    __shared__ float s_back[kCols];                // what undoes the row's scale and the weights' 2^-24
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int xrow = q.KB * 256 + 64;
+    const int xrow = q.KB * 256 + 64, groups = q.KB * PER;
     unsigned char* xs = smem_raw;
-    float* red = reinterpret_cast<float*>(smem_raw + (size_t)M * xrow);
+    float* xsum = reinterpret_cast<float*>(smem_raw + (size_t)M * xrow);
+    float* red = xsum + (size_t)groups * kCols;
     const int lane_in = warp % split, team = warp / split, teams = warps / split;
 
     // this warp's stream of (tile, block): tiles tile0, tile0 + step, ..., blocks lane_in, lane_in + split, ...
@@ -142,44 +206,77 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
 
     uint4 w[kQ4Depth][2];
     Q4Scales<PER, ZEROS> sc[kQ4Depth][2];
-    int f_tile = tile0, f_b = lane_in, f_i = 0;
-    long long f_at = 0;
+    int f_b = lane_in, f_tiles = tiles;
+    size_t f_blk = (size_t)tile0 * q.KB + lane_in;             // block of the next fetch, counted over all tiles
+    const size_t f_wrap = (size_t)step * q.KB - (size_t)(nb - 1) * split;
+    const uint4* const w_lane = q.w + lane;
+    const unsigned char* const sz_lane = q.sz + (lane >> 2) * kSz;
     auto fetch = [&](int d) {
-        if (f_at < total && f_b < q.KB) {
-            const size_t blk = (size_t)f_tile * q.KB + f_b;
-            const uint4* p = q.w + blk * 64 + lane;
+        if (f_tiles > 0 && f_b < q.KB) {
+            const uint4* p = w_lane + f_blk * 64;
             w[d][0] = __ldcs(p);
             w[d][1] = __ldcs(p + 32);
-            const unsigned char* s = q.sz + (blk * 16 + (lane >> 2)) * kSz;
+            const unsigned char* s = sz_lane + f_blk * (16 * kSz);
             sc[d][0].load(s);
             sc[d][1].load(s + 8 * kSz);
         }
-        ++f_at;
-        f_b += split;
-        if (++f_i == nb) { f_i = 0; f_b = lane_in; f_tile += step; }
+        if (f_b + split < nb * split) { f_b += split; f_blk += split; }
+        else { f_b = lane_in; f_blk += f_wrap; --f_tiles; }
     };
 #pragma unroll
     for (int d = 0; d < kQ4Depth; ++d) fetch(d);
 
-    // x in the MMA's order, 8 columns (16 bytes) at a time: 0 4 1 5 2 6 3 7; zero past K
-    for (int i = threadIdx.x; i < M * q.KB * 16; i += blockDim.x) {
-        const int m = i / (q.KB * 16), ch = i - m * (q.KB * 16);
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (ch * 8 < q.K) v = __ldg(reinterpret_cast<const uint4*>(x + (size_t)m * q.K) + ch);
-        *reinterpret_cast<uint4*>(xs + (size_t)m * xrow + ch * 16) =
-            make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410),
-                       __byte_perm(v.y, v.w, 0x7632));
+    const int units = q.KB * 16, all = M * units;
+    if (st.x) {
+        pdl_wait();                                // the kernel that lays x out; the weights above do not come from it
+        for (int m = 0; m < M; ++m)
+            for (int ch = threadIdx.x; ch < units; ch += blockDim.x)
+                cp_async16(xs + (size_t)m * xrow + ch * 16, st.x + (size_t)m * units + ch);
+        cp_async_commit();
+        for (int i = threadIdx.x; i < groups * kCols; i += blockDim.x) {
+            const int m = i % kCols;
+            xsum[i] = m < M ? st.sums[(size_t)m * groups + i / kCols] : 0.f;
+        }
+        if (threadIdx.x < M) s_back[threadIdx.x] = st.back[threadIdx.x];
+        cp_async_wait<0>();
+    } else {
+        // x, scaled, in the MMA's order, and its sums over the groups (16 neighbouring lanes hold 128 columns)
+        if (threadIdx.x < kCols) s_max[threadIdx.x] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < all; i += blockDim.x) {
+            const int m = i / units, ch = i - m * units;
+            if (ch * 8 >= q.K) continue;
+            float f[8];
+            Elem<TX>::load8(x + (size_t)m * q.K + ch * 8, f);
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7fffffffu);
+            if (top > s_max[m]) atomicMax(&s_max[m], top);
+        }
+        __syncthreads();
+        if (threadIdx.x < M) s_back[threadIdx.x] = exp2_int(24 - q4_exponent(s_max[threadIdx.x]));
+        for (int i0 = 0; i0 < all; i0 += blockDim.x) {
+            const int i = i0 + threadIdx.x, m = i < all ? i / units : 0, ch = i - m * units;
+            float f[8] = {}, sum = 0.f;
+            if (i < all) {
+                if (ch * 8 < q.K) Elem<TX>::load8(x + (size_t)m * q.K + ch * 8, f);
+                const float scale = exp2_int(q4_exponent(s_max[m]));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { f[e] *= scale; sum += f[e]; }
+                *reinterpret_cast<uint4*>(xs + (size_t)m * xrow + ch * 16) = q4_operand(f);
+            }
+#pragma unroll
+            for (int o = 1; o < 16 / PER; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (i < all && (ch & (16 / PER - 1)) == 0) xsum[ch / (16 / PER) * kCols + m] = sum * 0x1p-24f;
+        }
     }
     __syncthreads();
 
-    const int n_row = lane >> 2;
+    // columns of the result past M are never written: their lanes read row M - 1 (and sums nobody set)
     const unsigned char* xl[NT];
-    bool live[NT];
+    const float2* const sl = reinterpret_cast<const float2*>(xsum) + (lane & 3);
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        live[j] = 8 * j + n_row < M;
-        xl[j] = xs + (size_t)(live[j] ? 8 * j + n_row : 0) * xrow + (lane & 3) * 16;
-    }
+    for (int j = 0; j < NT; ++j) xl[j] = xs + (size_t)min(8 * j + (lane >> 2), M - 1) * xrow + (lane & 3) * 16;
     float acc[NT][4] = {};
     int b = lane_in, at = 0, turn = 0, tile = tile0;
     for (long long base = 0; base < total; base += kQ4Depth) {
@@ -200,28 +297,26 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
                     }
                     const uint32_t lo = i == 0 ? w[d][0].x : i == 1 ? w[d][0].y : i == 2 ? w[d][0].z : w[d][0].w;
                     const uint32_t hi = i == 0 ? w[d][1].x : i == 1 ? w[d][1].y : i == 2 ? w[d][1].z : w[d][1].w;
-                    const uint32_t zl = Q4Num<TX>::kMagic | sc[d][0].zero(g), zh = Q4Num<TX>::kMagic | sc[d][1].zero(g);
-                    uint32_t a[2][4];
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        a[p >> 1][(p & 1) * 2] = Q4Num<TX>::sub(((lo >> (4 * p)) & 0x000f000fu) | Q4Num<TX>::kMagic, zl);
-                        a[p >> 1][(p & 1) * 2 + 1] = Q4Num<TX>::sub(((hi >> (4 * p)) & 0x000f000fu) | Q4Num<TX>::kMagic, zh);
-                    }
+                    uint32_t l[4], h[4];
+                    q4_spread(lo, l);
+                    q4_spread(hi, h);
+                    const uint32_t a0[4] = {l[0], h[0], l[1], h[1]}, a1[4] = {l[2], h[2], l[3], h[3]};
 #pragma unroll
                     for (int j = 0; j < NT; ++j) {
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (live[j]) v = *reinterpret_cast<const uint4*>(xl[j] + b * 256 + i * 64);
-                        Q4Num<TX>::mma(part[j], a[0], v.x, v.y);
-                        Q4Num<TX>::mma(part[j], a[1], v.z, v.w);
+                        const uint4 v = *reinterpret_cast<const uint4*>(xl[j] + b * 256 + i * 64);
+                        q4_mma(part[j], a0, v.x, v.y);
+                        q4_mma(part[j], a1, v.z, v.w);
                     }
                     if (i % kChunks == kChunks - 1) {
                         const float s0 = sc[d][0].scale(g, q.scale_half), s1 = sc[d][1].scale(g, q.scale_half);
+                        const float z0 = -sc[d][0].zero(g), z1 = -sc[d][1].zero(g);
 #pragma unroll
                         for (int j = 0; j < NT; ++j) {
-                            acc[j][0] = fmaf(s0, part[j][0], acc[j][0]);
-                            acc[j][1] = fmaf(s0, part[j][1], acc[j][1]);
-                            acc[j][2] = fmaf(s1, part[j][2], acc[j][2]);
-                            acc[j][3] = fmaf(s1, part[j][3], acc[j][3]);
+                            const float2 u = sl[(b * PER + g) * (kCols / 2) + 4 * j];
+                            acc[j][0] = fmaf(s0, fmaf(z0, u.x, part[j][0]), acc[j][0]);
+                            acc[j][1] = fmaf(s0, fmaf(z0, u.y, part[j][1]), acc[j][1]);
+                            acc[j][2] = fmaf(s1, fmaf(z1, u.x, part[j][2]), acc[j][2]);
+                            acc[j][3] = fmaf(s1, fmaf(z1, u.y, part[j][3]), acc[j][3]);
                         }
                     }
                 }
@@ -232,7 +327,6 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
             // the tile is complete: join the team's parts and write 16 outputs of each row
             at = 0;
             b = lane_in;
-            constexpr int kCols = 8 * NT;
             float* mine = red + ((size_t)turn * warps + warp) * 16 * kCols;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
@@ -251,7 +345,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
                 float s = 0.f;
                 for (int p = 0; p < split; ++p) s += first[(size_t)p * 16 * kCols + e];
                 const long long n = (long long)tile * 16 + (e & 15);
-                if (n < q.N) store_as(out, (size_t)(e >> 4) * q.N + n, s, out_type);
+                if (n < q.N) store_as(out, (size_t)(e >> 4) * q.N + n, s * s_back[e >> 4], out_type);
             }
             turn ^= 1;
             tile += step;

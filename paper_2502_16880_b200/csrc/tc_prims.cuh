@@ -5,7 +5,7 @@
 #include <cuda.h>
 
 #include "common.cuh"
-#include "head_stream.cuh"   // mbarrier helpers
+#include "mbarrier.cuh"
 
 namespace coral {
 

@@ -106,7 +106,9 @@ _SIGNATURES = {
     "coral_lmhead_block_norm_backward": (_i, [ctypes.POINTER(coral_lmhead_norm_args), _vp, _vp]),
     "coral_lmhead_q4_packed_bytes": (_i, [ctypes.POINTER(coral_lmhead_q4_config), ctypes.POINTER(ctypes.c_size_t)]),
     "coral_lmhead_q4_pack": (_i, [ctypes.POINTER(coral_lmhead_q4_config), _vp, _vp, _vp, _vp, _vp]),
-    "coral_lmhead_q4_linear": (_i, [ctypes.POINTER(coral_lmhead_q4_config), _vp, _vp, _i, _i, _vp, _i, _vp]),
+    "coral_lmhead_q4_workspace_bytes": (_i, [ctypes.POINTER(coral_lmhead_q4_config), _i, ctypes.POINTER(ctypes.c_size_t)]),
+    "coral_lmhead_q4_linear": (_i, [ctypes.POINTER(coral_lmhead_q4_config), _vp, _vp, _i, _i, _vp, _i, _vp, _vp]),
+    "coral_lmhead_q4_status": (_i, [_vp, _vp]),
     "coral_lmhead_logits_process": (_i, [ctypes.POINTER(coral_lmhead_logits_args), _vp]),
     "coral_lmhead_error_string": (ctypes.c_char_p, [_i]),
     "coral_lmhead_destroy": (_i, [_vp]),
@@ -490,16 +492,31 @@ def coral_lmhead_q4_pack(cfg, Wq, scales, zeros, packed, stream=None) -> None:
         "coral_lmhead_q4_pack")
 
 
-def coral_lmhead_q4_linear(cfg, packed, x, out, stream=None) -> None:
-    """out [M, N] (fp32, bf16 or fp16) = x [M, K] (bf16 or fp16) times the packed weights' transpose."""
+def coral_lmhead_q4_workspace_bytes(cfg, M: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check((_lib or load_library()).coral_lmhead_q4_workspace_bytes(ctypes.byref(cfg), M, ctypes.byref(b)),
+           "coral_lmhead_q4_workspace_bytes")
+    return b.value
+
+
+def coral_lmhead_q4_linear(cfg, packed, x, out, workspace=None, stream=None) -> None:
+    """out [M, N] (fp32, bf16 or fp16) = x [M, K] (bf16 or fp16) times the packed weights' transpose.  workspace: CUDA uint8
+    tensor of coral_lmhead_q4_workspace_bytes(cfg, M), None if that is 0."""
     dev = _op_device(x, "x")
     M, N, K, group = x.shape[0], cfg.N, cfg.K, cfg.group
     if packed.numel() < (N + 15) // 16 * ((K + 127) // 128) * (1024 + 2048 // group * (4 if cfg.has_zeros else 2)):
         raise ValueError("packed is smaller than coral_lmhead_q4_packed_bytes(cfg)")
+    if workspace is not None and workspace.numel() < coral_lmhead_q4_workspace_bytes(cfg, M):
+        raise ValueError("workspace is smaller than coral_lmhead_q4_workspace_bytes(cfg, M)")
     _check((_lib or load_library()).coral_lmhead_q4_linear(
         ctypes.byref(cfg), _op_ptr("packed", packed, torch.uint8, None, dev), _op_ptr("x", x, x.dtype, (M, K), dev),
-        _type_of(x), M, _op_ptr("out", out, out.dtype, (M, N), dev), _type_of(out), _op_stream(stream, dev)),
-        "coral_lmhead_q4_linear")
+        _type_of(x), M, _op_ptr("out", out, out.dtype, (M, N), dev), _type_of(out),
+        _op_ptr("workspace", workspace, torch.uint8, None, dev), _op_stream(stream, dev)), "coral_lmhead_q4_linear")
+
+
+def coral_lmhead_q4_status(workspace, stream=None) -> int:
+    """Status word of the last call that used the workspace; waits for the stream."""
+    return int((_lib or load_library()).coral_lmhead_q4_status(None if workspace is None else workspace.data_ptr(), _stream_ptr(stream)))
 
 
 def _rows_ptr(name, t, dtype, shape, dev):
@@ -655,7 +672,14 @@ class Q4Linear:
         coral_lmhead_q4_pack(self.cfg, Wq, scales, zeros, self.packed)
 
     def forward(self, x, out=None, out_dtype=torch.float32, stream=None):
+        """x [M, K] times the weights' transpose; the scratch of a call comes from torch's allocator, call by call, so calls
+        on several streams do not share any."""
+        M = x.shape[0]
         if out is None:
-            out = torch.empty((x.shape[0], self.cfg.N), dtype=out_dtype, device=x.device)
-        coral_lmhead_q4_linear(self.cfg, self.packed, x, out, stream)
+            out = torch.empty((M, self.cfg.N), dtype=out_dtype, device=x.device)
+        n = coral_lmhead_q4_workspace_bytes(self.cfg, M)
+        workspace = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+        coral_lmhead_q4_linear(self.cfg, self.packed, x, out, workspace, stream)
+        if stream is not None and n:
+            workspace.record_stream(stream)
         return out

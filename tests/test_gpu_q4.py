@@ -2,7 +2,9 @@
 
 Tolerance.  u = 2^-24.  Integers and activations are exact operands; one MMA step adds 16 products and the running sum, each
 kept to at least 24 bits below the largest of them, so a step is off by at most 17 u of the sizes it adds and a group of g
-columns by 17 g / 16 u; the groups add K / g roundings, the split of the columns at most 16 more and the scale's product 1.
+columns by 17 g / 16 u.  The sums run over q x and z x apart, whose sizes together are at most (15 + z) / max(|q - z|) times the
+size of (q - z) x a column; a whole group's sizes are added up here as they are ("parts" below).  The activations' own sum adds
+g / 8 + 8 roundings, the groups add K / g, the split of the columns at most 16 more, the zero point and the scale 2.
 Then one rounding to the output type.
 """
 import numpy as np
@@ -31,7 +33,9 @@ def _linear(Wq, scales, z):
 def _check(got, Wq, scales, z, x, group):
     want, size = oor.q4_linear(Wq.numpy(), scales.double().numpy(), None if z is None else z.numpy(), x.double().numpy())
     K = x.shape[1]
-    tol = (17 * group / 16 + K / group + 17) * U * size
+    q = oor.q4_unpack(Wq.numpy()).astype(np.float64) + (8.0 if z is None else np.repeat(z.numpy().astype(np.float64), group, axis=1))
+    parts = np.abs(x.double().numpy()) @ (q * np.repeat(np.abs(scales.double().numpy()), group, axis=1)).T
+    tol = (17 * group / 16 + group / 8 + K / group + 26) * U * parts
     tol = tol + torch.finfo(got.dtype).eps / 2 * (np.abs(want) + tol) + (2.0 ** -25 if got.dtype == torch.float16 else 0)
     off = np.abs(got.double().cpu().numpy() - want)
     assert np.all(off <= tol), float(np.max(off / tol))

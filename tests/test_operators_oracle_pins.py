@@ -55,22 +55,26 @@ def test_q4_bad_configurations(lib, kw):
     vp = ctypes.c_void_p
     assert lib.coral_lmhead_q4_packed_bytes(ctypes.byref(c), ctypes.byref(n)) == lmhead.CORAL_ERR_INVALID
     assert lib.coral_lmhead_q4_pack(ctypes.byref(c), vp(P), vp(P), None, vp(P), None) == lmhead.CORAL_ERR_INVALID
-    assert lib.coral_lmhead_q4_linear(ctypes.byref(c), vp(P), vp(P), 1, 1, vp(P), 0, None) == lmhead.CORAL_ERR_INVALID
+    assert lib.coral_lmhead_q4_linear(ctypes.byref(c), vp(P), vp(P), 1, 1, vp(P), 0, None, None) == lmhead.CORAL_ERR_INVALID
+    assert lib.coral_lmhead_q4_workspace_bytes(ctypes.byref(c), 1, ctypes.byref(n)) == lmhead.CORAL_ERR_INVALID
 
 
 def test_q4_bad_arguments(lib):
     c, vp = _q4(), ctypes.c_void_p
     cz = _q4(has_zeros=1)
-    ok = [P, P, 1, 1, P, 0]
-    for i, bad in [(0, None), (0, P + 128), (1, None), (1, P + 8), (2, 0), (2, 3), (3, 0), (3, -2), (4, None), (4, P + 2), (5, 3), (5, -1)]:
+    ok = [P, P, 1, 1, P, 0, None]
+    for i, bad in [(0, None), (0, P + 128), (1, None), (1, P + 8), (2, 0), (2, 3), (3, 0), (3, -2), (4, None), (4, P + 2), (5, 3), (5, -1), (6, P + 64)]:
         a = list(ok)
         a[i] = bad
-        assert lib.coral_lmhead_q4_linear(ctypes.byref(c), vp(a[0]), vp(a[1]), a[2], a[3], vp(a[4]), a[5], None) == \
+        assert lib.coral_lmhead_q4_linear(ctypes.byref(c), vp(a[0]), vp(a[1]), a[2], a[3], vp(a[4]), a[5], vp(a[6]), None) == \
             lmhead.CORAL_ERR_INVALID, (i, bad)
     for cfg, W, s, z, p in [(c, None, P, None, P), (c, P, None, None, P), (c, P, P, P, P), (cz, P, P, None, P), (c, P, P, None, None),
                             (c, P + 4, P, None, P), (c, P, P + 1, None, P), (c, P, P, None, P + 16)]:
         assert lib.coral_lmhead_q4_pack(ctypes.byref(cfg), vp(W), vp(s), vp(z), vp(p), None) == lmhead.CORAL_ERR_INVALID
-    assert lib.coral_lmhead_q4_linear(None, vp(P), vp(P), 1, 1, vp(P), 0, None) == lmhead.CORAL_ERR_INVALID
+    assert lib.coral_lmhead_q4_linear(None, vp(P), vp(P), 1, 1, vp(P), 0, None, None) == lmhead.CORAL_ERR_INVALID
+    assert lmhead.coral_lmhead_q4_workspace_bytes(c, 1) == 0 and lmhead.coral_lmhead_q4_workspace_bytes(c, 60) > 60 * 256 * 2
+    for M in (17, 64, 1000):                               # a call that needs scratch and gets none
+        assert lib.coral_lmhead_q4_linear(ctypes.byref(c), vp(P), vp(P), 1, M, vp(P), 0, None, None) == lmhead.CORAL_ERR_INVALID
     # sizes: 7 tiles of 16 rows x 2 blocks of 128 columns x (1024 + 16 rows x 2 groups x 2 or 4 bytes)
     assert lmhead.coral_lmhead_q4_packed_bytes(c) == 14 * (1024 + 64)
     assert lmhead.coral_lmhead_q4_packed_bytes(cz) == 14 * (1024 + 128)
