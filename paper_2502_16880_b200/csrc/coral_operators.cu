@@ -153,22 +153,22 @@ Q4Layout q4_layout(const coral_lmhead_q4_config& c) {
     return L;
 }
 
-// How many warps share a tile's columns: the split whose busiest warp has the fewest column blocks to read (ties: the
-// smaller split, which joins fewer parts).
+// How many warps share a tile's columns: the split whose busiest warp has the least to do, joining the parts of a tile counted
+// as three fifths of a column block (128256 x 4096, one row: 63 us with 2 warps, 76 with 16).
 int q4_split(int T, int KB, int sms) {
     int best = 1;
     long long best_cost = -1;
     for (int s = 1; s <= kQ4Warps; s *= 2) {
         const long long teams = (long long)sms * (kQ4Warps / s);
-        const long long cost = ((T + teams - 1) / teams) * ((KB + s - 1) / s);
+        const long long cost = ((T + teams - 1) / teams) * (5 * ((KB + s - 1) / s) + 3);
         if (best_cost < 0 || cost < best_cost) { best = s; best_cost = cost; }
     }
     return best;
 }
 
-// The passes over the rows of a call: up to 64 rows each on the tensor cores while more than 16 are left (two thirds of the time
-// of two passes of 16 at 17 rows, a fifth of four at 60: @@TC@@), then up to 16 on the warps' MMA, fewer where very long rows do
-// not fit shared memory.  Rows that a block would spend long on scaling are laid out first, in the caller's workspace.
+// The passes over the rows of a call: up to 64 rows each on the tensor cores while more than 16 are left (152064 x 3584, groups of
+// 64: 198 us at 17 rows and 228 at 64; the warps' MMA takes 103 for every 16), then up to 16 on the warps' MMA, fewer where very
+// long rows do not fit shared memory.  Rows that a block would spend long on scaling are laid out first, in the caller's workspace.
 constexpr int kQ4StageUnits = 1024;              // 8-column pieces that a block of the product scales itself
 
 struct Q4Pass {
