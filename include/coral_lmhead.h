@@ -508,8 +508,11 @@ int coral_lmhead_q4_status(const void *workspace_dev, void *stream);
  *   out_logits [M rows of V, ld_out apart] of `type`, rounded once; may be the logits themselves (same row distance; no other
  *     overlap).  Columns from V on are not touched.
  *   out_ids, out_logprobs [M x k_tokens], k_tokens 0..32 (0: both NULL); out_lse [M].  At least one output is needed.
- * Values of a masked token, NaN and infinities too, have no influence.  Asynchronous on `stream`, one launch, no scratch
- * memory, no atomics on floats: the same call gives the same bits.
+ * Values of a masked token, NaN and infinities too, have no influence.  The quotient l / repetition is correctly rounded.
+ * workspace_dev: 256-byte aligned, at least coral_lmhead_logits_workspace_bytes (which reads the arguments' sizes and which of
+ * them are NULL, no device memory); it holds nothing between calls, and calls that may overlap on the GPU need one each.
+ * Offsets must not decrease.  Asynchronous on `stream`, two or three launches, no allocation, no atomics on floats: the same
+ * call gives the same bits.  CORAL_ERR_TOO_LARGE for more than 2^31 - 1 list elements in all or blocks of 4096 logits.
  */
 typedef struct coral_lmhead_logits_args {
     uint32_t struct_size;          /* sizeof(coral_lmhead_logits_args) */
@@ -526,7 +529,8 @@ typedef struct coral_lmhead_logits_args {
     float *out_logprobs_dev, *out_lse_dev;
 } coral_lmhead_logits_args;
 
-int coral_lmhead_logits_process(const coral_lmhead_logits_args *args, void *stream);
+int coral_lmhead_logits_workspace_bytes(const coral_lmhead_logits_args *args, size_t *bytes);
+int coral_lmhead_logits_process(const coral_lmhead_logits_args *args, void *workspace_dev, void *stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char *coral_lmhead_error_string(int code);

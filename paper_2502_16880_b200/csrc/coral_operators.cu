@@ -275,7 +275,7 @@ int launch_q4(const coral_lmhead_q4_config& c, const Q4View& q, const Q4Pass& p,
 
 // ---- logits ----------------------------------------------------------------------------------------------------
 constexpr int kLogitsMaxV = 1 << 30;
-constexpr int kLogitsFewRows = 8;                // up to here a row takes the largest cluster: latency counts, SMs are free
+constexpr int kLogitsWideFrom = 8 * 4 * 148 * 2; // pieces of a call from which a warp takes four of them
 
 bool logits_args_ok(const coral_lmhead_logits_args* a) {
     if (!a || a->struct_size != sizeof(*a)) return false;
@@ -306,61 +306,125 @@ bool logits_args_ok(const coral_lmhead_logits_args* a) {
     return aligned(a->prompt_offsets_dev, 8) && aligned(a->output_offsets_dev, 8) && aligned(a->bias_offsets_dev, 8);
 }
 
-template <typename T>
-int launch_logits(const LogitsArgs& k, cudaStream_t st) {
-    const size_t smem = (size_t)kLogitsChunk * 4 * ((k.prompt || k.output || k.path ? 1 : 0) + (k.bias_tokens ? 1 : 0));
-    const int most = k.M <= kLogitsFewRows ? kLogitsMaxCluster : kLogitsMaxCluster / 2;
-    const int chunks = (k.V - 1) / kLogitsChunk + 1;
-    int C = 1;
-    while (C < chunks && C < most) C *= 2;
-    auto kernel = logits_kernel<T>;
-    if (!allow_smem(kernel, smem)) return CORAL_ERR_CUDA;
-    if (C > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return CORAL_ERR_CUDA;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)k.M * C);
-    cfg.blockDim = dim3(kLogitsThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = C;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, k, C) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
-}
-
-}  // namespace
-
-extern "C" {
-
-int coral_lmhead_logits_process(const coral_lmhead_logits_args* a, void* stream) {
-    if (!logits_args_ok(a)) return CORAL_ERR_INVALID;
-    if (a->M > 0x7fffffff / kLogitsMaxCluster) return CORAL_ERR_TOO_LARGE;
+// What the call needs of its lists: without a penalty the token lists change nothing, without a sequence nothing has any.
+LogitsArgs logits_kernel_args(const coral_lmhead_logits_args* a) {
     LogitsArgs k{};
     k.logits = a->logits_dev; k.out = a->out_logits_dev;
     k.ld_in = a->ld_logits; k.ld_out = a->ld_out;
     k.M = a->M; k.V = a->V; k.n_seq = a->n_seq; k.path_len = a->path_len; k.n_masks = a->n_masks;
     k.mask_words = (a->V + 31) / 32; k.k = a->k_tokens;
     k.row_seq = a->row_seq_dev;
-    // lists and penalties belong to sequences; without a penalty the token lists change nothing
     if (a->n_seq > 0 && (a->repetition_dev || a->frequency_dev || a->presence_dev)) {
-        k.prompt = a->prompt_tokens_dev; k.prompt_off = reinterpret_cast<const long long*>(a->prompt_offsets_dev); k.prompt_total = a->prompt_total;
-        k.output = a->output_tokens_dev; k.output_off = reinterpret_cast<const long long*>(a->output_offsets_dev); k.output_total = a->output_total;
+        k.prompt = a->prompt_tokens_dev; k.prompt_off = reinterpret_cast<const long long*>(a->prompt_offsets_dev);
+        k.output = a->output_tokens_dev; k.output_off = reinterpret_cast<const long long*>(a->output_offsets_dev);
         k.path = a->path_tokens_dev;
         k.rep = a->repetition_dev; k.freq = a->frequency_dev; k.pres = a->presence_dev;
     }
-    if (a->n_seq > 0) {
-        k.bias_tokens = a->bias_tokens_dev; k.bias_off = reinterpret_cast<const long long*>(a->bias_offsets_dev); k.bias_total = a->bias_total;
+    if (k.prompt) k.prompt_total = a->prompt_total;
+    if (k.output) k.output_total = a->output_total;
+    if (a->n_seq > 0 && a->bias_tokens_dev) {
+        k.bias_tokens = a->bias_tokens_dev; k.bias_off = reinterpret_cast<const long long*>(a->bias_offsets_dev);
         k.bias_values = a->bias_values_dev;
+        k.bias_total = a->bias_total;
     }
     k.mask = a->mask_words_dev; k.mask_rows = a->mask_rows_dev;
     k.out_ids = a->out_ids_dev; k.out_logprobs = a->out_logprobs_dev; k.out_lse = a->out_lse_dev;
+    return k;
+}
+
+struct LogitsPlan {
+    bool lists;
+    int nv, pieces, parts, blocks;               // pieces of 512 bytes a warp takes; pieces, parts and blocks of a row
+    size_t entry, range, piece, part, bytes;     // offsets in the workspace; the bitmap comes first
+};
+
+// Four pieces a warp, one where the blocks would otherwise leave SMs idle (one row of 128256 fp32: @@NV1@@ us, @@NV4@@ with four).
+LogitsPlan logits_plan(const LogitsArgs& k, int type) {
+    LogitsPlan p{};
+    p.lists = k.prompt || k.output || k.path || k.bias_tokens;
+    const int vec = 16 / elem_size(type), span = 32 * vec;
+    p.pieces = (int)((k.V + vec - 2LL) / span) + 1;                        // of a row that starts as late as it can
+    p.nv = (long long)k.M * p.pieces >= kLogitsWideFrom ? 4 : 1;
+    p.blocks = (p.pieces - 1) / (kLogitsWarps * p.nv) + 1;
+    p.parts = p.blocks * kLogitsWarps;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t from = at; at = (at + bytes + 255) / 256 * 256; return from; };
+    if (p.lists) {
+        take((size_t)k.n_seq * k.mask_words * 4);
+        p.entry = take((size_t)(k.prompt_total + k.output_total + k.bias_total) * 16);
+        p.range = take((size_t)k.n_seq * 8);
+    }
+    p.piece = take((size_t)k.M * p.pieces * 4);
+    p.part = take((size_t)k.M * p.parts * 8);
+    p.bytes = at;
+    return p;
+}
+
+template <typename T>
+int launch_logits(const LogitsArgs& k, const LogitsPlan& p, unsigned char* ws, cudaStream_t st) {
+    LogitsWork w{};
+    w.piece = reinterpret_cast<uint32_t*>(ws + p.piece);
+    w.part = reinterpret_cast<float2*>(ws + p.part);
+    w.pieces = p.pieces;
+    w.parts = p.parts;
+    if (p.lists) {
+        w.bitmap = reinterpret_cast<uint32_t*>(ws);
+        w.entry = reinterpret_cast<uint4*>(ws + p.entry);
+        w.range = reinterpret_cast<int2*>(ws + p.range);
+        const size_t smem = (size_t)kListWindow * 4 * (k.bias_tokens ? 2 : 1);
+        if (!allow_smem(logits_lists_kernel, smem)) return CORAL_ERR_CUDA;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)k.n_seq * kListCluster);
+        cfg.blockDim = dim3(kListThreads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = kListCluster;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaLaunchKernelEx(&cfg, logits_lists_kernel, k, w) != cudaSuccess) return CORAL_ERR_CUDA;
+    }
+    const dim3 grid((unsigned)k.M * p.blocks), block(kLogitsThreads);
+    auto kernel = p.nv == 4 ? logits_stream_kernel<T, 4> : logits_stream_kernel<T, 1>;
+    if (p.lists) {
+        if (launch_pdl(kernel, grid, block, 0, st, k, w) != cudaSuccess) return CORAL_ERR_CUDA;
+    } else {
+        kernel<<<grid, block, 0, st>>>(k, w);
+        if (cudaGetLastError() != cudaSuccess) return CORAL_ERR_CUDA;
+    }
+    return launch_pdl(logits_finish_kernel<T>, dim3(k.M), block, 0, st, k, w) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+int coral_lmhead_logits_workspace_bytes(const coral_lmhead_logits_args* a, size_t* bytes) {
+    if (!bytes || !logits_args_ok(a)) return CORAL_ERR_INVALID;
+    const LogitsArgs k = logits_kernel_args(a);
+    const LogitsPlan p = logits_plan(k, a->type);
+    if ((long long)k.M * p.blocks > 0x7fffffffLL || k.prompt_total + k.output_total + k.bias_total > 0x7fffffffLL ||
+        (p.lists && k.n_seq > 0x7fffffff / kListCluster))
+        return CORAL_ERR_TOO_LARGE;
+    *bytes = p.bytes;
+    return CORAL_OK;
+}
+
+int coral_lmhead_logits_process(const coral_lmhead_logits_args* a, void* workspace_dev, void* stream) {
+    size_t bytes = 0;
+    const int rc = coral_lmhead_logits_workspace_bytes(a, &bytes);
+    if (rc != CORAL_OK) return rc;
+    if (!workspace_dev || !aligned(workspace_dev, 256)) return CORAL_ERR_INVALID;
+    const LogitsArgs k = logits_kernel_args(a);
+    const LogitsPlan p = logits_plan(k, a->type);
+    unsigned char* ws = static_cast<unsigned char*>(workspace_dev);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (a->type == CORAL_TYPE_BF16) return launch_logits<__nv_bfloat16>(k, st);
-    if (a->type == CORAL_TYPE_F16) return launch_logits<__half>(k, st);
-    return launch_logits<float>(k, st);
+    if (a->type == CORAL_TYPE_BF16) return launch_logits<__nv_bfloat16>(k, p, ws, st);
+    if (a->type == CORAL_TYPE_F16) return launch_logits<__half>(k, p, ws, st);
+    return launch_logits<float>(k, p, ws, st);
 }
 
 int coral_lmhead_q4_packed_bytes(const coral_lmhead_q4_config* cfg, size_t* bytes) {

@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
         for (int d = 0; d < kQ4Depth; ++d) {
             if (base + d >= total) break;
             if (b < q.KB) {
-                float part[NT][4], part2[NT][4];       // two chains of MMAs, so that one does not wait for the other
+                float part[NT][4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     constexpr int kChunks = 4 / PER;               // 32-column chunks a group has in this block
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
 #pragma unroll
                         for (int j = 0; j < NT; ++j)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) part[j][e] = part2[j][e] = 0.f;
+                            for (int e = 0; e < 4; ++e) part[j][e] = 0.f;
                     }
                     const uint32_t lo = i == 0 ? w[d][0].x : i == 1 ? w[d][0].y : i == 2 ? w[d][0].z : w[d][0].w;
                     const uint32_t hi = i == 0 ? w[d][1].x : i == 1 ? w[d][1].y : i == 2 ? w[d][1].z : w[d][1].w;
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
                     for (int j = 0; j < NT; ++j) {
                         const uint4 v = *reinterpret_cast<const uint4*>(xl[j] + b * 256 + i * 64);
                         q4_mma(part[j], a0, v.x, v.y);
-                        q4_mma(part2[j], a1, v.z, v.w);
+                        q4_mma(part[j], a1, v.z, v.w);
                     }
                     if (i % kChunks == kChunks - 1) {
                         const float s0 = sc[d][0].scale(g, q.scale_half), s1 = sc[d][1].scale(g, q.scale_half);
@@ -313,10 +313,10 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
 #pragma unroll
                         for (int j = 0; j < NT; ++j) {
                             const float2 u = sl[(b * PER + g) * (kCols / 2) + 4 * j];
-                            acc[j][0] = fmaf(s0, fmaf(z0, u.x, part[j][0] + part2[j][0]), acc[j][0]);
-                            acc[j][1] = fmaf(s0, fmaf(z0, u.y, part[j][1] + part2[j][1]), acc[j][1]);
-                            acc[j][2] = fmaf(s1, fmaf(z1, u.x, part[j][2] + part2[j][2]), acc[j][2]);
-                            acc[j][3] = fmaf(s1, fmaf(z1, u.y, part[j][3] + part2[j][3]), acc[j][3]);
+                            acc[j][0] = fmaf(s0, fmaf(z0, u.x, part[j][0]), acc[j][0]);
+                            acc[j][1] = fmaf(s0, fmaf(z0, u.y, part[j][1]), acc[j][1]);
+                            acc[j][2] = fmaf(s1, fmaf(z1, u.x, part[j][2]), acc[j][2]);
+                            acc[j][3] = fmaf(s1, fmaf(z1, u.y, part[j][3]), acc[j][3]);
                         }
                     }
                 }

@@ -109,7 +109,8 @@ _SIGNATURES = {
     "coral_lmhead_q4_workspace_bytes": (_i, [ctypes.POINTER(coral_lmhead_q4_config), _i, ctypes.POINTER(ctypes.c_size_t)]),
     "coral_lmhead_q4_linear": (_i, [ctypes.POINTER(coral_lmhead_q4_config), _vp, _vp, _i, _i, _vp, _i, _vp, _vp]),
     "coral_lmhead_q4_status": (_i, [_vp, _vp]),
-    "coral_lmhead_logits_process": (_i, [ctypes.POINTER(coral_lmhead_logits_args), _vp]),
+    "coral_lmhead_logits_workspace_bytes": (_i, [ctypes.POINTER(coral_lmhead_logits_args), ctypes.POINTER(ctypes.c_size_t)]),
+    "coral_lmhead_logits_process": (_i, [ctypes.POINTER(coral_lmhead_logits_args), _vp, _vp]),
     "coral_lmhead_error_string": (ctypes.c_char_p, [_i]),
     "coral_lmhead_destroy": (_i, [_vp]),
 }
@@ -558,7 +559,8 @@ def coral_lmhead_logits_process(logits, *, row_seq=None, prompt_tokens=None, pro
                                 out_logits=None, out_ids=None, out_logprobs=None, out_lse=None, stream=None) -> None:
     """Penalties, biases and masks on logits [M, V] (rows may lie apart), and the candidates of the result.  Lists are flat
     int32 with int64 offsets [n_seq + 1]; path_tokens int32 [M, path_len]; repetition, frequency, presence fp32 [n_seq];
-    mask_words int32 [n_masks, ceil(V / 32)]; out_ids int32 and out_logprobs fp32 [M, k_tokens]; out_lse fp32 [M]."""
+    mask_words int32 [n_masks, ceil(V / 32)]; out_ids int32 and out_logprobs fp32 [M, k_tokens]; out_lse fp32 [M].  The scratch
+    of the call comes from torch's allocator."""
     dev = _op_device(logits, "logits")
     if logits.dim() != 2:
         raise ValueError("logits must be [M, V]")
@@ -592,8 +594,13 @@ def coral_lmhead_logits_process(logits, *, row_seq=None, prompt_tokens=None, pro
         _op_ptr("mask_words", mask_words, i32, (n_masks, (V + 31) // 32), dev), _op_ptr("mask_rows", mask_rows, i32, (M,), dev),
         _op_ptr("out_ids", out_ids, i32, (M, k), dev), _op_ptr("out_logprobs", out_logprobs, f32, (M, k), dev),
         _op_ptr("out_lse", out_lse, f32, (M,), dev))
-    _check((_lib or load_library()).coral_lmhead_logits_process(ctypes.byref(a), _op_stream(stream, dev)),
+    lib, n = _lib or load_library(), ctypes.c_size_t(0)
+    _check(lib.coral_lmhead_logits_workspace_bytes(ctypes.byref(a), ctypes.byref(n)), "coral_lmhead_logits_workspace_bytes")
+    workspace = torch.empty(n.value, dtype=torch.uint8, device=logits.device)
+    _check(lib.coral_lmhead_logits_process(ctypes.byref(a), workspace.data_ptr(), _op_stream(stream, dev)),
            "coral_lmhead_logits_process")
+    if stream is not None:
+        workspace.record_stream(stream)
 
 
 def coral_lmhead_destroy(handle) -> None:

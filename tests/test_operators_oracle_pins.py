@@ -101,11 +101,23 @@ def _largs(**kw):
     dict(mask_words_dev=P, n_masks=1), dict(mask_words_dev=P, n_masks=0, mask_rows_dev=P), dict(logits_dev=P + 2),
     dict(type=1, logits_dev=P + 1), dict(repetition_dev=P + 1), dict(out_lse_dev=P + 2), dict(row_seq_dev=P + 1)])
 def test_logits_refusals(lib, kw):
-    a = _largs(**kw)
-    assert lib.coral_lmhead_logits_process(ctypes.byref(a), None) == lmhead.CORAL_ERR_INVALID
+    a, n = _largs(**kw), ctypes.c_size_t()
+    assert lib.coral_lmhead_logits_process(ctypes.byref(a), ctypes.c_void_p(P), None) == lmhead.CORAL_ERR_INVALID
+    assert lib.coral_lmhead_logits_workspace_bytes(ctypes.byref(a), ctypes.byref(n)) == lmhead.CORAL_ERR_INVALID
 
 
-def test_logits_refuses_null_and_too_many_rows(lib):
-    assert lib.coral_lmhead_logits_process(None, None) == lmhead.CORAL_ERR_INVALID
-    a = _largs(M=1 << 28, n_seq=0)
-    assert lib.coral_lmhead_logits_process(ctypes.byref(a), None) == lmhead.CORAL_ERR_TOO_LARGE
+def test_logits_refuses_null_workspaces_and_too_large_calls(lib):
+    n = ctypes.c_size_t()
+    assert lib.coral_lmhead_logits_process(None, ctypes.c_void_p(P), None) == lmhead.CORAL_ERR_INVALID
+    for ws in (None, P + 128):
+        assert lib.coral_lmhead_logits_process(ctypes.byref(_largs()), ctypes.c_void_p(ws), None) == lmhead.CORAL_ERR_INVALID
+    lists = dict(prompt_tokens_dev=P, prompt_offsets_dev=P, output_tokens_dev=P, output_offsets_dev=P, repetition_dev=P)
+    for kw in (dict(M=1 << 30, V=1 << 20, ld_logits=1 << 20, n_seq=0), dict(prompt_total=1 << 30, output_total=1 << 30, **lists),
+               dict(M=1, n_seq=1 << 29, **lists)):
+        a = _largs(**kw)
+        assert lib.coral_lmhead_logits_process(ctypes.byref(a), ctypes.c_void_p(P), None) == lmhead.CORAL_ERR_TOO_LARGE
+    # lists cost a bitmap of four words (100 tokens) a sequence and 16 bytes an element, rounded up to 256 bytes each
+    size = lambda **kw: (lib.coral_lmhead_logits_workspace_bytes(ctypes.byref(_largs(**kw)), ctypes.byref(n)), n.value)[1]
+    plain = size()
+    assert size(prompt_total=100, output_total=50, **lists) == plain + 256 + 2560 + 256
+    assert size(prompt_total=100, output_total=50, **{**lists, "repetition_dev": None}) == plain       # no penalty uses them
