@@ -335,7 +335,7 @@ LogitsArgs logits_kernel_args(const coral_lmhead_logits_args* a) {
 struct LogitsPlan {
     bool lists;
     int nv, pieces, parts, blocks;               // pieces of 512 bytes a warp takes; pieces, parts and blocks of a row
-    size_t entry, range, piece, part, bytes;     // offsets in the workspace; the bitmap comes first
+    size_t before, entry, token, range, piece, part, bytes;         // offsets in the workspace; the bitmap comes first
 };
 
 // Four pieces a warp, one where the blocks would otherwise leave SMs idle (one row of 128256 fp32: @@NV1@@ us, @@NV4@@ with four).
@@ -351,7 +351,10 @@ LogitsPlan logits_plan(const LogitsArgs& k, int type) {
     auto take = [&](size_t bytes) { const size_t from = at; at = (at + bytes + 255) / 256 * 256; return from; };
     if (p.lists) {
         take((size_t)k.n_seq * k.mask_words * 4);
-        p.entry = take((size_t)(k.prompt_total + k.output_total + k.bias_total) * 16);
+        p.before = take((size_t)k.n_seq * k.mask_words * 4);
+        const size_t listed = (size_t)(k.prompt_total + k.output_total + k.bias_total);
+        p.entry = take(listed * 8);
+        p.token = take(listed * 4);
         p.range = take((size_t)k.n_seq * 8);
     }
     p.piece = take((size_t)k.M * p.pieces * 4);
@@ -369,7 +372,12 @@ int launch_logits(const LogitsArgs& k, const LogitsPlan& p, unsigned char* ws, c
     w.parts = p.parts;
     if (p.lists) {
         w.bitmap = reinterpret_cast<uint32_t*>(ws);
-        w.entry = reinterpret_cast<uint4*>(ws + p.entry);
+        w.before = reinterpret_cast<uint32_t*>(ws + p.before);
+        w.entry = reinterpret_cast<uint2*>(ws + p.entry);
+        w.token = reinterpret_cast<int32_t*>(ws + p.token);
+        // the candidates' pieces are read again, and 16 bits of a listed token's result are not its logit any more
+        w.late = k.out == k.logits && sizeof(T) == 2 && k.k > 0;
+        w.final = k.out == k.logits && sizeof(T) == 4;
         w.range = reinterpret_cast<int2*>(ws + p.range);
         const size_t smem = (size_t)kListWindow * 4 * (k.bias_tokens ? 2 : 1);
         if (!allow_smem(logits_lists_kernel, smem)) return CORAL_ERR_CUDA;
@@ -388,10 +396,11 @@ int launch_logits(const LogitsArgs& k, const LogitsPlan& p, unsigned char* ws, c
         if (cudaLaunchKernelEx(&cfg, logits_lists_kernel, k, w) != cudaSuccess) return CORAL_ERR_CUDA;
     }
     const dim3 grid((unsigned)k.M * p.blocks), block(kLogitsThreads);
-    auto kernel = p.nv == 4 ? logits_stream_kernel<T, 4> : logits_stream_kernel<T, 1>;
     if (p.lists) {
+        auto kernel = p.nv == 4 ? logits_stream_kernel<T, 4, true> : logits_stream_kernel<T, 1, true>;
         if (launch_pdl(kernel, grid, block, 0, st, k, w) != cudaSuccess) return CORAL_ERR_CUDA;
     } else {
+        auto kernel = p.nv == 4 ? logits_stream_kernel<T, 4, false> : logits_stream_kernel<T, 1, false>;
         kernel<<<grid, block, 0, st>>>(k, w);
         if (cudaGetLastError() != cudaSuccess) return CORAL_ERR_CUDA;
     }

@@ -4,15 +4,14 @@
 //   l4 = l3 + bias(x)      out = x allowed ? l4 : -inf            (each step one fp32 operation, in this order)
 // Bound by the logits' bytes, so a row is streamed once, by a kernel with no more in it than that needs, and what is rare or
 // needs a whole row is done by two small kernels around it:
-//   logits_lists_kernel   per sequence: counts its token lists into tables in shared memory (whole numbers: the order of the
-//                         atomics does not matter), writes the listed tokens with their counts and biases, in a fixed order,
-//                         and a bitmap of them;
-//   logits_stream_kernel  reads the logits, leaves out listed tokens (bitmap) and those of the row's path, applies the mask,
+//   logits_lists_kernel   per sequence: counts its token lists into a table in shared memory (whole numbers: the order of the
+//                         atomics does not matter) and writes the listed tokens with their counts and biases in the tokens'
+//                         order, a bitmap of them, and how many lie before each word of it;
+//   logits_stream_kernel  reads the logits, works on the listed tokens (bitmap) and those of the row's path, applies the mask,
 //                         writes the result, and keeps the maximum of every 512 bytes and a (maximum, sum of exponentials)
 //                         of every warp's part;
-//   logits_finish_kernel  per row: the listed and path tokens one a thread (their logits are read again, a few bytes each), the
-//                         log-sum-exp, and the candidates: only the k pieces of 512 bytes with the largest maxima can hold
-//                         one of the k best of the streamed tokens, so only they are read again.
+//   logits_finish_kernel  per row: the log-sum-exp, and the candidates: only the k pieces of 512 bytes with the largest maxima
+//                         can hold one, so only they are read again.
 // (Everything in one kernel, a cluster of blocks a row, took 850 us for 960 x 128256 fp32: candidates and lists cost each block
 // a chain of barriers a row, and their code pushed the streaming loop out of the instruction cache.)
 #pragma once
@@ -28,7 +27,7 @@ constexpr int kLogitsThreads = 256;
 constexpr int kLogitsWarps = kLogitsThreads / 32;
 constexpr int kLogitsCap = 2048;                 // keys ranked by counting
 constexpr int kLogitsMaxPath = 64;
-constexpr int kListThreads = 512;
+constexpr int kListThreads = 1024;
 constexpr int kListWindow = 16384;               // tokens of a block's table
 constexpr int kListCluster = 8;
 
@@ -54,11 +53,15 @@ struct LogitsArgs {
 // Scratch of a call (the caller's workspace).
 struct LogitsWork {
     uint32_t* bitmap;                            // [n_seq][mask_words] listed tokens of a sequence
-    uint4* entry;                                // token, table word, bias; a sequence's from its lists' offsets on
+    uint32_t* before;                            // [n_seq][mask_words] its entry of a word's first listed token, counted over all
+    uint2* entry;                                // table word and bias of listed tokens, a sequence's from its lists' offsets on
+    int32_t* token;                              // which tokens they are
     int2* range;                                 // [n_seq] first entry and number
     uint32_t* piece;                             // [M][pieces] largest value (logit_order) of 512 bytes of logits
     float2* part;                                // [M][parts] maximum and sum of a warp's vectors
     int pieces, parts;
+    int late;                                    // over the logits, in 16 bits: the last kernel stores listed tokens
+    int final;                                   // over the logits, in 32 bits: the last kernel reads results, not logits
 };
 
 // Monotone map of a float to an unsigned integer; NaN and -inf (no candidate) become 0.  -0 counts as +0.
@@ -136,10 +139,12 @@ __device__ __forceinline__ float divide(float l, float rep, float inv) {
 // ---- token lists of a sequence -----------------------------------------------------------------------------
 // grid: n_seq clusters of kListCluster blocks; a block counts the tokens of windows rank, rank + kListCluster, ...
 // dynamic shared memory: the table, and a second one (1 + place of a token's last bias) if there are biases.
-__global__ void __launch_bounds__(kListThreads, 1) logits_lists_kernel(const __grid_constant__ LogitsArgs a, LogitsWork w) {
+__global__ void __launch_bounds__(kListThreads, 1) logits_lists_kernel(const __grid_constant__ LogitsArgs a, const __grid_constant__ LogitsWork w) {
     namespace cg = cooperative_groups;
     extern __shared__ __align__(16) uint32_t tables[];
-    __shared__ int s_warp[kListThreads / 32], s_total;
+    constexpr int kWords = kListWindow / 32;
+    __shared__ uint32_t s_bits[kWords];
+    __shared__ int s_warp[kListThreads / 32], s_total[2];
     auto cluster = cg::this_cluster();
     const int seq = blockIdx.x / kListCluster, rank = blockIdx.x % kListCluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t* places = tables + kListWindow;
@@ -148,12 +153,14 @@ __global__ void __launch_bounds__(kListThreads, 1) logits_lists_kernel(const __g
     if (a.prompt) list_range(a.prompt_off, seq, a.prompt_total, p0, p1);
     if (a.output) list_range(a.output_off, seq, a.output_total, o0, o1);
     if (a.bias_tokens) list_range(a.bias_off, seq, a.bias_total, b0, b1);
-    long long at = p0 + o0 + b0;                 // a sequence has room for as many entries as its lists are long
-    const long long first = at;
-    for (int base = 0; base < a.V; base += kListCluster * kListWindow) {
-        const int lo = base + rank * kListWindow, n = min(kListWindow, a.V - lo);
+    const long long first = p0 + o0 + b0;        // a sequence has room for as many entries as its lists are long
+    long long at = first;
+    int turn = 0;
+    for (int base = 0; base < a.V; base += kListCluster * kListWindow, turn ^= 1) {
+        const int lo = base + rank * kListWindow, n = min(kListWindow, a.V - lo);           // n < 1: behind the last token
         const int words = (a.bias_tokens ? 2 : 1) * kListWindow;
         for (int i = threadIdx.x * 4; i < words; i += kListThreads * 4) *reinterpret_cast<uint4*>(tables + i) = make_uint4(0, 0, 0, 0);
+        for (int i = threadIdx.x; i < kWords; i += kListThreads) s_bits[i] = 0;
         __syncthreads();
         auto each = [&](const int32_t* tokens, long long from, long long to, auto put) {
             for (long long i = from + threadIdx.x; i < to; i += 4 * kListThreads) {
@@ -161,54 +168,72 @@ __global__ void __launch_bounds__(kListThreads, 1) logits_lists_kernel(const __g
 #pragma unroll
                 for (int u = 0; u < 4; ++u) t[u] = i + u * kListThreads < to ? tokens[i + u * kListThreads] : -1;
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (t[u] >= lo && t[u] - lo < n) put(t[u] - lo, (uint32_t)(i + u * kListThreads - from) + 1u);
+                for (int u = 0; u < 4; ++u) {
+                    const int x = t[u] - lo;
+                    if (t[u] < lo || x >= n) continue;
+                    // whoever finds the word empty is the first to list the token
+                    if (put(x, (uint32_t)(i + u * kListThreads - from) + 1u) == 0) atomicOr(&s_bits[x >> 5], 1u << (x & 31));
+                }
             }
         };
-        if (a.prompt) each(a.prompt, p0, p1, [&](int t, uint32_t) { atomicOr(tables + t, kSeenBit); });
-        if (a.output) each(a.output, o0, o1, [&](int t, uint32_t) { atomicAdd(tables + t, 1u); });
+        if (a.prompt) each(a.prompt, p0, p1, [&](int x, uint32_t) { return atomicOr(tables + x, kSeenBit); });
+        if (a.output) each(a.output, o0, o1, [&](int x, uint32_t) { return atomicAdd(tables + x, 1u); });
         if (a.bias_tokens)
-            each(a.bias_tokens, b0, b1, [&](int t, uint32_t place) {
-                atomicOr(tables + t, kBiasBit);
-                atomicMax(places + t, place);
+            each(a.bias_tokens, b0, b1, [&](int x, uint32_t place) {
+                atomicMax(places + x, place);
+                return atomicOr(tables + x, kBiasBit);
             });
         __syncthreads();
-        // the bitmap, and the number of entries: a warp takes 1024 neighbouring tokens at a time, a lane 32 of them by ballots
-        int mine = 0;
-        for (int i = warp * 32; i < n; i += kListThreads) {
-            const uint32_t bits = __ballot_sync(0xffffffffu, i + lane < n && tables[i + lane] != 0);
-            if (lane == 0) w.bitmap[(size_t)seq * a.mask_words + (lo + i) / 32] = bits;
-            mine += __popc(bits);                // the same in every lane
+        // entries before each word of the bitmap: over the block, then over the cluster
+        const uint32_t bits = threadIdx.x < kWords ? s_bits[threadIdx.x] : 0;
+        int upto = __popc(bits);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
         }
-        if (lane == 0) s_warp[warp] = mine;
+        if (lane == 31) s_warp[warp] = upto;
         __syncthreads();
-        int before = 0, total = 0;
-        for (int i = 0; i < kListThreads / 32; ++i) {
+        int before = upto - __popc(bits), total = 0;
+#pragma unroll
+        for (int i = 0; i < kWords / 32; ++i) {
             before += i < warp ? s_warp[i] : 0;
             total += s_warp[i];
         }
-        if (threadIdx.x == 0) s_total = total;
+        if (threadIdx.x == 0) s_total[turn] = total;
         cluster.sync();
+        int others[kListCluster];
+#pragma unroll
+        for (int c = 0; c < kListCluster; ++c) others[c] = *cluster.map_shared_rank(&s_total[turn], c);
         long long next = at;
+#pragma unroll
         for (int c = 0; c < kListCluster; ++c) {
-            const int t = *cluster.map_shared_rank(&s_total, c);
-            if (c < rank) before += t;
-            next += t;
+            if (c < rank) before += others[c];
+            next += others[c];
         }
-        cluster.sync();                          // s_total has been read
-        uint4* out = w.entry + at + before;
-        for (int i = warp * 32; i < n; i += kListThreads) {
-            const uint32_t word = i + lane < n ? tables[i + lane] : 0, bits = __ballot_sync(0xffffffffu, word != 0);
-            if (word) {
-                const float bias = word & kBiasBit ? a.bias_values[b0 + places[i + lane] - 1] : 0.f;
-                out[__popc(bits & ((1u << lane) - 1))] = make_uint4((uint32_t)(lo + i + lane), word, __float_as_uint(bias), 0);
+        if (threadIdx.x < kWords && (int)threadIdx.x * 32 < n) {
+            const size_t word = (size_t)seq * a.mask_words + lo / 32 + threadIdx.x;
+            w.bitmap[word] = bits;
+            w.before[word] = (uint32_t)(at + before);
+            for (uint32_t left = bits; left; left &= left - 1, ++before) {
+                const int x = threadIdx.x * 32 + __ffs(left) - 1;
+                w.entry[at + before] = make_uint2(tables[x], 0);
+                w.token[at + before] = lo + x;
+                tables[x] = (uint32_t)before;    // by which the biases find it
             }
-            out += __popc(bits);
+        }
+        if (a.bias_tokens) {
+            __syncthreads();
+            for (long long i = b0 + threadIdx.x; i < b1; i += kListThreads) {
+                const int t = a.bias_tokens[i], x = t - lo;
+                if (t >= lo && x < n && places[x] == (uint32_t)(i - b0) + 1u) w.entry[at + tables[x]].y = __float_as_uint(a.bias_values[i]);
+            }
         }
         at = next;
         __syncthreads();
     }
     if (rank == 0 && threadIdx.x == 0) w.range[seq] = make_int2((int)first, (int)(at - first));
+    cluster.sync();                              // the others' totals have been read
 }
 
 // ---- the pass over the logits ------------------------------------------------------------------------------
@@ -241,54 +266,111 @@ __device__ __noinline__ uint32_t mask_bits(const uint32_t* mask, int j0, int n, 
 }
 
 
+// A row's parameters for tokens of its lists and its path.
+struct LogitsRow {
+    float rep, inv, freq, pres;
+    const uint32_t *listed, *before;             // of the row's sequence; null: none
+    const int32_t* path;                         // null: none
+};
+__device__ __forceinline__ LogitsRow row_params(const LogitsArgs& a, const LogitsWork& w, int row, int seq) {
+    LogitsRow r{1.f, 1.f, 0.f, 0.f, nullptr, nullptr, nullptr};
+    if (!w.bitmap || seq < 0 || seq >= a.n_seq) return r;              // a row of no sequence has no lists and no penalties
+    if (a.rep) r.rep = a.rep[seq];
+    if (a.freq) r.freq = a.freq[seq];
+    if (a.pres) r.pres = a.pres[seq];
+    r.inv = __frcp_rn(r.rep);
+    r.listed = w.bitmap + (size_t)seq * a.mask_words;
+    r.before = w.before + (size_t)seq * a.mask_words;
+    if (a.path) r.path = a.path + (size_t)row * a.path_len;
+    return r;
+}
+
+// Penalties and bias of a token with this entry (zeros: it is on the path only).
+__device__ __forceinline__ float adjust_inline(float l, int token, uint2 e, const LogitsRow& r, int path_len) {
+    uint32_t n = e.x & kCountMask;
+    if (r.path)
+        for (int q = 0; q < path_len; ++q) n += r.path[q] == token;
+    if (n || (e.x & kSeenBit)) l = l > 0.f ? divide(l, r.rep, r.inv) : __fmul_rn(l, r.rep);
+    if (n) l = __fsub_rn(__fsub_rn(l, __fmul_rn(r.freq, (float)n)), r.pres);
+    if (e.x & kBiasBit) l = __fadd_rn(l, __uint_as_float(e.y));
+    return l;
+}
+__device__ __noinline__ float adjust(float l, int token, uint2 e, const LogitsRow& r, int path_len) {
+    return adjust_inline(l, token, e, r, path_len);
+}
+// The entry of the first listed token from token j on: the number of those before it.
+__device__ __forceinline__ uint32_t entry_at(const LogitsRow& r, int j) {
+    return __ldcg(r.before + (j >> 5)) + __popc(__ldcg(r.listed + (j >> 5)) & ((1u << (j & 31)) - 1));
+}
+__device__ __forceinline__ uint2 entry_of(const LogitsRow& r, const LogitsWork& w, int token) {
+    return (__ldcg(r.listed + (token >> 5)) >> (token & 31)) & 1u ? __ldcg(w.entry + entry_at(r, token)) : make_uint2(0, 0);
+}
+
 // grid: M * ceil(pieces / (8 NV)) blocks of 8 warps; a warp takes NV pieces, 8 apart.
-template <typename T, int NV>
+// LISTS: the call has token lists, paths or biases.
+template <typename T, int NV, bool LISTS>
 __global__ void __launch_bounds__(kLogitsThreads) logits_stream_kernel(const __grid_constant__ LogitsArgs a, const __grid_constant__ LogitsWork w) {
     constexpr int kVec = LogitsVec<T>::kVec, kPiece = LogitsVec<T>::kPiece, kSpan = kLogitsWarps * NV * kPiece;
-    __shared__ uint32_t s_path[kSpan / 32];      // path tokens among the block's positions
+    __shared__ __align__(16) float s_adjusted[LISTS ? kSpan : 1];
+    __shared__ uint32_t s_special[LISTS ? kSpan / 32 : 1];
     const int per_row = (w.pieces + kLogitsWarps * NV - 1) / (kLogitsWarps * NV);
     const int row = blockIdx.x / per_row, block = blockIdx.x - row * per_row, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const T* in = reinterpret_cast<const T*>(a.logits) + (size_t)row * a.ld_in;
     T* out = reinterpret_cast<T*>(a.out) + (a.out ? (size_t)row * a.ld_out : 0);
     const int shift = (int)((reinterpret_cast<uintptr_t>(in) & 15) / sizeof(T)), end = a.V + shift;
     const int p_block = block * kSpan, p0 = p_block + warp * kPiece + lane * kVec;
+    // every load the block needs is on its way before the first is waited for
+    const int seq = !LISTS ? -1 : a.row_seq ? a.row_seq[row] : row, mr = !a.mask ? -1 : a.mask_rows ? a.mask_rows[row] : row;
     uint4 raw[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int p = p0 + i * kLogitsWarps * kPiece;
         raw[i] = p >= shift && p + kVec <= end ? __ldcs(reinterpret_cast<const uint4*>(in - shift + p)) : load_edge(in, p, shift, end);
     }
-    const uint32_t* mask = nullptr;
-    bool nothing = false;
-    if (a.mask) {
-        const int mr = a.mask_rows ? a.mask_rows[row] : row;
-        nothing = mr >= a.n_masks;               // no such mask: allow nothing
-        if (mr >= 0 && !nothing) mask = a.mask + (size_t)mr * a.mask_words;
+    const LogitsRow par = row_params(a, w, row, seq);
+    const bool nothing = mr >= a.n_masks && a.mask;                                // no such mask: allow nothing
+    const uint32_t* const mask = mr >= 0 && !nothing ? a.mask + (size_t)mr * a.mask_words : nullptr;
+    uint32_t keep_word[NV];                      // of the mask, where a vector lies in one word of it
+    if (LISTS) {
+        for (int i = threadIdx.x; i < kSpan / 32; i += kLogitsThreads) s_special[i] = 0;
+        pdl_wait();                              // what follows of the lists comes from the kernel before
     }
-    const uint32_t* listed = nullptr;
-    bool path = false;
-    if (w.bitmap) {
-        const int seq = a.row_seq ? a.row_seq[row] : row;
-        if (seq >= 0 && seq < a.n_seq) {         // a row of no sequence has no lists and no penalties
-            listed = w.bitmap + (size_t)seq * a.mask_words;
-            path = a.path != nullptr;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int p = p0 + i * kLogitsWarps * kPiece, at = min(p, a.V - 1) >> 5;
+        keep_word[i] = mask && shift == 0 ? __ldg(mask + at) : 0;
+    }
+    if (LISTS && par.listed) {                   // one thread a token that is listed or on the path, wherever it lies in the block
+        const int lo = max(p_block - shift, 0), hi = min(p_block + kSpan - shift, a.V);
+        uint32_t first = 0;
+        int n = 0;
+        if (lo < hi) first = entry_at(par, lo);  // (the last block of a row may lie behind its end)
+        if (lo >= hi) n = 0;
+        else if (hi < a.V) n = (int)(entry_at(par, hi) - first);
+        else {
+            const int2 range = __ldcg(w.range + seq);
+            n = range.x + range.y - (int)first;
         }
-    }
-    if (path) {
-        for (int i = threadIdx.x; i < kSpan / 32; i += kLogitsThreads) s_path[i] = 0;
         __syncthreads();
-        if (threadIdx.x < a.path_len) {
-            const int token = a.path[(size_t)row * a.path_len + threadIdx.x], at = token + shift - p_block;
-            if (token >= 0 && token < a.V && at >= 0 && at < kSpan) atomicOr(&s_path[at >> 5], 1u << (at & 31));
+        const int total = n + (par.path ? a.path_len : 0);
+#pragma unroll 1
+        for (int i = threadIdx.x; i < total; i += kLogitsThreads) {
+            int token;
+            uint2 entry = make_uint2(0, 0);
+            if (i < n) {
+                token = __ldcg(w.token + first + i);
+                entry = __ldcg(w.entry + first + i);
+            } else {
+                token = par.path[i - n];
+                if (token < lo || token >= hi || (__ldcg(par.listed + (token >> 5)) >> (token & 31)) & 1u) continue;
+            }
+            const int at = token + shift - p_block;
+            s_adjusted[at] = adjust_inline(Elem<T>::up(in[token]), token, entry, par, a.path_len);
+            atomicOr(&s_special[at >> 5], 1u << (at & 31));
         }
         __syncthreads();
     }
-    if (w.bitmap) pdl_wait();                    // the bitmap comes from the kernel before
     const bool vec_out = a.out && (int)((reinterpret_cast<uintptr_t>(out) & 15) / sizeof(T)) == shift;
-    auto bits_of = [&](const uint32_t* words, int p) {
-        const int j0 = p - shift;
-        return shift == 0 && p < end ? __ldg(words + (j0 >> 5)) >> (j0 & 31) : mask_bits(words, j0, kVec, a.V);
-    };
     float val[NV][kVec];
     uint32_t top[NV];
 #pragma unroll
@@ -297,19 +379,22 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_stream_kernel(const __g
         const T* r = reinterpret_cast<const T*>(&raw[i]);
 #pragma unroll
         for (int e = 0; e < kVec; ++e) val[i][e] = Elem<T>::up(r[e]);
-        uint32_t keep = nothing ? 0u : ~0u, skip = 0;          // bit e: token p + e - shift is allowed; is listed or on the path
-        if (mask) keep = bits_of(mask, p);
-        if (listed) skip = bits_of(listed, p);
-        if (path) skip |= s_path[(p - p_block) >> 5] >> ((p - p_block) & 31);
-        skip &= (1u << kVec) - 1;
-        if (mask || nothing || skip) {
-            const uint32_t bits = keep & ~skip;
+        uint32_t keep = nothing ? 0u : ~0u;      // bit e: token p + e - shift is allowed
+        if (mask) keep = shift == 0 ? keep_word[i] >> (p & 31) : mask_bits(mask, p - shift, kVec, a.V);
+        const uint32_t special = LISTS && par.listed ? (s_special[(p - p_block) >> 5] >> (p & 31)) & ((1u << kVec) - 1) : 0;
+        if (LISTS && special) {
 #pragma unroll
             for (int e = 0; e < kVec; ++e)
-                if (!(bits & (1u << e))) val[i][e] = kNegInf;
+                if ((special >> e) & 1u) val[i][e] = s_adjusted[p - p_block + e];
+        }
+        if (mask || nothing) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                if (!(keep & (1u << e))) val[i][e] = kNegInf;
         }
         if (a.out) {
             T* to = out - shift + p;
+            const uint32_t skip = LISTS && w.late ? special : 0;
             if (vec_out && p >= shift && p + kVec <= end && !skip) {
                 uint4 o;
                 T* t = reinterpret_cast<T*>(&o);
@@ -350,8 +435,6 @@ struct LogitsShared {
     uint32_t warp_u[32];
     float warp_m[kLogitsWarps], warp_s[kLogitsWarps];
     int n;
-    int path[kLogitsMaxPath];
-    uint32_t path_bits[64];                      // hashed path tokens, to pass most entries over
 };
 
 // Largest key of the block, in every thread.
@@ -389,123 +472,30 @@ __device__ __noinline__ void rank_keys(int n, int k, LogitsShared& s) {
     __syncthreads();
 }
 
+// The rank of every lane's key among the first n lanes' (distinct ones, n <= 32); 32 and more behind them.
+__device__ __forceinline__ int warp_rank(unsigned long long key, int n) {
+    int r = (int)(threadIdx.x & 31) < n ? 0 : 32;
+    for (int j = 0; j < n; ++j) r += __shfl_sync(0xffffffffu, key, j) > key ? 1 : 0;
+    return r;
+}
+
 // grid: M blocks.
 template <typename T>
 __global__ void __launch_bounds__(kLogitsThreads) logits_finish_kernel(const __grid_constant__ LogitsArgs a, const __grid_constant__ LogitsWork w) {
-    constexpr int kVec = LogitsVec<T>::kVec, kPiece = LogitsVec<T>::kPiece;
+    constexpr int kVec = LogitsVec<T>::kVec, kPiece = LogitsVec<T>::kPiece, kMost = 32 / kLogitsWarps, kHeld = 8;
     __shared__ LogitsShared s;
     const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const T* in = reinterpret_cast<const T*>(a.logits) + (size_t)row * a.ld_in;
     T* out = reinterpret_cast<T*>(a.out) + (a.out ? (size_t)row * a.ld_out : 0);
     const int shift = (int)((reinterpret_cast<uintptr_t>(in) & 15) / sizeof(T)), end = a.V + shift;
-    const uint32_t* mask = nullptr;
-    bool nothing = false;
-    if (a.mask) {
-        const int mr = a.mask_rows ? a.mask_rows[row] : row;
-        nothing = mr >= a.n_masks;
-        if (mr >= 0 && !nothing) mask = a.mask + (size_t)mr * a.mask_words;
-    }
-    const int seq = !w.bitmap ? -1 : a.row_seq ? a.row_seq[row] : row;
-    const bool known = seq >= 0 && seq < a.n_seq, path = known && a.path;
-    const uint32_t* listed = known ? w.bitmap + (size_t)seq * a.mask_words : nullptr;
+    const int seq = !w.bitmap ? -1 : a.row_seq ? a.row_seq[row] : row, mr = !a.mask ? -1 : a.mask_rows ? a.mask_rows[row] : row;
+    const bool nothing = mr >= a.n_masks && a.mask;
+    const uint32_t* const mask = mr >= 0 && !nothing ? a.mask + (size_t)mr * a.mask_words : nullptr;
     if (threadIdx.x == 0) s.n = 0;
-    if (threadIdx.x < 64) s.path_bits[threadIdx.x] = 0;
-    if (path && threadIdx.x < a.path_len) s.path[threadIdx.x] = a.path[(size_t)row * a.path_len + threadIdx.x];
-    __syncthreads();
-    auto on_path = [&](int token) { return path && (s.path_bits[(token >> 5) & 63] >> (token & 31)) & 1u; };
-    if (path && threadIdx.x < a.path_len && s.path[threadIdx.x] >= 0)
-        atomicOr(&s.path_bits[(s.path[threadIdx.x] >> 5) & 63], 1u << (s.path[threadIdx.x] & 31));
+    const LogitsRow par = row_params(a, w, row, seq);
     pdl_wait();
-    __syncthreads();
 
-    // the k pieces with the largest maxima (equal ones: the lower), in s.best
-    const uint32_t* piece = w.piece + (size_t)row * w.pieces;
-    uint32_t tau = 0;                            // order of the last one's maximum: no streamed candidate is below it
-    int n_pieces = 0;
-    if (a.k) {
-        uint32_t top = 0;
-        for (int i = threadIdx.x; i < w.pieces; i += kLogitsThreads) top = max(top, piece[i]);
-        // at least k pieces reach the k-th largest of the warps' four largest threads
-        uint32_t best = top;
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t t = __reduce_max_sync(0xffffffffu, best);
-            if (lane == 0) s.warp_u[warp * 4 + i] = t;
-            if (lane == __ffs(__ballot_sync(0xffffffffu, best == t)) - 1) best = 0;
-        }
-        __syncthreads();
-        const uint32_t floor = max(kth_largest(s.warp_u[lane], 32, a.k), 1u);
-        if (top >= floor)
-            for (int i = threadIdx.x; i < w.pieces; i += kLogitsThreads)
-                if (piece[i] >= floor) {
-                    const int at = atomicAdd(&s.n, 1);
-                    if (at < kLogitsCap) s.buf[at] = logit_key(piece[i], i);
-                }
-        __syncthreads();
-        const int n = s.n;
-        if (n <= kLogitsCap) rank_keys(n, a.k, s);
-        else {                                   // very many pieces with one maximum: k rounds over them
-            unsigned long long last = ~0ull;
-            for (int i = 0; i < a.k; ++i) {
-                unsigned long long key = 0;
-                for (int j = threadIdx.x; j < w.pieces; j += kLogitsThreads) {
-                    const unsigned long long mine = logit_key(piece[j], j);
-                    if (mine < last && mine > key) key = mine;
-                }
-                last = block_max_key(key, s);
-                if (threadIdx.x == 0) s.best[i] = last;
-            }
-            __syncthreads();
-        }
-        n_pieces = min(n, a.k);
-        if (n_pieces == a.k) tau = (uint32_t)(s.best[a.k - 1] >> 32);
-        __syncthreads();
-        if (threadIdx.x == 0) s.n = 0;
-        __syncthreads();
-        // their tokens from tau on; of a piece with more than k of them the best k
-        for (int i = warp; i < n_pieces; i += kLogitsWarps) {
-            const int p = (int)(0xffffffffu - (uint32_t)s.best[i]) * kPiece + lane * kVec, j0 = p - shift;
-            const uint4 raw = p >= shift && p + kVec <= end ? *reinterpret_cast<const uint4*>(in - shift + p) : load_edge(in, p, shift, end);
-            const T* r = reinterpret_cast<const T*>(&raw);
-            uint32_t keep = ~0u;
-            if (mask) keep = mask_bits(mask, j0, kVec, a.V);
-            if (listed) keep &= ~mask_bits(listed, j0, kVec, a.V);
-            unsigned long long key[kVec];
-            int found = 0;
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                bool use = (keep >> e) & 1u;
-                if (use && on_path(j0 + e))
-                    for (int q = 0; q < a.path_len; ++q) use &= s.path[q] != j0 + e;
-                const uint32_t order = use ? logit_order(Elem<T>::up(r[e])) : 0;
-                key[e] = order >= max(tau, 1u) ? logit_key(order, j0 + e) : 0;
-                found += key[e] != 0;
-            }
-            const int total = __reduce_add_sync(0xffffffffu, found);
-            if (total <= a.k) {
-#pragma unroll
-                for (int e = 0; e < kVec; ++e)
-                    if (key[e]) s.buf[atomicAdd(&s.n, 1)] = key[e];
-            } else {
-                for (int t = 0; t < a.k; ++t) {
-                    unsigned long long best = 0;
-#pragma unroll
-                    for (int e = 0; e < kVec; ++e) best = key[e] > best ? key[e] : best;
-                    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32));
-                    const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32) == hi ? (uint32_t)best : 0u);
-                    best = ((unsigned long long)hi << 32) | lo;
-#pragma unroll
-                    for (int e = 0; e < kVec; ++e)
-                        if (key[e] == best) {
-                            s.buf[atomicAdd(&s.n, 1)] = best;
-                            key[e] = 0;
-                        }
-                }
-            }
-        }
-        __syncthreads();
-    }
-
-    // this thread's share of the streamed sums
+    // this thread's share of the streamed sums, and of the pieces' maxima
     float mx = kNegInf, sum = 0.f;
     auto add = [&](float m, float t) {
         if (m > mx) {
@@ -514,64 +504,169 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_finish_kernel(const __g
         }
         sum += t * exp_fast(m - (mx == kNegInf ? 0.f : mx));
     };
+    const uint32_t* piece = w.piece + (size_t)row * w.pieces;
+    uint32_t held[kHeld], top = 0;               // the thread's first pieces; those of very long rows are read again
+    if (a.k) {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int at = threadIdx.x + i * kLogitsThreads;
+            held[i] = at < w.pieces ? piece[at] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) top = max(top, held[i]);
+        for (int i = threadIdx.x + kHeld * kLogitsThreads; i < w.pieces; i += kLogitsThreads) top = max(top, piece[i]);
+    }
+#pragma unroll 4
     for (int i = threadIdx.x; i < w.parts; i += kLogitsThreads) {
         const float2 v = w.part[(size_t)row * w.parts + i];
         add(v.x, v.y);
     }
-    // the listed tokens, then those of the path that are not listed, one a thread
-    if (known) {
-        const float rep = a.rep ? a.rep[seq] : 1.f, inv = __frcp_rn(rep), freq = a.freq ? a.freq[seq] : 0.f, pres = a.pres ? a.pres[seq] : 0.f;
-        const int2 range = w.range[seq];
-        const int total = range.y + (path ? a.path_len : 0);
-        uint4 entry = make_uint4(0, 0, 0, 0);
-        T raw = Elem<T>::down(0.f);
-        auto fetch = [&](int i) {                // the next entry and its logit are on their way while one is worked on
-            entry.y = 0;
-            if (i < range.y) entry = __ldg(w.entry + range.x + i);
-            else if (i < total) {
-                const int q = i - range.y, token = s.path[q];
-                bool first = token >= 0 && token < a.V && !((listed[token >> 5] >> (token & 31)) & 1u);
-                for (int j = 0; j < q; ++j) first &= s.path[j] != token;          // one of equal tokens stands for all
-                if (first) entry = make_uint4((uint32_t)token, kCountMask + 1, 0, 0);   // marked; counted below
+
+    uint32_t tau = 0;                            // a lower bound of the k-th candidate (logit_order)
+    if (a.k) {
+        // the k largest of the warps' four largest values: k distinct ones, so the k-th bounds what is asked for
+        auto bound_of = [&](uint32_t v) {
+            for (int i = 0; i < 4; ++i) {        // (the barrier behind it also covers s.n)
+                const uint32_t t = __reduce_max_sync(0xffffffffu, v);
+                if (lane == 0) s.warp_u[warp * 4 + i] = t;
+                if (lane == __ffs(__ballot_sync(0xffffffffu, v == t)) - 1) v = 0;
             }
-            if (entry.y) raw = in[entry.x];
+            __syncthreads();
+            return kth_largest(s.warp_u[lane], 32, a.k);
         };
-        fetch(threadIdx.x);
+        // the k pieces with the largest maxima (equal ones: the lower)
+        tau = bound_of(top);
+        const uint32_t floor = max(tau, 1u);
+        auto collect = [&](uint32_t v, int i) {
+            if (v < floor) return;
+            const int at = atomicAdd(&s.n, 1);
+            if (at < kLogitsCap) s.buf[at] = logit_key(v, i);
+        };
+        if (top >= floor) {
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) collect(held[i], threadIdx.x + i * kLogitsThreads);
+            for (int i = threadIdx.x + kHeld * kLogitsThreads; i < w.pieces; i += kLogitsThreads) collect(piece[i], i);
+        }
         __syncthreads();
-        int room = kLogitsCap - s.n;
-        __syncthreads();                         // read by everyone before the first adds to it
-        for (int i0 = 0; i0 < total; i0 += kLogitsThreads) {
-            const uint4 e = entry;
-            float l = Elem<T>::up(raw);
-            const bool extra = i0 + (int)threadIdx.x >= range.y;
-            fetch(i0 + kLogitsThreads + threadIdx.x);
-            uint32_t order = 0;
-            const int token = (int)e.x;
-            if (e.y) {
-                uint32_t n_out = extra ? 0 : e.y & kCountMask;
-                if (on_path(token))
-                    for (int q = 0; q < a.path_len; ++q) n_out += s.path[q] == token;
-                if (n_out || (!extra && (e.y & kSeenBit))) l = l > 0.f ? divide(l, rep, inv) : __fmul_rn(l, rep);
-                if (n_out) l = __fsub_rn(__fsub_rn(l, __fmul_rn(freq, (float)n_out)), pres);
-                if (!extra && (e.y & kBiasBit)) l = __fadd_rn(l, __uint_as_float(e.z));
-                if (nothing || (mask && !((__ldg(mask + (token >> 5)) >> (token & 31)) & 1u))) l = kNegInf;
-                if (a.out) out[token] = Elem<T>::down(l);
-                add(l, 1.f);
-                order = logit_order(l);
+        const int n = s.n, n_pieces = min(n, a.k);
+        // piece number i of this warp, in pos[i]; -1: none
+        int pos[kMost];
+        if (n <= 32) {
+            const unsigned long long key = lane < n ? s.buf[lane] : 0;
+            const int r = warp_rank(key, n);
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) {
+                const int want = warp + i * kLogitsWarps;
+                const unsigned long long k_i = __shfl_sync(0xffffffffu, key, (__ffs(__ballot_sync(0xffffffffu, r == want)) - 1) & 31);
+                pos[i] = want < n_pieces ? (int)(0xffffffffu - (uint32_t)k_i) : -1;
             }
-            if (a.k == 0) continue;
-            if (order && order >= tau) s.buf[atomicAdd(&s.n, 1)] = logit_key(order, token);
-            room -= kLogitsThreads;
-            if (room < kLogitsThreads && i0 + kLogitsThreads < total) {           // uniform: room for one more turn at all times
+            if (n >= a.k)
+                tau = max(tau, (uint32_t)(__shfl_sync(0xffffffffu, key, (__ffs(__ballot_sync(0xffffffffu, r == a.k - 1)) - 1) & 31) >> 32));
+        } else {
+            if (n <= kLogitsCap) rank_keys(n, a.k, s);
+            else {                               // very many pieces with one maximum: k rounds over them
+                unsigned long long last = ~0ull;
+                for (int i = 0; i < a.k; ++i) {
+                    unsigned long long key = 0;
+                    for (int j = threadIdx.x; j < w.pieces; j += kLogitsThreads) {
+                        const unsigned long long mine = logit_key(piece[j], j);
+                        if (mine < last && mine > key) key = mine;
+                    }
+                    last = block_max_key(key, s);
+                    if (threadIdx.x == 0) s.best[i] = last;
+                }
                 __syncthreads();
-                const int n = s.n;
-                rank_keys(n, a.k, s);
-                if (threadIdx.x < 32 && threadIdx.x < a.k) s.buf[threadIdx.x] = s.best[threadIdx.x];
-                if (threadIdx.x == 0) s.n = min(n, a.k);
-                __syncthreads();
-                if (n >= a.k) tau = max(tau, (uint32_t)(s.best[a.k - 1] >> 32));
-                room = kLogitsCap - a.k;
             }
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) {
+                const int want = warp + i * kLogitsWarps;
+                pos[i] = want < n_pieces ? (int)(0xffffffffu - (uint32_t)s.best[want]) : -1;
+            }
+            tau = max(tau, (uint32_t)(s.best[a.k - 1] >> 32));
+        }
+        // their values that may be candidates (logit_order, 0: none)
+        uint32_t val[kMost][kVec], most = 0;
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            const int p = pos[i] * kPiece + lane * kVec, j0 = p - shift;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            uint32_t keep = 0, special = 0;      // allowed; listed or on the path
+            if (pos[i] >= 0) {
+                v = p >= shift && p + kVec <= end ? *reinterpret_cast<const uint4*>(in - shift + p) : load_edge(in, p, shift, end);
+                keep = mask ? mask_bits(mask, j0, kVec, a.V) : ~0u;
+                if (par.listed) special = mask_bits(par.listed, j0, kVec, a.V);
+                if (par.path)
+                    for (int q = 0; q < a.path_len; ++q) {
+                        const int at = par.path[q] - j0;
+                        if (at >= 0 && at < kVec) special |= 1u << at;
+                    }
+            }
+            const T* r = reinterpret_cast<const T*>(&v);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                float l = Elem<T>::up(r[e]);
+                const bool use = (keep >> e) & 1u && p + e >= shift && p + e < end;
+                if (use && ((special >> e) & 1u) && !w.final) l = adjust(l, j0 + e, entry_of(par, w, j0 + e), par, a.path_len);
+                val[i][e] = use ? logit_order(l) : 0;
+                most = max(most, val[i][e]);
+            }
+        }
+        // with few pieces their maxima bound little; lanes' maxima over them do
+        if (n_pieces < a.k) tau = max(tau, bound_of(most));
+        __syncthreads();
+        if (threadIdx.x == 0) s.n = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            int found = 0;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                if (val[i][e] < tau) val[i][e] = 0;
+                found += val[i][e] != 0;
+            }
+            const int j0 = pos[i] * kPiece + lane * kVec - shift, all = __reduce_add_sync(0xffffffffu, found);
+            if (all <= a.k) {
+                if (found)
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e)
+                        if (val[i][e]) s.buf[atomicAdd(&s.n, 1)] = logit_key(val[i][e], j0 + e);
+            } else                               // values that pile up: the best k of the piece
+#pragma unroll 1
+                for (int t = 0; t < a.k; ++t) {
+                    unsigned long long best = 0;
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e) {
+                        const unsigned long long key = logit_key(val[i][e], j0 + e);
+                        best = key > best ? key : best;
+                    }
+                    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32));
+                    const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32) == hi ? (uint32_t)best : 0u);
+                    best = ((unsigned long long)hi << 32) | lo;
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e)
+                        if (val[i][e] && logit_key(val[i][e], j0 + e) == best) {
+                            s.buf[atomicAdd(&s.n, 1)] = best;
+                            val[i][e] = 0;
+                        }
+                }
+        }
+        __syncthreads();
+    }
+
+    if (w.late && par.listed) {                  // every reader of the logits is done: the listed tokens and the path's can be stored
+        const int2 range = w.range[seq];
+        const int total = range.y + (par.path ? a.path_len : 0);
+        __syncthreads();
+        for (int i = threadIdx.x; i < total; i += kLogitsThreads) {
+            int token = i < range.y ? __ldcg(w.token + range.x + i) : par.path[i - range.y];
+            if (i >= range.y) {                  // a path token that is listed, or an equal one before it, is stored already
+                bool first = token >= 0 && token < a.V && !((__ldcg(par.listed + (token >> 5)) >> (token & 31)) & 1u);
+                for (int q = 0; q < i - range.y && first; ++q) first = par.path[q] != token;
+                if (!first) continue;
+            }
+            float l = adjust(Elem<T>::up(in[token]), token, entry_of(par, w, token), par, a.path_len);
+            if (nothing || (mask && !((mask[token >> 5] >> (token & 31)) & 1u))) l = kNegInf;
+            out[token] = Elem<T>::down(l);
         }
     }
     // the row's log-sum-exp, added up in a fixed order, and its candidates
@@ -587,11 +682,21 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_finish_kernel(const __g
     const float lse = base + logf(t);
     if (threadIdx.x == 0 && a.out_lse) a.out_lse[row] = lse;
     if (a.k == 0) return;
-    rank_keys(s.n, a.k, s);
-    if (threadIdx.x < a.k) {
-        const unsigned long long key = s.best[threadIdx.x];
-        a.out_ids[(size_t)row * a.k + threadIdx.x] = key ? (int32_t)(0xffffffffu - (uint32_t)key) : kNoToken;
-        a.out_logprobs[(size_t)row * a.k + threadIdx.x] = key ? logit_unorder((uint32_t)(key >> 32)) - lse : kNegInf;
+    const int n = s.n;
+    unsigned long long key = 0;
+    int at = threadIdx.x;                        // the thread's key and its place
+    if (n <= 32) {
+        if (warp) return;
+        key = lane < n ? s.buf[lane] : 0;
+        at = warp_rank(key, n);
+        if (lane >= n) at = lane;                // places without a key
+    } else {
+        rank_keys(n, a.k, s);
+        if (at < a.k) key = s.best[at];
+    }
+    if (at < a.k) {
+        a.out_ids[(size_t)row * a.k + at] = key ? (int32_t)(0xffffffffu - (uint32_t)key) : kNoToken;
+        a.out_logprobs[(size_t)row * a.k + at] = key ? logit_unorder((uint32_t)(key >> 32)) - lse : kNegInf;
     }
 }
 

@@ -116,8 +116,8 @@ def test_logits_refuses_null_workspaces_and_too_large_calls(lib):
                dict(M=1, n_seq=1 << 29, **lists)):
         a = _largs(**kw)
         assert lib.coral_lmhead_logits_process(ctypes.byref(a), ctypes.c_void_p(P), None) == lmhead.CORAL_ERR_TOO_LARGE
-    # lists cost a bitmap of four words (100 tokens) a sequence and 16 bytes an element, rounded up to 256 bytes each
+    # lists cost two times four words (100 tokens) and a range a sequence and 8 + 4 bytes an element, rounded up to 256 bytes each
     size = lambda **kw: (lib.coral_lmhead_logits_workspace_bytes(ctypes.byref(_largs(**kw)), ctypes.byref(n)), n.value)[1]
     plain = size()
-    assert size(prompt_total=100, output_total=50, **lists) == plain + 256 + 2560 + 256
+    assert size(prompt_total=100, output_total=50, **lists) == plain + 256 + 256 + 1280 + 768 + 256
     assert size(prompt_total=100, output_total=50, **{**lists, "repetition_dev": None}) == plain       # no penalty uses them
