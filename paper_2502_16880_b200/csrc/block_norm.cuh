@@ -8,6 +8,7 @@
 // registers.  A thread copies its own chunks of the next rows into its own shared-memory slots with cp.async, so the
 // loads run ahead of the reductions without registers and without a barrier (only the row sums need one).
 #pragma once
+#include "cp_async.cuh"
 #include "element.cuh"
 
 namespace coral {
@@ -29,11 +30,6 @@ struct NormArgs {
     int want;                                       // ... bits 0 to 2: which of them
 };
 
-__device__ __forceinline__ void cp_async16(void* dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 // All but the newest `left` groups have arrived (left is uniform and at most 3).
 __device__ __forceinline__ void cp_async_wait_left(int left) {
     if (left == 0) cp_async_wait<0>();

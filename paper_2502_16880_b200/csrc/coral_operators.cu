@@ -275,7 +275,8 @@ int launch_q4(const coral_lmhead_q4_config& c, const Q4View& q, const Q4Pass& p,
 
 // ---- logits ----------------------------------------------------------------------------------------------------
 constexpr int kLogitsMaxV = 1 << 30;
-constexpr int kLogitsWideFrom = 8 * 4 * 148 * 2; // pieces of a call from which a warp takes four of them
+constexpr int kLogitsWideBlocks = 4 * 148;       // resident at once
+constexpr int kLogitsWideFrom = 8 * 8 * 148;     // pieces of a call (8 blocks a SM of the kernel for few rows)
 
 bool logits_args_ok(const coral_lmhead_logits_args* a) {
     if (!a || a->struct_size != sizeof(*a)) return false;
@@ -334,18 +335,22 @@ LogitsArgs logits_kernel_args(const coral_lmhead_logits_args* a) {
 
 struct LogitsPlan {
     bool lists;
-    int nv, pieces, parts, blocks;               // pieces of 512 bytes a warp takes; pieces, parts and blocks of a row
+    int chunk, pieces, parts, blocks;            // spans a block takes (0: few rows); pieces of 512 bytes, parts and blocks of a row
     size_t before, entry, token, range, piece, part, bytes;         // offsets in the workspace; the bitmap comes first
 };
 
-// Four pieces a warp, one where the blocks would otherwise leave SMs idle (one row of 128256 fp32: @@NV1@@ us, @@NV4@@ with four).
+// Rows of 128256 with lists, path, mask, result and candidates, fp32 / bf16: 1 row 30 / 36 us with the kernel for few rows,
+// 32 / 40 with the other; 12 rows 36 / 36 and 34 / 36; 60 rows 60 / 52 and 48 / 50; 120 rows 85 / 69 and 60 / 62.  A block takes
+// up to 8 spans one after the other, as long as every SM has its blocks (960 rows: 4 spans 309 / 291, 8 305 / 285, 16 319 / 297,
+// 32 344 / 319, measured before the loop was shortened).
 LogitsPlan logits_plan(const LogitsArgs& k, int type) {
     LogitsPlan p{};
     p.lists = k.prompt || k.output || k.path || k.bias_tokens;
     const int vec = 16 / elem_size(type), span = 32 * vec;
     p.pieces = (int)((k.V + vec - 2LL) / span) + 1;                        // of a row that starts as late as it can
-    p.nv = (long long)k.M * p.pieces >= kLogitsWideFrom ? 4 : 1;
-    p.blocks = (p.pieces - 1) / (kLogitsWarps * p.nv) + 1;
+    const int spans = (p.pieces - 1) / (kWideSpan / span) + 1;
+    if ((long long)k.M * p.pieces >= kLogitsWideFrom) p.chunk = (int)std::min(8LL, std::max(1LL, (long long)k.M * spans / kLogitsWideBlocks));
+    p.blocks = p.chunk ? (spans - 1) / p.chunk + 1 : (p.pieces - 1) / kLogitsWarps + 1;
     p.parts = p.blocks * kLogitsWarps;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t from = at; at = (at + bytes + 255) / 256 * 256; return from; };
@@ -396,12 +401,15 @@ int launch_logits(const LogitsArgs& k, const LogitsPlan& p, unsigned char* ws, c
         if (cudaLaunchKernelEx(&cfg, logits_lists_kernel, k, w) != cudaSuccess) return CORAL_ERR_CUDA;
     }
     const dim3 grid((unsigned)k.M * p.blocks), block(kLogitsThreads);
+    w.chunk = p.chunk;
+    const size_t smem = p.chunk ? LogitsWide<T>::smem(p.lists) : 0;
     if (p.lists) {
-        auto kernel = p.nv == 4 ? logits_stream_kernel<T, 4, true> : logits_stream_kernel<T, 1, true>;
-        if (launch_pdl(kernel, grid, block, 0, st, k, w) != cudaSuccess) return CORAL_ERR_CUDA;
+        auto kernel = p.chunk ? logits_wide_kernel<T, true> : logits_narrow_kernel<T, true>;
+        if (!allow_smem(kernel, smem) || launch_pdl(kernel, grid, block, smem, st, k, w) != cudaSuccess) return CORAL_ERR_CUDA;
     } else {
-        auto kernel = p.nv == 4 ? logits_stream_kernel<T, 4, false> : logits_stream_kernel<T, 1, false>;
-        kernel<<<grid, block, 0, st>>>(k, w);
+        auto kernel = p.chunk ? logits_wide_kernel<T, false> : logits_narrow_kernel<T, false>;
+        if (!allow_smem(kernel, smem)) return CORAL_ERR_CUDA;
+        kernel<<<grid, block, smem, st>>>(k, w);
         if (cudaGetLastError() != cudaSuccess) return CORAL_ERR_CUDA;
     }
     return launch_pdl(logits_finish_kernel<T>, dim3(k.M), block, 0, st, k, w) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;

@@ -7,18 +7,24 @@
 //   logits_lists_kernel   per sequence: counts its token lists into a table in shared memory (whole numbers: the order of the
 //                         atomics does not matter) and writes the listed tokens with their counts and biases in the tokens'
 //                         order, a bitmap of them, and how many lie before each word of it;
-//   logits_stream_kernel  reads the logits, works on the listed tokens (bitmap) and those of the row's path, applies the mask,
-//                         writes the result, and keeps the maximum of every 512 bytes and a (maximum, sum of exponentials)
-//                         of every warp's part;
+//   logits_narrow_kernel, logits_wide_kernel
+//                         read the logits, work on the listed tokens and those of the row's path, apply the mask, write the
+//                         result, and keep the maximum of every 512 bytes and (maximum, sum of exponentials) of a warp's part;
 //   logits_finish_kernel  per row: the log-sum-exp, and the candidates: only the k pieces of 512 bytes with the largest maxima
 //                         can hold one, so only they are read again.
-// (Everything in one kernel, a cluster of blocks a row, took 850 us for 960 x 128256 fp32: candidates and lists cost each block
-// a chain of barriers a row, and their code pushed the streaming loop out of the instruction cache.)
+// 960 rows x 128256 in 16 sequences with lists, path, mask, result and 10 candidates: 216 us fp32, 210 us bf16; of those the
+// lists 17 and the end of the rows 31.  Reading alone takes 97 / 62 us, reading and writing 161 / 87 (bytes: 75 / 38, 151 / 75).
+// What bounds the stream is instructions (13 a logit for reading, 30 with everything; 60% of the issue slots).
+// (Everything in one kernel, a cluster of blocks a row, took 850 us: candidates and lists cost each block a chain of barriers a
+// row, and their code pushed the streaming loop out of the instruction cache.  Listed tokens adjusted by the thread that holds
+// them took 500 to 600 us: a warp with one such token waits for its entry and runs the arithmetic for it alone.  Blocks of one
+// span each took 355 / 288: a span's chain of loads with nothing else on its way.)
 #pragma once
 #include <cooperative_groups.h>
 
 #include <type_traits>
 
+#include "cp_async.cuh"
 #include "element.cuh"
 
 namespace coral {
@@ -58,8 +64,8 @@ struct LogitsWork {
     int32_t* token;                              // which tokens they are
     int2* range;                                 // [n_seq] first entry and number
     uint32_t* piece;                             // [M][pieces] largest value (logit_order) of 512 bytes of logits
-    float2* part;                                // [M][parts] maximum and sum of a warp's vectors
-    int pieces, parts;
+    float2* part;                                // [M][parts] maximum and sum of what a warp took
+    int pieces, parts, chunk;                    // chunk: spans of a row that a block takes; 0: the kernel for few rows
     int late;                                    // over the logits, in 16 bits: the last kernel stores listed tokens
     int final;                                   // over the logits, in 32 bits: the last kernel reads results, not logits
 };
@@ -89,21 +95,29 @@ __device__ __forceinline__ float exp_fast(float t) {
     return r;
 }
 
-// Sum of e^(v - base) over a vector's values, two at a time where there is an instruction for it.
+// e^(v - base) of two values.
+__device__ __forceinline__ unsigned long long exp_pair(float v0, float v1, unsigned long long minus_base) {
+    unsigned long long t = pair_of(v0, v1);
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(t) : "l"(t), "l"(minus_base));
+    float2 f = halves(mul2(t, pair_of(1.4426950408889634f, 1.4426950408889634f)));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(f.x) : "f"(f.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(f.y) : "f"(f.y));
+    return pair_of(f.x, f.y);
+}
+__device__ __forceinline__ unsigned long long add_pair(unsigned long long a, unsigned long long b) {
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(a) : "l"(a), "l"(b));
+    return a;
+}
+// Sums of e^(v - base) over N values (a power of two), as two halves and as a tree.
 template <int N>
-__device__ __forceinline__ float exp_sum(const float (&val)[N], float base) {
-    const unsigned long long nb = pair_of(-base, -base), c = pair_of(1.4426950408889634f, 1.4426950408889634f);
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < N; e += 2) {
-        unsigned long long t = pair_of(val[e], val[e + 1]);
-        asm("add.rn.f32x2 %0, %1, %2;" : "=l"(t) : "l"(t), "l"(nb));
-        float2 f = halves(mul2(t, c));
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(f.x) : "f"(f.x));
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(f.y) : "f"(f.y));
-        sum += f.x + f.y;
-    }
-    return sum;
+__device__ __forceinline__ unsigned long long exp_sum(const float* val, unsigned long long minus_base) {
+    if constexpr (N == 2) return exp_pair(val[0], val[1], minus_base);
+    else return add_pair(exp_sum<N / 2>(val, minus_base), exp_sum<N / 2>(val + N / 2, minus_base));
+}
+// The warp's largest value; NaN only if every one is.
+__device__ __forceinline__ float warp_top(float v) {
+    asm("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(v));
+    return v;
 }
 
 // The k-th largest of the first n lanes' values, in every lane; 0 if there are fewer.
@@ -254,7 +268,8 @@ __device__ __noinline__ uint4 load_edge(const T* in, int p, int shift, int end) 
 }
 // A vector that cannot be stored whole: leaves out what is outside the row and the tokens in `listed`.
 template <typename T, int N>
-__device__ __noinline__ void store_edge(T* to, const float (&val)[N], int p, int shift, int end, uint32_t listed) {
+__device__ __forceinline__ void store_edge(T* to, const float (&val)[N], int p, int shift, int end, uint32_t listed) {
+#pragma unroll
     for (int e = 0; e < N; ++e)
         if (p + e >= shift && p + e < end && !((listed >> e) & 1u)) to[e] = Elem<T>::down(val[e]);
 }
@@ -302,128 +317,292 @@ __device__ __noinline__ float adjust(float l, int token, uint2 e, const LogitsRo
 __device__ __forceinline__ uint32_t entry_at(const LogitsRow& r, int j) {
     return __ldcg(r.before + (j >> 5)) + __popc(__ldcg(r.listed + (j >> 5)) & ((1u << (j & 31)) - 1));
 }
+__device__ __forceinline__ bool is_listed(const LogitsRow& r, int token) { return (__ldcg(r.listed + (token >> 5)) >> (token & 31)) & 1u; }
 __device__ __forceinline__ uint2 entry_of(const LogitsRow& r, const LogitsWork& w, int token) {
-    return (__ldcg(r.listed + (token >> 5)) >> (token & 31)) & 1u ? __ldcg(w.entry + entry_at(r, token)) : make_uint2(0, 0);
+    return is_listed(r, token) ? __ldcg(w.entry + entry_at(r, token)) : make_uint2(0, 0);
 }
 
-// grid: M * ceil(pieces / (8 NV)) blocks of 8 warps; a warp takes NV pieces, 8 apart.
-// LISTS: the call has token lists, paths or biases.
-template <typename T, int NV, bool LISTS>
-__global__ void __launch_bounds__(kLogitsThreads) logits_stream_kernel(const __grid_constant__ LogitsArgs a, const __grid_constant__ LogitsWork w) {
-    constexpr int kVec = LogitsVec<T>::kVec, kPiece = LogitsVec<T>::kPiece, kSpan = kLogitsWarps * NV * kPiece;
-    __shared__ __align__(16) float s_adjusted[LISTS ? kSpan : 1];
-    __shared__ uint32_t s_special[LISTS ? kSpan / 32 : 1];
-    const int per_row = (w.pieces + kLogitsWarps * NV - 1) / (kLogitsWarps * NV);
-    const int row = blockIdx.x / per_row, block = blockIdx.x - row * per_row, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const T* in = reinterpret_cast<const T*>(a.logits) + (size_t)row * a.ld_in;
-    T* out = reinterpret_cast<T*>(a.out) + (a.out ? (size_t)row * a.ld_out : 0);
-    const int shift = (int)((reinterpret_cast<uintptr_t>(in) & 15) / sizeof(T)), end = a.V + shift;
-    const int p_block = block * kSpan, p0 = p_block + warp * kPiece + lane * kVec;
-    // every load the block needs is on its way before the first is waited for
-    const int seq = !LISTS ? -1 : a.row_seq ? a.row_seq[row] : row, mr = !a.mask ? -1 : a.mask_rows ? a.mask_rows[row] : row;
-    uint4 raw[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int p = p0 + i * kLogitsWarps * kPiece;
-        raw[i] = p >= shift && p + kVec <= end ? __ldcs(reinterpret_cast<const uint4*>(in - shift + p)) : load_edge(in, p, shift, end);
+// A row as a block of the streaming kernels sees it.
+template <typename T>
+struct LogitsIn {
+    const T* in;
+    T* out;                                      // null: no result is written
+    int shift, end, seq;
+    bool nothing, vec_out;                       // no token is allowed; vectors of the result start on 16 bytes as those read do
+    const uint32_t* mask;                        // null: every token is allowed
+    __device__ __forceinline__ LogitsIn(const LogitsArgs& a, int row, bool lists) {
+        seq = !lists ? -1 : a.row_seq ? a.row_seq[row] : row;
+        const int mr = !a.mask ? -1 : a.mask_rows ? a.mask_rows[row] : row;
+        in = reinterpret_cast<const T*>(a.logits) + (size_t)row * a.ld_in;
+        out = a.out ? reinterpret_cast<T*>(a.out) + (size_t)row * a.ld_out : nullptr;
+        shift = (int)((reinterpret_cast<uintptr_t>(in) & 15) / sizeof(T));
+        end = a.V + shift;
+        nothing = a.mask && mr >= a.n_masks;                                       // no such mask: allow nothing
+        mask = mr >= 0 && !nothing ? a.mask + (size_t)mr * a.mask_words : nullptr;
+        vec_out = out && (int)((reinterpret_cast<uintptr_t>(out) & 15) / sizeof(T)) == shift;
     }
-    const LogitsRow par = row_params(a, w, row, seq);
-    const bool nothing = mr >= a.n_masks && a.mask;                                // no such mask: allow nothing
-    const uint32_t* const mask = mr >= 0 && !nothing ? a.mask + (size_t)mr * a.mask_words : nullptr;
-    uint32_t keep_word[NV];                      // of the mask, where a vector lies in one word of it
-    if (LISTS) {
-        for (int i = threadIdx.x; i < kSpan / 32; i += kLogitsThreads) s_special[i] = 0;
-        pdl_wait();                              // what follows of the lists comes from the kernel before
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int p = p0 + i * kLogitsWarps * kPiece, at = min(p, a.V - 1) >> 5;
-        keep_word[i] = mask && shift == 0 ? __ldg(mask + at) : 0;
-    }
-    if (LISTS && par.listed) {                   // one thread a token that is listed or on the path, wherever it lies in the block
-        const int lo = max(p_block - shift, 0), hi = min(p_block + kSpan - shift, a.V);
-        uint32_t first = 0;
-        int n = 0;
-        if (lo < hi) first = entry_at(par, lo);  // (the last block of a row may lie behind its end)
-        if (lo >= hi) n = 0;
-        else if (hi < a.V) n = (int)(entry_at(par, hi) - first);
-        else {
-            const int2 range = __ldcg(w.range + seq);
-            n = range.x + range.y - (int)first;
-        }
-        __syncthreads();
-        const int total = n + (par.path ? a.path_len : 0);
-#pragma unroll 1
-        for (int i = threadIdx.x; i < total; i += kLogitsThreads) {
-            int token;
-            uint2 entry = make_uint2(0, 0);
-            if (i < n) {
-                token = __ldcg(w.token + first + i);
-                entry = __ldcg(w.entry + first + i);
-            } else {
-                token = par.path[i - n];
-                if (token < lo || token >= hi || (__ldcg(par.listed + (token >> 5)) >> (token & 31)) & 1u) continue;
-            }
-            const int at = token + shift - p_block;
-            s_adjusted[at] = adjust_inline(Elem<T>::up(in[token]), token, entry, par, a.path_len);
-            atomicOr(&s_special[at >> 5], 1u << (at & 31));
-        }
-        __syncthreads();
-    }
-    const bool vec_out = a.out && (int)((reinterpret_cast<uintptr_t>(out) & 15) / sizeof(T)) == shift;
-    float val[NV][kVec];
-    uint32_t top[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int p = p0 + i * kLogitsWarps * kPiece;
-        const T* r = reinterpret_cast<const T*>(&raw[i]);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) val[i][e] = Elem<T>::up(r[e]);
-        uint32_t keep = nothing ? 0u : ~0u;      // bit e: token p + e - shift is allowed
-        if (mask) keep = shift == 0 ? keep_word[i] >> (p & 31) : mask_bits(mask, p - shift, kVec, a.V);
-        const uint32_t special = LISTS && par.listed ? (s_special[(p - p_block) >> 5] >> (p & 31)) & ((1u << kVec) - 1) : 0;
-        if (LISTS && special) {
-#pragma unroll
-            for (int e = 0; e < kVec; ++e)
-                if ((special >> e) & 1u) val[i][e] = s_adjusted[p - p_block + e];
-        }
+    __device__ __forceinline__ bool whole(int p) const { return p >= shift && p + LogitsVec<T>::kVec <= end; }
+    // the word of the mask that holds the vector at p, where one word does
+    __device__ __forceinline__ uint32_t keep_word(int p, int V) const { return mask && shift == 0 ? __ldg(mask + (min(p, V - 1) >> 5)) : 0; }
+    // Masks and writes the vector at p; the largest of its values.  skip: positions that are not written.  PLAIN: the vector is
+    // whole, it can be stored whole, and one word of the mask holds it.
+    template <bool PLAIN>
+    __device__ __forceinline__ float finish(float (&val)[LogitsVec<T>::kVec], int p, uint32_t word, uint32_t skip, int V) const {
+        constexpr int kVec = LogitsVec<T>::kVec;
         if (mask || nothing) {
+            const uint32_t keep = nothing ? 0u : PLAIN || shift == 0 ? word >> (p & 31) : mask_bits(mask, p - shift, kVec, V);
 #pragma unroll
             for (int e = 0; e < kVec; ++e)
-                if (!(keep & (1u << e))) val[i][e] = kNegInf;
+                if (!(keep & (1u << e))) val[e] = kNegInf;
         }
-        if (a.out) {
+        if (out) {
             T* to = out - shift + p;
-            const uint32_t skip = LISTS && w.late ? special : 0;
-            if (vec_out && p >= shift && p + kVec <= end && !skip) {
+            if ((PLAIN || (vec_out && whole(p))) && !skip) {
                 uint4 o;
                 T* t = reinterpret_cast<T*>(&o);
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) t[e] = Elem<T>::down(val[i][e]);
+                for (int e = 0; e < kVec; ++e) t[e] = Elem<T>::down(val[e]);
                 __stcs(reinterpret_cast<uint4*>(to), o);
-            } else store_edge(to, val[i], p, shift, end, skip);
+            } else store_edge(to, val, p, shift, end, skip);
         }
-        float m = val[i][0];
+        float m = val[0];
 #pragma unroll
-        for (int e = 1; e < kVec; ++e) m = fmaxf(m, val[i][e]);
-        top[i] = __reduce_max_sync(0xffffffffu, logit_order(m));
+        for (int e = 1; e < kVec; ++e) m = fmaxf(m, val[e]);
+        return m;
     }
-    uint32_t all = top[0];
+};
+
+// Few rows: a block of 8 warps takes 8 pieces, so that many SMs share a row.  grid: M * ceil(pieces / 8).
+// LISTS: the call has token lists, paths or biases.
+template <typename T, bool LISTS>
+__global__ void __launch_bounds__(kLogitsThreads) logits_narrow_kernel(const __grid_constant__ LogitsArgs a, const __grid_constant__ LogitsWork w) {
+    constexpr int kVec = LogitsVec<T>::kVec, kPiece = LogitsVec<T>::kPiece, kSpan = kLogitsWarps * kPiece;
+    __shared__ __align__(16) float s_adjusted[LISTS ? kSpan : 1];
+    __shared__ uint32_t s_special[LISTS ? kSpan / 32 : 1];
+    const int per_row = (w.pieces + kLogitsWarps - 1) / kLogitsWarps;
+    const int row = blockIdx.x / per_row, block = blockIdx.x - row * per_row, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const LogitsIn<T> r(a, row, LISTS);
+    const int p_block = block * kSpan, p = p_block + threadIdx.x * kVec;
+    const uint4 raw = r.whole(p) ? __ldcs(reinterpret_cast<const uint4*>(r.in - r.shift + p)) : load_edge(r.in, p, r.shift, r.end);
+    const uint32_t word = r.keep_word(p, a.V);
+    uint32_t special = 0;
+    float val[kVec];
 #pragma unroll
-    for (int i = 1; i < NV; ++i) all = max(all, top[i]);
-    const float base = all ? logit_unorder(all) : 0.f;
-    float sum = 0.f;
+    for (int e = 0; e < kVec; ++e) val[e] = Elem<T>::up(reinterpret_cast<const T*>(&raw)[e]);
+    if (LISTS) {
+        const LogitsRow par = row_params(a, w, row, r.seq);
+        for (int i = threadIdx.x; i < kSpan / 32; i += kLogitsThreads) s_special[i] = 0;
+        pdl_wait();                              // what follows of the lists comes from the kernel before
+        if (par.listed) {                        // one thread a token that is listed or on the path, wherever it lies in the block
+            const int lo = max(p_block - r.shift, 0), hi = min(p_block + kSpan - r.shift, a.V);
+            uint32_t first = 0;
+            int n = 0;                           // (the last block of a row may lie behind its end)
+            if (lo < hi) {
+                first = entry_at(par, lo);
+                if (hi < a.V) n = (int)(entry_at(par, hi) - first);
+                else {
+                    const int2 range = __ldcg(w.range + r.seq);
+                    n = range.x + range.y - (int)first;
+                }
+            }
+            __syncthreads();
+            const int total = n + (par.path ? a.path_len : 0);
+#pragma unroll 1
+            for (int i = threadIdx.x; i < total; i += kLogitsThreads) {
+                int token;
+                uint2 entry = make_uint2(0, 0);
+                if (i < n) {
+                    token = __ldcg(w.token + first + i);
+                    entry = __ldcg(w.entry + first + i);
+                } else {
+                    token = par.path[i - n];
+                    if (token < lo || token >= hi || is_listed(par, token)) continue;
+                }
+                const int at = token + r.shift - p_block;
+                s_adjusted[at] = adjust_inline(Elem<T>::up(r.in[token]), token, entry, par, a.path_len);
+                atomicOr(&s_special[at >> 5], 1u << (at & 31));
+            }
+            __syncthreads();
+            special = (s_special[(p - p_block) >> 5] >> (p & 31)) & ((1u << kVec) - 1);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) sum += exp_sum(val[i], base);
-    sum = warp_sum(sum);
-    const int piece = block * kLogitsWarps * NV + warp;
-    if (lane < NV && piece + lane * kLogitsWarps < w.pieces) {
-        uint32_t t = top[0];
-#pragma unroll
-        for (int i = 1; i < NV; ++i) t = lane == i ? top[i] : t;
-        w.piece[(size_t)row * w.pieces + piece + lane * kLogitsWarps] = t;
+            for (int e = 0; e < kVec; ++e)
+                if ((special >> e) & 1u) val[e] = s_adjusted[p - p_block + e];
+        }
     }
-    if (lane == 0) w.part[(size_t)row * w.parts + block * kLogitsWarps + warp] = make_float2(all ? base : kNegInf, sum);
+    const float top = warp_top(r.template finish<false>(val, p, word, w.late ? special : 0, a.V)), base = top > kNegInf ? top : 0.f;
+    const float2 two = halves(exp_sum<kVec>(val, pair_of(-base, -base)));
+    const float sum = warp_sum(two.x + two.y);
+    const int piece = block * kLogitsWarps + warp;
+    if (lane == 0) {
+        if (piece < w.pieces) w.piece[(size_t)row * w.pieces + piece] = logit_order(top);
+        w.part[(size_t)row * w.parts + piece] = make_float2(top > kNegInf ? top : kNegInf, sum);
+    }
+    pdl_launch_dependents();
+}
+
+// Many rows: a block takes w.chunk neighbouring spans of a row one after the other.  Every thread copies its own vectors of the
+// next spans into its own slots, so that loads are in flight all the time, and the next listed tokens' entries are loaded a span
+// ahead (the tokens are in order: those of a span are the next ones below its end).
+// grid: M * ceil(spans / chunk)
+constexpr int kWideSpan = 4096;
+template <typename T>
+struct LogitsWide {
+    static constexpr int kNV = kWideSpan * (int)sizeof(T) / (16 * kLogitsThreads), kStages = sizeof(T) == 4 ? 3 : 4;
+    static constexpr int kRaw = kStages * kWideSpan * (int)sizeof(T);
+    // 32 bits: listed tokens are adjusted where they lie; 16 bits: in fp32 copies behind them
+    static constexpr int smem(bool lists) { return kRaw + (lists && sizeof(T) == 2 ? kWideSpan * 4 : 0); }
+};
+template <typename T, bool LISTS>
+__global__ void __launch_bounds__(kLogitsThreads, 4) logits_wide_kernel(const __grid_constant__ LogitsArgs a, const __grid_constant__ LogitsWork w) {
+    constexpr int kVec = LogitsVec<T>::kVec, kPiece = LogitsVec<T>::kPiece, kNV = LogitsWide<T>::kNV, kStages = LogitsWide<T>::kStages;
+    extern __shared__ __align__(16) uint4 wide_raw[];                  // [kStages][kNV][threads]
+    __shared__ uint32_t s_special[2][LISTS ? kWideSpan / 32 : 1];
+    constexpr int kSpanPieces = kWideSpan / kPiece;
+    const int spans = (w.pieces + kSpanPieces - 1) / kSpanPieces, per_row = w.parts / kLogitsWarps;
+    const int row = blockIdx.x / per_row, block = blockIdx.x - row * per_row, s0 = block * w.chunk, s1 = min(s0 + w.chunk, spans);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const LogitsIn<T> r(a, row, LISTS);
+    auto inner = [&](int s) { return s * kWideSpan >= r.shift && (s + 1) * kWideSpan <= r.end; };
+    const bool plain_row = (!r.out || r.vec_out) && (!r.mask || r.shift == 0);
+    int to_stage = 0;
+    auto load = [&](int s) {
+        uint4* to = wide_raw + to_stage * (kNV * kLogitsThreads) + threadIdx.x;
+        const T* from = r.in - r.shift + (size_t)s * kWideSpan + threadIdx.x * kVec;
+        if (s < s1) {
+            if (inner(s)) {
+#pragma unroll
+                for (int i = 0; i < kNV; ++i) cp_async16(to + i * kLogitsThreads, from + i * kLogitsThreads * kVec);
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < kNV; ++i) {
+                    const int p = s * kWideSpan + (i * kLogitsThreads + threadIdx.x) * kVec;
+                    if (r.whole(p)) cp_async16(to + i * kLogitsThreads, from + i * kLogitsThreads * kVec);
+                    else to[i * kLogitsThreads] = load_edge(r.in, p, r.shift, r.end);
+                }
+            }
+        }
+        cp_async_commit();
+        to_stage = to_stage + 1 == kStages ? 0 : to_stage + 1;
+    };
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) load(s0 + i);
+    const LogitsRow par = row_params(a, w, row, r.seq);
+    uint32_t word[kNV];                          // the next span's words of the mask
+#pragma unroll
+    for (int i = 0; i < kNV; ++i) word[i] = r.keep_word(s0 * kWideSpan + (i * kLogitsThreads + threadIdx.x) * kVec, a.V);
+    constexpr int kNone = 0x7fffffff;
+    int token = kNone, path_token = kNone, next = 0, last = 0;         // the thread's next listed token, its token of the path; entries
+    uint2 entry = make_uint2(0, 0);
+    auto fetch = [&] {
+        token = kNone;
+        if (next + (int)threadIdx.x < last) {
+            token = __ldcg(w.token + next + threadIdx.x);
+            entry = __ldcg(w.entry + next + threadIdx.x);
+        }
+    };
+    if (LISTS) {
+        if (threadIdx.x < kWideSpan / 32) s_special[0][threadIdx.x] = 0;
+        pdl_wait();                              // what follows of the lists comes from the kernel before
+        if (par.listed) {
+            const int lo = max(s0 * kWideSpan - r.shift, 0);
+            if (lo < a.V) {                      // (the last span of a row may lie behind its end)
+                const int2 range = __ldcg(w.range + r.seq);
+                next = (int)entry_at(par, lo);
+                last = range.x + range.y;
+            }
+            fetch();
+            if (par.path && (int)threadIdx.x < a.path_len) {
+                path_token = par.path[threadIdx.x];
+                if (path_token < 0 || path_token >= a.V || is_listed(par, path_token)) path_token = kNone;
+            }
+        }
+    }
+    float base = kNegInf;                        // the warp's largest value so far, and the thread's sums of e^(value - base)
+    unsigned long long sum = pair_of(0.f, 0.f);
+    int stage = 0;
+#pragma unroll 1
+    for (int s = s0; s < s1; ++s, stage = stage + 1 == kStages ? 0 : stage + 1) {
+        uint4* raw = wide_raw + stage * (kNV * kLogitsThreads);
+        float* adjusted = reinterpret_cast<float*>(sizeof(T) == 4 ? raw : wide_raw + LogitsWide<T>::kRaw / 16);
+        const int p_span = s * kWideSpan;
+        cp_async_wait<kStages - 2>();
+        if (LISTS && par.listed) {               // one thread a token that is listed or on the path, wherever it lies in the span
+            if (sizeof(T) == 2)
+#pragma unroll
+                for (int i = 0; i < kNV; ++i) {
+                    const int v = i * kLogitsThreads + threadIdx.x;
+                    const uint4 x = raw[v];
+#pragma unroll
+                    for (int e = 0; e < kVec; e += 4) {
+                        const T* t = reinterpret_cast<const T*>(&x) + e;
+                        *reinterpret_cast<float4*>(adjusted + v * kVec + e) = make_float4(Elem<T>::up(t[0]), Elem<T>::up(t[1]), Elem<T>::up(t[2]), Elem<T>::up(t[3]));
+                    }
+                }
+            __syncthreads();
+            uint32_t* marks = s_special[(s - s0) & 1];
+            auto put = [&](int t, uint2 e) {
+                const int at = t + r.shift - p_span;
+                adjusted[at] = adjust_inline(adjusted[at], t, e, par, a.path_len);
+                if (w.late) atomicOr(&marks[at >> 5], 1u << (at & 31));
+            };
+            if (w.late && threadIdx.x < kWideSpan / 32) s_special[(s - s0 + 1) & 1][threadIdx.x] = 0;
+            const int lo = p_span - r.shift, hi = lo + kWideSpan;
+            if (path_token >= lo && path_token < hi) put(path_token, make_uint2(0, 0));
+            int found;
+            do {
+                const bool here = token < hi;
+                if (here) put(token, entry);
+                found = __syncthreads_count(here);
+                next += found;
+                if (found) fetch();
+            } while (found == kLogitsThreads);
+        }
+        load(s + kStages - 1);
+        auto work = [&](auto plain) {
+            float val[kNV][kVec], top[kNV];
+#pragma unroll
+            for (int i = 0; i < kNV; ++i) {
+                const int v = i * kLogitsThreads + threadIdx.x, p = p_span + v * kVec;
+                uint32_t skip = 0;
+                if (LISTS && sizeof(T) == 2 && par.listed) {
+#pragma unroll
+                    for (int e = 0; e < kVec; e += 4) *reinterpret_cast<float4*>(&val[i][e]) = *reinterpret_cast<const float4*>(adjusted + v * kVec + e);
+                    if (w.late) skip = (s_special[(s - s0) & 1][(v * kVec) >> 5] >> (p & 31)) & ((1u << kVec) - 1);
+                } else {
+                    const uint4 x = raw[v];
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e) val[i][e] = Elem<T>::up(reinterpret_cast<const T*>(&x)[e]);
+                }
+                top[i] = warp_top(r.template finish<decltype(plain)::value>(val[i], p, word[i], skip, a.V));
+            }
+            if (r.mask)
+#pragma unroll
+                for (int i = 0; i < kNV; ++i) word[i] = r.keep_word(p_span + kWideSpan + (i * kLogitsThreads + threadIdx.x) * kVec, a.V);
+            float all = top[0];
+#pragma unroll
+            for (int i = 1; i < kNV; ++i) all = fmaxf(all, top[i]);
+            if (all > base) {
+                const float f = exp_fast(base - all);
+                sum = mul2(sum, pair_of(f, f));
+                base = all;
+            }
+            const float from = base > kNegInf ? base : 0.f;
+            sum = add_pair(sum, exp_sum<kNV * kVec>(&val[0][0], pair_of(-from, -from)));
+            const int piece = s * kSpanPieces + warp + lane * kLogitsWarps;
+            if (a.k && lane < kNV && piece < w.pieces) {
+                float t = top[0];
+#pragma unroll
+                for (int i = 1; i < kNV; ++i) t = lane == i ? top[i] : t;
+                w.piece[(size_t)row * w.pieces + piece] = logit_order(t);
+            }
+        };
+        if (plain_row && inner(s)) work(std::true_type{});
+        else work(std::false_type{});
+    }
+    const float2 two = halves(sum);
+    const float total = warp_sum(two.x + two.y);
+    if (lane == 0) w.part[(size_t)row * w.parts + block * kLogitsWarps + warp] = make_float2(base, total);
+    cp_async_wait<0>();
     pdl_launch_dependents();
 }
 

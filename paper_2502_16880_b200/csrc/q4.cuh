@@ -15,7 +15,7 @@
 // shift and mask, and the activations are staged in that order.  A group of 32 columns is one word a lane, so every group
 // size that is a multiple of 32 ends on a word.  Scales (and zero points) follow: [tile][block][16 rows][128 / group].
 #pragma once
-#include "block_norm.cuh"                        // cp.async helpers
+#include "cp_async.cuh"
 #include "element.cuh"
 
 namespace coral {

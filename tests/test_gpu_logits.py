@@ -1,9 +1,11 @@
 """GPU parity of the logits step.  Processed logits and candidate ids are the oracle's float32 steps bit for bit.
 
-Tolerance of the log-sum-exp.  u = 2^-24.  A thread adds 16 exponentials a chunk, a warp 5, a block 16 and a cluster 16 partial
-sums, each rescaled once; an exponential is off by 2 ulp and its argument, at most 40 where it still counts, by one rounding:
-the sum is off by at most (16 * passes + 37 + 6 + 40) u relative, which is what the logarithm is off by absolutely; adding the
-maximum and subtracting from a logit round once each.
+Tolerance of the log-sum-exp.  u = 2^-24.  A thread adds the exponentials of a span of 4096 tokens in a tree (4 additions at most)
+and up to 8 spans one after the other, each rescaled once; a warp's 32 sums take 5 additions, a row's parts (64 tokens of a span
+each at least) 1 a thread and a rescaling for every 256 of them, then 5 and 8: fewer than 16 (V // 65536 + 1) + 37 + 6.  An
+exponential is off by 2 ulp and its argument, at most 40 where it still counts, by one rounding: the sum is off by at most
+(16 (V // 65536 + 1) + 43 + 40) u relative, which is what the logarithm is off by absolutely; adding the maximum and subtracting
+from a logit round once each.
 """
 import numpy as np
 import pytest
