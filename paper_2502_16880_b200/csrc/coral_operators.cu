@@ -412,7 +412,7 @@ int launch_logits(const LogitsArgs& k, const LogitsPlan& p, unsigned char* ws, c
         kernel<<<grid, block, smem, st>>>(k, w);
         if (cudaGetLastError() != cudaSuccess) return CORAL_ERR_CUDA;
     }
-    return launch_pdl(logits_finish_kernel<T>, dim3(k.M), block, 0, st, k, w) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+    return launch_pdl(logits_finish_kernel<T>, dim3(k.M), dim3(kFinishThreads), 0, st, k, w) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
 }
 
 }  // namespace

@@ -607,12 +607,15 @@ __global__ void __launch_bounds__(kLogitsThreads, 4) logits_wide_kernel(const __
 }
 
 // ---- the end of a row ----------------------------------------------------------------------------------------
+constexpr int kFinishThreads = 512, kFinishWarps = kFinishThreads / 32;
+constexpr int kFinishTops = 32 / kFinishWarps;     // of a warp's values, for a first bound
 struct LogitsShared {
     unsigned long long buf[kLogitsCap];
+    uint32_t value[kFinishWarps][256];           // a piece of a warp's (logit_order)
     unsigned long long best[32];
-    unsigned long long warp_key[kLogitsWarps];
+    unsigned long long warp_key[kFinishWarps];
     uint32_t warp_u[32];
-    float warp_m[kLogitsWarps], warp_s[kLogitsWarps];
+    float warp_m[kFinishWarps], warp_s[kFinishWarps];
     int n;
 };
 
@@ -628,7 +631,7 @@ __device__ __forceinline__ unsigned long long block_max_key(unsigned long long k
     __syncthreads();
     unsigned long long best = 0;
 #pragma unroll
-    for (int w = 0; w < kLogitsWarps; ++w) best = s.warp_key[w] > best ? s.warp_key[w] : best;
+    for (int w = 0; w < kFinishWarps; ++w) best = s.warp_key[w] > best ? s.warp_key[w] : best;
     return best;
 }
 
@@ -638,9 +641,9 @@ __device__ __noinline__ void rank_keys(int n, int k, LogitsShared& s) {
     __syncthreads();
     if (threadIdx.x < 32) s.best[threadIdx.x] = 0;
     __syncthreads();
-    const int log2s = n <= kLogitsThreads / 16 ? 4 : n <= kLogitsThreads / 8 ? 3 : n <= kLogitsThreads / 4 ? 2 : n <= kLogitsThreads / 2 ? 1 : 0;
+    const int log2s = n <= kFinishThreads / 16 ? 4 : n <= kFinishThreads / 8 ? 3 : n <= kFinishThreads / 4 ? 2 : n <= kFinishThreads / 2 ? 1 : 0;
     const int share = 1 << log2s;
-    for (int i = 0; (i >> log2s) < n; i += kLogitsThreads) {
+    for (int i = 0; (i >> log2s) < n; i += kFinishThreads) {
         const int at = (i + threadIdx.x) >> log2s;
         const unsigned long long mine = at < n ? s.buf[at] : ~0ull;
         int r = 0;
@@ -660,8 +663,8 @@ __device__ __forceinline__ int warp_rank(unsigned long long key, int n) {
 
 // grid: M blocks.
 template <typename T>
-__global__ void __launch_bounds__(kLogitsThreads) logits_finish_kernel(const __grid_constant__ LogitsArgs a, const __grid_constant__ LogitsWork w) {
-    constexpr int kVec = LogitsVec<T>::kVec, kPiece = LogitsVec<T>::kPiece, kMost = 32 / kLogitsWarps, kHeld = 8;
+__global__ void __launch_bounds__(kFinishThreads) logits_finish_kernel(const __grid_constant__ LogitsArgs a, const __grid_constant__ LogitsWork w) {
+    constexpr int kVec = LogitsVec<T>::kVec, kPiece = LogitsVec<T>::kPiece, kMost = 32 / kFinishWarps, kHeld = 4;
     __shared__ LogitsShared s;
     const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const T* in = reinterpret_cast<const T*>(a.logits) + (size_t)row * a.ld_in;
@@ -688,26 +691,27 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_finish_kernel(const __g
     if (a.k) {
 #pragma unroll
         for (int i = 0; i < kHeld; ++i) {
-            const int at = threadIdx.x + i * kLogitsThreads;
+            const int at = threadIdx.x + i * kFinishThreads;
             held[i] = at < w.pieces ? piece[at] : 0;
         }
 #pragma unroll
         for (int i = 0; i < kHeld; ++i) top = max(top, held[i]);
-        for (int i = threadIdx.x + kHeld * kLogitsThreads; i < w.pieces; i += kLogitsThreads) top = max(top, piece[i]);
+        for (int i = threadIdx.x + kHeld * kFinishThreads; i < w.pieces; i += kFinishThreads) top = max(top, piece[i]);
     }
 #pragma unroll 4
-    for (int i = threadIdx.x; i < w.parts; i += kLogitsThreads) {
+    for (int i = threadIdx.x; i < w.parts; i += kFinishThreads) {
         const float2 v = w.part[(size_t)row * w.parts + i];
         add(v.x, v.y);
     }
 
     uint32_t tau = 0;                            // a lower bound of the k-th candidate (logit_order)
     if (a.k) {
-        // the k largest of the warps' four largest values: k distinct ones, so the k-th bounds what is asked for
+        // the k largest of the warps' largest values: k distinct ones, so the k-th bounds what is asked for
         auto bound_of = [&](uint32_t v) {
-            for (int i = 0; i < 4; ++i) {        // (the barrier behind it also covers s.n)
+#pragma unroll
+            for (int i = 0; i < kFinishTops; ++i) { // (the barrier behind it also covers s.n)
                 const uint32_t t = __reduce_max_sync(0xffffffffu, v);
-                if (lane == 0) s.warp_u[warp * 4 + i] = t;
+                if (lane == 0) s.warp_u[warp * kFinishTops + i] = t;
                 if (lane == __ffs(__ballot_sync(0xffffffffu, v == t)) - 1) v = 0;
             }
             __syncthreads();
@@ -723,8 +727,8 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_finish_kernel(const __g
         };
         if (top >= floor) {
 #pragma unroll
-            for (int i = 0; i < kHeld; ++i) collect(held[i], threadIdx.x + i * kLogitsThreads);
-            for (int i = threadIdx.x + kHeld * kLogitsThreads; i < w.pieces; i += kLogitsThreads) collect(piece[i], i);
+            for (int i = 0; i < kHeld; ++i) collect(held[i], threadIdx.x + i * kFinishThreads);
+            for (int i = threadIdx.x + kHeld * kFinishThreads; i < w.pieces; i += kFinishThreads) collect(piece[i], i);
         }
         __syncthreads();
         const int n = s.n, n_pieces = min(n, a.k);
@@ -735,7 +739,7 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_finish_kernel(const __g
             const int r = warp_rank(key, n);
 #pragma unroll
             for (int i = 0; i < kMost; ++i) {
-                const int want = warp + i * kLogitsWarps;
+                const int want = warp + i * kFinishWarps;
                 const unsigned long long k_i = __shfl_sync(0xffffffffu, key, (__ffs(__ballot_sync(0xffffffffu, r == want)) - 1) & 31);
                 pos[i] = want < n_pieces ? (int)(0xffffffffu - (uint32_t)k_i) : -1;
             }
@@ -747,7 +751,7 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_finish_kernel(const __g
                 unsigned long long last = ~0ull;
                 for (int i = 0; i < a.k; ++i) {
                     unsigned long long key = 0;
-                    for (int j = threadIdx.x; j < w.pieces; j += kLogitsThreads) {
+                    for (int j = threadIdx.x; j < w.pieces; j += kFinishThreads) {
                         const unsigned long long mine = logit_key(piece[j], j);
                         if (mine < last && mine > key) key = mine;
                     }
@@ -758,76 +762,94 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_finish_kernel(const __g
             }
 #pragma unroll
             for (int i = 0; i < kMost; ++i) {
-                const int want = warp + i * kLogitsWarps;
+                const int want = warp + i * kFinishWarps;
                 pos[i] = want < n_pieces ? (int)(0xffffffffu - (uint32_t)s.best[want]) : -1;
             }
             tau = max(tau, (uint32_t)(s.best[a.k - 1] >> 32));
         }
-        // their values that may be candidates (logit_order, 0: none)
-        uint32_t val[kMost][kVec], most = 0;
-#pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-            const int p = pos[i] * kPiece + lane * kVec, j0 = p - shift;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            uint32_t keep = 0, special = 0;      // allowed; listed or on the path
-            if (pos[i] >= 0) {
-                v = p >= shift && p + kVec <= end ? *reinterpret_cast<const uint4*>(in - shift + p) : load_edge(in, p, shift, end);
-                keep = mask ? mask_bits(mask, j0, kVec, a.V) : ~0u;
-                if (par.listed) special = mask_bits(par.listed, j0, kVec, a.V);
-                if (par.path)
-                    for (int q = 0; q < a.path_len; ++q) {
-                        const int at = par.path[q] - j0;
-                        if (at >= 0 && at < kVec) special |= 1u << at;
-                    }
-            }
-            const T* r = reinterpret_cast<const T*>(&v);
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                float l = Elem<T>::up(r[e]);
-                const bool use = (keep >> e) & 1u && p + e >= shift && p + e < end;
-                if (use && ((special >> e) & 1u) && !w.final) l = adjust(l, j0 + e, entry_of(par, w, j0 + e), par, a.path_len);
-                val[i][e] = use ? logit_order(l) : 0;
-                most = max(most, val[i][e]);
-            }
-        }
-        // with few pieces their maxima bound little; lanes' maxima over them do
-        if (n_pieces < a.k) tau = max(tau, bound_of(most));
-        __syncthreads();
-        if (threadIdx.x == 0) s.n = 0;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-            int found = 0;
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                if (val[i][e] < tau) val[i][e] = 0;
-                found += val[i][e] != 0;
-            }
-            const int j0 = pos[i] * kPiece + lane * kVec - shift, all = __reduce_add_sync(0xffffffffu, found);
-            if (all <= a.k) {
-                if (found)
-#pragma unroll
-                    for (int e = 0; e < kVec; ++e)
-                        if (val[i][e]) s.buf[atomicAdd(&s.n, 1)] = logit_key(val[i][e], j0 + e);
-            } else                               // values that pile up: the best k of the piece
+        // Their values that may be candidates.  With few pieces their maxima bound little: a first pass takes a bound from lanes'
+        // maxima over all their values.
 #pragma unroll 1
-                for (int t = 0; t < a.k; ++t) {
-                    unsigned long long best = 0;
-#pragma unroll
-                    for (int e = 0; e < kVec; ++e) {
-                        const unsigned long long key = logit_key(val[i][e], j0 + e);
-                        best = key > best ? key : best;
-                    }
-                    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32));
-                    const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32) == hi ? (uint32_t)best : 0u);
-                    best = ((unsigned long long)hi << 32) | lo;
-#pragma unroll
-                    for (int e = 0; e < kVec; ++e)
-                        if (val[i][e] && logit_key(val[i][e], j0 + e) == best) {
-                            s.buf[atomicAdd(&s.n, 1)] = best;
-                            val[i][e] = 0;
+        for (int pass = n_pieces < a.k ? 0 : 1; pass < 2; ++pass) {
+            uint32_t most = 0;
+            if (pass == 1) {
+                __syncthreads();
+                if (threadIdx.x == 0) s.n = 0;
+                __syncthreads();
+            }
+#pragma unroll 1
+            for (int i = 0; i < kMost; ++i) {
+                const int at_piece = i == 0 ? pos[0] : pos[1];
+                if (at_piece < 0) break;         // (the warp's others are none either)
+                const int p = at_piece * kPiece + lane * kVec, j0 = p - shift;
+                const uint4 v = p >= shift && p + kVec <= end ? *reinterpret_cast<const uint4*>(in - shift + p) : load_edge(in, p, shift, end);
+                const uint32_t keep = nothing ? 0u : mask ? mask_bits(mask, j0, kVec, a.V) : ~0u;
+                uint32_t special = 0, val[kVec]; // listed or on the path; logit_order, 0: no candidate
+                if (par.listed && !w.final) {
+                    special = mask_bits(par.listed, j0, kVec, a.V);
+                    if (par.path)
+                        for (int q = 0; q < a.path_len; ++q) {
+                            const int at = par.path[q] - j0;
+                            if (at >= 0 && at < kVec) special |= 1u << at;
                         }
                 }
+                uint32_t in_row = 0;
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) {
+                    if (p + e >= shift && p + e < end) in_row |= 1u << e;
+                    const bool use = (keep >> e) & 1u && p + e >= shift && p + e < end;
+                    val[e] = use ? logit_order(Elem<T>::up(reinterpret_cast<const T*>(&v)[e])) : 0;
+                }
+                if (__any_sync(0xffffffffu, special & keep & in_row)) {
+                    uint32_t* mine = s.value[warp] + lane * kVec;
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e) mine[e] = val[e];
+                    for (uint32_t left = special & keep & in_row & ((1u << kVec) - 1); left; left &= left - 1) {
+                        const int e = __ffs(left) - 1, j = j0 + e;
+                        mine[e] = logit_order(adjust(Elem<T>::up(in[j]), j, entry_of(par, w, j), par, a.path_len));
+                    }
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e) val[e] = mine[e];
+                    __syncwarp();
+                }
+                if (pass == 0) {
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e) most = max(most, val[e]);
+                    continue;
+                }
+                int found = 0;
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) {
+                    if (val[e] < tau) val[e] = 0;
+                    found += val[e] != 0;
+                }
+                const int all = __reduce_add_sync(0xffffffffu, found);
+                if (all <= a.k) {
+                    if (found)
+#pragma unroll
+                        for (int e = 0; e < kVec; ++e)
+                            if (val[e]) s.buf[atomicAdd(&s.n, 1)] = logit_key(val[e], j0 + e);
+                } else                           // values that pile up: the best k of the piece
+#pragma unroll 1
+                    for (int t = 0; t < a.k; ++t) {
+                        unsigned long long best = 0;
+#pragma unroll
+                        for (int e = 0; e < kVec; ++e) {
+                            const unsigned long long key = logit_key(val[e], j0 + e);
+                            best = key > best ? key : best;
+                        }
+                        const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32));
+                        const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32) == hi ? (uint32_t)best : 0u);
+                        best = ((unsigned long long)hi << 32) | lo;
+#pragma unroll
+                        for (int e = 0; e < kVec; ++e)
+                            if (val[e] && logit_key(val[e], j0 + e) == best) {
+                                s.buf[atomicAdd(&s.n, 1)] = best;
+                                val[e] = 0;
+                            }
+                    }
+            }
+            if (pass == 0) tau = max(tau, bound_of(most));
         }
         __syncthreads();
     }
@@ -836,7 +858,7 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_finish_kernel(const __g
         const int2 range = w.range[seq];
         const int total = range.y + (par.path ? a.path_len : 0);
         __syncthreads();
-        for (int i = threadIdx.x; i < total; i += kLogitsThreads) {
+        for (int i = threadIdx.x; i < total; i += kFinishThreads) {
             int token = i < range.y ? __ldcg(w.token + range.x + i) : par.path[i - range.y];
             if (i >= range.y) {                  // a path token that is listed, or an equal one before it, is stored already
                 bool first = token >= 0 && token < a.V && !((__ldcg(par.listed + (token >> 5)) >> (token & 31)) & 1u);
@@ -854,10 +876,10 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_finish_kernel(const __g
     __syncthreads();
     float m = s.warp_m[0], t = 0.f;
 #pragma unroll
-    for (int i = 1; i < kLogitsWarps; ++i) m = fmaxf(m, s.warp_m[i]);
+    for (int i = 1; i < kFinishWarps; ++i) m = fmaxf(m, s.warp_m[i]);
     const float base = m == kNegInf ? 0.f : m;
 #pragma unroll
-    for (int i = 0; i < kLogitsWarps; ++i) t += s.warp_s[i] * exp_fast(s.warp_m[i] - base);
+    for (int i = 0; i < kFinishWarps; ++i) t += s.warp_s[i] * exp_fast(s.warp_m[i] - base);
     const float lse = base + logf(t);
     if (threadIdx.x == 0 && a.out_lse) a.out_lse[row] = lse;
     if (a.k == 0) return;
