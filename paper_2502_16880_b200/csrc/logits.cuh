@@ -414,6 +414,7 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_narrow_kernel(const __g
                 if (i < n) {
                     token = __ldcg(w.token + first + i);
                     entry = __ldcg(w.entry + first + i);
+                    if (token < lo || token >= hi) continue;           // decreasing offsets: another sequence wrote here
                 } else {
                     token = par.path[i - n];
                     if (token < lo || token >= hi || is_listed(par, token)) continue;
@@ -550,7 +551,7 @@ __global__ void __launch_bounds__(kLogitsThreads, 4) logits_wide_kernel(const __
             if (path_token >= lo && path_token < hi) put(path_token, make_uint2(0, 0));
             int found;
             do {
-                const bool here = token < hi;
+                const bool here = token >= lo && token < hi;           // (below lo: decreasing offsets, another sequence wrote here)
                 if (here) put(token, entry);
                 found = __syncthreads_count(here);
                 next += found;

@@ -417,6 +417,15 @@ def _op_stream(stream, dev) -> int:
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
+def _op_scratch(n, device, stream):
+    """Scratch of one call, of the pool of the stream that runs it: what had the memory before and what gets it next run on
+    that stream too, before and behind the call."""
+    if stream is None:
+        return torch.empty(n, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=torch.uint8, device=device)
+
+
 _NORM_SIZE = ctypes.sizeof(coral_lmhead_norm_args)
 
 
@@ -596,11 +605,9 @@ def coral_lmhead_logits_process(logits, *, row_seq=None, prompt_tokens=None, pro
         _op_ptr("out_lse", out_lse, f32, (M,), dev))
     lib, n = _lib or load_library(), ctypes.c_size_t(0)
     _check(lib.coral_lmhead_logits_workspace_bytes(ctypes.byref(a), ctypes.byref(n)), "coral_lmhead_logits_workspace_bytes")
-    workspace = torch.empty(n.value, dtype=torch.uint8, device=logits.device)
+    workspace = _op_scratch(n.value, logits.device, stream)
     _check(lib.coral_lmhead_logits_process(ctypes.byref(a), workspace.data_ptr(), _op_stream(stream, dev)),
            "coral_lmhead_logits_process")
-    if stream is not None:
-        workspace.record_stream(stream)
 
 
 def coral_lmhead_destroy(handle) -> None:
@@ -685,8 +692,5 @@ class Q4Linear:
         if out is None:
             out = torch.empty((M, self.cfg.N), dtype=out_dtype, device=x.device)
         n = coral_lmhead_q4_workspace_bytes(self.cfg, M)
-        workspace = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
-        coral_lmhead_q4_linear(self.cfg, self.packed, x, out, workspace, stream)
-        if stream is not None and n:
-            workspace.record_stream(stream)
+        coral_lmhead_q4_linear(self.cfg, self.packed, x, out, _op_scratch(n, x.device, stream) if n else None, stream)
         return out

@@ -287,3 +287,45 @@ def test_binding_refuses_wrong_tensors():
         call(torch.zeros(64, 4, device="cuda").t(), out_ids=ids, out_logprobs=lps)
     with pytest.raises(lmhead.CoralError):
         call(x, out_ids=torch.empty(4, 33, dtype=torch.int32, device="cuda"), out_logprobs=torch.empty(4, 33, device="cuda"))
+
+
+def test_scratch_belongs_to_the_stream_that_runs_the_call():
+    """Memory that another stream still has work on must not become the scratch of a call."""
+    M, V = 64, 5000
+    logits, d = _random(12, M, V, torch.float32, 4, 200, 100, 3, 5)
+    want = _run(logits, 10, **d)
+    st = torch.cuda.Stream()
+    kw = dict(out_ids=torch.empty(M, 10, dtype=torch.int32, device="cuda"), out_logprobs=torch.empty(M, 10, device="cuda"),
+              out_lse=torch.empty(M, device="cuda"))
+    x = logits.cuda()
+    plain = _run(logits, 10, write=False)
+    torch.cuda.synchronize()
+    for kb in (8, 16, 64, 256, 1024):                        # whatever size the scratch has
+        old = [torch.empty(kb << 10, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        torch.cuda._sleep(20_000_000)                        # ~10 ms before the current stream writes to it
+        for o in old:
+            o.fill_(255)
+        del old, o
+        lmhead.coral_lmhead_logits_process(x, stream=st, **kw)
+        torch.cuda.synchronize()
+        assert np.array_equal(kw["out_ids"].cpu().numpy(), plain["ids"]) and np.array_equal(kw["out_lse"].cpu().numpy(), plain["lse"])
+    assert not np.array_equal(want["ids"], plain["ids"])
+
+
+def test_decreasing_offsets_stay_in_bounds():
+    """Offsets that go back (a caller's mistake): the sequences whose lists do not overlap are right, nothing else is touched."""
+    M, V = 200, 9000
+    rng = np.random.default_rng(13)
+    logits = torch.from_numpy(rng.normal(size=(M, V)).astype(np.float32))
+    tok = torch.from_numpy(rng.integers(0, V, 600).astype(np.int32)).cuda()
+    off = torch.tensor([0, 400, 100, 380, 390], device="cuda")                    # [0, 400), none, [100, 380), [380, 390)
+    seq = torch.tensor([m % 5 - 1 for m in range(M)], dtype=torch.int32)
+    out = torch.full((M + 2, V), 7.0, device="cuda")
+    for rows in (M, 3):                                                           # both kernels: many rows and few
+        lmhead.coral_lmhead_logits_process(logits[:rows].cuda(), row_seq=seq[:rows].cuda(), output_tokens=tok, output_offsets=off,
+                                           presence=torch.ones(4, device="cuda"), out_logits=out[1:rows + 1])
+        torch.cuda.synchronize()
+        assert torch.all(out[0] == 7) and torch.all(out[M + 1] == 7)
+        for m in range(rows):
+            if seq[m] in (-1, 1):
+                assert torch.equal(out[m + 1].cpu(), logits[m]), m

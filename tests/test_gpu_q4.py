@@ -143,3 +143,19 @@ def test_binding_refuses_wrong_tensors():
         lmhead.Q4Linear(Wq.cuda(), s.float().cuda())
     with pytest.raises(ValueError):
         lmhead.Q4Linear(Wq.cuda(), s.cuda(), z[:, :2].contiguous().cuda())
+
+
+def test_status_of_a_workspace():
+    """Calls of many rows leave their status in the workspace, the others have none."""
+    Wq, s, z, x = _make(6, 33, 300, 512, 64, False, torch.bfloat16, torch.bfloat16)
+    lin, x = _linear(Wq, s, z), x.cuda()
+    n = lmhead.coral_lmhead_q4_workspace_bytes(lin.cfg, 33)
+    assert n > 0 and lmhead.coral_lmhead_q4_workspace_bytes(lin.cfg, 1) == 0
+    out = torch.empty(33, 300, device="cuda")
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    lmhead.coral_lmhead_q4_linear(lin.cfg, lin.packed, x, out, ws)
+    assert lmhead.coral_lmhead_q4_status(ws) == 0
+    _check(out, Wq, s, z, x.cpu(), 64)
+    for bad in (None, torch.empty(n - 1, dtype=torch.uint8, device="cuda"), torch.empty(n, dtype=torch.uint8)):
+        with pytest.raises((ValueError, lmhead.CoralError)):
+            lmhead.coral_lmhead_q4_linear(lin.cfg, lin.packed, x, out, bad)
