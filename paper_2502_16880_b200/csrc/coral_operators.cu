@@ -3,6 +3,8 @@
 
 #include <cuda_runtime.h>
 
+#include <algorithm>
+
 #include "block_norm.cuh"
 #include "launch.cuh"
 #include "logits.cuh"
@@ -166,8 +168,26 @@ int q4_split(int T, int KB, int sms) {
     return best;
 }
 
+// Passes of 256 output rows on the tensor cores: every SM takes as many as all can, and those left over are split by columns, so
+// that they do not cost a whole pass (152064 x 3584 has 594 of them for 148 SMs: 157 -> 138 us with 60 rows and groups of 128, 218 -> 185 with
+// groups of 64; 4096 x 4096 has 16: 40 -> 19.5).  A part has 256 columns at least.
+Q4Share q4_share(int T, int KB, int sms) {
+    const int passes = (T - 1) / kQ4TcTiles + 1;
+    Q4Share s{};
+    s.full = passes / sms;
+    s.tail = passes % sms;
+    s.split = s.tail ? std::max(1, std::min({sms / s.tail, kQ4TcMaxSplit, KB / 2})) : 1;
+    return s;
+}
+// ... and the most memory their parts take, whatever the number of SMs.
+size_t q4_part_bytes(int T, int KB, int slab_rows) {
+    const long long passes = (T - 1) / kQ4TcTiles + 1;
+    const long long parts = std::min<long long>(kQ4TcMaxParts, passes * std::max(1, std::min(kQ4TcMaxSplit, KB / 2)));
+    return (size_t)parts * slab_rows * 256 * sizeof(float);
+}
+
 // The passes over the rows of a call: up to 64 rows each on the tensor cores while more than 16 are left (152064 x 3584, groups of
-// 64: 198 us at 17 rows and 228 at 64; the warps' MMA takes 103 for every 16), then up to 16 on the warps' MMA, fewer where very
+// 64: 158 us at 17 rows and 185 at 64; the warps' MMA takes 103 for every 16), then up to 16 on the warps' MMA, fewer where very
 // long rows do not fit shared memory.  Rows that a block would spend long on scaling are laid out first, in the caller's workspace.
 constexpr int kQ4StageUnits = 1024;              // 8-column pieces that a block of the product scales itself
 
@@ -211,7 +231,8 @@ bool q4_next_pass(const coral_lmhead_q4_config& c, int KB, int M, int* first, si
             p->bytes = p->back_bytes + p->sum_bytes + up((size_t)p->rows * KB * 256);
         }
     }
-    if (p->bytes && *at == 0) *at = 256;         // the status word comes first
+    // the status word comes first, then the parts of the widest tensor-core pass, the first one
+    if (p->bytes && *at == 0) *at = 256 + (p->slab_rows ? q4_part_bytes((c.N - 1) / 16 + 1, KB, p->slab_rows) : 0);
     p->at = *at;
     *at += p->bytes;
     *first += p->rows;
@@ -233,15 +254,21 @@ int launch_q4_pass(const Q4View& q, const Q4Pass& p, const void* x_all, void* ou
         if (cudaGetLastError() != cudaSuccess) return CORAL_ERR_CUDA;
     }
     if (p.slab_rows) {
-        const int grid = q.T < sms ? q.T : sms;
+        Q4Share share = q4_share(q.T, q.KB, sms);
+        share.part = reinterpret_cast<float*>(ws + 256);
+        const int grid = share.full ? sms : share.tail * share.split;
         DeviceState* state = reinterpret_cast<DeviceState*>(ws);
         auto run = [&](auto kernel, size_t smem) {
-            return allow_smem(kernel, smem) && launch_pdl(kernel, dim3(grid), dim3(kQ4TcThreads), smem, st, q, s, p.rows, out, out_type,
-                                                          state) == cudaSuccess;
+            return allow_smem(kernel, smem) && launch_pdl(kernel, dim3(grid), dim3(kQ4TcThreads), smem, st, q, s, share, p.rows, out,
+                                                          out_type, state) == cudaSuccess;
         };
         const bool ok = p.slab_rows == 32 ? run(q4_tc_kernel<32, PER, ZEROS>, q4_tc_smem_bytes<32>())
                                           : run(q4_tc_kernel<64, PER, ZEROS>, q4_tc_smem_bytes<64>());
-        return ok ? CORAL_OK : CORAL_ERR_CUDA;
+        if (!ok) return CORAL_ERR_CUDA;
+        if (share.split > 1 && launch_pdl(q4_join_kernel, dim3(share.tail, p.rows), dim3(256), 0, st, share, share.full * sms * 256, p.slab_rows,
+                                          q.N, out, out_type) != cudaSuccess)
+            return CORAL_ERR_CUDA;
+        return CORAL_OK;
     }
     const int split = q4_split(q.T, q.KB, sms);
     const long long units = (long long)q.T * split;              // warps that have a tile to work on
@@ -490,6 +517,7 @@ int coral_lmhead_q4_linear(const coral_lmhead_q4_config* cfg, const void* packed
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int sms = 0;
     if (!device_sms(&sms)) return CORAL_ERR_CUDA;
+    if (sms > kQ4TcMaxParts) sms = kQ4TcMaxParts;
     const Q4Layout L = q4_layout(*cfg);
     Q4View q{};
     q.w = static_cast<const uint4*>(packed_dev);

@@ -6,6 +6,8 @@
 //   * one thread issues the MMAs of a group of columns, accumulating from zero,
 //   * the same eight warps read a finished group's sums back, scale them in fp32 and add them up in registers.
 // Operands and sums of two groups are in flight, so a group is unpacked while the tensor cores work on the one before.
+// Each tile has its own barriers and its own issuing thread: one thread alone issues an MMA every 45 cycles, two of them keep the
+// 32 that one takes (152064 x 3584, 60 rows: 181 -> 157 us with groups of 128, 226 -> 218 with groups of 64).
 // The activations (laid out by q4_stage_kernel, swizzled) come through a ring of 64-column slabs, one bulk copy each, shared by
 // the block's 256 output rows.
 #pragma once
@@ -14,11 +16,19 @@
 
 namespace coral {
 
-constexpr int kQ4TcWarps = 8;                      // unpacking warps; warp 8 issues the MMAs, warp 9 the copies
-constexpr int kQ4TcThreads = (kQ4TcWarps + 2) * 32;
+constexpr int kQ4TcWarps = 8;                      // unpacking warps; warps 8 and 9 issue the MMAs of a tile each, warp 10 the copies
+constexpr int kQ4TcThreads = (kQ4TcWarps + 3) * 32;
 constexpr int kQ4TcTiles = 16;                     // 16-row weight tiles of a pass: two MMA tiles of 128 rows
 constexpr int kQ4TcSlabs = 8;                      // slabs of activations in flight
 constexpr int kQ4TcMaxRows = 64;                   // activation rows of a launch
+constexpr int kQ4TcMaxSplit = 16, kQ4TcMaxParts = 160;
+
+// Who computes what: block i takes the passes (256 output rows each) i, i + full_step, ... of the first `full` a block, and then
+// one of the `tail` passes left over, or a part of its columns: they are split into `split` parts where that keeps more SMs busy.
+struct Q4Share {
+    int full, tail, split;
+    float* part;                                   // [tail * split][activation row][256] sums of the parts
+};
 
 template <int MP>
 constexpr size_t q4_tc_smem_bytes() { return 1024 + (size_t)kQ4TcSlabs * MP * 128 + MP * 4 + 256; }
@@ -44,10 +54,10 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint
         ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// grid: any number of blocks; block i takes the weight tiles [T i / grid, T (i + 1) / grid).  K columns are PER groups a block of
-// 128; `st` holds the slabs of MP rows.
+// grid: the SMs, or tail * split blocks if there are no full passes.  K columns are PER groups a block of 128; `st` holds the
+// slabs of MP rows.
 template <int MP, int PER, bool ZEROS>
-__global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Staged st, int M, void* __restrict__ out, int out_type, DeviceState* state) {
+__global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Staged st, Q4Share share, int M, void* __restrict__ out, int out_type, DeviceState* state) {
     extern __shared__ unsigned char q4_smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(q4_smem_raw) + 1023) & ~(uintptr_t)1023);
     constexpr int kSlabBytes = MP * 128;
@@ -55,19 +65,19 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
     float* s_back = reinterpret_cast<float*>(smem + (size_t)kQ4TcSlabs * kSlabBytes);
     uint64_t* x_full = reinterpret_cast<uint64_t*>(s_back + MP);
     uint64_t* x_empty = x_full + kQ4TcSlabs;
-    uint64_t* a_full = x_empty + kQ4TcSlabs;       // [2] a group's operands are in tensor memory (and the buffer's old sums out)
-    uint64_t* d_full = a_full + 2;                 // [2] its sums are
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(d_full + 2);
+    uint64_t* a_full = x_empty + kQ4TcSlabs;       // [tile][2] a group's operands are in tensor memory (and the buffer's old sums out)
+    uint64_t* d_full = a_full + 4;                 // [2][2] its sums are
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(d_full + 4);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kQ4TcSlabs; ++i) {
             mbar_init(smem_u32(&x_full[i]), 1);
-            mbar_init(smem_u32(&x_empty[i]), 1);
+            mbar_init(smem_u32(&x_empty[i]), 2);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&a_full[i]), kQ4TcWarps);
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(smem_u32(&a_full[i]), kQ4TcWarps / 2);
             mbar_init(smem_u32(&d_full[i]), 1);
         }
         *abort_flag = 0;
@@ -86,18 +96,24 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
     auto d_at = [&](int tile, int buf) { return tmem + (uint32_t)((tile * 2 + buf) * MP); };
     auto a_at = [&](int tile, int buf) { return tmem + (uint32_t)(4 * MP + (tile * 2 + buf) * 64); };
 
-    const int t_lo = (int)((long long)q.T * blockIdx.x / gridDim.x), t_hi = (int)((long long)q.T * (blockIdx.x + 1) / gridDim.x);
-    const int passes = (t_hi - t_lo + kQ4TcTiles - 1) / kQ4TcTiles;
+    const int passes = share.full + ((int)blockIdx.x < share.tail * share.split ? 1 : 0);
     constexpr int kGroupCols = 128 / PER;
     const int groups = q.K / kGroupCols, slabs = (q.K + 63) / 64;
+    // a pass of this block: its first 16-row weight tile and its blocks of 128 columns
+    auto tile_of = [&](int pass) {
+        return (pass < share.full ? pass * (int)gridDim.x + (int)blockIdx.x : share.full * (int)gridDim.x + (int)blockIdx.x / share.split) * kQ4TcTiles;
+    };
+    auto from_block = [&](int pass) { return pass < share.full ? 0 : (int)(blockIdx.x % share.split) * q.KB / share.split; };
+    auto to_block = [&](int pass) { return pass < share.full ? q.KB : ((int)(blockIdx.x % share.split) + 1) * q.KB / share.split; };
 
-    if (warp == kQ4TcWarps + 1) {
+    if (warp == kQ4TcWarps + 2) {
         if (lane == 0) {
             pdl_wait();
             int stage = 0;
             uint32_t phase = 0;
+            int copies = 0;
             for (int pass = 0; pass < passes; ++pass)
-                for (int i = 0; i < slabs; ++i) {
+                for (int i = from_block(pass) * 2; i < min(to_block(pass) * 2, slabs); ++i, ++copies) {
                     tc_wait(smem_u32(&x_empty[stage]), phase ^ 1u, abort_flag, state);
                     const uint32_t bar = smem_u32(&x_full[stage]);
                     mbar_expect_tx(bar, kSlabBytes);
@@ -105,18 +121,18 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
                     if (++stage == kQ4TcSlabs) { stage = 0; phase ^= 1u; }
                 }
             // nothing is left on its way when the block ends, an expired wait elsewhere included
-            const int copies = passes * slabs;
             for (int i = 0; i < kQ4TcSlabs && i < copies; ++i)
                 tc_wait(smem_u32(&x_full[i]), (uint32_t)((copies - 1 - i) / kQ4TcSlabs) & 1u, abort_flag, state);
         }
-    } else if (warp == kQ4TcWarps) {
+    } else if (warp >= kQ4TcWarps) {
         if (lane == 0) {
+            const int tile = warp - kQ4TcWarps;
             int stage = 0, unit = 0;
             uint32_t phase = 0;
             for (int pass = 0; pass < passes; ++pass)
-                for (int g = 0; g < groups; ++g, ++unit) {
+                for (int g = from_block(pass) * PER, to = min(to_block(pass) * PER, groups); g < to; ++g, ++unit) {
                     const int buf = unit & 1;
-                    tc_wait(smem_u32(&a_full[buf]), (uint32_t)(unit >> 1) & 1u, abort_flag, state);
+                    tc_wait(smem_u32(&a_full[tile * 2 + buf]), (uint32_t)(unit >> 1) & 1u, abort_flag, state);
                     constexpr int kSteps = kGroupCols / 16;            // MMAs of a group and tile; 4 a slab
 #pragma unroll
                     for (int k0 = 0; k0 < kSteps; k0 += 4) {
@@ -127,18 +143,16 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
 #pragma unroll
                         for (int kk = 0; kk < (kSteps < 4 ? kSteps : 4); ++kk) {
                             const uint64_t bdesc = tc_smem_desc(sb + (half + kk) * 32);
-#pragma unroll
-                            for (int tile = 0; tile < 2; ++tile)
-                                tc_mma_ts(d_at(tile, buf), a_at(tile, buf) + (uint32_t)((k0 + kk) * 8), bdesc, kIdesc, k0 + kk > 0 ? 1u : 0u);
+                            tc_mma_ts(d_at(tile, buf), a_at(tile, buf) + (uint32_t)((k0 + kk) * 8), bdesc, kIdesc, k0 + kk > 0 ? 1u : 0u);
                         }
-                        if (PER != 4 || half == 2 || g + 1 == groups) {
+                        if (PER != 4 || half == 2 || g + 1 == to) {
                             tc_commit(smem_u32(&x_empty[stage]));
                             if (++stage == kQ4TcSlabs) { stage = 0; phase ^= 1u; }
                         }
                     }
-                    tc_commit(smem_u32(&d_full[buf]));
+                    tc_commit(smem_u32(&d_full[tile * 2 + buf]));
                 }
-            if (unit > 0) tc_wait(smem_u32(&d_full[(unit - 1) & 1]), (uint32_t)((unit - 1) >> 1) & 1u, abort_flag, state);
+            if (unit > 0) tc_wait(smem_u32(&d_full[tile * 2 + ((unit - 1) & 1)]), (uint32_t)((unit - 1) >> 1) & 1u, abort_flag, state);
         }
     } else {
         const int tile = warp >> 2, row = (warp & 3) * 32 + lane;          // this thread's row of its 128-row tile
@@ -151,26 +165,22 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
         asm volatile("bar.sync 1, 256;" ::: "memory");
         int unit = 0;
         for (int pass = 0; pass < passes; ++pass) {
-            // this pass's tiles, spread evenly over the passes and the two MMA tiles
-            const int left = t_hi - t_lo - (int)((long long)(t_hi - t_lo) * pass / passes);
-            const int n = (int)((long long)(t_hi - t_lo) * (pass + 1) / passes) - (t_hi - t_lo - left);
-            const int first = t_hi - left + (tile ? (n + 1) / 2 : 0), mine = tile ? n / 2 : (n + 1) / 2;
-            const bool live = (row >> 4) < mine;
-            const int t16 = first + (row >> 4);
-            const size_t blk0 = (size_t)t16 * q.KB;
+            const int first = tile_of(pass) + tile * 8, t16 = first + (row >> 4), kb0 = from_block(pass), kb1 = to_block(pass);
+            const bool live = t16 < q.T;
+            const size_t blk0 = live ? (size_t)t16 * q.KB : 0;
             const uint4* wp = q.w + blk0 * 64 + ((row >> 3) & 1) * 32 + (row & 7) * 4;
             const unsigned char* sp = q.sz + (blk0 * 16 + (row & 15)) * kSz;
             uint4 w[2][4];                                             // two blocks of 128 columns ahead
             Q4Scales<PER, ZEROS> sc[2];
             auto fetch = [&](int d, int b) {
-                if (!live || b >= q.KB) return;
+                if (!live || b >= kb1) return;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) w[d][c] = __ldg(wp + (size_t)b * 64 + c);
                 sc[d].load(sp + (size_t)b * 16 * kSz);
-                if (b + 8 < q.KB) asm volatile("prefetch.global.L2 [%0];" ::"l"(wp + (size_t)(b + 8) * 64));
+                if (b + 8 < kb1) asm volatile("prefetch.global.L2 [%0];" ::"l"(wp + (size_t)(b + 8) * 64));
             };
-            fetch(0, 0);
-            fetch(1, 1);
+            fetch(0, kb0);
+            fetch(1, kb0 + 1);
             unsigned long long acc[MP / 2];
 #pragma unroll
             for (int i = 0; i < MP / 2; ++i) acc[i] = 0;
@@ -178,7 +188,7 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
             // the sums of the group two before: out of tensor memory, scaled, added
             auto drain = [&](int u) {
                 const int buf = u & 1;
-                tc_wait(smem_u32(&d_full[buf]), (uint32_t)(u >> 1) & 1u, abort_flag, state);
+                tc_wait(smem_u32(&d_full[tile * 2 + buf]), (uint32_t)(u >> 1) & 1u, abort_flag, state);
                 tc_fence_after();
                 const unsigned long long s2 = pair_of(s_old, s_old);
 #pragma unroll
@@ -190,16 +200,16 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
                 }
             };
 #pragma unroll 1
-            for (int b0 = 0; b0 < q.KB; b0 += 2) {
+            for (int b0 = kb0; b0 < kb1; b0 += 2) {
 #pragma unroll
                 for (int d = 0; d < 2; ++d) {
                     const int b = b0 + d;
-                    if (b >= q.KB) break;
+                    if (b >= kb1) break;
 #pragma unroll
                     for (int gi = 0; gi < PER; ++gi) {
                         const int g = b * PER + gi;
                         if (g >= groups) break;
-                        if (g >= 2) drain(unit - 2);
+                        if (g >= kb0 * PER + 2) drain(unit - 2);
                         s_old = s_new;
                         s_new = live ? sc[d].scale(gi, q.scale_half) : 0.f;
                         // zero points as subnormals, once as they are and once times 16
@@ -224,17 +234,25 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
                         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&a_full[unit & 1]));
+                        if (lane == 0) mbar_arrive(smem_u32(&a_full[tile * 2 + (unit & 1)]));
                         ++unit;
                     }
                     fetch(d, b + 2);
                 }
             }
-            if (groups >= 2) drain(unit - 2);
+            if (min(kb1 * PER, groups) >= kb0 * PER + 2) drain(unit - 2);
             s_old = s_new;
             drain(unit - 1);
             const long long n_row = (long long)t16 * 16 + (row & 15);
-            if (live && n_row < q.N) {
+            if (pass >= share.full && share.split > 1) {
+                float* to = share.part + (size_t)blockIdx.x * MP * 256 + tile * 128 + row;
+#pragma unroll
+                for (int i = 0; i < MP / 2; ++i) {
+                    const float2 f = halves(acc[i]);
+                    if (2 * i < M) to[(size_t)(2 * i) * 256] = f.x * s_back[2 * i];
+                    if (2 * i + 1 < M) to[(size_t)(2 * i + 1) * 256] = f.y * s_back[2 * i + 1];
+                }
+            } else if (live && n_row < q.N) {
 #pragma unroll
                 for (int i = 0; i < MP / 2; ++i) {
                     const float2 f = halves(acc[i]);
@@ -250,6 +268,19 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
+    pdl_launch_dependents();
+}
+
+// Adds up the parts of the tail passes, in order.  grid: tail passes x activation rows; 256 threads, one an output row.
+__global__ void __launch_bounds__(256) q4_join_kernel(Q4Share share, int first_row, int MP, int N, void* __restrict__ out, int out_type) {
+    const long long n = first_row + (long long)blockIdx.x * 256 + threadIdx.x;
+    pdl_wait();
+    if (n >= N) return;
+    const float* from = share.part + ((size_t)blockIdx.x * share.split * MP + blockIdx.y) * 256 + threadIdx.x;
+    float sum = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < share.split; ++i) sum += __ldcg(from + (size_t)i * MP * 256);
+    store_as(out, (size_t)blockIdx.y * N + n, sum, out_type);
 }
 
 }  // namespace coral
