@@ -319,8 +319,8 @@ __global__ void __launch_bounds__(kNormMaxThreads) block_norm_backward_kernel(No
     pdl_launch_dependents();
 }
 
-// Column sums of the partial rows [n][3][H]: a block takes 32 columns, its warps every eighth partial row.
-constexpr int kNormColWarps = 8;
+// Column sums of the partial rows [n][3][H]: a block takes 32 columns, its warps every sixteenth partial row.
+constexpr int kNormColWarps = 16;
 __global__ void __launch_bounds__(kNormColWarps * 32) block_norm_columns_kernel(const float* __restrict__ part, int n, int H,
                                                                                float* d_w_pre, float* d_w_post, float* d_gate) {
     __shared__ float s[kNormColWarps][32];
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(kNormColWarps * 32) block_norm_columns_kernel(
     float acc = 0.f;
     if (col < H) {
         const float* p = part + (size_t)blockIdx.y * H + col;
-#pragma unroll 4
+#pragma unroll 8
         for (int i = warp; i < n; i += kNormColWarps) acc += p[(size_t)i * 3 * H];
     }
     s[warp][lane] = acc;
