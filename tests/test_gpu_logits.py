@@ -329,3 +329,32 @@ def test_decreasing_offsets_stay_in_bounds():
         for m in range(rows):
             if seq[m] in (-1, 1):
                 assert torch.equal(out[m + 1].cpu(), logits[m]), m
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("M,V,plen", [(300, 9001, 3000), (400, 60001, 6000), (200, 32768, 10)])
+def test_many_rows_alignment_in_place_and_special_values(M, V, plen, t):
+    """The pipelined kernel: one span a block and several, dense lists (more than a block's threads in a span), rows that start on
+    any address, in place, rows that allow nothing, infinities and NaN in masked and in allowed places."""
+    logits, d = _random(M + V, M, V, t, 7, plen, plen // 2, 5, 30)
+    bad = [float("inf"), float("-inf"), float("nan")]
+    for i in range(0, M, 5):
+        logits[i, (i * 37) % V] = bad[i % 3]
+    d["mask"][3] = 0
+    d["mask_rows"][9:12] = torch.tensor([3, M, 2 ** 31 - 1], dtype=torch.int32)       # nothing, and no such mask
+    d["rep"][2], d["rep"][4] = 1.0, 0.7
+    rows = sorted({0, 1, 4, 5, 9, 10, 11, M // 2, M - 2, M - 1, *range(0, M, max(5, M // 40 * 5))})[:40]
+    for off, ld, ooff, old in [(0, V, 0, V), (3, V + 5, 1, V + 2)]:
+        buf = torch.full((off + ld * M + 8,), 3.0, dtype=t, device="cuda")
+        obuf = torch.full((ooff + old * M + 8,), 4.0, dtype=t, device="cuda")
+        x = buf[off:off + ld * M].view(M, ld)[:, :V]
+        o = obuf[ooff:ooff + old * M].view(M, old)[:, :V]
+        x.copy_(logits)
+        _check(_run(logits, 10, logits_dev=x, out=o, **d), logits, 10, rows=rows, **d)
+        touched = torch.zeros_like(obuf, dtype=torch.bool)
+        touched[ooff:ooff + old * M].view(M, old)[:, :V] = True
+        assert torch.all(obuf[~touched] == 4.0)
+        apart = o.clone()
+        _check(_run(logits, 10, logits_dev=x, out=x, **d), logits, 10, rows=rows[:6], **d)
+        assert torch.equal(torch.nan_to_num(x, nan=9.0), torch.nan_to_num(apart, nan=9.0))
+        assert torch.all(buf[off:off + ld * M].view(M, ld)[:, V:] == 3.0)

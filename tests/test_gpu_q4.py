@@ -159,3 +159,16 @@ def test_status_of_a_workspace():
     for bad in (None, torch.empty(n - 1, dtype=torch.uint8, device="cuda"), torch.empty(n, dtype=torch.uint8)):
         with pytest.raises((ValueError, lmhead.CoralError)):
             lmhead.coral_lmhead_q4_linear(lin.cfg, lin.packed, x, out, bad)
+
+
+@pytest.mark.parametrize("M,N,K,group", [(33, 4001, 37 * 64, 64), (60, 38001, 2048, 128), (18, 70000, 1056, 32), (130, 257, 4096, 128),
+                                         (64, 16 * 148 * 16, 256, 64)])
+def test_left_over_passes_split_by_columns(M, N, K, group):
+    """Whole passes, left-over ones in parts of unequal size, a last part that ends inside a block of columns, no left-over pass."""
+    Wq, s, z, x = _make(M + N, M, N, K, group, True, torch.bfloat16, torch.float16)
+    lin, xc = _linear(Wq, s, z), x.cuda()
+    got = lin.forward(xc)
+    _check(got, Wq, s, z, x, group)
+    for _ in range(3):
+        assert torch.equal(lin.forward(xc), got)
+    _check(lin.forward(xc, out_dtype=torch.bfloat16), Wq, s, z, x, group)
