@@ -302,6 +302,7 @@ int launch_q4(const coral_lmhead_q4_config& c, const Q4View& q, const Q4Pass& p,
 
 // ---- logits ----------------------------------------------------------------------------------------------------
 constexpr int kLogitsMaxV = 1 << 30;
+constexpr int kLogitsMaxChunk = 8;
 constexpr int kLogitsWideBlocks = 4 * 148;       // resident at once
 constexpr int kLogitsWideFrom = 8 * 8 * 148;     // pieces of a call (8 blocks a SM of the kernel for few rows)
 
@@ -366,17 +367,29 @@ struct LogitsPlan {
     size_t before, entry, token, range, piece, part, bytes;         // offsets in the workspace; the bitmap comes first
 };
 
+// Spans a block takes: as many as make the least of rounds of resident blocks times (spans + what starting a block costs):
+// 512 rows of 32000 in fp32 71 us with 8 at most that leave no SM without a block, 62 so; 60 rows of 152064 50 and 48.  More than
+// 8 gain nothing (960 rows of 128256: 213 and 213).
+int logits_chunk(int M, int spans) {
+    int best = 1;
+    long long best_cost = -1;
+    for (int c = 1; c <= kLogitsMaxChunk; ++c) {
+        const long long blocks = (long long)M * ((spans - 1) / c + 1);
+        const long long cost = ((blocks - 1) / kLogitsWideBlocks + 1) * (2 * c + 3);
+        if (best_cost < 0 || cost < best_cost) { best = c; best_cost = cost; }
+    }
+    return best;
+}
+
 // Rows of 128256 with lists, path, mask, result and candidates, fp32 / bf16: 1 row 30 / 36 us with the kernel for few rows,
-// 32 / 40 with the other; 12 rows 36 / 36 and 34 / 36; 60 rows 60 / 52 and 48 / 50; 120 rows 85 / 69 and 60 / 62.  A block takes
-// up to 8 spans one after the other, as long as every SM has its blocks (960 rows: 4 spans 309 / 291, 8 305 / 285, 16 319 / 297,
-// 32 344 / 319, measured before the loop was shortened).
+// 32 / 40 with the other; 12 rows 36 / 36 and 34 / 36; 60 rows 60 / 52 and 48 / 50; 120 rows 85 / 69 and 60 / 62.
 LogitsPlan logits_plan(const LogitsArgs& k, int type) {
     LogitsPlan p{};
     p.lists = k.prompt || k.output || k.path || k.bias_tokens;
     const int vec = 16 / elem_size(type), span = 32 * vec;
     p.pieces = (int)((k.V + vec - 2LL) / span) + 1;                        // of a row that starts as late as it can
     const int spans = (p.pieces - 1) / (kWideSpan / span) + 1;
-    if ((long long)k.M * p.pieces >= kLogitsWideFrom) p.chunk = (int)std::min(8LL, std::max(1LL, (long long)k.M * spans / kLogitsWideBlocks));
+    if ((long long)k.M * p.pieces >= kLogitsWideFrom) p.chunk = logits_chunk(k.M, spans);
     p.blocks = p.chunk ? (spans - 1) / p.chunk + 1 : (p.pieces - 1) / kLogitsWarps + 1;
     p.parts = p.blocks * kLogitsWarps;
     size_t at = 0;

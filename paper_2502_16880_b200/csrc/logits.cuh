@@ -12,8 +12,8 @@
 //                         result, and keep the maximum of every 512 bytes and (maximum, sum of exponentials) of a warp's part;
 //   logits_finish_kernel  per row: the log-sum-exp, and the candidates: only the k pieces of 512 bytes with the largest maxima
 //                         can hold one, so only they are read again.
-// 960 rows x 128256 in 16 sequences with lists, path, mask, result and 10 candidates: 216 us fp32, 210 us bf16; of those the
-// lists 17 and the end of the rows 31.  Reading alone takes 97 / 62 us, reading and writing 161 / 87 (bytes: 75 / 38, 151 / 75).
+// 960 rows x 128256 in 16 sequences with lists, path, mask, result and 10 candidates: 209 us fp32, 202 us bf16; of those the
+// lists 16 and the end of the rows 28.  Reading alone takes 97 / 62 us, reading and writing 161 / 87 (bytes: 75 / 38, 151 / 75).
 // What bounds the stream is instructions (13 a logit for reading, 30 with everything; 60% of the issue slots).
 // (Everything in one kernel, a cluster of blocks a row, took 850 us: candidates and lists cost each block a chain of barriers a
 // row, and their code pushed the streaming loop out of the instruction cache.  Listed tokens adjusted by the thread that holds
@@ -158,11 +158,12 @@ __global__ void __launch_bounds__(kListThreads, 1) logits_lists_kernel(const __g
     extern __shared__ __align__(16) uint32_t tables[];
     constexpr int kWords = kListWindow / 32;
     __shared__ uint32_t s_bits[kWords];
-    __shared__ int s_warp[kListThreads / 32], s_total[2];
+    __shared__ int s_warp[kListThreads / 32], s_total[2][kListCluster];      // every block's total, pushed by it
     auto cluster = cg::this_cluster();
     const int seq = blockIdx.x / kListCluster, rank = blockIdx.x % kListCluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t* places = tables + kListWindow;
     pdl_launch_dependents();
+    cluster.barrier_arrive();                    // every block has started before another writes to it
     long long p0 = 0, p1 = 0, o0 = 0, o1 = 0, b0 = 0, b1 = 0;
     if (a.prompt) list_range(a.prompt_off, seq, a.prompt_total, p0, p1);
     if (a.output) list_range(a.output_off, seq, a.output_total, o0, o1);
@@ -214,16 +215,14 @@ __global__ void __launch_bounds__(kListThreads, 1) logits_lists_kernel(const __g
             before += i < warp ? s_warp[i] : 0;
             total += s_warp[i];
         }
-        if (threadIdx.x == 0) s_total[turn] = total;
-        cluster.sync();
-        int others[kListCluster];
-#pragma unroll
-        for (int c = 0; c < kListCluster; ++c) others[c] = *cluster.map_shared_rank(&s_total[turn], c);
+        if (base == 0) cluster.barrier_wait();
+        if (threadIdx.x < kListCluster) *cluster.map_shared_rank(&s_total[turn][rank], threadIdx.x) = total;
+        cluster.sync();                          // (a buffer is written again behind the next one's, when all have read it)
         long long next = at;
 #pragma unroll
         for (int c = 0; c < kListCluster; ++c) {
-            if (c < rank) before += others[c];
-            next += others[c];
+            if (c < rank) before += s_total[turn][c];
+            next += s_total[turn][c];
         }
         if (threadIdx.x < kWords && (int)threadIdx.x * 32 < n) {
             const size_t word = (size_t)seq * a.mask_words + lo / 32 + threadIdx.x;
@@ -247,7 +246,6 @@ __global__ void __launch_bounds__(kListThreads, 1) logits_lists_kernel(const __g
         __syncthreads();
     }
     if (rank == 0 && threadIdx.x == 0) w.range[seq] = make_int2((int)first, (int)(at - first));
-    cluster.sync();                              // the others' totals have been read
 }
 
 // ---- the pass over the logits ------------------------------------------------------------------------------
@@ -381,6 +379,7 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_narrow_kernel(const __g
     __shared__ uint32_t s_special[LISTS ? kSpan / 32 : 1];
     const int per_row = (w.pieces + kLogitsWarps - 1) / kLogitsWarps;
     const int row = blockIdx.x / per_row, block = blockIdx.x - row * per_row, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    pdl_launch_dependents();                     // the last kernel waits for this one's end, its launch need not
     const LogitsIn<T> r(a, row, LISTS);
     const int p_block = block * kSpan, p = p_block + threadIdx.x * kVec;
     const uint4 raw = r.whole(p) ? __ldcs(reinterpret_cast<const uint4*>(r.in - r.shift + p)) : load_edge(r.in, p, r.shift, r.end);
@@ -438,7 +437,6 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_narrow_kernel(const __g
         if (piece < w.pieces) w.piece[(size_t)row * w.pieces + piece] = logit_order(top);
         w.part[(size_t)row * w.parts + piece] = make_float2(top > kNegInf ? top : kNegInf, sum);
     }
-    pdl_launch_dependents();
 }
 
 // Many rows: a block takes w.chunk neighbouring spans of a row one after the other.  Every thread copies its own vectors of the
@@ -462,6 +460,7 @@ __global__ void __launch_bounds__(kLogitsThreads, 4) logits_wide_kernel(const __
     const int spans = (w.pieces + kSpanPieces - 1) / kSpanPieces, per_row = w.parts / kLogitsWarps;
     const int row = blockIdx.x / per_row, block = blockIdx.x - row * per_row, s0 = block * w.chunk, s1 = min(s0 + w.chunk, spans);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    pdl_launch_dependents();
     const LogitsIn<T> r(a, row, LISTS);
     auto inner = [&](int s) { return s * kWideSpan >= r.shift && (s + 1) * kWideSpan <= r.end; };
     const bool plain_row = (!r.out || r.vec_out) && (!r.mask || r.shift == 0);
@@ -604,7 +603,6 @@ __global__ void __launch_bounds__(kLogitsThreads, 4) logits_wide_kernel(const __
     const float total = warp_sum(two.x + two.y);
     if (lane == 0) w.part[(size_t)row * w.parts + block * kLogitsWarps + warp] = make_float2(base, total);
     cp_async_wait<0>();
-    pdl_launch_dependents();
 }
 
 // ---- the end of a row ----------------------------------------------------------------------------------------
