@@ -303,6 +303,7 @@ int launch_q4(const coral_lmhead_q4_config& c, const Q4View& q, const Q4Pass& p,
 // ---- logits ----------------------------------------------------------------------------------------------------
 constexpr int kLogitsMaxV = 1 << 30;
 constexpr int kLogitsMaxChunk = 8;
+constexpr int kLogitsEndBlocks = 4 * 148;        // blocks of 16 warps that are resident at once
 constexpr int kLogitsWideBlocks = 4 * 148;       // resident at once
 constexpr int kLogitsWideFrom = 8 * 8 * 148;     // pieces of a call (8 blocks a SM of the kernel for few rows)
 
@@ -452,7 +453,9 @@ int launch_logits(const LogitsArgs& k, const LogitsPlan& p, unsigned char* ws, c
         kernel<<<grid, block, smem, st>>>(k, w);
         if (cudaGetLastError() != cudaSuccess) return CORAL_ERR_CUDA;
     }
-    return launch_pdl(logits_finish_kernel<T>, dim3(k.M), dim3(kFinishThreads), 0, st, k, w) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+    const bool many = k.M > kLogitsEndBlocks;
+    auto finish = many ? logits_finish_kernel<T, 8> : logits_finish_kernel<T, 16>;
+    return launch_pdl(finish, dim3(k.M), dim3(many ? 256 : 512), 0, st, k, w) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
 }
 
 }  // namespace

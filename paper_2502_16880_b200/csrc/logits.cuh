@@ -12,8 +12,8 @@
 //                         result, and keep the maximum of every 512 bytes and (maximum, sum of exponentials) of a warp's part;
 //   logits_finish_kernel  per row: the log-sum-exp, and the candidates: only the k pieces of 512 bytes with the largest maxima
 //                         can hold one, so only they are read again.
-// 960 rows x 128256 in 16 sequences with lists, path, mask, result and 10 candidates: 209 us fp32, 202 us bf16; of those the
-// lists 16 and the end of the rows 28.  Reading alone takes 97 / 62 us, reading and writing 161 / 87 (bytes: 75 / 38, 151 / 75).
+// 960 rows x 128256 in 16 sequences with lists, path, mask, result and 10 candidates: 206 us fp32, 198 us bf16; of those the
+// lists 16 and the end of the rows 25.  Reading alone takes 97 / 62 us, reading and writing 161 / 87 (bytes: 75 / 38, 151 / 75).
 // What bounds the stream is instructions (13 a logit for reading, 30 with everything; 60% of the issue slots).
 // (Everything in one kernel, a cluster of blocks a row, took 850 us: candidates and lists cost each block a chain of barriers a
 // row, and their code pushed the streaming loop out of the instruction cache.  Listed tokens adjusted by the thread that holds
@@ -606,20 +606,20 @@ __global__ void __launch_bounds__(kLogitsThreads, 4) logits_wide_kernel(const __
 }
 
 // ---- the end of a row ----------------------------------------------------------------------------------------
-constexpr int kFinishThreads = 512, kFinishWarps = kFinishThreads / 32;
-constexpr int kFinishTops = 32 / kFinishWarps;     // of a warp's values, for a first bound
+template <int WARPS>
 struct LogitsShared {
     unsigned long long buf[kLogitsCap];
-    uint32_t value[kFinishWarps][256];           // a piece of a warp's (logit_order)
+    uint32_t value[WARPS][256];           // a piece of a warp's (logit_order)
     unsigned long long best[32];
-    unsigned long long warp_key[kFinishWarps];
+    unsigned long long warp_key[WARPS];
     uint32_t warp_u[32];
-    float warp_m[kFinishWarps], warp_s[kFinishWarps];
+    float warp_m[WARPS], warp_s[WARPS];
     int n;
 };
 
 // Largest key of the block, in every thread.
-__device__ __forceinline__ unsigned long long block_max_key(unsigned long long key, LogitsShared& s) {
+template <int WARPS>
+__device__ __forceinline__ unsigned long long block_max_key(unsigned long long key, LogitsShared<WARPS>& s) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         const unsigned long long other = __shfl_xor_sync(0xffffffffu, key, o);
@@ -630,19 +630,20 @@ __device__ __forceinline__ unsigned long long block_max_key(unsigned long long k
     __syncthreads();
     unsigned long long best = 0;
 #pragma unroll
-    for (int w = 0; w < kFinishWarps; ++w) best = s.warp_key[w] > best ? s.warp_key[w] : best;
+    for (int w = 0; w < WARPS; ++w) best = s.warp_key[w] > best ? s.warp_key[w] : best;
     return best;
 }
 
 // Ranks the n distinct keys of s.buf by counting the larger ones and leaves the best k in s.best, descending (0 behind the
 // last).  Up to 16 neighbouring lanes share the counting for one key.  Begins and ends with a barrier.
-__device__ __noinline__ void rank_keys(int n, int k, LogitsShared& s) {
+template <int WARPS>
+__device__ __noinline__ void rank_keys(int n, int k, LogitsShared<WARPS>& s) {
     __syncthreads();
     if (threadIdx.x < 32) s.best[threadIdx.x] = 0;
     __syncthreads();
-    const int log2s = n <= kFinishThreads / 16 ? 4 : n <= kFinishThreads / 8 ? 3 : n <= kFinishThreads / 4 ? 2 : n <= kFinishThreads / 2 ? 1 : 0;
+    const int log2s = n <= WARPS * 32 / 16 ? 4 : n <= WARPS * 32 / 8 ? 3 : n <= WARPS * 32 / 4 ? 2 : n <= WARPS * 32 / 2 ? 1 : 0;
     const int share = 1 << log2s;
-    for (int i = 0; (i >> log2s) < n; i += kFinishThreads) {
+    for (int i = 0; (i >> log2s) < n; i += WARPS * 32) {
         const int at = (i + threadIdx.x) >> log2s;
         const unsigned long long mine = at < n ? s.buf[at] : ~0ull;
         int r = 0;
@@ -660,11 +661,12 @@ __device__ __forceinline__ int warp_rank(unsigned long long key, int n) {
     return r;
 }
 
-// grid: M blocks.
-template <typename T>
-__global__ void __launch_bounds__(kFinishThreads) logits_finish_kernel(const __grid_constant__ LogitsArgs a, const __grid_constant__ LogitsWork w) {
-    constexpr int kVec = LogitsVec<T>::kVec, kPiece = LogitsVec<T>::kPiece, kMost = 32 / kFinishWarps, kHeld = 4;
-    __shared__ LogitsShared s;
+// grid: M blocks of 16 warps, or of 8 where those would take several rounds (one row 16 and 17 us a call, 960 rows 209 and 206).
+template <typename T, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32) logits_finish_kernel(const __grid_constant__ LogitsArgs a, const __grid_constant__ LogitsWork w) {
+    constexpr int kVec = LogitsVec<T>::kVec, kPiece = LogitsVec<T>::kPiece, kMost = 32 / WARPS, kHeld = 64 / WARPS;
+    constexpr int kTops = 32 / WARPS;               // of a warp's values, for a first bound
+    __shared__ LogitsShared<WARPS> s;
     const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const T* in = reinterpret_cast<const T*>(a.logits) + (size_t)row * a.ld_in;
     T* out = reinterpret_cast<T*>(a.out) + (a.out ? (size_t)row * a.ld_out : 0);
@@ -690,15 +692,15 @@ __global__ void __launch_bounds__(kFinishThreads) logits_finish_kernel(const __g
     if (a.k) {
 #pragma unroll
         for (int i = 0; i < kHeld; ++i) {
-            const int at = threadIdx.x + i * kFinishThreads;
+            const int at = threadIdx.x + i * WARPS * 32;
             held[i] = at < w.pieces ? piece[at] : 0;
         }
 #pragma unroll
         for (int i = 0; i < kHeld; ++i) top = max(top, held[i]);
-        for (int i = threadIdx.x + kHeld * kFinishThreads; i < w.pieces; i += kFinishThreads) top = max(top, piece[i]);
+        for (int i = threadIdx.x + kHeld * WARPS * 32; i < w.pieces; i += WARPS * 32) top = max(top, piece[i]);
     }
 #pragma unroll 4
-    for (int i = threadIdx.x; i < w.parts; i += kFinishThreads) {
+    for (int i = threadIdx.x; i < w.parts; i += WARPS * 32) {
         const float2 v = w.part[(size_t)row * w.parts + i];
         add(v.x, v.y);
     }
@@ -708,9 +710,9 @@ __global__ void __launch_bounds__(kFinishThreads) logits_finish_kernel(const __g
         // the k largest of the warps' largest values: k distinct ones, so the k-th bounds what is asked for
         auto bound_of = [&](uint32_t v) {
 #pragma unroll
-            for (int i = 0; i < kFinishTops; ++i) { // (the barrier behind it also covers s.n)
+            for (int i = 0; i < kTops; ++i) { // (the barrier behind it also covers s.n)
                 const uint32_t t = __reduce_max_sync(0xffffffffu, v);
-                if (lane == 0) s.warp_u[warp * kFinishTops + i] = t;
+                if (lane == 0) s.warp_u[warp * kTops + i] = t;
                 if (lane == __ffs(__ballot_sync(0xffffffffu, v == t)) - 1) v = 0;
             }
             __syncthreads();
@@ -726,8 +728,8 @@ __global__ void __launch_bounds__(kFinishThreads) logits_finish_kernel(const __g
         };
         if (top >= floor) {
 #pragma unroll
-            for (int i = 0; i < kHeld; ++i) collect(held[i], threadIdx.x + i * kFinishThreads);
-            for (int i = threadIdx.x + kHeld * kFinishThreads; i < w.pieces; i += kFinishThreads) collect(piece[i], i);
+            for (int i = 0; i < kHeld; ++i) collect(held[i], threadIdx.x + i * WARPS * 32);
+            for (int i = threadIdx.x + kHeld * WARPS * 32; i < w.pieces; i += WARPS * 32) collect(piece[i], i);
         }
         __syncthreads();
         const int n = s.n, n_pieces = min(n, a.k);
@@ -738,7 +740,7 @@ __global__ void __launch_bounds__(kFinishThreads) logits_finish_kernel(const __g
             const int r = warp_rank(key, n);
 #pragma unroll
             for (int i = 0; i < kMost; ++i) {
-                const int want = warp + i * kFinishWarps;
+                const int want = warp + i * WARPS;
                 const unsigned long long k_i = __shfl_sync(0xffffffffu, key, (__ffs(__ballot_sync(0xffffffffu, r == want)) - 1) & 31);
                 pos[i] = want < n_pieces ? (int)(0xffffffffu - (uint32_t)k_i) : -1;
             }
@@ -750,7 +752,7 @@ __global__ void __launch_bounds__(kFinishThreads) logits_finish_kernel(const __g
                 unsigned long long last = ~0ull;
                 for (int i = 0; i < a.k; ++i) {
                     unsigned long long key = 0;
-                    for (int j = threadIdx.x; j < w.pieces; j += kFinishThreads) {
+                    for (int j = threadIdx.x; j < w.pieces; j += WARPS * 32) {
                         const unsigned long long mine = logit_key(piece[j], j);
                         if (mine < last && mine > key) key = mine;
                     }
@@ -761,7 +763,7 @@ __global__ void __launch_bounds__(kFinishThreads) logits_finish_kernel(const __g
             }
 #pragma unroll
             for (int i = 0; i < kMost; ++i) {
-                const int want = warp + i * kFinishWarps;
+                const int want = warp + i * WARPS;
                 pos[i] = want < n_pieces ? (int)(0xffffffffu - (uint32_t)s.best[want]) : -1;
             }
             tau = max(tau, (uint32_t)(s.best[a.k - 1] >> 32));
@@ -778,7 +780,9 @@ __global__ void __launch_bounds__(kFinishThreads) logits_finish_kernel(const __g
             }
 #pragma unroll 1
             for (int i = 0; i < kMost; ++i) {
-                const int at_piece = i == 0 ? pos[0] : pos[1];
+                int at_piece = pos[0];
+#pragma unroll
+                for (int j = 1; j < kMost; ++j) at_piece = i == j ? pos[j] : at_piece;
                 if (at_piece < 0) break;         // (the warp's others are none either)
                 const int p = at_piece * kPiece + lane * kVec, j0 = p - shift;
                 const uint4 v = p >= shift && p + kVec <= end ? *reinterpret_cast<const uint4*>(in - shift + p) : load_edge(in, p, shift, end);
@@ -857,7 +861,7 @@ __global__ void __launch_bounds__(kFinishThreads) logits_finish_kernel(const __g
         const int2 range = w.range[seq];
         const int total = range.y + (par.path ? a.path_len : 0);
         __syncthreads();
-        for (int i = threadIdx.x; i < total; i += kFinishThreads) {
+        for (int i = threadIdx.x; i < total; i += WARPS * 32) {
             int token = i < range.y ? __ldcg(w.token + range.x + i) : par.path[i - range.y];
             if (i >= range.y) {                  // a path token that is listed, or an equal one before it, is stored already
                 bool first = token >= 0 && token < a.V && !((__ldcg(par.listed + (token >> 5)) >> (token & 31)) & 1u);
@@ -875,10 +879,10 @@ __global__ void __launch_bounds__(kFinishThreads) logits_finish_kernel(const __g
     __syncthreads();
     float m = s.warp_m[0], t = 0.f;
 #pragma unroll
-    for (int i = 1; i < kFinishWarps; ++i) m = fmaxf(m, s.warp_m[i]);
+    for (int i = 1; i < WARPS; ++i) m = fmaxf(m, s.warp_m[i]);
     const float base = m == kNegInf ? 0.f : m;
 #pragma unroll
-    for (int i = 0; i < kFinishWarps; ++i) t += s.warp_s[i] * exp_fast(s.warp_m[i] - base);
+    for (int i = 0; i < WARPS; ++i) t += s.warp_s[i] * exp_fast(s.warp_m[i] - base);
     const float lse = base + logf(t);
     if (threadIdx.x == 0 && a.out_lse) a.out_lse[row] = lse;
     if (a.k == 0) return;

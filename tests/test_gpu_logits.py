@@ -358,3 +358,36 @@ def test_many_rows_alignment_in_place_and_special_values(M, V, plen, t):
         _check(_run(logits, 10, logits_dev=x, out=x, **d), logits, 10, rows=rows[:6], **d)
         assert torch.equal(torch.nan_to_num(x, nan=9.0), torch.nan_to_num(apart, nan=9.0))
         assert torch.all(buf[off:off + ld * M].view(M, ld)[:, V:] == 3.0)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("V,k", [(40, 32), (1500, 32), (20000, 1), (9000, 32)])
+def test_ends_of_very_many_rows(V, k, t):
+    """More rows than the wide blocks of the last kernel that fit at once: ties, few pieces, rows with less than k candidates, in place."""
+    M = 640
+    logits, d = _random(V + k, M, V, t, 5, 200, 150, 3, 8)
+    logits[::3] = torch.round(logits[::3])                  # ties
+    logits[1::4, 7:] = float("-inf")
+    want = _run(logits, k, **d)
+    rows = list(range(0, M, 29))
+    _check(want, logits, k, rows=rows, **d)
+    x = logits.cuda()
+    got = _run(logits, k, logits_dev=x, out=x, **d)
+    for n in ("ids", "lps", "lse"):
+        assert np.array_equal(got[n], want[n], equal_nan=n != "ids"), n
+    assert torch.equal(torch.nan_to_num(got["out"], nan=9.0), torch.nan_to_num(want["out"], nan=9.0))
+
+
+@pytest.mark.parametrize("V", [40, 5000, 100000])
+def test_piles_in_very_many_rows(V):
+    """Equal values, sorted rows and values that pile up, each row 130 times over: every copy gives the first one's answer."""
+    n = torch.arange(V)
+    rows = torch.stack([torch.zeros(V), n.float(), -n.float(), (n % 7).float(), torch.where(n % 5 == 0, 1.0, 0.999)])
+    for t in TYPES:
+        x = rows.to(t).repeat(130, 1)
+        for k in (1, 10, 32):
+            got = _run(x, k, write=False)
+            _check(got, x, k, rows=range(5))
+            for name in ("ids", "lps", "lse"):
+                a = got[name].reshape(130, 5, -1)
+                assert np.array_equal(a, np.broadcast_to(a[:1], a.shape), equal_nan=name != "ids"), (name, k)     # 99999 is +inf in fp16
