@@ -225,12 +225,15 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
         if (f_b + split < nb * split) { f_b += split; f_blk += split; }
         else { f_b = lane_in; f_blk += f_wrap; --f_tiles; }
     };
+    // With x laid out by a kernel of this call, that kernel began behind all that came before the call, so the weights may be
+    // fetched before its end.  Else the kernel before is the caller's: it may still be writing x or the weights, or reading out.
+    if (!st.x) pdl_wait();
 #pragma unroll
     for (int d = 0; d < kQ4Depth; ++d) fetch(d);
 
     const int units = q.KB * 16, all = M * units;
     if (st.x) {
-        pdl_wait();                                // the kernel that lays x out; the weights above do not come from it
+        pdl_wait();                                // the kernel that lays x out
         for (int m = 0; m < M; ++m)
             for (int ch = threadIdx.x; ch < units; ch += blockDim.x)
                 cp_async16(xs + (size_t)m * xrow + ch * 16, st.x + (size_t)m * units + ch);
