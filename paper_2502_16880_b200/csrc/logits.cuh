@@ -514,6 +514,9 @@ __global__ void __launch_bounds__(kLogitsThreads, 4) logits_wide_kernel(const __
             if (par.path && (int)threadIdx.x < a.path_len) {
                 path_token = par.path[threadIdx.x];
                 if (path_token < 0 || path_token >= a.V || is_listed(par, path_token)) path_token = kNone;
+                // one thread a token: it is adjusted in place, and the count has its repeats already
+                for (int q = 0; q < (int)threadIdx.x; ++q)
+                    if (par.path[q] == path_token) path_token = kNone;
             }
         }
     }

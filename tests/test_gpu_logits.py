@@ -391,3 +391,24 @@ def test_piles_in_very_many_rows(V):
             for name in ("ids", "lps", "lse"):
                 a = got[name].reshape(130, 5, -1)
                 assert np.array_equal(a, np.broadcast_to(a[:1], a.shape), equal_nan=name != "ids"), (name, k)     # 99999 is +inf in fp16
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("path_len", [6, 31, 33, 48, 64])
+def test_tokens_again_and_again_on_long_paths(path_len, t):
+    """A path's token is penalised once, with the count of its repeats, wherever on the path they stand (also 32 and more apart,
+    next to one another, listed or not, everywhere), for few and many rows, written apart and in place."""
+    for M, V in ((3, 9001), (300, 9001), (120, 32768)):
+        logits, d = _random(path_len + M, M, V, t, 4, 80, 60, path_len, 9)
+        p, half = d["path"], path_len // 2
+        p[:, path_len - half:] = p[:, :half]                                 # the second half repeats the first
+        p[1::4, :] = p[1::4, :1].abs().clamp(max=V - 1)                      # one token all along
+        p[2::4, ::3] = torch.tensor([d["output"][int(s)][0] for s in d["row_seq"][2::4]], dtype=torch.int32)[:, None]      # a listed one
+        p[3::4, 1::2] = p[3::4, ::2][:, :path_len // 2]                      # pairs
+        got = _run(logits, 10, **d)
+        _check(got, logits, 10, rows=range(0, M, max(1, M // 60)), **d)
+        for _ in range(3):
+            x = logits.cuda()
+            again = _run(logits, 10, logits_dev=x, out=x, **d)
+            assert torch.equal(torch.nan_to_num(again["out"].float(), nan=1.0), torch.nan_to_num(got["out"].float(), nan=1.0))
+            assert np.array_equal(again["ids"], got["ids"]) and np.array_equal(again["lps"], got["lps"]) and np.array_equal(again["lse"], got["lse"])
