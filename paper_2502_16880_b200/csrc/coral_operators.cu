@@ -247,7 +247,7 @@ int launch_q4_pass(const Q4View& q, const Q4Pass& p, const void* x_all, void* ou
     Q4Staged s{};
     if (p.staged) {
         s.status = first ? reinterpret_cast<int*>(ws) : nullptr;
-        s.back = reinterpret_cast<float*>(ws + p.at);
+        s.back = reinterpret_cast<int*>(ws + p.at);
         s.sums = reinterpret_cast<float*>(ws + p.at + p.back_bytes);
         s.x = reinterpret_cast<uint4*>(ws + p.at + p.back_bytes + p.sum_bytes);
         q4_stage_kernel<TX, PER><<<p.slab_rows ? p.slab_rows : p.rows, 256, 0, st>>>(x, p.rows, q.K, q.KB, p.slab_rows, s);
@@ -265,7 +265,7 @@ int launch_q4_pass(const Q4View& q, const Q4Pass& p, const void* x_all, void* ou
         const bool ok = p.slab_rows == 32 ? run(q4_tc_kernel<32, PER, ZEROS>, q4_tc_smem_bytes<32>())
                                           : run(q4_tc_kernel<64, PER, ZEROS>, q4_tc_smem_bytes<64>());
         if (!ok) return CORAL_ERR_CUDA;
-        if (share.split > 1 && launch_pdl(q4_join_kernel, dim3(share.tail, p.rows), dim3(256), 0, st, share, share.full * sms * 256, p.slab_rows,
+        if (share.split > 1 && launch_pdl(q4_join_kernel, dim3(share.tail, p.rows), dim3(256), 0, st, share, (const int*)s.back, share.full * sms * 256, p.slab_rows,
                                           q.N, out, out_type) != cudaSuccess)
             return CORAL_ERR_CUDA;
         return CORAL_OK;

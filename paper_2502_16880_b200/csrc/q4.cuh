@@ -87,13 +87,17 @@ __device__ __forceinline__ void q4_spread(uint32_t w, uint32_t (&v)[4]) {
     v[3] = w & 0x00f000f0u;
 }
 
-// The power of two that brings the largest absolute value (as bits) to 2^14..2^15; 1 for a row that is not finite.
-__device__ __forceinline__ int q4_exponent(uint32_t max_bits) {
-    if (max_bits >= 0x7f800000u) return 0;
-    const int e = 14 - ((int)(max_bits >> 23) - 127);
-    return e > 100 ? 100 : e < -100 ? -100 : e;
-}
+// The power of two that brings the largest absolute value (as bits) to 2^14..2^15 (below that, subnormal bf16 numbers: at least
+// to 2^8, all of them whole); 1 for a row that is not finite.
+__device__ __forceinline__ int q4_exponent(uint32_t max_bits) { return max_bits >= 0x7f800000u ? 0 : 141 - (int)(max_bits >> 23); }
 __device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// v 2^e for e from -252 to 254: as two factors, since rows of bf16 want exponents from -113 to 141 and those that undo them.
+// Neither product leaves the range of fp32 unless the result does.
+struct Q4Power {
+    float a, b;
+    __device__ __forceinline__ explicit Q4Power(int e) : a(exp2_int(e / 2)), b(exp2_int(e - e / 2)) {}
+    __device__ __forceinline__ float operator()(float v) const { return v * a * b; }
+};
 
 // Eight scaled activations in the order of q4_spread.
 __device__ __forceinline__ uint4 q4_operand(const float (&f)[8]) {
@@ -138,7 +142,7 @@ struct Q4Staged {
     int* status;                                   // the call's status word, cleared here, or null
     uint4* x;                                      // rows: [M][KB * 16]; slabs: [ceil(K / 64)][slab_rows][8]
     float* sums;                                   // rows: [M][KB * PER]
-    float* back;                                   // what undoes a row's scale and the weights' 2^-24
+    int* back;                                     // the power of two that undoes a row's scale and the weights' 2^-24
 };
 
 template <typename TX, int PER>
@@ -163,14 +167,14 @@ __global__ void __launch_bounds__(256) q4_stage_kernel(const TX* __restrict__ x,
 #pragma unroll
     for (int w = 1; w < 8; ++w) top = max(top, s_max[w]);
     const int e2 = q4_exponent(top);
-    const float scale = exp2_int(e2);
-    if (threadIdx.x == 0) st.back[m] = exp2_int(24 - e2);
+    const Q4Power scale(e2);
+    if (threadIdx.x == 0) st.back[m] = 24 - e2;
     for (int c0 = 0; c0 < chunks; c0 += 256) {
         const int ch = c0 + threadIdx.x;
         float f[8] = {}, sum = 0.f;
         if (ch * 8 < K && m < M) Elem<TX>::load8(row + ch * 8, f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { f[e] *= scale; sum += f[e]; }
+        for (int e = 0; e < 8; ++e) { f[e] = scale(f[e]); sum += f[e]; }
         if (slab_rows) {
             if (ch < chunks) st.x[((size_t)(ch >> 3) * slab_rows + m) * 8 + ((ch & 7) ^ (m & 7))] = q4_operand(f);
             continue;
@@ -191,7 +195,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
     extern __shared__ __align__(16) unsigned char smem_raw[];
     constexpr int kCols = 8 * NT;
     __shared__ uint32_t s_max[kCols];
-    __shared__ float s_back[kCols];                // what undoes the row's scale and the weights' 2^-24
+    __shared__ int s_back[kCols];                  // the power of two that undoes the row's scale and the weights' 2^-24
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int xrow = q.KB * 256 + 64, groups = q.KB * PER;
     unsigned char* xs = smem_raw;
@@ -259,15 +263,15 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
             if (top > s_max[m]) atomicMax(&s_max[m], top);
         }
         __syncthreads();
-        if (threadIdx.x < M) s_back[threadIdx.x] = exp2_int(24 - q4_exponent(s_max[threadIdx.x]));
+        if (threadIdx.x < M) s_back[threadIdx.x] = 24 - q4_exponent(s_max[threadIdx.x]);
         for (int i0 = 0; i0 < all; i0 += blockDim.x) {
             const int i = i0 + threadIdx.x, m = i < all ? i / units : 0, ch = i - m * units;
             float f[8] = {}, sum = 0.f;
             if (i < all) {
                 if (ch * 8 < q.K) Elem<TX>::load8(x + (size_t)m * q.K + ch * 8, f);
-                const float scale = exp2_int(q4_exponent(s_max[m]));
+                const Q4Power scale(q4_exponent(s_max[m]));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) { f[e] *= scale; sum += f[e]; }
+                for (int e = 0; e < 8; ++e) { f[e] = scale(f[e]); sum += f[e]; }
                 *reinterpret_cast<uint4*>(xs + (size_t)m * xrow + ch * 16) = q4_operand(f);
             }
 #pragma unroll
@@ -350,7 +354,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
                 float s = 0.f;
                 for (int p = 0; p < split; ++p) s += first[(size_t)p * 16 * kCols + e];
                 const long long n = (long long)tile * 16 + (e & 15);
-                if (n < q.N) store_as(out, (size_t)(e >> 4) * q.N + n, s * s_back[e >> 4], out_type);
+                if (n < q.N) store_as(out, (size_t)(e >> 4) * q.N + n, Q4Power(s_back[e >> 4])(s), out_type);
             }
             turn ^= 1;
             tile += step;

@@ -27,7 +27,7 @@ constexpr int kQ4TcMaxSplit = 16, kQ4TcMaxParts = 160;
 // one of the `tail` passes left over, or a part of its columns: they are split into `split` parts where that keeps more SMs busy.
 struct Q4Share {
     int full, tail, split;
-    float* part;                                   // [tail * split][activation row][256] sums of the parts
+    float* part;                                   // [tail * split][activation row][256] sums of the parts, as yet scaled
 };
 
 template <int MP>
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(q4_smem_raw) + 1023) & ~(uintptr_t)1023);
     constexpr int kSlabBytes = MP * 128;
     constexpr uint32_t kIdesc = (1u << 4) | ((uint32_t)(MP >> 3) << 17) | (8u << 24);      // D fp32, A and B fp16, 128 x MP
-    float* s_back = reinterpret_cast<float*>(smem + (size_t)kQ4TcSlabs * kSlabBytes);
+    int* s_back = reinterpret_cast<int*>(smem + (size_t)kQ4TcSlabs * kSlabBytes);
     uint64_t* x_full = reinterpret_cast<uint64_t*>(s_back + MP);
     uint64_t* x_empty = x_full + kQ4TcSlabs;
     uint64_t* a_full = x_empty + kQ4TcSlabs;       // [tile][2] a group's operands are in tensor memory (and the buffer's old sums out)
@@ -249,15 +249,15 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
 #pragma unroll
                 for (int i = 0; i < MP / 2; ++i) {
                     const float2 f = halves(acc[i]);
-                    if (2 * i < M) to[(size_t)(2 * i) * 256] = f.x * s_back[2 * i];
-                    if (2 * i + 1 < M) to[(size_t)(2 * i + 1) * 256] = f.y * s_back[2 * i + 1];
+                    if (2 * i < M) to[(size_t)(2 * i) * 256] = f.x;
+                    if (2 * i + 1 < M) to[(size_t)(2 * i + 1) * 256] = f.y;
                 }
             } else if (live && n_row < q.N) {
 #pragma unroll
                 for (int i = 0; i < MP / 2; ++i) {
                     const float2 f = halves(acc[i]);
-                    if (2 * i < M) store_as(out, (size_t)(2 * i) * q.N + n_row, f.x * s_back[2 * i], out_type);
-                    if (2 * i + 1 < M) store_as(out, (size_t)(2 * i + 1) * q.N + n_row, f.y * s_back[2 * i + 1], out_type);
+                    if (2 * i < M) store_as(out, (size_t)(2 * i) * q.N + n_row, Q4Power(s_back[2 * i])(f.x), out_type);
+                    if (2 * i + 1 < M) store_as(out, (size_t)(2 * i + 1) * q.N + n_row, Q4Power(s_back[2 * i + 1])(f.y), out_type);
                 }
             }
         }
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
 }
 
 // Adds up the parts of the tail passes, in order.  grid: tail passes x activation rows; 256 threads, one an output row.
-__global__ void __launch_bounds__(256) q4_join_kernel(Q4Share share, int first_row, int MP, int N, void* __restrict__ out, int out_type) {
+__global__ void __launch_bounds__(256) q4_join_kernel(Q4Share share, const int* back, int first_row, int MP, int N, void* __restrict__ out, int out_type) {
     const long long n = first_row + (long long)blockIdx.x * 256 + threadIdx.x;
     pdl_wait();
     if (n >= N) return;
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(256) q4_join_kernel(Q4Share share, int first_r
     float sum = 0.f;
 #pragma unroll 4
     for (int i = 0; i < share.split; ++i) sum += __ldcg(from + (size_t)i * MP * 256);
-    store_as(out, (size_t)blockIdx.y * N + n, sum, out_type);
+    store_as(out, (size_t)blockIdx.y * N + n, Q4Power(__ldcg(back + blockIdx.y))(sum), out_type);
 }
 
 }  // namespace coral

@@ -172,3 +172,33 @@ def test_left_over_passes_split_by_columns(M, N, K, group):
     for _ in range(3):
         assert torch.equal(lin.forward(xc), got)
     _check(lin.forward(xc, out_dtype=torch.bfloat16), Wq, s, z, x, group)
+
+
+@pytest.mark.parametrize("M", [1, 3, 8, 16, 24, 60])
+def test_rows_of_any_size(M):
+    """A row is scaled by a power of two before it becomes fp16, so rows times a power of two give outputs times that power, bit for
+    bit, from the smallest bf16 numbers to the largest.  (Weight scales near 2^-10 keep the largest outputs finite; those below
+    2^-126 are rounded at 2^-150.)"""
+    N, K, group = 75, 1024, 64
+    Wq, s, z, x = _make(50 + M, M, N, K, group, M % 2 == 0, torch.bfloat16, torch.bfloat16)
+    s, x = (s / 8).bfloat16(), ((x * 16).round() / 16).bfloat16()             # (few bits, so that they stay exact below 2^-126 too)
+    lin = _linear(Wq, s, z)
+    base = lin.forward(x.cuda()).double().cpu()
+    for k in (-118, -100, -87, -60, 60, 86, 100, 116, 120, 124):
+        scaled = (x.double() * 2.0 ** k).bfloat16()
+        assert torch.equal(scaled.double(), x.double() * 2.0 ** k)
+        got = lin.forward(scaled.cuda()).double().cpu()
+        assert torch.all((got - base * 2.0 ** k).abs() <= (2.0 ** -150 if k < -100 else 0)), k
+    # the very smallest, and the largest beside ordinary ones, row by row
+    tiny = (torch.randint(-127, 128, (M, K), generator=torch.Generator().manual_seed(M)).double() * 2.0 ** -133).bfloat16()
+    ones = (tiny.double() * 2.0 ** 133).bfloat16()
+    got, want = lin.forward(tiny.cuda()).double().cpu(), lin.forward(ones.cuda()).double().cpu() * 2.0 ** -133
+    assert torch.all((got - want).abs() <= 2.0 ** -150)
+    big = torch.full((K,), torch.finfo(torch.bfloat16).max).bfloat16() * torch.where(torch.arange(K) % 3 == 0, 1.0, -0.5).bfloat16()
+    mixed = x.clone()
+    mixed[M - 1] = big
+    got = lin.forward(mixed.cuda())
+    assert torch.all(torch.isfinite(got)) and torch.equal(got[:M - 1].double().cpu(), base[:M - 1])
+    _check(got[M - 1:], Wq, s, z, big[None], group)
+    mixed[M - 1] = 0
+    assert not lin.forward(mixed.cuda())[M - 1].any()
