@@ -95,6 +95,7 @@ __device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint3
 // Neither product leaves the range of fp32 unless the result does.
 struct Q4Power {
     float a, b;
+    Q4Power() = default;
     __device__ __forceinline__ explicit Q4Power(int e) : a(exp2_int(e / 2)), b(exp2_int(e - e / 2)) {}
     __device__ __forceinline__ float operator()(float v) const { return v * a * b; }
 };
@@ -195,7 +196,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
     extern __shared__ __align__(16) unsigned char smem_raw[];
     constexpr int kCols = 8 * NT;
     __shared__ uint32_t s_max[kCols];
-    __shared__ int s_back[kCols];                  // the power of two that undoes the row's scale and the weights' 2^-24
+    __shared__ Q4Power s_back[kCols];              // what undoes the row's scale and the weights' 2^-24
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int xrow = q.KB * 256 + 64, groups = q.KB * PER;
     unsigned char* xs = smem_raw;
@@ -246,7 +247,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
             const int m = i % kCols;
             xsum[i] = m < M ? st.sums[(size_t)m * groups + i / kCols] : 0.f;
         }
-        if (threadIdx.x < M) s_back[threadIdx.x] = st.back[threadIdx.x];
+        if (threadIdx.x < M) s_back[threadIdx.x] = Q4Power(st.back[threadIdx.x]);
         cp_async_wait<0>();
     } else {
         // x, scaled, in the MMA's order, and its sums over the groups (16 neighbouring lanes hold 128 columns)
@@ -263,7 +264,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
             if (top > s_max[m]) atomicMax(&s_max[m], top);
         }
         __syncthreads();
-        if (threadIdx.x < M) s_back[threadIdx.x] = 24 - q4_exponent(s_max[threadIdx.x]);
+        if (threadIdx.x < M) s_back[threadIdx.x] = Q4Power(24 - q4_exponent(s_max[threadIdx.x]));
         for (int i0 = 0; i0 < all; i0 += blockDim.x) {
             const int i = i0 + threadIdx.x, m = i < all ? i / units : 0, ch = i - m * units;
             float f[8] = {}, sum = 0.f;
@@ -354,7 +355,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_rows_kernel(Q4View q, const 
                 float s = 0.f;
                 for (int p = 0; p < split; ++p) s += first[(size_t)p * 16 * kCols + e];
                 const long long n = (long long)tile * 16 + (e & 15);
-                if (n < q.N) store_as(out, (size_t)(e >> 4) * q.N + n, Q4Power(s_back[e >> 4])(s), out_type);
+                if (n < q.N) store_as(out, (size_t)(e >> 4) * q.N + n, s_back[e >> 4](s), out_type);
             }
             turn ^= 1;
             tile += step;

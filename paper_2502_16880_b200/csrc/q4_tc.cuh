@@ -31,7 +31,7 @@ struct Q4Share {
 };
 
 template <int MP>
-constexpr size_t q4_tc_smem_bytes() { return 1024 + (size_t)kQ4TcSlabs * MP * 128 + MP * 4 + 256; }
+constexpr size_t q4_tc_smem_bytes() { return 1024 + (size_t)kQ4TcSlabs * MP * 128 + MP * sizeof(Q4Power) + 256; }
 
 __device__ __forceinline__ uint32_t q4_sub_f16x2(uint32_t a, uint32_t b) {
     uint32_t d;
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(q4_smem_raw) + 1023) & ~(uintptr_t)1023);
     constexpr int kSlabBytes = MP * 128;
     constexpr uint32_t kIdesc = (1u << 4) | ((uint32_t)(MP >> 3) << 17) | (8u << 24);      // D fp32, A and B fp16, 128 x MP
-    int* s_back = reinterpret_cast<int*>(smem + (size_t)kQ4TcSlabs * kSlabBytes);
+    Q4Power* s_back = reinterpret_cast<Q4Power*>(smem + (size_t)kQ4TcSlabs * kSlabBytes);
     uint64_t* x_full = reinterpret_cast<uint64_t*>(s_back + MP);
     uint64_t* x_empty = x_full + kQ4TcSlabs;
     uint64_t* a_full = x_empty + kQ4TcSlabs;       // [tile][2] a group's operands are in tensor memory (and the buffer's old sums out)
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
         constexpr int kSz = Q4Scales<PER, ZEROS>::kBytes;
         if (threadIdx.x < MP) {
             pdl_wait();
-            s_back[threadIdx.x] = st.back[threadIdx.x];
+            s_back[threadIdx.x] = Q4Power(st.back[threadIdx.x]);
         }
         asm volatile("bar.sync 1, 256;" ::: "memory");
         int unit = 0;
@@ -256,8 +256,8 @@ __global__ void __launch_bounds__(kQ4TcThreads, 1) q4_tc_kernel(Q4View q, Q4Stag
 #pragma unroll
                 for (int i = 0; i < MP / 2; ++i) {
                     const float2 f = halves(acc[i]);
-                    if (2 * i < M) store_as(out, (size_t)(2 * i) * q.N + n_row, Q4Power(s_back[2 * i])(f.x), out_type);
-                    if (2 * i + 1 < M) store_as(out, (size_t)(2 * i + 1) * q.N + n_row, Q4Power(s_back[2 * i + 1])(f.y), out_type);
+                    if (2 * i < M) store_as(out, (size_t)(2 * i) * q.N + n_row, s_back[2 * i](f.x), out_type);
+                    if (2 * i + 1 < M) store_as(out, (size_t)(2 * i + 1) * q.N + n_row, s_back[2 * i + 1](f.y), out_type);
                 }
             }
         }
