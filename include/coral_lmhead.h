@@ -448,9 +448,9 @@ int coral_lmhead_block_norm_backward(const coral_lmhead_norm_args *args, void *w
  * verify a draft; Section 1 has the target model verify in one pass) and the drafter's projections, which are bound by their
  * weight bytes as the draft head is:
  *   out[m][n] = sum_g scale[n][g] * sum_{k in group g} (q[n][k] - zero[n][g]) * x[m][k]
- * The sum inside a group is over exact operands (an integer and an activation; an activation under 2^-25 of its row's largest
- * is rounded at 2^-40 of that) with fp32 accumulation; the scale multiplies that fp32 sum; groups add up in fp32; one rounding
- * to the output type.  A row that holds an infinity or a NaN gives no finite outputs; other rows are not touched by it.
+ * The sum inside a group is over exact operands (an integer and an activation; an activation under 2^-24 of its row's largest
+ * may be off by up to 2^-35 of that largest) with fp32 accumulation; the scale multiplies that fp32 sum; groups add up in fp32;
+ * one rounding to the output type.  A row that holds an infinity or a NaN gives no finite outputs; other rows are not touched by it.
  *
  * coral_lmhead_q4_config: N outputs, K inputs (a multiple of group, at most 65536), group 32, 64 or 128 columns,
  *   scale_type CORAL_TYPE_BF16 or CORAL_TYPE_F16, has_zeros 0 (zero = 8 everywhere) or 1.

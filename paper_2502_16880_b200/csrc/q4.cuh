@@ -4,8 +4,9 @@
 // four bits under a mask are a subnormal fp16 number, q 2^-24, so a word becomes operands with five instructions (q under the
 // upper mask is 16 times that, which the activations of those columns make good).  What the group's sum then has too much,
 // zero point times the sum of the activations, is taken off in fp32 before the scale multiplies it.  Activations come as fp16
-// numbers too: a row is scaled by a power of two that brings its largest value to 2^14..2^15, so bf16 rows fit as well and a
-// value is exact unless it is 2^-25 times smaller than the row's largest (and then off by 2^-40 of that at most).
+// numbers too: a row is scaled by a power of two that brings its largest value to 2^14..2^15, so bf16 rows fit as well.  A value of
+// 2^-24 of the row's largest is at least 2^-10, 2^-14 where it is divided by 16, and exact; a smaller one is off by half a
+// subnormal step, 2^-25, times 16 at most: 2^-35 of the largest.
 // Few rows are bound by the weight bytes, so a weight is read once, straight into registers in the order the MMA wants
 // (the packed layout below), with several kilobytes a warp in flight.  One row of 128256 x 4096 takes 56 us (4.8 TB/s, 73% of
 // what a copy reaches), 8 rows of 32000 x 4096 with zero points 20.5: a block of columns is a chain of unpacking, MMAs and one

@@ -202,3 +202,37 @@ def test_rows_of_any_size(M):
     _check(got[M - 1:], Wq, s, z, big[None], group)
     mixed[M - 1] = 0
     assert not lin.forward(mixed.cuda())[M - 1].any()
+
+
+@pytest.mark.parametrize("xt", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("M", [1, 8, 24])
+def test_small_activations_beside_a_large_one(M, xt):
+    """Activations become fp16 numbers (every second column's divided by 16) under a power of two that brings the row's largest to
+    2^14..2^15.  A value of 2^-24 of the largest is then at least 2^-10, an exact operand of 11 bits; a smaller one is off by half a
+    subnormal step, 2^-25, times 16: 2^-35 of the largest.  The large value stands at a weight of zero, the small ones in columns
+    of one parity at a time or alone; scales are powers of two, so an output of one column is exact but for the operand."""
+    N, K, group = 48, 128, 32
+    g = torch.Generator().manual_seed(M)
+    q = torch.randint(1, 16, (N, K), generator=g)
+    q[:, 40] = 0
+    Wq = (q[:, 0::2] | q[:, 1::2] << 4).to(torch.uint8)
+    s, z = torch.full((N, K // group), 0.25).to(xt), torch.zeros(N, K // group, dtype=torch.uint8)
+    lin = _linear(Wq, s, z)
+    weight = q.double() * 0.25
+    for top in (2.0 ** 14, 2.0 ** 15 - 16, 2.0 ** 14 * 1.5):
+        top = torch.tensor(top).to(xt)
+        largest = float(top)
+        for power in (-9, -10, -11, -12, -14, -16, -20, -24):                  # of the small values; fp16 holds no smaller ones
+            v = ((1 + torch.rand(M, K, generator=g)) * 2.0 ** power * torch.where(torch.rand(M, K, generator=g) < 0.5, -1, 1)).to(xt)
+            for cols in [list(range(p, K, 2)) for p in (0, 1)] + [[c] for c in range(8)]:
+                x = torch.zeros(M, K, dtype=xt)
+                x[:, cols] = v[:, cols]
+                x[:, 40] = top
+                got = lin.forward(x.cuda()).double().cpu()
+                small = x.double()
+                small[:, 40] = 0
+                want, size = small @ weight.T, small.abs() @ weight.T
+                exact = small.abs().amax() == 0 or float(small[small != 0].abs().min()) >= 2.0 ** -24 * largest
+                off = 0 if exact else 2.0 ** -35 * largest * weight[:, cols].sum(1)
+                rounding = 0 if len(cols) == 1 else (17 * group / 16 + group / 8 + K / group + 26) * U * size
+                assert torch.all((got - want).abs() <= off + rounding), (power, cols[:2])
