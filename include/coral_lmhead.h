@@ -461,7 +461,8 @@ int coral_lmhead_block_norm_backward(const coral_lmhead_norm_args *args, void *w
  * coral_lmhead_q4_workspace_bytes: scratch a call of M rows needs (0 for the fewest rows; above 16 rows about twice the size of
  *   x in bf16 and up to 10 MiB for parts of split sums).
  * coral_lmhead_q4_linear: x_dev [M x K] of x_type (bf16 or fp16), 16-byte aligned; out_dev [M x N] of out_type (fp32, bf16 or
- *   fp16).  M >= 1; the weights are read once per pass of 64 rows (of 16 for what is left, if that is no more).
+ *   fp16).  M >= 1; the weights are read once per pass of 64 rows.  What is left, if that is 16 rows or fewer, is passes of as
+ *   many rows as fit shared memory: 16 up to K = 5632, then fewer (11 at 8192, 7 at 14336, 3 at 28672, 1 at 65536).
  *   workspace_dev: 256-byte aligned, at least that size (NULL if 0), holds nothing between calls; calls that may overlap on
  *   the GPU need one each, the packed copy they can share.
  * coral_lmhead_q4_status: synchronises `stream` and returns the status word of the last call that used the workspace (0 or

@@ -121,3 +121,15 @@ def test_logits_refuses_null_workspaces_and_too_large_calls(lib):
     plain = size()
     assert size(prompt_total=100, output_total=50, **lists) == plain + 256 + 256 + 1280 + 768 + 256
     assert size(prompt_total=100, output_total=50, **{**lists, "repetition_dev": None}) == plain       # no penalty uses them
+
+
+def test_q4_rows_of_a_pass_over_the_weights(lib):
+    """The passes a call of up to 16 rows takes show in its workspace: behind the status word each has, rounded up to 256 bytes, an
+    exponent a row, group sums and the rows themselves (rows of up to 1024 pieces of 8 columns are laid out in the kernel)."""
+    up = lambda n: (n + 255) // 256 * 256
+    for K, rows in ((4096, 16), (5632, 16), (8192, 11), (14336, 7), (28672, 3), (65536, 1)):
+        c, KB = _q4(K=K, group=128), K // 128
+        for M in (1, 2, 3, 7, 8, 11, 12, 16):
+            parts = [min(rows, M - m) for m in range(0, M, rows)]
+            want = sum(up(4 * r) + up(4 * r * KB) + up(256 * r * KB) for r in parts if r * KB * 16 > 1024)
+            assert lmhead.coral_lmhead_q4_workspace_bytes(c, M) == (256 + want if want else 0), (K, M)
