@@ -683,14 +683,21 @@ class Q4Linear:
             raise ValueError("scales must be bfloat16 or float16")
         self.cfg = make_q4_config(N, K, K // scales.shape[1], scales.dtype, zeros is not None)
         self.packed = torch.empty(coral_lmhead_q4_packed_bytes(self.cfg), dtype=torch.uint8, device=Wq.device)
+        self._workspace = None
         coral_lmhead_q4_pack(self.cfg, Wq, scales, zeros, self.packed)
 
     def forward(self, x, out=None, out_dtype=torch.float32, stream=None):
         """x [M, K] times the weights' transpose; the scratch of a call comes from torch's allocator, call by call, so calls
-        on several streams do not share any."""
+        on several streams do not share any.  That of the last call is kept for status()."""
         M = x.shape[0]
         if out is None:
             out = torch.empty((M, self.cfg.N), dtype=out_dtype, device=x.device)
         n = coral_lmhead_q4_workspace_bytes(self.cfg, M)
-        coral_lmhead_q4_linear(self.cfg, self.packed, x, out, _op_scratch(n, x.device, stream) if n else None, stream)
+        self._workspace = workspace = _op_scratch(n, x.device, stream) if n else None
+        coral_lmhead_q4_linear(self.cfg, self.packed, x, out, workspace, stream)
         return out
+
+    def status(self, stream=None):
+        """Status of the last forward (0, or CORAL_ERR_TIMEOUT: a bounded wait ran out and the results mean nothing); waits for
+        `stream`, the one that ran it."""
+        return coral_lmhead_q4_status(self._workspace, stream)

@@ -236,3 +236,16 @@ def test_small_activations_beside_a_large_one(M, xt):
                 off = 0 if exact else 2.0 ** -35 * largest * weight[:, cols].sum(1)
                 rounding = 0 if len(cols) == 1 else (17 * group / 16 + group / 8 + K / group + 26) * U * size
                 assert torch.all((got - want).abs() <= off + rounding), (power, cols[:2])
+
+
+def test_status_of_the_last_product():
+    Wq, s, z, x = _make(7, 130, 900, 1024, 64, True, torch.bfloat16, torch.bfloat16)
+    lin, x, st = _linear(Wq, s, z), x.cuda(), torch.cuda.Stream()
+    lin.forward(x)
+    assert lin.status() == 0
+    for M in (1, 8, 17, 64, 130):
+        out = torch.empty(M, 900, device="cuda")
+        torch.cuda.synchronize()
+        lin.forward(x[:M], out=out, stream=st)
+        assert lin.status(st) == 0                           # (the stream has been waited for)
+        _check(out, Wq, s, z, x[:M].cpu(), 64)

@@ -133,3 +133,25 @@ def test_q4_rows_of_a_pass_over_the_weights(lib):
             parts = [min(rows, M - m) for m in range(0, M, rows)]
             want = sum(up(4 * r) + up(4 * r * KB) + up(256 * r * KB) for r in parts if r * KB * 16 > 1024)
             assert lmhead.coral_lmhead_q4_workspace_bytes(c, M) == (256 + want if want else 0), (K, M)
+
+
+def test_q4_linear_asks_for_the_status_of_its_last_call(lib, monkeypatch):
+    """Without a GPU: forward hands the library a workspace, status asks about that one, and calls that need none have status 0."""
+    import torch
+    calls, asked = [], []
+
+    def status(workspace, stream=None):
+        asked.append(workspace)
+        return 0 if workspace is None else lmhead.CORAL_ERR_TIMEOUT
+
+    monkeypatch.setattr(lmhead, "coral_lmhead_q4_pack", lambda *a: None)
+    monkeypatch.setattr(lmhead, "coral_lmhead_q4_linear", lambda cfg, packed, x, out, workspace, stream: calls.append(workspace))
+    monkeypatch.setattr(lmhead, "coral_lmhead_q4_status", status)
+    lin = lmhead.Q4Linear(torch.zeros(48, 128, dtype=torch.uint8), torch.ones(48, 4, dtype=torch.bfloat16))
+    assert lin.status() == 0 and asked == [None]
+    for M in (33, 60):
+        lin.forward(torch.zeros(M, 256, dtype=torch.bfloat16))
+        assert calls[-1].numel() == lmhead.coral_lmhead_q4_workspace_bytes(lin.cfg, M)
+        assert lin.status() == lmhead.CORAL_ERR_TIMEOUT and asked[-1] is calls[-1]
+    lin.forward(torch.zeros(1, 256, dtype=torch.bfloat16))
+    assert calls[-1] is None and lin.status() == 0
