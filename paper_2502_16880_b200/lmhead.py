@@ -426,6 +426,17 @@ def _op_scratch(n, device, stream):
         return torch.empty(n, dtype=torch.uint8, device=device)
 
 
+def _op_output(shape, dtype, device, stream):
+    """A result that `stream` writes and the caller's current stream reads: of the pool of the former, like scratch, and given
+    back only when what the latter has been asked to do by then is done."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        out = torch.empty(shape, dtype=dtype, device=device)
+    out.record_stream(torch.cuda.current_stream(device))
+    return out
+
+
 _NORM_SIZE = ctypes.sizeof(coral_lmhead_norm_args)
 
 
@@ -691,7 +702,7 @@ class Q4Linear:
         on several streams do not share any.  That of the last call is kept for status()."""
         M = x.shape[0]
         if out is None:
-            out = torch.empty((M, self.cfg.N), dtype=out_dtype, device=x.device)
+            out = _op_output((M, self.cfg.N), out_dtype, x.device, stream)
         n = coral_lmhead_q4_workspace_bytes(self.cfg, M)
         self._workspace = workspace = _op_scratch(n, x.device, stream) if n else None
         coral_lmhead_q4_linear(self.cfg, self.packed, x, out, workspace, stream)

@@ -249,3 +249,31 @@ def test_status_of_the_last_product():
         lin.forward(x[:M], out=out, stream=st)
         assert lin.status(st) == 0                           # (the stream has been waited for)
         _check(out, Wq, s, z, x[:M].cpu(), 64)
+
+
+@pytest.mark.parametrize("M", [1, 40])
+def test_a_new_output_belongs_to_the_stream_that_writes_it(M):
+    """Memory that the current stream still has work on must not become the output of a call on another stream, and that output's
+    memory must not be written there while the current stream still reads it."""
+    Wq, s, z, x = _make(8, M, 3000, 256, 64, False, torch.bfloat16, torch.bfloat16)
+    lin, x = _linear(Wq, s, z), x.cuda()
+    want = lin.forward(x)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for dtype in (torch.float32, torch.bfloat16):
+        old = [torch.empty_like(want, dtype=dtype) for _ in range(4)]
+        torch.cuda._sleep(20_000_000)                        # ~10 ms before the current stream writes to it
+        for o in old:
+            o.fill_(9)
+        del old, o
+        out = lin.forward(x, out_dtype=dtype, stream=st)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want.to(dtype))
+        torch.cuda._sleep(20_000_000)
+        copy = out.clone()                                   # read late, freed before
+        del out
+        with torch.cuda.stream(st):
+            new = [torch.full_like(want, 7, dtype=dtype) for _ in range(4)]
+        torch.cuda.synchronize()
+        assert torch.equal(copy, want.to(dtype))
+        del new
