@@ -17,7 +17,6 @@
 namespace coral {
 
 constexpr int kNormMaxThreads = 512;
-constexpr int kNormMaxNV = 4;                       // chunks of 8 columns per thread: H <= 512 * 4 * 8
 constexpr int kNormMaxRowBytes = 32768;             // H * element size: five staged rows fit shared memory
 constexpr int kNormWarps = kNormMaxThreads / 32;
 

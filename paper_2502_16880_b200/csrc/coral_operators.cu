@@ -47,6 +47,7 @@ struct NormPlan {
 // another's row is worked on (16384 x 4096 forward: 109 us, 133 with one chunk a thread and 512 threads).  Threads are the
 // chunks over nv rounded up to a warp: a row of 3584 columns runs 224 threads and wastes none.
 void norm_block(int H, int* nv, int* threads) {
+    static_assert(kNormMaxRowBytes / 2 / 8 <= 4 * kNormMaxThreads, "rows of 16 bits fit four chunks a thread");
     const int chunks = H / 8;
     *nv = chunks <= kNormSmallBlock ? 1 : chunks <= 2 * kNormMaxThreads ? 2 : 4;
     *threads = ((chunks + *nv - 1) / *nv + 31) / 32 * 32;
@@ -118,8 +119,10 @@ int launch_norm(const NormArgs& k, const NormPlan& p, bool backward, cudaStream_
 template <typename T>
 int launch_norm_nv(const NormArgs& k, const NormPlan& p, bool backward, cudaStream_t st) {
     if (p.nv == 1) return launch_norm<T, 1>(k, p, backward, st);
-    if (p.nv == 2) return launch_norm<T, 2>(k, p, backward, st);
-    return launch_norm<T, 4>(k, p, backward, st);
+    if constexpr (sizeof(T) == 4) {
+        static_assert(kNormMaxRowBytes / 4 / 8 <= 2 * kNormMaxThreads, "fp32 rows never want four chunks a thread");
+        return launch_norm<T, 2>(k, p, backward, st);
+    } else return p.nv == 2 ? launch_norm<T, 2>(k, p, backward, st) : launch_norm<T, 4>(k, p, backward, st);
 }
 
 int launch_norm_type(int type, const NormArgs& k, const NormPlan& p, bool backward, cudaStream_t st) {
@@ -302,6 +305,7 @@ int launch_q4(const coral_lmhead_q4_config& c, const Q4View& q, const Q4Pass& p,
 
 // ---- logits ----------------------------------------------------------------------------------------------------
 constexpr int kLogitsMaxV = 1 << 30;
+static_assert(CORAL_MAX_PATH <= kLogitsThreads, "logits_wide_kernel has a thread a token of a path");
 constexpr int kLogitsMaxChunk = 8;
 constexpr int kLogitsEndBlocks = 4 * 148;        // blocks of 16 warps that are resident at once
 constexpr int kLogitsWideBlocks = 4 * 148;       // resident at once

@@ -32,7 +32,6 @@ namespace coral {
 constexpr int kLogitsThreads = 256;
 constexpr int kLogitsWarps = kLogitsThreads / 32;
 constexpr int kLogitsCap = 2048;                 // keys ranked by counting
-constexpr int kLogitsMaxPath = 64;
 constexpr int kListThreads = 1024;
 constexpr int kListWindow = 16384;               // tokens of a block's table
 constexpr int kListCluster = 8;

@@ -28,8 +28,6 @@ constexpr int kQ4Threads = kQ4Warps * 32;
 constexpr int kQ4Depth = 4;                        // column blocks a warp has in flight
 constexpr int kQ4PassRows = 16;                    // activation rows of one launch
 
-__host__ __device__ __forceinline__ size_t q4_tile_bytes(int KB) { return (size_t)KB * 1024; }
-
 struct Q4View {
     const uint4* w;                                // packed weights
     const unsigned char* sz;                       // scales (2 bytes) or scale and zero point (4 bytes)
