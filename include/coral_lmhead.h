@@ -466,7 +466,8 @@ int coral_lmhead_block_norm_backward(const coral_lmhead_norm_args *args, void *w
  *   workspace_dev: 256-byte aligned, at least that size (NULL if 0), holds nothing between calls; calls that may overlap on
  *   the GPU need one each, the packed copy they can share.
  * coral_lmhead_q4_status: synchronises `stream` and returns the status word of the last call that used the workspace (0 or
- *   CORAL_ERR_TIMEOUT; 0 for NULL).
+ *   CORAL_ERR_TIMEOUT: a bounded wait ran out, the results mean nothing; 0 for NULL).  A call that needs no workspace leaves the
+ *   word of one that it is given as it was.
  * Asynchronous on `stream` but for the last; no allocation.  CORAL_ERR_INVALID for a bad configuration, NULL or misaligned
  * pointers, M < 1.
  */
@@ -497,7 +498,7 @@ int coral_lmhead_q4_status(const void *workspace_dev, void *stream);
  * of the fp32 values.  A value of -inf or NaN is no candidate; candidates that do not exist have id 0x7fffffff and
  * log-probability -inf.  A row that allows nothing has lse -inf; a row with an allowed NaN or +inf has lse NaN.
  *
- * logits_dev [M rows of V, ld_logits apart] of `type`.  Optional parts (NULL = absent):
+ * logits_dev [M rows of V, ld_logits apart] of `type`; V at most 2^30.  Optional parts (NULL = absent):
  *   row_seq [M]: sequence of a row, negative or >= n_seq: a row without lists and penalties.  NULL: row m is sequence m
  *     (n_seq >= M; n_seq = 0: no sequence at all).
  *   prompt_tokens, output_tokens (int32) with offsets (int64 [n_seq + 1], in elements) and the number of list elements in
@@ -509,12 +510,12 @@ int coral_lmhead_q4_status(const void *workspace_dev, void *stream);
  *     negative: everything is allowed, >= n_masks: nothing is.  NULL: row m has mask m.
  *   out_logits [M rows of V, ld_out apart] of `type`, rounded once; may be the logits themselves (same row distance; no other
  *     overlap).  Columns from V on are not touched.
- *   out_ids, out_logprobs [M x k_tokens], k_tokens 0..32 (0: both NULL); out_lse [M].  At least one output is needed.
+ *   out_ids, out_logprobs [M x k_tokens], k_tokens 0..32 and at most V (0: both NULL); out_lse [M].  At least one output is needed.
  * Values of a masked token, NaN and infinities too, have no influence.  The quotient l / repetition is correctly rounded.
  * workspace_dev: 256-byte aligned, at least coral_lmhead_logits_workspace_bytes (which reads the arguments' sizes and which of
  * them are NULL, no device memory); it holds nothing between calls, and calls that may overlap on the GPU need one each.
- * Offsets must not decrease (results of sequences whose lists overlap are unspecified).  Asynchronous on `stream`, two or three launches, no allocation, no atomics on floats: the same
- * call gives the same bits.  CORAL_ERR_TOO_LARGE for more than 2^31 - 1 list elements in all or blocks of 32768 logits.
+ * Offsets must not decrease (results of sequences whose lists overlap are unspecified).  Asynchronous on `stream`, two or three
+ * launches, no allocation, no atomics on floats: the same call gives the same bits.  CORAL_ERR_TOO_LARGE for more than 2^31 - 1 list elements in all or blocks of 32768 logits.
  */
 typedef struct coral_lmhead_logits_args {
     uint32_t struct_size;          /* sizeof(coral_lmhead_logits_args) */
