@@ -510,11 +510,13 @@ __global__ void __launch_bounds__(kLogitsThreads, 4) logits_wide_kernel(const __
                 last = range.x + range.y;
             }
             fetch();
-            if (par.path && (int)threadIdx.x < a.path_len) {
-                path_token = par.path[threadIdx.x];
+            if (par.path && warp * 32 < a.path_len) {
+                if ((int)threadIdx.x < a.path_len) path_token = par.path[threadIdx.x];
                 if (path_token < 0 || path_token >= a.V || is_listed(par, path_token)) path_token = kNone;
                 // one thread a token: it is adjusted in place, and the count has its repeats already
-                for (int q = 0; q < (int)threadIdx.x; ++q)
+                if (__ffs(__match_any_sync(0xffffffffu, path_token)) - 1 != lane) path_token = kNone;
+#pragma unroll 8
+                for (int q = 0; q < warp * 32; ++q)
                     if (par.path[q] == path_token) path_token = kNone;
             }
         }
