@@ -7,9 +7,12 @@
 // is read once: a block owns a row, a thread owns the same 8-column chunks of every row, and the weights stay in its
 // registers.  A thread copies its own chunks of the next rows into its own shared-memory slots with cp.async, so the
 // loads run ahead of the reductions without registers and without a barrier (only the row sums need one).
-// bf16 with both norms and a gate a column: 16384 x 4096 forward 108 us (4.95 TB/s; bound by issue slots, 67% of them used,
-// and by the two row sums), gradient of 8192 x 4096 124 us (3.2 TB/s; three column sums of 16 columns a thread take the
-// registers, 16 warps a SM are left to hide three row sums in turn).
+// bf16 with both norms and a gate a column: 16384 x 4096 forward 108-113 us (4.95 TB/s; bound by issue slots, 67% of them used,
+// and by the two row sums; 64 registers a thread, 64 bytes more spilled), gradient of 8192 x 4096 124 us (3.2 TB/s; three column
+// sums of 16 columns a thread take the registers, 16 warps a SM are left to hide three row sums in turn.  All three are kept
+// even where two of them are one: with S = sum dY xh, a gate a column has dgate = w_post S and dw_post = gate S).  fp32: forward
+// of 8192 x 4096 117 us, gradient of 4096 x 4096 110.  Rows of more than 8192 columns in 16 bits take four chunks a thread, and
+// their gradient spills 490 bytes: 2048 x 16384 bf16 210 us (forward of 4096 rows 124).
 #pragma once
 #include "cp_async.cuh"
 #include "element.cuh"

@@ -190,8 +190,9 @@ size_t q4_part_bytes(int T, int KB, int slab_rows) {
 }
 
 // The passes over the rows of a call: up to 64 rows each on the tensor cores while more than 16 are left (152064 x 3584, groups of
-// 64: 158 us at 17 rows and 185 at 64; the warps' MMA takes 103 for every 16), then up to 16 on the warps' MMA, fewer where very
-// long rows do not fit shared memory.  Rows that a block would spend long on scaling are laid out first, in the caller's workspace.
+// 64: 158 us at 17 rows and 185 at 64; the warps' MMA takes 103 for every 16), then up to 16 on the warps' MMA, fewer where
+// long rows do not fit shared memory: 15 at K = 6144, 7 at 14336.  (The rule does not look at K, so that 8 to 16 long rows take
+// several passes where 17 take one: 4096 x 14336, groups of 128, 8 rows 41 us, 16 rows 62, 17 rows 26.)  Rows that a block would spend long on scaling are laid out first, in the caller's workspace.
 constexpr int kQ4StageUnits = 1024;              // 8-column pieces that a block of the product scales itself
 
 struct Q4Pass {
