@@ -515,7 +515,8 @@ int coral_lmhead_q4_status(const void *workspace_dev, void *stream);
  * workspace_dev: 256-byte aligned, at least coral_lmhead_logits_workspace_bytes (which reads the arguments' sizes and which of
  * them are NULL, no device memory); it holds nothing between calls, and calls that may overlap on the GPU need one each.
  * Offsets must not decrease (results of sequences whose lists overlap are unspecified).  Asynchronous on `stream`, two or three
- * launches, no allocation, no atomics on floats: the same call gives the same bits.  CORAL_ERR_TOO_LARGE for more than 2^31 - 1 list elements in all or blocks of 32768 logits.
+ * launches, no allocation, no atomics on floats: the same call gives the same bits.  CORAL_ERR_TOO_LARGE for more than 2^31 - 1 list elements in
+ * all, 2^30 - 1 output tokens (a count of theirs has 30 bits), or 2^31 - 1 blocks of 32768 logits.
  */
 typedef struct coral_lmhead_logits_args {
     uint32_t struct_size;          /* sizeof(coral_lmhead_logits_args) */

@@ -471,7 +471,7 @@ int coral_lmhead_logits_workspace_bytes(const coral_lmhead_logits_args* a, size_
     if (!bytes || !logits_args_ok(a)) return CORAL_ERR_INVALID;
     const LogitsArgs k = logits_kernel_args(a);
     const LogitsPlan p = logits_plan(k, a->type);
-    if ((long long)k.M * p.blocks > 0x7fffffffLL || k.prompt_total + k.output_total + k.bias_total > 0x7fffffffLL ||
+    if ((long long)k.M * p.blocks > 0x7fffffffLL || k.output_total > kCountMask || k.prompt_total + k.output_total + k.bias_total > 0x7fffffffLL ||
         (p.lists && k.n_seq > 0x7fffffff / kListCluster))
         return CORAL_ERR_TOO_LARGE;
     *bytes = p.bytes;

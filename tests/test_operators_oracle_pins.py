@@ -155,3 +155,15 @@ def test_q4_linear_asks_for_the_status_of_its_last_call(lib, monkeypatch):
         assert lin.status() == lmhead.CORAL_ERR_TIMEOUT and asked[-1] is calls[-1]
     lin.forward(torch.zeros(1, 256, dtype=torch.bfloat16))
     assert calls[-1] is None and lin.status() == 0
+
+
+def test_logits_refuses_more_output_tokens_than_a_count_holds(lib):
+    n = ctypes.c_size_t()
+    lists = dict(output_tokens_dev=P, output_offsets_dev=P)
+    most = (1 << 30) - 1
+    size = lambda **kw: lib.coral_lmhead_logits_workspace_bytes(ctypes.byref(_largs(**lists, **kw)), ctypes.byref(n))
+    assert size(frequency_dev=P, output_total=most) == 0
+    assert size(frequency_dev=P, output_total=most + 1) == lmhead.CORAL_ERR_TOO_LARGE
+    a = _largs(frequency_dev=P, output_total=most + 1, **lists)
+    assert lib.coral_lmhead_logits_process(ctypes.byref(a), ctypes.c_void_p(P), None) == lmhead.CORAL_ERR_TOO_LARGE
+    assert size(output_total=most + 1) == 0                  # no penalty: nothing is counted
