@@ -710,5 +710,7 @@ class Q4Linear:
 
     def status(self, stream=None):
         """Status of the last forward (0, or CORAL_ERR_TIMEOUT: a bounded wait ran out and the results mean nothing); waits for
-        `stream`, the one that ran it."""
+        `stream`, the one that ran it, or else for the device.  A forward captured into a graph has one once the graph has run."""
+        if stream is None and self._workspace is not None:
+            torch.cuda.synchronize(self._workspace.device)
         return coral_lmhead_q4_status(self._workspace, stream)

@@ -277,3 +277,24 @@ def test_a_new_output_belongs_to_the_stream_that_writes_it(M):
         torch.cuda.synchronize()
         assert torch.equal(copy, want.to(dtype))
         del new
+
+
+def test_status_waits_for_a_call_on_another_stream():
+    Wq, s, z, x = _make(9, 40, 300, 512, 64, False, torch.bfloat16, torch.bfloat16)
+    lin, x, st = _linear(Wq, s, z), x.cuda(), torch.cuda.Stream()
+    out = torch.empty(40, 300, device="cuda")
+    n = lmhead.coral_lmhead_q4_workspace_bytes(lin.cfg, 40)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(st):
+            junk = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]    # what the scratch holds at first
+            del junk
+            torch.cuda._sleep(20_000_000)
+        lin.forward(x, out=out, stream=st)
+        assert lin.status() == 0
+    _check(out, Wq, s, z, x.cpu(), 64)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        lin.forward(x, out=out)
+    g.replay()
+    assert lin.status() == 0

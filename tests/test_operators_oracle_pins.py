@@ -147,6 +147,7 @@ def test_q4_linear_asks_for_the_status_of_its_last_call(lib, monkeypatch):
     monkeypatch.setattr(lmhead, "coral_lmhead_q4_pack", lambda *a: None)
     monkeypatch.setattr(lmhead, "coral_lmhead_q4_linear", lambda cfg, packed, x, out, workspace, stream: calls.append(workspace))
     monkeypatch.setattr(lmhead, "coral_lmhead_q4_status", status)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda device=None: None)
     lin = lmhead.Q4Linear(torch.zeros(48, 128, dtype=torch.uint8), torch.ones(48, 4, dtype=torch.bfloat16))
     assert lin.status() == 0 and asked == [None]
     for M in (33, 60):
