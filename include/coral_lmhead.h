@@ -536,6 +536,116 @@ typedef struct coral_lmhead_logits_args {
 int coral_lmhead_logits_workspace_bytes(const coral_lmhead_logits_args *args, size_t *bytes);
 int coral_lmhead_logits_process(const coral_lmhead_logits_args *args, void *workspace_dev, void *stream);
 
+/*
+ * The drafter's attention (Section 2.2: the drafter is one decoder layer under the head).  Four operators, each feeding the next:
+ * norms and rotation of queries and keys, attention over whole prompts, a cache that holds keys and values in 4 bits, and attention
+ * of few queries (the next token of a sequence, or the nodes of its draft tree) over that cache.  Heads of a token lie side by side, [D]
+ * each; tokens are ld_* elements apart (a slice of a fused projection will do).  16-bit rows are 16-byte aligned, pointers and ld alike.
+ */
+
+/*
+ * Norms of queries and keys for each head, with the position rotation.  For every token t and head, all sums in fp32, one rounding:
+ *   n = w ? x / sqrt(mean(x^2) + eps) * w : x          over the head's D columns
+ *   y = n with each pair (a, b) of its first rot columns turned by position[t] * freq[i], i = 0 .. rot / 2 - 1:
+ *       (a cos - b sin, b cos + a sin); CORAL_ROPE_HALVES: pair i is columns i and rot / 2 + i, CORAL_ROPE_PAIRS: 2 i and 2 i + 1.
+ * The product position * freq, and the whole turns taken off it, are in 64 bits.
+ *   q [T x n_q x D], k [T x n_k x D] of `type` (fp32, bf16 or fp16); q or k may be NULL with n_q or n_k 0.  w_q, w_k [D] of `type`, or
+ *   NULL: no norm of that one.  positions [T]; freqs fp32 [rot / 2], NULL if rot is 0.  out_q, out_k like q and k, may be their buffers
+ *   (same ld; no other overlap).
+ * T >= 1; D a multiple of 8, 8 to 256; rot a multiple of 8, 0 to D; n_q, n_k at most 4096; ld at least heads * D and
+ * ld * element size a multiple of 16; pointers 16-byte aligned (positions, freqs: 4); eps >= 0; else CORAL_ERR_INVALID.
+ * Asynchronous on `stream`, one launch, no scratch memory.
+ */
+#define CORAL_ROPE_HALVES 0
+#define CORAL_ROPE_PAIRS 1
+
+typedef struct coral_lmhead_qk_args {
+    uint32_t struct_size;          /* sizeof(coral_lmhead_qk_args) */
+    int32_t type, T, n_q, n_k, D, rot, style;
+    float eps;
+    int64_t ld_q, ld_k, ld_out_q, ld_out_k, ld_dout_q, ld_dout_k, ld_dq, ld_dk;
+    const void *q_dev, *k_dev, *w_q_dev, *w_k_dev;
+    const int32_t *positions_dev;
+    const float *freqs_dev;
+    void *out_q_dev, *out_k_dev;                       /* coral_lmhead_qk_rotate */
+    const void *dout_q_dev, *dout_k_dev;               /* coral_lmhead_qk_rotate_backward: gradients of out_q, out_k */
+    void *dq_dev, *dk_dev;
+    float *dw_q_dev, *dw_k_dev;
+} coral_lmhead_qk_args;
+
+int coral_lmhead_qk_rotate(const coral_lmhead_qk_args *args, void *stream);
+
+/*
+ * Gradient of the above.  Reads q, k, w_q, w_k, positions, freqs as above (out_q, out_k are not looked at) and dout_q, dout_k:
+ *   d = dout turned back;  dq = w ? r (d w - xh mean(d w xh)) : d  with r = 1 / sqrt(mean(q^2) + eps), xh = r q;  dw_q = sum d xh
+ *   over tokens and heads, fp32 [D], NULL when w_q is or when not wanted; the same for k.
+ * A tensor without a norm need not be given (q_dev may be NULL when w_q is).  dq may be the buffer of q or dout_q.
+ * workspace_dev: 256-byte aligned, at least coral_lmhead_qk_rotate_backward_bytes, NULL if no dw is wanted; holds nothing
+ * between calls, calls that may overlap on the GPU need one each.  Sums go through a fixed order: the same call gives the same bits.
+ */
+int coral_lmhead_qk_rotate_backward_bytes(int T, int n_q, int n_k, int D, size_t *bytes);
+int coral_lmhead_qk_rotate_backward(const coral_lmhead_qk_args *args, void *workspace_dev, void *stream);
+
+/*
+ * A paged cache of keys and values in 4 bits.  A group of columns of a token's head is held as
+ *   low = min x,  step = round_to_type((max x - min x) / 15),  code = round((x - low) / step) in 0..15,  and stands for low + step code
+ * (step 0: code 0).  A group that holds an infinity or a NaN stands for NaN.  coral_lmhead_kv4_config: type CORAL_TYPE_BF16 or _F16 (of
+ * tokens, steps, queries and outputs), n_pages pages of `page` tokens (a multiple of 16), n_heads key heads of D = 64 or 128 columns, group
+ * 32, 64 or 128 columns and at most D; n_pages * page below 2^31.
+ * coral_lmhead_kv4_bytes: size of the cache: n_heads * (D + 8 D / group) bytes a token.  The buffer is the caller's, 256-byte aligned.
+ * coral_lmhead_kv4_store: tokens k, v [T x n_heads x D] of `type`, ld_* apart, to slots [T] (page * tokens of a page + place in it);
+ *   a slot outside the cache (-1) is passed over.  What two tokens of one call leave in one slot is unspecified.
+ * coral_lmhead_kv4_load: the reverse; rows of slots outside the cache are zeros.  out_k or out_v may be NULL.
+ * Both: T >= 0 (0: nothing to do), T * n_heads below 2^31 (else CORAL_ERR_TOO_LARGE), asynchronous, one launch, no scratch memory.
+ */
+typedef struct coral_lmhead_kv4_config {
+    uint32_t struct_size;          /* sizeof(coral_lmhead_kv4_config) */
+    int32_t type, n_pages, page, n_heads, D, group;
+} coral_lmhead_kv4_config;
+
+int coral_lmhead_kv4_bytes(const coral_lmhead_kv4_config *cfg, size_t *bytes);
+int coral_lmhead_kv4_store(const coral_lmhead_kv4_config *cfg, void *cache_dev, const void *k_dev, int64_t ld_k, const void *v_dev,
+                           int64_t ld_v, const int64_t *slots_dev, int T, void *stream);
+int coral_lmhead_kv4_load(const coral_lmhead_kv4_config *cfg, const void *cache_dev, const int64_t *slots_dev, int T, void *out_k_dev,
+                          int64_t ld_k, void *out_v_dev, int64_t ld_v, void *stream);
+
+/*
+ * Attention of few queries over that cache: the next token of each sequence, several of them, or the nodes of a draft tree.
+ * Sequence s has n = q_offsets[s + 1] - q_offsets[s] query rows (q_offsets NULL: max_q rows each), which are its last n cached
+ * tokens, and lens[s] tokens in the cache, its j-th at place j % page of page table[s][j / page].  For query row i of the
+ * sequence and query head h, with the keys and values of head h / (n_q / n_heads) as the cache holds them:
+ *   out = sum_j softmax_j(scale q . k_j) v_j  over j <= lens - n + i (tree_mask NULL), or over the j < lens - n and those
+ *   j = lens - n + b with bit b of the row's tree_mask word (a node sees its ancestors and itself);  lse = log-sum-exp of scale q . k_j.
+ * Sums and softmax in fp32; a weight is rounded to fp16 next to its value's step.  A row that sees nothing has out 0 and lse -inf.
+ * Tokens that a row does not see have no influence, infinities and NaN too; pages outside [0, n_pages) hold no tokens.
+ *   q, out [n_rows x n_q x D] of the cache's type; out_lse fp32 [n_rows x n_q] or NULL; n_q a multiple of n_heads.  Rows outside the
+ *   sequences, and rows from max_q on of a sequence, are left as they are.  lens is clamped to width * page, offsets to n_rows.
+ *   q_offsets int64 [n_seq + 1], not decreasing; tree_mask uint64 [n_rows], needs max_q <= 64.  table int32 [n_seq x width], ld_table apart.
+ * n_seq, n_rows >= 0 (0: nothing to do); max_q, n_q, width >= 1; scale finite.  max_q bounds the work that is started, so it should
+ * be no more than the longest sequence's rows.  workspace_dev: 256-byte aligned, at least coral_lmhead_kv4_attention_bytes; holds nothing between calls
+ * but the status word; calls that may overlap on the GPU need one each.  Asynchronous, one launch or two, no atomics: the same call
+ * gives the same bits.  CORAL_ERR_TOO_LARGE for more blocks than a launch takes.
+ * coral_lmhead_attention_status: synchronises `stream` and returns the status word of the last call that used the workspace
+ * (0 or CORAL_ERR_TIMEOUT: a bounded wait ran out, the results mean nothing), for both kinds of attention.
+ */
+typedef struct coral_lmhead_kv4_attention_args {
+    uint32_t struct_size;          /* sizeof(coral_lmhead_kv4_attention_args) */
+    int32_t n_seq, n_rows, max_q, n_q, width;
+    float scale;
+    int64_t ld_q, ld_out, ld_table;
+    const void *q_dev;
+    const int32_t *table_dev, *lens_dev;
+    const int64_t *q_offsets_dev;
+    const uint64_t *tree_mask_dev;
+    void *out_dev;
+    float *out_lse_dev;
+} coral_lmhead_kv4_attention_args;
+
+int coral_lmhead_kv4_attention_bytes(const coral_lmhead_kv4_config *cfg, const coral_lmhead_kv4_attention_args *args, size_t *bytes);
+int coral_lmhead_kv4_attention(const coral_lmhead_kv4_config *cfg, const void *cache_dev, const coral_lmhead_kv4_attention_args *args,
+                               void *workspace_dev, void *stream);
+int coral_lmhead_attention_status(const void *workspace_dev, void *stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char *coral_lmhead_error_string(int code);
 

@@ -1,0 +1,274 @@
+// C ABI of the drafter's attention: argument checks and kernel launches.  See include/coral_lmhead.h.
+#include "coral_lmhead.h"
+
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "kv4.cuh"
+#include "launch.cuh"
+#include "qk_rotate.cuh"
+
+using namespace coral;
+
+namespace {
+
+constexpr int kSms = 148;                          // of a B200: what grids and workspaces are sized for
+
+bool type16(int type) { return type == CORAL_TYPE_BF16 || type == CORAL_TYPE_F16; }
+
+// Rows of `heads` heads of D columns, ld apart.
+bool rows_ok(const void* p, int64_t ld, int heads, int D, int esize) {
+    return p && aligned(p, 16) && ld >= (int64_t)heads * D && ld <= (1LL << 40) && ld * esize % 16 == 0;
+}
+
+// ---- norm and rotation of queries and keys -------------------------------------------------------------------
+constexpr int kQkMaxHeads = 4096;
+constexpr int kQkMaxGrid = 4 * kSms;               // blocks of a backward call, a partial row of column sums each
+
+bool qk_args_ok(const coral_lmhead_qk_args* a) {
+    if (!a || a->struct_size != sizeof(*a)) return false;
+    if (a->type != CORAL_TYPE_F32 && !type16(a->type)) return false;
+    if (a->T < 1 || a->D < 8 || a->D > kQkMaxD || a->D % 8 != 0 || a->rot < 0 || a->rot > a->D || a->rot % 8 != 0) return false;
+    if (a->n_q < 0 || a->n_k < 0 || a->n_q > kQkMaxHeads || a->n_k > kQkMaxHeads || a->n_q + a->n_k < 1) return false;
+    if ((a->style != CORAL_ROPE_HALVES && a->style != CORAL_ROPE_PAIRS) || !(a->eps >= 0.f)) return false;
+    if (!a->positions_dev || !aligned(a->positions_dev, 4) || !aligned(a->freqs_dev, 4) || (a->rot && !a->freqs_dev)) return false;
+    return aligned(a->w_q_dev, 16) && aligned(a->w_k_dev, 16);
+}
+
+// Two granules an item, of eight columns where the members of a pair lie a multiple of eight apart, else of four.
+bool qk_eight(const coral_lmhead_qk_args* a) { return a->style == CORAL_ROPE_PAIRS || a->rot % 16 == 0; }
+
+QkArgs qk_kernel_args(const coral_lmhead_qk_args* a) {
+    QkArgs k{};
+    k.T = a->T; k.n_q = a->n_q; k.n_k = a->n_k; k.D = a->D; k.rot = a->rot; k.eps = a->eps;
+    const int N = qk_eight(a) ? 8 : 4, turned = a->style == CORAL_ROPE_HALVES ? a->rot : 0;
+    k.items = turned / 2 / N + (a->D - turned + 2 * N - 1) / (2 * N);
+    for (k.lanes = 1; k.lanes < k.items; k.lanes *= 2) {}
+    // tokens a block: the more, the fewer threads compute angles; few tokens go to as many blocks as there are
+    k.tokens = std::clamp(a->T / (4 * kSms), 1, kQkTokens);
+    k.pos = a->positions_dev; k.freq = a->freqs_dev;
+    k.x[0] = a->q_dev; k.x[1] = a->k_dev; k.ld_x[0] = a->ld_q; k.ld_x[1] = a->ld_k;
+    k.w[0] = a->w_q_dev; k.w[1] = a->w_k_dev;
+    return k;
+}
+
+template <typename T>
+int launch_qk(const coral_lmhead_qk_args* a, const QkArgs& k, bool backward, int grid, cudaStream_t st) {
+    const bool pairs = a->style == CORAL_ROPE_PAIRS, eight = qk_eight(a);
+    size_t smem = (size_t)k.tokens * k.rot * 4;
+    if (backward) {
+        smem = std::max(smem, (size_t)kQkThreads * 2 * (eight ? 8 : 4) * 4);
+        auto f = pairs ? qk_rotate_backward_kernel<T, false, 8> : eight ? qk_rotate_backward_kernel<T, true, 8> : qk_rotate_backward_kernel<T, true, 4>;
+        return launch_pdl(f, dim3(grid), dim3(kQkThreads), smem, st, k) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+    }
+    auto f = pairs ? qk_rotate_kernel<T, false, 8> : eight ? qk_rotate_kernel<T, true, 8> : qk_rotate_kernel<T, true, 4>;
+    return launch_pdl(f, dim3(grid), dim3(kQkThreads), smem, st, k) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+}
+
+int launch_qk_type(const coral_lmhead_qk_args* a, const QkArgs& k, bool backward, int grid, cudaStream_t st) {
+    if (a->type == CORAL_TYPE_BF16) return launch_qk<__nv_bfloat16>(a, k, backward, grid, st);
+    if (a->type == CORAL_TYPE_F16) return launch_qk<__half>(a, k, backward, grid, st);
+    return launch_qk<float>(a, k, backward, grid, st);
+}
+
+// ---- cache in 4 bits -----------------------------------------------------------------------------------------
+bool kv4_config_ok(const coral_lmhead_kv4_config* c) {
+    if (!c || c->struct_size != sizeof(*c) || !type16(c->type)) return false;
+    if (c->D != 64 && c->D != 128) return false;
+    if ((c->group != 32 && c->group != 64 && c->group != 128) || c->group > c->D) return false;
+    if (c->n_pages < 1 || c->page < kKv4Block || c->page % kKv4Block != 0 || c->n_heads < 1 || c->n_heads > kQkMaxHeads) return false;
+    return (int64_t)c->n_pages * c->page <= 0x7fffffff;
+}
+
+Kv4Cache kv4_cache(const coral_lmhead_kv4_config* c, const void* base) {
+    Kv4Cache k{};
+    k.base = static_cast<unsigned char*>(const_cast<void*>(base));
+    k.slots = c->n_pages * c->page;
+    k.n_k = c->n_heads; k.page = c->page; k.groups = c->D / c->group;
+    return k;
+}
+
+int launch_kv4_rows(const coral_lmhead_kv4_config* c, bool store, const void* cache, const Kv4Rows& r, cudaStream_t st) {
+    const bool wide = c->D == 128, bf16 = c->type == CORAL_TYPE_BF16;
+    const int per = kKv4RowThreads / (c->D / 8);
+    const dim3 grid((r.rows - 1) / per + 1, 2);
+    void (*f)(Kv4Cache, Kv4Rows);
+    if (store) f = bf16 ? (wide ? kv4_store_kernel<__nv_bfloat16, 128> : kv4_store_kernel<__nv_bfloat16, 64>) : (wide ? kv4_store_kernel<__half, 128> : kv4_store_kernel<__half, 64>);
+    else f = bf16 ? (wide ? kv4_load_kernel<__nv_bfloat16, 128> : kv4_load_kernel<__nv_bfloat16, 64>) : (wide ? kv4_load_kernel<__half, 128> : kv4_load_kernel<__half, 64>);
+    return launch_pdl(f, grid, dim3(kKv4RowThreads), 0, st, kv4_cache(c, cache), r) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+}
+
+struct Kv4Plan {
+    int nr, row_groups, row_blocks, splits;
+    long long units;                               // blocks without the split
+    size_t ml, o, bytes;                           // offsets in the workspace and its size
+};
+
+bool kv4_attention_ok(const coral_lmhead_kv4_config* c, const coral_lmhead_kv4_attention_args* a) {
+    if (!kv4_config_ok(c) || !a || a->struct_size != sizeof(*a)) return false;
+    if (a->n_seq < 0 || a->n_rows < 0 || a->max_q < 1 || a->width < 1 || a->ld_table < a->width || !std::isfinite(a->scale)) return false;
+    if (a->n_q < 1 || a->n_q > kQkMaxHeads || a->n_q % c->n_heads != 0) return false;
+    if (a->tree_mask_dev && a->max_q > kKv4MaxTree) return false;
+    if (!a->q_offsets_dev && (int64_t)a->n_seq * a->max_q > a->n_rows) return false;
+    if (!a->table_dev || !aligned(a->table_dev, 4) || !a->lens_dev || !aligned(a->lens_dev, 4) || !aligned(a->q_offsets_dev, 8) ||
+        !aligned(a->tree_mask_dev, 8) || !aligned(a->out_lse_dev, 4))
+        return false;
+    return rows_ok(a->q_dev, a->ld_q, a->n_q, c->D, 2) && rows_ok(a->out_dev, a->ld_out, a->n_q, c->D, 2);
+}
+
+Kv4Plan kv4_plan(const coral_lmhead_kv4_config* c, const coral_lmhead_kv4_attention_args* a) {
+    Kv4Plan p{};
+    const long long rows = (long long)a->max_q * (a->n_q / c->n_heads);
+    p.nr = rows <= 8 ? 1 : 2;
+    for (p.row_groups = 1; p.row_groups < kKv4Warps && p.row_groups * 8 * p.nr < rows; p.row_groups *= 2) {}
+    p.row_blocks = (int)((rows - 1) / (p.row_groups * 8 * p.nr) + 1);
+    p.units = (long long)a->n_seq * c->n_heads * p.row_blocks;
+    // as many parts as keep every resident block busy, of a stage at least
+    const long long resident = (p.nr == 1 ? 2 : 1) * kSms, stages = ((long long)a->width * c->page + kKv4StageTokens - 1) / kKv4StageTokens;
+    long long splits = p.units ? resident / p.units : 1;
+    if (p.units * 4 > resident) splits = (4 * resident + p.units - 1) / std::max(1LL, p.units);
+    p.splits = (int)std::clamp(splits, 1LL, std::min(stages, 256LL));
+    if (p.units == 0) p.splits = 1;
+    size_t at = 256;
+    if (p.splits > 1) {
+        const size_t n = (size_t)p.splits * a->n_rows * a->n_q;
+        p.ml = at;
+        at += (n * 8 + 255) / 256 * 256;
+        p.o = at;
+        at += n * c->D * 4;
+    }
+    p.bytes = at;
+    return p;
+}
+
+template <typename T, int D, int NG, int NR>
+cudaError_t launch_kv4(const Kv4Args& k, const Kv4Plan& p, cudaStream_t st) {
+    constexpr size_t smem = (size_t)kKv4Stages * 8 * (kKv4Block * D + 128 * NG);
+    if (!allow_smem(kv4_attention_kernel<T, D, NG, NR>, smem)) return cudaErrorUnknown;
+    return launch_pdl(kv4_attention_kernel<T, D, NG, NR>, dim3((unsigned)(p.units * p.splits)), dim3(kKv4Threads), smem, st, k);
+}
+
+template <typename T, int D>
+int launch_kv4_groups(const Kv4Args& k, const Kv4Plan& p, cudaStream_t st) {
+    cudaError_t e = cudaErrorUnknown;
+    if (k.c.groups == 1) e = p.nr == 1 ? launch_kv4<T, D, 1, 1>(k, p, st) : launch_kv4<T, D, 1, 2>(k, p, st);
+    else if (k.c.groups == 2) e = p.nr == 1 ? launch_kv4<T, D, 2, 1>(k, p, st) : launch_kv4<T, D, 2, 2>(k, p, st);
+    else if constexpr (D == 128) e = p.nr == 1 ? launch_kv4<T, D, 4, 1>(k, p, st) : launch_kv4<T, D, 4, 2>(k, p, st);
+    if (e != cudaSuccess) return CORAL_ERR_CUDA;
+    if (p.splits == 1) return CORAL_OK;
+    const long long rows = (long long)k.n_seq * k.max_q * k.n_q;
+    return launch_pdl(kv4_join_kernel<T, D>, dim3((unsigned)((rows - 1) / 8 + 1)), dim3(256), 0, st, k) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+int coral_lmhead_qk_rotate(const coral_lmhead_qk_args* a, void* stream) {
+    if (!qk_args_ok(a)) return CORAL_ERR_INVALID;
+    const int e = elem_size(a->type);
+    if (a->n_q && (!rows_ok(a->q_dev, a->ld_q, a->n_q, a->D, e) || !rows_ok(a->out_q_dev, a->ld_out_q, a->n_q, a->D, e))) return CORAL_ERR_INVALID;
+    if (a->n_k && (!rows_ok(a->k_dev, a->ld_k, a->n_k, a->D, e) || !rows_ok(a->out_k_dev, a->ld_out_k, a->n_k, a->D, e))) return CORAL_ERR_INVALID;
+    QkArgs k = qk_kernel_args(a);
+    k.y[0] = a->out_q_dev; k.y[1] = a->out_k_dev; k.ld_y[0] = a->ld_out_q; k.ld_y[1] = a->ld_out_k;
+    return launch_qk_type(a, k, false, (a->T - 1) / k.tokens + 1, static_cast<cudaStream_t>(stream));
+}
+
+int coral_lmhead_qk_rotate_backward_bytes(int T, int n_q, int n_k, int D, size_t* bytes) {
+    if (!bytes || T < 1 || n_q < 0 || n_k < 0 || n_q + n_k < 1 || n_q > kQkMaxHeads || n_k > kQkMaxHeads || D < 8 || D > kQkMaxD || D % 8 != 0)
+        return CORAL_ERR_INVALID;
+    *bytes = (size_t)std::min(T, kQkMaxGrid) * 2 * D * sizeof(float);
+    return CORAL_OK;
+}
+
+int coral_lmhead_qk_rotate_backward(const coral_lmhead_qk_args* a, void* workspace_dev, void* stream) {
+    if (!qk_args_ok(a)) return CORAL_ERR_INVALID;
+    const int e = elem_size(a->type);
+    if (a->n_q && (!rows_ok(a->dout_q_dev, a->ld_dout_q, a->n_q, a->D, e) || !rows_ok(a->dq_dev, a->ld_dq, a->n_q, a->D, e) ||
+                   (a->w_q_dev && !rows_ok(a->q_dev, a->ld_q, a->n_q, a->D, e))))
+        return CORAL_ERR_INVALID;
+    if (a->n_k && (!rows_ok(a->dout_k_dev, a->ld_dout_k, a->n_k, a->D, e) || !rows_ok(a->dk_dev, a->ld_dk, a->n_k, a->D, e) ||
+                   (a->w_k_dev && !rows_ok(a->k_dev, a->ld_k, a->n_k, a->D, e))))
+        return CORAL_ERR_INVALID;
+    if ((a->dw_q_dev && (!a->w_q_dev || !a->n_q)) || (a->dw_k_dev && (!a->w_k_dev || !a->n_k)) || !aligned(a->dw_q_dev, 4) || !aligned(a->dw_k_dev, 4))
+        return CORAL_ERR_INVALID;
+    const bool want = a->dw_q_dev || a->dw_k_dev;
+    if ((want && !workspace_dev) || !aligned(workspace_dev, 256)) return CORAL_ERR_INVALID;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    QkArgs k = qk_kernel_args(a);
+    k.dy[0] = a->dout_q_dev; k.dy[1] = a->dout_k_dev; k.ld_dy[0] = a->ld_dout_q; k.ld_dy[1] = a->ld_dout_k;
+    k.y[0] = a->dq_dev; k.y[1] = a->dk_dev; k.ld_y[0] = a->ld_dq; k.ld_y[1] = a->ld_dk;
+    k.part = want ? static_cast<float*>(workspace_dev) : nullptr;
+    const int grid = std::min((a->T - 1) / k.tokens + 1, kQkMaxGrid);
+    const int rc = launch_qk_type(a, k, true, grid, st);
+    if (rc != CORAL_OK || !want) return rc;
+    return launch_pdl(qk_columns_kernel, dim3((a->D + 31) / 32, 2), dim3(kQkColWarps * 32), 0, st, k.part, grid, a->D, a->dw_q_dev, a->dw_k_dev) == cudaSuccess
+               ? CORAL_OK : CORAL_ERR_CUDA;
+}
+
+int coral_lmhead_kv4_bytes(const coral_lmhead_kv4_config* c, size_t* bytes) {
+    if (!kv4_config_ok(c) || !bytes) return CORAL_ERR_INVALID;
+    *bytes = (size_t)c->n_pages * (c->page / kKv4Block) * c->n_heads * kv4_cache(c, nullptr).block_bytes(c->D);
+    return CORAL_OK;
+}
+
+int coral_lmhead_kv4_store(const coral_lmhead_kv4_config* c, void* cache_dev, const void* k_dev, int64_t ld_k, const void* v_dev, int64_t ld_v,
+                           const int64_t* slots_dev, int T, void* stream) {
+    if (!kv4_config_ok(c) || !cache_dev || !aligned(cache_dev, 256) || T < 0) return CORAL_ERR_INVALID;
+    if (!rows_ok(k_dev, ld_k, c->n_heads, c->D, 2) || !rows_ok(v_dev, ld_v, c->n_heads, c->D, 2) || !slots_dev || !aligned(slots_dev, 8)) return CORAL_ERR_INVALID;
+    if ((int64_t)T * c->n_heads > 0x7fffffff - kKv4RowThreads) return CORAL_ERR_TOO_LARGE;
+    if (T == 0) return CORAL_OK;
+    const Kv4Rows r{slots_dev, T * c->n_heads, const_cast<void*>(k_dev), const_cast<void*>(v_dev), ld_k, ld_v};
+    return launch_kv4_rows(c, true, cache_dev, r, static_cast<cudaStream_t>(stream));
+}
+
+int coral_lmhead_kv4_load(const coral_lmhead_kv4_config* c, const void* cache_dev, const int64_t* slots_dev, int T, void* out_k_dev, int64_t ld_k,
+                          void* out_v_dev, int64_t ld_v, void* stream) {
+    if (!kv4_config_ok(c) || !cache_dev || !aligned(cache_dev, 256) || T < 0 || !slots_dev || !aligned(slots_dev, 8)) return CORAL_ERR_INVALID;
+    if ((!out_k_dev && !out_v_dev) || (out_k_dev && !rows_ok(out_k_dev, ld_k, c->n_heads, c->D, 2)) || (out_v_dev && !rows_ok(out_v_dev, ld_v, c->n_heads, c->D, 2)))
+        return CORAL_ERR_INVALID;
+    if ((int64_t)T * c->n_heads > 0x7fffffff - kKv4RowThreads) return CORAL_ERR_TOO_LARGE;
+    if (T == 0) return CORAL_OK;
+    const Kv4Rows r{slots_dev, T * c->n_heads, out_k_dev, out_v_dev, ld_k, ld_v};
+    return launch_kv4_rows(c, false, cache_dev, r, static_cast<cudaStream_t>(stream));
+}
+
+int coral_lmhead_kv4_attention_bytes(const coral_lmhead_kv4_config* c, const coral_lmhead_kv4_attention_args* a, size_t* bytes) {
+    if (!bytes || !kv4_attention_ok(c, a)) return CORAL_ERR_INVALID;
+    const Kv4Plan p = kv4_plan(c, a);
+    if (p.units * p.splits > 0x7fffffffLL || (int64_t)a->n_seq * a->max_q * a->n_q > 0x7fffffffLL) return CORAL_ERR_TOO_LARGE;
+    *bytes = p.bytes;
+    return CORAL_OK;
+}
+
+int coral_lmhead_kv4_attention(const coral_lmhead_kv4_config* c, const void* cache_dev, const coral_lmhead_kv4_attention_args* a, void* workspace_dev,
+                               void* stream) {
+    size_t bytes = 0;
+    const int rc = coral_lmhead_kv4_attention_bytes(c, a, &bytes);
+    if (rc != CORAL_OK) return rc;
+    if (!cache_dev || !aligned(cache_dev, 256) || !workspace_dev || !aligned(workspace_dev, 256)) return CORAL_ERR_INVALID;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const Kv4Plan p = kv4_plan(c, a);
+    if (p.units == 0 || a->n_rows == 0) return cudaMemsetAsync(workspace_dev, 0, sizeof(DeviceState), st) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+    unsigned char* ws = static_cast<unsigned char*>(workspace_dev);
+    Kv4Args k{};
+    k.c = kv4_cache(c, cache_dev);
+    k.n_seq = a->n_seq; k.n_rows = a->n_rows; k.max_q = a->max_q; k.n_q = a->n_q; k.G = a->n_q / c->n_heads; k.width = a->width; k.n_pages = c->n_pages;
+    k.row_groups = p.row_groups; k.row_blocks = p.row_blocks; k.splits = p.splits;
+    k.scale2 = a->scale * 1.4426950408889634f;
+    k.ld_table = a->ld_table; k.ld_q = a->ld_q; k.ld_out = a->ld_out;
+    k.q = a->q_dev; k.table = a->table_dev; k.lens = a->lens_dev; k.q_offsets = a->q_offsets_dev;
+    k.tree = reinterpret_cast<const unsigned long long*>(a->tree_mask_dev);
+    k.out = a->out_dev; k.lse = a->out_lse_dev;
+    k.part_ml = reinterpret_cast<float2*>(ws + p.ml);
+    k.part_o = reinterpret_cast<float*>(ws + p.o);
+    k.st = reinterpret_cast<DeviceState*>(ws);
+    if (c->type == CORAL_TYPE_BF16) return c->D == 128 ? launch_kv4_groups<__nv_bfloat16, 128>(k, p, st) : launch_kv4_groups<__nv_bfloat16, 64>(k, p, st);
+    return c->D == 128 ? launch_kv4_groups<__half, 128>(k, p, st) : launch_kv4_groups<__half, 64>(k, p, st);
+}
+
+int coral_lmhead_attention_status(const void* workspace_dev, void* stream) { return coral_lmhead_q4_status(workspace_dev, stream); }
+
+}  // extern "C"

@@ -15,22 +15,6 @@ using namespace coral;
 
 namespace {
 
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-inline int elem_size(int type) { return type == CORAL_TYPE_F32 ? 4 : 2; }
-
-bool device_sms(int* sms) {
-    int dev = 0;
-    return cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess;
-}
-
-// The attribute is per kernel and device; above 48 KB, static shared memory (at most 16 KB in kernels that have both) counted in, it has
-// to be raised before the launch.
-template <typename K>
-bool allow_smem(K kernel, size_t bytes) {
-    return bytes <= 32 * 1024 ||
-           cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
-}
-
 // ---- block norm ----------------------------------------------------------------------------------------------
 constexpr int kNormFwdThreadsPerSm = 1024, kNormBwdThreadsPerSm = 512;
 constexpr int kNormSmallBlock = 256;             // threads of a block while a row fits two chunks a thread

@@ -1,6 +1,9 @@
-// Host-side launch helper shared by the translation units of the library.
+// Host-side checks and launch helpers shared by the translation units of the library.
 #pragma once
 #include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "coral_lmhead.h"
 
 namespace coral {
 
@@ -19,6 +22,22 @@ cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t s
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline int elem_size(int type) { return type == CORAL_TYPE_F32 ? 4 : 2; }
+
+inline bool device_sms(int* sms) {
+    int dev = 0;
+    return cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess;
+}
+
+// The attribute is per kernel and device; above 48 KB, static shared memory (at most 16 KB in kernels that have both) counted in, it has
+// to be raised before the launch.
+template <typename K>
+bool allow_smem(K kernel, size_t bytes) {
+    return bytes <= 32 * 1024 ||
+           cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
 }
 
 }  // namespace coral

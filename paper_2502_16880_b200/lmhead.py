@@ -30,6 +30,7 @@ CORAL_ROUTE_STATIC_MAX_ROWS = 64
 CORAL_OUTPUT_JOINT, CORAL_OUTPUT_FACTORISED, CORAL_OUTPUT_FACTORISED_RENORM = 0, 1, 2
 CORAL_TYPE_F32, CORAL_TYPE_BF16, CORAL_TYPE_F16 = 0, 1, 2
 CORAL_GATE_NONE, CORAL_GATE_CHANNEL, CORAL_GATE_ROW, CORAL_GATE_FULL = 0, 1, 2, 3
+CORAL_ROPE_HALVES, CORAL_ROPE_PAIRS = 0, 1
 CORAL_PATH_AUTO, CORAL_PATH_STREAM, CORAL_PATH_TCGEN05, CORAL_PATH_SIMT_PLAIN, CORAL_PATH_ADAPTIVE = 0, 1, 2, 3, 4
 
 
@@ -68,6 +69,26 @@ class coral_lmhead_logits_args(ctypes.Structure):
             "bias_tokens_dev", "prompt_offsets_dev", "output_offsets_dev", "bias_offsets_dev", "repetition_dev",
             "frequency_dev", "presence_dev", "bias_values_dev", "mask_words_dev", "mask_rows_dev", "out_ids_dev",
             "out_logprobs_dev", "out_lse_dev")]
+
+
+class coral_lmhead_qk_args(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [
+        (n, ctypes.c_int32) for n in ("type", "T", "n_q", "n_k", "D", "rot", "style")] + [("eps", ctypes.c_float)] + [
+        (n, ctypes.c_int64) for n in ("ld_q", "ld_k", "ld_out_q", "ld_out_k", "ld_dout_q", "ld_dout_k", "ld_dq", "ld_dk")] + [
+        (n, ctypes.c_void_p) for n in ("q_dev", "k_dev", "w_q_dev", "w_k_dev", "positions_dev", "freqs_dev", "out_q_dev", "out_k_dev",
+                                       "dout_q_dev", "dout_k_dev", "dq_dev", "dk_dev", "dw_q_dev", "dw_k_dev")]
+
+
+class coral_lmhead_kv4_config(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [
+        (n, ctypes.c_int32) for n in ("type", "n_pages", "page", "n_heads", "D", "group")]
+
+
+class coral_lmhead_kv4_attention_args(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [
+        (n, ctypes.c_int32) for n in ("n_seq", "n_rows", "max_q", "n_q", "width")] + [("scale", ctypes.c_float)] + [
+        (n, ctypes.c_int64) for n in ("ld_q", "ld_out", "ld_table")] + [
+        (n, ctypes.c_void_p) for n in ("q_dev", "table_dev", "lens_dev", "q_offsets_dev", "tree_mask_dev", "out_dev", "out_lse_dev")]
 
 
 _lib = None
@@ -111,6 +132,16 @@ _SIGNATURES = {
     "coral_lmhead_q4_status": (_i, [_vp, _vp]),
     "coral_lmhead_logits_workspace_bytes": (_i, [ctypes.POINTER(coral_lmhead_logits_args), ctypes.POINTER(ctypes.c_size_t)]),
     "coral_lmhead_logits_process": (_i, [ctypes.POINTER(coral_lmhead_logits_args), _vp, _vp]),
+    "coral_lmhead_qk_rotate": (_i, [ctypes.POINTER(coral_lmhead_qk_args), _vp]),
+    "coral_lmhead_qk_rotate_backward_bytes": (_i, [_i, _i, _i, _i, ctypes.POINTER(ctypes.c_size_t)]),
+    "coral_lmhead_qk_rotate_backward": (_i, [ctypes.POINTER(coral_lmhead_qk_args), _vp, _vp]),
+    "coral_lmhead_kv4_bytes": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), ctypes.POINTER(ctypes.c_size_t)]),
+    "coral_lmhead_kv4_store": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), _vp, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, _i, _vp]),
+    "coral_lmhead_kv4_load": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), _vp, _vp, _i, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp]),
+    "coral_lmhead_kv4_attention_bytes": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), ctypes.POINTER(coral_lmhead_kv4_attention_args),
+                                              ctypes.POINTER(ctypes.c_size_t)]),
+    "coral_lmhead_kv4_attention": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), _vp, ctypes.POINTER(coral_lmhead_kv4_attention_args), _vp, _vp]),
+    "coral_lmhead_attention_status": (_i, [_vp, _vp]),
     "coral_lmhead_error_string": (ctypes.c_char_p, [_i]),
     "coral_lmhead_destroy": (_i, [_vp]),
 }
@@ -621,6 +652,169 @@ def coral_lmhead_logits_process(logits, *, row_seq=None, prompt_tokens=None, pro
            "coral_lmhead_logits_process")
 
 
+def _heads_ptr(name, t, dtype, shape, dev):
+    """Pointer and token distance of rows [T, heads, D] whose tokens may lie apart (a slice of a fused projection)."""
+    if t is None:
+        return None, 0
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{dev}")
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    T, heads, D = shape
+    if t.is_contiguous():
+        return t.data_ptr(), heads * D
+    ld = t.stride(0) if T > 1 else heads * D
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != D) or ld < heads * D:
+        raise ValueError(f"{name}: the heads of a token must be contiguous and tokens must not overlap")
+    return t.data_ptr(), ld
+
+
+_QK_SIZE = ctypes.sizeof(coral_lmhead_qk_args)
+
+
+def _qk_args(q, k, positions, freqs, w_q, w_k, eps, style, like, out_q=None, out_k=None, dout_q=None, dout_k=None, dq=None, dk=None,
+             dw_q=None, dw_k=None):
+    """`like`: the tensors that say how many heads there are."""
+    first = like[0] if like[0] is not None else like[1]
+    if first is None or first.dim() != 3:
+        raise ValueError("queries and keys must be [T, heads, D]")
+    dev, t, f32 = _op_device(first, "q and k"), first.dtype, torch.float32
+    T, _, D = first.shape
+    n = [0 if x is None else x.shape[1] for x in like]
+    rows = lambda name, x, i: _heads_ptr(name, x, t, (T, n[i], D), dev)
+    (q_p, ld_q), (k_p, ld_k), (oq, ld_oq), (ok, ld_ok) = rows("q", q, 0), rows("k", k, 1), rows("out_q", out_q, 0), rows("out_k", out_k, 1)
+    (gq, ld_gq), (gk, ld_gk), (dq_p, ld_dq), (dk_p, ld_dk) = rows("dout_q", dout_q, 0), rows("dout_k", dout_k, 1), rows("dq", dq, 0), rows("dk", dk, 1)
+    rot = 0 if freqs is None else 2 * freqs.shape[0]
+    return coral_lmhead_qk_args(
+        _QK_SIZE, _type_of(first), T, n[0], n[1], D, rot, style, eps, ld_q, ld_k, ld_oq, ld_ok, ld_gq, ld_gk, ld_dq, ld_dk, q_p, k_p,
+        _op_ptr("w_q", w_q, t, (D,), dev), _op_ptr("w_k", w_k, t, (D,), dev), _op_ptr("positions", positions, torch.int32, (T,), dev),
+        _op_ptr("freqs", freqs, f32, (rot // 2,), dev), oq, ok, gq, gk, dq_p, dk_p, _op_ptr("dw_q", dw_q, f32, (D,), dev),
+        _op_ptr("dw_k", dw_k, f32, (D,), dev)), dev
+
+
+def coral_lmhead_qk_rotate(q, k, positions, freqs, out_q, out_k, w_q=None, w_k=None, eps=1e-6, style=CORAL_ROPE_HALVES, stream=None):
+    """Norm (where w_q, w_k [D] are given) and rotation of queries [T, n_q, D] and keys [T, n_k, D], tokens any distance apart (one of
+    the two may be None with its output).  positions int32 [T]; freqs fp32 [rot / 2] (None: no rotation); outputs like q and k, or
+    those themselves."""
+    a, dev = _qk_args(q, k, positions, freqs, w_q, w_k, eps, style, (q, k), out_q, out_k)
+    _check((_lib or load_library()).coral_lmhead_qk_rotate(ctypes.byref(a), _op_stream(stream, dev)), "coral_lmhead_qk_rotate")
+
+
+def coral_lmhead_qk_rotate_backward_bytes(T: int, n_q: int, n_k: int, D: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check((_lib or load_library()).coral_lmhead_qk_rotate_backward_bytes(T, n_q, n_k, D, ctypes.byref(b)), "coral_lmhead_qk_rotate_backward_bytes")
+    return b.value
+
+
+def coral_lmhead_qk_rotate_backward(q, k, positions, freqs, dout_q, dout_k, dq, dk, w_q=None, w_k=None, eps=1e-6, style=CORAL_ROPE_HALVES,
+                                    dw_q=None, dw_k=None, workspace=None, stream=None):
+    """Gradient of coral_lmhead_qk_rotate: dq, dk like q and k, dw_q, dw_k fp32 [D] (None: not wanted).  q (k) is needed where w_q (w_k)
+    is.  workspace: CUDA uint8 tensor of coral_lmhead_qk_rotate_backward_bytes, needed where dw_q or dw_k is."""
+    a, dev = _qk_args(q, k, positions, freqs, w_q, w_k, eps, style, (dout_q, dout_k), None, None, dout_q, dout_k, dq, dk, dw_q, dw_k)
+    if workspace is not None and workspace.numel() < coral_lmhead_qk_rotate_backward_bytes(a.T, a.n_q, a.n_k, a.D):
+        raise ValueError("workspace is smaller than coral_lmhead_qk_rotate_backward_bytes(T, n_q, n_k, D)")
+    _check((_lib or load_library()).coral_lmhead_qk_rotate_backward(
+        ctypes.byref(a), _op_ptr("workspace", workspace, torch.uint8, None, dev), _op_stream(stream, dev)), "coral_lmhead_qk_rotate_backward")
+
+
+def make_kv4_config(n_pages, page, n_heads, D, group, dtype) -> coral_lmhead_kv4_config:
+    return coral_lmhead_kv4_config(ctypes.sizeof(coral_lmhead_kv4_config), _TYPES[dtype], int(n_pages), int(page), int(n_heads), int(D), int(group))
+
+
+def coral_lmhead_kv4_bytes(cfg) -> int:
+    b = ctypes.c_size_t(0)
+    _check((_lib or load_library()).coral_lmhead_kv4_bytes(ctypes.byref(cfg), ctypes.byref(b)), "coral_lmhead_kv4_bytes")
+    return b.value
+
+
+def _kv4_cache_ptr(cfg, cache, dev):
+    if cache.numel() < coral_lmhead_kv4_bytes(cfg):
+        raise ValueError("cache is smaller than coral_lmhead_kv4_bytes(cfg)")
+    return _op_ptr("cache", cache, torch.uint8, None, dev)
+
+
+def _kv4_dtype(cfg):
+    return torch.bfloat16 if cfg.type == CORAL_TYPE_BF16 else torch.float16
+
+
+def coral_lmhead_kv4_store(cfg, cache, k, v, slots, stream=None) -> None:
+    """Tokens k, v [T, n_heads, D] (any distance apart) to slots int64 [T] of the cache (uint8, coral_lmhead_kv4_bytes(cfg)); tokens
+    whose slot lies outside the cache (-1) are passed over."""
+    dev, dt = _op_device(cache, "cache"), _kv4_dtype(cfg)
+    T = slots.shape[0]
+    shape = (T, cfg.n_heads, cfg.D)
+    (k_p, ld_k), (v_p, ld_v) = _heads_ptr("k", k, dt, shape, dev), _heads_ptr("v", v, dt, shape, dev)
+    c_p, s_p = _kv4_cache_ptr(cfg, cache, dev), _op_ptr("slots", slots, torch.int64, (T,), dev)
+    if T == 0:
+        return
+    _check((_lib or load_library()).coral_lmhead_kv4_store(ctypes.byref(cfg), c_p, k_p, ld_k, v_p, ld_v, s_p, T, _op_stream(stream, dev)),
+           "coral_lmhead_kv4_store")
+
+
+def coral_lmhead_kv4_load(cfg, cache, slots, out_k=None, out_v=None, stream=None) -> None:
+    """What the cache holds at slots int64 [T], into out_k, out_v [T, n_heads, D] of the cache's type (one may be None); slots outside the
+    cache give zeros."""
+    dev, dt = _op_device(cache, "cache"), _kv4_dtype(cfg)
+    T = slots.shape[0]
+    shape = (T, cfg.n_heads, cfg.D)
+    (k_p, ld_k), (v_p, ld_v) = _heads_ptr("out_k", out_k, dt, shape, dev), _heads_ptr("out_v", out_v, dt, shape, dev)
+    c_p, s_p = _kv4_cache_ptr(cfg, cache, dev), _op_ptr("slots", slots, torch.int64, (T,), dev)
+    if T == 0:
+        return
+    _check((_lib or load_library()).coral_lmhead_kv4_load(ctypes.byref(cfg), c_p, s_p, T, k_p, ld_k, v_p, ld_v, _op_stream(stream, dev)),
+           "coral_lmhead_kv4_load")
+
+
+def _kv4_attention_args(cfg, q, table, lens, out, max_q, q_offsets, tree_mask, scale, out_lse, dev):
+    dt, n_seq = _kv4_dtype(cfg), lens.shape[0]
+    if q.dim() != 3 or table.dim() != 2:
+        raise ValueError("q must be [rows, n_q, D] and table [n_seq, width]")
+    rows, n_q, _ = q.shape
+    shape = (rows, n_q, cfg.D)
+    width = table.shape[1]
+    (q_p, ld_q), (o_p, ld_o), (t_p, ld_t) = _heads_ptr("q", q, dt, shape, dev), _heads_ptr("out", out, dt, shape, dev), _rows_ptr(
+        "table", table, torch.int32, (n_seq, width), dev)
+    return coral_lmhead_kv4_attention_args(
+        ctypes.sizeof(coral_lmhead_kv4_attention_args), n_seq, rows, max_q, n_q, width, cfg.D ** -0.5 if scale is None else scale, ld_q, ld_o, ld_t,
+        q_p, t_p, _op_ptr("lens", lens, torch.int32, (n_seq,), dev), _op_ptr("q_offsets", q_offsets, torch.int64, (n_seq + 1,), dev),
+        _op_ptr("tree_mask", tree_mask, torch.int64, (rows,), dev), o_p, _op_ptr("out_lse", out_lse, torch.float32, (rows, n_q), dev))
+
+
+def coral_lmhead_kv4_attention_bytes(cfg, args) -> int:
+    b = ctypes.c_size_t(0)
+    _check((_lib or load_library()).coral_lmhead_kv4_attention_bytes(ctypes.byref(cfg), ctypes.byref(args), ctypes.byref(b)),
+           "coral_lmhead_kv4_attention_bytes")
+    return b.value
+
+
+def coral_lmhead_kv4_attention(cfg, cache, q, table, lens, out, max_q=1, q_offsets=None, tree_mask=None, scale=None, out_lse=None, workspace=None,
+                               stream=None):
+    """Attention of query rows q [rows, n_q, D] over the cache: sequence s has the rows q_offsets[s] .. q_offsets[s + 1] (int64 [n_seq + 1];
+    None: max_q rows each, at most max_q in any case), which are its last cached tokens, and lens[s] (int32) tokens on the pages
+    table[s] (int32 [n_seq, width]).  tree_mask int64 [rows]: bit b lets a row see the sequence's b-th query token (None: causal).
+    scale: 1 / sqrt(D) if None.  out like q; out_lse fp32 [rows, n_q].  Returns the scratch of the call, which holds the word that
+    coral_lmhead_attention_status reads (from torch's allocator if workspace is None)."""
+    dev = _op_device(cache, "cache")
+    a = _kv4_attention_args(cfg, q, table, lens, out, max_q, q_offsets, tree_mask, scale, out_lse, dev)
+    c_p = _kv4_cache_ptr(cfg, cache, dev)
+    if a.n_seq == 0 or a.n_rows == 0:
+        return workspace
+    n = coral_lmhead_kv4_attention_bytes(cfg, a)
+    if workspace is None:
+        workspace = _op_scratch(n, cache.device, stream)
+    elif workspace.numel() < n:
+        raise ValueError("workspace is smaller than coral_lmhead_kv4_attention_bytes(cfg, args)")
+    _check((_lib or load_library()).coral_lmhead_kv4_attention(
+        ctypes.byref(cfg), c_p, ctypes.byref(a), _op_ptr("workspace", workspace, torch.uint8, None, dev), _op_stream(stream, dev)),
+        "coral_lmhead_kv4_attention")
+    return workspace
+
+
+def coral_lmhead_attention_status(workspace, stream=None) -> int:
+    """Status word of the last attention call that used the workspace; waits for the stream."""
+    return int((_lib or load_library()).coral_lmhead_attention_status(None if workspace is None else workspace.data_ptr(), _stream_ptr(stream)))
+
+
 def coral_lmhead_destroy(handle) -> None:
     _check(load_library().coral_lmhead_destroy(handle), "coral_lmhead_destroy")
 
@@ -714,3 +908,44 @@ class Q4Linear:
         if stream is None and self._workspace is not None:
             torch.cuda.synchronize(self._workspace.device)
         return coral_lmhead_q4_status(self._workspace, stream)
+
+
+class Kv4Cache:
+    """Owns the pages of a 4-bit cache of keys and values: n_pages pages of `page` tokens with n_heads heads of D columns."""
+
+    def __init__(self, n_pages, page, n_heads, D, group=128, dtype=torch.bfloat16, device="cuda"):
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("the cache's type must be bfloat16 or float16")
+        self.cfg = make_kv4_config(n_pages, page, n_heads, D, group, dtype)
+        self.dtype = dtype
+        self.pages = torch.empty(coral_lmhead_kv4_bytes(self.cfg), dtype=torch.uint8, device=device)
+        self._workspace = None
+
+    def store(self, k, v, slots, stream=None):
+        """Tokens k, v [T, n_heads, D] to slots int64 [T] (page * tokens of a page + place in it; -1: passed over)."""
+        coral_lmhead_kv4_store(self.cfg, self.pages, k, v, slots, stream)
+
+    def load(self, slots, out_k=None, out_v=None, stream=None):
+        """The keys and values that stand at slots int64 [T], both if no output is given."""
+        shape = (slots.shape[0], self.cfg.n_heads, self.cfg.D)
+        if out_k is None and out_v is None:
+            out_k, out_v = (_op_output(shape, self.dtype, self.pages.device, stream) for _ in range(2))
+        coral_lmhead_kv4_load(self.cfg, self.pages, slots, out_k, out_v, stream)
+        return out_k, out_v
+
+    def attend(self, q, table, lens, max_q=1, q_offsets=None, tree_mask=None, scale=None, out=None, out_lse=None, stream=None):
+        """coral_lmhead_kv4_attention over this cache; the scratch of a call comes from torch's allocator, that of the last call is kept
+        for status().  A new output holds zeros in rows that belong to no sequence."""
+        if out is None:
+            out = _op_output(q.shape, self.dtype, q.device, stream)
+            if q_offsets is not None or out.shape[0] != lens.shape[0] * max_q:
+                with torch.cuda.stream(torch.cuda.current_stream(q.device) if stream is None else stream):
+                    out.zero_()
+        self._workspace = coral_lmhead_kv4_attention(self.cfg, self.pages, q, table, lens, out, max_q, q_offsets, tree_mask, scale, out_lse, None, stream)
+        return out
+
+    def status(self, stream=None):
+        """Status of the last attend (0, or CORAL_ERR_TIMEOUT: the results mean nothing); waits for `stream`, or else for the device."""
+        if stream is None and self._workspace is not None:
+            torch.cuda.synchronize(self._workspace.device)
+        return coral_lmhead_attention_status(self._workspace, stream)
