@@ -587,6 +587,37 @@ int coral_lmhead_qk_rotate_backward_bytes(int T, int n_q, int n_k, int D, size_t
 int coral_lmhead_qk_rotate_backward(const coral_lmhead_qk_args *args, void *workspace_dev, void *stream);
 
 /*
+ * Attention over whole prompts: packed sequences, causal, grouped heads.  Sequence s has the query rows q_offsets[s] .. q_offsets[s + 1]
+ * and the key rows k_offsets[s] .. k_offsets[s + 1], of which the queries are the last (a prompt's next part behind keys that were
+ * there before; coral_lmhead_kv4_load brings those out of the cache).  For query i of Lq, with Lk keys, and query head h, with the
+ * keys and values of head h / (n_q / n_k):
+ *   out = sum_j softmax_j(scale q . k_j) v_j  over j <= i + Lk - Lq;  lse = log-sum-exp of scale q . k_j over the same
+ * Scores, softmax statistics and sums in fp32; the weights are rounded to `type` for the product with the values.  A row that sees
+ * no key (Lk < Lq), or whose scores are all -inf, has out 0 and lse -inf.  Keys and values that a row does not see have no influence on it,
+ * infinities and NaN too.
+ *   type CORAL_TYPE_BF16 or _F16.  q, out [T x n_q x D], k, v [Tk x n_k x D], tokens ld_* apart; D a multiple of 8, 8 to 128; n_q a
+ *   multiple of n_k.  q_offsets, k_offsets int64 [n_seq + 1], not decreasing, clamped to T and Tk; k_offsets NULL: those of the
+ *   queries (Tk = T).  out_lse fp32 [T x n_q] or NULL.  Rows outside the sequences are left as they are.  out may not overlap an input.
+ * n_seq, T, Tk >= 0 (n_seq or T 0: nothing to do); scale > 0 and finite.  workspace_dev: CORAL_PROMPT_WORKSPACE_BYTES, 256-byte aligned, for the
+ * status word that coral_lmhead_attention_status reads; calls that may overlap on the GPU need one each.  Asynchronous, one launch, no
+ * atomics: the same call gives the same bits.  CORAL_ERR_TOO_LARGE for more blocks than a launch takes.
+ */
+#define CORAL_PROMPT_WORKSPACE_BYTES 256
+
+typedef struct coral_lmhead_prompt_args {
+    uint32_t struct_size;          /* sizeof(coral_lmhead_prompt_args) */
+    int32_t type, n_seq, T, Tk, n_q, n_k, D;
+    float scale;
+    int64_t ld_q, ld_k, ld_v, ld_out;
+    const void *q_dev, *k_dev, *v_dev;
+    const int64_t *q_offsets_dev, *k_offsets_dev;
+    void *out_dev;
+    float *out_lse_dev;
+} coral_lmhead_prompt_args;
+
+int coral_lmhead_prompt_attention(const coral_lmhead_prompt_args *args, void *workspace_dev, void *stream);
+
+/*
  * A paged cache of keys and values in 4 bits.  A group of columns of a token's head is held as
  *   low = min x,  step = round_to_type((max x - min x) / 15),  code = round((x - low) / step) in 0..15,  and stands for low + step code
  * (step 0: code 0).  A group that holds an infinity or a NaN stands for NaN.  coral_lmhead_kv4_config: type CORAL_TYPE_BF16 or _F16 (of

@@ -122,6 +122,14 @@ __device__ __forceinline__ void warp_argbest(float& v, int& k) {
     }
 }
 
+// Rows offsets[i] .. offsets[i + 1] of `most`, whatever the offsets hold: first row and number of rows.
+__device__ __forceinline__ void clamped_range(const int64_t* offsets, int i, int most, int* first, int* n) {
+    const long long from = offsets[i], to = offsets[i + 1];
+    const int a = (int)(from < 0 ? 0 : from > most ? most : from), b = (int)(to < a ? a : to > most ? most : to);
+    *first = a;
+    *n = b - a;
+}
+
 // Programmatic dependent launch: a kernel launched with the programmatic-serialisation attribute may start
 // while its predecessor in the stream still runs; pdl_wait() blocks until the predecessor has completed
 // and its writes are visible (no-op without the attribute).  pdl_launch_dependents() lets the successor start.

@@ -8,7 +8,9 @@
 
 #include "kv4.cuh"
 #include "launch.cuh"
+#include "prompt_attention.cuh"
 #include "qk_rotate.cuh"
+#include "tensor_map.cuh"
 
 using namespace coral;
 
@@ -162,6 +164,41 @@ int launch_kv4_groups(const Kv4Args& k, const Kv4Plan& p, cudaStream_t st) {
     return launch_pdl(kv4_join_kernel<T, D>, dim3((unsigned)((rows - 1) / 8 + 1)), dim3(256), 0, st, k) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
 }
 
+// ---- attention over prompts ----------------------------------------------------------------------------------
+bool prompt_args_ok(const coral_lmhead_prompt_args* a) {
+    if (!a || a->struct_size != sizeof(*a) || !type16(a->type)) return false;
+    if (a->n_seq < 0 || a->T < 0 || a->Tk < 0 || a->n_k < 1 || a->n_q < a->n_k || a->n_q > kQkMaxHeads || a->n_q % a->n_k != 0) return false;
+    if (a->D < 8 || a->D > 128 || a->D % 8 != 0 || !(a->scale > 0.f) || !std::isfinite(a->scale)) return false;
+    if (!a->q_offsets_dev || !aligned(a->q_offsets_dev, 8) || !aligned(a->k_offsets_dev, 8) || !aligned(a->out_lse_dev, 4)) return false;
+    if (!a->k_offsets_dev && a->Tk != a->T) return false;
+    return rows_ok(a->q_dev, a->ld_q, a->n_q, a->D, 2) && rows_ok(a->out_dev, a->ld_out, a->n_q, a->D, 2) &&
+           rows_ok(a->k_dev, a->ld_k, a->n_k, a->D, 2) && rows_ok(a->v_dev, a->ld_v, a->n_k, a->D, 2);
+}
+
+// Rows [T x heads x D] in boxes of 64 columns x `heads_box` heads x `tokens` tokens, 128-byte swizzle; columns past D read as zero.
+bool make_rows_map(CUtensorMap* map, int type, const void* base, int T, int heads, int D, long long ld, int heads_box, int tokens) {
+    static const EncodeTiledFn enc = encode_tiled_fn();
+    if (!enc) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)std::max(T, 1)};
+    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)ld * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)heads_box, (cuuint32_t)tokens}, ones[3] = {1, 1, 1};
+    return enc(map, type == CORAL_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims,
+               strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int DB>
+int launch_prompt(const coral_lmhead_prompt_args* a, const PaArgs& k, unsigned blocks, cudaStream_t st) {
+    CUtensorMap q, kk, v;
+    if (!make_rows_map(&q, a->type, a->q_dev, a->T, a->n_q, a->D, a->ld_q, k.gp, 128 / k.gp) ||
+        !make_rows_map(&kk, a->type, a->k_dev, a->Tk, a->n_k, a->D, a->ld_k, 1, kPaKeys) ||
+        !make_rows_map(&v, a->type, a->v_dev, a->Tk, a->n_k, a->D, a->ld_v, 1, kPaKeys))
+        return CORAL_ERR_CUDA;
+    constexpr size_t smem = pa_smem_bytes<DB>();
+    if (!allow_smem(prompt_attention_kernel<T, DB>, smem)) return CORAL_ERR_CUDA;
+    return launch_pdl(prompt_attention_kernel<T, DB>, dim3(blocks), dim3(kPaThreads), smem, st, k, q, kk, v) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+}
+
 }  // namespace
 
 extern "C" {
@@ -206,6 +243,28 @@ int coral_lmhead_qk_rotate_backward(const coral_lmhead_qk_args* a, void* workspa
     if (rc != CORAL_OK || !want) return rc;
     return launch_pdl(qk_columns_kernel, dim3((a->D + 31) / 32, 2), dim3(kQkColWarps * 32), 0, st, k.part, grid, a->D, a->dw_q_dev, a->dw_k_dev) == cudaSuccess
                ? CORAL_OK : CORAL_ERR_CUDA;
+}
+
+int coral_lmhead_prompt_attention(const coral_lmhead_prompt_args* a, void* workspace_dev, void* stream) {
+    if (!prompt_args_ok(a) || !workspace_dev || !aligned(workspace_dev, 256)) return CORAL_ERR_INVALID;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (a->n_seq == 0 || a->T == 0) return cudaMemsetAsync(workspace_dev, 0, sizeof(DeviceState), st) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+    PaArgs k{};
+    k.n_seq = a->n_seq; k.T = a->T; k.Tk = a->Tk; k.n_q = a->n_q; k.n_k = a->n_k; k.G = a->n_q / a->n_k; k.D = a->D;
+    // heads side by side in a tile: the largest power of two that divides a group
+    for (k.gp = 1; k.gp < 128 && k.G % (2 * k.gp) == 0; k.gp *= 2) ++k.gp_log2;
+    k.c = a->scale * 1.4426950408889634f;
+    k.q_offsets = a->q_offsets_dev; k.k_offsets = a->k_offsets_dev;
+    k.q = a->q_dev; k.k = a->k_dev; k.v = a->v_dev;
+    k.ld_q = a->ld_q; k.ld_k = a->ld_k; k.ld_v = a->ld_v; k.ld_out = a->ld_out;
+    k.out = a->out_dev; k.lse = a->out_lse_dev;
+    k.st = static_cast<DeviceState*>(workspace_dev);
+    const int per = 256 / k.gp;                        // tokens of a block; sequences have at most T / per + n_seq blocks of them in all
+    const long long slots = std::min((long long)a->T, (long long)a->T / per + a->n_seq), blocks = slots * a->n_k * (k.G / k.gp);
+    if (blocks > 0x7fffffffLL) return CORAL_ERR_TOO_LARGE;
+    if (a->type == CORAL_TYPE_BF16)
+        return a->D > 64 ? launch_prompt<__nv_bfloat16, 2>(a, k, (unsigned)blocks, st) : launch_prompt<__nv_bfloat16, 1>(a, k, (unsigned)blocks, st);
+    return a->D > 64 ? launch_prompt<__half, 2>(a, k, (unsigned)blocks, st) : launch_prompt<__half, 1>(a, k, (unsigned)blocks, st);
 }
 
 int coral_lmhead_kv4_bytes(const coral_lmhead_kv4_config* c, size_t* bytes) {

@@ -15,6 +15,7 @@
 #include "tc_probe.cuh"
 #include "csra.cuh"
 #include "launch.cuh"
+#include "tensor_map.cuh"
 #include "merge.cuh"
 #include "route.cuh"
 #include "tree.cuh"
@@ -289,20 +290,6 @@ int tc_max_pairs(int sms) {
     int n = 0;
     if (cudaOccupancyMaxActiveClusters(&n, head_tc_kernel, &cfg) != cudaSuccess) { cudaGetLastError(); return 0; }
     return n < sms / 2 ? n : sms / 2;
-}
-
-// cuTensorMapEncodeTiled, looked up through the runtime so that the library does not link against libcuda.
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_tiled_fn() {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess)
-        return nullptr;
-    return reinterpret_cast<EncodeTiledFn>(fn);
 }
 
 // Tensor map of the tensor-core path: the packed weights as a 5-d tensor (column in block, row in item,

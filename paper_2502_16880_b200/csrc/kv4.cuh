@@ -178,19 +178,13 @@ struct Kv4Args {
 
 // First row and number of rows of a sequence.
 __device__ __forceinline__ void kv4_rows_of(const Kv4Args& a, int seq, int* first, int* n) {
-    long long q0, q1;
     if (a.q_offsets) {
-        q0 = a.q_offsets[seq];
-        q1 = a.q_offsets[seq + 1];
-        q0 = q0 < 0 ? 0 : q0 > a.n_rows ? a.n_rows : q0;
-        q1 = q1 < q0 ? q0 : q1 > a.n_rows ? a.n_rows : q1;
-        if (q1 > q0 + a.max_q) q1 = q0 + a.max_q;
+        clamped_range(a.q_offsets, seq, a.n_rows, first, n);
+        *n = min(*n, a.max_q);
     } else {
-        q0 = (long long)seq * a.max_q;
-        q1 = q0 + a.max_q;
+        *first = seq * a.max_q;
+        *n = a.max_q;
     }
-    *first = (int)q0;
-    *n = (int)(q1 - q0);
 }
 
 __device__ __forceinline__ float exp2_fast(float x) {

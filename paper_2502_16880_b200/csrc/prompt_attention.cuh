@@ -1,0 +1,422 @@
+// Attention over whole prompts on the 5th-generation tensor cores: packed sequences, causal, grouped heads.  For query i of a
+// sequence with Lq queries and Lk keys (the queries stand at its end), and query head h with key head h / G:
+//   out = sum_j softmax_j(scale q . k_j) v_j,  j <= i + Lk - Lq;   lse = log-sum-exp of scale q . k_j
+// in one pass over the keys (running maximum and sum).
+//
+// A block takes two tiles of 128 rows: a row is a token and a query head, Gp heads (a power of two) of a group next to one another, so
+// that few tokens fill a tile too.  Both tiles read the same keys and values, 128 at a time, through a ring filled by TMA.
+//   S_t = Q_t K^T           operands in shared memory, sums in tensor memory (128 columns a tile)
+//   P_t = exp2(S_t - max)   by four warps a tile, a thread a row, back into tensor memory over S_t as 16-bit values
+//   O_t += P_t V            operand A from tensor memory, V as it lies (N-major); sums stay in tensor memory
+// One thread issues all MMAs; while it works on one tile, the other tile's warps do their exponentials.  The maximum is a
+// reference that moves only when a score passes it by 2^8 (P stays below 2^8, its sum is fp32), so O is scaled in place a few times
+// a row at most, by the softmax warps themselves, and nothing else touches it before the end.
+// Masked scores are -inf before anything is computed of them; but a value row with an infinity or a NaN would reach every row of
+// the tile through 0 * inf.  Rows whose result is not finite although their sum is are therefore computed again at the end
+// by a warp each, over the keys that they see.
+#pragma once
+#include <type_traits>
+
+#include "element.cuh"
+#include "tc_prims.cuh"
+
+namespace coral {
+
+constexpr int kPaThreads = 10 * 32;                // warps 0..3 and 4..7: softmax of a tile each, 8: MMAs, 9: copies
+constexpr int kPaKeys = 128;                       // keys of a step
+constexpr int kPaBlock = 128 * 128;                // bytes of 128 rows x 64 columns
+
+struct PaArgs {
+    int n_seq, T, Tk, n_q, n_k, G, gp, D;          // gp: heads side by side in a tile, gp_log2 of them
+    int gp_log2;
+    float c;                                       // scale log2(e)
+    const int64_t *q_offsets, *k_offsets;
+    const void *q, *k, *v;
+    long long ld_q, ld_k, ld_v, ld_out;
+    void* out;
+    float* lse;
+    DeviceState* st;
+};
+
+// A block's share, found once and kept in shared memory.
+struct PaShare {
+    int q0, k0, Lq, Lk, pair;                      // pair < 0: none
+};
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x0, int x1, int x2, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(map), "r"(x0), "r"(x1), "r"(x2), "r"(bar) : "memory");
+}
+// Descriptor of an N-major operand: rows of 64 columns (128 bytes, 128-byte swizzle), eight of them 1024 bytes; the next 64 columns kPaBlock
+// bytes on.
+__device__ __forceinline__ uint64_t pa_desc_n(uint32_t saddr) {
+    return (uint64_t)((saddr >> 4) & 0x3FFF) | ((uint64_t)(kPaBlock >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void pa_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void pa_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// 32 columns of this thread's tensor-memory lane, not waited for.
+__device__ __forceinline__ void pa_ld32(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void pa_st32(uint32_t taddr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+          "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+          "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void pa_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, DeviceState* st) {
+    if (!mbar_try_wait(bar, parity)) mbar_wait(bar, parity, abort_flag, st);
+}
+__device__ __forceinline__ void pa_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void pa_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float pa_exp2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float pa_max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+template <typename T> __device__ __forceinline__ uint32_t pa_pack(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pa_pack<__nv_bfloat16>(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <> __device__ __forceinline__ uint32_t pa_pack<__half>(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// The sequence and pair of tiles of slot `slot` (pairs of a sequence from its end: the longest rows start first).  All threads.
+__device__ __forceinline__ void pa_find(const PaArgs& a, int slot, PaShare* out, int* s_scan) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = 256 >> a.gp_log2;
+    int before = 0;
+    for (int base = 0; base < a.n_seq; base += kPaThreads) {
+        const int seq = base + threadIdx.x;
+        int q0 = 0, Lq = 0;
+        if (seq < a.n_seq) clamped_range(a.q_offsets, seq, a.T, &q0, &Lq);
+        const int n = (Lq + per - 1) / per;
+        int sum = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        if (lane == 31) s_scan[warp] = sum;
+        __syncthreads();
+        int at = before;
+        for (int w = 0; w < kPaThreads / 32; ++w) {
+            if (w < warp) at += s_scan[w];
+            before += s_scan[w];
+        }
+        const int first = at + sum - n;
+        if (slot >= first && slot < first + n) {
+            int k0 = q0, Lk = Lq;
+            if (a.k_offsets) clamped_range(a.k_offsets, seq, a.Tk, &k0, &Lk);
+            *out = PaShare{q0, k0, Lq, Lk, n - 1 - (slot - first)};
+        }
+        __syncthreads();
+        if (slot < before) return;
+    }
+}
+
+// One row again, by a warp: only keys that it sees take part.  m is the reference in powers of two, four columns a lane.
+template <typename T>
+__device__ __noinline__ void pa_row_again(const PaArgs& a, const T* q, const T* k, const T* v, int seen, float m, float inv, T* out) {
+    const int lane = threadIdx.x & 31;
+    float acc[4] = {};
+    for (int j0 = 0; j0 < seen; j0 += 32) {
+        const int j = j0 + lane;
+        float p = 0.f;
+        if (j < seen) {
+            float s = 0.f;
+            for (int c = 0; c < a.D; c += 8) {
+                float x[8], y[8];
+                Elem<T>::load8(q + c, x);
+                Elem<T>::load8(k + (long long)j * a.ld_k + c, y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s = fmaf(x[i], y[i], s);
+            }
+            p = pa_exp2(s * a.c - m);
+        }
+        for (int i = 0; i < min(32, seen - j0); ++i) {
+            const float w = __shfl_sync(0xffffffffu, p, i);
+            if (lane * 4 < a.D) {
+                const uint2 r = *reinterpret_cast<const uint2*>(v + (long long)(j0 + i) * a.ld_v + lane * 4);
+                T h[4];
+                *reinterpret_cast<uint2*>(h) = r;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, Elem<T>::up(h[e]), acc[e]);
+            }
+        }
+    }
+    if (lane * 4 < a.D) {
+        T h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = Elem<T>::down(acc[e] * inv);
+        *reinterpret_cast<uint2*>(out + lane * 4) = *reinterpret_cast<const uint2*>(h);
+    }
+}
+
+// DB: blocks of 64 columns of a head (1 or 2).  STAGES: tiles of 128 keys or values in the ring.
+template <int DB> constexpr int kPaStages = DB == 2 ? 5 : 8;
+template <int DB> constexpr size_t pa_smem_bytes() { return 1024 + (size_t)(2 + kPaStages<DB>) * DB * kPaBlock; }
+
+template <typename T, int DB>
+__global__ void __launch_bounds__(kPaThreads, 1)
+prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                        const __grid_constant__ CUtensorMap map_v) {
+    constexpr int STAGES = kPaStages<DB>, kTile = DB * kPaBlock;
+    extern __shared__ unsigned char pa_smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pa_smem_raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char* s_kv = smem + 2 * kTile;
+    __shared__ __align__(8) uint64_t q_full, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_full[2], pv_done[2];
+    __shared__ PaShare share;
+    __shared__ int s_scan[kPaThreads / 32];
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    pdl_wait();
+    const int hgs = a.n_k * (a.G >> a.gp_log2), hg = blockIdx.x % hgs, slot = blockIdx.x / hgs;
+    if (threadIdx.x == 0) {
+        share.pair = -1;
+        if (blockIdx.x == 0) a.st->status = 0;      // a wait would have to fail millions of polls before this
+        mbar_init(smem_u32(&q_full), 1);
+        for (int i = 0; i < STAGES; ++i) {
+            mbar_init(smem_u32(&kv_full[i]), 1);
+            mbar_init(smem_u32(&kv_empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&s_full[i]), 1);
+            mbar_init(smem_u32(&p_full[i]), 4);
+            mbar_init(smem_u32(&pv_done[i]), 1);
+        }
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+    pa_find(a, slot, &share, s_scan);
+    __syncthreads();
+    const PaShare sh = share;
+    if (sh.pair < 0) return;
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const int tile_tokens = 128 >> a.gp_log2, per_head = a.G >> a.gp_log2;
+    const int kv_head = hg / per_head, head0 = kv_head * a.G + (hg - kv_head * per_head) * a.gp;
+    const int past = sh.Lk - sh.Lq;                            // token i sees keys up to i + past
+    // steps of a tile: keys that its last token sees
+    auto steps_of = [&](int t) {
+        const int tok0 = (sh.pair * 2 + t) * tile_tokens;
+        if (tok0 >= sh.Lq) return 0;
+        const int last = min(tok0 + tile_tokens, sh.Lq) - 1;
+        return max(0, min(last + past + 1, sh.Lk) + kPaKeys - 1) / kPaKeys;
+    };
+    const int n0 = steps_of(0), n1 = steps_of(1), n = max(n0, n1);
+
+    if (warp == 9) {
+        if (lane == 0 && n > 0) {
+            mbar_expect_tx(smem_u32(&q_full), 2 * kTile);
+            for (int t = 0; t < 2; ++t)
+                for (int b = 0; b < DB; ++b)
+                    tma_load_3d(smem_u32(smem + t * kTile + b * kPaBlock), &map_q, b * 64, head0, sh.q0 + (sh.pair * 2 + t) * tile_tokens, smem_u32(&q_full));
+            int stage = 0;
+            uint32_t phase = 0;
+            for (int i = 0; i < 2 * n; ++i) {
+                pa_wait(smem_u32(&kv_empty[stage]), phase ^ 1u, &abort_flag, a.st);
+                const uint32_t bar = smem_u32(&kv_full[stage]);
+                mbar_expect_tx(bar, kTile);
+                for (int b = 0; b < DB; ++b)
+                    tma_load_3d(smem_u32(s_kv + stage * kTile + b * kPaBlock), i & 1 ? &map_v : &map_k, b * 64, kv_head, sh.k0 + (i >> 1) * kPaKeys, bar);
+                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            }
+            // nothing is left on its way when the block ends, an expired wait elsewhere included
+            pa_wait(smem_u32(&q_full), 0, &abort_flag, a.st);
+            for (int i = max(0, 2 * n - STAGES); i < 2 * n; ++i) pa_wait(smem_u32(&kv_full[i % STAGES]), (uint32_t)(i / STAGES) & 1u, &abort_flag, a.st);
+        }
+    } else if (warp == 8) {
+        if (lane == 0 && n > 0) {
+            constexpr uint32_t kType = std::is_same_v<T, __nv_bfloat16> ? 1u : 0u;
+            const int d16 = (a.D + 15) / 16;
+            const uint32_t base = (1u << 4) | (kType << 7) | (kType << 10) | (8u << 24);
+            const uint32_t idesc_s = base | (16u << 17), idesc_o = base | (1u << 16) | ((uint32_t)(2 * d16) << 17);
+            const uint32_t sq = smem_u32(smem), skv = smem_u32(s_kv);
+            auto scores = [&](int t, int i) {                  // i: place in the ring's order
+                const uint32_t q = sq + t * kTile, k = skv + (i % STAGES) * kTile;
+                for (int kk = 0; kk < d16; ++kk) {
+                    const uint32_t off = (kk >> 2) * kPaBlock + (kk & 3) * 32;
+                    pa_mma_ss(tmem + t * 128, tc_smem_desc(q + off), tc_smem_desc(k + off), idesc_s, kk > 0);
+                }
+                tc_commit(smem_u32(&s_full[t]));
+            };
+            auto full = [&](int i) { pa_wait(smem_u32(&kv_full[i % STAGES]), (uint32_t)(i / STAGES) & 1u, &abort_flag, a.st); };
+            pa_wait(smem_u32(&q_full), 0, &abort_flag, a.st);
+            full(0);
+            tc_fence_after();
+            if (n0 > 0) scores(0, 0);
+            if (n1 > 0) scores(1, 0);
+            tc_commit(smem_u32(&kv_empty[0]));
+            for (int j = 0; j < n; ++j) {
+                full(2 * j + 1);
+                if (j + 1 < n) full(2 * j + 2);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const int nt = t ? n1 : n0;
+                    if (j < nt) {
+                        pa_wait(smem_u32(&p_full[t]), (uint32_t)j & 1u, &abort_flag, a.st);
+                        tc_fence_after();
+                        const uint32_t v = skv + ((2 * j + 1) % STAGES) * kTile;
+#pragma unroll
+                        for (int kk = 0; kk < kPaKeys / 16; ++kk)
+                            pa_mma_ts(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, pa_desc_n(v + kk * 2048), idesc_o, j > 0 || kk > 0);
+                        tc_commit(smem_u32(&pv_done[t]));
+                    }
+                    if (t == 1) tc_commit(smem_u32(&kv_empty[(2 * j + 1) % STAGES]));
+                    if (j + 1 < nt) scores(t, 2 * j + 2);
+                }
+                if (j + 1 < n) tc_commit(smem_u32(&kv_empty[(2 * j + 2) % STAGES]));
+            }
+        }
+    } else {
+        const int t = warp >> 2, row = (warp & 3) * 32 + lane, nt = t ? n1 : n0;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t ts = tmem + t * 128 + lanes, to = tmem + 256 + t * 128 + lanes;
+        const int tok0 = (sh.pair * 2 + t) * tile_tokens, tok = tok0 + (row >> a.gp_log2), head = head0 + (row & (a.gp - 1));
+        const int seen = max(0, min(tok + past + 1, sh.Lk));   // keys that this row sees
+        const int all_see = max(0, min(tok0 + past + 1, sh.Lk));
+        float m = kNegInf, mc = 0.f;                           // reference, raw and in powers of two
+        unsigned long long sum2 = 0;
+        float s[128];
+        uint32_t* sr = reinterpret_cast<uint32_t*>(s);
+        for (int j = 0; j < nt; ++j) {
+            pa_wait(smem_u32(&s_full[t]), (uint32_t)j & 1u, &abort_flag, a.st);
+            // done since the scores are, but a phase that is not waited for would be taken for the one after the next
+            if (j > 0) pa_wait(smem_u32(&pv_done[t]), (uint32_t)(j - 1) & 1u, &abort_flag, a.st);
+            __syncwarp();
+            tc_fence_after();
+#pragma unroll
+            for (int b = 0; b < 4; ++b) pa_ld32(ts + b * 32, sr + b * 32);
+            pa_ld_wait();
+            if ((j + 1) * kPaKeys > all_see) {
+                const int left = seen - j * kPaKeys;
+#pragma unroll
+                for (int i = 0; i < 128; ++i) s[i] = i < left ? s[i] : kNegInf;
+            }
+            float m4[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+            for (int i = 4; i < 128; i += 8)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m4[e] = i + 4 + e < 128 ? pa_max3(m4[e], s[i + e], s[i + 4 + e]) : fmaxf(m4[e], s[i + e]);
+            const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            const bool moves = top * a.c > mc + 8.f || (m == kNegInf && top > kNegInf);
+            if (__any_sync(0xffffffffu, moves)) {
+                const float next = moves ? top : m, next_c = next == kNegInf ? 0.f : next * a.c;
+                const float f = !moves ? 1.f : m == kNegInf ? 0.f : pa_exp2(mc - next_c);
+                m = next;
+                mc = next_c;
+                sum2 = mul2(sum2, pair_of(f, f));
+                if (j > 0) {
+#pragma unroll 1
+                    for (int b = 0; b < 2 * DB; ++b) {
+                        uint32_t o[32];
+                        pa_ld32(to + b * 32, o);
+                        pa_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                        pa_st32(to + b * 32, o);
+                    }
+                    pa_st_wait();
+                }
+            }
+            const unsigned long long c2 = pair_of(a.c, a.c), m2 = pair_of(-mc, -mc);
+            uint32_t p[64];
+#pragma unroll
+            for (int i = 0; i < 64; ++i) {
+                const float2 x = halves(fma2(pair_of(s[2 * i], s[2 * i + 1]), c2, m2));
+                const float lo = pa_exp2(x.x), hi = pa_exp2(x.y);
+                asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum2) : "l"(pair_of(lo, hi)));
+                p[i] = pa_pack<T>(lo, hi);
+            }
+            pa_st32(ts, p);
+            pa_st32(ts + 32, p + 32);
+            pa_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&p_full[t]));
+        }
+        const float2 sums = halves(sum2);
+        const float sum = sums.x + sums.y, inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (nt > 0) {
+            pa_wait(smem_u32(&pv_done[t]), (uint32_t)(nt - 1) & 1u, &abort_flag, a.st);
+            __syncwarp();
+            tc_fence_after();
+        }
+        const bool live = tok < sh.Lq;
+        T* out = static_cast<T*>(a.out) + (long long)(sh.q0 + tok) * a.ld_out + (long long)head * a.D;
+        float odd = 0.f;                                       // NaN where a result is not finite
+#pragma unroll
+        for (int b = 0; b < 2 * DB; ++b) {
+            if (b * 32 >= a.D) break;
+            uint32_t o[32];
+            if (nt > 0) {
+                pa_ld32(to + b * 32, o);
+                pa_ld_wait();
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int col = b * 32 + g * 8;
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = sum == 0.f ? 0.f : __uint_as_float(o[g * 8 + e]) * inv;
+                    if (col < a.D) odd = fmaf(x[e], 0.f, odd);
+                }
+                if (live && col < a.D) Elem<T>::store8(out + col, x);
+            }
+        }
+        if (live && a.lse) a.lse[(long long)(sh.q0 + tok) * a.n_q + head] = sum == 0.f ? kNegInf : (mc + log2f(sum)) * 0.69314718055994531f;
+        // rows of finite weights whose result is not: values that they do not see may be the reason
+        const bool again = live && sum > 0.f && sum < __int_as_float(0x7f800000) && odd != 0.f;
+        for (uint32_t todo = __ballot_sync(0xffffffffu, again); todo; todo &= todo - 1) {
+            const int r = __ffs(todo) - 1;
+            const int tok_r = __shfl_sync(0xffffffffu, tok, r), head_r = __shfl_sync(0xffffffffu, head, r), seen_r = __shfl_sync(0xffffffffu, seen, r);
+            const float mc_r = __shfl_sync(0xffffffffu, mc, r), inv_r = __shfl_sync(0xffffffffu, inv, r);
+            pa_row_again<T>(a, static_cast<const T*>(a.q) + (long long)(sh.q0 + tok_r) * a.ld_q + (long long)head_r * a.D,
+                            static_cast<const T*>(a.k) + (long long)sh.k0 * a.ld_k + (long long)kv_head * a.D,
+                            static_cast<const T*>(a.v) + (long long)sh.k0 * a.ld_v + (long long)kv_head * a.D, seen_r, mc_r, inv_r,
+                            static_cast<T*>(a.out) + (long long)(sh.q0 + tok_r) * a.ld_out + (long long)head_r * a.D);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+    pdl_launch_dependents();
+}
+
+}  // namespace coral

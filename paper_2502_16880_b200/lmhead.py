@@ -31,6 +31,7 @@ CORAL_OUTPUT_JOINT, CORAL_OUTPUT_FACTORISED, CORAL_OUTPUT_FACTORISED_RENORM = 0,
 CORAL_TYPE_F32, CORAL_TYPE_BF16, CORAL_TYPE_F16 = 0, 1, 2
 CORAL_GATE_NONE, CORAL_GATE_CHANNEL, CORAL_GATE_ROW, CORAL_GATE_FULL = 0, 1, 2, 3
 CORAL_ROPE_HALVES, CORAL_ROPE_PAIRS = 0, 1
+CORAL_PROMPT_WORKSPACE_BYTES = 256
 CORAL_PATH_AUTO, CORAL_PATH_STREAM, CORAL_PATH_TCGEN05, CORAL_PATH_SIMT_PLAIN, CORAL_PATH_ADAPTIVE = 0, 1, 2, 3, 4
 
 
@@ -77,6 +78,13 @@ class coral_lmhead_qk_args(ctypes.Structure):
         (n, ctypes.c_int64) for n in ("ld_q", "ld_k", "ld_out_q", "ld_out_k", "ld_dout_q", "ld_dout_k", "ld_dq", "ld_dk")] + [
         (n, ctypes.c_void_p) for n in ("q_dev", "k_dev", "w_q_dev", "w_k_dev", "positions_dev", "freqs_dev", "out_q_dev", "out_k_dev",
                                        "dout_q_dev", "dout_k_dev", "dq_dev", "dk_dev", "dw_q_dev", "dw_k_dev")]
+
+
+class coral_lmhead_prompt_args(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [
+        (n, ctypes.c_int32) for n in ("type", "n_seq", "T", "Tk", "n_q", "n_k", "D")] + [("scale", ctypes.c_float)] + [
+        (n, ctypes.c_int64) for n in ("ld_q", "ld_k", "ld_v", "ld_out")] + [
+        (n, ctypes.c_void_p) for n in ("q_dev", "k_dev", "v_dev", "q_offsets_dev", "k_offsets_dev", "out_dev", "out_lse_dev")]
 
 
 class coral_lmhead_kv4_config(ctypes.Structure):
@@ -135,6 +143,7 @@ _SIGNATURES = {
     "coral_lmhead_qk_rotate": (_i, [ctypes.POINTER(coral_lmhead_qk_args), _vp]),
     "coral_lmhead_qk_rotate_backward_bytes": (_i, [_i, _i, _i, _i, ctypes.POINTER(ctypes.c_size_t)]),
     "coral_lmhead_qk_rotate_backward": (_i, [ctypes.POINTER(coral_lmhead_qk_args), _vp, _vp]),
+    "coral_lmhead_prompt_attention": (_i, [ctypes.POINTER(coral_lmhead_prompt_args), _vp, _vp]),
     "coral_lmhead_kv4_bytes": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), ctypes.POINTER(ctypes.c_size_t)]),
     "coral_lmhead_kv4_store": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), _vp, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, _i, _vp]),
     "coral_lmhead_kv4_load": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), _vp, _vp, _i, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp]),
@@ -715,6 +724,39 @@ def coral_lmhead_qk_rotate_backward(q, k, positions, freqs, dout_q, dout_k, dq, 
         raise ValueError("workspace is smaller than coral_lmhead_qk_rotate_backward_bytes(T, n_q, n_k, D)")
     _check((_lib or load_library()).coral_lmhead_qk_rotate_backward(
         ctypes.byref(a), _op_ptr("workspace", workspace, torch.uint8, None, dev), _op_stream(stream, dev)), "coral_lmhead_qk_rotate_backward")
+
+
+_PROMPT_SIZE = ctypes.sizeof(coral_lmhead_prompt_args)
+
+
+def coral_lmhead_prompt_attention(q, k, v, q_offsets, out, k_offsets=None, scale=None, out_lse=None, workspace=None, stream=None):
+    """Causal attention of packed sequences: queries q [T, n_q, D] over keys and values k, v [Tk, n_k, D], tokens any distance apart.
+    Sequence s has the query rows q_offsets[s] .. q_offsets[s + 1] (int64 [n_seq + 1]) and the keys k_offsets[s] .. k_offsets[s + 1]
+    (None: those of the queries), of which the queries are the last.  scale: 1 / sqrt(D) if None.  out like q; out_lse fp32 [T, n_q].
+    Returns the scratch of the call (CORAL_PROMPT_WORKSPACE_BYTES), which holds the word that coral_lmhead_attention_status reads (from
+    torch's allocator if workspace is None)."""
+    dev = _op_device(q, "q")
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k must be [tokens, heads, D]")
+    t = q.dtype
+    (T, n_q, D), (Tk, n_k, _) = q.shape, k.shape
+    kv = (Tk, n_k, D)
+    (q_p, ld_q), (k_p, ld_k), (v_p, ld_v), (o_p, ld_o) = (_heads_ptr("q", q, t, (T, n_q, D), dev), _heads_ptr("k", k, t, kv, dev),
+                                                          _heads_ptr("v", v, t, kv, dev), _heads_ptr("out", out, t, (T, n_q, D), dev))
+    n_seq = q_offsets.shape[0] - 1
+    a = coral_lmhead_prompt_args(
+        _PROMPT_SIZE, _type_of(q), n_seq, T, Tk, n_q, n_k, D, D ** -0.5 if scale is None else scale, ld_q, ld_k, ld_v, ld_o, q_p, k_p, v_p,
+        _op_ptr("q_offsets", q_offsets, torch.int64, (n_seq + 1,), dev), _op_ptr("k_offsets", k_offsets, torch.int64, (n_seq + 1,), dev), o_p,
+        _op_ptr("out_lse", out_lse, torch.float32, (T, n_q), dev))
+    if n_seq == 0 or T == 0:
+        return workspace
+    if workspace is None:
+        workspace = _op_scratch(CORAL_PROMPT_WORKSPACE_BYTES, q.device, stream)
+    elif workspace.numel() < CORAL_PROMPT_WORKSPACE_BYTES:
+        raise ValueError("workspace is smaller than CORAL_PROMPT_WORKSPACE_BYTES")
+    _check((_lib or load_library()).coral_lmhead_prompt_attention(
+        ctypes.byref(a), _op_ptr("workspace", workspace, torch.uint8, None, dev), _op_stream(stream, dev)), "coral_lmhead_prompt_attention")
+    return workspace
 
 
 def make_kv4_config(n_pages, page, n_heads, D, group, dtype) -> coral_lmhead_kv4_config:
