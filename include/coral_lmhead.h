@@ -650,7 +650,7 @@ int coral_lmhead_kv4_load(const coral_lmhead_kv4_config *cfg, const void *cache_
  * Sums and softmax in fp32; a weight is rounded to fp16 next to its value's step.  A row that sees nothing has out 0 and lse -inf.
  * Tokens that a row does not see have no influence, infinities and NaN too; pages outside [0, n_pages) hold no tokens.
  *   q, out [n_rows x n_q x D] of the cache's type; out_lse fp32 [n_rows x n_q] or NULL; n_q a multiple of n_heads.  Rows outside the
- *   sequences, and rows from max_q on of a sequence, are left as they are.  lens is clamped to width * page, offsets to n_rows.
+ *   sequences, and a sequence's rows from max_q on, are left as they are.  lens is clamped to width * page, offsets to n_rows.
  *   q_offsets int64 [n_seq + 1], not decreasing; tree_mask uint64 [n_rows], needs max_q <= 64.  table int32 [n_seq x width], ld_table apart.
  * n_seq, n_rows >= 0 (0: nothing to do); max_q, n_q, width >= 1; scale finite.  max_q bounds the work that is started, so it should
  * be no more than the longest sequence's rows.  workspace_dev: 256-byte aligned, at least coral_lmhead_kv4_attention_bytes; holds nothing between calls

@@ -176,11 +176,10 @@ struct Kv4Args {
     DeviceState* st;
 };
 
-// First row and number of rows of a sequence.
+// First row and number of rows of a sequence; no more than max_q of them are worked on.
 __device__ __forceinline__ void kv4_rows_of(const Kv4Args& a, int seq, int* first, int* n) {
     if (a.q_offsets) {
         clamped_range(a.q_offsets, seq, a.n_rows, first, n);
-        *n = min(*n, a.max_q);
     } else {
         *first = seq * a.max_q;
         *n = a.max_q;
@@ -239,7 +238,7 @@ __global__ void __launch_bounds__(kKv4Threads, NR == 1 ? 2 : 1) kv4_attention_ke
     const int head = unit % a.c.n_k, seq = unit / a.c.n_k;
     int q0, n;
     kv4_rows_of(a, seq, &q0, &n);
-    const int rows = n * a.G, row0 = row_block * 8 * NR * a.row_groups;
+    const int rows = min(n, a.max_q) * a.G, row0 = row_block * 8 * NR * a.row_groups;
     if (row0 >= rows) return;
     const long long most = (long long)a.width * a.c.page;
     const int len = (int)max(0LL, min((long long)a.lens[seq], most));
@@ -386,8 +385,8 @@ __global__ void __launch_bounds__(kKv4Threads, NR == 1 ? 2 : 1) kv4_attention_ke
                     s[r][e] = s[r][e] * back1[r][e & 1] * back2[r][e & 1];
                     if constexpr (CUT) {
                         const int t = token + g + (e < 2 ? 0 : 8), at = t - (len - n), row = node[r][e & 1];
-                        bool see = t < len && row < n;
-                        if (see && at >= 0) see = a.tree ? __ldg(a.tree + q0 + row) >> at & 1ull : at <= row;
+                        bool see = t < len && (row0 + (group * NR + r) * 8 + 2 * c + (e & 1)) < rows;
+                        if (see && at >= 0) see = a.tree ? at < kKv4MaxTree && __ldg(a.tree + q0 + row) >> at & 1ull : at <= row;
                         if (!see) {
                             seen &= ~(1u << (4 * r + e));
                             s[r][e] = kNegInf;
@@ -619,7 +618,7 @@ __global__ void __launch_bounds__(256) kv4_join_kernel(const Kv4Args a) {
     int q0, n;
     kv4_rows_of(a, (int)seq, &q0, &n);
     const int tok = (int)(node - seq * a.max_q);
-    if (tok >= n) return;
+    if (tok >= min(n, a.max_q)) return;
     const long long at = (long long)(q0 + tok) * a.n_q + head, step = (long long)a.n_rows * a.n_q;
     float top = kNegInf;
     for (int s = lane; s < a.splits; s += 32) top = fmaxf(top, __ldcg(&a.part_ml[s * step + at]).x);
