@@ -27,7 +27,7 @@ bool rows_ok(const void* p, int64_t ld, int heads, int D, int esize) {
 
 // ---- norm and rotation of queries and keys -------------------------------------------------------------------
 constexpr int kQkMaxHeads = 4096;
-constexpr int kQkMaxGrid = 4 * kSms;               // blocks of a backward call, a partial row of column sums each
+constexpr int kQkBlocks = 2;                       // resident blocks a SM; a block of a backward call has a partial row of column sums
 
 bool qk_args_ok(const coral_lmhead_qk_args* a) {
     if (!a || a->struct_size != sizeof(*a)) return false;
@@ -42,31 +42,55 @@ bool qk_args_ok(const coral_lmhead_qk_args* a) {
 // Two granules an item, of eight columns where the members of a pair lie a multiple of eight apart, else of four.
 bool qk_eight(const coral_lmhead_qk_args* a) { return a->style == CORAL_ROPE_PAIRS || a->rot % 16 == 0; }
 
+// Threads a head if that is 4 or 8 and each has a whole item (heads of 64 and 128 columns, as a rule), else 0.
+int qk_whole(const coral_lmhead_qk_args* a, const QkArgs& k) {
+    const int N = qk_eight(a) ? 8 : 4;
+    return N == 8 && k.items == k.lanes && a->D % 16 == 0 && (k.lanes == 4 || k.lanes == 8) ? k.lanes : 0;
+}
+
 QkArgs qk_kernel_args(const coral_lmhead_qk_args* a) {
     QkArgs k{};
     k.T = a->T; k.n_q = a->n_q; k.n_k = a->n_k; k.D = a->D; k.rot = a->rot; k.eps = a->eps;
     const int N = qk_eight(a) ? 8 : 4, turned = a->style == CORAL_ROPE_HALVES ? a->rot : 0;
     k.items = turned / 2 / N + (a->D - turned + 2 * N - 1) / (2 * N);
     for (k.lanes = 1; k.lanes < k.items; k.lanes *= 2) {}
-    // tokens a block: the more, the fewer threads compute angles; few tokens go to as many blocks as there are
-    k.tokens = std::clamp(a->T / (4 * kSms), 1, kQkTokens);
+    // a warp takes all heads of a token, or as few at a time as give every warp of the GPU some, since each computes the angles anew
+    const int rows = 32 / k.lanes, most = std::max(a->n_q, a->n_k);
+    k.shares = (int)std::clamp((16LL * kSms + a->T - 1) / a->T, 1LL, (long long)(most + rows - 1) / rows);
+    for (int i = 0; i < 2; ++i) {
+        const int heads = i ? a->n_k : a->n_q;
+        k.span[i] = (heads + k.shares - 1) / k.shares;
+    }
     k.pos = a->positions_dev; k.freq = a->freqs_dev;
     k.x[0] = a->q_dev; k.x[1] = a->k_dev; k.ld_x[0] = a->ld_q; k.ld_x[1] = a->ld_k;
     k.w[0] = a->w_q_dev; k.w[1] = a->w_k_dev;
     return k;
 }
 
+// Blocks of a call: no more than have turns, or than are resident.
+int qk_grid(const QkArgs& k) {
+    const long long turns = (long long)k.T * k.shares;
+    return (int)std::min((turns + kQkWarps - 1) / kQkWarps, (long long)kQkBlocks * kSms);
+}
+
+template <typename T, bool HALVES, int N, int L>
+cudaError_t launch_qk_kernel(const QkArgs& k, bool backward, int grid, cudaStream_t st) {
+    return launch_pdl(backward ? qk_rotate_backward_kernel<T, HALVES, N, L> : qk_rotate_kernel<T, HALVES, N, L>, dim3(grid), dim3(kQkThreads), 0, st, k);
+}
+
 template <typename T>
 int launch_qk(const coral_lmhead_qk_args* a, const QkArgs& k, bool backward, int grid, cudaStream_t st) {
-    const bool pairs = a->style == CORAL_ROPE_PAIRS, eight = qk_eight(a);
-    size_t smem = (size_t)k.tokens * k.rot * 4;
-    if (backward) {
-        smem = std::max(smem, (size_t)kQkThreads * 2 * (eight ? 8 : 4) * 4);
-        auto f = pairs ? qk_rotate_backward_kernel<T, false, 8> : eight ? qk_rotate_backward_kernel<T, true, 8> : qk_rotate_backward_kernel<T, true, 4>;
-        return launch_pdl(f, dim3(grid), dim3(kQkThreads), smem, st, k) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
-    }
-    auto f = pairs ? qk_rotate_kernel<T, false, 8> : eight ? qk_rotate_kernel<T, true, 8> : qk_rotate_kernel<T, true, 4>;
-    return launch_pdl(f, dim3(grid), dim3(kQkThreads), smem, st, k) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+    const int L = qk_whole(a, k);
+    cudaError_t e;
+    if (a->style == CORAL_ROPE_PAIRS)
+        e = L == 8 ? launch_qk_kernel<T, false, 8, 8>(k, backward, grid, st) : L == 4 ? launch_qk_kernel<T, false, 8, 4>(k, backward, grid, st)
+                   : launch_qk_kernel<T, false, 8, 0>(k, backward, grid, st);
+    else if (qk_eight(a))
+        e = L == 8 ? launch_qk_kernel<T, true, 8, 8>(k, backward, grid, st) : L == 4 ? launch_qk_kernel<T, true, 8, 4>(k, backward, grid, st)
+                   : launch_qk_kernel<T, true, 8, 0>(k, backward, grid, st);
+    else
+        e = launch_qk_kernel<T, true, 4, 0>(k, backward, grid, st);
+    return e == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
 }
 
 int launch_qk_type(const coral_lmhead_qk_args* a, const QkArgs& k, bool backward, int grid, cudaStream_t st) {
@@ -210,13 +234,14 @@ int coral_lmhead_qk_rotate(const coral_lmhead_qk_args* a, void* stream) {
     if (a->n_k && (!rows_ok(a->k_dev, a->ld_k, a->n_k, a->D, e) || !rows_ok(a->out_k_dev, a->ld_out_k, a->n_k, a->D, e))) return CORAL_ERR_INVALID;
     QkArgs k = qk_kernel_args(a);
     k.y[0] = a->out_q_dev; k.y[1] = a->out_k_dev; k.ld_y[0] = a->ld_out_q; k.ld_y[1] = a->ld_out_k;
-    return launch_qk_type(a, k, false, (a->T - 1) / k.tokens + 1, static_cast<cudaStream_t>(stream));
+    return launch_qk_type(a, k, false, qk_grid(k), static_cast<cudaStream_t>(stream));
 }
 
 int coral_lmhead_qk_rotate_backward_bytes(int T, int n_q, int n_k, int D, size_t* bytes) {
     if (!bytes || T < 1 || n_q < 0 || n_k < 0 || n_q + n_k < 1 || n_q > kQkMaxHeads || n_k > kQkMaxHeads || D < 8 || D > kQkMaxD || D % 8 != 0)
         return CORAL_ERR_INVALID;
-    *bytes = (size_t)std::min(T, kQkMaxGrid) * 2 * D * sizeof(float);
+    const long long turns = (long long)T * std::max(n_q, n_k);        // at most: a head each
+    *bytes = (size_t)std::min((turns + kQkWarps - 1) / kQkWarps, (long long)kQkBlocks * kSms) * 2 * D * sizeof(float);
     return CORAL_OK;
 }
 
@@ -238,7 +263,7 @@ int coral_lmhead_qk_rotate_backward(const coral_lmhead_qk_args* a, void* workspa
     k.dy[0] = a->dout_q_dev; k.dy[1] = a->dout_k_dev; k.ld_dy[0] = a->ld_dout_q; k.ld_dy[1] = a->ld_dout_k;
     k.y[0] = a->dq_dev; k.y[1] = a->dk_dev; k.ld_y[0] = a->ld_dq; k.ld_y[1] = a->ld_dk;
     k.part = want ? static_cast<float*>(workspace_dev) : nullptr;
-    const int grid = std::min((a->T - 1) / k.tokens + 1, kQkMaxGrid);
+    const int grid = qk_grid(k);
     const int rc = launch_qk_type(a, k, true, grid, st);
     if (rc != CORAL_OK || !want) return rc;
     return launch_pdl(qk_columns_kernel, dim3((a->D + 31) / 32, 2), dim3(kQkColWarps * 32), 0, st, k.part, grid, a->D, a->dw_q_dev, a->dw_k_dev) == cudaSuccess

@@ -6,20 +6,24 @@
 // Backward, with d = dy turned back, r = 1 / sqrt(mean(x^2) + eps), xh = r x:
 //   dx = w ? r (d w - xh mean(d w xh)) : d,   dw = sum over tokens and heads of d xh
 // Bound by the bytes of the rows (2 resp. 3 tensors).  A thread takes an item of 16 (or 8) columns of a head that holds both
-// members of its pairs, so nothing but the row sums crosses threads, and those stay inside a part of a warp.  The angles of a
-// token serve all of its heads: a block of several tokens computes them once into shared memory, the product position * freq
-// and what is left of it after whole turns in 64 bits (in 32, a position of a million is off by a tenth of a turn).
+// members of its pairs, so nothing but the row sums crosses threads, and those stay inside a part of a warp.  A warp takes a token
+// and some of its heads at a time: it computes the token's angles once, the product position * freq and what is left of it after
+// whole turns in 64 bits (in 32, a position of a million is off by a tenth of a turn), and its threads keep what their item
+// needs of them, times the weights, in registers over all of those heads.  No block-wide barrier but for the column sums.
 #pragma once
+#include <type_traits>
+
 #include "element.cuh"
 
 namespace coral {
 
 constexpr int kQkThreads = 256;
-constexpr int kQkTokens = 8;                        // most tokens of a block's turn
+constexpr int kQkWarps = kQkThreads / 32;
 constexpr int kQkMaxD = 256;
 
 struct QkArgs {
-    int T, n_q, n_k, D, rot, items, lanes, tokens;   // items of a head, threads a head (a power of two), tokens a turn
+    int T, n_q, n_k, D, rot, items, lanes;           // items of a head, threads a head (a power of two)
+    int shares, span[2];                             // warps that share a token, query and key heads of each
     float eps;
     const int32_t* pos;
     const float* freq;
@@ -29,45 +33,61 @@ struct QkArgs {
     float* part;                                     // backward: [grid][2][D] column sums, or null
 };
 
-// N (4 or 8) consecutive elements, widened, and back.
-template <typename T, int N>
-__device__ __forceinline__ void load_cols(const T* p, float (&v)[N]) {
-    if constexpr (N == 8) {
-        Elem<T>::load8(p, v);
-    } else if constexpr (sizeof(T) == 4) {
-        const float4 a = *reinterpret_cast<const float4*>(p);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    } else {
-        const uint2 a = *reinterpret_cast<const uint2*>(p);
-        T h[4];
-        *reinterpret_cast<uint2*>(h) = a;
+// N (4 or 8) consecutive elements as N / 2 pairs of fp32 (the two-wide instructions do the arithmetic), and back.
+template <int N> struct QkCols {
+    unsigned long long p[N / 2];
+};
+template <typename T, int N> struct QkRaw {
+    static constexpr int kWords = N * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (kWords == 2) {
+            *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(p);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = Elem<T>::up(h[i]);
+            for (int i = 0; i < kWords; i += 4) *reinterpret_cast<uint4*>(w + i) = reinterpret_cast<const uint4*>(p)[i / 4];
+        }
     }
-}
-template <typename T, int N>
-__device__ __forceinline__ void store_cols(T* p, const float (&v)[N]) {
-    if constexpr (N == 8) {
-        Elem<T>::store8(p, v);
-    } else if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    } else {
-        T h[4];
+    __device__ __forceinline__ QkCols<N> cols() const {
+        QkCols<N> r;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = Elem<T>::down(v[i]);
-        *reinterpret_cast<uint2*>(p) = *reinterpret_cast<uint2*>(h);
+        for (int i = 0; i < N / 2; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                r.p[i] = pair_of(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+            } else if constexpr (std::is_same_v<T, __half>) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                r.p[i] = pair_of(f.x, f.y);
+            } else {
+                r.p[i] = pair_of(bf16_lo(w[i]), bf16_hi(w[i]));
+            }
+        }
+        return r;
+    }
+};
+template <typename T, int N>
+__device__ __forceinline__ void store_cols(T* p, const QkCols<N>& v) {
+    if constexpr (N == 8) {
+        store8v<T>(p, V8{{v.p[0], v.p[1], v.p[2], v.p[3]}});
+    } else {
+        const float2 a = halves(v.p[0]), b = halves(v.p[1]);
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4*>(p) = make_float4(a.x, a.y, b.x, b.y);
+        } else {
+            const T h[4] = {Elem<T>::down(a.x), Elem<T>::down(a.y), Elem<T>::down(b.x), Elem<T>::down(b.y)};
+            *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(h);
+        }
     }
 }
 
-// What this thread's item covers: columns at c0 and at c1 (N each, c1 < 0: none), the first of its pairs, and whether its
-// granules are rotated.  HALVES: pair i is columns i and rot / 2 + i, an item is N pairs; behind the rotated columns come items of
-// two neighbouring granules.  Otherwise pair i is columns 2 i and 2 i + 1, and all items are two neighbouring granules.
-template <bool HALVES, int N>
+// What this thread's item covers: columns at c0 and at c1 (N each, < 0: none), the first of its pairs, and whether its granules are
+// turned.  HALVES: pair i is columns i and rot / 2 + i, an item is N pairs; behind the turned columns come items of two neighbouring
+// granules.  Otherwise pair i is columns 2 i and 2 i + 1, and all items are two neighbouring granules.  ALL: every thread has both.
+template <typename T, bool HALVES, int N, bool ALL>
 struct QkItem {
     int c0 = -1, c1 = -1, pair = 0;
     bool turn0 = false, turn1 = false;
     __device__ __forceinline__ QkItem(int i, const QkArgs& a) {
-        if (i >= a.items) return;
+        if (!ALL && i >= a.items) return;
         const int turned = HALVES ? a.rot / 2 / N : 0;
         if (i < turned) {
             c0 = i * N;
@@ -76,203 +96,272 @@ struct QkItem {
             turn0 = turn1 = true;
         } else {
             c0 = (HALVES ? a.rot : 0) + (i - turned) * 2 * N;
-            c1 = c0 + N < a.D ? c0 + N : -1;
+            c1 = ALL || c0 + N < a.D ? c0 + N : -1;
             pair = c0 / 2;
             turn0 = !HALVES && c0 < a.rot;
             turn1 = !HALVES && c1 >= 0 && c1 < a.rot;
         }
     }
-    // Turns the item's pairs (back: by the opposite angle).
-    __device__ __forceinline__ void turn(float (&u)[N], float (&v)[N], const float* cs, const float* sn, float back) const {
-        if (HALVES) {
-            if (!turn0) return;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float c = cs[pair + i], s = sn[pair + i] * back, a = u[i], b = v[i];
-                u[i] = a * c - b * s;
-                v[i] = b * c + a * s;
-            }
-        } else {
-            half(u, turn0, cs + pair, sn + pair, back);
-            half(v, turn1, cs + pair + N / 2, sn + pair + N / 2, back);
-        }
+    __device__ __forceinline__ void load(const T* row, bool on, QkRaw<T, N>& u, QkRaw<T, N>& v) const {
+        u = v = QkRaw<T, N>{};
+        if (on && (ALL || c0 >= 0)) u.load(row + c0);
+        if (on && (ALL || c1 >= 0)) v.load(row + c1);
     }
-    static __device__ __forceinline__ void half(float (&u)[N], bool on, const float* cs, const float* sn, float back) {
-        if (!on) return;
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            const float c = cs[i], s = sn[i] * back, a = u[2 * i], b = u[2 * i + 1];
-            u[2 * i] = a * c - b * s;
-            u[2 * i + 1] = b * c + a * s;
-        }
+    __device__ __forceinline__ void store(T* row, const QkCols<N>& u, const QkCols<N>& v) const {
+        if (ALL || c0 >= 0) store_cols<T, N>(row + c0, u);
+        if (ALL || c1 >= 0) store_cols<T, N>(row + c1, v);
     }
 };
 
-// Cosines and sines of a turn's tokens: the product in 64 bits is exact to 2^-53, and so are the turns taken off it.
-__device__ __forceinline__ void qk_angles(const QkArgs& a, int t0, int n, float* cs, float* sn) {
-    const int half = a.rot >> 1;
-    for (int i = threadIdx.x; i < n * half; i += blockDim.x) {
-        const int t = i / half;
-        const double turns = (double)a.pos[t0 + t] * (double)a.freq[i - t * half] * 0.15915494309189533577;
-        sincospif((float)(2.0 * (turns - rint(turns))), &sn[i], &cs[i]);
+// The turn of an item as factors, times weights: u' = u uc + v~ us, v' = v vc + u~ vs, where v~ is the other granule (HALVES) or the
+// granule itself with the members of its pairs exchanged.  Columns that are not turned have the factors (weight, 0).
+template <int N> struct QkTurn {
+    QkCols<N> uc, us, vc, vs;
+    template <bool HALVES>
+    __device__ __forceinline__ void operator()(QkCols<N>& u, QkCols<N>& v) const {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const unsigned long long a = u.p[i], b = v.p[i];
+            unsigned long long a2 = a, b2 = b;
+            if (!HALVES) {
+                const float2 x = halves(a), y = halves(b);
+                a2 = pair_of(x.y, x.x);
+                b2 = pair_of(y.y, y.x);
+            }
+            u.p[i] = fma2(HALVES ? b2 : a2, us.p[i], mul2(a, uc.p[i]));
+            v.p[i] = fma2(HALVES ? a2 : b2, vs.p[i], mul2(b, vc.p[i]));
+        }
     }
+};
+// wu, wv: the weights of the item's own columns.  BACK: the opposite angle.
+template <bool HALVES, bool BACK, int N, typename Item>
+__device__ __forceinline__ QkTurn<N> qk_turn(const Item& it, const float* cs, const float* sn, const QkCols<N>& wu, const QkCols<N>& wv) {
+    QkTurn<N> r;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        const float2 x = halves(wu.p[i]), y = halves(wv.p[i]);
+        if (HALVES) {
+            const int j = it.pair + 2 * i;
+            const float c0 = it.turn0 ? cs[j] : 1.f, c1 = it.turn0 ? cs[j + 1] : 1.f;
+            const float s0 = it.turn0 ? (BACK ? -sn[j] : sn[j]) : 0.f, s1 = it.turn0 ? (BACK ? -sn[j + 1] : sn[j + 1]) : 0.f;
+            r.uc.p[i] = pair_of(c0 * x.x, c1 * x.y);
+            r.us.p[i] = pair_of(-s0 * y.x, -s1 * y.y);
+            r.vc.p[i] = pair_of(c0 * y.x, c1 * y.y);
+            r.vs.p[i] = pair_of(s0 * x.x, s1 * x.y);
+        } else {
+            const int j = it.pair + i, k = j + N / 2;
+            const float c0 = it.turn0 ? cs[j] : 1.f, s0 = it.turn0 ? (BACK ? -sn[j] : sn[j]) : 0.f;
+            const float c1 = it.turn1 ? cs[k] : 1.f, s1 = it.turn1 ? (BACK ? -sn[k] : sn[k]) : 0.f;
+            r.uc.p[i] = pair_of(c0 * x.x, c0 * x.y);
+            r.us.p[i] = pair_of(-s0 * x.y, s0 * x.x);
+            r.vc.p[i] = pair_of(c1 * y.x, c1 * y.y);
+            r.vs.p[i] = pair_of(-s1 * y.y, s1 * y.x);
+        }
+    }
+    return r;
 }
 
+template <int N>
+__device__ __forceinline__ QkCols<N> mul_cols(const QkCols<N>& a, const QkCols<N>& b) {
+    QkCols<N> r;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) r.p[i] = mul2(a.p[i], b.p[i]);
+    return r;
+}
+template <int N>
+__device__ __forceinline__ QkCols<N> scale_cols(const QkCols<N>& a, float f) {
+    QkCols<N> r;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) r.p[i] = mul2(a.p[i], pair_of(f, f));
+    return r;
+}
+// sum over both granules of a b
+template <int N>
+__device__ __forceinline__ float dot_cols(const QkCols<N>& a0, const QkCols<N>& b0, const QkCols<N>& a1, const QkCols<N>& b1) {
+    unsigned long long x = 0, y = 0;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        x = fma2(a0.p[i], b0.p[i], x);
+        y = fma2(a1.p[i], b1.p[i], y);
+    }
+    const float2 s = halves(x), t = halves(y);
+    return (s.x + s.y) + (t.x + t.y);
+}
+template <int N>
+__device__ __forceinline__ void add_products(QkCols<N>& acc, const QkCols<N>& a, const QkCols<N>& b) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) acc.p[i] = fma2(a.p[i], b.p[i], acc.p[i]);
+}
+
+// Cosines and sines of a token, by a warp: the product in 64 bits is exact to 2^-53, and so are the turns taken off it.
+__device__ __forceinline__ void qk_angles(const QkArgs& a, int t, float* cs, float* sn) {
+    const double p = (double)a.pos[t] * 0.15915494309189533577;
+    __syncwarp();
+    for (int i = threadIdx.x & 31; i < a.rot >> 1; i += 32) {
+        const double turns = p * (double)a.freq[i];
+        sincospif((float)(2.0 * (turns - rint(turns))), &sn[i], &cs[i]);
+    }
+    __syncwarp();
+}
+
+template <int L>
 __device__ __forceinline__ float lanes_sum(float v, int lanes) {
-    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+#pragma unroll
+    for (int o = (L ? L : 32) / 2; o > 0; o >>= 1)
+        if (L || o < lanes) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 
-// The heads of one tensor in a turn, `lanes` threads each: f(token of the turn, head, whether there is one), the same number of
-// times in all threads of a warp.
-template <typename F>
-__device__ __forceinline__ void qk_rows(const QkArgs& a, int heads, int n, F f) {
-    const int per = kQkThreads / a.lanes, mine = threadIdx.x / a.lanes, first = (threadIdx.x & ~31) / a.lanes;
-    int t = mine / heads, h = mine - t * heads;
-    const int step_t = per / heads, step_h = per - step_t * heads;
-    for (int r = first; r < n * heads; r += per) {
-        f(t, h, t < n);
-        t += step_t;
-        h += step_h;
-        if (h >= heads) {
-            h -= heads;
-            ++t;
-        }
-    }
-}
-
-template <typename T, bool HALVES, int N>
-__global__ void __launch_bounds__(kQkThreads) qk_rotate_kernel(QkArgs a) {
-    extern __shared__ float qk_smem[];
-    float *cs = qk_smem, *sn = qk_smem + a.tokens * (a.rot >> 1);
-    const int lane = threadIdx.x & (a.lanes - 1), half = a.rot >> 1;
-    const QkItem<HALVES, N> it(lane, a);
+// L: threads a head where every item is whole (0: any number, at run time).  A warp's turn is a token with a share of its query heads and
+// one of its key heads; two rows of heads are worked on while the next two are on their way.
+template <typename T, bool HALVES, int N, int L>
+__global__ void __launch_bounds__(kQkThreads, 2) qk_rotate_kernel(const __grid_constant__ QkArgs a) {
+    __shared__ __align__(16) float s_cs[kQkWarps][kQkMaxD / 2], s_sn[kQkWarps][kQkMaxD / 2];
+    float *cs = s_cs[threadIdx.x >> 5], *sn = s_sn[threadIdx.x >> 5];
+    const int lanes = L ? L : a.lanes, lane = threadIdx.x & 31, row = lane / lanes, rows = 32 / lanes;
+    const QkItem<T, HALVES, N, L != 0> it(lane & (lanes - 1), a);
     const float inv_d = 1.f / (float)a.D;
+    const int warps = gridDim.x * kQkWarps, step = rows * a.D;
+    const long long units = (long long)a.T * a.shares;
     pdl_wait();
-    const int t0 = blockIdx.x * a.tokens, n = min(a.tokens, a.T - t0);
-    qk_angles(a, t0, n, cs, sn);
-    __syncthreads();
+    for (long long unit = blockIdx.x * kQkWarps + (threadIdx.x >> 5); unit < units; unit += warps) {
+        const int t = a.shares == 1 ? (int)unit : (int)(unit / a.shares), share = (int)(unit - (long long)t * a.shares);
+        bool known = false;                                    // the token's angles
+#pragma unroll 1
+        for (int part = 0; part < 2; ++part) {
+            const int h0 = share * a.span[part], heads = min(a.span[part], (part ? a.n_k : a.n_q) - h0);
+            if (heads <= 0) continue;
+            const T *w = static_cast<const T*>(a.w[part]), *from = static_cast<const T*>(a.x[part]) + t * a.ld_x[part] + (h0 + row) * a.D;
+            T* to = static_cast<T*>(a.y[part]) + t * a.ld_y[part] + (h0 + row) * a.D;
+            QkRaw<T, N> u0[2], v0[2], u1[2], v1[2];
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-        const int heads = part ? a.n_k : a.n_q;
-        if (heads == 0) continue;
-        const T* x = static_cast<const T*>(a.x[part]);
-        const T* w = static_cast<const T*>(a.w[part]);
-        T* y = static_cast<T*>(a.y[part]);
-        qk_rows(a, heads, n, [&](int t, int h, bool on) {
-            const T* from = x + (size_t)(t0 + t) * a.ld_x[part] + (size_t)h * a.D;
-            float u[N] = {}, v[N] = {};
-            if (on && it.c0 >= 0) load_cols<T, N>(from + it.c0, u);
-            if (on && it.c1 >= 0) load_cols<T, N>(from + it.c1, v);
-            if (w) {
-                float ss = 0.f;
+            for (int i = 0; i < 2; ++i) it.load(from + i * step, row + i * rows < heads, u0[i], v0[i]);
+            if (!known) qk_angles(a, t, cs, sn);
+            known = true;
+            it.load(w, w != nullptr, u1[0], v1[0]);            // from L1: kept in the turn's factors only
+            QkCols<N> wu = u1[0].cols(), wv = v1[0].cols();
+            if (!w)
 #pragma unroll
-                for (int i = 0; i < N; ++i) ss += u[i] * u[i] + v[i] * v[i];
-                const float r = 1.f / sqrtf(lanes_sum(ss, a.lanes) * inv_d + a.eps);
-                float wu[N] = {}, wv[N] = {};
-                if (it.c0 >= 0) load_cols<T, N>(w + it.c0, wu);
-                if (it.c1 >= 0) load_cols<T, N>(w + it.c1, wv);
+                for (int i = 0; i < N / 2; ++i) wu.p[i] = wv.p[i] = pair_of(1.f, 1.f);
+            const QkTurn<N> f = qk_turn<HALVES, false>(it, cs, sn, wu, wv);
+            for (int h = row; h - row < heads; h += 2 * rows) {
+                from += 2 * step;
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    u[i] *= r * wu[i];
-                    v[i] *= r * wv[i];
+                for (int i = 0; i < 2; ++i) it.load(from + i * step, h + (2 + i) * rows < heads, u1[i], v1[i]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    QkCols<N> u = u0[i].cols(), v = v0[i].cols();
+                    if (w) {
+                        const float r = rsqrtf(fmaf(lanes_sum<L>(dot_cols(u, u, v, v), lanes), inv_d, a.eps));
+                        u = scale_cols(u, r);
+                        v = scale_cols(v, r);
+                    }
+                    f.template operator()<HALVES>(u, v);
+                    if (h + i * rows < heads) it.store(to + i * step, u, v);
+                    u0[i] = u1[i];
+                    v0[i] = v1[i];
                 }
+                to += 2 * step;
             }
-            if (!on) return;
-            it.turn(u, v, cs + t * half, sn + t * half, 1.f);
-            T* to = y + (size_t)(t0 + t) * a.ld_y[part] + (size_t)h * a.D;
-            if (it.c0 >= 0) store_cols<T, N>(to + it.c0, u);
-            if (it.c1 >= 0) store_cols<T, N>(to + it.c1, v);
-        });
+        }
     }
     pdl_launch_dependents();
 }
 
-// Blocks take turns of tokens, grid apart, and keep the column sums of all their rows in registers; the sums go through a fixed
-// order (a thread's rows, the block's threads, the blocks' partial rows), so the same call gives the same bits.
-template <typename T, bool HALVES, int N>
-__global__ void __launch_bounds__(kQkThreads) qk_rotate_backward_kernel(QkArgs a) {
-    extern __shared__ float qk_smem[];
-    float *cs = qk_smem, *sn = qk_smem + a.tokens * (a.rot >> 1);
-    const int lane = threadIdx.x & (a.lanes - 1), half = a.rot >> 1;
-    const QkItem<HALVES, N> it(lane, a);
+// The column sums of a warp's rows stay in registers; they go through a fixed order (a thread's rows, the block's threads, the blocks'
+// partial rows), so the same call gives the same bits.
+template <typename T, bool HALVES, int N, int L>
+__global__ void __launch_bounds__(kQkThreads, 2) qk_rotate_backward_kernel(const __grid_constant__ QkArgs a) {
+    __shared__ __align__(16) float s_cs[kQkWarps][kQkMaxD / 2], s_sn[kQkWarps][kQkMaxD / 2];
+    __shared__ float s_sum[2 * N * kQkThreads];               // [column of an item][thread]
+    float *cs = s_cs[threadIdx.x >> 5], *sn = s_sn[threadIdx.x >> 5];
+    const int lanes = L ? L : a.lanes, lane = threadIdx.x & 31, row = lane / lanes, rows = 32 / lanes;
+    const QkItem<T, HALVES, N, L != 0> it(lane & (lanes - 1), a);
     const float inv_d = 1.f / (float)a.D;
-    float acc[2][2 * N] = {};
+    const int warps = gridDim.x * kQkWarps;
+    const long long units = (long long)a.T * a.shares;
+    QkCols<N> one;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) one.p[i] = pair_of(1.f, 1.f);
     pdl_wait();
-    for (int t0 = blockIdx.x * a.tokens; t0 < a.T; t0 += gridDim.x * a.tokens) {
-        const int n = min(a.tokens, a.T - t0);
-        __syncthreads();
-        qk_angles(a, t0, n, cs, sn);
-        __syncthreads();
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            const int heads = part ? a.n_k : a.n_q;
-            if (heads == 0) continue;
-            const T* x = static_cast<const T*>(a.x[part]);
-            const T* w = static_cast<const T*>(a.w[part]);
-            const T* dy = static_cast<const T*>(a.dy[part]);
-            T* dx = static_cast<T*>(a.y[part]);
-            qk_rows(a, heads, n, [&](int t, int h, bool on) {
-                const size_t tok = (size_t)(t0 + t), head = (size_t)h * a.D;
-                float u[N] = {}, v[N] = {}, du[N] = {}, dv[N] = {};
-                if (on && it.c0 >= 0) load_cols<T, N>(dy + tok * a.ld_dy[part] + head + it.c0, du);
-                if (on && it.c1 >= 0) load_cols<T, N>(dy + tok * a.ld_dy[part] + head + it.c1, dv);
-                if (w) {
-                    if (on && it.c0 >= 0) load_cols<T, N>(x + tok * a.ld_x[part] + head + it.c0, u);
-                    if (on && it.c1 >= 0) load_cols<T, N>(x + tok * a.ld_x[part] + head + it.c1, v);
-                }
-                if (on) it.turn(du, dv, cs + t * half, sn + t * half, -1.f);
-                if (w) {
-                    float ss = 0.f, dot = 0.f;
-                    float wu[N] = {}, wv[N] = {};
-                    if (it.c0 >= 0) load_cols<T, N>(w + it.c0, wu);
-                    if (it.c1 >= 0) load_cols<T, N>(w + it.c1, wv);
-#pragma unroll
-                    for (int i = 0; i < N; ++i) {
-                        ss += u[i] * u[i] + v[i] * v[i];
-                        dot += du[i] * wu[i] * u[i] + dv[i] * wv[i] * v[i];
-                    }
-                    for (int o = a.lanes >> 1; o > 0; o >>= 1) {
-                        ss += __shfl_xor_sync(0xffffffffu, ss, o);
-                        dot += __shfl_xor_sync(0xffffffffu, dot, o);
-                    }
-                    const float r = 1.f / sqrtf(ss * inv_d + a.eps);
-                    const float m = dot * r * inv_d;                        // mean(d w xh)
-                    if (on) {
-#pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            const float xu = r * u[i], xv = r * v[i];
-                            acc[part][i] += du[i] * xu;
-                            acc[part][N + i] += dv[i] * xv;
-                            du[i] = r * (du[i] * wu[i] - xu * m);
-                            dv[i] = r * (dv[i] * wv[i] - xv * m);
-                        }
-                    }
-                }
-                if (!on) return;
-                T* to = dx + tok * a.ld_y[part] + head;
-                if (it.c0 >= 0) store_cols<T, N>(to + it.c0, du);
-                if (it.c1 >= 0) store_cols<T, N>(to + it.c1, dv);
-            });
+#pragma unroll 1
+    for (int part = 0; part < 2; ++part) {
+        const int all_heads = part ? a.n_k : a.n_q;
+        if (all_heads == 0) continue;
+        const T *x = static_cast<const T*>(a.x[part]), *dy = static_cast<const T*>(a.dy[part]), *w = static_cast<const T*>(a.w[part]);
+        T* dx = static_cast<T*>(a.y[part]);
+        const long long ld_x = a.ld_x[part], ld_dy = a.ld_dy[part], ld_dx = a.ld_y[part];
+        QkCols<N> acc_u{}, acc_v{}, wu, wv;
+        {
+            QkRaw<T, N> ru, rv;
+            it.load(w, w != nullptr, ru, rv);
+            wu = ru.cols();
+            wv = rv.cols();
         }
-    }
-    if (a.part) {
-        float* s = qk_smem;                                                 // [threads a column][columns of an item]
+        for (long long unit = blockIdx.x * kQkWarps + (threadIdx.x >> 5); unit < units; unit += warps) {
+            const int t = a.shares == 1 ? (int)unit : (int)(unit / a.shares), h0 = (int)(unit - (long long)t * a.shares) * a.span[part];
+            const int heads = min(a.span[part], all_heads - h0);
+            if (heads <= 0) continue;
+            const T *from = x + t * ld_x + (h0 + row) * a.D, *from_dy = dy + t * ld_dy + (h0 + row) * a.D;
+            T* to = dx + t * ld_dx + (h0 + row) * a.D;
+            QkRaw<T, N> u0, v0, u1, v1, p0, q0, p1, q1;
+            it.load(from_dy, row < heads, p0, q0);
+            it.load(from, row < heads && w, u0, v0);
+            qk_angles(a, t, cs, sn);
+            const QkTurn<N> f = qk_turn<HALVES, true>(it, cs, sn, one, one);
+            for (int h = row; h - row < heads; h += rows) {
+                from += rows * a.D;
+                from_dy += rows * a.D;
+                it.load(from_dy, h + rows < heads, p1, q1);
+                it.load(from, h + rows < heads && w, u1, v1);
+                QkCols<N> du = p0.cols(), dv = q0.cols();
+                f.template operator()<HALVES>(du, dv);
+                if (w) {
+                    QkCols<N> u = u0.cols(), v = v0.cols();
+                    const QkCols<N> dwu = mul_cols(du, wu), dwv = mul_cols(dv, wv);
+                    const float ss = lanes_sum<L>(dot_cols(u, u, v, v), lanes), dot = lanes_sum<L>(dot_cols(dwu, u, dwv, v), lanes);
+                    const float r = rsqrtf(fmaf(ss, inv_d, a.eps));
+                    u = scale_cols(u, r);                                       // xh
+                    v = scale_cols(v, r);
+                    if (h < heads) {
+                        add_products(acc_u, du, u);
+                        add_products(acc_v, dv, v);
+                    }
+                    // r d w - xh r mean(d w xh)
+                    const float m = -dot * r * inv_d * r;
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < 2 * N; ++i) s[i * kQkThreads + threadIdx.x] = acc[part][i];
-            __syncthreads();
-            // one thread a column of an item: its sum over the block's heads
-            for (int c = threadIdx.x; c < 2 * N * a.lanes; c += kQkThreads) {
-                const int i = c / a.lanes, l = c - i * a.lanes;
-                float sum = 0.f;
-                for (int j = l; j < kQkThreads; j += a.lanes) sum += s[i * kQkThreads + j];
-                const QkItem<HALVES, N> of(l, a);
-                const int col = i < N ? of.c0 : of.c1;
-                if (col >= 0) a.part[((size_t)blockIdx.x * 2 + part) * a.D + col + (i < N ? i : i - N)] = sum;
+                    for (int i = 0; i < N / 2; ++i) {
+                        du.p[i] = fma2(u.p[i], pair_of(m, m), mul2(dwu.p[i], pair_of(r, r)));
+                        dv.p[i] = fma2(v.p[i], pair_of(m, m), mul2(dwv.p[i], pair_of(r, r)));
+                    }
+                }
+                if (h < heads) it.store(to, du, dv);
+                to += rows * a.D;
+                u0 = u1;
+                v0 = v1;
+                p0 = p1;
+                q0 = q1;
             }
+        }
+        if (!a.part) continue;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const float2 p = halves(acc_u.p[i]), q = halves(acc_v.p[i]);
+            s_sum[(2 * i) * kQkThreads + threadIdx.x] = p.x;
+            s_sum[(2 * i + 1) * kQkThreads + threadIdx.x] = p.y;
+            s_sum[(N + 2 * i) * kQkThreads + threadIdx.x] = q.x;
+            s_sum[(N + 2 * i + 1) * kQkThreads + threadIdx.x] = q.y;
+        }
+        __syncthreads();
+        // one thread a column of an item: its sum over the block's heads
+        for (int c = threadIdx.x; c < 2 * N * lanes; c += kQkThreads) {
+            const int i = c / lanes, l = c - i * lanes;
+            float sum = 0.f;
+            for (int j = l; j < kQkThreads; j += lanes) sum += s_sum[i * kQkThreads + j];
+            const QkItem<T, HALVES, N, L != 0> of(l, a);
+            const int col = i < N ? of.c0 : of.c1;
+            if (col >= 0) a.part[((size_t)blockIdx.x * 2 + part) * a.D + col + (i < N ? i : i - N)] = sum;
         }
     }
     pdl_launch_dependents();
