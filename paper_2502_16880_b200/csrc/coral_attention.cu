@@ -113,6 +113,8 @@ Kv4Cache kv4_cache(const coral_lmhead_kv4_config* c, const void* base) {
     k.base = static_cast<unsigned char*>(const_cast<void*>(base));
     k.slots = c->n_pages * c->page;
     k.n_k = c->n_heads; k.page = c->page; k.groups = c->D / c->group;
+    k.heads = Divide(c->n_heads);
+    k.subs = Divide(c->page / kKv4Block);
     return k;
 }
 
@@ -151,11 +153,11 @@ Kv4Plan kv4_plan(const coral_lmhead_kv4_config* c, const coral_lmhead_kv4_attent
     for (p.row_groups = 1; p.row_groups < kKv4Warps && p.row_groups * 8 * p.nr < rows; p.row_groups *= 2) {}
     p.row_blocks = (int)((rows - 1) / (p.row_groups * 8 * p.nr) + 1);
     p.units = (long long)a->n_seq * c->n_heads * p.row_blocks;
-    // as many parts as keep every resident block busy, of a stage at least
-    const long long resident = (p.nr == 1 ? 2 : 1) * kSms, stages = ((long long)a->width * c->page + kKv4StageTokens - 1) / kKv4StageTokens;
+    // as many parts as keep every resident block busy, of a span at least
+    const long long resident = (p.nr == 1 ? 2 : 1) * kSms, spans = ((long long)a->width * c->page - 1) / (kKv4SpanBlocks * kKv4Block) + 1;
     long long splits = p.units ? resident / p.units : 1;
     if (p.units * 4 > resident) splits = (4 * resident + p.units - 1) / std::max(1LL, p.units);
-    p.splits = (int)std::clamp(splits, 1LL, std::min(stages, 256LL));
+    p.splits = (int)std::clamp(splits, 1LL, std::min(spans, (long long)kKv4MaxSplits));
     if (p.units == 0) p.splits = 1;
     size_t at = 256;
     if (p.splits > 1) {
@@ -170,8 +172,11 @@ Kv4Plan kv4_plan(const coral_lmhead_kv4_config* c, const coral_lmhead_kv4_attent
 }
 
 template <typename T, int D, int NG, int NR>
-cudaError_t launch_kv4(const Kv4Args& k, const Kv4Plan& p, cudaStream_t st) {
-    constexpr size_t smem = (size_t)kKv4Stages * 8 * (kKv4Block * D + 128 * NG);
+cudaError_t launch_kv4(Kv4Args k, const Kv4Plan& p, cudaStream_t st) {
+    constexpr int chunk = kKv4Chunk<NG, NR> * Kv4Rowset<T, D, NG, NR>::kBytes, outputs = kKv4Warps * 8 * NR * D * 4;
+    const int streams = kKv4Warps / p.row_groups;
+    k.slots = std::min(kKv4Ring<NR> / (streams * chunk), kKv4MaxSlots);
+    const size_t smem = std::max(streams * k.slots * chunk, outputs);          // the warps' outputs take the ring's place
     if (!allow_smem(kv4_attention_kernel<T, D, NG, NR>, smem)) return cudaErrorUnknown;
     return launch_pdl(kv4_attention_kernel<T, D, NG, NR>, dim3((unsigned)(p.units * p.splits)), dim3(kKv4Threads), smem, st, k);
 }
@@ -185,7 +190,7 @@ int launch_kv4_groups(const Kv4Args& k, const Kv4Plan& p, cudaStream_t st) {
     if (e != cudaSuccess) return CORAL_ERR_CUDA;
     if (p.splits == 1) return CORAL_OK;
     const long long rows = (long long)k.n_seq * k.max_q * k.n_q;
-    return launch_pdl(kv4_join_kernel<T, D>, dim3((unsigned)((rows - 1) / 8 + 1)), dim3(256), 0, st, k) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+    return launch_pdl(kv4_join_kernel<T, D>, dim3((unsigned)rows), dim3(kKv4JoinWarps * 32), 0, st, k) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
 }
 
 // ---- attention over prompts ----------------------------------------------------------------------------------

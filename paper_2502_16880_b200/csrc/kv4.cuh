@@ -24,15 +24,28 @@ namespace coral {
 
 constexpr int kKv4Block = 16;                       // tokens of a block
 
+// Quotients by a divisor known on the host: n / d = (umulhi(n, m) + n) >> s for n below 2^31, with s = ceil(log2 d) and
+// m = floor(2^32 (2^s - d) / d) + 1 (the multiply-and-shift division of Granlund and Montgomery).
+struct Divide {
+    uint32_t m, s, d;
+    Divide() = default;
+    __host__ explicit Divide(uint32_t by) : m(0), s(0), d(by) {
+        while ((1u << s) < by) ++s;
+        m = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << s) - by)) / by + 1);
+    }
+    __device__ __forceinline__ int operator()(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> s); }
+};
+
 struct Kv4Cache {
     unsigned char* base;
     int slots;                                      // pages * page
     int n_k, page, groups;
+    Divide heads, subs;                             // by n_k, and by the blocks of a page
     __host__ __device__ int block_bytes(int D) const { return kKv4Block * D + 128 * groups; }
     // start of the block that holds slot `slot` of head `head`
     __device__ __forceinline__ unsigned char* block(int slot, int head, int D) const {
-        const int subs = page / kKv4Block, sub = slot / kKv4Block, page_at = sub / subs;
-        return base + (((long long)page_at * n_k + head) * subs + (sub - page_at * subs)) * block_bytes(D);
+        const int sub = slot / kKv4Block, page_at = subs(sub), per = (int)subs.d;
+        return base + ((long long)(page_at * n_k + head) * per + (sub - page_at * per)) * block_bytes(D);
     }
 };
 
@@ -45,6 +58,7 @@ template <> __device__ __forceinline__ float2 kv4_pair<__nv_bfloat16>(uint32_t w
 template <> __device__ __forceinline__ float2 kv4_pair<__half>(uint32_t w) { return __half22float2(*reinterpret_cast<__half2*>(&w)); }
 
 // ---- tokens into the cache and out of it ---------------------------------------------------------------------
+// Bound by instructions: eight columns a thread, whose codes (and their way to the values' layout) are integer work.
 constexpr int kKv4RowThreads = 256;
 struct Kv4Rows {
     const int64_t* slots;
@@ -53,116 +67,167 @@ struct Kv4Rows {
     long long ld_k, ld_v;
 };
 
-// D / 8 threads a row of a head, eight columns each.  grid: (rows, keys and values).
+// Eight 4-bit numbers of eight threads, transposed: thread i's word of numbers n becomes thread n's word of numbers i.
+__device__ __forceinline__ uint32_t nibbles_transposed(uint32_t w, int lane) {
+    // by distance 4, 2, 1: the half of the numbers that belongs to the partner goes there
+    uint32_t o = __shfl_xor_sync(0xffffffffu, w, 4);
+    w = lane & 4 ? (w & 0xffff0000u) | o >> 16 : (w & 0x0000ffffu) | o << 16;
+    o = __shfl_xor_sync(0xffffffffu, w, 2);
+    w = lane & 2 ? (w & 0xff00ff00u) | (o >> 8 & 0x00ff00ffu) : (w & 0x00ff00ffu) | (o & 0x00ff00ffu) << 8;
+    o = __shfl_xor_sync(0xffffffffu, w, 1);
+    return lane & 1 ? (w & 0xf0f0f0f0u) | (o >> 4 & 0x0f0f0f0fu) : (w & 0x0f0f0f0fu) | (o & 0x0f0f0f0fu) << 4;
+}
+
+// What a thread of D / 8 a row of a head works on: eight columns of the keys (blockIdx.y 0) or values (1).
+template <int D>
+struct Kv4Place {
+    static constexpr int L = D / 8;
+    int row, token, head, l, slot;
+    bool is_v, on;
+    __device__ __forceinline__ Kv4Place(const Kv4Cache& c, const Kv4Rows& a) {
+        row = (int)(blockIdx.x * (kKv4RowThreads / L) + threadIdx.x / L);
+        l = threadIdx.x & (L - 1);
+        is_v = blockIdx.y != 0;
+        token = c.heads(row);
+        head = row - token * c.n_k;
+        const int64_t at = row < a.rows ? a.slots[token] : -1;
+        on = at >= 0 && at < c.slots;
+        slot = (int)at;
+    }
+    template <typename T>
+    __device__ __forceinline__ T* columns(const Kv4Rows& a) const {
+        return static_cast<T*>(is_v ? a.v : a.k) + token * (is_v ? a.ld_v : a.ld_k) + head * D + 8 * l;
+    }
+    // of the thread's word of codes and of its group's (step, low) in the block
+    __device__ __forceinline__ uint32_t* word(unsigned char* blk) const {
+        const int t = slot & 15, n = l & 7;
+        return reinterpret_cast<uint32_t*>(is_v ? blk + 8 * D + (t >> 3) * (4 * D) + ((n * 4 + ((t & 7) >> 1)) * 2 + (t & 1)) * (D / 16) + 4 * (l >> 3)
+                                                : blk + (t * 4 + (l & 3)) * (D / 8) + 4 * (l >> 2));
+    }
+    __device__ __forceinline__ uint32_t* pair(unsigned char* blk, int groups) const {
+        return reinterpret_cast<uint32_t*>(blk + 16 * D) + ((is_v ? groups : 0) + l / (L / groups)) * 16 + (slot & 15);
+    }
+};
+
+// (lowest, - highest) of eight elements; a NaN stays one.
+template <typename T> struct Kv4Range;
+template <> struct Kv4Range<__nv_bfloat16> {
+    using Two = __nv_bfloat162;
+    static __device__ __forceinline__ Two min2(Two a, Two b) { return __hmin2_nan(a, b); }
+    static __device__ __forceinline__ Two max2(Two a, Two b) { return __hmax2_nan(a, b); }
+    static __device__ __forceinline__ Two ends(Two low, Two high) {
+        const __nv_bfloat16 l = __hmin_nan(low.x, low.y), h = __hmax_nan(high.x, high.y);
+        return __halves2bfloat162(l, __hneg(h));
+    }
+};
+template <> struct Kv4Range<__half> {
+    using Two = __half2;
+    static __device__ __forceinline__ Two min2(Two a, Two b) { return __hmin2_nan(a, b); }
+    static __device__ __forceinline__ Two max2(Two a, Two b) { return __hmax2_nan(a, b); }
+    static __device__ __forceinline__ Two ends(Two low, Two high) {
+        const __half l = __hmin_nan(__low2half(low), __high2half(low)), h = __hmax_nan(__low2half(high), __high2half(high));
+        return __halves2half2(l, __hneg(h));
+    }
+};
+
 template <typename T, int D>
-__global__ void __launch_bounds__(kKv4RowThreads) kv4_store_kernel(Kv4Cache c, Kv4Rows a) {
+__global__ void __launch_bounds__(kKv4RowThreads) kv4_store_kernel(const __grid_constant__ Kv4Cache c, const __grid_constant__ Kv4Rows a) {
     constexpr int L = D / 8;
+    using Range = Kv4Range<T>;
+    using Two = typename Range::Two;
     pdl_wait();
-    const int row = (int)(blockIdx.x * (kKv4RowThreads / L) + threadIdx.x / L);
-    const int lane = threadIdx.x & 31, l = lane & (L - 1);
-    const bool is_v = blockIdx.y != 0;
-    const int token = row / c.n_k, head = row - token * c.n_k;
-    const int64_t at = row < a.rows ? a.slots[token] : -1;
-    const bool on = at >= 0 && at < c.slots;
-    const int slot = (int)at;
-    float x[8] = {};
-    if (on) Elem<T>::load8(static_cast<const T*>(is_v ? a.v : a.k) + token * (is_v ? a.ld_v : a.ld_k) + head * D + 8 * l, x);
-    float low = x[0], high = x[0], bad = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        low = fminf(low, x[i]);
-        high = fmaxf(high, x[i]);
-        bad += x[i] * 0.f;                          // NaN for an infinity or a NaN
-    }
+    const Kv4Place<D> p(c, a);
+    uint32_t raw[4] = {};
+    if (p.on) *reinterpret_cast<uint4*>(raw) = *reinterpret_cast<const uint4*>(p.template columns<T>(a));
+    const Two* r2 = reinterpret_cast<const Two*>(raw);
+    Two ends = Range::ends(Range::min2(Range::min2(r2[0], r2[1]), Range::min2(r2[2], r2[3])), Range::max2(Range::max2(r2[0], r2[1]), Range::max2(r2[2], r2[3])));
     const int per = L / c.groups;                   // threads of a group
-    for (int o = 1; o < per; o <<= 1) {
-        low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
-        high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
-        bad += __shfl_xor_sync(0xffffffffu, bad, o);
-    }
-    const uint32_t step_bits = kv4_bits<T>((high - low) / 15.f + bad);
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1)
+        if (o < per) {
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<uint32_t*>(&ends), o);
+            ends = Range::min2(ends, *reinterpret_cast<const Two*>(&other));
+        }
+    const float2 lh = kv4_pair<T>(*reinterpret_cast<uint32_t*>(&ends));
+    const float range = -lh.y - lh.x, bad = range * 0.f;       // NaN for an infinity or a NaN, and for a range that fp32 does not hold
+    const uint32_t step_bits = kv4_bits<T>(range / 15.f + bad);
     const float step = kv4_pair<T>(step_bits).x;
+    // Codes by the reciprocal and one step towards the quotient, rounded by adding 1.5 2^23.  A quotient in the middle between two
+    // codes has few bits and comes out exact.  (A subnormal step has no reciprocal in fp32.)
+    const float inv = step > 1e-37f ? __frcp_rn(step) : 0.f;
+    constexpr float kRound = 12582912.f;
+    const unsigned long long inv2 = pair_of(inv, inv), low2 = pair_of(-lh.x, -lh.x), step2 = pair_of(-step, -step), round2 = pair_of(kRound, kRound);
     uint32_t word = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float n = step > 0.f ? fminf(fmaxf(rintf((x[i] - low) / step), 0.f), 15.f) : 0.f;
-        word |= (uint32_t)n << (4 * i);
+    for (int i = 0; i < 4; ++i) {
+        const float2 x = kv4_pair<T>(raw[i]);
+        const unsigned long long d = add2(pair_of(x.x, x.y), low2), q = mul2(d, inv2);
+        const float2 f = halves(fma2(fma2(q, step2, d), inv2, q));
+        const float2 n = halves(add2(pair_of(fminf(f.x, 15.f), fminf(f.y, 15.f)), round2));
+        word += __float_as_uint(n.x) << (8 * i);
+        word += __float_as_uint(n.y) << (8 * i + 4);
     }
-    if (is_v) {                                     // from eight columns a thread to one column place a thread
-        uint32_t turned = 0;
-        const int first = lane & ~(L - 1), n = l & 7, half = l & 8;
+    constexpr uint32_t kBits = 0x4b400000u;         // of kRound: what each code has added
+    word -= kBits * 0x11111111u;
+    if (step > 0.f && !(step > 1e-37f)) {
+        word = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) turned |= (__shfl_sync(0xffffffffu, word, first + half + j) >> (4 * n) & 15u) << (4 * j);
-        word = turned;
+        for (int i = 0; i < 8; ++i) {
+            const float2 x = kv4_pair<T>(raw[i / 2]);
+            word |= (uint32_t)fminf(rintf(((i & 1 ? x.y : x.x) - lh.x) / step), 15.f) << (4 * i);
+        }
     }
-    if (!on) return;
-    unsigned char* blk = c.block(slot, head, D);
-    const int t = (int)(slot & 15);
-    if (!is_v) {
-        *reinterpret_cast<uint32_t*>(blk + (t * 4 + (l & 3)) * (D / 8) + 4 * (l >> 2)) = word;
-    } else {
-        const int n = l & 7;
-        *reinterpret_cast<uint32_t*>(blk + 8 * D + (t >> 3) * (4 * D) + ((n * 4 + ((t & 7) >> 1)) * 2 + (t & 1)) * (D / 16) + 4 * (l >> 3)) = word;
-    }
-    if (l % per == 0)
-        reinterpret_cast<uint32_t*>(blk + 16 * D)[((is_v ? c.groups : 0) + l / per) * 16 + t] = step_bits | kv4_bits<T>(low + bad) << 16;
+    if (p.is_v) word = nibbles_transposed(word, p.l);
+    if (!p.on) return;
+    unsigned char* blk = c.block(p.slot, p.head, D);
+    *p.word(blk) = word;
+    if ((p.l & (per - 1)) == 0) *p.pair(blk, c.groups) = step_bits | kv4_bits<T>(lh.x + bad) << 16;
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kKv4RowThreads) kv4_load_kernel(Kv4Cache c, Kv4Rows a) {
-    constexpr int L = D / 8;
+__global__ void __launch_bounds__(kKv4RowThreads) kv4_load_kernel(const __grid_constant__ Kv4Cache c, const __grid_constant__ Kv4Rows a) {
     pdl_wait();
     if (!(blockIdx.y ? a.v : a.k)) return;
-    const int row = (int)(blockIdx.x * (kKv4RowThreads / L) + threadIdx.x / L);
-    const int lane = threadIdx.x & 31, l = lane & (L - 1);
-    const bool is_v = blockIdx.y != 0;
-    const int token = row / c.n_k, head = row - token * c.n_k;
-    const int64_t at = row < a.rows ? a.slots[token] : -1;
-    const bool on = at >= 0 && at < c.slots;
-    const int slot = (int)at;
+    const Kv4Place<D> p(c, a);
     uint32_t word = 0, pair = 0;
-    if (on) {
-        const unsigned char* blk = c.block(slot, head, D);
-        const int t = (int)(slot & 15), n = l & 7;
-        word = *reinterpret_cast<const uint32_t*>(
-            !is_v ? blk + (t * 4 + (l & 3)) * (D / 8) + 4 * (l >> 2)
-                  : blk + 8 * D + (t >> 3) * (4 * D) + ((n * 4 + ((t & 7) >> 1)) * 2 + (t & 1)) * (D / 16) + 4 * (l >> 3));
-        pair = reinterpret_cast<const uint32_t*>(blk + 16 * D)[((is_v ? c.groups : 0) + l / (L / c.groups)) * 16 + t];
+    if (p.on) {
+        unsigned char* blk = c.block(p.slot, p.head, D);
+        word = *p.word(blk);
+        pair = *p.pair(blk, c.groups);
     }
-    if (is_v) {
-        uint32_t turned = 0;
-        const int first = lane & ~(L - 1), i = l & 7, half = l & 8;
-#pragma unroll
-        for (int n = 0; n < 8; ++n) turned |= (__shfl_sync(0xffffffffu, word, first + half + n) >> (4 * i) & 15u) << (4 * n);
-        word = turned;
-    }
-    if (row >= a.rows) return;
+    if (p.is_v) word = nibbles_transposed(word, p.l);
+    if (p.row >= a.rows) return;
     const float2 s = kv4_pair<T>(pair);
-    float x[8];
+    constexpr uint32_t kBits = 0x4b000000u;         // 2^23: a code in its lowest bits becomes a number without a conversion
+    const unsigned long long less = pair_of(-8388608.f, -8388608.f), step = pair_of(s.x, s.x), low = pair_of(s.y, s.y);
+    V8 x;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = fmaf((float)(word >> (4 * j) & 15u), s.x, s.y);
-    T* to = static_cast<T*>(is_v ? a.v : a.k) + token * (is_v ? a.ld_v : a.ld_k) + head * D + 8 * l;
-    Elem<T>::store8(to, x);
+    for (int i = 0; i < 4; ++i) {
+        const float n0 = __uint_as_float((word >> (8 * i) & 15u) | kBits), n1 = __uint_as_float((word >> (8 * i + 4) & 15u) | kBits);
+        x.p[i] = fma2(add2(pair_of(n0, n1), less), step, low);
+    }
+    store8v<T>(p.template columns<T>(a), x);
 }
 
 // ---- attention -----------------------------------------------------------------------------------------------
 // A block takes up to 8 NR row_groups rows (query tokens of a sequence times the query heads of one key head) and a span of the
-// sequence's cache.  Its producer warp brings stages of eight blocks of 16 tokens into a ring, one bulk copy a block (whatever
-// the page size); eight warps, in row groups that share the tokens of a stage, take a block of 16 tokens each:
+// sequence's cache.  Its eight warps are row groups of `parts` warps; warp i of each group takes every parts-th chunk of U blocks
+// of 16 tokens, so the warps of one number share a stream of chunks and the others do without them:
 //   scores  [16 tokens x 8 rows] = K (operand A, unpacked) Q^T,   out [D x 8 rows] += V^T (operand A, unpacked) P^T
 // with tokens and columns on the MMA's long side, so one sequence's few rows cost no more than 8 and an unpacked operand serves
-// NR MMAs.  The running maximum is a reference, moved only when a score passes it by 2^8, so that most blocks need a vote and no
-// shuffles.  Long caches are split over blocks, and kv4_join_kernel adds the parts up.
+// NR MMAs.  A stream has a ring of chunks, filled by its first warp with one bulk copy a block (whatever the page size).  The running
+// maximum is a reference, moved only when a score passes it by 2^8, so that most chunks need one vote and no shuffles.  Long
+// caches are split over blocks, and kv4_join_kernel adds the parts up.
 constexpr int kKv4Warps = 8;
-constexpr int kKv4Threads = (kKv4Warps + 1) * 32;
-constexpr int kKv4Stages = 4;
-constexpr int kKv4StageTokens = 8 * kKv4Block;
+constexpr int kKv4Threads = kKv4Warps * 32;
+constexpr int kKv4SpanBlocks = 16;                  // spans of a split are a multiple of so many blocks of 16 tokens
+constexpr int kKv4MaxSplits = 256;
 constexpr int kKv4MaxTree = 64;                     // query tokens under a tree mask
 
 struct Kv4Args {
     Kv4Cache c;
     int n_seq, n_rows, max_q, n_q, G, width, n_pages;
-    int row_groups, row_blocks, splits;
+    int row_groups, row_blocks, splits, slots;      // slots: chunks of a stream's ring
     float scale2;                                   // scale log2(e)
     long long ld_table, ld_q, ld_out;
     const void* q;
@@ -202,97 +267,37 @@ __device__ __forceinline__ uint32_t tile_transpose(uint32_t v) {
     return r;
 }
 
+constexpr float kKv4NoMax = -3e38f;                 // the reference before any score; finite, so that nothing is inf - inf
+
+// What a warp keeps of its 8 NR rows.  Accumulators of the MMA: columns 16 j + g and + 8 (times 16), rows 2c and 2c + 1 of a tile, with
+// g = lane / 4, c = lane % 4; everything a row has is kept for the pair of rows 2c, 2c + 1.
 template <typename T, int D, int NG, int NR>
-__global__ void __launch_bounds__(kKv4Threads, NR == 1 ? 2 : 1) kv4_attention_kernel(const Kv4Args a) {
-    constexpr int kBytes = kKv4Block * D + 128 * NG;          // of a block of 16 tokens
-    constexpr int kStage = 8 * kBytes;
-    constexpr int W = D / 32, J = D / 16;                     // words of a lane and token; tiles of 16 columns
+struct Kv4Rowset {
+    static constexpr int kBytes = kKv4Block * D + 128 * NG;  // of a block of 16 tokens
+    static constexpr int W = D / 32, J = D / 16;             // words of a lane and token; tiles of 16 columns
     // fp16 outputs: what the rounding of p step loses is made good at the middle of the codes, so that it weighs code - 7.5 and not
     // code (0.0005 -> 0.0003 of the output; bf16 outputs, rounded to 0.0017, do not show it)
-    constexpr bool kCentre = std::is_same_v<T, __half>;
-    static_assert(kKv4Warps * 8 * NR * D * 4 <= kKv4Stages * kStage, "the warps' outputs fit the ring");
-    extern __shared__ __align__(128) unsigned char kv4_smem[];
-    __shared__ __align__(8) uint64_t full[kKv4Stages], empty[kKv4Stages];
-    __shared__ uint32_t present[kKv4Stages];                  // which blocks of a stage there are
-    __shared__ float2 s_ml[kKv4Warps][8 * NR];
-    __shared__ volatile int abort_flag;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < kKv4Stages; ++i) {
-            mbar_init(smem_u32(&full[i]), 1);
-            mbar_init(smem_u32(&empty[i]), kKv4Warps);
-        }
-        abort_flag = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    }
-    __syncthreads();
-    pdl_wait();
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.st->status = 0;      // a wait would have to fail millions of polls before this
+    static constexpr bool kCentre = std::is_same_v<T, __half>;
+    using Pair = unsigned long long;
 
-    unsigned unit = blockIdx.x;
-    const int split = unit % a.splits;
-    unit /= a.splits;
-    const int row_block = unit % a.row_blocks;
-    unit /= a.row_blocks;
-    const int head = unit % a.c.n_k, seq = unit / a.c.n_k;
-    int q0, n;
-    kv4_rows_of(a, seq, &q0, &n);
-    const int rows = min(n, a.max_q) * a.G, row0 = row_block * 8 * NR * a.row_groups;
-    if (row0 >= rows) return;
-    const long long most = (long long)a.width * a.c.page;
-    const int len = (int)max(0LL, min((long long)a.lens[seq], most));
-    const int all = (len + kKv4StageTokens - 1) / kKv4StageTokens, per = (all + a.splits - 1) / a.splits;
-    const int from = min(split * per, all), to = min(from + per, all);
+    float acc[NR][J][4];
+    float m[NR][2];
+    Pair l[NR], corr[NR][NG], lost[NR][NG];
+    float limit;                                             // steps up to here fit the scale of p step, 2^(127 - f_exp)
+    int f_exp;
+    // operand B of the scores, sums of the scaled queries (times 2^-24), and what makes a raw score one in powers of two
+    uint4 qf[NR][W];
+    Pair low[NR][NG], back[NR];
+    int node[NR][2];                                         // query token of a row, past all of them for rows that do not exist
 
-    const int parts = kKv4Warps / a.row_groups;               // warps that share a row group's tokens
-    const int group = warp / parts, mine = warp - group * parts;
-    float acc[NR][J][4] = {};
-    float m[NR][2], l[NR][2] = {}, corr[NR][NG][2] = {}, lost[NR][NG][2] = {};
-    uint32_t limit = 0, f_exp = 127;                          // steps up to `limit` (bits) fit the scale of p step, 2^(127 - f_exp)
+    static __device__ __forceinline__ Pair both(float v) { return pair_of(v, v); }
 
-    if (warp == kKv4Warps) {
-        const int32_t* table = a.table + seq * a.ld_table;
-        const int subs = a.c.page / kKv4Block;
-        // page of the block of 16 tokens that this lane copies of stage i, -1: none
-        auto page_of = [&](int i) {
-            const int sub = i * 8 + lane;
-            return lane < 8 && i < to && sub * kKv4Block < len ? __ldg(table + sub / subs) : -1;
-        };
-        int next = page_of(from), stage = 0;
-        uint32_t phase = 0;
-        for (int i = from; i < to; ++i) {
-            const int page = next;
-            next = page_of(i + 1);
-            const bool there = page >= 0 && page < a.n_pages;
-            const uint32_t which = __ballot_sync(0xffffffffu, there);
-            mbar_wait(smem_u32(&empty[stage]), phase ^ 1u, &abort_flag, a.st);
-            const uint32_t bar = smem_u32(&full[stage]);
-            if (lane == 0) {
-                present[stage] = which;
-                mbar_expect_tx(bar, __popc(which) * kBytes);
-            }
-            __syncwarp();
-            if (there) {
-                const int sub = i * 8 + lane;
-                const unsigned char* src = a.c.base + (((long long)page * a.c.n_k + head) * subs + sub % subs) * kBytes;
-                bulk_g2s(smem_u32(kv4_smem + stage * kStage + lane * kBytes), src, kBytes, bar);
-            }
-            if (++stage == kKv4Stages) { stage = 0; phase ^= 1u; }
-        }
-        // nothing is left on its way when the ring is used again or the block ends, an expired wait elsewhere included
-        for (int i = max(from, to - kKv4Stages); i < to; ++i)
-            mbar_wait(smem_u32(&full[(i - from) % kKv4Stages]), (uint32_t)((i - from) / kKv4Stages) & 1u, &abort_flag, a.st);
-    } else {
-        const int g = lane >> 2, c = lane & 3;
-        // Operand B of the scores: this lane's rows g (one a tile), columns 32 w + 8 c ..., brought into fp16's range by a power of two.
-        uint4 qf[NR][W];
-        float lows[NR][NG][2];                                // sums of the scaled queries of rows 2c, 2c + 1, times 2^-24
-        float back1[NR][2], back2[NR][2];                     // what turns a raw score of these rows into one in powers of two
-        int node[NR][2];
+    // Rows row0 ... of the sequence whose first query row is q0; columns 32 w + 8 c ... of row g are this lane's part of operand B.
+    __device__ __forceinline__ void begin(const Kv4Args& a, int q0, int head, int row0, int rows) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            const int row = row0 + (group * NR + r) * 8 + g;
+            const int row = row0 + r * 8 + g;
             float f[W][8] = {};
             if (row < rows) {
                 const int tok = row / a.G;
@@ -307,8 +312,9 @@ __global__ void __launch_bounds__(kKv4Threads, NR == 1 ? 2 : 1) kv4_attention_ke
                 for (int i = 0; i < 8; ++i) big = max(big, __float_as_uint(f[w][i]) & 0x7fffffffu);
             big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
             big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
-            const int e = q4_exponent(big);
+            const int e = q4_exponent(big);                  // the power of two that brings the row into fp16's range
             const Q4Power up(e), down(24 - e);
+            const float undo = a.scale2 * down.a * down.b;
             float sum[NG] = {};
 #pragma unroll
             for (int w = 0; w < W; ++w) {
@@ -324,251 +330,379 @@ __global__ void __launch_bounds__(kKv4Threads, NR == 1 ? 2 : 1) kv4_attention_ke
                 sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
                 sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
                 sum[i] *= 0x1p-24f;
+                low[r][i] = pair_of(__shfl_sync(0xffffffffu, sum[i], 8 * c), __shfl_sync(0xffffffffu, sum[i], 8 * c + 4));
+                corr[r][i] = lost[r][i] = 0;
             }
+            back[r] = pair_of(__shfl_sync(0xffffffffu, undo, 8 * c), __shfl_sync(0xffffffffu, undo, 8 * c + 4));
+            l[r] = 0;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                const int of = (2 * c + s) * 4;
+                const int at = row0 + r * 8 + 2 * c + s;
+                node[r][s] = at < rows ? at / a.G : 0x7fffffff;
+                m[r][s] = kKv4NoMax;
+            }
 #pragma unroll
-                for (int i = 0; i < NG; ++i) lows[r][i][s] = __shfl_sync(0xffffffffu, sum[i], of);
-                back1[r][s] = __shfl_sync(0xffffffffu, down.a, of);
-                back2[r][s] = __shfl_sync(0xffffffffu, down.b, of) * a.scale2;
-                node[r][s] = (row0 + (group * NR + r) * 8 + 2 * c + s) / a.G;
-                m[r][s] = kNegInf;
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) acc[r][j][x] = 0.f;
+        }
+        limit = 0.f;
+        f_exp = 127;
+    }
+
+    // Raw scores of a block's tokens g and g + 8: s[row tile][token].
+    __device__ __forceinline__ void scores(const unsigned char* blk, Pair (&s)[NR][2]) const {
+        const int lane = threadIdx.x & 31;
+        const uint32_t* pk = reinterpret_cast<const uint32_t*>(blk + 16 * D) + (lane >> 2);
+        uint32_t kw[2][W];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const unsigned char* p = blk + h * 4 * D + lane * (D / 8);
+            if constexpr (D == 128) *reinterpret_cast<uint4*>(kw[h]) = *reinterpret_cast<const uint4*>(p);
+            else *reinterpret_cast<uint2*>(kw[h]) = *reinterpret_cast<const uint2*>(p);
+        }
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            float d[NR][2][4] = {};                           // two chains of MMAs
+#pragma unroll
+            for (int w = i * W / NG; w < (i + 1) * W / NG; ++w) {
+                uint32_t u[4], v[4];
+                q4_spread(kw[0][w], u);
+                q4_spread(kw[1][w], v);
+                const uint32_t a0[4] = {u[0], v[0], u[1], v[1]}, a1[4] = {u[2], v[2], u[3], v[3]};
+#pragma unroll
+                for (int r = 0; r < NR; ++r) {
+                    q4_mma(d[r][0], a0, qf[r][w].x, qf[r][w].y);
+                    q4_mma(d[r][W / NG > 1 ? 1 : 0], a1, qf[r][w].z, qf[r][w].w);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float2 p = kv4_pair<T>(pk[i * 16 + 8 * h]);
+#pragma unroll
+                for (int r = 0; r < NR; ++r) {
+                    Pair x = pair_of(d[r][0][2 * h], d[r][0][2 * h + 1]);
+                    if (W / NG > 1) x = add2(x, pair_of(d[r][1][2 * h], d[r][1][2 * h + 1]));
+                    const Pair y = i == 0 ? mul2(both(p.y), low[r][i]) : fma2(both(p.y), low[r][i], s[r][h]);
+                    s[r][h] = fma2(both(p.x), x, y);
+                }
             }
         }
+    }
 
-        // Sixteen tokens from `token` on, at `blk`.  CUT: not every row sees all of them.
-        auto work = [&](const unsigned char* blk, int token, auto cut) {
-            constexpr bool CUT = decltype(cut)::value;
-            float s[NR][4];
-            const uint32_t* pk = reinterpret_cast<const uint32_t*>(blk + 16 * D) + g;
-            {
-                uint32_t kw[2][W];
+    // The maximum's reference and the scale of p step follow what these scores (where seen, x > -inf) and steps ask for.
+    template <int U>
+    __device__ __forceinline__ void move(const Pair (&s)[U][NR][2], Pair (&x)[U][NR][2], float step) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const unsigned char* p = blk + h * 4 * D + lane * (D / 8);
-                    if constexpr (D == 128) *reinterpret_cast<uint4*>(kw[h]) = *reinterpret_cast<const uint4*>(p);
-                    else *reinterpret_cast<uint2*>(kw[h]) = *reinterpret_cast<const uint2*>(p);
-                }
+        for (int r = 0; r < NR; ++r) {
+            float f[2];
 #pragma unroll
-                for (int i = 0; i < NG; ++i) {
-                    float d[NR][4] = {};
+            for (int e = 0; e < 2; ++e) {
+                float t = m[r][e];
 #pragma unroll
-                    for (int w = i * W / NG; w < (i + 1) * W / NG; ++w) {
-                        uint32_t u[4], v[4];
-                        q4_spread(kw[0][w], u);
-                        q4_spread(kw[1][w], v);
-                        const uint32_t a0[4] = {u[0], v[0], u[1], v[1]}, a1[4] = {u[2], v[2], u[3], v[3]};
-#pragma unroll
-                        for (int r = 0; r < NR; ++r) {
-                            q4_mma(d[r], a0, qf[r][w].x, qf[r][w].y);
-                            q4_mma(d[r], a1, qf[r][w].z, qf[r][w].w);
-                        }
-                    }
-                    const float2 p0 = kv4_pair<T>(pk[i * 16]), p1 = kv4_pair<T>(pk[i * 16 + 8]);
-#pragma unroll
-                    for (int r = 0; r < NR; ++r)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float2 p = e < 2 ? p0 : p1;
-                            const float x = fmaf(p.x, d[r][e], p.y * lows[r][i][e & 1]);
-                            s[r][e] = i == 0 ? x : s[r][e] + x;
-                        }
-                }
-            }
-            uint32_t seen = ~0u;                              // bit 4 r + e
-            bool above = false;
-#pragma unroll
-            for (int r = 0; r < NR; ++r)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[r][e] = s[r][e] * back1[r][e & 1] * back2[r][e & 1];
-                    if constexpr (CUT) {
-                        const int t = token + g + (e < 2 ? 0 : 8), at = t - (len - n), row = node[r][e & 1];
-                        bool see = t < len && (row0 + (group * NR + r) * 8 + 2 * c + (e & 1)) < rows;
-                        if (see && at >= 0) see = a.tree ? at < kKv4MaxTree && __ldg(a.tree + q0 + row) >> at & 1ull : at <= row;
-                        if (!see) {
-                            seen &= ~(1u << (4 * r + e));
-                            s[r][e] = kNegInf;
-                        }
-                    }
-                    above |= s[r][e] > m[r][e & 1] + 8.f;
-                }
-            if (__any_sync(0xffffffffu, above)) {
-#pragma unroll
-                for (int r = 0; r < NR; ++r)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        float t = fmaxf(m[r][h], fmaxf(s[r][h], s[r][2 + h]));
-#pragma unroll
-                        for (int o = 4; o < 32; o <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
-                        const float f = m[r][h] == t ? 1.f : exp2_fast(m[r][h] - t);
-                        m[r][h] = t;
-                        l[r][h] *= f;
-#pragma unroll
-                        for (int i = 0; i < NG; ++i) {
-                            corr[r][i][h] *= f;
-                            if constexpr (kCentre) lost[r][i][h] *= f;
-                        }
-#pragma unroll
-                        for (int j = 0; j < J; ++j) {
-                            acc[r][j][h] *= f;
-                            acc[r][j][2 + h] *= f;
-                        }
+                        const float2 now = halves(x[u][r][h]), raw = halves(mul2(s[u][r][h], back[r]));
+                        if ((e ? now.y : now.x) > kNegInf) t = fmaxf(t, e ? raw.y : raw.x);
                     }
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+                f[e] = m[r][e] == t ? 1.f : exp2_fast(m[r][e] - t);
+                m[r][e] = t;
             }
+            const Pair f2 = pair_of(f[0], f[1]);
+            l[r] = mul2(l[r], f2);
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                corr[r][i] = mul2(corr[r][i], f2);
+                if constexpr (kCentre) lost[r][i] = mul2(lost[r][i], f2);
+            }
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[r][j][k] *= f[k & 1];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float2 old = halves(x[u][r][h]), now = halves(fma2(s[u][r][h], back[r], pair_of(-m[r][0], -m[r][1])));
+                    x[u][r][h] = pair_of(old.x == kNegInf ? kNegInf : now.x, old.y == kNegInf ? kNegInf : now.y);
+                }
+        }
+        const float top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(step)));
+        if (top > limit) {
+            // 2^(127 - f_exp) brings the largest step so far to at most 2^6, and p is at most 2^8: fp16 holds their product
+            const int e = max(1, min((int)(__float_as_uint(top) >> 23), 253));
+            const Q4Power f(f_exp - e);
+            f_exp = e;
+            limit = e + 6 < 254 ? __uint_as_float((uint32_t)(e + 6) << 23) : 3.4e38f;
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[r][j][k] = f(acc[r][j][k]);
+                if constexpr (kCentre)
+#pragma unroll
+                    for (int i = 0; i < NG; ++i) lost[r][i] = mul2(mul2(lost[r][i], both(f.a)), both(f.b));
+            }
+        }
+    }
+
+    // U blocks of 16 tokens from `token` on, side by side at blk.  CUT: not every row sees all of them (past: tokens that all rows see, len:
+    // tokens of the sequence, there: which of the U blocks there are).
+    template <int U, bool CUT>
+    __device__ __forceinline__ void work(const Kv4Args& a, const unsigned char* blk, int token, int q0, int past, int len, uint32_t there) {
+        const int lane = threadIdx.x & 31, g = lane >> 2;
+        Pair s[U][NR][2], x[U][NR][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u) scores(blk + u * kBytes, s[u]);
+        float above = kNegInf, step = 0.f;
+        uint32_t vp[U][NG][2], seen = ~0u;                    // bit ((u NR + r) 2 + h) 2 + e
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t* pv = reinterpret_cast<const uint32_t*>(blk + u * kBytes + 16 * D) + NG * 16 + g;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int t = token + 16 * u + 8 * h + g;
+                const bool real = !CUT || (t < len && (there >> u & 1u));
+#pragma unroll
+                for (int i = 0; i < NG; ++i) {
+                    vp[u][i][h] = pv[i * 16 + 8 * h];
+                    if (real) step = fmaxf(step, kv4_pair<T>(vp[u][i][h]).x);      // (a NaN is passed over)
+                }
+#pragma unroll
+                for (int r = 0; r < NR; ++r) {
+                    x[u][r][h] = fma2(s[u][r][h], back[r], pair_of(-m[r][0], -m[r][1]));
+                    float2 v = halves(x[u][r][h]);
+                    if constexpr (CUT) {
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int at = t - past, row = node[r][e];
+                            bool see = real && row != 0x7fffffff;
+                            if (see && at >= 0) see = a.tree ? at < kKv4MaxTree && __ldg(a.tree + q0 + row) >> at & 1ull : at <= row;
+                            if (!see) {
+                                seen &= ~(1u << (((u * NR + r) * 2 + h) * 2 + e));
+                                (e ? v.y : v.x) = kNegInf;
+                            }
+                        }
+                        x[u][r][h] = pair_of(v.x, v.y);
+                    }
+                    above = fmaxf(above, fmaxf(v.x, v.y));
+                }
+            }
+        }
+        if (__any_sync(0xffffffffu, above > 8.f || step > limit)) move<U>(s, x, step);
+        const float f = __uint_as_float((uint32_t)(254 - f_exp) << 23);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            uint32_t b[NR][NG][2];
+            Pair p[NR][2];
 #pragma unroll
             for (int r = 0; r < NR; ++r)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[r][e] = exp2_fast(s[r][e] - (m[r][e & 1] == kNegInf ? 0.f : m[r][e & 1]));
-                    l[r][e & 1] += s[r][e];
+                for (int h = 0; h < 2; ++h) {
+                    const float2 v = halves(x[u][r][h]);
+                    p[r][h] = pair_of(exp2_fast(v.x), exp2_fast(v.y));
+                    l[r] = add2(l[r], p[r][h]);
                 }
-            // The scale of p step: 2^(127 - f_exp) brings the largest step so far to at most 2^6, and p is at most 2^8.
-            uint32_t vp[NG][2], top = 0;
 #pragma unroll
             for (int i = 0; i < NG; ++i)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    vp[i][h] = pk[(NG + i) * 16 + 8 * h];
-                    const uint32_t b = __float_as_uint(kv4_pair<T>(vp[i][h]).x);
-                    if ((!CUT || token + g + 8 * h < len) && b < 0x7f800000u) top = max(top, b);
-                }
-            top = __reduce_max_sync(0xffffffffu, top);
-            if (top > limit) {
-                const uint32_t e = max(1u, min(top >> 23, 253u));
-                const Q4Power f((int)f_exp - (int)e);
-                f_exp = e;
-                limit = e + 6 < 254 ? (e + 6) << 23 : 0x7f7fffffu;
+                    const float2 pr = kv4_pair<T>(vp[u][i][h]);
+                    const Pair by = both(pr.x * f), lowest = both(pr.y);
 #pragma unroll
-                for (int r = 0; r < NR; ++r)
-#pragma unroll
-                    for (int j = 0; j < J; ++j)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) acc[r][j][x] = f(acc[r][j][x]);
-                if constexpr (kCentre) {
-#pragma unroll
-                    for (int r = 0; r < NR; ++r)
-#pragma unroll
-                        for (int i = 0; i < NG; ++i)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) lost[r][i][h] = f(lost[r][i][h]);
-                }
-            }
-            const float f = __uint_as_float((254u - f_exp) << 23);
-            uint32_t b0[NR][NG], b1[NR][NG];
-#pragma unroll
-            for (int i = 0; i < NG; ++i) {
-                const float2 p0 = kv4_pair<T>(vp[i][0]), p1 = kv4_pair<T>(vp[i][1]);
-#pragma unroll
-                for (int r = 0; r < NR; ++r) {
-                    float x[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 p = e < 2 ? p0 : p1;
-                        x[e] = s[r][e] * (p.x * f);
-                        float y = s[r][e] * p.y;
-                        if (CUT && !(seen >> (4 * r + e) & 1u)) x[e] = y = 0.f;      // a step or lowest value that is not finite
-                        corr[r][i][e & 1] += y;
+                    for (int r = 0; r < NR; ++r) {
+                        float2 w;
+                        if constexpr (CUT) {                  // a step or lowest value that is not finite has no part in what is not seen
+                            const uint32_t on = seen >> (((u * NR + r) * 2 + h) * 2);
+                            const float2 q = halves(mul2(p[r][h], by)), y = halves(mul2(p[r][h], lowest));
+                            w = make_float2(on & 1u ? q.x : 0.f, on & 2u ? q.y : 0.f);
+                            corr[r][i] = add2(corr[r][i], pair_of(on & 1u ? y.x : 0.f, on & 2u ? y.y : 0.f));
+                        } else {
+                            w = halves(mul2(p[r][h], by));
+                            corr[r][i] = fma2(p[r][h], lowest, corr[r][i]);
+                        }
+                        const uint32_t two = half_pair(w.x, w.y);
+                        if constexpr (kCentre) {
+                            const float2 kept = kv4_pair<__half>(two);
+                            lost[r][i] = add2(lost[r][i], pair_of(w.x - kept.x, w.y - kept.y));
+                        }
+                        b[r][i][h] = tile_transpose(two);
                     }
-                    const uint32_t h0 = half_pair(x[0], x[1]), h1 = half_pair(x[2], x[3]);
-                    if constexpr (kCentre) {
-                        const float2 f0 = kv4_pair<__half>(h0), f1 = kv4_pair<__half>(h1);
-                        lost[r][i][0] += (x[0] - f0.x) + (x[2] - f1.x);
-                        lost[r][i][1] += (x[1] - f0.y) + (x[3] - f1.y);
-                    }
-                    b0[r][i] = tile_transpose(h0);
-                    b1[r][i] = tile_transpose(h1);
                 }
-            }
             uint32_t vw[2][2][W / 2];                         // [eight tokens][token of the pair][word]
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const unsigned char* p = blk + 8 * D + h * 4 * D + lane * (D / 8);
-                if constexpr (D == 128) *reinterpret_cast<uint4*>(vw[h]) = *reinterpret_cast<const uint4*>(p);
-                else *reinterpret_cast<uint2*>(vw[h]) = *reinterpret_cast<const uint2*>(p);
+                const unsigned char* at = blk + u * kBytes + 8 * D + h * 4 * D + lane * (D / 8);
+                if constexpr (D == 128) *reinterpret_cast<uint4*>(vw[h]) = *reinterpret_cast<const uint4*>(at);
+                else *reinterpret_cast<uint2*>(vw[h]) = *reinterpret_cast<const uint2*>(at);
             }
 #pragma unroll
             for (int w = 0; w < W / 2; ++w)
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    uint32_t u[4], v[4];
-                    q4_spread(__byte_perm(vw[0][0][w], vw[0][1][w], half ? 0x7632 : 0x5410), u);
-                    q4_spread(__byte_perm(vw[1][0][w], vw[1][1][w], half ? 0x7632 : 0x5410), v);
-                    const uint32_t a0[4] = {u[0], u[1], v[0], v[1]}, a1[4] = {u[2], u[3], v[2], v[3]};
+                    uint32_t c[4], d[4];
+                    q4_spread(__byte_perm(vw[0][0][w], vw[0][1][w], half ? 0x7632 : 0x5410), c);
+                    q4_spread(__byte_perm(vw[1][0][w], vw[1][1][w], half ? 0x7632 : 0x5410), d);
+                    const uint32_t a0[4] = {c[0], c[1], d[0], d[1]}, a1[4] = {c[2], c[3], d[2], d[3]};
                     const int j = 4 * w + 2 * half;
 #pragma unroll
                     for (int r = 0; r < NR; ++r) {
-                        q4_mma(acc[r][j], a0, b0[r][j * NG / J], b1[r][j * NG / J]);
-                        q4_mma(acc[r][j + 1], a1, b0[r][(j + 1) * NG / J], b1[r][(j + 1) * NG / J]);
+                        q4_mma(acc[r][j], a0, b[r][j * NG / J][0], b[r][j * NG / J][1]);
+                        q4_mma(acc[r][j + 1], a1, b[r][(j + 1) * NG / J][0], b[r][(j + 1) * NG / J][1]);
                     }
                 }
-        };
-
-        const bool live = row0 + group * NR * 8 < rows;
-        const int open = len - n + (a.tree ? 0 : 1);          // every row sees the tokens before this one
-        int stage = 0;
-        uint32_t phase = 0;
-        for (int i = from; i < to; ++i) {
-            mbar_wait(smem_u32(&full[stage]), phase, &abort_flag, a.st);
-            const uint32_t which = abort_flag ? 0u : present[stage];
-            if (live)
-                for (int b = mine; b < 8; b += parts)
-                    if (which >> b & 1u) {
-                        const int token = (i * 8 + b) * kKv4Block;
-                        const unsigned char* blk = kv4_smem + stage * kStage + b * kBytes;
-                        if (token + kKv4Block <= open) work(blk, token, std::false_type{});
-                        else work(blk, token, std::true_type{});
-                    }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // read here, refilled by a bulk copy
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
-            if (++stage == kKv4Stages) { stage = 0; phase ^= 1u; }
-        }
-#pragma unroll
-        for (int r = 0; r < NR; ++r)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int o = 4; o < 32; o <<= 1) {
-                    l[r][h] += __shfl_xor_sync(0xffffffffu, l[r][h], o);
-#pragma unroll
-                    for (int i = 0; i < NG; ++i) corr[r][i][h] += __shfl_xor_sync(0xffffffffu, corr[r][i][h], o);
-                }
-        if constexpr (kCentre) {
-            const Q4Power undo((int)f_exp - 127);
-#pragma unroll
-            for (int r = 0; r < NR; ++r)
-#pragma unroll
-                for (int i = 0; i < NG; ++i)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float x = undo(lost[r][i][h]) * 7.5f;
-#pragma unroll
-                        for (int o = 4; o < 32; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-                        corr[r][i][h] += x;
-                    }
         }
     }
-    __syncthreads();                                          // every warp is done with the ring
-    float* s_out = reinterpret_cast<float*>(kv4_smem);        // [warp][row of its group][D]
-    if (warp < kKv4Warps) {
-        const int g = lane >> 2, c = lane & 3;
-        const Q4Power undo((int)f_exp - 127 + 24);
+
+    // Sums over the lanes of a row; out [row of the set][D] unnormalised and ml [row] (reference, sum).
+    __device__ __forceinline__ void end(float* out, float2* ml) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+        auto over_lanes = [](Pair v) {
+            float2 f = halves(v);
 #pragma unroll
-        for (int r = 0; r < NR; ++r)
+            for (int o = 4; o < 32; o <<= 1) {
+                f.x += __shfl_xor_sync(0xffffffffu, f.x, o);
+                f.y += __shfl_xor_sync(0xffffffffu, f.y, o);
+            }
+            return f;
+        };
+        const Q4Power undo(f_exp - 127 + 24), scale(f_exp - 127);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            float fix[NG][2];
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                const float2 v = over_lanes(corr[r][i]);
+                fix[i][0] = v.x;
+                fix[i][1] = v.y;
+                if constexpr (kCentre) {
+                    const float2 w = over_lanes(lost[r][i]);
+                    fix[i][0] += scale(w.x) * 7.5f;
+                    fix[i][1] += scale(w.y) * 7.5f;
+                }
+            }
+            const float2 sum = over_lanes(l[r]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int row = r * 8 + 2 * c + h;
-                float* o = s_out + (warp * 8 * NR + row) * D;
-                if (g == 0) s_ml[warp][row] = make_float2(m[r][h], l[r][h]);
+                if (g == 0) ml[row] = make_float2(m[r][h], h ? sum.y : sum.x);
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
-                    o[16 * j + g] = undo(acc[r][j][h]) + corr[r][j * NG / J][h];
-                    o[16 * j + 8 + g] = undo(acc[r][j][2 + h]) * 0.0625f + corr[r][j * NG / J][h];
+                    out[row * D + 16 * j + g] = undo(acc[r][j][h]) + fix[j * NG / J][h];
+                    out[row * D + 16 * j + 8 + g] = undo(acc[r][j][2 + h]) * 0.0625f + fix[j * NG / J][h];
                 }
             }
+        }
     }
+};
+
+// Blocks of 16 tokens a chunk, ring of a block in bytes: two blocks a SM where a warp has eight rows.
+template <int NG, int NR> constexpr int kKv4Chunk = NR == 1 && NG < 4 ? 2 : 1;
+template <int NR> constexpr int kKv4Ring = NR == 1 ? 108 * 1024 : 192 * 1024;
+constexpr int kKv4MaxSlots = 12;
+
+template <typename T, int D, int NG, int NR>
+__global__ void __launch_bounds__(kKv4Threads, NR == 1 ? 2 : 1) kv4_attention_kernel(const __grid_constant__ Kv4Args a) {
+    using Rowset = Kv4Rowset<T, D, NG, NR>;
+    constexpr int kBytes = Rowset::kBytes, U = kKv4Chunk<NG, NR>;
+    extern __shared__ __align__(128) unsigned char kv4_smem[];
+    __shared__ __align__(8) uint64_t full[kKv4Warps * kKv4MaxSlots], empty[kKv4Warps * kKv4MaxSlots];
+    __shared__ uint32_t present[kKv4Warps * kKv4MaxSlots];    // which blocks of a chunk there are
+    __shared__ float2 s_ml[kKv4Warps][8 * NR];
+    __shared__ volatile int abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int parts = kKv4Warps / a.row_groups, group = warp / parts, mine = warp - group * parts;
+    if (threadIdx.x == 0) abort_flag = 0;
+    for (int i = threadIdx.x; i < parts * a.slots; i += kKv4Threads) {
+        mbar_init(smem_u32(&full[i]), 1);
+        mbar_init(smem_u32(&empty[i]), a.row_groups);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    pdl_wait();
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.st->status = 0;      // a wait would have to fail millions of polls before this
+
+    unsigned unit = blockIdx.x;
+    const int split = unit % a.splits;
+    unit /= a.splits;
+    const int row_block = unit % a.row_blocks;
+    unit /= a.row_blocks;
+    const int head = unit % a.c.n_k, seq = unit / a.c.n_k;
+    int q0, n;
+    kv4_rows_of(a, seq, &q0, &n);
+    const int rows = min(n, a.max_q) * a.G, row0 = row_block * 8 * NR * a.row_groups;
+    if (row0 >= rows) return;
+    const int len = (int)max(0LL, min((long long)a.lens[seq], min((long long)a.width * a.c.page, 0x7fff0000LL)));
+    const int spans = (len + kKv4SpanBlocks * kKv4Block - 1) / (kKv4SpanBlocks * kKv4Block), per = (spans + a.splits - 1) / a.splits;
+    // chunks of this block, and those of this warp's stream: from + mine, from + mine + parts, ...
+    const int from = min(split * per, spans) * (kKv4SpanBlocks / U), to = min(min(split * per, spans) + per, spans) * (kKv4SpanBlocks / U);
+    const int chunks = (to - from - mine + parts - 1) / parts;
+
+    unsigned char* ring = kv4_smem + mine * a.slots * (U * kBytes);
+    const int bar0 = mine * a.slots;
+    const int32_t* table = a.table + seq * a.ld_table;
+    // page of the block that this lane copies of the stream's chunk i, -1: none
+    auto page_of = [&](int i) {
+        const int sub = (from + mine + i * parts) * U + lane;
+        return lane < U && i < chunks && sub * kKv4Block < len ? __ldg(table + a.c.subs(sub)) : -1;
+    };
+    int next = -1;                                            // of the chunk to be copied next
+    auto copy = [&](int i, int slot) {
+        const int page = next;
+        next = page_of(i + 1);
+        const bool there = page >= 0 && page < a.n_pages;
+        const uint32_t which = __ballot_sync(0xffffffffu, there), bar = smem_u32(&full[bar0 + slot]);
+        if (lane == 0) {
+            present[bar0 + slot] = which;
+            mbar_expect_tx(bar, __popc(which) * kBytes);
+        }
+        __syncwarp();
+        if (there) {
+            const int sub = (from + mine + i * parts) * U + lane, subs = (int)a.c.subs.d;
+            bulk_g2s(smem_u32(ring + (slot * U + lane) * kBytes), a.c.base + (((long long)page * a.c.n_k + head) * subs + sub - a.c.subs(sub) * subs) * kBytes, kBytes, bar);
+        }
+    };
+    if (group == 0) {
+        next = page_of(0);
+        for (int i = 0; i < min(a.slots, chunks); ++i) copy(i, i);
+    }
+    Rowset set;
+    set.begin(a, q0, head, row0 + group * 8 * NR, rows);
+    const bool live = row0 + group * NR * 8 < rows;
+    const int past = len - n, open = past + (a.tree ? 0 : 1);          // every row sees the tokens before `open`
+    int slot = 0;
+    uint32_t phase = 0;
+#pragma unroll 1
+    for (int i = 0; i < chunks; ++i) {
+        mbar_wait(smem_u32(&full[bar0 + slot]), phase, &abort_flag, a.st);
+        const uint32_t there = abort_flag || !live ? 0u : present[bar0 + slot];
+        const int token = (from + mine + i * parts) * U * kKv4Block;
+        const unsigned char* blk = ring + slot * (U * kBytes);
+        if (there == (1u << U) - 1 && token + U * kKv4Block <= open) set.template work<U, false>(a, blk, token, q0, past, len, there);
+        else if (there) set.template work<U, true>(a, blk, token, q0, past, len, there);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // read here, refilled by a bulk copy
+        __syncwarp();
+        if (a.row_groups == 1) {
+            if (i + a.slots < chunks) copy(i + a.slots, slot);
+        } else {
+            if (lane == 0) mbar_arrive(smem_u32(&empty[bar0 + slot]));
+            // the chunk before this one, which the stream's other warps have left by now, as a rule
+            const int last = slot ? slot - 1 : a.slots - 1;
+            if (group == 0 && i > 0 && i - 1 + a.slots < chunks) {
+                mbar_wait(smem_u32(&empty[bar0 + last]), slot ? phase : phase ^ 1u, &abort_flag, a.st);
+                copy(i - 1 + a.slots, last);
+            }
+        }
+        if (++slot == a.slots) { slot = 0; phase ^= 1u; }
+    }
+    __syncthreads();                                          // every warp is done with the ring
+    float* s_out = reinterpret_cast<float*>(kv4_smem);        // [warp][row of its group][D]
+    set.end(s_out + warp * 8 * NR * D, s_ml[warp]);
     __syncthreads();
     // the warps of a row group, four columns a thread
     for (int i = threadIdx.x; i < a.row_groups * 8 * NR * (D / 4); i += kKv4Threads) {
@@ -581,7 +715,7 @@ __global__ void __launch_bounds__(kKv4Threads, NR == 1 ? 2 : 1) kv4_attention_ke
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int w = 0; w < parts; ++w) {
             const float2 ml = s_ml[grp * parts + w][r];
-            if (ml.x == kNegInf && ml.y == 0.f) continue;
+            if (ml.y == 0.f) continue;                        // saw nothing
             const float f = ml.x == top ? 1.f : exp2_fast(ml.x - top);
             const float4 v = *reinterpret_cast<const float4*>(s_out + ((grp * parts + w) * 8 * NR + r) * D + col);
             sum += f * ml.y;
@@ -604,48 +738,62 @@ __global__ void __launch_bounds__(kKv4Threads, NR == 1 ? 2 : 1) kv4_attention_ke
     pdl_launch_dependents();
 }
 
-// Adds up the parts of split caches.  A warp a row and head, D / 32 columns a lane.
+// Adds up the parts of split caches, in a fixed order: a block a row and head, every fourth part a warp, D / 32 columns a lane.
+constexpr int kKv4JoinWarps = 4;
 template <typename T, int D>
-__global__ void __launch_bounds__(256) kv4_join_kernel(const Kv4Args a) {
+__global__ void __launch_bounds__(kKv4JoinWarps * 32) kv4_join_kernel(const __grid_constant__ Kv4Args a) {
     constexpr int N = D / 32;
-    const long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
+    __shared__ float s_o[kKv4JoinWarps][D];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
-    const int head = (int)(i % a.n_q);
-    const long long node = i / a.n_q;
-    const long long seq = node / a.max_q;
-    if (seq >= a.n_seq) return;
+    const int node = blockIdx.x / a.n_q, head = blockIdx.x - node * a.n_q, seq = node / a.max_q, tok = node - seq * a.max_q;
     int q0, n;
-    kv4_rows_of(a, (int)seq, &q0, &n);
-    const int tok = (int)(node - seq * a.max_q);
+    kv4_rows_of(a, seq, &q0, &n);
     if (tok >= min(n, a.max_q)) return;
     const long long at = (long long)(q0 + tok) * a.n_q + head, step = (long long)a.n_rows * a.n_q;
+    constexpr int kMost = kKv4MaxSplits / 32;
+    float2 ml[kMost];                                         // part 32 i + lane
     float top = kNegInf;
-    for (int s = lane; s < a.splits; s += 32) top = fmaxf(top, __ldcg(&a.part_ml[s * step + at]).x);
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        const int s = i * 32 + lane;
+        ml[i] = s < a.splits ? __ldcg(&a.part_ml[s * step + at]) : make_float2(kNegInf, 0.f);
+        if (ml[i].y != 0.f) top = fmaxf(top, ml[i].x);        // parts that saw nothing have a sum of 0
+    }
     top = warp_max(top);
     float sum = 0.f, o[N] = {};
-    for (int s = 0; s < a.splits; ++s) {
-        const float2 ml = __ldcg(&a.part_ml[s * step + at]);
-        if (ml.x == kNegInf && ml.y == 0.f) continue;
-        const float f = ml.x == top ? 1.f : exp2_fast(ml.x - top);
-        sum += f * ml.y;
-        const float* p = a.part_o + (s * step + at) * D + lane * N;
-        if constexpr (N == 4) {
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
-            o[0] += f * v.x; o[1] += f * v.y; o[2] += f * v.z; o[3] += f * v.w;
-        } else {
-            const float2 v = __ldcg(reinterpret_cast<const float2*>(p));
-            o[0] += f * v.x; o[1] += f * v.y;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        const float f = ml[i].y == 0.f ? 0.f : ml[i].x == top ? 1.f : exp2_fast(ml[i].x - top);
+        sum += f * ml[i].y;
+        if (i * 32 >= a.splits) break;
+#pragma unroll
+        for (int j = 0; j < 32 / kKv4JoinWarps; ++j) {
+            const int s = i * 32 + j * kKv4JoinWarps + warp;
+            const float g = __shfl_sync(0xffffffffu, f, j * kKv4JoinWarps + warp);
+            if (s >= a.splits || g == 0.f) continue;
+            const float* p = a.part_o + (s * step + at) * D + lane * N;
+            if constexpr (N == 4) {
+                const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
+                o[0] += g * v.x; o[1] += g * v.y; o[2] += g * v.z; o[3] += g * v.w;
+            } else {
+                const float2 v = __ldcg(reinterpret_cast<const float2*>(p));
+                o[0] += g * v.x; o[1] += g * v.y;
+            }
         }
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    T v[N];
+    sum = warp_sum(sum);
 #pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = Elem<T>::down(o[j] * inv);
-    T* out = static_cast<T*>(a.out) + (long long)(q0 + tok) * a.ld_out + (long long)head * D + lane * N;
-    if constexpr (N == 4) *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(v);
-    else *reinterpret_cast<uint32_t*>(out) = *reinterpret_cast<const uint32_t*>(v);
-    if (a.lse && lane == 0) a.lse[at] = sum == 0.f ? kNegInf : (top + log2f(sum)) * 0.69314718055994531f;
+    for (int j = 0; j < N; ++j) s_o[warp][lane * N + j] = o[j];
+    __syncthreads();
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    for (int c = threadIdx.x; c < D; c += kKv4JoinWarps * 32) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kKv4JoinWarps; ++w) v += s_o[w][c];
+        static_cast<T*>(a.out)[(long long)(q0 + tok) * a.ld_out + head * D + c] = Elem<T>::down(v * inv);
+    }
+    if (a.lse && threadIdx.x == 0) a.lse[at] = sum == 0.f ? kNegInf : (top + log2f(sum)) * 0.69314718055994531f;
 }
 
 }  // namespace coral
