@@ -622,7 +622,7 @@ int coral_lmhead_prompt_attention(const coral_lmhead_prompt_args *args, void *wo
  *   low = min x,  step = round_to_type((max x - min x) / 15),  code = round((x - low) / step) in 0..15,  and stands for low + step code
  * (step 0: code 0).  A group that holds an infinity or a NaN, or whose max x - min x passes fp32's range, stands for NaN.  coral_lmhead_kv4_config: type CORAL_TYPE_BF16 or _F16 (of
  * tokens, steps, queries and outputs), n_pages pages of `page` tokens (a multiple of 16), n_heads key heads of D = 64 or 128 columns, group
- * 32, 64 or 128 columns and at most D; n_pages * page below 2^31.
+ * 32, 64 or 128 columns and at most D; n_pages * page, and n_pages * page / 16 * n_heads, below 2^31.
  * coral_lmhead_kv4_bytes: size of the cache: n_heads * (D + 8 D / group) bytes a token.  The buffer is the caller's, 256-byte aligned.
  * coral_lmhead_kv4_store: tokens k, v [T x n_heads x D] of `type`, ld_* apart, to slots [T] (page * tokens of a page + place in it);
  *   a slot outside the cache (-1) is passed over.  What two tokens of one call leave in one slot is unspecified.

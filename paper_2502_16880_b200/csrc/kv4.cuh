@@ -11,9 +11,9 @@
 //
 // Layout: tokens in blocks of 16, [page][head][block of 16]: keys, values, (step, low) pairs of keys [group][16], of values.
 //   keys:   [16][4 lanes] of D / 8 bytes: column c is nibble c % 8 of word c / 32 of lane (c / 8) % 4
-//   values: [2][8 columns][4 pairs of tokens][2] of D / 16 bytes: column c is nibble c / 8 of column place c % 8
-// so that a lane's MMA operands are one 16-byte (D = 64: 8-byte) shared-memory load each, without bank conflicts, and no two tokens
-// share a byte.
+//   values: [2][8 column places][4 pairs of tokens][D / 32][2 tokens] 16-bit pieces: column c is nibble (c / 8) % 4 of piece c / 32 of place c % 8
+// so that a lane's MMA operands are one 16-byte (D = 64: 8-byte) shared-memory load each, without bank conflicts, the two tokens of
+// an operand's pair lie in the halves of a word, and no two tokens share a byte.
 #pragma once
 #include <type_traits>
 
@@ -98,12 +98,24 @@ struct Kv4Place {
     __device__ __forceinline__ T* columns(const Kv4Rows& a) const {
         return static_cast<T*>(is_v ? a.v : a.k) + token * (is_v ? a.ld_v : a.ld_k) + head * D + 8 * l;
     }
-    // of the thread's word of codes and of its group's (step, low) in the block
-    __device__ __forceinline__ uint32_t* word(unsigned char* blk) const {
-        const int t = slot & 15, n = l & 7;
-        return reinterpret_cast<uint32_t*>(is_v ? blk + 8 * D + (t >> 3) * (4 * D) + ((n * 4 + ((t & 7) >> 1)) * 2 + (t & 1)) * (D / 16) + 4 * (l >> 3)
-                                                : blk + (t * 4 + (l & 3)) * (D / 8) + 4 * (l >> 2));
+    // The thread's word of codes: eight columns of the keys, or two pieces of a column place of the values.
+    __device__ __forceinline__ uint32_t* keys(unsigned char* blk) const {
+        return reinterpret_cast<uint32_t*>(blk + ((slot & 15) * 4 + (l & 3)) * (D / 8) + 4 * (l >> 2));
     }
+    __device__ __forceinline__ uint16_t* values(unsigned char* blk) const {
+        const int t = slot & 15;
+        return reinterpret_cast<uint16_t*>(blk + 8 * D + (t >> 3) * (4 * D) + ((l & 7) * 4 + ((t & 7) >> 1)) * (D / 8) + 8 * (l >> 3)) + (t & 1);
+    }
+    __device__ __forceinline__ void put(unsigned char* blk, uint32_t word) const {
+        if (is_v) {
+            values(blk)[0] = (uint16_t)word;
+            values(blk)[2] = (uint16_t)(word >> 16);
+        } else {
+            *keys(blk) = word;
+        }
+    }
+    __device__ __forceinline__ uint32_t get(unsigned char* blk) const { return is_v ? values(blk)[0] | (uint32_t)values(blk)[2] << 16 : *keys(blk); }
+    // its group's (step, low)
     __device__ __forceinline__ uint32_t* pair(unsigned char* blk, int groups) const {
         return reinterpret_cast<uint32_t*>(blk + 16 * D) + ((is_v ? groups : 0) + l / (L / groups)) * 16 + (slot & 15);
     }
@@ -180,7 +192,7 @@ __global__ void __launch_bounds__(kKv4RowThreads) kv4_store_kernel(const __grid_
     if (p.is_v) word = nibbles_transposed(word, p.l);
     if (!p.on) return;
     unsigned char* blk = c.block(p.slot, p.head, D);
-    *p.word(blk) = word;
+    p.put(blk, word);
     if ((p.l & (per - 1)) == 0) *p.pair(blk, c.groups) = step_bits | kv4_bits<T>(lh.x + bad) << 16;
 }
 
@@ -192,7 +204,7 @@ __global__ void __launch_bounds__(kKv4RowThreads) kv4_load_kernel(const __grid_c
     uint32_t word = 0, pair = 0;
     if (p.on) {
         unsigned char* blk = c.block(p.slot, p.head, D);
-        word = *p.word(blk);
+        word = p.get(blk);
         pair = *p.pair(blk, c.groups);
     }
     if (p.is_v) word = nibbles_transposed(word, p.l);
@@ -260,6 +272,11 @@ __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+__device__ __forceinline__ uint32_t half2_minus(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
 // The transpose of an 8 x 8 tile of 16-bit values, a row's pair a thread.
 __device__ __forceinline__ uint32_t tile_transpose(uint32_t v) {
     uint32_t r;
@@ -275,14 +292,14 @@ template <typename T, int D, int NG, int NR>
 struct Kv4Rowset {
     static constexpr int kBytes = kKv4Block * D + 128 * NG;  // of a block of 16 tokens
     static constexpr int W = D / 32, J = D / 16;             // words of a lane and token; tiles of 16 columns
-    // fp16 outputs: what the rounding of p step loses is made good at the middle of the codes, so that it weighs code - 7.5 and not
-    // code (0.0005 -> 0.0003 of the output; bf16 outputs, rounded to 0.0017, do not show it)
+    // fp16 outputs: the values' operand is code - 8 (exact as well), so that the rounding of p step weighs that and not code
+    // (0.0005 -> 0.0003 of the output; bf16 outputs, rounded to 0.0017, do not show it)
     static constexpr bool kCentre = std::is_same_v<T, __half>;
     using Pair = unsigned long long;
 
     float acc[NR][J][4];
     float m[NR][2];
-    Pair l[NR], corr[NR][NG], lost[NR][NG];
+    Pair l[NR], corr[NR][NG];
     float limit;                                             // steps up to here fit the scale of p step, 2^(127 - f_exp)
     int f_exp;
     // operand B of the scores, sums of the scaled queries (times 2^-24), and what makes a raw score one in powers of two
@@ -331,7 +348,7 @@ struct Kv4Rowset {
                 sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
                 sum[i] *= 0x1p-24f;
                 low[r][i] = pair_of(__shfl_sync(0xffffffffu, sum[i], 8 * c), __shfl_sync(0xffffffffu, sum[i], 8 * c + 4));
-                corr[r][i] = lost[r][i] = 0;
+                corr[r][i] = 0;
             }
             back[r] = pair_of(__shfl_sync(0xffffffffu, undo, 8 * c), __shfl_sync(0xffffffffu, undo, 8 * c + 4));
             l[r] = 0;
@@ -414,10 +431,7 @@ struct Kv4Rowset {
             const Pair f2 = pair_of(f[0], f[1]);
             l[r] = mul2(l[r], f2);
 #pragma unroll
-            for (int i = 0; i < NG; ++i) {
-                corr[r][i] = mul2(corr[r][i], f2);
-                if constexpr (kCentre) lost[r][i] = mul2(lost[r][i], f2);
-            }
+            for (int i = 0; i < NG; ++i) corr[r][i] = mul2(corr[r][i], f2);
 #pragma unroll
             for (int j = 0; j < J; ++j)
 #pragma unroll
@@ -438,15 +452,11 @@ struct Kv4Rowset {
             f_exp = e;
             limit = e + 6 < 254 ? __uint_as_float((uint32_t)(e + 6) << 23) : 3.4e38f;
 #pragma unroll
-            for (int r = 0; r < NR; ++r) {
+            for (int r = 0; r < NR; ++r)
 #pragma unroll
                 for (int j = 0; j < J; ++j)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) acc[r][j][k] = f(acc[r][j][k]);
-                if constexpr (kCentre)
-#pragma unroll
-                    for (int i = 0; i < NG; ++i) lost[r][i] = mul2(mul2(lost[r][i], both(f.a)), both(f.b));
-            }
         }
     }
 
@@ -512,7 +522,7 @@ struct Kv4Rowset {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float2 pr = kv4_pair<T>(vp[u][i][h]);
-                    const Pair by = both(pr.x * f), lowest = both(pr.y);
+                    const Pair by = both(pr.x * f), lowest = both(kCentre ? fmaf(8.f, pr.x, pr.y) : pr.y);
 #pragma unroll
                     for (int r = 0; r < NR; ++r) {
                         float2 w;
@@ -525,15 +535,10 @@ struct Kv4Rowset {
                             w = halves(mul2(p[r][h], by));
                             corr[r][i] = fma2(p[r][h], lowest, corr[r][i]);
                         }
-                        const uint32_t two = half_pair(w.x, w.y);
-                        if constexpr (kCentre) {
-                            const float2 kept = kv4_pair<__half>(two);
-                            lost[r][i] = add2(lost[r][i], pair_of(w.x - kept.x, w.y - kept.y));
-                        }
-                        b[r][i][h] = tile_transpose(two);
+                        b[r][i][h] = tile_transpose(half_pair(w.x, w.y));
                     }
                 }
-            uint32_t vw[2][2][W / 2];                         // [eight tokens][token of the pair][word]
+            uint32_t vw[2][W];                                // [eight tokens][four columns of a pair of tokens]
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const unsigned char* at = blk + u * kBytes + 8 * D + h * 4 * D + lane * (D / 8);
@@ -541,20 +546,24 @@ struct Kv4Rowset {
                 else *reinterpret_cast<uint2*>(vw[h]) = *reinterpret_cast<const uint2*>(at);
             }
 #pragma unroll
-            for (int w = 0; w < W / 2; ++w)
+            for (int w = 0; w < W; ++w) {
+                uint32_t c[4], d[4];
+                q4_spread(vw[0][w], c);
+                q4_spread(vw[1][w], d);
+                if constexpr (kCentre)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    uint32_t c[4], d[4];
-                    q4_spread(__byte_perm(vw[0][0][w], vw[0][1][w], half ? 0x7632 : 0x5410), c);
-                    q4_spread(__byte_perm(vw[1][0][w], vw[1][1][w], half ? 0x7632 : 0x5410), d);
-                    const uint32_t a0[4] = {c[0], c[1], d[0], d[1]}, a1[4] = {c[2], c[3], d[2], d[3]};
-                    const int j = 4 * w + 2 * half;
+                    for (int k = 0; k < 4; ++k) {
+                        c[k] = half2_minus(c[k], k & 1 ? 0x00800080u : 0x00080008u);
+                        d[k] = half2_minus(d[k], k & 1 ? 0x00800080u : 0x00080008u);
+                    }
+                const uint32_t a0[4] = {c[0], c[1], d[0], d[1]}, a1[4] = {c[2], c[3], d[2], d[3]};
+                const int j = 2 * w;
 #pragma unroll
                     for (int r = 0; r < NR; ++r) {
                         q4_mma(acc[r][j], a0, b[r][j * NG / J][0], b[r][j * NG / J][1]);
                         q4_mma(acc[r][j + 1], a1, b[r][(j + 1) * NG / J][0], b[r][(j + 1) * NG / J][1]);
                     }
-                }
+            }
         }
     }
 
@@ -570,7 +579,7 @@ struct Kv4Rowset {
             }
             return f;
         };
-        const Q4Power undo(f_exp - 127 + 24), scale(f_exp - 127);
+        const Q4Power undo(f_exp - 127 + 24);
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
             float fix[NG][2];
@@ -579,11 +588,6 @@ struct Kv4Rowset {
                 const float2 v = over_lanes(corr[r][i]);
                 fix[i][0] = v.x;
                 fix[i][1] = v.y;
-                if constexpr (kCentre) {
-                    const float2 w = over_lanes(lost[r][i]);
-                    fix[i][0] += scale(w.x) * 7.5f;
-                    fix[i][1] += scale(w.y) * 7.5f;
-                }
             }
             const float2 sum = over_lanes(l[r]);
 #pragma unroll
@@ -646,31 +650,27 @@ __global__ void __launch_bounds__(kKv4Threads, NR == 1 ? 2 : 1) kv4_attention_ke
     unsigned char* ring = kv4_smem + mine * a.slots * (U * kBytes);
     const int bar0 = mine * a.slots;
     const int32_t* table = a.table + seq * a.ld_table;
-    // page of the block that this lane copies of the stream's chunk i, -1: none
-    auto page_of = [&](int i) {
-        const int sub = (from + mine + i * parts) * U + lane;
-        return lane < U && i < chunks && sub * kKv4Block < len ? __ldg(table + a.c.subs(sub)) : -1;
+    // Where the stream's blocks lie in the cache, 32 of them at a time, one a lane (-1: none).
+    int place = -1;
+    auto look_up = [&](int i) {
+        const int k = i + lane / U, sub = (from + mine + k * parts) * U + lane % U, at = a.c.subs(sub), subs = (int)a.c.subs.d;
+        const int page = k < chunks && sub * kKv4Block < len ? __ldg(table + at) : -1;
+        place = page >= 0 && page < a.n_pages ? (page * a.c.n_k + head) * subs + sub - at * subs : -1;
     };
-    int next = -1;                                            // of the chunk to be copied next
     auto copy = [&](int i, int slot) {
-        const int page = next;
-        next = page_of(i + 1);
-        const bool there = page >= 0 && page < a.n_pages;
+        if (i % (32 / U) == 0) look_up(i);
+        const int at = __shfl_sync(0xffffffffu, place, (i * U + lane) & 31);
+        const bool there = lane < U && at >= 0;
         const uint32_t which = __ballot_sync(0xffffffffu, there), bar = smem_u32(&full[bar0 + slot]);
         if (lane == 0) {
             present[bar0 + slot] = which;
             mbar_expect_tx(bar, __popc(which) * kBytes);
         }
         __syncwarp();
-        if (there) {
-            const int sub = (from + mine + i * parts) * U + lane, subs = (int)a.c.subs.d;
-            bulk_g2s(smem_u32(ring + (slot * U + lane) * kBytes), a.c.base + (((long long)page * a.c.n_k + head) * subs + sub - a.c.subs(sub) * subs) * kBytes, kBytes, bar);
-        }
+        if (there) bulk_g2s(smem_u32(ring + (slot * U + lane) * kBytes), a.c.base + (long long)at * kBytes, kBytes, bar);
     };
-    if (group == 0) {
-        next = page_of(0);
+    if (group == 0)
         for (int i = 0; i < min(a.slots, chunks); ++i) copy(i, i);
-    }
     Rowset set;
     set.begin(a, q0, head, row0 + group * 8 * NR, rows);
     const bool live = row0 + group * NR * 8 < rows;
