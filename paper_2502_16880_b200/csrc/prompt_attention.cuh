@@ -4,11 +4,12 @@
 // in one pass over the keys (running maximum and sum).
 //
 // A block takes two tiles of 128 rows: a row is a token and a query head, Gp heads (a power of two) of a group next to one another, so
-// that few tokens fill a tile too.  Both tiles read the same keys and values, 128 at a time, through a ring filled by TMA.
-//   S_t = Q_t K^T           operands in shared memory, sums in tensor memory (128 columns a tile)
-//   P_t = exp2(S_t - max)   by four warps a tile, a thread a row, back into tensor memory over S_t as 16-bit values
-//   O_t += P_t V            operand A from tensor memory, V as it lies (N-major); sums stay in tensor memory
-// One thread issues all MMAs; while it works on one tile, the other tile's warps do their exponentials.  The maximum is a
+// that few tokens fill a tile too.  Both tiles read the same keys and values, 64 at a time, through a ring filled by TMA.
+//   S = Q K^T           operands in shared memory, sums in tensor memory (two buffers of 64 columns a tile)
+//   P = exp2(S - max)   by four warps a tile, a thread a row, back into tensor memory over S as 16-bit values
+//   O += P V            operand A from tensor memory, V as it lies (N-major); sums stay in tensor memory
+// With two buffers a tile's warps do their exponentials while the tensor cores take the step before (its P V, then the scores
+// of the step after the next into the same buffer).  Each tile has its own thread that issues MMAs.  The maximum is a
 // reference that moves only when a score passes it by 2^8 (P stays below 2^8, its sum is fp32), so O is scaled in place a few times
 // a row at most, by the softmax warps themselves, and nothing else touches it before the end.
 // Masked scores are -inf before anything is computed of them; but a value row with an infinity or a NaN would reach every row of
@@ -22,9 +23,10 @@
 
 namespace coral {
 
-constexpr int kPaThreads = 10 * 32;                // warps 0..3 and 4..7: softmax of a tile each, 8: MMAs, 9: copies
-constexpr int kPaKeys = 128;                       // keys of a step
-constexpr int kPaBlock = 128 * 128;                // bytes of 128 rows x 64 columns
+constexpr int kPaThreads = 12 * 32;                // warps 0..3 and 4..7: softmax of a tile each, 8 and 9: a tile's MMAs each, 10: copies
+constexpr int kPaKeys = 64;                        // keys of a step
+constexpr int kPaRows = 128 * 128;                 // bytes of 64 columns of 128 query rows
+constexpr int kPaBlock = kPaKeys * 128;            // ... of a step's keys or values
 
 struct PaArgs {
     int n_seq, T, Tk, n_q, n_k, G, gp, D;          // gp: heads side by side in a tile, gp_log2 of them
@@ -48,18 +50,29 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
         "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
         ::"r"(dst), "l"(map), "r"(x0), "r"(x1), "r"(x2), "r"(bar) : "memory");
 }
-// Descriptor of an N-major operand: rows of 64 columns (128 bytes, 128-byte swizzle), eight of them 1024 bytes; the next 64 columns kPaBlock
-// bytes on.
-__device__ __forceinline__ uint64_t pa_desc_n(uint32_t saddr) {
-    return (uint64_t)((saddr >> 4) & 0x3FFF) | ((uint64_t)(kPaBlock >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+// Shared-memory descriptors by their low words (start address / 16, leading offset); what a tile's rows of 128 bytes, eight of them 1024
+// bytes, 128-byte swizzle need beside that is the same for both kinds.  N-major (the values): the next 64 columns lie kPaBlock bytes on.
+constexpr uint32_t kPaDescHi = 64u | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t pa_desc_k(uint32_t saddr) { return (saddr >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t pa_desc_n(uint32_t saddr) { return (saddr >> 4) | ((uint32_t)(kPaBlock >> 4) << 16); }
+// D (+)= A B, A from shared or from tensor memory.  ADD is known where the instruction is written, and the addresses are the same for
+// the warp: the issuing thread has next to nothing to do beside the MMAs.
+template <bool ADD>
+__device__ __forceinline__ void pa_mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %4};\n\tmov.b64 db, {%2, %4};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(kPaDescHi), "n"(ADD ? 1 : 0) : "memory");
 }
-__device__ __forceinline__ void pa_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+template <bool ADD>
+__device__ __forceinline__ void pa_mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 db, {%2, %4};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(kPaDescHi), "n"(ADD ? 1 : 0) : "memory");
 }
-__device__ __forceinline__ void pa_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+__device__ __forceinline__ bool pa_elect() {
+    uint32_t on;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(on));
+    return on != 0;
 }
 // 32 columns of this thread's tensor-memory lane, not waited for.
 __device__ __forceinline__ void pa_ld32(uint32_t taddr, uint32_t* r) {
@@ -174,19 +187,19 @@ __device__ __noinline__ void pa_row_again(const PaArgs& a, const T* q, const T* 
     }
 }
 
-// DB: blocks of 64 columns of a head (1 or 2).  STAGES: tiles of 128 keys or values in the ring.
-template <int DB> constexpr int kPaStages = DB == 2 ? 5 : 8;
-template <int DB> constexpr size_t pa_smem_bytes() { return 1024 + (size_t)(2 + kPaStages<DB>) * DB * kPaBlock; }
+// DB: blocks of 64 columns of a head (1 or 2).  Stages: steps' keys or values in the ring.
+template <int DB> constexpr int kPaStages = DB == 2 ? 10 : 16;
+template <int DB> constexpr size_t pa_smem_bytes() { return 1024 + (size_t)DB * (2 * kPaRows + kPaStages<DB> * kPaBlock); }
 
 template <typename T, int DB>
 __global__ void __launch_bounds__(kPaThreads, 1)
 prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                         const __grid_constant__ CUtensorMap map_v) {
-    constexpr int STAGES = kPaStages<DB>, kTile = DB * kPaBlock;
+    constexpr int STAGES = kPaStages<DB>, kTile = DB * kPaRows, kStep = DB * kPaBlock;
     extern __shared__ unsigned char pa_smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pa_smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* s_kv = smem + 2 * kTile;
-    __shared__ __align__(8) uint64_t q_full, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_full[2], pv_done[2];
+    __shared__ __align__(8) uint64_t q_full, kv_full[STAGES], kv_empty[STAGES], s_full[4], p_full[4], pv_done[4];   // [tile][buffer]
     __shared__ PaShare share;
     __shared__ int s_scan[kPaThreads / 32];
     __shared__ uint32_t tmem_slot;
@@ -201,9 +214,9 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
         mbar_init(smem_u32(&q_full), 1);
         for (int i = 0; i < STAGES; ++i) {
             mbar_init(smem_u32(&kv_full[i]), 1);
-            mbar_init(smem_u32(&kv_empty[i]), 1);
+            mbar_init(smem_u32(&kv_empty[i]), 2);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 4; ++i) {
             mbar_init(smem_u32(&s_full[i]), 1);
             mbar_init(smem_u32(&p_full[i]), 4);
             mbar_init(smem_u32(&pv_done[i]), 1);
@@ -237,70 +250,89 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
     };
     const int n0 = steps_of(0), n1 = steps_of(1), n = max(n0, n1);
 
-    if (warp == 9) {
+    if (warp == 10) {
         if (lane == 0 && n > 0) {
             mbar_expect_tx(smem_u32(&q_full), 2 * kTile);
             for (int t = 0; t < 2; ++t)
                 for (int b = 0; b < DB; ++b)
-                    tma_load_3d(smem_u32(smem + t * kTile + b * kPaBlock), &map_q, b * 64, head0, sh.q0 + (sh.pair * 2 + t) * tile_tokens, smem_u32(&q_full));
+                    tma_load_3d(smem_u32(smem + t * kTile + b * kPaRows), &map_q, b * 64, head0, sh.q0 + (sh.pair * 2 + t) * tile_tokens, smem_u32(&q_full));
             int stage = 0;
             uint32_t phase = 0;
-            for (int i = 0; i < 2 * n; ++i) {
+            auto load = [&](const CUtensorMap* map, int j) {
                 pa_wait(smem_u32(&kv_empty[stage]), phase ^ 1u, &abort_flag, a.st);
                 const uint32_t bar = smem_u32(&kv_full[stage]);
-                mbar_expect_tx(bar, kTile);
-                for (int b = 0; b < DB; ++b)
-                    tma_load_3d(smem_u32(s_kv + stage * kTile + b * kPaBlock), i & 1 ? &map_v : &map_k, b * 64, kv_head, sh.k0 + (i >> 1) * kPaKeys, bar);
+                mbar_expect_tx(bar, kStep);
+                for (int b = 0; b < DB; ++b) tma_load_3d(smem_u32(s_kv + stage * kStep + b * kPaBlock), map, b * 64, kv_head, sh.k0 + j * kPaKeys, bar);
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            };
+            // the order in which they are used: keys of steps 0 and 1, then a step's values and the keys of the step after the next
+            load(&map_k, 0);
+            if (n > 1) load(&map_k, 1);
+            for (int j = 0; j < n; ++j) {
+                load(&map_v, j);
+                if (j + 2 < n) load(&map_k, j + 2);
             }
             // nothing is left on its way when the block ends, an expired wait elsewhere included
             pa_wait(smem_u32(&q_full), 0, &abort_flag, a.st);
             for (int i = max(0, 2 * n - STAGES); i < 2 * n; ++i) pa_wait(smem_u32(&kv_full[i % STAGES]), (uint32_t)(i / STAGES) & 1u, &abort_flag, a.st);
         }
-    } else if (warp == 8) {
-        if (lane == 0 && n > 0) {
-            constexpr uint32_t kType = std::is_same_v<T, __nv_bfloat16> ? 1u : 0u;
-            const int d16 = (a.D + 15) / 16;
-            const uint32_t base = (1u << 4) | (kType << 7) | (kType << 10) | (8u << 24);
-            const uint32_t idesc_s = base | (16u << 17), idesc_o = base | (1u << 16) | ((uint32_t)(2 * d16) << 17);
-            const uint32_t sq = smem_u32(smem), skv = smem_u32(s_kv);
-            auto scores = [&](int t, int i) {                  // i: place in the ring's order
-                const uint32_t q = sq + t * kTile, k = skv + (i % STAGES) * kTile;
-                for (int kk = 0; kk < d16; ++kk) {
-                    const uint32_t off = (kk >> 2) * kPaBlock + (kk & 3) * 32;
-                    pa_mma_ss(tmem + t * 128, tc_smem_desc(q + off), tc_smem_desc(k + off), idesc_s, kk > 0);
-                }
-                tc_commit(smem_u32(&s_full[t]));
-            };
-            auto full = [&](int i) { pa_wait(smem_u32(&kv_full[i % STAGES]), (uint32_t)(i / STAGES) & 1u, &abort_flag, a.st); };
-            pa_wait(smem_u32(&q_full), 0, &abort_flag, a.st);
-            full(0);
-            tc_fence_after();
-            if (n0 > 0) scores(0, 0);
-            if (n1 > 0) scores(1, 0);
-            tc_commit(smem_u32(&kv_empty[0]));
-            for (int j = 0; j < n; ++j) {
-                full(2 * j + 1);
-                if (j + 1 < n) full(2 * j + 2);
+    } else if (warp == 8 || warp == 9) {
+        // The MMAs of tile t, in the ring's order; both tiles' warps free a place of it.
+        const int t = warp - 8, nt = t ? n1 : n0;
+        constexpr uint32_t kType = std::is_same_v<T, __nv_bfloat16> ? 1u : 0u;
+        constexpr uint32_t kBase = (1u << 4) | (kType << 7) | (kType << 10) | (8u << 24);
+        const int d16 = (a.D + 15) / 16;
+        const uint32_t idesc_s = kBase | ((uint32_t)(kPaKeys / 8) << 17), idesc_o = kBase | (1u << 16) | ((uint32_t)(2 * d16) << 17);
+        const uint32_t q = pa_desc_k(smem_u32(smem) + t * kTile), kv = smem_u32(s_kv), ts = tmem + t * 128, to = tmem + 256 + t * 128;
+        int stage = 0;
+        uint32_t phase = 0;
+        auto full = [&]() { pa_wait(smem_u32(&kv_full[stage]), phase, &abort_flag, a.st); };
+        auto next = [&]() {
+            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        };
+        auto scores = [&](int j) {                             // S = Q K^T of step j; the keys are free behind it
+            full();
+            if (j < nt) {
+                tc_fence_after();
+                if (pa_elect()) {
+                    const uint32_t k = pa_desc_k(kv + stage * kStep), to_s = ts + (j & 1) * kPaKeys;
+                    pa_mma_ss<false>(to_s, q, k, idesc_s);
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const int nt = t ? n1 : n0;
-                    if (j < nt) {
-                        pa_wait(smem_u32(&p_full[t]), (uint32_t)j & 1u, &abort_flag, a.st);
-                        tc_fence_after();
-                        const uint32_t v = skv + ((2 * j + 1) % STAGES) * kTile;
-#pragma unroll
-                        for (int kk = 0; kk < kPaKeys / 16; ++kk)
-                            pa_mma_ts(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, pa_desc_n(v + kk * 2048), idesc_o, j > 0 || kk > 0);
-                        tc_commit(smem_u32(&pv_done[t]));
-                    }
-                    if (t == 1) tc_commit(smem_u32(&kv_empty[(2 * j + 1) % STAGES]));
-                    if (j + 1 < nt) scores(t, 2 * j + 2);
+                    for (int kk = 1; kk < DB * 4; ++kk)
+                        if (kk < d16) pa_mma_ss<true>(to_s, q + (kk >> 2) * (kPaRows / 16) + (kk & 3) * 2, k + (kk >> 2) * (kPaBlock / 16) + (kk & 3) * 2, idesc_s);
+                    tc_commit(smem_u32(&s_full[t * 2 + (j & 1)]));
+                    tc_commit(smem_u32(&kv_empty[stage]));
                 }
-                if (j + 1 < n) tc_commit(smem_u32(&kv_empty[(2 * j + 2) % STAGES]));
+            } else if (lane == 0) {
+                mbar_arrive(smem_u32(&kv_empty[stage]));       // the other tile's alone
             }
+            next();
+        };
+        if (n > 0) pa_wait(smem_u32(&q_full), 0, &abort_flag, a.st);
+        if (n > 0) scores(0);
+        if (n > 1) scores(1);
+        for (int j = 0; j < n; ++j) {
+            full();
+            if (j < nt) {
+                const int buf = j & 1;
+                pa_wait(smem_u32(&p_full[t * 2 + buf]), (uint32_t)(j >> 1) & 1u, &abort_flag, a.st);
+                tc_fence_after();
+                if (pa_elect()) {
+                    const uint32_t v = pa_desc_n(kv + stage * kStep), p = ts + buf * kPaKeys;
+                    if (j == 0) pa_mma_ts<false>(to, p, v, idesc_o);
+                    else pa_mma_ts<true>(to, p, v, idesc_o);
+#pragma unroll
+                    for (int kk = 1; kk < kPaKeys / 16; ++kk) pa_mma_ts<true>(to, p + kk * 8, v + kk * 128, idesc_o);
+                    tc_commit(smem_u32(&pv_done[t * 2 + buf]));
+                    tc_commit(smem_u32(&kv_empty[stage]));
+                }
+            } else if (lane == 0) {
+                mbar_arrive(smem_u32(&kv_empty[stage]));
+            }
+            next();
+            if (j + 2 < n) scores(j + 2);
         }
-    } else {
+    } else if (warp < 8) {
         const int t = warp >> 2, row = (warp & 3) * 32 + lane, nt = t ? n1 : n0;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = tmem + t * 128 + lanes, to = tmem + 256 + t * 128 + lanes;
@@ -309,27 +341,27 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
         const int all_see = max(0, min(tok0 + past + 1, sh.Lk));
         float m = kNegInf, mc = 0.f;                           // reference, raw and in powers of two
         unsigned long long sum2 = 0;
-        float s[128];
+        float s[kPaKeys];
         uint32_t* sr = reinterpret_cast<uint32_t*>(s);
         for (int j = 0; j < nt; ++j) {
-            pa_wait(smem_u32(&s_full[t]), (uint32_t)j & 1u, &abort_flag, a.st);
-            // done since the scores are, but a phase that is not waited for would be taken for the one after the next
-            if (j > 0) pa_wait(smem_u32(&pv_done[t]), (uint32_t)(j - 1) & 1u, &abort_flag, a.st);
+            const int buf = j & 1;
+            pa_wait(smem_u32(&s_full[t * 2 + buf]), (uint32_t)(j >> 1) & 1u, &abort_flag, a.st);
             __syncwarp();
             tc_fence_after();
-#pragma unroll
-            for (int b = 0; b < 4; ++b) pa_ld32(ts + b * 32, sr + b * 32);
+            const uint32_t at = ts + buf * kPaKeys;
+            pa_ld32(at, sr);
+            pa_ld32(at + 32, sr + 32);
             pa_ld_wait();
             if ((j + 1) * kPaKeys > all_see) {
                 const int left = seen - j * kPaKeys;
 #pragma unroll
-                for (int i = 0; i < 128; ++i) s[i] = i < left ? s[i] : kNegInf;
+                for (int i = 0; i < kPaKeys; ++i) s[i] = i < left ? s[i] : kNegInf;
             }
             float m4[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-            for (int i = 4; i < 128; i += 8)
+            for (int i = 4; i < kPaKeys; i += 8)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) m4[e] = i + 4 + e < 128 ? pa_max3(m4[e], s[i + e], s[i + 4 + e]) : fmaxf(m4[e], s[i + e]);
+                for (int e = 0; e < 4; ++e) m4[e] = i + 4 + e < kPaKeys ? pa_max3(m4[e], s[i + e], s[i + 4 + e]) : fmaxf(m4[e], s[i + e]);
             const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
             const bool moves = top * a.c > mc + 8.f || (m == kNegInf && top > kNegInf);
             if (__any_sync(0xffffffffu, moves)) {
@@ -338,7 +370,10 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
                 m = next;
                 mc = next_c;
                 sum2 = mul2(sum2, pair_of(f, f));
-                if (j > 0) {
+                if (j > 0) {                                   // O, once the step before is in it
+                    pa_wait(smem_u32(&pv_done[t * 2 + (buf ^ 1)]), (uint32_t)((j - 1) >> 1) & 1u, &abort_flag, a.st);
+                    __syncwarp();
+                    tc_fence_after();
 #pragma unroll 1
                     for (int b = 0; b < 2 * DB; ++b) {
                         uint32_t o[32];
@@ -352,25 +387,24 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
                 }
             }
             const unsigned long long c2 = pair_of(a.c, a.c), m2 = pair_of(-mc, -mc);
-            uint32_t p[64];
+            uint32_t p[kPaKeys / 2];
 #pragma unroll
-            for (int i = 0; i < 64; ++i) {
+            for (int i = 0; i < kPaKeys / 2; ++i) {
                 const float2 x = halves(fma2(pair_of(s[2 * i], s[2 * i + 1]), c2, m2));
                 const float lo = pa_exp2(x.x), hi = pa_exp2(x.y);
-                asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum2) : "l"(pair_of(lo, hi)));
+                sum2 = add2(sum2, pair_of(lo, hi));
                 p[i] = pa_pack<T>(lo, hi);
             }
-            pa_st32(ts, p);
-            pa_st32(ts + 32, p + 32);
+            pa_st32(at, p);
             pa_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&p_full[t]));
+            if (lane == 0) mbar_arrive(smem_u32(&p_full[t * 2 + buf]));
         }
         const float2 sums = halves(sum2);
         const float sum = sums.x + sums.y, inv = sum == 0.f ? 0.f : 1.f / sum;
         if (nt > 0) {
-            pa_wait(smem_u32(&pv_done[t]), (uint32_t)(nt - 1) & 1u, &abort_flag, a.st);
+            pa_wait(smem_u32(&pv_done[t * 2 + ((nt - 1) & 1)]), (uint32_t)((nt - 1) >> 1) & 1u, &abort_flag, a.st);
             __syncwarp();
             tc_fence_after();
         }
