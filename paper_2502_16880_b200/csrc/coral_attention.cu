@@ -296,12 +296,14 @@ int coral_lmhead_prompt_attention(const coral_lmhead_prompt_args* a, void* works
     k.ld_q = a->ld_q; k.ld_k = a->ld_k; k.ld_v = a->ld_v; k.ld_out = a->ld_out;
     k.out = a->out_dev; k.lse = a->out_lse_dev;
     k.st = static_cast<DeviceState*>(workspace_dev);
-    const int per = 256 / k.gp;                        // tokens of a block; sequences have at most T / per + n_seq blocks of them in all
-    const long long slots = std::min((long long)a->T, (long long)a->T / per + a->n_seq), blocks = slots * a->n_k * (k.G / k.gp);
-    if (blocks > 0x7fffffffLL) return CORAL_ERR_TOO_LARGE;
+    const int per = 256 / k.gp;                        // tokens of a pair of tiles; sequences have at most T / per + n_seq pairs in all
+    const long long slots = std::min((long long)a->T, (long long)a->T / per + a->n_seq), units = slots * a->n_k * (k.G / k.gp);
+    if (units > 0x7fffffffLL) return CORAL_ERR_TOO_LARGE;
+    k.units = (int)units;
+    const unsigned blocks = (unsigned)std::min(units, (long long)kSms);
     if (a->type == CORAL_TYPE_BF16)
-        return a->D > 64 ? launch_prompt<__nv_bfloat16, 2>(a, k, (unsigned)blocks, st) : launch_prompt<__nv_bfloat16, 1>(a, k, (unsigned)blocks, st);
-    return a->D > 64 ? launch_prompt<__half, 2>(a, k, (unsigned)blocks, st) : launch_prompt<__half, 1>(a, k, (unsigned)blocks, st);
+        return a->D > 64 ? launch_prompt<__nv_bfloat16, 2>(a, k, blocks, st) : launch_prompt<__nv_bfloat16, 1>(a, k, blocks, st);
+    return a->D > 64 ? launch_prompt<__half, 2>(a, k, blocks, st) : launch_prompt<__half, 1>(a, k, blocks, st);
 }
 
 int coral_lmhead_kv4_bytes(const coral_lmhead_kv4_config* c, size_t* bytes) {

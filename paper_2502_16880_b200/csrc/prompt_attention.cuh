@@ -23,14 +23,15 @@
 
 namespace coral {
 
-constexpr int kPaThreads = 12 * 32;                // warps 0..3 and 4..7: softmax of a tile each, 8 and 9: a tile's MMAs each, 10: copies
+constexpr int kPaThreads = 12 * 32;                // warps 0..3 and 4..7: softmax of a tile each, 8 and 9: a tile's MMAs each, 10: copies, 11: shares
+constexpr int kPaShares = 4;                       // shares of a block known ahead
 constexpr int kPaKeys = 64;                        // keys of a step
 constexpr int kPaRows = 128 * 128;                 // bytes of 64 columns of 128 query rows
 constexpr int kPaBlock = kPaKeys * 128;            // ... of a step's keys or values
 
 struct PaArgs {
     int n_seq, T, Tk, n_q, n_k, G, gp, D;          // gp: heads side by side in a tile, gp_log2 of them
-    int gp_log2;
+    int gp_log2, units;                            // units: places for pairs of tiles of all sequences, times groups of heads
     float c;                                       // scale log2(e)
     const int64_t *q_offsets, *k_offsets;
     const void *q, *k, *v;
@@ -40,9 +41,9 @@ struct PaArgs {
     DeviceState* st;
 };
 
-// A block's share, found once and kept in shared memory.
+// One turn of a block: a pair of tiles of a sequence (and a group of heads, which goes by the turn's number).
 struct PaShare {
-    int q0, k0, Lq, Lk, pair;                      // pair < 0: none
+    int q0, k0, Lq, Lk, pair, hg;                  // pair < 0: none
 };
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x0, int x1, int x2, uint32_t bar) {
@@ -116,38 +117,116 @@ template <> __device__ __forceinline__ uint32_t pa_pack<__half>(float lo, float 
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// The sequence and pair of tiles of slot `slot` (pairs of a sequence from its end: the longest rows start first).  All threads.
-__device__ __forceinline__ void pa_find(const PaArgs& a, int slot, PaShare* out, int* s_scan) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = 256 >> a.gp_log2;
-    int before = 0;
-    for (int base = 0; base < a.n_seq; base += kPaThreads) {
-        const int seq = base + threadIdx.x;
-        int q0 = 0, Lq = 0;
-        if (seq < a.n_seq) clamped_range(a.q_offsets, seq, a.T, &q0, &Lq);
-        const int n = (Lq + per - 1) / per;
-        int sum = n;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, sum, o);
-            if (lane >= o) sum += v;
-        }
-        if (lane == 31) s_scan[warp] = sum;
-        __syncthreads();
-        int at = before;
-        for (int w = 0; w < kPaThreads / 32; ++w) {
-            if (w < warp) at += s_scan[w];
-            before += s_scan[w];
-        }
-        const int first = at + sum - n;
-        if (slot >= first && slot < first + n) {
-            int k0 = q0, Lk = Lq;
-            if (a.k_offsets) clamped_range(a.k_offsets, seq, a.Tk, &k0, &Lk);
-            *out = PaShare{q0, k0, Lq, Lk, n - 1 - (slot - first)};
-        }
-        __syncthreads();
-        if (slot < before) return;
-    }
+// The turns of a block: every grid-th unit, forwards and backwards in turn.  Units come with their rows' lengths falling, so the blocks'
+// sums come out alike (nine packed prompts of 1 to 2048 tokens: 113 us sequence by sequence, 97 so).
+__device__ __forceinline__ int pa_unit(const PaArgs& a, int turn) {
+    const long long u = (long long)turn * gridDim.x + (turn & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    return u < a.units ? (int)u : -1;
 }
+__device__ __forceinline__ int pa_turns(const PaArgs& a) { return (a.units - 1) / (int)gridDim.x + 1; }
+
+// Finds units' sequences, by a warp; the units that it is asked for must not go down.  Up to 128 sequences: pair p of every sequence that
+// has one, then pair p - 1 ...; more: the sequences in turn, each from its end.
+struct PaFinder {
+    static constexpr int kWays = 4;
+    int n[kWays];                                  // pairs of tiles of sequences 32 i + lane
+    int level = 0, base = 0, before = 0;           // pair looked at, sequences passed, units in front of them
+    bool by_level;
+
+    __device__ __forceinline__ explicit PaFinder(const PaArgs& a) : by_level(a.n_seq <= 32 * kWays) {
+        if (!by_level) return;
+        int most = 0;
+#pragma unroll
+        for (int i = 0; i < kWays; ++i) {
+            const int seq = i * 32 + (threadIdx.x & 31);
+            int q0 = 0, Lq = 0;
+            if (seq < a.n_seq) clamped_range(a.q_offsets, seq, a.T, &q0, &Lq);
+            n[i] = pairs(a, Lq);
+            most = max(most, n[i]);
+        }
+        level = __reduce_max_sync(0xffffffffu, most) - 1;
+    }
+    static __device__ __forceinline__ int pairs(const PaArgs& a, int Lq) {
+        const int per = 256 >> a.gp_log2;
+        return (Lq + per - 1) / per;
+    }
+    // the sequence's share, by all lanes
+    static __device__ __forceinline__ PaShare share(const PaArgs& a, int seq, int pair, int hg) {
+        PaShare s{0, 0, 0, 0, pair, hg};
+        clamped_range(a.q_offsets, seq, a.T, &s.q0, &s.Lq);
+        s.k0 = s.q0;
+        s.Lk = s.Lq;
+        if (a.k_offsets) clamped_range(a.k_offsets, seq, a.Tk, &s.k0, &s.Lk);
+        return s;
+    }
+    __device__ __forceinline__ PaShare operator()(const PaArgs& a, int unit) {
+        const int lane = threadIdx.x & 31, hgs = a.n_k * (a.G >> a.gp_log2), slot = unit / hgs, hg = unit - slot * hgs;
+        if (by_level) {
+            for (; level >= 0; --level) {
+                uint32_t has[kWays];
+                int all = 0;
+#pragma unroll
+                for (int i = 0; i < kWays; ++i) {
+                    has[i] = __ballot_sync(0xffffffffu, n[i] > level);
+                    all += __popc(has[i]);
+                }
+                if (slot >= before + all) {
+                    before += all;
+                    continue;
+                }
+                int r = slot - before, seq = -1;   // the r-th of those that have it
+#pragma unroll
+                for (int i = 0; i < kWays; ++i) {
+                    const uint32_t at = __ballot_sync(0xffffffffu, (has[i] >> lane & 1u) && __popc(has[i] & ((1u << lane) - 1)) == r);
+                    if (seq < 0 && at) seq = i * 32 + __ffs(at) - 1;
+                    r = seq >= 0 ? -1 : r - __popc(has[i]);
+                }
+                return share(a, seq, level, hg);
+            }
+        } else {
+            for (; base < a.n_seq; base += 32) {
+                const int seq = base + lane;
+                int q0 = 0, Lq = 0;
+                if (seq < a.n_seq) clamped_range(a.q_offsets, seq, a.T, &q0, &Lq);
+                const int mine = pairs(a, Lq);
+                int sum = mine;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int v = __shfl_up_sync(0xffffffffu, sum, o);
+                    if (lane >= o) sum += v;
+                }
+                const int all = __shfl_sync(0xffffffffu, sum, 31);
+                if (slot >= before + all) {
+                    before += all;
+                    continue;
+                }
+                const int first = before + sum - mine, from = __ffs(__ballot_sync(0xffffffffu, slot >= first && slot < first + mine)) - 1;
+                return share(a, base + from, __shfl_sync(0xffffffffu, mine - 1 - (slot - first), from), hg);
+            }
+        }
+        return PaShare{0, 0, 0, 0, -1, 0};
+    }
+};
+
+// What a unit's share means.
+struct PaUnit {
+    PaShare sh;
+    int tile_tokens, kv_head, head0, past, n[2], steps;
+    __device__ __forceinline__ PaUnit(const PaArgs& a, const PaShare& share) : sh(share) {
+        tile_tokens = 128 >> a.gp_log2;
+        const int per_head = a.G >> a.gp_log2;
+        kv_head = sh.hg / per_head;
+        head0 = kv_head * a.G + (sh.hg - kv_head * per_head) * a.gp;
+        past = sh.Lk - sh.Lq;                      // token i sees keys up to i + past
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {              // steps of a tile: keys that its last token sees
+            const int tok0 = token0(t), last = min(tok0 + tile_tokens, sh.Lq) - 1;
+            n[t] = tok0 >= sh.Lq ? 0 : (max(0, min(last + past + 1, sh.Lk)) + kPaKeys - 1) / kPaKeys;
+        }
+        steps = max(n[0], n[1]);
+    }
+    __device__ __forceinline__ int token0(int t) const { return (sh.pair * 2 + t) * tile_tokens; }
+};
 
 // One row again, by a warp: only keys that it sees take part.  m is the reference in powers of two, four columns a lane.
 template <typename T>
@@ -199,19 +278,16 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
     extern __shared__ unsigned char pa_smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pa_smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* s_kv = smem + 2 * kTile;
-    __shared__ __align__(8) uint64_t q_full, kv_full[STAGES], kv_empty[STAGES], s_full[4], p_full[4], pv_done[4];   // [tile][buffer]
-    __shared__ PaShare share;
-    __shared__ int s_scan[kPaThreads / 32];
+    __shared__ __align__(8) uint64_t q_full, q_empty, kv_full[STAGES], kv_empty[STAGES], s_full[4], p_full[4], pv_done[4];   // [tile][buffer]
+    __shared__ __align__(8) uint64_t o_free[2], share_full[kPaShares], share_empty[kPaShares];
+    __shared__ PaShare shares[kPaShares];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-    pdl_wait();
-    const int hgs = a.n_k * (a.G >> a.gp_log2), hg = blockIdx.x % hgs, slot = blockIdx.x / hgs;
     if (threadIdx.x == 0) {
-        share.pair = -1;
-        if (blockIdx.x == 0) a.st->status = 0;      // a wait would have to fail millions of polls before this
         mbar_init(smem_u32(&q_full), 1);
+        mbar_init(smem_u32(&q_empty), 2);
         for (int i = 0; i < STAGES; ++i) {
             mbar_init(smem_u32(&kv_full[i]), 1);
             mbar_init(smem_u32(&kv_empty[i]), 2);
@@ -221,15 +297,15 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
             mbar_init(smem_u32(&p_full[i]), 4);
             mbar_init(smem_u32(&pv_done[i]), 1);
         }
+        for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&o_free[i]), 4);
+        for (int i = 0; i < kPaShares; ++i) {
+            mbar_init(smem_u32(&share_full[i]), 1);
+            mbar_init(smem_u32(&share_empty[i]), 11);
+        }
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    __syncthreads();
-    pa_find(a, slot, &share, s_scan);
-    __syncthreads();
-    const PaShare sh = share;
-    if (sh.pair < 0) return;
     if (warp == 8) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -237,106 +313,154 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    pdl_wait();
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.st->status = 0;      // a wait would have to fail millions of polls before this
     const uint32_t tmem = tmem_slot;
-    const int tile_tokens = 128 >> a.gp_log2, per_head = a.G >> a.gp_log2;
-    const int kv_head = hg / per_head, head0 = kv_head * a.G + (hg - kv_head * per_head) * a.gp;
-    const int past = sh.Lk - sh.Lq;                            // token i sees keys up to i + past
-    // steps of a tile: keys that its last token sees
-    auto steps_of = [&](int t) {
-        const int tok0 = (sh.pair * 2 + t) * tile_tokens;
-        if (tok0 >= sh.Lq) return 0;
-        const int last = min(tok0 + tile_tokens, sh.Lq) - 1;
-        return max(0, min(last + past + 1, sh.Lk) + kPaKeys - 1) / kPaKeys;
+    const int turns = pa_turns(a);
+    // The share of a turn, by all lanes of a warp or by one thread alone (which then counts for its warp).
+    auto share_of = [&](int turn, bool alone) {
+        const int i = turn % kPaShares;
+        pa_wait(smem_u32(&share_full[i]), (uint32_t)(turn / kPaShares) & 1u, &abort_flag, a.st);
+        const PaShare sh = shares[i];
+        if (!alone) __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&share_empty[i]));
+        return sh;
     };
-    const int n0 = steps_of(0), n1 = steps_of(1), n = max(n0, n1);
 
-    if (warp == 10) {
-        if (lane == 0 && n > 0) {
-            mbar_expect_tx(smem_u32(&q_full), 2 * kTile);
-            for (int t = 0; t < 2; ++t)
-                for (int b = 0; b < DB; ++b)
-                    tma_load_3d(smem_u32(smem + t * kTile + b * kPaRows), &map_q, b * 64, head0, sh.q0 + (sh.pair * 2 + t) * tile_tokens, smem_u32(&q_full));
-            int stage = 0;
+    if (warp == 11) {
+        PaFinder find(a);
+        for (int turn = 0; turn < turns; ++turn) {
+            const int unit = pa_unit(a, turn), i = turn % kPaShares;
+            PaShare sh{0, 0, 0, 0, -1, 0};
+            if (unit >= 0) sh = find(a, unit);
+            pa_wait(smem_u32(&share_empty[i]), ((uint32_t)(turn / kPaShares) & 1u) ^ 1u, &abort_flag, a.st);
+            __syncwarp();
+            if (lane == 0) {
+                shares[i] = sh;
+                mbar_arrive(smem_u32(&share_full[i]));
+            }
+        }
+    } else if (warp == 10) {
+        if (lane == 0) {
+            int stage = 0, loads = 0, queries = 0;
             uint32_t phase = 0;
-            auto load = [&](const CUtensorMap* map, int j) {
-                pa_wait(smem_u32(&kv_empty[stage]), phase ^ 1u, &abort_flag, a.st);
-                const uint32_t bar = smem_u32(&kv_full[stage]);
-                mbar_expect_tx(bar, kStep);
-                for (int b = 0; b < DB; ++b) tma_load_3d(smem_u32(s_kv + stage * kStep + b * kPaBlock), map, b * 64, kv_head, sh.k0 + j * kPaKeys, bar);
-                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-            };
-            // the order in which they are used: keys of steps 0 and 1, then a step's values and the keys of the step after the next
-            load(&map_k, 0);
-            if (n > 1) load(&map_k, 1);
-            for (int j = 0; j < n; ++j) {
-                load(&map_v, j);
-                if (j + 2 < n) load(&map_k, j + 2);
+            for (int turn = 0; turn < turns; ++turn) {
+                const PaShare sh = share_of(turn, true);
+                if (sh.pair < 0) continue;
+                const PaUnit u(a, sh);
+                if (u.steps == 0) continue;
+                auto load = [&](const CUtensorMap* map, int j) {
+                    pa_wait(smem_u32(&kv_empty[stage]), phase ^ 1u, &abort_flag, a.st);
+                    const uint32_t bar = smem_u32(&kv_full[stage]);
+                    mbar_expect_tx(bar, kStep);
+                    for (int b = 0; b < DB; ++b) tma_load_3d(smem_u32(s_kv + stage * kStep + b * kPaBlock), map, b * 64, u.kv_head, sh.k0 + j * kPaKeys, bar);
+                    ++loads;
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                };
+                // the order in which they are used: keys of steps 0 and 1, then a step's values and the keys of the step after the next
+                load(&map_k, 0);
+                pa_wait(smem_u32(&q_empty), (uint32_t)(queries & 1) ^ 1u, &abort_flag, a.st);
+                mbar_expect_tx(smem_u32(&q_full), 2 * kTile);
+                for (int t = 0; t < 2; ++t)
+                    for (int b = 0; b < DB; ++b)
+                        tma_load_3d(smem_u32(smem + t * kTile + b * kPaRows), &map_q, b * 64, u.head0, sh.q0 + u.token0(t), smem_u32(&q_full));
+                ++queries;
+                if (u.steps > 1) load(&map_k, 1);
+                for (int j = 0; j < u.steps; ++j) {
+                    load(&map_v, j);
+                    if (j + 2 < u.steps) load(&map_k, j + 2);
+                }
             }
             // nothing is left on its way when the block ends, an expired wait elsewhere included
-            pa_wait(smem_u32(&q_full), 0, &abort_flag, a.st);
-            for (int i = max(0, 2 * n - STAGES); i < 2 * n; ++i) pa_wait(smem_u32(&kv_full[i % STAGES]), (uint32_t)(i / STAGES) & 1u, &abort_flag, a.st);
+            if (queries) pa_wait(smem_u32(&q_full), (uint32_t)(queries - 1) & 1u, &abort_flag, a.st);
+            for (int i = max(0, loads - STAGES); i < loads; ++i) pa_wait(smem_u32(&kv_full[i % STAGES]), (uint32_t)(i / STAGES) & 1u, &abort_flag, a.st);
         }
     } else if (warp == 8 || warp == 9) {
         // The MMAs of tile t, in the ring's order; both tiles' warps free a place of it.
-        const int t = warp - 8, nt = t ? n1 : n0;
+        const int t = warp - 8;
         constexpr uint32_t kType = std::is_same_v<T, __nv_bfloat16> ? 1u : 0u;
         constexpr uint32_t kBase = (1u << 4) | (kType << 7) | (kType << 10) | (8u << 24);
         const int d16 = (a.D + 15) / 16;
         const uint32_t idesc_s = kBase | ((uint32_t)(kPaKeys / 8) << 17), idesc_o = kBase | (1u << 16) | ((uint32_t)(2 * d16) << 17);
         const uint32_t q = pa_desc_k(smem_u32(smem) + t * kTile), kv = smem_u32(s_kv), ts = tmem + t * 128, to = tmem + 256 + t * 128;
-        int stage = 0;
+        int stage = 0, queries = 0, outputs = 0, done = 0;     // done: steps of this tile in earlier turns
         uint32_t phase = 0;
         auto full = [&]() { pa_wait(smem_u32(&kv_full[stage]), phase, &abort_flag, a.st); };
         auto next = [&]() {
             if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         };
-        auto scores = [&](int j) {                             // S = Q K^T of step j; the keys are free behind it
-            full();
-            if (j < nt) {
-                tc_fence_after();
-                if (pa_elect()) {
-                    const uint32_t k = pa_desc_k(kv + stage * kStep), to_s = ts + (j & 1) * kPaKeys;
-                    pa_mma_ss<false>(to_s, q, k, idesc_s);
+        for (int turn = 0; turn < turns; ++turn) {
+            const PaShare sh = share_of(turn, false);
+            if (sh.pair < 0) continue;
+            const PaUnit u(a, sh);
+            const int n = u.steps, nt = u.n[t];
+            if (n == 0) continue;
+            auto scores = [&](int j) {                         // S = Q K^T of step j; the keys are free behind it
+                full();
+                if (j < nt) {
+                    tc_fence_after();
+                    if (pa_elect()) {
+                        const int buf = (done + j) & 1;
+                        const uint32_t k = pa_desc_k(kv + stage * kStep), to_s = ts + buf * kPaKeys;
+                        pa_mma_ss<false>(to_s, q, k, idesc_s);
 #pragma unroll
-                    for (int kk = 1; kk < DB * 4; ++kk)
-                        if (kk < d16) pa_mma_ss<true>(to_s, q + (kk >> 2) * (kPaRows / 16) + (kk & 3) * 2, k + (kk >> 2) * (kPaBlock / 16) + (kk & 3) * 2, idesc_s);
-                    tc_commit(smem_u32(&s_full[t * 2 + (j & 1)]));
-                    tc_commit(smem_u32(&kv_empty[stage]));
+                        for (int kk = 1; kk < DB * 4; ++kk)
+                            if (kk < d16) pa_mma_ss<true>(to_s, q + (kk >> 2) * (kPaRows / 16) + (kk & 3) * 2, k + (kk >> 2) * (kPaBlock / 16) + (kk & 3) * 2, idesc_s);
+                        tc_commit(smem_u32(&s_full[t * 2 + buf]));
+                        tc_commit(smem_u32(&kv_empty[stage]));
+                        if (j == nt - 1) tc_commit(smem_u32(&q_empty));
+                    }
+                } else if (lane == 0) {
+                    mbar_arrive(smem_u32(&kv_empty[stage]));   // the other tile's alone
                 }
-            } else if (lane == 0) {
-                mbar_arrive(smem_u32(&kv_empty[stage]));       // the other tile's alone
-            }
-            next();
-        };
-        if (n > 0) pa_wait(smem_u32(&q_full), 0, &abort_flag, a.st);
-        if (n > 0) scores(0);
-        if (n > 1) scores(1);
-        for (int j = 0; j < n; ++j) {
+                next();
+            };
+            // the keys' place comes before the queries, as the copies do
             full();
-            if (j < nt) {
-                const int buf = j & 1;
-                pa_wait(smem_u32(&p_full[t * 2 + buf]), (uint32_t)(j >> 1) & 1u, &abort_flag, a.st);
-                tc_fence_after();
-                if (pa_elect()) {
-                    const uint32_t v = pa_desc_n(kv + stage * kStep), p = ts + buf * kPaKeys;
-                    if (j == 0) pa_mma_ts<false>(to, p, v, idesc_o);
-                    else pa_mma_ts<true>(to, p, v, idesc_o);
+            pa_wait(smem_u32(&q_full), (uint32_t)(queries & 1), &abort_flag, a.st);
+            ++queries;
+            if (nt == 0 && lane == 0) mbar_arrive(smem_u32(&q_empty));
+            scores(0);
+            if (n > 1) scores(1);
+            for (int j = 0; j < n; ++j) {
+                full();
+                if (j < nt) {
+                    const int buf = (done + j) & 1;
+                    if (j == 0) pa_wait(smem_u32(&o_free[t]), (uint32_t)(outputs & 1) ^ 1u, &abort_flag, a.st);
+                    pa_wait(smem_u32(&p_full[t * 2 + buf]), (uint32_t)((done + j) >> 1) & 1u, &abort_flag, a.st);
+                    tc_fence_after();
+                    if (pa_elect()) {
+                        const uint32_t v = pa_desc_n(kv + stage * kStep), p = ts + buf * kPaKeys;
+                        if (j == 0) pa_mma_ts<false>(to, p, v, idesc_o);
+                        else pa_mma_ts<true>(to, p, v, idesc_o);
 #pragma unroll
-                    for (int kk = 1; kk < kPaKeys / 16; ++kk) pa_mma_ts<true>(to, p + kk * 8, v + kk * 128, idesc_o);
-                    tc_commit(smem_u32(&pv_done[t * 2 + buf]));
-                    tc_commit(smem_u32(&kv_empty[stage]));
+                        for (int kk = 1; kk < kPaKeys / 16; ++kk) pa_mma_ts<true>(to, p + kk * 8, v + kk * 128, idesc_o);
+                        tc_commit(smem_u32(&pv_done[t * 2 + buf]));
+                        tc_commit(smem_u32(&kv_empty[stage]));
+                    }
+                } else if (lane == 0) {
+                    mbar_arrive(smem_u32(&kv_empty[stage]));
                 }
-            } else if (lane == 0) {
-                mbar_arrive(smem_u32(&kv_empty[stage]));
+                next();
+                if (j + 2 < n) scores(j + 2);
             }
-            next();
-            if (j + 2 < n) scores(j + 2);
+            done += nt;
+            if (nt > 0) ++outputs;
         }
-    } else if (warp < 8) {
-        const int t = warp >> 2, row = (warp & 3) * 32 + lane, nt = t ? n1 : n0;
+        // the last products are done before the block ends
+        if (done > 0) pa_wait(smem_u32(&pv_done[t * 2 + ((done - 1) & 1)]), (uint32_t)((done - 1) >> 1) & 1u, &abort_flag, a.st);
+    } else {
+        const int t = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = tmem + t * 128 + lanes, to = tmem + 256 + t * 128 + lanes;
-        const int tok0 = (sh.pair * 2 + t) * tile_tokens, tok = tok0 + (row >> a.gp_log2), head = head0 + (row & (a.gp - 1));
+        int done = 0;                                          // steps of this tile in earlier turns
+        for (int turn = 0; turn < turns; ++turn) {
+        const PaShare sh = share_of(turn, false);
+        if (sh.pair < 0) continue;
+        const PaUnit u(a, sh);
+        const int nt = u.n[t], tok0 = u.token0(t), past = u.past, kv_head = u.kv_head;
+        if (tok0 >= sh.Lq) continue;
+        const int tok = tok0 + (row >> a.gp_log2), head = u.head0 + (row & (a.gp - 1));
         const int seen = max(0, min(tok + past + 1, sh.Lk));   // keys that this row sees
         const int all_see = max(0, min(tok0 + past + 1, sh.Lk));
         float m = kNegInf, mc = 0.f;                           // reference, raw and in powers of two
@@ -344,8 +468,8 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
         float s[kPaKeys];
         uint32_t* sr = reinterpret_cast<uint32_t*>(s);
         for (int j = 0; j < nt; ++j) {
-            const int buf = j & 1;
-            pa_wait(smem_u32(&s_full[t * 2 + buf]), (uint32_t)(j >> 1) & 1u, &abort_flag, a.st);
+            const int at_step = done + j, buf = at_step & 1;
+            pa_wait(smem_u32(&s_full[t * 2 + buf]), (uint32_t)(at_step >> 1) & 1u, &abort_flag, a.st);
             __syncwarp();
             tc_fence_after();
             const uint32_t at = ts + buf * kPaKeys;
@@ -371,7 +495,7 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
                 mc = next_c;
                 sum2 = mul2(sum2, pair_of(f, f));
                 if (j > 0) {                                   // O, once the step before is in it
-                    pa_wait(smem_u32(&pv_done[t * 2 + (buf ^ 1)]), (uint32_t)((j - 1) >> 1) & 1u, &abort_flag, a.st);
+                    pa_wait(smem_u32(&pv_done[t * 2 + (buf ^ 1)]), (uint32_t)((at_step - 1) >> 1) & 1u, &abort_flag, a.st);
                     __syncwarp();
                     tc_fence_after();
 #pragma unroll 1
@@ -404,7 +528,8 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
         const float2 sums = halves(sum2);
         const float sum = sums.x + sums.y, inv = sum == 0.f ? 0.f : 1.f / sum;
         if (nt > 0) {
-            pa_wait(smem_u32(&pv_done[t * 2 + ((nt - 1) & 1)]), (uint32_t)((nt - 1) >> 1) & 1u, &abort_flag, a.st);
+            done += nt;
+            pa_wait(smem_u32(&pv_done[t * 2 + ((done - 1) & 1)]), (uint32_t)((done - 1) >> 1) & 1u, &abort_flag, a.st);
             __syncwarp();
             tc_fence_after();
         }
@@ -431,6 +556,11 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
                 if (live && col < a.D) Elem<T>::store8(out + col, x);
             }
         }
+        if (nt > 0) {                                          // the next turn's sums may go there
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&o_free[t]));
+        }
         if (live && a.lse) a.lse[(long long)(sh.q0 + tok) * a.n_q + head] = sum == 0.f ? kNegInf : (mc + log2f(sum)) * 0.69314718055994531f;
         // rows of finite weights whose result is not: values that they do not see may be the reason
         const bool again = live && sum > 0.f && sum < __int_as_float(0x7f800000) && odd != 0.f;
@@ -442,6 +572,7 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
                             static_cast<const T*>(a.k) + (long long)sh.k0 * a.ld_k + (long long)kv_head * a.D,
                             static_cast<const T*>(a.v) + (long long)sh.k0 * a.ld_v + (long long)kv_head * a.D, seen_r, mc_r, inv_r,
                             static_cast<T*>(a.out) + (long long)(sh.q0 + tok_r) * a.ld_out + (long long)head_r * a.D);
+        }
         }
     }
     tc_fence_before();
