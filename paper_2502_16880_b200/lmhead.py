@@ -9,7 +9,9 @@ wrapper that owns the device buffers.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
+import struct
 
 import torch
 
@@ -140,16 +142,16 @@ _SIGNATURES = {
     "coral_lmhead_q4_status": (_i, [_vp, _vp]),
     "coral_lmhead_logits_workspace_bytes": (_i, [ctypes.POINTER(coral_lmhead_logits_args), ctypes.POINTER(ctypes.c_size_t)]),
     "coral_lmhead_logits_process": (_i, [ctypes.POINTER(coral_lmhead_logits_args), _vp, _vp]),
-    "coral_lmhead_qk_rotate": (_i, [ctypes.POINTER(coral_lmhead_qk_args), _vp]),
+    # (argument structures of the attention operators: by reference, or as packed bytes)
+    "coral_lmhead_qk_rotate": (_i, [_vp, _vp]),
     "coral_lmhead_qk_rotate_backward_bytes": (_i, [_i, _i, _i, _i, ctypes.POINTER(ctypes.c_size_t)]),
-    "coral_lmhead_qk_rotate_backward": (_i, [ctypes.POINTER(coral_lmhead_qk_args), _vp, _vp]),
-    "coral_lmhead_prompt_attention": (_i, [ctypes.POINTER(coral_lmhead_prompt_args), _vp, _vp]),
+    "coral_lmhead_qk_rotate_backward": (_i, [_vp, _vp, _vp]),
+    "coral_lmhead_prompt_attention": (_i, [_vp, _vp, _vp]),
     "coral_lmhead_kv4_bytes": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), ctypes.POINTER(ctypes.c_size_t)]),
     "coral_lmhead_kv4_store": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), _vp, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, _i, _vp]),
     "coral_lmhead_kv4_load": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), _vp, _vp, _i, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp]),
-    "coral_lmhead_kv4_attention_bytes": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), ctypes.POINTER(coral_lmhead_kv4_attention_args),
-                                              ctypes.POINTER(ctypes.c_size_t)]),
-    "coral_lmhead_kv4_attention": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), _vp, ctypes.POINTER(coral_lmhead_kv4_attention_args), _vp, _vp]),
+    "coral_lmhead_kv4_attention_bytes": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), _vp, ctypes.POINTER(ctypes.c_size_t)]),
+    "coral_lmhead_kv4_attention": (_i, [ctypes.POINTER(coral_lmhead_kv4_config), _vp, _vp, _vp, _vp]),
     "coral_lmhead_attention_status": (_i, [_vp, _vp]),
     "coral_lmhead_error_string": (ctypes.c_char_p, [_i]),
     "coral_lmhead_destroy": (_i, [_vp]),
@@ -448,7 +450,7 @@ def _op_ptr(name, t, dtype, shape, dev):
 
 def _op_device(t, name) -> int:
     dev = t.get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != torch._C._cuda_getDevice():
         raise ValueError(f"{name} must be on the current CUDA device")
     return dev
 
@@ -664,51 +666,61 @@ def coral_lmhead_logits_process(logits, *, row_seq=None, prompt_tokens=None, pro
 def _heads_ptr(name, t, dtype, shape, dev):
     """Pointer and token distance of rows [T, heads, D] whose tokens may lie apart (a slice of a fused projection)."""
     if t is None:
-        return None, 0
+        return 0, 0
+    if t.dtype is dtype and t.get_device() == dev and t.shape == shape:
+        T, heads, D = shape
+        if t.is_contiguous():
+            return t.data_ptr(), heads * D
+        a, b, c = t.stride()
+        if c == 1 and (b == D or heads == 1) and (a >= heads * D or T == 1):
+            return t.data_ptr(), a if T > 1 else heads * D
+        raise ValueError(f"{name}: the heads of a token must be contiguous and tokens must not overlap")
     if t.get_device() != dev:
         raise ValueError(f"{name} is on {t.device}, not on cuda:{dev}")
-    if t.dtype is not dtype or t.shape != shape:
-        raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    T, heads, D = shape
-    if t.is_contiguous():
-        return t.data_ptr(), heads * D
-    ld = t.stride(0) if T > 1 else heads * D
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != D) or ld < heads * D:
-        raise ValueError(f"{name}: the heads of a token must be contiguous and tokens must not overlap")
-    return t.data_ptr(), ld
+    raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
 
 
-_QK_SIZE = ctypes.sizeof(coral_lmhead_qk_args)
+def _packer(structure):
+    """The structure's fields as struct.pack takes them: filling a ctypes structure costs more than the launch behind it."""
+    code = {ctypes.c_uint32: "I", ctypes.c_int32: "i", ctypes.c_int64: "q", ctypes.c_float: "f", ctypes.c_void_p: "P"}
+    form = struct.Struct("@" + "".join(code[t] for _, t in structure._fields_) + "0P")
+    if form.size != ctypes.sizeof(structure):
+        raise TypeError(f"{structure.__name__} is not laid out as struct packs it")
+    return functools.partial(form.pack, form.size)
 
 
-def _qk_args(q, k, positions, freqs, w_q, w_k, eps, style, like, out_q=None, out_k=None, dout_q=None, dout_k=None, dq=None, dk=None,
-             dw_q=None, dw_k=None):
-    """`like`: the tensors that say how many heads there are."""
-    first = like[0] if like[0] is not None else like[1]
+_pack_qk, _pack_prompt, _pack_kv4 = _packer(coral_lmhead_qk_args), _packer(coral_lmhead_prompt_args), _packer(coral_lmhead_kv4_attention_args)
+
+
+def _qk_sizes(q, k):
+    first = k if q is None else q
     if first is None or first.dim() != 3:
         raise ValueError("queries and keys must be [T, heads, D]")
-    dev, t, f32 = _op_device(first, "q and k"), first.dtype, torch.float32
     T, _, D = first.shape
-    n = [0 if x is None else x.shape[1] for x in like]
-    rows = lambda name, x, i: _heads_ptr(name, x, t, (T, n[i], D), dev)
-    (q_p, ld_q), (k_p, ld_k), (oq, ld_oq), (ok, ld_ok) = rows("q", q, 0), rows("k", k, 1), rows("out_q", out_q, 0), rows("out_k", out_k, 1)
-    (gq, ld_gq), (gk, ld_gk), (dq_p, ld_dq), (dk_p, ld_dk) = rows("dout_q", dout_q, 0), rows("dout_k", dout_k, 1), rows("dq", dq, 0), rows("dk", dk, 1)
-    rot = 0 if freqs is None else 2 * freqs.shape[0]
-    return coral_lmhead_qk_args(
-        _QK_SIZE, _type_of(first), T, n[0], n[1], D, rot, style, eps, ld_q, ld_k, ld_oq, ld_ok, ld_gq, ld_gk, ld_dq, ld_dk, q_p, k_p,
-        _op_ptr("w_q", w_q, t, (D,), dev), _op_ptr("w_k", w_k, t, (D,), dev), _op_ptr("positions", positions, torch.int32, (T,), dev),
-        _op_ptr("freqs", freqs, f32, (rot // 2,), dev), oq, ok, gq, gk, dq_p, dk_p, _op_ptr("dw_q", dw_q, f32, (D,), dev),
-        _op_ptr("dw_k", dw_k, f32, (D,), dev)), dev
+    return first, _op_device(first, "q and k"), T, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], D
 
 
 def coral_lmhead_qk_rotate(q, k, positions, freqs, out_q, out_k, w_q=None, w_k=None, eps=1e-6, style=CORAL_ROPE_HALVES, stream=None):
     """Norm (where w_q, w_k [D] are given) and rotation of queries [T, n_q, D] and keys [T, n_k, D], tokens any distance apart (one of
     the two may be None with its output).  positions int32 [T]; freqs fp32 [rot / 2] (None: no rotation); outputs like q and k, or
     those themselves."""
-    a, dev = _qk_args(q, k, positions, freqs, w_q, w_k, eps, style, (q, k), out_q, out_k)
-    _check((_lib or load_library()).coral_lmhead_qk_rotate(ctypes.byref(a), _op_stream(stream, dev)), "coral_lmhead_qk_rotate")
+    first, dev, T, n_q, n_k, D = _qk_sizes(q, k)
+    t, half = first.dtype, 0 if freqs is None else freqs.shape[0]
+    sq, sk, w = (T, n_q, D), (T, n_k, D), (D,)
+    q_p, ld_q = _heads_ptr("q", q, t, sq, dev)
+    k_p, ld_k = _heads_ptr("k", k, t, sk, dev)
+    oq, ld_oq = _heads_ptr("out_q", out_q, t, sq, dev)
+    ok, ld_ok = _heads_ptr("out_k", out_k, t, sk, dev)
+    a = _pack_qk(_type_of(first), T, n_q, n_k, D, 2 * half, style, eps, ld_q, ld_k, ld_oq, ld_ok, 0, 0, 0, 0, q_p, k_p,
+                 _op_ptr("w_q", w_q, t, w, dev) or 0, _op_ptr("w_k", w_k, t, w, dev) or 0,
+                 _op_ptr("positions", positions, torch.int32, (T,), dev) or 0, _op_ptr("freqs", freqs, torch.float32, (half,), dev) or 0,
+                 oq, ok, 0, 0, 0, 0, 0, 0)
+    rc = (_lib or load_library()).coral_lmhead_qk_rotate(a, _op_stream(stream, dev))
+    if rc:
+        _check(rc, "coral_lmhead_qk_rotate")
 
 
+@functools.lru_cache(maxsize=256)
 def coral_lmhead_qk_rotate_backward_bytes(T: int, n_q: int, n_k: int, D: int) -> int:
     b = ctypes.c_size_t(0)
     _check((_lib or load_library()).coral_lmhead_qk_rotate_backward_bytes(T, n_q, n_k, D, ctypes.byref(b)), "coral_lmhead_qk_rotate_backward_bytes")
@@ -719,14 +731,24 @@ def coral_lmhead_qk_rotate_backward(q, k, positions, freqs, dout_q, dout_k, dq, 
                                     dw_q=None, dw_k=None, workspace=None, stream=None):
     """Gradient of coral_lmhead_qk_rotate: dq, dk like q and k, dw_q, dw_k fp32 [D] (None: not wanted).  q (k) is needed where w_q (w_k)
     is.  workspace: CUDA uint8 tensor of coral_lmhead_qk_rotate_backward_bytes, needed where dw_q or dw_k is."""
-    a, dev = _qk_args(q, k, positions, freqs, w_q, w_k, eps, style, (dout_q, dout_k), None, None, dout_q, dout_k, dq, dk, dw_q, dw_k)
-    if workspace is not None and workspace.numel() < coral_lmhead_qk_rotate_backward_bytes(a.T, a.n_q, a.n_k, a.D):
+    first, dev, T, n_q, n_k, D = _qk_sizes(dout_q, dout_k)
+    t, f32, half = first.dtype, torch.float32, 0 if freqs is None else freqs.shape[0]
+    sq, sk, w = (T, n_q, D), (T, n_k, D), (D,)
+    q_p, ld_q = _heads_ptr("q", q, t, sq, dev)
+    k_p, ld_k = _heads_ptr("k", k, t, sk, dev)
+    gq, ld_gq = _heads_ptr("dout_q", dout_q, t, sq, dev)
+    gk, ld_gk = _heads_ptr("dout_k", dout_k, t, sk, dev)
+    dq_p, ld_dq = _heads_ptr("dq", dq, t, sq, dev)
+    dk_p, ld_dk = _heads_ptr("dk", dk, t, sk, dev)
+    a = _pack_qk(_type_of(first), T, n_q, n_k, D, 2 * half, style, eps, ld_q, ld_k, 0, 0, ld_gq, ld_gk, ld_dq, ld_dk, q_p, k_p,
+                 _op_ptr("w_q", w_q, t, w, dev) or 0, _op_ptr("w_k", w_k, t, w, dev) or 0,
+                 _op_ptr("positions", positions, torch.int32, (T,), dev) or 0, _op_ptr("freqs", freqs, f32, (half,), dev) or 0,
+                 0, 0, gq, gk, dq_p, dk_p, _op_ptr("dw_q", dw_q, f32, w, dev) or 0, _op_ptr("dw_k", dw_k, f32, w, dev) or 0)
+    if workspace is not None and workspace.numel() < coral_lmhead_qk_rotate_backward_bytes(T, n_q, n_k, D):
         raise ValueError("workspace is smaller than coral_lmhead_qk_rotate_backward_bytes(T, n_q, n_k, D)")
-    _check((_lib or load_library()).coral_lmhead_qk_rotate_backward(
-        ctypes.byref(a), _op_ptr("workspace", workspace, torch.uint8, None, dev), _op_stream(stream, dev)), "coral_lmhead_qk_rotate_backward")
-
-
-_PROMPT_SIZE = ctypes.sizeof(coral_lmhead_prompt_args)
+    rc = (_lib or load_library()).coral_lmhead_qk_rotate_backward(a, _op_ptr("workspace", workspace, torch.uint8, None, dev), _op_stream(stream, dev))
+    if rc:
+        _check(rc, "coral_lmhead_qk_rotate_backward")
 
 
 def coral_lmhead_prompt_attention(q, k, v, q_offsets, out, k_offsets=None, scale=None, out_lse=None, workspace=None, stream=None):
@@ -738,24 +760,27 @@ def coral_lmhead_prompt_attention(q, k, v, q_offsets, out, k_offsets=None, scale
     dev = _op_device(q, "q")
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q and k must be [tokens, heads, D]")
-    t = q.dtype
-    (T, n_q, D), (Tk, n_k, _) = q.shape, k.shape
-    kv = (Tk, n_k, D)
-    (q_p, ld_q), (k_p, ld_k), (v_p, ld_v), (o_p, ld_o) = (_heads_ptr("q", q, t, (T, n_q, D), dev), _heads_ptr("k", k, t, kv, dev),
-                                                          _heads_ptr("v", v, t, kv, dev), _heads_ptr("out", out, t, (T, n_q, D), dev))
-    n_seq = q_offsets.shape[0] - 1
-    a = coral_lmhead_prompt_args(
-        _PROMPT_SIZE, _type_of(q), n_seq, T, Tk, n_q, n_k, D, D ** -0.5 if scale is None else scale, ld_q, ld_k, ld_v, ld_o, q_p, k_p, v_p,
-        _op_ptr("q_offsets", q_offsets, torch.int64, (n_seq + 1,), dev), _op_ptr("k_offsets", k_offsets, torch.int64, (n_seq + 1,), dev), o_p,
-        _op_ptr("out_lse", out_lse, torch.float32, (T, n_q), dev))
+    t, sq = q.dtype, q.shape
+    T, n_q, D = sq
+    Tk, n_k, _ = k.shape
+    sk, so = (Tk, n_k, D), q_offsets.shape
+    q_p, ld_q = _heads_ptr("q", q, t, sq, dev)
+    k_p, ld_k = _heads_ptr("k", k, t, sk, dev)
+    v_p, ld_v = _heads_ptr("v", v, t, sk, dev)
+    o_p, ld_o = _heads_ptr("out", out, t, sq, dev)
+    n_seq = so[0] - 1
+    a = _pack_prompt(_type_of(q), n_seq, T, Tk, n_q, n_k, D, D ** -0.5 if scale is None else scale, ld_q, ld_k, ld_v, ld_o, q_p, k_p, v_p,
+                     _op_ptr("q_offsets", q_offsets, torch.int64, (n_seq + 1,), dev) or 0, _op_ptr("k_offsets", k_offsets, torch.int64, so, dev) or 0,
+                     o_p, _op_ptr("out_lse", out_lse, torch.float32, (T, n_q), dev) or 0)
     if n_seq == 0 or T == 0:
         return workspace
     if workspace is None:
         workspace = _op_scratch(CORAL_PROMPT_WORKSPACE_BYTES, q.device, stream)
     elif workspace.numel() < CORAL_PROMPT_WORKSPACE_BYTES:
         raise ValueError("workspace is smaller than CORAL_PROMPT_WORKSPACE_BYTES")
-    _check((_lib or load_library()).coral_lmhead_prompt_attention(
-        ctypes.byref(a), _op_ptr("workspace", workspace, torch.uint8, None, dev), _op_stream(stream, dev)), "coral_lmhead_prompt_attention")
+    rc = (_lib or load_library()).coral_lmhead_prompt_attention(a, _op_ptr("workspace", workspace, torch.uint8, None, dev), _op_stream(stream, dev))
+    if rc:
+        _check(rc, "coral_lmhead_prompt_attention")
     return workspace
 
 
@@ -770,7 +795,7 @@ def coral_lmhead_kv4_bytes(cfg) -> int:
 
 
 def _kv4_cache_ptr(cfg, cache, dev):
-    if cache.numel() < coral_lmhead_kv4_bytes(cfg):
+    if cache.numel() < cfg.n_pages * cfg.page * cfg.n_heads * (cfg.D + 8 * cfg.D // max(cfg.group, 1)):
         raise ValueError("cache is smaller than coral_lmhead_kv4_bytes(cfg)")
     return _op_ptr("cache", cache, torch.uint8, None, dev)
 
@@ -782,51 +807,48 @@ def _kv4_dtype(cfg):
 def coral_lmhead_kv4_store(cfg, cache, k, v, slots, stream=None) -> None:
     """Tokens k, v [T, n_heads, D] (any distance apart) to slots int64 [T] of the cache (uint8, coral_lmhead_kv4_bytes(cfg)); tokens
     whose slot lies outside the cache (-1) are passed over."""
-    dev, dt = _op_device(cache, "cache"), _kv4_dtype(cfg)
-    T = slots.shape[0]
+    dev, dt, T = _op_device(cache, "cache"), _kv4_dtype(cfg), slots.shape[0]
     shape = (T, cfg.n_heads, cfg.D)
-    (k_p, ld_k), (v_p, ld_v) = _heads_ptr("k", k, dt, shape, dev), _heads_ptr("v", v, dt, shape, dev)
+    k_p, ld_k = _heads_ptr("k", k, dt, shape, dev)
+    v_p, ld_v = _heads_ptr("v", v, dt, shape, dev)
     c_p, s_p = _kv4_cache_ptr(cfg, cache, dev), _op_ptr("slots", slots, torch.int64, (T,), dev)
     if T == 0:
         return
-    _check((_lib or load_library()).coral_lmhead_kv4_store(ctypes.byref(cfg), c_p, k_p, ld_k, v_p, ld_v, s_p, T, _op_stream(stream, dev)),
-           "coral_lmhead_kv4_store")
+    rc = (_lib or load_library()).coral_lmhead_kv4_store(cfg, c_p, k_p, ld_k, v_p, ld_v, s_p, T, _op_stream(stream, dev))
+    if rc:
+        _check(rc, "coral_lmhead_kv4_store")
 
 
 def coral_lmhead_kv4_load(cfg, cache, slots, out_k=None, out_v=None, stream=None) -> None:
     """What the cache holds at slots int64 [T], into out_k, out_v [T, n_heads, D] of the cache's type (one may be None); slots outside the
     cache give zeros."""
-    dev, dt = _op_device(cache, "cache"), _kv4_dtype(cfg)
-    T = slots.shape[0]
+    dev, dt, T = _op_device(cache, "cache"), _kv4_dtype(cfg), slots.shape[0]
     shape = (T, cfg.n_heads, cfg.D)
-    (k_p, ld_k), (v_p, ld_v) = _heads_ptr("out_k", out_k, dt, shape, dev), _heads_ptr("out_v", out_v, dt, shape, dev)
+    k_p, ld_k = _heads_ptr("out_k", out_k, dt, shape, dev)
+    v_p, ld_v = _heads_ptr("out_v", out_v, dt, shape, dev)
     c_p, s_p = _kv4_cache_ptr(cfg, cache, dev), _op_ptr("slots", slots, torch.int64, (T,), dev)
     if T == 0:
         return
-    _check((_lib or load_library()).coral_lmhead_kv4_load(ctypes.byref(cfg), c_p, s_p, T, k_p, ld_k, v_p, ld_v, _op_stream(stream, dev)),
-           "coral_lmhead_kv4_load")
-
-
-def _kv4_attention_args(cfg, q, table, lens, out, max_q, q_offsets, tree_mask, scale, out_lse, dev):
-    dt, n_seq = _kv4_dtype(cfg), lens.shape[0]
-    if q.dim() != 3 or table.dim() != 2:
-        raise ValueError("q must be [rows, n_q, D] and table [n_seq, width]")
-    rows, n_q, _ = q.shape
-    shape = (rows, n_q, cfg.D)
-    width = table.shape[1]
-    (q_p, ld_q), (o_p, ld_o), (t_p, ld_t) = _heads_ptr("q", q, dt, shape, dev), _heads_ptr("out", out, dt, shape, dev), _rows_ptr(
-        "table", table, torch.int32, (n_seq, width), dev)
-    return coral_lmhead_kv4_attention_args(
-        ctypes.sizeof(coral_lmhead_kv4_attention_args), n_seq, rows, max_q, n_q, width, cfg.D ** -0.5 if scale is None else scale, ld_q, ld_o, ld_t,
-        q_p, t_p, _op_ptr("lens", lens, torch.int32, (n_seq,), dev), _op_ptr("q_offsets", q_offsets, torch.int64, (n_seq + 1,), dev),
-        _op_ptr("tree_mask", tree_mask, torch.int64, (rows,), dev), o_p, _op_ptr("out_lse", out_lse, torch.float32, (rows, n_q), dev))
+    rc = (_lib or load_library()).coral_lmhead_kv4_load(cfg, c_p, s_p, T, k_p, ld_k, v_p, ld_v, _op_stream(stream, dev))
+    if rc:
+        _check(rc, "coral_lmhead_kv4_load")
 
 
 def coral_lmhead_kv4_attention_bytes(cfg, args) -> int:
+    """args: a coral_lmhead_kv4_attention_args."""
     b = ctypes.c_size_t(0)
     _check((_lib or load_library()).coral_lmhead_kv4_attention_bytes(ctypes.byref(cfg), ctypes.byref(args), ctypes.byref(b)),
            "coral_lmhead_kv4_attention_bytes")
     return b.value
+
+
+@functools.lru_cache(maxsize=256)
+def _kv4_scratch_bytes(n_pages, page, n_heads, D, group, dtype, n_seq, n_rows, max_q, n_q, width, ragged):
+    """coral_lmhead_kv4_attention_bytes by sizes (it reads nothing else of its arguments; any pointer does)."""
+    P = 256
+    a = coral_lmhead_kv4_attention_args(ctypes.sizeof(coral_lmhead_kv4_attention_args), n_seq, n_rows, max_q, n_q, width, 1.0, n_q * D, n_q * D, width, P, P, P,
+                                        P if ragged else None, None, P, None)
+    return coral_lmhead_kv4_attention_bytes(make_kv4_config(n_pages, page, n_heads, D, group, dtype), a)
 
 
 def coral_lmhead_kv4_attention(cfg, cache, q, table, lens, out, max_q=1, q_offsets=None, tree_mask=None, scale=None, out_lse=None, workspace=None,
@@ -836,19 +858,28 @@ def coral_lmhead_kv4_attention(cfg, cache, q, table, lens, out, max_q=1, q_offse
     table[s] (int32 [n_seq, width]).  tree_mask int64 [rows]: bit b lets a row see the sequence's b-th query token (None: causal).
     scale: 1 / sqrt(D) if None.  out like q; out_lse fp32 [rows, n_q].  Returns the scratch of the call, which holds the word that
     coral_lmhead_attention_status reads (from torch's allocator if workspace is None)."""
-    dev = _op_device(cache, "cache")
-    a = _kv4_attention_args(cfg, q, table, lens, out, max_q, q_offsets, tree_mask, scale, out_lse, dev)
+    dev, dt, D = _op_device(cache, "cache"), _kv4_dtype(cfg), cfg.D
+    if q.dim() != 3 or table.dim() != 2:
+        raise ValueError("q must be [rows, n_q, D] and table [n_seq, width]")
+    n_seq, width, (rows, n_q, _) = lens.shape[0], table.shape[1], q.shape
+    shape = (rows, n_q, D)
+    q_p, ld_q = _heads_ptr("q", q, dt, shape, dev)
+    o_p, ld_o = _heads_ptr("out", out, dt, shape, dev)
+    t_p, ld_t = _rows_ptr("table", table, torch.int32, (n_seq, width), dev)
+    a = _pack_kv4(n_seq, rows, max_q, n_q, width, D ** -0.5 if scale is None else scale, ld_q, ld_o, ld_t, q_p, t_p,
+                  _op_ptr("lens", lens, torch.int32, (n_seq,), dev) or 0, _op_ptr("q_offsets", q_offsets, torch.int64, (n_seq + 1,), dev) or 0,
+                  _op_ptr("tree_mask", tree_mask, torch.int64, (rows,), dev) or 0, o_p, _op_ptr("out_lse", out_lse, torch.float32, (rows, n_q), dev) or 0)
     c_p = _kv4_cache_ptr(cfg, cache, dev)
-    if a.n_seq == 0 or a.n_rows == 0:
+    if n_seq == 0 or rows == 0:
         return workspace
-    n = coral_lmhead_kv4_attention_bytes(cfg, a)
+    n = _kv4_scratch_bytes(cfg.n_pages, cfg.page, cfg.n_heads, D, cfg.group, dt, n_seq, rows, max_q, n_q, width, q_offsets is not None)
     if workspace is None:
         workspace = _op_scratch(n, cache.device, stream)
     elif workspace.numel() < n:
         raise ValueError("workspace is smaller than coral_lmhead_kv4_attention_bytes(cfg, args)")
-    _check((_lib or load_library()).coral_lmhead_kv4_attention(
-        ctypes.byref(cfg), c_p, ctypes.byref(a), _op_ptr("workspace", workspace, torch.uint8, None, dev), _op_stream(stream, dev)),
-        "coral_lmhead_kv4_attention")
+    rc = (_lib or load_library()).coral_lmhead_kv4_attention(cfg, c_p, a, _op_ptr("workspace", workspace, torch.uint8, None, dev), _op_stream(stream, dev))
+    if rc:
+        _check(rc, "coral_lmhead_kv4_attention")
     return workspace
 
 
