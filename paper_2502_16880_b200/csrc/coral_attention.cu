@@ -113,6 +113,7 @@ Kv4Cache kv4_cache(const coral_lmhead_kv4_config* c, const void* base) {
     k.base = static_cast<unsigned char*>(const_cast<void*>(base));
     k.slots = c->n_pages * c->page;
     k.n_k = c->n_heads; k.page = c->page; k.groups = c->D / c->group;
+    k.share = c->group == 32 ? 2 : c->group == 64 ? 3 : 4;
     k.heads = Divide(c->n_heads);
     k.subs = Divide(c->page / kKv4Block);
     return k;

@@ -39,13 +39,13 @@ struct Divide {
 struct Kv4Cache {
     unsigned char* base;
     int slots;                                      // pages * page
-    int n_k, page, groups;
+    int n_k, page, groups, share;                   // share: log2 of the threads, of eight columns each, that have a group
     Divide heads, subs;                             // by n_k, and by the blocks of a page
     __host__ __device__ int block_bytes(int D) const { return kKv4Block * D + 128 * groups; }
     // start of the block that holds slot `slot` of head `head`
     __device__ __forceinline__ unsigned char* block(int slot, int head, int D) const {
         const int sub = slot / kKv4Block, page_at = subs(sub), per = (int)subs.d;
-        return base + ((long long)(page_at * n_k + head) * per + (sub - page_at * per)) * block_bytes(D);
+        return base + (long long)((page_at * n_k + head) * per + (sub - page_at * per)) * block_bytes(D);
     }
 };
 
@@ -116,8 +116,8 @@ struct Kv4Place {
     }
     __device__ __forceinline__ uint32_t get(unsigned char* blk) const { return is_v ? values(blk)[0] | (uint32_t)values(blk)[2] << 16 : *keys(blk); }
     // its group's (step, low)
-    __device__ __forceinline__ uint32_t* pair(unsigned char* blk, int groups) const {
-        return reinterpret_cast<uint32_t*>(blk + 16 * D) + ((is_v ? groups : 0) + l / (L / groups)) * 16 + (slot & 15);
+    __device__ __forceinline__ uint32_t* pair(unsigned char* blk, const Kv4Cache& c) const {
+        return reinterpret_cast<uint32_t*>(blk + 16 * D) + ((is_v ? c.groups : 0) + (l >> c.share)) * 16 + (slot & 15);
     }
 };
 
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kKv4RowThreads) kv4_store_kernel(const __grid_
     if (p.on) *reinterpret_cast<uint4*>(raw) = *reinterpret_cast<const uint4*>(p.template columns<T>(a));
     const Two* r2 = reinterpret_cast<const Two*>(raw);
     Two ends = Range::ends(Range::min2(Range::min2(r2[0], r2[1]), Range::min2(r2[2], r2[3])), Range::max2(Range::max2(r2[0], r2[1]), Range::max2(r2[2], r2[3])));
-    const int per = L / c.groups;                   // threads of a group
+    const int per = 1 << c.share;                   // threads of a group
 #pragma unroll
     for (int o = 1; o < L; o <<= 1)
         if (o < per) {
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kKv4RowThreads) kv4_store_kernel(const __grid_
     if (!p.on) return;
     unsigned char* blk = c.block(p.slot, p.head, D);
     p.put(blk, word);
-    if ((p.l & (per - 1)) == 0) *p.pair(blk, c.groups) = step_bits | kv4_bits<T>(lh.x + bad) << 16;
+    if ((p.l & (per - 1)) == 0) *p.pair(blk, c) = step_bits | kv4_bits<T>(lh.x + bad) << 16;
 }
 
 template <typename T, int D>
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kKv4RowThreads) kv4_load_kernel(const __grid_c
     if (p.on) {
         unsigned char* blk = c.block(p.slot, p.head, D);
         word = p.get(blk);
-        pair = *p.pair(blk, c.groups);
+        pair = *p.pair(blk, c);
     }
     if (p.is_v) word = nibbles_transposed(word, p.l);
     if (p.row >= a.rows) return;
