@@ -6,7 +6,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "kv4.cuh"
+#include "kv4_tc.cuh"
 #include "launch.cuh"
 #include "prompt_attention.cuh"
 #include "qk_rotate.cuh"
@@ -129,8 +129,11 @@ int launch_kv4_rows(const coral_lmhead_kv4_config* c, bool store, const void* ca
     return launch_pdl(f, grid, dim3(kKv4RowThreads), 0, st, kv4_cache(c, cache), r) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
 }
 
+// From how many rows of a key head on (query tokens times heads of its group) the tensor-core kernel takes a call.
+constexpr long long kKv4ManyFrom = 33;
+
 struct Kv4Plan {
-    int nr, row_groups, row_blocks, splits;
+    int nr, row_groups, row_blocks, splits;        // nr 0: kv4_many_kernel
     long long units;                               // blocks without the split
     size_t ml, o, bytes;                           // offsets in the workspace and its size
 };
@@ -150,9 +153,12 @@ bool kv4_attention_ok(const coral_lmhead_kv4_config* c, const coral_lmhead_kv4_a
 Kv4Plan kv4_plan(const coral_lmhead_kv4_config* c, const coral_lmhead_kv4_attention_args* a) {
     Kv4Plan p{};
     const long long rows = (long long)a->max_q * (a->n_q / c->n_heads);
-    p.nr = rows <= 8 ? 1 : 2;
-    for (p.row_groups = 1; p.row_groups < kKv4Warps && p.row_groups * 8 * p.nr < rows; p.row_groups *= 2) {}
-    p.row_blocks = (int)((rows - 1) / (p.row_groups * 8 * p.nr) + 1);
+    p.nr = rows <= 8 ? 1 : rows < kKv4ManyFrom ? 2 : 0;
+    p.row_groups = 1;
+    if (p.nr)
+        for (; p.row_groups < kKv4Warps && p.row_groups * 8 * p.nr < rows; p.row_groups *= 2) {}
+    const int per_block = p.nr ? p.row_groups * 8 * p.nr : 256;
+    p.row_blocks = (int)((rows - 1) / per_block + 1);
     p.units = (long long)a->n_seq * c->n_heads * p.row_blocks;
     // The number of parts whose rounds of resident blocks take the least, a block counted as its tokens plus 512 for what it begins and
     // ends with (64 sequences of up to 4096 tokens, 256 blocks unsplit: 58 us in 5 parts, 43 in one).  A part has a span at least.
@@ -189,12 +195,20 @@ cudaError_t launch_kv4(Kv4Args k, const Kv4Plan& p, cudaStream_t st) {
     return launch_pdl(kv4_attention_kernel<T, D, NG, NR>, dim3((unsigned)(p.units * p.splits)), dim3(kKv4Threads), smem, st, k);
 }
 
+template <typename T, int D, int NG>
+cudaError_t launch_kv4_rows_by(const Kv4Args& k, const Kv4Plan& p, cudaStream_t st) {
+    if (p.nr) return p.nr == 1 ? launch_kv4<T, D, NG, 1>(k, p, st) : launch_kv4<T, D, NG, 2>(k, p, st);
+    constexpr size_t smem = kt_smem_bytes<D, NG>();
+    if (!allow_smem(kv4_many_kernel<T, D, NG>, smem)) return cudaErrorUnknown;
+    return launch_pdl(kv4_many_kernel<T, D, NG>, dim3((unsigned)(p.units * p.splits)), dim3(kKtThreads), smem, st, k);
+}
+
 template <typename T, int D>
 int launch_kv4_groups(const Kv4Args& k, const Kv4Plan& p, cudaStream_t st) {
     cudaError_t e = cudaErrorUnknown;
-    if (k.c.groups == 1) e = p.nr == 1 ? launch_kv4<T, D, 1, 1>(k, p, st) : launch_kv4<T, D, 1, 2>(k, p, st);
-    else if (k.c.groups == 2) e = p.nr == 1 ? launch_kv4<T, D, 2, 1>(k, p, st) : launch_kv4<T, D, 2, 2>(k, p, st);
-    else if constexpr (D == 128) e = p.nr == 1 ? launch_kv4<T, D, 4, 1>(k, p, st) : launch_kv4<T, D, 4, 2>(k, p, st);
+    if (k.c.groups == 1) e = launch_kv4_rows_by<T, D, 1>(k, p, st);
+    else if (k.c.groups == 2) e = launch_kv4_rows_by<T, D, 2>(k, p, st);
+    else if constexpr (D == 128) e = launch_kv4_rows_by<T, D, 4>(k, p, st);
     if (e != cudaSuccess) return CORAL_ERR_CUDA;
     if (p.splits == 1) return CORAL_OK;
     const long long rows = (long long)k.n_seq * k.max_q * k.n_q;

@@ -1,0 +1,535 @@
+// Attention of many rows (the nodes of draft trees, times the heads of a group) over the 4-bit cache, on the 5th-generation tensor cores: the
+// products of prompt_attention.cuh, two tiles of 128 rows a block, with keys and values unpacked by four warps instead of copied.
+//   * a warp brings the packed blocks of 64 tokens a step into a ring of their own, one bulk copy each,
+//   * four warps turn them into fp16 tiles, low + step code, each token times a power of two that brings its largest value to
+//     2^14..2^15; the powers, exact, come back in the scores (kf) and in the weights (vf), so a value is rounded once, to 2^-12 of itself,
+//   * a thread of the softmax has a row: S kf c - m in powers of two, P vf to fp16.  The reference m holds the largest vf so far as well,
+//     so that P vf is at most 2^8 whatever the values' size.
+// Columns lie in another order than in memory: 0 4 1 5 2 6 3 7 within eight (queries and keys alike, for the sums it is all one), and
+// place by place for the values (column 8 i + n at n D / 8 + ...), which the outputs undo.
+// What bounds it: see kv4_many_from in the host code for both sides' times.
+#pragma once
+#include "kv4.cuh"
+#include "prompt_attention.cuh"
+
+namespace coral {
+
+constexpr int kKtThreads = 16 * 32;                // warps 0..7 softmax, 8 and 9 MMAs of a tile each, 10 copies, 12..15 unpacking
+constexpr int kKtRaw = 4;                          // steps of packed tokens in flight
+constexpr int kKtBlocks = kPaKeys / kKv4Block;     // blocks of 16 tokens a step
+constexpr int kKtFactors = 8;                      // steps whose factors are kept
+constexpr int kKtPresent = 16;
+template <int D> constexpr int kKtStages = D == 128 ? 7 : 10;
+template <int D, int NG> constexpr size_t kt_smem_bytes() {
+    return 1024 + (size_t)2 * 128 * D * 2 + (size_t)kKtStages<D> * kPaKeys * D * 2 + (size_t)kKtRaw * kKtBlocks * (kKv4Block * D + 128 * NG) + kKtFactors * kPaKeys * 8;
+}
+
+// What to multiply a token by, and back: the power of two that brings the largest of |low|, |low + 15 step| to 2^14..2^15.
+struct KtPower {
+    float up, back;
+    template <typename T, int NG>
+    static __device__ __forceinline__ KtPower of(const uint32_t (&pairs)[NG]) {
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            const float2 p = kv4_pair<T>(pairs[i]);
+            top = fmaxf(top, fmaxf(fabsf(p.y), fabsf(fmaf(15.f, p.x, p.y))));
+        }
+        const int e = min(max((int)(__float_as_uint(top) >> 23), 16), 254);
+        return KtPower{__uint_as_float((uint32_t)(268 - e) << 23), __uint_as_float((uint32_t)(e - 14) << 23)};
+    }
+};
+__device__ __forceinline__ uint32_t kt_half2(float lo, float hi) { return half_pair(lo, hi); }
+// A word's eight codes as values, pairs (0,4), (1,5), (2,6), (3,7): step and low as fp16 pairs, one rounding.
+__device__ __forceinline__ uint4 kt_values(uint32_t w, uint32_t step, uint32_t low) {
+    uint32_t r[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t bits = ((k < 2 ? w : w >> 8) & (k & 1 ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;    // 1024 + code, or + 16 code
+        uint32_t code;
+        if (k & 1) asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(code) : "r"(bits), "r"(0x2c002c00u), "r"(0xd400d400u));     // / 16 - 64
+        else asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(code) : "r"(bits), "r"(0x64006400u));
+        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r[k]) : "r"(code), "r"(step), "r"(low));
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+// Where chunk `chunk` (eight columns) of row `row` lies in a tile of `rows` rows, 64 columns a part, 128-byte swizzle.
+__device__ __forceinline__ uint32_t kt_chunk(int row, int chunk, int rows) { return (chunk >> 3) * rows * 128 + row * 128 + ((chunk ^ row) & 7) * 16; }
+
+// A row again, by a warp, from the packed tokens it sees (see prompt_attention.cuh); four columns a lane.
+template <typename T, int D, int NG>
+__device__ __noinline__ void kt_row_again(const Kv4Args& a, const int32_t* table, int head, const T* q, int from, int len, int past, int node,
+                                          unsigned long long tree, float m, float inv, float* acc) {
+    const int lane = threadIdx.x & 31;
+    constexpr int N = D / 32;
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] = 0.f;
+    for (int j0 = from; j0 < len; j0 += 32) {
+        const int j = j0 + lane, at = j - past;
+        long long block = -1;
+        if (j < len) {
+            const int sub = j / kKv4Block, per = (int)a.c.subs.d, page_at = a.c.subs(sub), page = __ldg(table + page_at);
+            if (page >= 0 && page < a.n_pages) block = (long long)((page * a.c.n_k + head) * per + sub - page_at * per) * (kKv4Block * D + 128 * NG);
+        }
+        const bool see = block >= 0 && (at < 0 || (a.tree ? at < kKv4MaxTree && tree >> at & 1ull : at <= node));
+        float p = 0.f;
+        if (see) {
+            const unsigned char* blk = a.c.base + block;
+            float s = 0.f;
+            for (int c = 0; c < D; ++c) {
+                const float2 pr = kv4_pair<T>(reinterpret_cast<const uint32_t*>(blk + 16 * D)[c * NG / D * 16 + (j & 15)]);
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(blk + ((j & 15) * 4 + (c >> 3 & 3)) * (D / 8) + 4 * (c >> 5));
+                s = fmaf(Elem<T>::up(q[c]), fmaf((float)(w >> (4 * (c & 7)) & 15u), pr.x, pr.y), s);
+            }
+            p = exp2_fast(s * a.scale2 - m);
+        }
+        for (uint32_t todo = __ballot_sync(0xffffffffu, see); todo; todo &= todo - 1) {
+            const int i = __ffs(todo) - 1, t = (j0 + i) & 15;
+            const float w = __shfl_sync(0xffffffffu, p, i);
+            const unsigned char* blk = a.c.base + __shfl_sync(0xffffffffu, block, i);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const int c = lane * N + e, n = c & 7, k = c >> 3;
+                const float2 pr = kv4_pair<T>(reinterpret_cast<const uint32_t*>(blk + 16 * D)[(NG + c * NG / D) * 16 + t]);
+                const uint16_t piece = reinterpret_cast<const uint16_t*>(blk + 8 * D + (t >> 3) * (4 * D) + (n * 4 + ((t & 7) >> 1)) * (D / 8) + 4 * (k >> 2))[t & 1];
+                acc[e] = fmaf(w, fmaf((float)(piece >> (4 * (k & 3)) & 15u), pr.x, pr.y), acc[e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] *= inv;
+}
+
+template <typename T, int D, int NG>
+__global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_constant__ Kv4Args a) {
+    constexpr int STAGES = kKtStages<D>, kTile = 128 * D * 2, kStep = kPaKeys * D * 2, kBytes = kKv4Block * D + 128 * NG, W = D / 32, DB = D / 64;
+    extern __shared__ unsigned char kt_smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(kt_smem_raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char *s_kv = smem + 2 * kTile, *s_raw = s_kv + STAGES * kStep;
+    float* s_fac = reinterpret_cast<float*>(s_raw + kKtRaw * kKtBlocks * kBytes);           // [step][keys, values][token]
+    __shared__ __align__(8) uint64_t q_full, kv_full[STAGES], kv_empty[STAGES], s_full[4], p_full[4], pv_done[4];
+    __shared__ __align__(8) uint64_t raw_full[kKtRaw], raw_empty[kKtRaw], fac_full[kKtFactors];
+    __shared__ uint32_t present[kKtPresent];
+    __shared__ __align__(16) float s_top[kKtFactors][4];
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&q_full), 8);
+        for (int i = 0; i < STAGES; ++i) {
+            mbar_init(smem_u32(&kv_full[i]), 4);
+            mbar_init(smem_u32(&kv_empty[i]), 2);
+        }
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(smem_u32(&s_full[i]), 1);
+            mbar_init(smem_u32(&p_full[i]), 4);
+            mbar_init(smem_u32(&pv_done[i]), 1);
+        }
+        for (int i = 0; i < kKtRaw; ++i) {
+            mbar_init(smem_u32(&raw_full[i]), 1);
+            mbar_init(smem_u32(&raw_empty[i]), 4);
+        }
+        for (int i = 0; i < kKtFactors; ++i) mbar_init(smem_u32(&fac_full[i]), 4);
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+    pdl_wait();
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.st->status = 0;      // a wait would have to fail millions of polls before this
+
+    unsigned unit = blockIdx.x;
+    const int split = unit % a.splits;
+    unit /= a.splits;
+    const int row_block = unit % a.row_blocks;
+    unit /= a.row_blocks;
+    const int head = unit % a.c.n_k, seq = unit / a.c.n_k;
+    int q0, n_q;
+    kv4_rows_of(a, seq, &q0, &n_q);
+    const int rows = min(n_q, a.max_q) * a.G, row0 = row_block * 256;
+    if (row0 >= rows) return;
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const int len = (int)max(0LL, min((long long)a.lens[seq], min((long long)a.width * a.c.page, 0x7fff0000LL)));
+    const int spans = (len + kKv4SpanBlocks * kKv4Block - 1) / (kKv4SpanBlocks * kKv4Block), per = (spans + a.splits - 1) / a.splits;
+    constexpr int kPer = kKv4SpanBlocks / kKtBlocks;               // steps of a span
+    const int step0 = min(split * per, spans) * kPer, steps = min(min(min(split * per, spans) + per, spans) * kPer, (len + kPaKeys - 1) / kPaKeys) - step0;
+    const int past = len - n_q, open = past + (a.tree ? 0 : 1);    // every row sees the tokens before `open`
+    const int n0 = max(steps, 0), n1 = rows - row0 > 128 ? n0 : 0, n = n0;
+    const int32_t* table = a.table + seq * a.ld_table;
+
+    if (warp == 10) {
+        int place = -1;
+        for (int j = 0; j < n; ++j) {
+            // where the blocks of eight steps lie in the cache, one a lane (-1: none)
+            if (j % 8 == 0) {
+                const int sub = (step0 + j) * kKtBlocks + lane, at = a.c.subs(sub), subs = (int)a.c.subs.d;
+                const int page = sub * kKv4Block < len ? __ldg(table + at) : -1;
+                place = page >= 0 && page < a.n_pages ? (page * a.c.n_k + head) * subs + sub - at * subs : -1;
+            }
+            const int at = __shfl_sync(0xffffffffu, place, (j % 8) * kKtBlocks + lane % kKtBlocks), slot = j % kKtRaw;
+            const bool there = lane < kKtBlocks && at >= 0;
+            const uint32_t which = __ballot_sync(0xffffffffu, there), bar = smem_u32(&raw_full[slot]);
+            pa_wait(smem_u32(&raw_empty[slot]), ((uint32_t)(j / kKtRaw) & 1u) ^ 1u, &abort_flag, a.st);
+            __syncwarp();
+            if (lane == 0) {
+                present[j % kKtPresent] = which;
+                mbar_expect_tx(bar, __popc(which) * kBytes);
+            }
+            __syncwarp();
+            if (there) bulk_g2s(smem_u32(s_raw + (slot * kKtBlocks + lane) * kBytes), a.c.base + (long long)at * kBytes, kBytes, bar);
+        }
+        // nothing is left on its way when the block ends, an expired wait elsewhere included
+        for (int j = max(0, n - kKtRaw); j < n; ++j) pa_wait(smem_u32(&raw_full[j % kKtRaw]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
+    } else if (warp >= 12) {
+        const int w4 = warp - 12;
+        int stage = 0;
+        uint32_t phase = 0;
+        // this warp's two groups of eight tokens of a step
+        auto unpack = [&](int j, auto values) {
+            constexpr bool V = decltype(values)::value;
+            const int slot = j % kKtRaw, base = (step0 + j) * kPaKeys;
+            if (!V) pa_wait(smem_u32(&raw_full[slot]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
+            pa_wait(smem_u32(&kv_empty[stage]), phase ^ 1u, &abort_flag, a.st);
+            const uint32_t there = present[j % kKtPresent];
+            unsigned char* tile = s_kv + stage * kStep;
+            float top = 0.f;
+#pragma unroll
+            for (int pass = 0; pass < 2; ++pass) {
+                const int g8 = pass * 4 + w4, b = g8 >> 1, h = g8 & 1;
+                const unsigned char* blk = s_raw + (slot * kKtBlocks + b) * kBytes;
+                const uint32_t* pairs = reinterpret_cast<const uint32_t*>(blk + 16 * D) + h * 8;
+                const unsigned char* at = blk + (V ? 8 * D : 0) + h * 4 * D + lane * (D / 8);
+                uint32_t w[W];
+                if constexpr (D == 128) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(at);
+                else *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(at);
+                const int hi = lane >> 2, lo = lane & 3;
+                if constexpr (!V) {
+                    // token hi, chunks 4 w + lo; and both factors of the token
+                    const int token = g8 * 8 + hi;
+                    const bool real = (there >> b & 1u) && base + token < len;
+                    uint32_t pk[NG], pv[NG];
+#pragma unroll
+                    for (int i = 0; i < NG; ++i) {
+                        pk[i] = real ? pairs[i * 16 + hi] : 0u;
+                        pv[i] = real ? pairs[(NG + i) * 16 + hi] : 0u;
+                    }
+                    const KtPower pw = KtPower::of<T, NG>(pk), vw = KtPower::of<T, NG>(pv);
+                    if (lo == 0) {
+                        float* fac = s_fac + (j % kKtFactors) * 2 * kPaKeys + token;
+                        fac[0] = pw.back;
+                        fac[kPaKeys] = vw.back;
+                    }
+                    top = fmaxf(top, vw.back);
+#pragma unroll
+                    for (int k = 0; k < W; ++k) {
+                        const float2 p = kv4_pair<T>(pk[k * NG / W]);
+                        const uint4 v = kt_values(w[k], kt_half2(p.x * pw.up, p.x * pw.up), kt_half2(p.y * pw.up, p.y * pw.up));
+                        *reinterpret_cast<uint4*>(tile + kt_chunk(token, 4 * k + lo, kPaKeys)) = v;
+                    }
+                } else {
+                    // place hi of tokens 2 lo and 2 lo + 1
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const int token = g8 * 8 + 2 * lo + s;
+                        const bool real = (there >> b & 1u) && base + token < len;
+                        uint32_t pv[NG];
+#pragma unroll
+                        for (int i = 0; i < NG; ++i) pv[i] = real ? pairs[(NG + i) * 16 + 2 * lo + s] : 0u;
+                        const KtPower vw = KtPower::of<T, NG>(pv);
+#pragma unroll
+                        for (int k = 0; k < W; k += 2) {
+                            const float2 p = kv4_pair<T>(pv[k * NG / W]), q = kv4_pair<T>(pv[(k + 1) * NG / W]);
+                            const uint4 v = kt_values(__byte_perm(w[k], w[k + 1], s ? 0x7632 : 0x5410), kt_half2(p.x * vw.up, q.x * vw.up), kt_half2(p.y * vw.up, q.y * vw.up));
+                            *reinterpret_cast<uint4*>(tile + kt_chunk(token, hi * (W / 2) + k / 2, kPaKeys)) = v;
+                        }
+                    }
+                }
+            }
+            if constexpr (!V) {
+                top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+                if (lane == 0) s_top[j % kKtFactors][w4] = top;
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // written here, read by the MMAs
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(smem_u32(&kv_full[stage]));
+                mbar_arrive(V ? smem_u32(&raw_empty[slot]) : smem_u32(&fac_full[j % kKtFactors]));
+            }
+            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        };
+        if (n > 0) unpack(0, std::false_type{});
+        if (n > 1) unpack(1, std::false_type{});
+        for (int j = 0; j < n; ++j) {
+            unpack(j, std::true_type{});
+            if (j + 2 < n) unpack(j + 2, std::false_type{});
+        }
+    } else if (warp == 8 || warp == 9) {
+        // the MMAs of tile t, as in prompt_attention_kernel
+        const int t = warp - 8, nt = t ? n1 : n0;
+        constexpr uint32_t kBase = (1u << 4) | (8u << 24);
+        constexpr uint32_t idesc_s = kBase | ((uint32_t)(kPaKeys / 8) << 17), idesc_o = kBase | (1u << 16) | ((uint32_t)(D / 8) << 17);
+        const uint32_t q = pa_desc_k(smem_u32(smem) + t * kTile), kv = smem_u32(s_kv), ts = tmem + t * 128, to = tmem + 256 + t * 128;
+        int stage = 0;
+        uint32_t phase = 0;
+        auto full = [&]() { pa_wait(smem_u32(&kv_full[stage]), phase, &abort_flag, a.st); };
+        auto next = [&]() {
+            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        };
+        auto scores = [&](int j) {
+            full();
+            if (j < nt) {
+                tc_fence_after();
+                if (pa_elect()) {
+                    const uint32_t k = pa_desc_k(kv + stage * kStep), to_s = ts + (j & 1) * kPaKeys;
+                    pa_mma_ss<false>(to_s, q, k, idesc_s);
+#pragma unroll
+                    for (int kk = 1; kk < DB * 4; ++kk) pa_mma_ss<true>(to_s, q + (kk >> 2) * (kPaRows / 16) + (kk & 3) * 2, k + (kk >> 2) * (kPaBlock / 16) + (kk & 3) * 2, idesc_s);
+                    tc_commit(smem_u32(&s_full[t * 2 + (j & 1)]));
+                    tc_commit(smem_u32(&kv_empty[stage]));
+                }
+            } else if (lane == 0) {
+                mbar_arrive(smem_u32(&kv_empty[stage]));
+            }
+            next();
+        };
+        if (n > 0) pa_wait(smem_u32(&q_full), 0, &abort_flag, a.st);
+        if (n > 0) scores(0);
+        if (n > 1) scores(1);
+        for (int j = 0; j < n; ++j) {
+            full();
+            if (j < nt) {
+                const int buf = j & 1;
+                pa_wait(smem_u32(&p_full[t * 2 + buf]), (uint32_t)(j >> 1) & 1u, &abort_flag, a.st);
+                tc_fence_after();
+                if (pa_elect()) {
+                    const uint32_t v = pa_desc_n(kv + stage * kStep), p = ts + buf * kPaKeys;
+                    if (j == 0) pa_mma_ts<false>(to, p, v, idesc_o);
+                    else pa_mma_ts<true>(to, p, v, idesc_o);
+#pragma unroll
+                    for (int kk = 1; kk < kPaKeys / 16; ++kk) pa_mma_ts<true>(to, p + kk * 8, v + kk * 128, idesc_o);
+                    tc_commit(smem_u32(&pv_done[t * 2 + buf]));
+                    tc_commit(smem_u32(&kv_empty[stage]));
+                }
+            } else if (lane == 0) {
+                mbar_arrive(smem_u32(&kv_empty[stage]));
+            }
+            next();
+            if (j + 2 < n) scores(j + 2);
+        }
+        if (nt > 0) pa_wait(smem_u32(&pv_done[t * 2 + ((nt - 1) & 1)]), (uint32_t)((nt - 1) >> 1) & 1u, &abort_flag, a.st);
+    } else if (warp < 8) {
+        const int t = warp >> 2, local = (warp & 3) * 32 + lane, row = row0 + t * 128 + local, nt = t ? n1 : n0;
+        const bool live = row < rows;
+        const int tok = live ? row / a.G : 0, q_head = head * a.G + row - tok * a.G;
+        const T* q_row = static_cast<const T*>(a.q) + (q0 + tok) * a.ld_q + (long long)(live ? q_head : 0) * D;
+        // the row of operand A: scaled by a power of two, turned round where the scale is negative
+        float c;                                               // from a raw score to powers of two
+        {
+            uint32_t raw[D / 2] = {};
+            uint32_t big = 0;
+            if (live)
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) *reinterpret_cast<uint4*>(raw + 4 * i) = reinterpret_cast<const uint4*>(q_row)[i];
+#pragma unroll
+            for (int i = 0; i < D / 2; ++i) {
+                const float2 f = kv4_pair<T>(raw[i]);
+                big = max(big, max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu));
+            }
+            const int e = q4_exponent(big);
+            const Q4Power up(e), down(-e);
+            c = fabsf(a.scale2) * down.a * down.b;
+            const float sign = a.scale2 < 0.f ? -1.f : 1.f;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) {
+                float f[8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 x = kv4_pair<T>(raw[4 * i + k]);
+                    f[2 * k] = up(x.x) * sign;
+                    f[2 * k + 1] = up(x.y) * sign;
+                }
+                *reinterpret_cast<uint4*>(smem + t * kTile + kt_chunk(local, i, 128)) =
+                    make_uint4(half_pair(f[0], f[4]), half_pair(f[1], f[5]), half_pair(f[2], f[6]), half_pair(f[3], f[7]));
+            }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");           // written here, read by the MMAs
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&q_full));
+
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t ts = tmem + t * 128 + lanes, to = tmem + 256 + t * 128 + lanes;
+        const unsigned long long tree = a.tree && live ? __ldg(a.tree + q0 + tok) : 0ull;
+        float m = kNegInf, vtop = 0.f, mc = 0.f;               // reference: of the scores, of the values' factors, and both together
+        unsigned long long sum2 = 0;
+        float s[kPaKeys];
+        uint32_t* sr = reinterpret_cast<uint32_t*>(s);
+        for (int j = 0; j < nt; ++j) {
+            const int buf = j & 1, slot = j % kKtFactors, base = (step0 + j) * kPaKeys;
+            pa_wait(smem_u32(&fac_full[slot]), (uint32_t)(j / kKtFactors) & 1u, &abort_flag, a.st);
+            pa_wait(smem_u32(&s_full[t * 2 + buf]), (uint32_t)(j >> 1) & 1u, &abort_flag, a.st);
+            __syncwarp();
+            tc_fence_after();
+            const uint32_t at = ts + buf * kPaKeys;
+            pa_ld32(at, sr);
+            pa_ld32(at + 32, sr + 32);
+            const float4 *kf = reinterpret_cast<const float4*>(s_fac + slot * 2 * kPaKeys), *vf = kf + kPaKeys / 4;
+            const float4 t4 = *reinterpret_cast<const float4*>(s_top[slot]);
+            const float vnow = fmaxf(fmaxf(t4.x, t4.y), fmaxf(t4.z, t4.w));
+            const uint32_t there = present[j % kKtPresent];
+            pa_ld_wait();
+#pragma unroll
+            for (int i = 0; i < kPaKeys / 4; ++i) {
+                const float4 f = kf[i];
+                const float2 x = halves(mul2(pair_of(s[4 * i], s[4 * i + 1]), pair_of(f.x, f.y))), y = halves(mul2(pair_of(s[4 * i + 2], s[4 * i + 3]), pair_of(f.z, f.w)));
+                s[4 * i] = x.x;
+                s[4 * i + 1] = x.y;
+                s[4 * i + 2] = y.x;
+                s[4 * i + 3] = y.y;
+            }
+            if (base + kPaKeys > open || there != (1u << kKtBlocks) - 1) {
+                // which tokens of the step this row sees
+                unsigned long long see = 0;
+#pragma unroll
+                for (int b = 0; b < kKtBlocks; ++b)
+                    if (there >> b & 1u) see |= 0xffffull << (16 * b);
+                const int d = past - base;                     // tokens in front of the query tokens
+                const unsigned long long own = a.tree ? tree : tok >= 63 ? ~0ull : (2ull << tok) - 1;
+                if (a.tree) {
+                    if (d < 64) see &= d > 0 ? ((1ull << d) - 1) | own << d : d > -64 ? own >> -d : 0ull;
+                } else {
+                    const int upto = d + tok + 1;              // tokens from the step's first on
+                    if (upto < 64) see &= upto > 0 ? (1ull << upto) - 1 : 0ull;
+                }
+                if (len - base < 64) see &= len > base ? (1ull << (len - base)) - 1 : 0ull;
+#pragma unroll
+                for (int i = 0; i < kPaKeys; ++i) s[i] = see >> i & 1ull ? s[i] : kNegInf;
+            }
+            float m4[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+            for (int i = 4; i < kPaKeys; i += 8)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m4[e] = i + 4 + e < kPaKeys ? pa_max3(m4[e], s[i + e], s[i + 4 + e]) : fmaxf(m4[e], s[i + e]);
+            const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            const bool moves = top * c > (m == kNegInf ? 0.f : m * c) + 8.f || (m == kNegInf && top > kNegInf);
+            if (__any_sync(0xffffffffu, moves) || vnow > vtop) {
+                const float next = moves ? top : m, vnext = fmaxf(vtop, vnow);
+                const float next_c = (next == kNegInf ? 0.f : next * c) + (float)((int)(__float_as_uint(vnext) >> 23) - 127);
+                const float f = m == kNegInf ? 0.f : exp2_fast(mc - next_c);
+                m = next;
+                mc = next_c;
+                vtop = vnext;
+                sum2 = mul2(sum2, pair_of(f, f));
+                if (j > 0) {                                   // O, once the step before is in it
+                    pa_wait(smem_u32(&pv_done[t * 2 + (buf ^ 1)]), (uint32_t)((j - 1) >> 1) & 1u, &abort_flag, a.st);
+                    __syncwarp();
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int b = 0; b < 2 * DB; ++b) {
+                        uint32_t o[32];
+                        pa_ld32(to + b * 32, o);
+                        pa_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                        pa_st32(to + b * 32, o);
+                    }
+                    pa_st_wait();
+                }
+            }
+            const unsigned long long c2 = pair_of(c, c), m2 = pair_of(-mc, -mc);
+            uint32_t p[kPaKeys / 2];
+#pragma unroll
+            for (int i = 0; i < kPaKeys / 4; ++i) {
+                const float4 f = vf[i];
+                const float2 x = halves(fma2(pair_of(s[4 * i], s[4 * i + 1]), c2, m2)), y = halves(fma2(pair_of(s[4 * i + 2], s[4 * i + 3]), c2, m2));
+                const unsigned long long e = pair_of(pa_exp2(x.x), pa_exp2(x.y)), g = pair_of(pa_exp2(y.x), pa_exp2(y.y));
+                sum2 = add2(sum2, add2(e, g));
+                const float2 u = halves(mul2(e, pair_of(f.x, f.y))), v = halves(mul2(g, pair_of(f.z, f.w)));
+                p[2 * i] = half_pair(u.x, u.y);
+                p[2 * i + 1] = half_pair(v.x, v.y);
+            }
+            pa_st32(at, p);
+            pa_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&p_full[t * 2 + buf]));
+        }
+        const float2 sums = halves(sum2);
+        const float sum = sums.x + sums.y;
+        const bool whole = a.splits == 1;
+        const float inv = sum == 0.f ? 0.f : whole ? 1.f / sum : 1.f;
+        if (nt > 0) {
+            pa_wait(smem_u32(&pv_done[t * 2 + ((nt - 1) & 1)]), (uint32_t)((nt - 1) >> 1) & 1u, &abort_flag, a.st);
+            __syncwarp();
+            tc_fence_after();
+        }
+        const long long at = (long long)(q0 + tok) * a.n_q + q_head, part = (long long)split * a.n_rows * a.n_q + at;
+        T* out = static_cast<T*>(a.out) + (long long)(q0 + tok) * a.ld_out + (long long)q_head * D;
+        float* part_o = a.part_o + part * D;
+        float odd = 0.f;                                       // NaN where a result is not finite
+        // 32 places of the values: column 8 i + n stands at place n D / 8 + 8 (i / 8) + (0 2 4 6 1 3 5 7 for i % 8)
+        constexpr int kPlaces = D / 8, kCols = 32 / kPlaces;   // columns n side by side in 32 places (2 or 4)
+#pragma unroll
+        for (int b = 0; b < 2 * DB; ++b) {
+            uint32_t o[32];
+            if (nt > 0) {
+                pa_ld32(to + b * 32, o);
+                pa_ld_wait();
+            }
+#pragma unroll
+            for (int i = 0; i < kPlaces; ++i) {
+                float x[kCols];
+#pragma unroll
+                for (int k = 0; k < kCols; ++k) {
+                    x[k] = sum == 0.f ? 0.f : __uint_as_float(o[k * kPlaces + (i & ~7) + ((i & 3) * 2 + (i >> 2 & 1))]) * inv;
+                    odd = fmaf(x[k], 0.f, odd);
+                }
+                const int col = 8 * i + b * kCols;
+                if (!live) continue;
+                if (!whole) {
+                    if constexpr (kCols == 2) *reinterpret_cast<float2*>(part_o + col) = make_float2(x[0], x[1]);
+                    else *reinterpret_cast<float4*>(part_o + col) = make_float4(x[0], x[1], x[2], x[3]);
+                } else {
+                    T v[kCols];
+#pragma unroll
+                    for (int k = 0; k < kCols; ++k) v[k] = Elem<T>::down(x[k]);
+                    if constexpr (kCols == 2) *reinterpret_cast<uint32_t*>(out + col) = *reinterpret_cast<const uint32_t*>(v);
+                    else *reinterpret_cast<uint2*>(out + col) = *reinterpret_cast<const uint2*>(v);
+                }
+            }
+        }
+        if (live && !whole) a.part_ml[part] = make_float2(sum == 0.f ? kKv4NoMax : mc, sum);
+        if (live && whole && a.lse) a.lse[at] = sum == 0.f ? kNegInf : (mc + log2f(sum)) * 0.69314718055994531f;
+        // rows of finite weights whose result is not: values that they do not see may be the reason
+        const bool again = live && sum > 0.f && sum < __int_as_float(0x7f800000) && odd != 0.f;
+        for (uint32_t todo = __ballot_sync(0xffffffffu, again); todo; todo &= todo - 1) {
+            const int r = __ffs(todo) - 1, tok_r = __shfl_sync(0xffffffffu, tok, r), head_r = __shfl_sync(0xffffffffu, q_head, r);
+            const unsigned long long tree_r = __shfl_sync(0xffffffffu, tree, r);
+            const float mc_r = __shfl_sync(0xffffffffu, mc, r), inv_r = __shfl_sync(0xffffffffu, inv, r);
+            float acc[D / 32];
+            kt_row_again<T, D, NG>(a, table, head, static_cast<const T*>(a.q) + (q0 + tok_r) * a.ld_q + (long long)head_r * D, step0 * kPaKeys,
+                                   min(len, (step0 + n) * kPaKeys), past, tok_r, tree_r, mc_r, inv_r, acc);
+            const long long at_r = (long long)(q0 + tok_r) * a.n_q + head_r;
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) {
+                if (whole) static_cast<T*>(a.out)[(long long)(q0 + tok_r) * a.ld_out + (long long)head_r * D + lane * (D / 32) + e] = Elem<T>::down(acc[e]);
+                else a.part_o[((long long)split * a.n_rows * a.n_q + at_r) * D + lane * (D / 32) + e] = acc[e];
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+    pdl_launch_dependents();
+}
+
+}  // namespace coral
