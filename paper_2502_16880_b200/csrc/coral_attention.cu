@@ -212,7 +212,10 @@ int launch_kv4_groups(const Kv4Args& k, const Kv4Plan& p, cudaStream_t st) {
     if (e != cudaSuccess) return CORAL_ERR_CUDA;
     if (p.splits == 1) return CORAL_OK;
     const long long rows = (long long)k.n_seq * k.max_q * k.n_q;
-    return launch_pdl(kv4_join_kernel<T, D>, dim3((unsigned)rows), dim3(kKv4JoinWarps * 32), 0, st, k) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
+    // up to 8 parts: a warp a row; more: four
+    const bool few = p.splits <= 8;
+    const unsigned blocks = (unsigned)(few ? (rows - 1) / kKv4JoinWarps + 1 : rows);
+    return launch_pdl(few ? kv4_join_kernel<T, D, 1> : kv4_join_kernel<T, D, kKv4JoinWarps>, dim3(blocks), dim3(kKv4JoinWarps * 32), 0, st, k) == cudaSuccess ? CORAL_OK : CORAL_ERR_CUDA;
 }
 
 // ---- attention over prompts ----------------------------------------------------------------------------------

@@ -738,26 +738,27 @@ __global__ void __launch_bounds__(kKv4Threads, NR == 1 ? 2 : 1) kv4_attention_ke
     pdl_launch_dependents();
 }
 
-// Adds up the parts of split caches, in a fixed order: a block a row and head, every fourth part a warp, D / 32 columns a lane.
+// Adds up the parts of split caches, in a fixed order: WAYS warps a row and head (each every WAYS-th part), D / 32 columns a lane.
 constexpr int kKv4JoinWarps = 4;
-template <typename T, int D>
+template <typename T, int D, int WAYS>
 __global__ void __launch_bounds__(kKv4JoinWarps * 32) kv4_join_kernel(const __grid_constant__ Kv4Args a) {
     constexpr int N = D / 32;
     __shared__ float s_o[kKv4JoinWarps][D];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, way = warp % WAYS;
+    const int unit = blockIdx.x * (kKv4JoinWarps / WAYS) + warp / WAYS;
     pdl_wait();
-    const int node = blockIdx.x / a.n_q, head = blockIdx.x - node * a.n_q, seq = node / a.max_q, tok = node - seq * a.max_q;
-    int q0, n;
-    kv4_rows_of(a, seq, &q0, &n);
-    if (tok >= min(n, a.max_q)) return;
+    const int node = unit / a.n_q, head = unit - node * a.n_q, seq = node / a.max_q, tok = node - seq * a.max_q;
+    int q0 = 0, n = 0;
+    if (seq < a.n_seq) kv4_rows_of(a, seq, &q0, &n);
+    const bool live = tok < min(n, a.max_q);
     const long long at = (long long)(q0 + tok) * a.n_q + head, step = (long long)a.n_rows * a.n_q;
-    constexpr int kMost = kKv4MaxSplits / 32;
+    constexpr int kMost = WAYS == 1 ? 1 : kKv4MaxSplits / 32;
     float2 ml[kMost];                                         // part 32 i + lane
     float top = kNegInf;
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
         const int s = i * 32 + lane;
-        ml[i] = s < a.splits ? __ldcg(&a.part_ml[s * step + at]) : make_float2(kNegInf, 0.f);
+        ml[i] = live && s < a.splits ? __ldcg(&a.part_ml[s * step + at]) : make_float2(kNegInf, 0.f);
         if (ml[i].y != 0.f) top = fmaxf(top, ml[i].x);        // parts that saw nothing have a sum of 0
     }
     top = warp_max(top);
@@ -768,9 +769,10 @@ __global__ void __launch_bounds__(kKv4JoinWarps * 32) kv4_join_kernel(const __gr
         sum += f * ml[i].y;
         if (i * 32 >= a.splits) break;
 #pragma unroll
-        for (int j = 0; j < 32 / kKv4JoinWarps; ++j) {
-            const int s = i * 32 + j * kKv4JoinWarps + warp;
-            const float g = __shfl_sync(0xffffffffu, f, j * kKv4JoinWarps + warp);
+        for (int j = 0; j < 32 / WAYS; ++j) {
+            const int s = i * 32 + j * WAYS + way;
+            if (WAYS == 1 && s >= a.splits) break;
+            const float g = __shfl_sync(0xffffffffu, f, j * WAYS + way);
             if (s >= a.splits || g == 0.f) continue;
             const float* p = a.part_o + (s * step + at) * D + lane * N;
             if constexpr (N == 4) {
@@ -783,17 +785,26 @@ __global__ void __launch_bounds__(kKv4JoinWarps * 32) kv4_join_kernel(const __gr
         }
     }
     sum = warp_sum(sum);
-#pragma unroll
-    for (int j = 0; j < N; ++j) s_o[warp][lane * N + j] = o[j];
-    __syncthreads();
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    for (int c = threadIdx.x; c < D; c += kKv4JoinWarps * 32) {
-        float v = 0.f;
+    if constexpr (WAYS > 1) {
 #pragma unroll
-        for (int w = 0; w < kKv4JoinWarps; ++w) v += s_o[w][c];
-        static_cast<T*>(a.out)[(long long)(q0 + tok) * a.ld_out + head * D + c] = Elem<T>::down(v * inv);
+        for (int j = 0; j < N; ++j) s_o[warp][lane * N + j] = o[j];
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            o[j] = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAYS; ++w) o[j] += s_o[w][lane * N + j];
+        }
     }
-    if (a.lse && threadIdx.x == 0) a.lse[at] = sum == 0.f ? kNegInf : (top + log2f(sum)) * 0.69314718055994531f;
+    if (!live || way != 0) return;
+    T v[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = Elem<T>::down(o[j] * inv);
+    T* out = static_cast<T*>(a.out) + (long long)(q0 + tok) * a.ld_out + head * D + lane * N;
+    if constexpr (N == 4) *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(v);
+    else *reinterpret_cast<uint32_t*>(out) = *reinterpret_cast<const uint32_t*>(v);
+    if (a.lse && lane == 0) a.lse[at] = sum == 0.f ? kNegInf : (top + log2f(sum)) * 0.69314718055994531f;
 }
 
 }  // namespace coral

@@ -1,7 +1,7 @@
 // Attention of many rows (the nodes of draft trees, times the heads of a group) over the 4-bit cache, on the 5th-generation tensor cores: the
-// products of prompt_attention.cuh, two tiles of 128 rows a block, with keys and values unpacked by four warps instead of copied.
+// products of prompt_attention.cuh, two tiles of 128 rows a block, with keys and values unpacked by eight warps instead of copied.
 //   * a warp brings the packed blocks of 64 tokens a step into a ring of their own, one bulk copy each,
-//   * four warps turn them into fp16 tiles, low + step code, each token times a power of two that brings its largest value to
+//   * eight warps turn them into fp16 tiles, low + step code, each token times a power of two that brings its largest value to
 //     2^14..2^15; the powers, exact, come back in the scores (kf) and in the weights (vf), so a value is rounded once, to 2^-12 of itself,
 //   * a thread of the softmax has a row: S kf c - m in powers of two, P vf to fp16.  The reference m holds the largest vf so far as well,
 //     so that P vf is at most 2^8 whatever the values' size.
@@ -14,7 +14,12 @@
 
 namespace coral {
 
-constexpr int kKtThreads = 16 * 32;                // warps 0..7 softmax, 8 and 9 MMAs of a tile each, 10 copies, 12..15 unpacking
+constexpr int kKtUnpack = 8;                       // unpacking warps, which share a step's eight groups of eight tokens
+constexpr int kKtGroups = 8 / kKtUnpack;
+// Registers a thread: 96 at launch (640 threads); the softmax's two warpgroups take what the other three give up.
+constexpr int kKtRegsMany = 136, kKtRegsFew = 64;
+static_assert(2 * kKtRegsMany + 3 * kKtRegsFew <= 5 * 96, "a split above the launch's registers would wait forever");
+constexpr int kKtThreads = (12 + kKtUnpack) * 32;  // warps 0..7 softmax, 8 and 9 MMAs of a tile each, 10 copies, 12.. unpacking
 constexpr int kKtRaw = 4;                          // steps of packed tokens in flight
 constexpr int kKtBlocks = kPaKeys / kKv4Block;     // blocks of 16 tokens a step
 constexpr int kKtFactors = 8;                      // steps whose factors are kept
@@ -39,7 +44,6 @@ struct KtPower {
         return KtPower{__uint_as_float((uint32_t)(268 - e) << 23), __uint_as_float((uint32_t)(e - 14) << 23)};
     }
 };
-__device__ __forceinline__ uint32_t kt_half2(float lo, float hi) { return half_pair(lo, hi); }
 // A word's eight codes as values, pairs (0,4), (1,5), (2,6), (3,7): step and low as fp16 pairs, one rounding.
 __device__ __forceinline__ uint4 kt_values(uint32_t w, uint32_t step, uint32_t low) {
     uint32_t r[4];
@@ -110,14 +114,14 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
     __shared__ __align__(8) uint64_t q_full, kv_full[STAGES], kv_empty[STAGES], s_full[4], p_full[4], pv_done[4];
     __shared__ __align__(8) uint64_t raw_full[kKtRaw], raw_empty[kKtRaw], fac_full[kKtFactors];
     __shared__ uint32_t present[kKtPresent];
-    __shared__ __align__(16) float s_top[kKtFactors][4];
+    __shared__ __align__(16) float s_top[kKtFactors][kKtUnpack];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&q_full), 8);
         for (int i = 0; i < STAGES; ++i) {
-            mbar_init(smem_u32(&kv_full[i]), 4);
+            mbar_init(smem_u32(&kv_full[i]), kKtUnpack);
             mbar_init(smem_u32(&kv_empty[i]), 2);
         }
         for (int i = 0; i < 4; ++i) {
@@ -127,9 +131,9 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
         }
         for (int i = 0; i < kKtRaw; ++i) {
             mbar_init(smem_u32(&raw_full[i]), 1);
-            mbar_init(smem_u32(&raw_empty[i]), 4);
+            mbar_init(smem_u32(&raw_empty[i]), kKtUnpack);
         }
-        for (int i = 0; i < kKtFactors; ++i) mbar_init(smem_u32(&fac_full[i]), 4);
+        for (int i = 0; i < kKtFactors; ++i) mbar_init(smem_u32(&fac_full[i]), kKtUnpack);
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -164,167 +168,8 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
     const int n0 = max(steps, 0), n1 = rows - row0 > 128 ? n0 : 0, n = n0;
     const int32_t* table = a.table + seq * a.ld_table;
 
-    if (warp == 10) {
-        int place = -1;
-        for (int j = 0; j < n; ++j) {
-            // where the blocks of eight steps lie in the cache, one a lane (-1: none)
-            if (j % 8 == 0) {
-                const int sub = (step0 + j) * kKtBlocks + lane, at = a.c.subs(sub), subs = (int)a.c.subs.d;
-                const int page = sub * kKv4Block < len ? __ldg(table + at) : -1;
-                place = page >= 0 && page < a.n_pages ? (page * a.c.n_k + head) * subs + sub - at * subs : -1;
-            }
-            const int at = __shfl_sync(0xffffffffu, place, (j % 8) * kKtBlocks + lane % kKtBlocks), slot = j % kKtRaw;
-            const bool there = lane < kKtBlocks && at >= 0;
-            const uint32_t which = __ballot_sync(0xffffffffu, there), bar = smem_u32(&raw_full[slot]);
-            pa_wait(smem_u32(&raw_empty[slot]), ((uint32_t)(j / kKtRaw) & 1u) ^ 1u, &abort_flag, a.st);
-            __syncwarp();
-            if (lane == 0) {
-                present[j % kKtPresent] = which;
-                mbar_expect_tx(bar, __popc(which) * kBytes);
-            }
-            __syncwarp();
-            if (there) bulk_g2s(smem_u32(s_raw + (slot * kKtBlocks + lane) * kBytes), a.c.base + (long long)at * kBytes, kBytes, bar);
-        }
-        // nothing is left on its way when the block ends, an expired wait elsewhere included
-        for (int j = max(0, n - kKtRaw); j < n; ++j) pa_wait(smem_u32(&raw_full[j % kKtRaw]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
-    } else if (warp >= 12) {
-        const int w4 = warp - 12;
-        int stage = 0;
-        uint32_t phase = 0;
-        // this warp's two groups of eight tokens of a step
-        auto unpack = [&](int j, auto values) {
-            constexpr bool V = decltype(values)::value;
-            const int slot = j % kKtRaw, base = (step0 + j) * kPaKeys;
-            if (!V) pa_wait(smem_u32(&raw_full[slot]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
-            pa_wait(smem_u32(&kv_empty[stage]), phase ^ 1u, &abort_flag, a.st);
-            const uint32_t there = present[j % kKtPresent];
-            unsigned char* tile = s_kv + stage * kStep;
-            float top = 0.f;
-#pragma unroll
-            for (int pass = 0; pass < 2; ++pass) {
-                const int g8 = pass * 4 + w4, b = g8 >> 1, h = g8 & 1;
-                const unsigned char* blk = s_raw + (slot * kKtBlocks + b) * kBytes;
-                const uint32_t* pairs = reinterpret_cast<const uint32_t*>(blk + 16 * D) + h * 8;
-                const unsigned char* at = blk + (V ? 8 * D : 0) + h * 4 * D + lane * (D / 8);
-                uint32_t w[W];
-                if constexpr (D == 128) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(at);
-                else *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(at);
-                const int hi = lane >> 2, lo = lane & 3;
-                if constexpr (!V) {
-                    // token hi, chunks 4 w + lo; and both factors of the token
-                    const int token = g8 * 8 + hi;
-                    const bool real = (there >> b & 1u) && base + token < len;
-                    uint32_t pk[NG], pv[NG];
-#pragma unroll
-                    for (int i = 0; i < NG; ++i) {
-                        pk[i] = real ? pairs[i * 16 + hi] : 0u;
-                        pv[i] = real ? pairs[(NG + i) * 16 + hi] : 0u;
-                    }
-                    const KtPower pw = KtPower::of<T, NG>(pk), vw = KtPower::of<T, NG>(pv);
-                    if (lo == 0) {
-                        float* fac = s_fac + (j % kKtFactors) * 2 * kPaKeys + token;
-                        fac[0] = pw.back;
-                        fac[kPaKeys] = vw.back;
-                    }
-                    top = fmaxf(top, vw.back);
-#pragma unroll
-                    for (int k = 0; k < W; ++k) {
-                        const float2 p = kv4_pair<T>(pk[k * NG / W]);
-                        const uint4 v = kt_values(w[k], kt_half2(p.x * pw.up, p.x * pw.up), kt_half2(p.y * pw.up, p.y * pw.up));
-                        *reinterpret_cast<uint4*>(tile + kt_chunk(token, 4 * k + lo, kPaKeys)) = v;
-                    }
-                } else {
-                    // place hi of tokens 2 lo and 2 lo + 1
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const int token = g8 * 8 + 2 * lo + s;
-                        const bool real = (there >> b & 1u) && base + token < len;
-                        uint32_t pv[NG];
-#pragma unroll
-                        for (int i = 0; i < NG; ++i) pv[i] = real ? pairs[(NG + i) * 16 + 2 * lo + s] : 0u;
-                        const KtPower vw = KtPower::of<T, NG>(pv);
-#pragma unroll
-                        for (int k = 0; k < W; k += 2) {
-                            const float2 p = kv4_pair<T>(pv[k * NG / W]), q = kv4_pair<T>(pv[(k + 1) * NG / W]);
-                            const uint4 v = kt_values(__byte_perm(w[k], w[k + 1], s ? 0x7632 : 0x5410), kt_half2(p.x * vw.up, q.x * vw.up), kt_half2(p.y * vw.up, q.y * vw.up));
-                            *reinterpret_cast<uint4*>(tile + kt_chunk(token, hi * (W / 2) + k / 2, kPaKeys)) = v;
-                        }
-                    }
-                }
-            }
-            if constexpr (!V) {
-                top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
-                if (lane == 0) s_top[j % kKtFactors][w4] = top;
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // written here, read by the MMAs
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(smem_u32(&kv_full[stage]));
-                mbar_arrive(V ? smem_u32(&raw_empty[slot]) : smem_u32(&fac_full[j % kKtFactors]));
-            }
-            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-        };
-        if (n > 0) unpack(0, std::false_type{});
-        if (n > 1) unpack(1, std::false_type{});
-        for (int j = 0; j < n; ++j) {
-            unpack(j, std::true_type{});
-            if (j + 2 < n) unpack(j + 2, std::false_type{});
-        }
-    } else if (warp == 8 || warp == 9) {
-        // the MMAs of tile t, as in prompt_attention_kernel
-        const int t = warp - 8, nt = t ? n1 : n0;
-        constexpr uint32_t kBase = (1u << 4) | (8u << 24);
-        constexpr uint32_t idesc_s = kBase | ((uint32_t)(kPaKeys / 8) << 17), idesc_o = kBase | (1u << 16) | ((uint32_t)(D / 8) << 17);
-        const uint32_t q = pa_desc_k(smem_u32(smem) + t * kTile), kv = smem_u32(s_kv), ts = tmem + t * 128, to = tmem + 256 + t * 128;
-        int stage = 0;
-        uint32_t phase = 0;
-        auto full = [&]() { pa_wait(smem_u32(&kv_full[stage]), phase, &abort_flag, a.st); };
-        auto next = [&]() {
-            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-        };
-        auto scores = [&](int j) {
-            full();
-            if (j < nt) {
-                tc_fence_after();
-                if (pa_elect()) {
-                    const uint32_t k = pa_desc_k(kv + stage * kStep), to_s = ts + (j & 1) * kPaKeys;
-                    pa_mma_ss<false>(to_s, q, k, idesc_s);
-#pragma unroll
-                    for (int kk = 1; kk < DB * 4; ++kk) pa_mma_ss<true>(to_s, q + (kk >> 2) * (kPaRows / 16) + (kk & 3) * 2, k + (kk >> 2) * (kPaBlock / 16) + (kk & 3) * 2, idesc_s);
-                    tc_commit(smem_u32(&s_full[t * 2 + (j & 1)]));
-                    tc_commit(smem_u32(&kv_empty[stage]));
-                }
-            } else if (lane == 0) {
-                mbar_arrive(smem_u32(&kv_empty[stage]));
-            }
-            next();
-        };
-        if (n > 0) pa_wait(smem_u32(&q_full), 0, &abort_flag, a.st);
-        if (n > 0) scores(0);
-        if (n > 1) scores(1);
-        for (int j = 0; j < n; ++j) {
-            full();
-            if (j < nt) {
-                const int buf = j & 1;
-                pa_wait(smem_u32(&p_full[t * 2 + buf]), (uint32_t)(j >> 1) & 1u, &abort_flag, a.st);
-                tc_fence_after();
-                if (pa_elect()) {
-                    const uint32_t v = pa_desc_n(kv + stage * kStep), p = ts + buf * kPaKeys;
-                    if (j == 0) pa_mma_ts<false>(to, p, v, idesc_o);
-                    else pa_mma_ts<true>(to, p, v, idesc_o);
-#pragma unroll
-                    for (int kk = 1; kk < kPaKeys / 16; ++kk) pa_mma_ts<true>(to, p + kk * 8, v + kk * 128, idesc_o);
-                    tc_commit(smem_u32(&pv_done[t * 2 + buf]));
-                    tc_commit(smem_u32(&kv_empty[stage]));
-                }
-            } else if (lane == 0) {
-                mbar_arrive(smem_u32(&kv_empty[stage]));
-            }
-            next();
-            if (j + 2 < n) scores(j + 2);
-        }
-        if (nt > 0) pa_wait(smem_u32(&pv_done[t * 2 + ((nt - 1) & 1)]), (uint32_t)((nt - 1) >> 1) & 1u, &abort_flag, a.st);
-    } else if (warp < 8) {
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kKtRegsMany));
         const int t = warp >> 2, local = (warp & 3) * 32 + lane, row = row0 + t * 128 + local, nt = t ? n1 : n0;
         const bool live = row < rows;
         const int tok = live ? row / a.G : 0, q_head = head * a.G + row - tok * a.G;
@@ -332,26 +177,31 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
         // the row of operand A: scaled by a power of two, turned round where the scale is negative
         float c;                                               // from a raw score to powers of two
         {
-            uint32_t raw[D / 2] = {};
+            // twice over the row: registers are short
             uint32_t big = 0;
             if (live)
+#pragma unroll 4
+                for (int i = 0; i < D / 8; ++i) {
+                    uint32_t raw[4];
+                    *reinterpret_cast<uint4*>(raw) = reinterpret_cast<const uint4*>(q_row)[i];
 #pragma unroll
-                for (int i = 0; i < D / 8; ++i) *reinterpret_cast<uint4*>(raw + 4 * i) = reinterpret_cast<const uint4*>(q_row)[i];
-#pragma unroll
-            for (int i = 0; i < D / 2; ++i) {
-                const float2 f = kv4_pair<T>(raw[i]);
-                big = max(big, max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu));
-            }
+                    for (int k = 0; k < 4; ++k) {
+                        const float2 f = kv4_pair<T>(raw[k]);
+                        big = max(big, max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu));
+                    }
+                }
             const int e = q4_exponent(big);
             const Q4Power up(e), down(-e);
             c = fabsf(a.scale2) * down.a * down.b;
             const float sign = a.scale2 < 0.f ? -1.f : 1.f;
-#pragma unroll
+#pragma unroll 2
             for (int i = 0; i < D / 8; ++i) {
+                uint32_t raw[4] = {};
+                if (live) *reinterpret_cast<uint4*>(raw) = reinterpret_cast<const uint4*>(q_row)[i];
                 float f[8];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const float2 x = kv4_pair<T>(raw[4 * i + k]);
+                    const float2 x = kv4_pair<T>(raw[k]);
                     f[2 * k] = up(x.x) * sign;
                     f[2 * k + 1] = up(x.y) * sign;
                 }
@@ -380,8 +230,8 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
             pa_ld32(at, sr);
             pa_ld32(at + 32, sr + 32);
             const float4 *kf = reinterpret_cast<const float4*>(s_fac + slot * 2 * kPaKeys), *vf = kf + kPaKeys / 4;
-            const float4 t4 = *reinterpret_cast<const float4*>(s_top[slot]);
-            const float vnow = fmaxf(fmaxf(t4.x, t4.y), fmaxf(t4.z, t4.w));
+            const float4 t4 = *reinterpret_cast<const float4*>(s_top[slot]), u4 = *reinterpret_cast<const float4*>(s_top[slot] + 4);
+            const float vnow = fmaxf(fmaxf(fmaxf(t4.x, t4.y), fmaxf(t4.z, t4.w)), fmaxf(fmaxf(u4.x, u4.y), fmaxf(u4.z, u4.w)));
             const uint32_t there = present[j % kKtPresent];
             pa_ld_wait();
 #pragma unroll
@@ -521,6 +371,175 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
                 if (whole) static_cast<T*>(a.out)[(long long)(q0 + tok_r) * a.ld_out + (long long)head_r * D + lane * (D / 32) + e] = Elem<T>::down(acc[e]);
                 else a.part_o[((long long)split * a.n_rows * a.n_q + at_r) * D + lane * (D / 32) + e] = acc[e];
             }
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kKtRegsFew));
+        if (warp == 10) {
+            int place = -1;
+            for (int j = 0; j < n; ++j) {
+                // where the blocks of eight steps lie in the cache, one a lane (-1: none)
+                if (j % 8 == 0) {
+                    const int sub = (step0 + j) * kKtBlocks + lane, at = a.c.subs(sub), subs = (int)a.c.subs.d;
+                    const int page = sub * kKv4Block < len ? __ldg(table + at) : -1;
+                    place = page >= 0 && page < a.n_pages ? (page * a.c.n_k + head) * subs + sub - at * subs : -1;
+                }
+                const int at = __shfl_sync(0xffffffffu, place, (j % 8) * kKtBlocks + lane % kKtBlocks), slot = j % kKtRaw;
+                const bool there = lane < kKtBlocks && at >= 0;
+                const uint32_t which = __ballot_sync(0xffffffffu, there), bar = smem_u32(&raw_full[slot]);
+                pa_wait(smem_u32(&raw_empty[slot]), ((uint32_t)(j / kKtRaw) & 1u) ^ 1u, &abort_flag, a.st);
+                __syncwarp();
+                if (lane == 0) {
+                    present[j % kKtPresent] = which;
+                    mbar_expect_tx(bar, __popc(which) * kBytes);
+                }
+                __syncwarp();
+                if (there) bulk_g2s(smem_u32(s_raw + (slot * kKtBlocks + lane) * kBytes), a.c.base + (long long)at * kBytes, kBytes, bar);
+            }
+            // nothing is left on its way when the block ends, an expired wait elsewhere included
+            for (int j = max(0, n - kKtRaw); j < n; ++j) pa_wait(smem_u32(&raw_full[j % kKtRaw]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
+        } else if (warp >= 12) {
+            const int first = warp - 12, hi = lane >> 2, lo = lane & 3;
+            int stage = 0;
+            uint32_t phase = 0;
+            auto unpack = [&](int j, auto values) {
+                constexpr bool V = decltype(values)::value;
+                const int slot = j % kKtRaw, base = (step0 + j) * kPaKeys;
+                if (!V) pa_wait(smem_u32(&raw_full[slot]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
+                else pa_wait(smem_u32(&fac_full[j % kKtFactors]), (uint32_t)(j / kKtFactors) & 1u, &abort_flag, a.st);
+                const uint32_t there = present[j % kKtPresent];
+                unsigned char* tile = s_kv + stage * kStep;
+                float* fac = s_fac + (j % kKtFactors) * 2 * kPaKeys;
+                uint32_t w[kKtGroups][W];
+#pragma unroll
+                for (int i = 0; i < kKtGroups; ++i) {
+                    const int g8 = first + kKtUnpack * i;
+                    const unsigned char* at = s_raw + (slot * kKtBlocks + (g8 >> 1)) * kBytes + (V ? 8 * D : 0) + (g8 & 1) * 4 * D + lane * (D / 8);
+                    if constexpr (D == 128) *reinterpret_cast<uint4*>(w[i]) = *reinterpret_cast<const uint4*>(at);
+                    else *reinterpret_cast<uint2*>(w[i]) = *reinterpret_cast<const uint2*>(at);
+                }
+                if constexpr (!V) {
+                    // token hi, chunks 4 k + lo; and both factors of the token
+                    uint32_t pk[kKtGroups][NG];
+                    float up[kKtGroups], top = 0.f;
+#pragma unroll
+                    for (int i = 0; i < kKtGroups; ++i) {
+                        const int g8 = first + kKtUnpack * i, token = g8 * 8 + hi;
+                        const uint32_t* pairs = reinterpret_cast<const uint32_t*>(s_raw + (slot * kKtBlocks + (g8 >> 1)) * kBytes + 16 * D) + (g8 & 1) * 8 + hi;
+                        const bool real = (there >> (g8 >> 1) & 1u) && base + token < len;
+                        uint32_t pv[NG];
+#pragma unroll
+                        for (int k = 0; k < NG; ++k) {
+                            pk[i][k] = real ? pairs[k * 16] : 0u;
+                            pv[k] = real ? pairs[(NG + k) * 16] : 0u;
+                        }
+                        const KtPower pw = KtPower::of<T, NG>(pk[i]), vw = KtPower::of<T, NG>(pv);
+                        if (lo == 0) {
+                            fac[token] = pw.back;
+                            fac[kPaKeys + token] = vw.back;
+                        }
+                        up[i] = pw.up;
+                        top = fmaxf(top, vw.back);
+                    }
+                    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+                    if (lane == 0) s_top[j % kKtFactors][first] = top;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&fac_full[j % kKtFactors]));
+                    pa_wait(smem_u32(&kv_empty[stage]), phase ^ 1u, &abort_flag, a.st);
+#pragma unroll
+                    for (int i = 0; i < kKtGroups; ++i)
+#pragma unroll
+                        for (int k = 0; k < W; ++k) {
+                            const float2 p = kv4_pair<T>(pk[i][k * NG / W]);
+                            const uint4 v = kt_values(w[i][k], half_pair(p.x * up[i], p.x * up[i]), half_pair(p.y * up[i], p.y * up[i]));
+                            *reinterpret_cast<uint4*>(tile + kt_chunk((first + kKtUnpack * i) * 8 + hi, 4 * k + lo, kPaKeys)) = v;
+                        }
+                } else {
+                    pa_wait(smem_u32(&kv_empty[stage]), phase ^ 1u, &abort_flag, a.st);
+                    // place hi of tokens 2 lo and 2 lo + 1
+#pragma unroll
+                    for (int i = 0; i < kKtGroups; ++i)
+#pragma unroll
+                        for (int s = 0; s < 2; ++s) {
+                            const int g8 = first + kKtUnpack * i, token = g8 * 8 + 2 * lo + s;
+                            const uint32_t* pairs = reinterpret_cast<const uint32_t*>(s_raw + (slot * kKtBlocks + (g8 >> 1)) * kBytes + 16 * D) + (g8 & 1) * 8 + 2 * lo + s;
+                            const bool real = (there >> (g8 >> 1) & 1u) && base + token < len;
+                            const float up = __uint_as_float((254u << 23) - __float_as_uint(fac[kPaKeys + token]));
+#pragma unroll
+                            for (int k = 0; k < W; k += 2) {
+                                const float2 p = kv4_pair<T>(real ? pairs[(NG + k * NG / W) * 16] : 0u), q = kv4_pair<T>(real ? pairs[(NG + (k + 1) * NG / W) * 16] : 0u);
+                                const uint4 v = kt_values(__byte_perm(w[i][k], w[i][k + 1], s ? 0x7632 : 0x5410), half_pair(p.x * up, q.x * up), half_pair(p.y * up, q.y * up));
+                                *reinterpret_cast<uint4*>(tile + kt_chunk(token, hi * (W / 2) + k / 2, kPaKeys)) = v;
+                            }
+                        }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // written here, read by the MMAs
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(smem_u32(&kv_full[stage]));
+                    if (V) mbar_arrive(smem_u32(&raw_empty[slot]));
+                }
+                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            };
+            if (n > 0) unpack(0, std::false_type{});
+            if (n > 1) unpack(1, std::false_type{});
+            for (int j = 0; j < n; ++j) {
+                unpack(j, std::true_type{});
+                if (j + 2 < n) unpack(j + 2, std::false_type{});
+            }
+        } else if (warp == 8 || warp == 9) {
+            // the MMAs of tile t, as in prompt_attention_kernel
+            const int t = warp - 8, nt = t ? n1 : n0;
+            constexpr uint32_t kBase = (1u << 4) | (8u << 24);
+            constexpr uint32_t idesc_s = kBase | ((uint32_t)(kPaKeys / 8) << 17), idesc_o = kBase | (1u << 16) | ((uint32_t)(D / 8) << 17);
+            const uint32_t q = pa_desc_k(smem_u32(smem) + t * kTile), kv = smem_u32(s_kv), ts = tmem + t * 128, to = tmem + 256 + t * 128;
+            int stage = 0;
+            uint32_t phase = 0;
+            auto full = [&]() { pa_wait(smem_u32(&kv_full[stage]), phase, &abort_flag, a.st); };
+            auto next = [&]() {
+                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            };
+            auto scores = [&](int j) {
+                full();
+                if (j < nt) {
+                    tc_fence_after();
+                    if (pa_elect()) {
+                        const uint32_t k = pa_desc_k(kv + stage * kStep), to_s = ts + (j & 1) * kPaKeys;
+                        pa_mma_ss<false>(to_s, q, k, idesc_s);
+#pragma unroll
+                        for (int kk = 1; kk < DB * 4; ++kk) pa_mma_ss<true>(to_s, q + (kk >> 2) * (kPaRows / 16) + (kk & 3) * 2, k + (kk >> 2) * (kPaBlock / 16) + (kk & 3) * 2, idesc_s);
+                        tc_commit(smem_u32(&s_full[t * 2 + (j & 1)]));
+                        tc_commit(smem_u32(&kv_empty[stage]));
+                    }
+                } else if (lane == 0) {
+                    mbar_arrive(smem_u32(&kv_empty[stage]));
+                }
+                next();
+            };
+            if (n > 0) pa_wait(smem_u32(&q_full), 0, &abort_flag, a.st);
+            if (n > 0) scores(0);
+            if (n > 1) scores(1);
+            for (int j = 0; j < n; ++j) {
+                full();
+                if (j < nt) {
+                    const int buf = j & 1;
+                    pa_wait(smem_u32(&p_full[t * 2 + buf]), (uint32_t)(j >> 1) & 1u, &abort_flag, a.st);
+                    tc_fence_after();
+                    if (pa_elect()) {
+                        const uint32_t v = pa_desc_n(kv + stage * kStep), p = ts + buf * kPaKeys;
+                        if (j == 0) pa_mma_ts<false>(to, p, v, idesc_o);
+                        else pa_mma_ts<true>(to, p, v, idesc_o);
+#pragma unroll
+                        for (int kk = 1; kk < kPaKeys / 16; ++kk) pa_mma_ts<true>(to, p + kk * 8, v + kk * 128, idesc_o);
+                        tc_commit(smem_u32(&pv_done[t * 2 + buf]));
+                        tc_commit(smem_u32(&kv_empty[stage]));
+                    }
+                } else if (lane == 0) {
+                    mbar_arrive(smem_u32(&kv_empty[stage]));
+                }
+                next();
+                if (j + 2 < n) scores(j + 2);
+            }
+            if (nt > 0) pa_wait(smem_u32(&pv_done[t * 2 + ((nt - 1) & 1)]), (uint32_t)((nt - 1) >> 1) & 1u, &abort_flag, a.st);
         }
     }
     tc_fence_before();
