@@ -1,10 +1,11 @@
 // Attention of many rows (the nodes of draft trees, times the heads of a group) over the 4-bit cache, on the 5th-generation tensor cores: the
 // products of prompt_attention.cuh, two tiles of 128 rows a block, with keys and values unpacked by eight warps instead of copied.
 //   * a warp brings the packed blocks of 64 tokens a step into a ring of their own, one bulk copy each,
-//   * eight warps turn them into fp16 tiles, low + step code, each token times a power of two that brings its largest value to
-//     2^14..2^15; the powers, exact, come back in the scores (kf) and in the weights (vf), so a value is rounded once, to 2^-12 of itself,
-//   * a thread of the softmax has a row: S kf c - m in powers of two, P vf to fp16.  The reference m holds the largest vf so far as well,
-//     so that P vf is at most 2^8 whatever the values' size.
+//   * a warp finds the powers of two that bring the step's largest key and value to 2^14..2^15,
+//   * eight warps unpack the step to fp16 tiles, low + step code, times those powers: one rounding, to 2^-12 of a value (and to 2^-39 of the
+//     step's largest, where values differ by more than 2^28),
+//   * a thread of the softmax has a row: P = exp2(S c kf - m) in fp16, with the step's key power kf in the factor and its value power in the
+//     reference m, which so follows the largest score and the largest value; P stays below 2^15 whatever the values' size.
 // Columns lie in another order than in memory: 0 4 1 5 2 6 3 7 within eight (queries and keys alike, for the sums it is all one), and
 // place by place for the values (column 8 i + n at n D / 8 + ...), which the outputs undo.
 // What bounds it: see kv4_many_from in the host code for both sides' times.
@@ -14,36 +15,32 @@
 
 namespace coral {
 
-constexpr int kKtUnpack = 8;                       // unpacking warps, which share a step's eight groups of eight tokens
-constexpr int kKtGroups = 8 / kKtUnpack;
+constexpr int kKtUnpack = 8;                       // unpacking warps, eight tokens of a step each
 // Registers a thread: 96 at launch (640 threads); the softmax's two warpgroups take what the other three give up.
 constexpr int kKtRegsMany = 136, kKtRegsFew = 64;
 static_assert(2 * kKtRegsMany + 3 * kKtRegsFew <= 5 * 96, "a split above the launch's registers would wait forever");
-constexpr int kKtThreads = (12 + kKtUnpack) * 32;  // warps 0..7 softmax, 8 and 9 MMAs of a tile each, 10 copies, 12.. unpacking
+constexpr int kKtThreads = (12 + kKtUnpack) * 32;  // warps 0..7 softmax, 8 and 9 MMAs of a tile each, 10 copies, 11 powers, 12.. unpacking
 constexpr int kKtRaw = 4;                          // steps of packed tokens in flight
 constexpr int kKtBlocks = kPaKeys / kKv4Block;     // blocks of 16 tokens a step
-constexpr int kKtFactors = 8;                      // steps whose factors are kept
+constexpr int kKtPowers = 8;                       // steps whose powers are kept
 constexpr int kKtPresent = 16;
 template <int D> constexpr int kKtStages = D == 128 ? 7 : 10;
 template <int D, int NG> constexpr size_t kt_smem_bytes() {
-    return 1024 + (size_t)2 * 128 * D * 2 + (size_t)kKtStages<D> * kPaKeys * D * 2 + (size_t)kKtRaw * kKtBlocks * (kKv4Block * D + 128 * NG) + kKtFactors * kPaKeys * 8;
+    return 1024 + (size_t)2 * 128 * D * 2 + (size_t)kKtStages<D> * kPaKeys * D * 2 + (size_t)kKtRaw * kKtBlocks * (kKv4Block * D + 128 * NG);
 }
 
-// What to multiply a token by, and back: the power of two that brings the largest of |low|, |low + 15 step| to 2^14..2^15.
-struct KtPower {
-    float up, back;
-    template <typename T, int NG>
-    static __device__ __forceinline__ KtPower of(const uint32_t (&pairs)[NG]) {
-        float top = 0.f;
-#pragma unroll
-        for (int i = 0; i < NG; ++i) {
-            const float2 p = kv4_pair<T>(pairs[i]);
-            top = fmaxf(top, fmaxf(fabsf(p.y), fabsf(fmaf(15.f, p.x, p.y))));
-        }
-        const int e = min(max((int)(__float_as_uint(top) >> 23), 16), 254);
-        return KtPower{__uint_as_float((uint32_t)(268 - e) << 23), __uint_as_float((uint32_t)(e - 14) << 23)};
-    }
-};
+// The largest of |low| and |low + 15 step| (a NaN is passed over), and from it the power of two that undoes the one which brings it to
+// 2^14..2^15; that one's bits are kt_inverse's.
+template <typename T>
+__device__ __forceinline__ float kt_largest(float top, uint32_t pair) {
+    const float2 p = kv4_pair<T>(pair);
+    return fmaxf(top, fmaxf(fabsf(p.y), fabsf(fmaf(15.f, p.x, p.y))));
+}
+__device__ __forceinline__ float kt_power(float top) {
+    const int e = min(max((int)(__float_as_uint(top) >> 23), 16), 254);
+    return __uint_as_float((uint32_t)(e - 14) << 23);
+}
+__device__ __forceinline__ float kt_inverse(float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); }
 // A word's eight codes as values, pairs (0,4), (1,5), (2,6), (3,7): step and low as fp16 pairs, one rounding.
 __device__ __forceinline__ uint4 kt_values(uint32_t w, uint32_t step, uint32_t low) {
     uint32_t r[4];
@@ -110,11 +107,10 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
     extern __shared__ unsigned char kt_smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(kt_smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char *s_kv = smem + 2 * kTile, *s_raw = s_kv + STAGES * kStep;
-    float* s_fac = reinterpret_cast<float*>(s_raw + kKtRaw * kKtBlocks * kBytes);           // [step][keys, values][token]
     __shared__ __align__(8) uint64_t q_full, kv_full[STAGES], kv_empty[STAGES], s_full[4], p_full[4], pv_done[4];
-    __shared__ __align__(8) uint64_t raw_full[kKtRaw], raw_empty[kKtRaw], fac_full[kKtFactors];
+    __shared__ __align__(8) uint64_t raw_full[kKtRaw], raw_empty[kKtRaw], power_full[kKtPowers];
     __shared__ uint32_t present[kKtPresent];
-    __shared__ __align__(16) float s_top[kKtFactors][kKtUnpack];
+    __shared__ float2 s_power[kKtPowers];                     // of a step's keys and values
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -133,7 +129,7 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
             mbar_init(smem_u32(&raw_full[i]), 1);
             mbar_init(smem_u32(&raw_empty[i]), kKtUnpack);
         }
-        for (int i = 0; i < kKtFactors; ++i) mbar_init(smem_u32(&fac_full[i]), kKtUnpack);
+        for (int i = 0; i < kKtPowers; ++i) mbar_init(smem_u32(&power_full[i]), 1);
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -173,40 +169,46 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
         const int t = warp >> 2, local = (warp & 3) * 32 + lane, row = row0 + t * 128 + local, nt = t ? n1 : n0;
         const bool live = row < rows;
         const int tok = live ? row / a.G : 0, q_head = head * a.G + row - tok * a.G;
-        const T* q_row = static_cast<const T*>(a.q) + (q0 + tok) * a.ld_q + (long long)(live ? q_head : 0) * D;
-        // the row of operand A: scaled by a power of two, turned round where the scale is negative
-        float c;                                               // from a raw score to powers of two
+        // The warp's 32 rows of operand A, D / 8 threads a row: scaled by a power of two, turned round where the scale is negative.
+        float c = 0.f;                                         // this thread's row: from a raw score to powers of two
         {
-            // twice over the row: registers are short
-            uint32_t big = 0;
-            if (live)
-#pragma unroll 4
-                for (int i = 0; i < D / 8; ++i) {
-                    uint32_t raw[4];
-                    *reinterpret_cast<uint4*>(raw) = reinterpret_cast<const uint4*>(q_row)[i];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float2 f = kv4_pair<T>(raw[k]);
-                        big = max(big, max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu));
-                    }
-                }
-            const int e = q4_exponent(big);
-            const Q4Power up(e), down(-e);
-            c = fabsf(a.scale2) * down.a * down.b;
+            constexpr int L = D / 8, kRows = 32 / L;           // threads a row, rows at a time
+            const int l = lane % L, first = row0 + t * 128 + (warp & 3) * 32;
             const float sign = a.scale2 < 0.f ? -1.f : 1.f;
-#pragma unroll 2
-            for (int i = 0; i < D / 8; ++i) {
-                uint32_t raw[4] = {};
-                if (live) *reinterpret_cast<uint4*>(raw) = reinterpret_cast<const uint4*>(q_row)[i];
+            uint32_t raws[8][4];
+#pragma unroll 1
+            for (int i0 = 0; i0 < L; i0 += 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = first + (i0 + i) * kRows + lane / L, tk = r / a.G;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) raws[i][k] = 0;
+                if (r < rows)
+                    *reinterpret_cast<uint4*>(raws[i]) = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (q0 + tk) * a.ld_q + (long long)(head * a.G + r - tk * a.G) * D + 8 * l);
+            }
+#pragma unroll
+            for (int ii = 0; ii < 8; ++ii) {
+                const int i = i0 + ii, at = i * kRows + lane / L;
+                const uint32_t (&raw)[4] = raws[ii];
                 float f[8];
+                uint32_t big = 0;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const float2 x = kv4_pair<T>(raw[k]);
-                    f[2 * k] = up(x.x) * sign;
-                    f[2 * k + 1] = up(x.y) * sign;
+                    f[2 * k] = x.x;
+                    f[2 * k + 1] = x.y;
+                    big = max(big, max(__float_as_uint(x.x) & 0x7fffffffu, __float_as_uint(x.y) & 0x7fffffffu));
                 }
-                *reinterpret_cast<uint4*>(smem + t * kTile + kt_chunk(local, i, 128)) =
+#pragma unroll
+                for (int o = 1; o < L; o <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
+                const int e = q4_exponent(big), mine = __shfl_sync(0xffffffffu, e, lane % kRows * L);
+                const Q4Power up(e), down(-mine);
+                if (lane / kRows == i) c = fabsf(a.scale2) * down.a * down.b;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) f[k] = up(f[k]) * sign;
+                *reinterpret_cast<uint4*>(smem + t * kTile + kt_chunk((warp & 3) * 32 + at, l, 128)) =
                     make_uint4(half_pair(f[0], f[4]), half_pair(f[1], f[5]), half_pair(f[2], f[6]), half_pair(f[3], f[7]));
+            }
             }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");           // written here, read by the MMAs
@@ -216,33 +218,23 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = tmem + t * 128 + lanes, to = tmem + 256 + t * 128 + lanes;
         const unsigned long long tree = a.tree && live ? __ldg(a.tree + q0 + tok) : 0ull;
-        float m = kNegInf, vtop = 0.f, mc = 0.f;               // reference: of the scores, of the values' factors, and both together
+        float m = kNegInf, mc = 0.f;                           // largest score that moved the reference, and the reference: 2^7 below it
+        int vtop = -1000;                                      // exponent of the largest power of the values: O is in its units
         unsigned long long sum2 = 0;
         float s[kPaKeys];
         uint32_t* sr = reinterpret_cast<uint32_t*>(s);
         for (int j = 0; j < nt; ++j) {
-            const int buf = j & 1, slot = j % kKtFactors, base = (step0 + j) * kPaKeys;
-            pa_wait(smem_u32(&fac_full[slot]), (uint32_t)(j / kKtFactors) & 1u, &abort_flag, a.st);
+            const int buf = j & 1, slot = j % kKtPowers, base = (step0 + j) * kPaKeys;
+            pa_wait(smem_u32(&power_full[slot]), (uint32_t)(j / kKtPowers) & 1u, &abort_flag, a.st);
             pa_wait(smem_u32(&s_full[t * 2 + buf]), (uint32_t)(j >> 1) & 1u, &abort_flag, a.st);
             __syncwarp();
             tc_fence_after();
             const uint32_t at = ts + buf * kPaKeys;
             pa_ld32(at, sr);
             pa_ld32(at + 32, sr + 32);
-            const float4 *kf = reinterpret_cast<const float4*>(s_fac + slot * 2 * kPaKeys), *vf = kf + kPaKeys / 4;
-            const float4 t4 = *reinterpret_cast<const float4*>(s_top[slot]), u4 = *reinterpret_cast<const float4*>(s_top[slot] + 4);
-            const float vnow = fmaxf(fmaxf(fmaxf(t4.x, t4.y), fmaxf(t4.z, t4.w)), fmaxf(fmaxf(u4.x, u4.y), fmaxf(u4.z, u4.w)));
+            const float2 power = s_power[slot];
             const uint32_t there = present[j % kKtPresent];
             pa_ld_wait();
-#pragma unroll
-            for (int i = 0; i < kPaKeys / 4; ++i) {
-                const float4 f = kf[i];
-                const float2 x = halves(mul2(pair_of(s[4 * i], s[4 * i + 1]), pair_of(f.x, f.y))), y = halves(mul2(pair_of(s[4 * i + 2], s[4 * i + 3]), pair_of(f.z, f.w)));
-                s[4 * i] = x.x;
-                s[4 * i + 1] = x.y;
-                s[4 * i + 2] = y.x;
-                s[4 * i + 3] = y.y;
-            }
             if (base + kPaKeys > open || there != (1u << kKtBlocks) - 1) {
                 // which tokens of the step this row sees
                 unsigned long long see = 0;
@@ -267,15 +259,16 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
 #pragma unroll
                 for (int e = 0; e < 4; ++e) m4[e] = i + 4 + e < kPaKeys ? pa_max3(m4[e], s[i + e], s[i + 4 + e]) : fmaxf(m4[e], s[i + e]);
             const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-            const bool moves = top * c > (m == kNegInf ? 0.f : m * c) + 8.f || (m == kNegInf && top > kNegInf);
-            if (__any_sync(0xffffffffu, moves) || vnow > vtop) {
-                const float next = moves ? top : m, vnext = fmaxf(vtop, vnow);
-                const float next_c = (next == kNegInf ? 0.f : next * c) + (float)((int)(__float_as_uint(vnext) >> 23) - 127);
-                const float f = m == kNegInf ? 0.f : exp2_fast(mc - next_c);
+            const float cj = c * power.x, peak = top * cj;
+            const bool moves = peak > (m == kNegInf ? 0.f : m) + 8.f || (m == kNegInf && top > kNegInf);
+            const int v_now = (int)(__float_as_uint(power.y) >> 23) - 127;
+            if (__any_sync(0xffffffffu, moves) || v_now > vtop) {
+                const float next = moves ? peak : m, next_c = (next == kNegInf ? 0.f : next) - 7.f;
+                const float by = m == kNegInf ? 0.f : exp2_fast(mc - next_c), f = v_now > vtop ? by * exp2_fast((float)max(vtop - v_now, -252)) : by;
                 m = next;
                 mc = next_c;
-                vtop = vnext;
-                sum2 = mul2(sum2, pair_of(f, f));
+                vtop = max(vtop, v_now);
+                sum2 = mul2(sum2, pair_of(by, by));
                 if (j > 0) {                                   // O, once the step before is in it
                     pa_wait(smem_u32(&pv_done[t * 2 + (buf ^ 1)]), (uint32_t)((j - 1) >> 1) & 1u, &abort_flag, a.st);
                     __syncwarp();
@@ -292,18 +285,24 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
                     pa_st_wait();
                 }
             }
-            const unsigned long long c2 = pair_of(c, c), m2 = pair_of(-mc, -mc);
+            // The weights with the step's power of the values in O's units, and their sum without it.  Values below 2^-40 of the largest do not
+            // show in fp16 weights of at most 2^15.
+            const int shift = max(v_now - vtop, -40);
+            const float ref = (float)shift - mc, undo = exp2_int(-shift);
+            const unsigned long long c2 = pair_of(cj, cj), m2 = pair_of(ref, ref);
+            unsigned long long here = 0;
             uint32_t p[kPaKeys / 2];
 #pragma unroll
-            for (int i = 0; i < kPaKeys / 4; ++i) {
-                const float4 f = vf[i];
-                const float2 x = halves(fma2(pair_of(s[4 * i], s[4 * i + 1]), c2, m2)), y = halves(fma2(pair_of(s[4 * i + 2], s[4 * i + 3]), c2, m2));
-                const unsigned long long e = pair_of(pa_exp2(x.x), pa_exp2(x.y)), g = pair_of(pa_exp2(y.x), pa_exp2(y.y));
-                sum2 = add2(sum2, add2(e, g));
-                const float2 u = halves(mul2(e, pair_of(f.x, f.y))), v = halves(mul2(g, pair_of(f.z, f.w)));
-                p[2 * i] = half_pair(u.x, u.y);
-                p[2 * i + 1] = half_pair(v.x, v.y);
+            for (int i = 0; i < kPaKeys / 2; ++i) {
+                const float2 x = halves(fma2(pair_of(s[2 * i], s[2 * i + 1]), c2, m2));
+                const float lo = pa_exp2(x.x), hi = pa_exp2(x.y);
+                here = add2(here, pair_of(lo, hi));
+                p[i] = half_pair(lo, hi);
             }
+            if (v_now - vtop < -40)
+#pragma unroll
+                for (int i = 0; i < kPaKeys / 2; ++i) p[i] = 0;
+            sum2 = fma2(here, pair_of(undo, undo), sum2);
             pa_st32(at, p);
             pa_st_wait();
             tc_fence_before();
@@ -314,6 +313,7 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
         const float sum = sums.x + sums.y;
         const bool whole = a.splits == 1;
         const float inv = sum == 0.f ? 0.f : whole ? 1.f / sum : 1.f;
+        const Q4Power units(nt > 0 ? vtop : 0);
         if (nt > 0) {
             pa_wait(smem_u32(&pv_done[t * 2 + ((nt - 1) & 1)]), (uint32_t)((nt - 1) >> 1) & 1u, &abort_flag, a.st);
             __syncwarp();
@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
                 float x[kCols];
 #pragma unroll
                 for (int k = 0; k < kCols; ++k) {
-                    x[k] = sum == 0.f ? 0.f : __uint_as_float(o[k * kPlaces + (i & ~7) + ((i & 3) * 2 + (i >> 2 & 1))]) * inv;
+                    x[k] = sum == 0.f ? 0.f : units(__uint_as_float(o[k * kPlaces + (i & ~7) + ((i & 3) * 2 + (i >> 2 & 1))])) * inv;
                     odd = fmaf(x[k], 0.f, odd);
                 }
                 const int col = 8 * i + b * kCols;
@@ -397,82 +397,84 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
             }
             // nothing is left on its way when the block ends, an expired wait elsewhere included
             for (int j = max(0, n - kKtRaw); j < n; ++j) pa_wait(smem_u32(&raw_full[j % kKtRaw]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
+        } else if (warp == 11) {
+            for (int j = 0; j < n; ++j) {
+                const int slot = j % kKtRaw;
+                pa_wait(smem_u32(&raw_full[slot]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
+                const uint32_t there = present[j % kKtPresent];
+                float top_k = 0.f, top_v = 0.f;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int token = lane + 32 * i;
+                    const uint32_t* pairs = reinterpret_cast<const uint32_t*>(s_raw + (slot * kKtBlocks + (token >> 4)) * kBytes + 16 * D) + (token & 15);
+                    if (!(there >> (token >> 4) & 1u) || (step0 + j) * kPaKeys + token >= len) continue;
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        top_k = kt_largest<T>(top_k, pairs[g * 16]);
+                        top_v = kt_largest<T>(top_v, pairs[(NG + g) * 16]);
+                    }
+                }
+                top_k = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top_k)));
+                top_v = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top_v)));
+                if (lane == 0) {
+                    s_power[j % kKtPowers] = make_float2(kt_power(top_k), kt_power(top_v));
+                    mbar_arrive(smem_u32(&power_full[j % kKtPowers]));
+                }
+            }
         } else if (warp >= 12) {
-            const int first = warp - 12, hi = lane >> 2, lo = lane & 3;
+            const int g8 = warp - 12, b = g8 >> 1, h = g8 & 1, hi = lane >> 2, lo = lane & 3;     // this warp's eight tokens of a step
             int stage = 0;
             uint32_t phase = 0;
             auto unpack = [&](int j, auto values) {
                 constexpr bool V = decltype(values)::value;
-                const int slot = j % kKtRaw, base = (step0 + j) * kPaKeys;
-                if (!V) pa_wait(smem_u32(&raw_full[slot]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
-                else pa_wait(smem_u32(&fac_full[j % kKtFactors]), (uint32_t)(j / kKtFactors) & 1u, &abort_flag, a.st);
-                const uint32_t there = present[j % kKtPresent];
+                const int slot = j % kKtRaw, base = (step0 + j) * kPaKeys + g8 * 8;
+                if (!V) {
+                    pa_wait(smem_u32(&raw_full[slot]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
+                    pa_wait(smem_u32(&power_full[j % kKtPowers]), (uint32_t)(j / kKtPowers) & 1u, &abort_flag, a.st);
+                }
+                const float2 power = s_power[j % kKtPowers];
+                const float up = kt_inverse(V ? power.y : power.x);
+                const int real = present[j % kKtPresent] >> b & 1u ? len - base : 0;      // tokens of the eight that there are
                 unsigned char* tile = s_kv + stage * kStep;
-                float* fac = s_fac + (j % kKtFactors) * 2 * kPaKeys;
-                uint32_t w[kKtGroups][W];
-#pragma unroll
-                for (int i = 0; i < kKtGroups; ++i) {
-                    const int g8 = first + kKtUnpack * i;
-                    const unsigned char* at = s_raw + (slot * kKtBlocks + (g8 >> 1)) * kBytes + (V ? 8 * D : 0) + (g8 & 1) * 4 * D + lane * (D / 8);
-                    if constexpr (D == 128) *reinterpret_cast<uint4*>(w[i]) = *reinterpret_cast<const uint4*>(at);
-                    else *reinterpret_cast<uint2*>(w[i]) = *reinterpret_cast<const uint2*>(at);
-                }
+                const unsigned char* blk = s_raw + (slot * kKtBlocks + b) * kBytes;
+                const uint32_t* pairs = reinterpret_cast<const uint32_t*>(blk + 16 * D) + h * 8 + (V ? NG * 16 : 0);
+                const unsigned char* at = blk + (V ? 8 * D : 0) + h * 4 * D + lane * (D / 8);
+                uint32_t w[W];
+                if constexpr (D == 128) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(at);
+                else *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(at);
                 if constexpr (!V) {
-                    // token hi, chunks 4 k + lo; and both factors of the token
-                    uint32_t pk[kKtGroups][NG];
-                    float up[kKtGroups], top = 0.f;
+                    // token hi, chunks 4 k + lo
+                    uint32_t step[NG], low[NG];
 #pragma unroll
-                    for (int i = 0; i < kKtGroups; ++i) {
-                        const int g8 = first + kKtUnpack * i, token = g8 * 8 + hi;
-                        const uint32_t* pairs = reinterpret_cast<const uint32_t*>(s_raw + (slot * kKtBlocks + (g8 >> 1)) * kBytes + 16 * D) + (g8 & 1) * 8 + hi;
-                        const bool real = (there >> (g8 >> 1) & 1u) && base + token < len;
-                        uint32_t pv[NG];
-#pragma unroll
-                        for (int k = 0; k < NG; ++k) {
-                            pk[i][k] = real ? pairs[k * 16] : 0u;
-                            pv[k] = real ? pairs[(NG + k) * 16] : 0u;
-                        }
-                        const KtPower pw = KtPower::of<T, NG>(pk[i]), vw = KtPower::of<T, NG>(pv);
-                        if (lo == 0) {
-                            fac[token] = pw.back;
-                            fac[kPaKeys + token] = vw.back;
-                        }
-                        up[i] = pw.up;
-                        top = fmaxf(top, vw.back);
+                    for (int i = 0; i < NG; ++i) {
+                        const float2 p = kv4_pair<T>(hi < real ? pairs[i * 16 + hi] : 0u);
+                        step[i] = half_pair(p.x * up, p.x * up);
+                        low[i] = half_pair(p.y * up, p.y * up);
                     }
-                    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
-                    if (lane == 0) s_top[j % kKtFactors][first] = top;
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&fac_full[j % kKtFactors]));
                     pa_wait(smem_u32(&kv_empty[stage]), phase ^ 1u, &abort_flag, a.st);
 #pragma unroll
-                    for (int i = 0; i < kKtGroups; ++i)
-#pragma unroll
-                        for (int k = 0; k < W; ++k) {
-                            const float2 p = kv4_pair<T>(pk[i][k * NG / W]);
-                            const uint4 v = kt_values(w[i][k], half_pair(p.x * up[i], p.x * up[i]), half_pair(p.y * up[i], p.y * up[i]));
-                            *reinterpret_cast<uint4*>(tile + kt_chunk((first + kKtUnpack * i) * 8 + hi, 4 * k + lo, kPaKeys)) = v;
-                        }
+                    for (int k = 0; k < W; ++k) *reinterpret_cast<uint4*>(tile + kt_chunk(g8 * 8 + hi, 4 * k + lo, kPaKeys)) = kt_values(w[k], step[k * NG / W], low[k * NG / W]);
                 } else {
-                    pa_wait(smem_u32(&kv_empty[stage]), phase ^ 1u, &abort_flag, a.st);
                     // place hi of tokens 2 lo and 2 lo + 1
+                    uint32_t step[2][W / 2], low[2][W / 2];
 #pragma unroll
-                    for (int i = 0; i < kKtGroups; ++i)
+                    for (int s = 0; s < 2; ++s)
 #pragma unroll
-                        for (int s = 0; s < 2; ++s) {
-                            const int g8 = first + kKtUnpack * i, token = g8 * 8 + 2 * lo + s;
-                            const uint32_t* pairs = reinterpret_cast<const uint32_t*>(s_raw + (slot * kKtBlocks + (g8 >> 1)) * kBytes + 16 * D) + (g8 & 1) * 8 + 2 * lo + s;
-                            const bool real = (there >> (g8 >> 1) & 1u) && base + token < len;
-                            const float up = __uint_as_float((254u << 23) - __float_as_uint(fac[kPaKeys + token]));
-#pragma unroll
-                            for (int k = 0; k < W; k += 2) {
-                                const float2 p = kv4_pair<T>(real ? pairs[(NG + k * NG / W) * 16] : 0u), q = kv4_pair<T>(real ? pairs[(NG + (k + 1) * NG / W) * 16] : 0u);
-                                const uint4 v = kt_values(__byte_perm(w[i][k], w[i][k + 1], s ? 0x7632 : 0x5410), half_pair(p.x * up, q.x * up), half_pair(p.y * up, q.y * up));
-                                *reinterpret_cast<uint4*>(tile + kt_chunk(token, hi * (W / 2) + k / 2, kPaKeys)) = v;
-                            }
+                        for (int k = 0; k < W; k += 2) {
+                            const bool on = 2 * lo + s < real;
+                            const float2 p = kv4_pair<T>(on ? pairs[k * NG / W * 16 + 2 * lo + s] : 0u), q = kv4_pair<T>(on ? pairs[(k + 1) * NG / W * 16 + 2 * lo + s] : 0u);
+                            step[s][k / 2] = half_pair(p.x * up, q.x * up);
+                            low[s][k / 2] = half_pair(p.y * up, q.y * up);
                         }
+                    pa_wait(smem_u32(&kv_empty[stage]), phase ^ 1u, &abort_flag, a.st);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int k = 0; k < W; k += 2)
+                            *reinterpret_cast<uint4*>(tile + kt_chunk(g8 * 8 + 2 * lo + s, hi * (W / 2) + k / 2, kPaKeys)) =
+                                kt_values(__byte_perm(w[k], w[k + 1], s ? 0x7632 : 0x5410), step[s][k / 2], low[s][k / 2]);
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // written here, read by the MMAs
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // written here, read by the MMAs
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(smem_u32(&kv_full[stage]));
