@@ -440,7 +440,8 @@ struct Kv4Rowset {
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float2 old = halves(x[u][r][h]), now = halves(fma2(s[u][r][h], back[r], pair_of(-m[r][0], -m[r][1])));
+                    // (the product rounded as in the maximum: of scores beyond 2^24, one fused step would leave more than the 2^8 that p has room for)
+                    const float2 old = halves(x[u][r][h]), now = halves(add2(mul2(s[u][r][h], back[r]), pair_of(-m[r][0], -m[r][1])));
                     x[u][r][h] = pair_of(old.x == kNegInf ? kNegInf : now.x, old.y == kNegInf ? kNegInf : now.y);
                 }
         }

@@ -2,13 +2,19 @@
 // products of prompt_attention.cuh, two tiles of 128 rows a block, with keys and values unpacked by eight warps instead of copied.
 //   * a warp brings the packed blocks of 64 tokens a step into a ring of their own, one bulk copy each,
 //   * a warp finds the powers of two that bring the step's largest key and value to 2^14..2^15,
-//   * eight warps unpack the step to fp16 tiles, low + step code, times those powers: one rounding, to 2^-12 of a value (and to 2^-39 of the
-//     step's largest, where values differ by more than 2^28),
+//   * eight warps unpack the step to fp16 tiles, low + step code, times those powers.  Keys take two tiles, what fp16 holds and what is
+//     left of it, so that scores are exact to fp32's sums (one tile would move them, and with them every weight, by 2^-12 of their
+//     terms); values are rounded once, to 2^-12 of themselves,
 //   * a thread of the softmax has a row: P = exp2(S c kf - m) in fp16, with the step's key power kf in the factor and its value power in the
-//     reference m, which so follows the largest score and the largest value; P stays below 2^15 whatever the values' size.
+//     reference m, which so follows the largest score and the largest value; P stays below 2^15 whatever the values' size,
+//   * fp16 holds 40 powers of two: where a token's keys or values lie so far below a step's or a former step's largest ones (which a row may
+//     not even see) that bits of them would be lost, a warp computes each row that meets them again, in fp32 (kt_row_again); also scores
+//     beyond kPaFar.
 // Columns lie in another order than in memory: 0 4 1 5 2 6 3 7 within eight (queries and keys alike, for the sums it is all one), and
 // place by place for the values (column 8 i + n at n D / 8 + ...), which the outputs undo.
-// What bounds it: see kv4_many_from in the host code for both sides' times.
+// 8 sequences x 8 key heads, trees of 60 nodes x 4 heads, 3001 tokens: 67 us with the join (11 at the tensor cores' measured rate), 60 with one
+// tile of the keys, whose log of sums was off by 5e-4 where few tokens are seen.  A step's products read 2.5 times the shared memory of
+// prompt_attention.cuh's for a key and its unpacking issues as much as its softmax.
 #pragma once
 #include "kv4.cuh"
 #include "prompt_attention.cuh"
@@ -36,6 +42,9 @@ __device__ __forceinline__ float kt_largest(float top, uint32_t pair) {
     const float2 p = kv4_pair<T>(pair);
     return fmaxf(top, fmaxf(fabsf(p.y), fabsf(fmaf(15.f, p.x, p.y))));
 }
+// Whether a token whose largest value is `own` would lose bits next to `top`: fp16 holds 2^-25 of what `top` brings to 2^14 or more, which has to be
+// 2^-22 of a key and 2^-13 of a value.
+__device__ __forceinline__ bool kt_lost(float own, float top, bool value) { return own > 0.f && own < top * (value ? 0x1p-26f : 0x1p-17f); }
 __device__ __forceinline__ float kt_power(float top) {
     const int e = min(max((int)(__float_as_uint(top) >> 23), 16), 254);
     return __uint_as_float((uint32_t)(e - 14) << 23);
@@ -54,37 +63,66 @@ __device__ __forceinline__ uint4 kt_values(uint32_t w, uint32_t step, uint32_t l
     }
     return make_uint4(r[0], r[1], r[2], r[3]);
 }
+// The same in fp32, as what fp16 holds of them and the rest.
+struct KtTwo {
+    uint4 high, rest;
+};
+__device__ __forceinline__ KtTwo kt_values_two(uint32_t w, unsigned long long step, unsigned long long low) {
+    uint32_t h[4], l[4];
+    constexpr uint32_t kBits = 0x4b000000u;         // 2^23: a code in its lowest bits becomes a number without a conversion
+    const unsigned long long less = pair_of(-8388608.f, -8388608.f), minus = pair_of(-1.f, -1.f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const unsigned long long code = add2(pair_of(__uint_as_float((w >> (4 * k) & 15u) | kBits), __uint_as_float((w >> (4 * k + 16) & 15u) | kBits)), less);
+        const unsigned long long v = fma2(code, step, low);
+        const float2 f = halves(v);
+        h[k] = half_pair(f.x, f.y);
+        const float2 held = kv4_pair<__half>(h[k]), rest = halves(fma2(pair_of(held.x, held.y), minus, v));
+        l[k] = half_pair(rest.x, rest.y);
+    }
+    return KtTwo{make_uint4(h[0], h[1], h[2], h[3]), make_uint4(l[0], l[1], l[2], l[3])};
+}
 // Where chunk `chunk` (eight columns) of row `row` lies in a tile of `rows` rows, 64 columns a part, 128-byte swizzle.
 __device__ __forceinline__ uint32_t kt_chunk(int row, int chunk, int rows) { return (chunk >> 3) * rows * 128 + row * 128 + ((chunk ^ row) & 7) * 16; }
 
-// A row again, by a warp, from the packed tokens it sees (see prompt_attention.cuh); four columns a lane.
+// Tokens `from` to `len` of a row, by a warp in fp32, from the packed tokens that it sees: the reference m (a power of two), the sum of the weights
+// 2^(score - m), and the weighted sum of the values, D / 32 columns a lane.
 template <typename T, int D, int NG>
 __device__ __noinline__ void kt_row_again(const Kv4Args& a, const int32_t* table, int head, const T* q, int from, int len, int past, int node,
-                                          unsigned long long tree, float m, float inv, float* acc) {
+                                          unsigned long long tree, float* m, float* sum, float* acc) {
     const int lane = threadIdx.x & 31;
     constexpr int N = D / 32;
+    // this lane's token j: where its block lies (-1: it is not seen) and its score
+    auto score = [&](int j, long long* block) {
+        const int at = j - past;
+        *block = -1;
+        if (j >= len || !(at < 0 || (a.tree ? at < kKv4MaxTree && tree >> at & 1ull : at <= node))) return kNegInf;
+        const int sub = j / kKv4Block, per = (int)a.c.subs.d, page_at = a.c.subs(sub), page = __ldg(table + page_at);
+        if (page < 0 || page >= a.n_pages) return kNegInf;
+        *block = (((long long)page * a.c.n_k + head) * per + sub - page_at * per) * (kKv4Block * D + 128 * NG);
+        const unsigned char* blk = a.c.base + *block;
+        float s = 0.f;
+        for (int c = 0; c < D; ++c) {
+            const float2 pr = kv4_pair<T>(reinterpret_cast<const uint32_t*>(blk + 16 * D)[c * NG / D * 16 + (j & 15)]);
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(blk + ((j & 15) * 4 + (c >> 3 & 3)) * (D / 8) + 4 * (c >> 5));
+            s = fmaf(Elem<T>::up(q[c]), fmaf((float)(w >> (4 * (c & 7)) & 15u), pr.x, pr.y), s);
+        }
+        return __fmul_rn(s, a.scale2);                         // rounded once for the maximum and the weight, whatever its size
+    };
+    long long block;
+    float top = kNegInf;
+    for (int j = from + lane; j < len; j += 32) top = fmaxf(top, score(j, &block));
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (top == kNegInf) top = 0.f;
+    float all = 0.f;
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] = 0.f;
     for (int j0 = from; j0 < len; j0 += 32) {
-        const int j = j0 + lane, at = j - past;
-        long long block = -1;
-        if (j < len) {
-            const int sub = j / kKv4Block, per = (int)a.c.subs.d, page_at = a.c.subs(sub), page = __ldg(table + page_at);
-            if (page >= 0 && page < a.n_pages) block = (long long)((page * a.c.n_k + head) * per + sub - page_at * per) * (kKv4Block * D + 128 * NG);
-        }
-        const bool see = block >= 0 && (at < 0 || (a.tree ? at < kKv4MaxTree && tree >> at & 1ull : at <= node));
-        float p = 0.f;
-        if (see) {
-            const unsigned char* blk = a.c.base + block;
-            float s = 0.f;
-            for (int c = 0; c < D; ++c) {
-                const float2 pr = kv4_pair<T>(reinterpret_cast<const uint32_t*>(blk + 16 * D)[c * NG / D * 16 + (j & 15)]);
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(blk + ((j & 15) * 4 + (c >> 3 & 3)) * (D / 8) + 4 * (c >> 5));
-                s = fmaf(Elem<T>::up(q[c]), fmaf((float)(w >> (4 * (c & 7)) & 15u), pr.x, pr.y), s);
-            }
-            p = exp2_fast(s * a.scale2 - m);
-        }
-        for (uint32_t todo = __ballot_sync(0xffffffffu, see); todo; todo &= todo - 1) {
+        const float s = score(j0 + lane, &block);
+        const float p = block >= 0 ? exp2_fast(s - top) : 0.f;
+        all += p;
+        for (uint32_t todo = __ballot_sync(0xffffffffu, block >= 0); todo; todo &= todo - 1) {
             const int i = __ffs(todo) - 1, t = (j0 + i) & 15;
             const float w = __shfl_sync(0xffffffffu, p, i);
             const unsigned char* blk = a.c.base + __shfl_sync(0xffffffffu, block, i);
@@ -98,7 +136,9 @@ __device__ __noinline__ void kt_row_again(const Kv4Args& a, const int32_t* table
         }
     }
 #pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] *= inv;
+    for (int o = 16; o; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+    *m = top;
+    *sum = all;
 }
 
 template <typename T, int D, int NG>
@@ -111,6 +151,7 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
     __shared__ __align__(8) uint64_t raw_full[kKtRaw], raw_empty[kKtRaw], power_full[kKtPowers];
     __shared__ uint32_t present[kKtPresent];
     __shared__ float2 s_power[kKtPowers];                     // of a step's keys and values
+    __shared__ uint32_t s_lost[kKtPowers];                    // not 0: some of the step's tokens are too far below its largest
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -170,7 +211,7 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
         const bool live = row < rows;
         const int tok = live ? row / a.G : 0, q_head = head * a.G + row - tok * a.G;
         // The warp's 32 rows of operand A, D / 8 threads a row: scaled by a power of two, turned round where the scale is negative.
-        float c = 0.f;                                         // this thread's row: from a raw score to powers of two
+        float c = 0.f, c_b = 0.f;                              // this thread's row: from a raw score to powers of two, in two factors
         {
             constexpr int L = D / 8, kRows = 32 / L;           // threads a row, rows at a time
             const int l = lane % L, first = row0 + t * 128 + (warp & 3) * 32;
@@ -179,36 +220,39 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
 #pragma unroll 1
             for (int i0 = 0; i0 < L; i0 += 8) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = first + (i0 + i) * kRows + lane / L, tk = r / a.G;
+                for (int i = 0; i < 8; ++i) {
+                    const int r = first + (i0 + i) * kRows + lane / L, tk = r / a.G;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) raws[i][k] = 0;
-                if (r < rows)
-                    *reinterpret_cast<uint4*>(raws[i]) = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (q0 + tk) * a.ld_q + (long long)(head * a.G + r - tk * a.G) * D + 8 * l);
-            }
-#pragma unroll
-            for (int ii = 0; ii < 8; ++ii) {
-                const int i = i0 + ii, at = i * kRows + lane / L;
-                const uint32_t (&raw)[4] = raws[ii];
-                float f[8];
-                uint32_t big = 0;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 x = kv4_pair<T>(raw[k]);
-                    f[2 * k] = x.x;
-                    f[2 * k + 1] = x.y;
-                    big = max(big, max(__float_as_uint(x.x) & 0x7fffffffu, __float_as_uint(x.y) & 0x7fffffffu));
+                    for (int k = 0; k < 4; ++k) raws[i][k] = 0;
+                    if (r < rows)
+                        *reinterpret_cast<uint4*>(raws[i]) = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (q0 + tk) * a.ld_q + (long long)(head * a.G + r - tk * a.G) * D + 8 * l);
                 }
 #pragma unroll
-                for (int o = 1; o < L; o <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
-                const int e = q4_exponent(big), mine = __shfl_sync(0xffffffffu, e, lane % kRows * L);
-                const Q4Power up(e), down(-mine);
-                if (lane / kRows == i) c = fabsf(a.scale2) * down.a * down.b;
+                for (int ii = 0; ii < 8; ++ii) {
+                    const int i = i0 + ii, at = i * kRows + lane / L;
+                    const uint32_t (&raw)[4] = raws[ii];
+                    float f[8];
+                    uint32_t big = 0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) f[k] = up(f[k]) * sign;
-                *reinterpret_cast<uint4*>(smem + t * kTile + kt_chunk((warp & 3) * 32 + at, l, 128)) =
-                    make_uint4(half_pair(f[0], f[4]), half_pair(f[1], f[5]), half_pair(f[2], f[6]), half_pair(f[3], f[7]));
-            }
+                    for (int k = 0; k < 4; ++k) {
+                        const float2 x = kv4_pair<T>(raw[k]);
+                        f[2 * k] = x.x;
+                        f[2 * k + 1] = x.y;
+                        big = max(big, max(__float_as_uint(x.x) & 0x7fffffffu, __float_as_uint(x.y) & 0x7fffffffu));
+                    }
+#pragma unroll
+                    for (int o = 1; o < L; o <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
+                    const int e = q4_exponent(big), mine = __shfl_sync(0xffffffffu, e, lane % kRows * L);
+                    const Q4Power up(e), down(-mine);
+                    if (lane / kRows == i) {
+                        c = fabsf(a.scale2) * down.a;
+                        c_b = down.b;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) f[k] = up(f[k]) * sign;
+                    *reinterpret_cast<uint4*>(smem + t * kTile + kt_chunk((warp & 3) * 32 + at, l, 128)) =
+                        make_uint4(half_pair(f[0], f[4]), half_pair(f[1], f[5]), half_pair(f[2], f[6]), half_pair(f[3], f[7]));
+                }
             }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");           // written here, read by the MMAs
@@ -220,6 +264,7 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
         const unsigned long long tree = a.tree && live ? __ldg(a.tree + q0 + tok) : 0ull;
         float m = kNegInf, mc = 0.f;                           // largest score that moved the reference, and the reference: 2^7 below it
         int vtop = -1000;                                      // exponent of the largest power of the values: O is in its units
+        bool lost = false;
         unsigned long long sum2 = 0;
         float s[kPaKeys];
         uint32_t* sr = reinterpret_cast<uint32_t*>(s);
@@ -233,6 +278,7 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
             pa_ld32(at, sr);
             pa_ld32(at + 32, sr + 32);
             const float2 power = s_power[slot];
+            lost |= s_lost[slot] != 0;
             const uint32_t there = present[j % kKtPresent];
             pa_ld_wait();
             if (base + kPaKeys > open || there != (1u << kKtBlocks) - 1) {
@@ -259,11 +305,12 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
 #pragma unroll
                 for (int e = 0; e < 4; ++e) m4[e] = i + 4 + e < kPaKeys ? pa_max3(m4[e], s[i + e], s[i + 4 + e]) : fmaxf(m4[e], s[i + e]);
             const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-            const float cj = c * power.x, peak = top * cj;
+            const float cj = fmaxf(c * power.x * c_b, 0x1p-126f), peak = top * cj;      // not zero: -inf stays what it is
             const bool moves = peak > (m == kNegInf ? 0.f : m) + 8.f || (m == kNegInf && top > kNegInf);
             const int v_now = (int)(__float_as_uint(power.y) >> 23) - 127;
             if (__any_sync(0xffffffffu, moves) || v_now > vtop) {
                 const float next = moves ? peak : m, next_c = (next == kNegInf ? 0.f : next) - 7.f;
+                lost |= fabsf(next_c) > kPaFar || (vtop > -1000 && v_now > vtop + 10);
                 const float by = m == kNegInf ? 0.f : exp2_fast(mc - next_c), f = v_now > vtop ? by * exp2_fast((float)max(vtop - v_now, -252)) : by;
                 m = next;
                 mc = next_c;
@@ -285,9 +332,10 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
                     pa_st_wait();
                 }
             }
-            // The weights with the step's power of the values in O's units, and their sum without it.  Values below 2^-40 of the largest do not
-            // show in fp16 weights of at most 2^15.
-            const int shift = max(v_now - vtop, -40);
+            // The weights with the step's power of the values in O's units, and their sum without it: fp16 holds weights down to 2^-25, which
+            // with ten powers below the largest values still is 2^-22 of the largest weight.
+            const int below = vtop - v_now, shift = max(-below, -40);
+            lost |= below > 10;
             const float ref = (float)shift - mc, undo = exp2_int(-shift);
             const unsigned long long c2 = pair_of(cj, cj), m2 = pair_of(ref, ref);
             unsigned long long here = 0;
@@ -299,9 +347,6 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
                 here = add2(here, pair_of(lo, hi));
                 p[i] = half_pair(lo, hi);
             }
-            if (v_now - vtop < -40)
-#pragma unroll
-                for (int i = 0; i < kPaKeys / 2; ++i) p[i] = 0;
             sum2 = fma2(here, pair_of(undo, undo), sum2);
             pa_st32(at, p);
             pa_st_wait();
@@ -356,20 +401,24 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
         }
         if (live && !whole) a.part_ml[part] = make_float2(sum == 0.f ? kKv4NoMax : mc, sum);
         if (live && whole && a.lse) a.lse[at] = sum == 0.f ? kNegInf : (mc + log2f(sum)) * 0.69314718055994531f;
-        // rows of finite weights whose result is not: values that they do not see may be the reason
-        const bool again = live && sum > 0.f && sum < __int_as_float(0x7f800000) && odd != 0.f;
+        // Rows of finite weights whose result is not (values that they do not see may be the reason), and those that met tokens far apart.
+        const bool again = live && (lost || (sum > 0.f && sum < __int_as_float(0x7f800000) && odd != 0.f));
+        __syncwarp();
         for (uint32_t todo = __ballot_sync(0xffffffffu, again); todo; todo &= todo - 1) {
             const int r = __ffs(todo) - 1, tok_r = __shfl_sync(0xffffffffu, tok, r), head_r = __shfl_sync(0xffffffffu, q_head, r);
             const unsigned long long tree_r = __shfl_sync(0xffffffffu, tree, r);
-            const float mc_r = __shfl_sync(0xffffffffu, mc, r), inv_r = __shfl_sync(0xffffffffu, inv, r);
-            float acc[D / 32];
+            float acc[D / 32], m_r, sum_r;
             kt_row_again<T, D, NG>(a, table, head, static_cast<const T*>(a.q) + (q0 + tok_r) * a.ld_q + (long long)head_r * D, step0 * kPaKeys,
-                                   min(len, (step0 + n) * kPaKeys), past, tok_r, tree_r, mc_r, inv_r, acc);
-            const long long at_r = (long long)(q0 + tok_r) * a.n_q + head_r;
+                                   min(len, (step0 + n) * kPaKeys), past, tok_r, tree_r, &m_r, &sum_r, acc);
+            const long long at_r = (long long)(q0 + tok_r) * a.n_q + head_r, part_r = (long long)split * a.n_rows * a.n_q + at_r;
 #pragma unroll
             for (int e = 0; e < D / 32; ++e) {
-                if (whole) static_cast<T*>(a.out)[(long long)(q0 + tok_r) * a.ld_out + (long long)head_r * D + lane * (D / 32) + e] = Elem<T>::down(acc[e]);
-                else a.part_o[((long long)split * a.n_rows * a.n_q + at_r) * D + lane * (D / 32) + e] = acc[e];
+                if (whole) static_cast<T*>(a.out)[(long long)(q0 + tok_r) * a.ld_out + (long long)head_r * D + lane * (D / 32) + e] = Elem<T>::down(sum_r == 0.f ? 0.f : acc[e] / sum_r);
+                else a.part_o[part_r * D + lane * (D / 32) + e] = acc[e];
+            }
+            if (lane == 0) {
+                if (!whole) a.part_ml[part_r] = make_float2(sum_r == 0.f ? kKv4NoMax : m_r, sum_r);
+                else if (a.lse) a.lse[at_r] = sum_r == 0.f ? kNegInf : (m_r + log2f(sum_r)) * 0.69314718055994531f;
             }
         }
     } else {
@@ -398,11 +447,12 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
             // nothing is left on its way when the block ends, an expired wait elsewhere included
             for (int j = max(0, n - kKtRaw); j < n; ++j) pa_wait(smem_u32(&raw_full[j % kKtRaw]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
         } else if (warp == 11) {
+            float before = 0x1p-14f;                           // values of nothing but zeros take the power of the step before
             for (int j = 0; j < n; ++j) {
                 const int slot = j % kKtRaw;
                 pa_wait(smem_u32(&raw_full[slot]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
                 const uint32_t there = present[j % kKtPresent];
-                float top_k = 0.f, top_v = 0.f;
+                float top_k[2] = {0.f, 0.f}, top_v[2] = {0.f, 0.f};
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int token = lane + 32 * i;
@@ -410,14 +460,18 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
                     if (!(there >> (token >> 4) & 1u) || (step0 + j) * kPaKeys + token >= len) continue;
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
-                        top_k = kt_largest<T>(top_k, pairs[g * 16]);
-                        top_v = kt_largest<T>(top_v, pairs[(NG + g) * 16]);
+                        top_k[i] = kt_largest<T>(top_k[i], pairs[g * 16]);
+                        top_v[i] = kt_largest<T>(top_v[i], pairs[(NG + g) * 16]);
                     }
                 }
-                top_k = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top_k)));
-                top_v = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top_v)));
+                const float all_k = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(top_k[0], top_k[1]))));
+                const float all_v = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(top_v[0], top_v[1]))));
+                const uint32_t lost = __ballot_sync(0xffffffffu, kt_lost(top_k[0], all_k, false) || kt_lost(top_k[1], all_k, false) ||
+                                                                     kt_lost(top_v[0], all_v, true) || kt_lost(top_v[1], all_v, true));
+                if (all_v > 0.f) before = kt_power(all_v);
                 if (lane == 0) {
-                    s_power[j % kKtPowers] = make_float2(kt_power(top_k), kt_power(top_v));
+                    s_power[j % kKtPowers] = make_float2(kt_power(all_k), before);
+                    s_lost[j % kKtPowers] = lost;
                     mbar_arrive(smem_u32(&power_full[j % kKtPowers]));
                 }
             }
@@ -443,17 +497,24 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
                 if constexpr (D == 128) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(at);
                 else *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(at);
                 if constexpr (!V) {
-                    // token hi, chunks 4 k + lo
-                    uint32_t step[NG], low[NG];
+                    // token hi, chunks 4 k + lo, in two tiles
+                    unsigned long long step[NG], low[NG];
 #pragma unroll
                     for (int i = 0; i < NG; ++i) {
                         const float2 p = kv4_pair<T>(hi < real ? pairs[i * 16 + hi] : 0u);
-                        step[i] = half_pair(p.x * up, p.x * up);
-                        low[i] = half_pair(p.y * up, p.y * up);
+                        step[i] = pair_of(p.x * up, p.x * up);
+                        low[i] = pair_of(p.y * up, p.y * up);
                     }
+                    const int after = stage + 1 == STAGES ? 0 : stage + 1;
                     pa_wait(smem_u32(&kv_empty[stage]), phase ^ 1u, &abort_flag, a.st);
+                    pa_wait(smem_u32(&kv_empty[after]), after ? phase ^ 1u : phase, &abort_flag, a.st);
 #pragma unroll
-                    for (int k = 0; k < W; ++k) *reinterpret_cast<uint4*>(tile + kt_chunk(g8 * 8 + hi, 4 * k + lo, kPaKeys)) = kt_values(w[k], step[k * NG / W], low[k * NG / W]);
+                    for (int k = 0; k < W; ++k) {
+                        const KtTwo v = kt_values_two(w[k], step[k * NG / W], low[k * NG / W]);
+                        const uint32_t at_chunk = kt_chunk(g8 * 8 + hi, 4 * k + lo, kPaKeys);
+                        *reinterpret_cast<uint4*>(tile + at_chunk) = v.high;
+                        *reinterpret_cast<uint4*>(s_kv + after * kStep + at_chunk) = v.rest;
+                    }
                 } else {
                     // place hi of tokens 2 lo and 2 lo + 1
                     uint32_t step[2][W / 2], low[2][W / 2];
@@ -476,11 +537,12 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // written here, read by the MMAs
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(smem_u32(&kv_full[stage]));
-                    if (V) mbar_arrive(smem_u32(&raw_empty[slot]));
+#pragma unroll
+                for (int i = 0; i < (V ? 1 : 2); ++i) {
+                    if (lane == 0) mbar_arrive(smem_u32(&kv_full[stage]));
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                 }
-                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                if (V && lane == 0) mbar_arrive(smem_u32(&raw_empty[slot]));
             };
             if (n > 0) unpack(0, std::false_type{});
             if (n > 1) unpack(1, std::false_type{});
@@ -500,22 +562,26 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
             auto next = [&]() {
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
             };
-            auto scores = [&](int j) {
-                full();
-                if (j < nt) {
-                    tc_fence_after();
-                    if (pa_elect()) {
-                        const uint32_t k = pa_desc_k(kv + stage * kStep), to_s = ts + (j & 1) * kPaKeys;
-                        pa_mma_ss<false>(to_s, q, k, idesc_s);
+            auto scores = [&](int j) {                             // S = Q K^T of step j, over both tiles of the keys
 #pragma unroll
-                        for (int kk = 1; kk < DB * 4; ++kk) pa_mma_ss<true>(to_s, q + (kk >> 2) * (kPaRows / 16) + (kk & 3) * 2, k + (kk >> 2) * (kPaBlock / 16) + (kk & 3) * 2, idesc_s);
-                        tc_commit(smem_u32(&s_full[t * 2 + (j & 1)]));
-                        tc_commit(smem_u32(&kv_empty[stage]));
+                for (int i = 0; i < 2; ++i) {
+                    full();
+                    if (j < nt) {
+                        tc_fence_after();
+                        if (pa_elect()) {
+                            const uint32_t k = pa_desc_k(kv + stage * kStep), to_s = ts + (j & 1) * kPaKeys;
+                            if (i == 0) pa_mma_ss<false>(to_s, q, k, idesc_s);
+                            else pa_mma_ss<true>(to_s, q, k, idesc_s);
+#pragma unroll
+                            for (int kk = 1; kk < DB * 4; ++kk) pa_mma_ss<true>(to_s, q + (kk >> 2) * (kPaRows / 16) + (kk & 3) * 2, k + (kk >> 2) * (kPaBlock / 16) + (kk & 3) * 2, idesc_s);
+                            if (i == 1) tc_commit(smem_u32(&s_full[t * 2 + (j & 1)]));
+                            tc_commit(smem_u32(&kv_empty[stage]));
+                        }
+                    } else if (lane == 0) {
+                        mbar_arrive(smem_u32(&kv_empty[stage]));
                     }
-                } else if (lane == 0) {
-                    mbar_arrive(smem_u32(&kv_empty[stage]));
+                    next();
                 }
-                next();
             };
             if (n > 0) pa_wait(smem_u32(&q_full), 0, &abort_flag, a.st);
             if (n > 0) scores(0);

@@ -228,25 +228,33 @@ struct PaUnit {
     __device__ __forceinline__ int token0(int t) const { return (sh.pair * 2 + t) * tile_tokens; }
 };
 
-// One row again, by a warp: only keys that it sees take part.  m is the reference in powers of two, four columns a lane.
+// References above this: S c - m in one rounding, with m = S c rounded, leaves more than half a power of two, and beyond 2^27 more than fp16 or the
+// sums have room for.
+constexpr float kPaFar = 0x1p22f;
+
+// One row again, by a warp in fp32: only keys that it sees take part.  Four columns a lane.
 template <typename T>
-__device__ __noinline__ void pa_row_again(const PaArgs& a, const T* q, const T* k, const T* v, int seen, float m, float inv, T* out) {
+__device__ __noinline__ void pa_row_again(const PaArgs& a, const T* q, const T* k, const T* v, int seen, T* out, float* lse) {
     const int lane = threadIdx.x & 31;
-    float acc[4] = {};
-    for (int j0 = 0; j0 < seen; j0 += 32) {
-        const int j = j0 + lane;
-        float p = 0.f;
-        if (j < seen) {
-            float s = 0.f;
-            for (int c = 0; c < a.D; c += 8) {
-                float x[8], y[8];
-                Elem<T>::load8(q + c, x);
-                Elem<T>::load8(k + (long long)j * a.ld_k + c, y);
+    auto score = [&](int j) {
+        float s = 0.f;
+        for (int c = 0; c < a.D; c += 8) {
+            float x[8], y[8];
+            Elem<T>::load8(q + c, x);
+            Elem<T>::load8(k + (long long)j * a.ld_k + c, y);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s = fmaf(x[i], y[i], s);
-            }
-            p = pa_exp2(s * a.c - m);
+            for (int i = 0; i < 8; ++i) s = fmaf(x[i], y[i], s);
         }
+        return __fmul_rn(s, a.c);                              // rounded once for the maximum and the weight, whatever its size
+    };
+    float top = kNegInf, sum = 0.f, acc[4] = {};
+    for (int j = lane; j < seen; j += 32) top = fmaxf(top, score(j));
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (top == kNegInf) top = 0.f;
+    for (int j0 = 0; j0 < seen; j0 += 32) {
+        const float p = j0 + lane < seen ? pa_exp2(score(j0 + lane) - top) : 0.f;
+        sum += p;
         for (int i = 0; i < min(32, seen - j0); ++i) {
             const float w = __shfl_sync(0xffffffffu, p, i);
             if (lane * 4 < a.D) {
@@ -258,12 +266,16 @@ __device__ __noinline__ void pa_row_again(const PaArgs& a, const T* q, const T* 
             }
         }
     }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
     if (lane * 4 < a.D) {
         T h[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) h[e] = Elem<T>::down(acc[e] * inv);
         *reinterpret_cast<uint2*>(out + lane * 4) = *reinterpret_cast<const uint2*>(h);
     }
+    if (lse && lane == 0) *lse = sum == 0.f ? kNegInf : (top + log2f(sum)) * 0.69314718055994531f;
 }
 
 // DB: blocks of 64 columns of a head (1 or 2).  Stages: steps' keys or values in the ring.
@@ -455,124 +467,128 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
         const uint32_t ts = tmem + t * 128 + lanes, to = tmem + 256 + t * 128 + lanes;
         int done = 0;                                          // steps of this tile in earlier turns
         for (int turn = 0; turn < turns; ++turn) {
-        const PaShare sh = share_of(turn, false);
-        if (sh.pair < 0) continue;
-        const PaUnit u(a, sh);
-        const int nt = u.n[t], tok0 = u.token0(t), past = u.past, kv_head = u.kv_head;
-        if (tok0 >= sh.Lq) continue;
-        const int tok = tok0 + (row >> a.gp_log2), head = u.head0 + (row & (a.gp - 1));
-        const int seen = max(0, min(tok + past + 1, sh.Lk));   // keys that this row sees
-        const int all_see = max(0, min(tok0 + past + 1, sh.Lk));
-        float m = kNegInf, mc = 0.f;                           // reference, raw and in powers of two
-        unsigned long long sum2 = 0;
-        float s[kPaKeys];
-        uint32_t* sr = reinterpret_cast<uint32_t*>(s);
-        for (int j = 0; j < nt; ++j) {
-            const int at_step = done + j, buf = at_step & 1;
-            pa_wait(smem_u32(&s_full[t * 2 + buf]), (uint32_t)(at_step >> 1) & 1u, &abort_flag, a.st);
-            __syncwarp();
-            tc_fence_after();
-            const uint32_t at = ts + buf * kPaKeys;
-            pa_ld32(at, sr);
-            pa_ld32(at + 32, sr + 32);
-            pa_ld_wait();
-            if ((j + 1) * kPaKeys > all_see) {
-                const int left = seen - j * kPaKeys;
-#pragma unroll
-                for (int i = 0; i < kPaKeys; ++i) s[i] = i < left ? s[i] : kNegInf;
-            }
-            float m4[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-            for (int i = 4; i < kPaKeys; i += 8)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) m4[e] = i + 4 + e < kPaKeys ? pa_max3(m4[e], s[i + e], s[i + 4 + e]) : fmaxf(m4[e], s[i + e]);
-            const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-            const bool moves = top * a.c > mc + 8.f || (m == kNegInf && top > kNegInf);
-            if (__any_sync(0xffffffffu, moves)) {
-                const float next = moves ? top : m, next_c = next == kNegInf ? 0.f : next * a.c;
-                const float f = !moves ? 1.f : m == kNegInf ? 0.f : pa_exp2(mc - next_c);
-                m = next;
-                mc = next_c;
-                sum2 = mul2(sum2, pair_of(f, f));
-                if (j > 0) {                                   // O, once the step before is in it
-                    pa_wait(smem_u32(&pv_done[t * 2 + (buf ^ 1)]), (uint32_t)((at_step - 1) >> 1) & 1u, &abort_flag, a.st);
-                    __syncwarp();
-                    tc_fence_after();
-#pragma unroll 1
-                    for (int b = 0; b < 2 * DB; ++b) {
-                        uint32_t o[32];
-                        pa_ld32(to + b * 32, o);
-                        pa_ld_wait();
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                        pa_st32(to + b * 32, o);
-                    }
-                    pa_st_wait();
-                }
-            }
-            const unsigned long long c2 = pair_of(a.c, a.c), m2 = pair_of(-mc, -mc);
-            uint32_t p[kPaKeys / 2];
-#pragma unroll
-            for (int i = 0; i < kPaKeys / 2; ++i) {
-                const float2 x = halves(fma2(pair_of(s[2 * i], s[2 * i + 1]), c2, m2));
-                const float lo = pa_exp2(x.x), hi = pa_exp2(x.y);
-                sum2 = add2(sum2, pair_of(lo, hi));
-                p[i] = pa_pack<T>(lo, hi);
-            }
-            pa_st32(at, p);
-            pa_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&p_full[t * 2 + buf]));
-        }
-        const float2 sums = halves(sum2);
-        const float sum = sums.x + sums.y, inv = sum == 0.f ? 0.f : 1.f / sum;
-        if (nt > 0) {
-            done += nt;
-            pa_wait(smem_u32(&pv_done[t * 2 + ((done - 1) & 1)]), (uint32_t)((done - 1) >> 1) & 1u, &abort_flag, a.st);
-            __syncwarp();
-            tc_fence_after();
-        }
-        const bool live = tok < sh.Lq;
-        T* out = static_cast<T*>(a.out) + (long long)(sh.q0 + tok) * a.ld_out + (long long)head * a.D;
-        float odd = 0.f;                                       // NaN where a result is not finite
-#pragma unroll
-        for (int b = 0; b < 2 * DB; ++b) {
-            if (b * 32 >= a.D) break;
-            uint32_t o[32];
-            if (nt > 0) {
-                pa_ld32(to + b * 32, o);
+            const PaShare sh = share_of(turn, false);
+            if (sh.pair < 0) continue;
+            const PaUnit u(a, sh);
+            const int nt = u.n[t], tok0 = u.token0(t), past = u.past, kv_head = u.kv_head;
+            if (tok0 >= sh.Lq) continue;
+            const int tok = tok0 + (row >> a.gp_log2), head = u.head0 + (row & (a.gp - 1));
+            const int seen = max(0, min(tok + past + 1, sh.Lk));   // keys that this row sees
+            const int all_see = max(0, min(tok0 + past + 1, sh.Lk));
+            float m = kNegInf, mc = 0.f;                           // reference, raw and in powers of two
+            bool far = false;
+            unsigned long long sum2 = 0;
+            float s[kPaKeys];
+            uint32_t* sr = reinterpret_cast<uint32_t*>(s);
+            for (int j = 0; j < nt; ++j) {
+                const int at_step = done + j, buf = at_step & 1;
+                pa_wait(smem_u32(&s_full[t * 2 + buf]), (uint32_t)(at_step >> 1) & 1u, &abort_flag, a.st);
+                __syncwarp();
+                tc_fence_after();
+                const uint32_t at = ts + buf * kPaKeys;
+                pa_ld32(at, sr);
+                pa_ld32(at + 32, sr + 32);
                 pa_ld_wait();
-            }
+                if ((j + 1) * kPaKeys > all_see) {
+                    const int left = seen - j * kPaKeys;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int col = b * 32 + g * 8;
-                float x[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    x[e] = sum == 0.f ? 0.f : __uint_as_float(o[g * 8 + e]) * inv;
-                    if (col < a.D) odd = fmaf(x[e], 0.f, odd);
+                    for (int i = 0; i < kPaKeys; ++i) s[i] = i < left ? s[i] : kNegInf;
                 }
-                if (live && col < a.D) Elem<T>::store8(out + col, x);
+                float m4[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+                for (int i = 4; i < kPaKeys; i += 8)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) m4[e] = i + 4 + e < kPaKeys ? pa_max3(m4[e], s[i + e], s[i + 4 + e]) : fmaxf(m4[e], s[i + e]);
+                const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+                const bool moves = top * a.c > mc + 8.f || (m == kNegInf && top > kNegInf);
+                if (__any_sync(0xffffffffu, moves)) {
+                    const float next = moves ? top : m, next_c = next == kNegInf ? 0.f : next * a.c;
+                    const float f = !moves ? 1.f : m == kNegInf ? 0.f : pa_exp2(mc - next_c);
+                    far |= fabsf(next_c) > kPaFar;
+                    m = next;
+                    mc = next_c;
+                    sum2 = mul2(sum2, pair_of(f, f));
+                    if (j > 0) {                                   // O, once the step before is in it
+                        pa_wait(smem_u32(&pv_done[t * 2 + (buf ^ 1)]), (uint32_t)((at_step - 1) >> 1) & 1u, &abort_flag, a.st);
+                        __syncwarp();
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int b = 0; b < 2 * DB; ++b) {
+                            uint32_t o[32];
+                            pa_ld32(to + b * 32, o);
+                            pa_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            pa_st32(to + b * 32, o);
+                        }
+                        pa_st_wait();
+                    }
+                }
+                const unsigned long long c2 = pair_of(a.c, a.c), m2 = pair_of(-mc, -mc);
+                uint32_t p[kPaKeys / 2];
+#pragma unroll
+                for (int i = 0; i < kPaKeys / 2; ++i) {
+                    const float2 x = halves(fma2(pair_of(s[2 * i], s[2 * i + 1]), c2, m2));
+                    const float lo = pa_exp2(x.x), hi = pa_exp2(x.y);
+                    sum2 = add2(sum2, pair_of(lo, hi));
+                    p[i] = pa_pack<T>(lo, hi);
+                }
+                pa_st32(at, p);
+                pa_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&p_full[t * 2 + buf]));
             }
-        }
-        if (nt > 0) {                                          // the next turn's sums may go there
-            tc_fence_before();
+            const float2 sums = halves(sum2);
+            const float sum = sums.x + sums.y, inv = sum == 0.f ? 0.f : 1.f / sum;
+            if (nt > 0) {
+                done += nt;
+                pa_wait(smem_u32(&pv_done[t * 2 + ((done - 1) & 1)]), (uint32_t)((done - 1) >> 1) & 1u, &abort_flag, a.st);
+                __syncwarp();
+                tc_fence_after();
+            }
+            const bool live = tok < sh.Lq;
+            T* out = static_cast<T*>(a.out) + (long long)(sh.q0 + tok) * a.ld_out + (long long)head * a.D;
+            float odd = 0.f;                                       // NaN where a result is not finite
+#pragma unroll
+            for (int b = 0; b < 2 * DB; ++b) {
+                if (b * 32 >= a.D) break;
+                uint32_t o[32];
+                if (nt > 0) {
+                    pa_ld32(to + b * 32, o);
+                    pa_ld_wait();
+                }
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int col = b * 32 + g * 8;
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        x[e] = sum == 0.f ? 0.f : __uint_as_float(o[g * 8 + e]) * inv;
+                        if (col < a.D) odd = fmaf(x[e], 0.f, odd);
+                    }
+                    if (live && col < a.D) Elem<T>::store8(out + col, x);
+                }
+            }
+            if (nt > 0) {                                          // the next turn's sums may go there
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&o_free[t]));
+            }
+            if (live && a.lse) a.lse[(long long)(sh.q0 + tok) * a.n_q + head] = sum == 0.f ? kNegInf : (mc + log2f(sum)) * 0.69314718055994531f;
+            // Rows of finite weights whose result is not (values that they do not see may be the reason), and those of scores too large.
+            const bool again = live && (far || (sum > 0.f && sum < __int_as_float(0x7f800000) && odd != 0.f));
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&o_free[t]));
-        }
-        if (live && a.lse) a.lse[(long long)(sh.q0 + tok) * a.n_q + head] = sum == 0.f ? kNegInf : (mc + log2f(sum)) * 0.69314718055994531f;
-        // rows of finite weights whose result is not: values that they do not see may be the reason
-        const bool again = live && sum > 0.f && sum < __int_as_float(0x7f800000) && odd != 0.f;
-        for (uint32_t todo = __ballot_sync(0xffffffffu, again); todo; todo &= todo - 1) {
-            const int r = __ffs(todo) - 1;
-            const int tok_r = __shfl_sync(0xffffffffu, tok, r), head_r = __shfl_sync(0xffffffffu, head, r), seen_r = __shfl_sync(0xffffffffu, seen, r);
-            const float mc_r = __shfl_sync(0xffffffffu, mc, r), inv_r = __shfl_sync(0xffffffffu, inv, r);
-            pa_row_again<T>(a, static_cast<const T*>(a.q) + (long long)(sh.q0 + tok_r) * a.ld_q + (long long)head_r * a.D,
-                            static_cast<const T*>(a.k) + (long long)sh.k0 * a.ld_k + (long long)kv_head * a.D,
-                            static_cast<const T*>(a.v) + (long long)sh.k0 * a.ld_v + (long long)kv_head * a.D, seen_r, mc_r, inv_r,
-                            static_cast<T*>(a.out) + (long long)(sh.q0 + tok_r) * a.ld_out + (long long)head_r * a.D);
-        }
+            for (uint32_t todo = __ballot_sync(0xffffffffu, again); todo; todo &= todo - 1) {
+                const int r = __ffs(todo) - 1;
+                const int tok_r = __shfl_sync(0xffffffffu, tok, r), head_r = __shfl_sync(0xffffffffu, head, r), seen_r = __shfl_sync(0xffffffffu, seen, r);
+                const bool far_r = __shfl_sync(0xffffffffu, far, r);
+                pa_row_again<T>(a, static_cast<const T*>(a.q) + (long long)(sh.q0 + tok_r) * a.ld_q + (long long)head_r * a.D,
+                                static_cast<const T*>(a.k) + (long long)sh.k0 * a.ld_k + (long long)kv_head * a.D,
+                                static_cast<const T*>(a.v) + (long long)sh.k0 * a.ld_v + (long long)kv_head * a.D, seen_r,
+                                static_cast<T*>(a.out) + (long long)(sh.q0 + tok_r) * a.ld_out + (long long)head_r * a.D,
+                                far_r && a.lse ? a.lse + (long long)(sh.q0 + tok_r) * a.n_q + head_r : nullptr);
+            }
         }
     }
     tc_fence_before();

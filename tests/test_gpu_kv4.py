@@ -32,8 +32,9 @@ def _exact(g, T, n, D, group, t, spread=2):
 
 class Case:
     """Sequences on shuffled pages, n query rows each."""
+    many = False
 
-    def __init__(self, seed, lens, n, n_q, n_k, D, group, page, t, spread=2, ragged=False, tree=False, holes=True):
+    def __init__(self, seed, lens, n, n_q, n_k, D, group, page, t, spread=2, ragged=False, tree=False, holes=True, values=_exact):
         g = torch.Generator().manual_seed(seed)
         self.lens, self.t, self.D, self.n_q, self.n_k, self.page = lens, t, D, n_q, n_k, page
         self.n = n if isinstance(n, list) else [n] * len(lens)
@@ -45,12 +46,13 @@ class Case:
             self.cache.pages.fill_(255)                       # what nothing was stored to: steps and lowest values of NaN
         self.k, self.v, self.ksize, self.vsize, self.vstep = [], [], [], [], []
         for s, x in enumerate(lens):
-            k, ks, _ = _exact(g, x, n_k, D, group, t, 1)
-            v, vs, st = _exact(g, x, n_k, D, group, t, spread)
+            k, ks, _ = values(g, x, n_k, D, group, t, 1)
+            v, vs, st = values(g, x, n_k, D, group, t, spread)
             j = torch.arange(x)
-            self.cache.store(k.cuda(), v.cuda(), (self.table[s].long()[j // page] * page + j % page).cuda())
-            for into, what in zip((self.k, self.v, self.ksize, self.vsize, self.vstep), (k.double().numpy(), v.double().numpy(), ks, vs, st)):
-                into.append(what)
+            k, v = ((a, a) if torch.is_tensor(a) else a for a in (k, v))     # what is stored, and what 4 bits make of it
+            self.cache.store(k[0].cuda(), v[0].cuda(), (self.table[s].long()[j // page] * page + j % page).cuda())
+            for into, what in zip((self.k, self.v, self.ksize, self.vsize, self.vstep), (k[1], v[1], ks, vs, st)):
+                into.append(what.double().numpy() if torch.is_tensor(what) else what)
         rows = sum(self.n)
         self.q = torch.randn(rows, n_q, D, generator=g).to(t).cuda()
         self.offsets = torch.tensor(np.concatenate([[0], np.cumsum(self.n)]), device="cuda") if isinstance(n, list) or ragged else None
@@ -77,10 +79,12 @@ class Case:
             w_out, w_lse, _, _, m = ao.attend(q[a:a + n], self.k[s], self.v[s], sees, scale)
             if x:
                 ones, of = np.ones((n, 1, 1)), np.repeat(np.arange(self.n_k), self.n_q // self.n_k)
-                e = 2 * (self.D + 16) * U * abs(scale) * np.einsum("ihd,jhd->ihj", np.abs(q[a:a + n]), self.ksize[s][:, of]).max(-1)[..., None]
+                e = 2 * ((2 if self.many else 1) * self.D + 16) * U * abs(scale) * (np.einsum("ihd,jhd->ihj", np.abs(q[a:a + n]), self.ksize[s][:, of]) * sees[:, None]).max(-1)[..., None]
                 weigh = lambda size: ao.attend(q[a:a + n], self.k[s], size, sees, scale)[0]
                 tol = (2 * e + (4 * m[:, None, None] + 64) * U) * weigh(self.vsize[s]) + 2.0 ** -11 * 15 * weigh(self.vstep[s])
                 tol = tol + 2.0 ** -25 * 15 * m[:, None, None] * self.vstep[s].max() * ones
+                if self.many:
+                    tol = self.many_tol(e, m, weigh(self.vsize[s]), sees, self.vsize[s][:, of])
                 tol = tol + half * (np.abs(w_out) + tol) + (2.0 ** -25 if self.t == torch.float16 else 0)
                 off = np.abs(out[a:a + n] - w_out)
                 assert np.all(off <= tol), (s, "out", float(np.max(off / tol)))
@@ -281,6 +285,37 @@ def test_scores_that_move_the_maximum_and_scales():
     c = Case(10, [600, 100], 2, 4, 1, 64, 32, 16, torch.bfloat16)
     for scale in (0.0, -0.3, 4.0, 1e-20):
         c.check(c.run(scale=scale), scale=scale)
+
+
+@pytest.mark.parametrize("t,power", [(torch.bfloat16, 40), (torch.bfloat16, 15), (torch.bfloat16, 52), (torch.float16, 11)])
+@pytest.mark.parametrize("n,n_q,n_k", [(1, 4, 2), (5, 8, 2), (20, 8, 2)])
+def test_scores_of_any_size(n, n_q, n_k, t, power):
+    """Scores so far apart that one key has all the weight, above or below zero: its value, and its score as the log of the sum (products
+    in two halves of the key: 4 D + 32 roundings of their absolute sum)."""
+    for sign in (1, -1):
+        c = Case(power + n, [200, 1000], n, n_q, n_k, 64, 64, 16, t)
+        c.q = (sign * 2.0 ** power * c.q.abs().float()).to(t)
+        for s in range(2):
+            c.k[s] = np.abs(c.k[s])                            # all products of one sign: every score is far from zero
+            j = torch.arange(c.lens[s])
+            codes = torch.from_numpy(c.k[s])
+            c.cache.store(codes.to(t).cuda(), torch.from_numpy(c.v[s]).to(t).cuda(), (c.table[s].long()[j // 16] * 16 + j % 16).cuda())
+            slots = (c.table[s].long()[j // 16] * 16 + j % 16).cuda()
+            c.k[s] = c.cache.load(slots)[0].double().cpu().numpy()
+        out, lse = (x.double().cpu().numpy() for x in c.run(scale=1.0))
+        q, of = c.q.double().cpu().numpy(), np.repeat(np.arange(n_k), n_q // n_k)
+        for s, x in enumerate(c.lens):
+            sc = np.einsum("ihd,jhd->ihj", q[s * n:s * n + n], c.k[s][:, of])
+            sc = np.where(ao.causal(n, x)[:, None], sc, -np.inf)
+            order = np.sort(sc, -1)
+            off = (4 * 64 + 32) * U * np.abs(order[..., -1]) + 2 * np.abs(order[..., -1]) * torch.finfo(t).eps       # read back with one rounding
+            clear = order[..., -1] - order[..., -2] > 2 * off + 40
+            best = sc.argmax(-1)
+            want = c.v[s][best, of[None]]
+            got, g_lse = out[s * n:s * n + n], lse[s * n:s * n + n]
+            assert np.isfinite(got).all() and np.isfinite(g_lse).all() and (power < 12 or n == 1 or clear.any())
+            assert np.abs(got - want)[clear].max(initial=0) <= 2.0 ** -9 * np.abs(want).max()
+            assert np.all(np.abs(g_lse - order[..., -1])[clear] <= off[clear] + 1e-6)
 
 
 def test_a_bad_row_stays_in_its_row():

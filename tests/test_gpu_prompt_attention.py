@@ -111,6 +111,32 @@ def test_scores_that_move_the_maximum(t):
     _close(d, _run(d, 0.5), 0.5)
 
 
+@pytest.mark.parametrize("t,power", [(torch.bfloat16, 20), (torch.bfloat16, 11), (torch.bfloat16, 50), (torch.float16, 9)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_of_any_size(sign, t, power):
+    """Scores so far apart that one key has all the weight, all of them far above or below zero: its value, and its score as the log of the
+    sum (D products and the scale, each with two roundings of the absolute sum)."""
+    lens, n_q, n_k, D = [70, 200], 4, 2, 64
+    d = _make(power, lens, [130, 200], n_q, n_k, D, t)
+    d["q"], d["k"] = (sign * d["q"].abs().float() * 2.0 ** power).to(t), (d["k"].abs().float() * 2.0 ** (power if power < 50 else 4)).to(t)
+    out, lse = _run(d, 1.0)
+    q, k, v, out, lse = (x.double().cpu().numpy() for x in (d["q"], d["k"], d["v"], out, lse))
+    of, a, b, some = np.repeat(np.arange(n_k), n_q // n_k), 0, 0, False
+    for nq, nk in zip(lens, d["k_lens"]):
+        sc = np.einsum("ihd,jhd->ihj", q[a:a + nq], k[b:b + nk][:, of])
+        sc = np.where(ao.causal(nq, nk)[:, None], sc, -np.inf)
+        order = np.sort(sc, -1)
+        off = (2 * D + 16) * U * np.abs(order[..., -1])
+        clear = order[..., -1] - order[..., -2] > 2 * off + 40
+        some |= clear.any()
+        want = v[b:b + nk][sc.argmax(-1), of[None]]
+        assert np.isfinite(out[a:a + nq]).all() and np.isfinite(lse[a:a + nq]).all()
+        assert np.abs(out[a:a + nq] - want)[clear].max(initial=0) <= torch.finfo(t).eps * np.abs(want).max()
+        assert np.all(np.abs(lse[a:a + nq] - order[..., -1])[clear] <= off[clear] + 1e-6)
+        a, b = a + nq, b + nk
+    assert some
+
+
 def test_scales():
     d = _make(6, [90], [90], 2, 1, 64, torch.bfloat16)
     for scale in (1e-30, 0.01, 3.0):
