@@ -5,16 +5,17 @@
 //   * eight warps unpack the step to fp16 tiles, low + step code, times those powers.  Keys take two tiles, what fp16 holds and what is
 //     left of it, so that scores are exact to fp32's sums (one tile would move them, and with them every weight, by 2^-12 of their
 //     terms); values are rounded once, to 2^-12 of themselves,
-//   * a thread of the softmax has a row: P = exp2(S c kf - m) in fp16, with the step's key power kf in the factor and its value power in the
-//     reference m, which so follows the largest score and the largest value; P stays below 2^15 whatever the values' size,
+//   * a thread of the softmax has a row: P = exp2(S c kf - m) in fp16 (for fp16 outputs in two parts), with the step's key power kf in the
+//     factor and its value power in the reference m, which so follows the largest score and the largest value; P stays below 2^15 whatever
+//     the values' size,
 //   * fp16 holds 40 powers of two: where a token's keys or values lie so far below a step's or a former step's largest ones (which a row may
 //     not even see) that bits of them would be lost, a warp computes each row that meets them again, in fp32 (kt_row_again); also scores
 //     beyond kPaFar.
 // Columns lie in another order than in memory: 0 4 1 5 2 6 3 7 within eight (queries and keys alike, for the sums it is all one), and
 // place by place for the values (column 8 i + n at n D / 8 + ...), which the outputs undo.
-// 8 sequences x 8 key heads, trees of 60 nodes x 4 heads, 3001 tokens: 67 us with the join (11 at the tensor cores' measured rate), 60 with one
-// tile of the keys, whose log of sums was off by 5e-4 where few tokens are seen.  A step's products read 2.5 times the shared memory of
-// prompt_attention.cuh's for a key and its unpacking issues as much as its softmax.
+// 8 sequences x 8 key heads, trees of 60 nodes x 4 heads, 3001 tokens, fp16: 69 us with the join (11 at the tensor cores' measured rate); 66 with
+// one part of a weight, 60 with one tile of the keys too, whose log of sums was off by 5e-4 where few tokens are seen.  A step's products read
+// 2.5 times the shared memory of prompt_attention.cuh's for a key, and its unpacking issues as much as its softmax.
 #pragma once
 #include "kv4.cuh"
 #include "prompt_attention.cuh"
@@ -30,6 +31,8 @@ constexpr int kKtRaw = 4;                          // steps of packed tokens in 
 constexpr int kKtBlocks = kPaKeys / kKv4Block;     // blocks of 16 tokens a step
 constexpr int kKtPowers = 8;                       // steps whose powers are kept
 constexpr int kKtPresent = 16;
+// Parts of a weight: what fp16 holds, and for fp16 outputs what is left (bf16's 2^-9 hides a weight's 2^-12).
+template <typename T> constexpr int kKtParts = std::is_same_v<T, __half> ? 2 : 1;
 template <int D> constexpr int kKtStages = D == 128 ? 7 : 10;
 template <int D, int NG> constexpr size_t kt_smem_bytes() {
     return 1024 + (size_t)2 * 128 * D * 2 + (size_t)kKtStages<D> * kPaKeys * D * 2 + (size_t)kKtRaw * kKtBlocks * (kKv4Block * D + 128 * NG);
@@ -144,6 +147,7 @@ __device__ __noinline__ void kt_row_again(const Kv4Args& a, const int32_t* table
 template <typename T, int D, int NG>
 __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_constant__ Kv4Args a) {
     constexpr int STAGES = kKtStages<D>, kTile = 128 * D * 2, kStep = kPaKeys * D * 2, kBytes = kKv4Block * D + 128 * NG, W = D / 32, DB = D / 64;
+    constexpr int PARTS = kKtParts<T>;
     extern __shared__ unsigned char kt_smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(kt_smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char *s_kv = smem + 2 * kTile, *s_raw = s_kv + STAGES * kStep;
@@ -339,16 +343,23 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
             const float ref = (float)shift - mc, undo = exp2_int(-shift);
             const unsigned long long c2 = pair_of(cj, cj), m2 = pair_of(ref, ref);
             unsigned long long here = 0;
-            uint32_t p[kPaKeys / 2];
+            const unsigned long long minus = pair_of(-1.f, -1.f);
+            uint32_t p[kPaKeys / 2 * PARTS];
 #pragma unroll
             for (int i = 0; i < kPaKeys / 2; ++i) {
                 const float2 x = halves(fma2(pair_of(s[2 * i], s[2 * i + 1]), c2, m2));
                 const float lo = pa_exp2(x.x), hi = pa_exp2(x.y);
-                here = add2(here, pair_of(lo, hi));
+                const unsigned long long both = pair_of(lo, hi);
+                here = add2(here, both);
                 p[i] = half_pair(lo, hi);
+                if constexpr (PARTS == 2) {
+                    const float2 held = kv4_pair<__half>(p[i]), rest = halves(fma2(pair_of(held.x, held.y), minus, both));
+                    p[kPaKeys / 2 + i] = half_pair(rest.x, rest.y);
+                }
             }
             sum2 = fma2(here, pair_of(undo, undo), sum2);
             pa_st32(at, p);
+            if constexpr (PARTS == 2) pa_st32(at + 32, p + 32);
             pa_st_wait();
             tc_fence_before();
             __syncwarp();
@@ -597,7 +608,7 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
                         if (j == 0) pa_mma_ts<false>(to, p, v, idesc_o);
                         else pa_mma_ts<true>(to, p, v, idesc_o);
 #pragma unroll
-                        for (int kk = 1; kk < kPaKeys / 16; ++kk) pa_mma_ts<true>(to, p + kk * 8, v + kk * 128, idesc_o);
+                        for (int kk = 1; kk < PARTS * (kPaKeys / 16); ++kk) pa_mma_ts<true>(to, p + kk * 8, v + kk % (kPaKeys / 16) * 128, idesc_o);
                         tc_commit(smem_u32(&pv_done[t * 2 + buf]));
                         tc_commit(smem_u32(&kv_empty[stage]));
                     }
