@@ -620,9 +620,10 @@ int coral_lmhead_prompt_attention(const coral_lmhead_prompt_args *args, void *wo
 /*
  * A paged cache of keys and values in 4 bits.  A group of columns of a token's head is held as
  *   low = min x,  step = round_to_type((max x - min x) / 15),  code = round((x - low) / step) in 0..15,  and stands for low + step code
- * (step 0: code 0).  A group that holds an infinity or a NaN, or whose max x - min x passes fp32's range, stands for NaN.  coral_lmhead_kv4_config: type CORAL_TYPE_BF16 or _F16 (of
- * tokens, steps, queries and outputs), n_pages pages of `page` tokens (a multiple of 16), n_heads key heads of D = 64 or 128 columns, group
- * 32, 64 or 128 columns and at most D; n_pages * page, and n_pages * page / 16 * n_heads, below 2^31.
+ * (step 0: code 0).  A group that holds an infinity or a NaN, or whose max x - min x passes fp32's range, stands for NaN.
+ * coral_lmhead_kv4_config: type CORAL_TYPE_BF16 or _F16 (of tokens, steps, queries and outputs), n_pages pages of `page` tokens (a multiple of
+ * 16), n_heads key heads of D = 64 or 128 columns, group 32, 64 or 128 columns and at most D; n_pages * page, and n_pages * page / 16 * n_heads,
+ * below 2^31.
  * coral_lmhead_kv4_bytes: size of the cache: n_heads * (D + 8 D / group) bytes a token.  The buffer is the caller's, 256-byte aligned.
  * coral_lmhead_kv4_store: tokens k, v [T x n_heads x D] of `type`, ld_* apart, to slots [T] (page * tokens of a page + place in it);
  *   a slot outside the cache (-1) is passed over.  What two tokens of one call leave in one slot is unspecified.
@@ -647,14 +648,15 @@ int coral_lmhead_kv4_load(const coral_lmhead_kv4_config *cfg, const void *cache_
  * sequence and query head h, with the keys and values of head h / (n_q / n_heads) as the cache holds them:
  *   out = sum_j softmax_j(scale q . k_j) v_j  over j <= lens - n + i (tree_mask NULL), or over the j < lens - n and those
  *   j = lens - n + b with bit b of the row's tree_mask word (a node sees its ancestors and itself);  lse = log-sum-exp of scale q . k_j.
- * Sums and softmax in fp32; a weight is rounded to fp16 next to its value's step.  A row that sees nothing has out 0 and lse -inf.
+ * Sums and softmax in fp32.  For the product with the values a weight times a value's step, or from 33 rows of a key head on (max_q n_q / n_heads)
+ * a value, is rounded to fp16 (a weight too, where outputs are bf16).  A row that sees nothing has out 0 and lse -inf.
  * Tokens that a row does not see have no influence, infinities and NaN too; pages outside [0, n_pages) hold no tokens.
  *   q, out [n_rows x n_q x D] of the cache's type; out_lse fp32 [n_rows x n_q] or NULL; n_q a multiple of n_heads.  Rows outside the
  *   sequences, and a sequence's rows from max_q on, are left as they are.  lens is clamped to width * page, offsets to n_rows.
  *   q_offsets int64 [n_seq + 1], not decreasing; tree_mask uint64 [n_rows], needs max_q <= 64.  table int32 [n_seq x width], ld_table apart.
  * n_seq, n_rows >= 0 (0: nothing to do); max_q, n_q, width >= 1; scale finite.  max_q bounds the work that is started, so it should
- * be no more than the longest sequence's rows.  workspace_dev: 256-byte aligned, at least coral_lmhead_kv4_attention_bytes; holds nothing between calls
- * but the status word; calls that may overlap on the GPU need one each.  Asynchronous, one launch or two, no atomics: the same call
+ * be no more than the longest sequence's rows.  workspace_dev: 256-byte aligned, at least coral_lmhead_kv4_attention_bytes; holds nothing
+ * between calls but the status word; calls that may overlap on the GPU need one each.  Asynchronous, one launch or two, no atomics: the same call
  * gives the same bits.  CORAL_ERR_TOO_LARGE for more blocks than a launch takes.
  * coral_lmhead_attention_status: synchronises `stream` and returns the status word of the last call that used the workspace
  * (0 or CORAL_ERR_TIMEOUT: a bounded wait ran out, the results mean nothing), for both kinds of attention.

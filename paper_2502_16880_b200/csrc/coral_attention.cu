@@ -130,8 +130,9 @@ int launch_kv4_rows(const coral_lmhead_kv4_config* c, bool store, const void* ca
 }
 
 // From how many rows of a key head on (query tokens times heads of its group) the tensor-core kernel takes a call.  us, warp MMAs | tensor
-// cores, groups of 32 and of 128 columns of 128: 8 x 3000 tokens 32 rows 37 | 41, 36 rows 65 and 60 | 42 and 41, 128 rows 128 and 117 | 47; 60000
-// tokens 36 rows 144 and 131 | 79 and 78; 4000 tokens 36 rows 21 and 19 | 20 (up to 32 rows two row groups share what they unpack).
+// cores, groups of 32 and of 128 columns of 128, bf16: 8 x 3000 tokens 36 rows 65 and 60 | 48 and 46, 128 rows 128 and 117 | 52 and 50; 60000
+// tokens 36 rows 144 and 131 | 94 and 91; 4000 tokens 36 rows 21 and 19 | 20.  Up to 32 rows two row groups share what they unpack, and the warp
+// MMAs take 37 and 34, 76 and 70, 16 (the tensor cores the same as for 36).
 constexpr long long kKv4ManyFrom = 33;
 
 struct Kv4Plan {

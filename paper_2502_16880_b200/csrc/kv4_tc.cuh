@@ -13,9 +13,10 @@
 //     beyond kPaFar.
 // Columns lie in another order than in memory: 0 4 1 5 2 6 3 7 within eight (queries and keys alike, for the sums it is all one), and
 // place by place for the values (column 8 i + n at n D / 8 + ...), which the outputs undo.
-// 8 sequences x 8 key heads, trees of 60 nodes x 4 heads, 3001 tokens, fp16: 69 us with the join (11 at the tensor cores' measured rate); 66 with
-// one part of a weight, 60 with one tile of the keys too, whose log of sums was off by 5e-4 where few tokens are seen.  A step's products read
-// 2.5 times the shared memory of prompt_attention.cuh's for a key, and its unpacking issues as much as its softmax.
+// 8 sequences x 8 key heads, trees of 60 nodes x 4 heads, 3001 tokens, fp16: 68 us with the join (11 at the tensor cores' measured rate); 66 with
+// one part of a weight, 60 with one tile of the keys too, whose log of sums was off by 5e-4 where few tokens are seen.  What bounds it: 64 tokens
+// take 3500 cycles, of which the products' operands read shared memory for 2500 (2.5 times those of prompt_attention.cuh, since keys count
+// twice), and an unpacking warp is busy all the time, keys 1700 and values 1000 (with one tile of rows it alone sets the 3100 cycles).
 #pragma once
 #include "kv4.cuh"
 #include "prompt_attention.cuh"
@@ -493,10 +494,8 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
             auto unpack = [&](int j, auto values) {
                 constexpr bool V = decltype(values)::value;
                 const int slot = j % kKtRaw, base = (step0 + j) * kPaKeys + g8 * 8;
-                if (!V) {
-                    pa_wait(smem_u32(&raw_full[slot]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
-                    pa_wait(smem_u32(&power_full[j % kKtPowers]), (uint32_t)(j / kKtPowers) & 1u, &abort_flag, a.st);
-                }
+                // (the warp of the powers has waited for the packed tokens)
+                if (!V) pa_wait(smem_u32(&power_full[j % kKtPowers]), (uint32_t)(j / kKtPowers) & 1u, &abort_flag, a.st);
                 const float2 power = s_power[j % kKtPowers];
                 const float up = kt_inverse(V ? power.y : power.x);
                 const int real = present[j % kKtPresent] >> b & 1u ? len - base : 0;      // tokens of the eight that there are
@@ -517,7 +516,7 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
                         low[i] = pair_of(p.y * up, p.y * up);
                     }
                     const int after = stage + 1 == STAGES ? 0 : stage + 1;
-                    pa_wait(smem_u32(&kv_empty[stage]), phase ^ 1u, &abort_flag, a.st);
+                    // (stages get free in their order)
                     pa_wait(smem_u32(&kv_empty[after]), after ? phase ^ 1u : phase, &abort_flag, a.st);
 #pragma unroll
                     for (int k = 0; k < W; ++k) {
