@@ -598,7 +598,7 @@ int coral_lmhead_qk_rotate_backward(const coral_lmhead_qk_args *args, void *work
  *   type CORAL_TYPE_BF16 or _F16.  q, out [T x n_q x D], k, v [Tk x n_k x D], tokens ld_* apart; D a multiple of 8, 8 to 128; n_q a
  *   multiple of n_k.  q_offsets, k_offsets int64 [n_seq + 1], not decreasing, clamped to T and Tk; k_offsets NULL: those of the
  *   queries (Tk = T).  out_lse fp32 [T x n_q] or NULL.  Rows outside the sequences are left as they are.  out may not overlap an input.
- * n_seq, T, Tk >= 0 (n_seq or T 0: nothing to do); scale > 0 and finite.  workspace_dev: CORAL_PROMPT_WORKSPACE_BYTES, 256-byte aligned, for the
+ * n_seq, T, Tk >= 0 (n_seq or T 0: nothing to do; Tk 0: k and v may be NULL); scale > 0 and finite.  workspace_dev: CORAL_PROMPT_WORKSPACE_BYTES, 256-byte aligned, for the
  * status word that coral_lmhead_attention_status reads; calls that may overlap on the GPU need one each.  Asynchronous, one launch, no
  * atomics: the same call gives the same bits.  CORAL_ERR_TOO_LARGE for more blocks than a launch takes.
  */

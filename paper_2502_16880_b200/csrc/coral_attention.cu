@@ -229,14 +229,14 @@ bool prompt_args_ok(const coral_lmhead_prompt_args* a) {
     if (!a->q_offsets_dev || !aligned(a->q_offsets_dev, 8) || !aligned(a->k_offsets_dev, 8) || !aligned(a->out_lse_dev, 4)) return false;
     if (!a->k_offsets_dev && a->Tk != a->T) return false;
     return rows_ok(a->q_dev, a->ld_q, a->n_q, a->D, 2) && rows_ok(a->out_dev, a->ld_out, a->n_q, a->D, 2) &&
-           rows_ok(a->k_dev, a->ld_k, a->n_k, a->D, 2) && rows_ok(a->v_dev, a->ld_v, a->n_k, a->D, 2);
+           (a->Tk == 0 || (rows_ok(a->k_dev, a->ld_k, a->n_k, a->D, 2) && rows_ok(a->v_dev, a->ld_v, a->n_k, a->D, 2)));
 }
 
 // Rows [T x heads x D] in boxes of 64 columns x `heads_box` heads x `tokens` tokens, 128-byte swizzle; columns past D read as zero.
 bool make_rows_map(CUtensorMap* map, int type, const void* base, int T, int heads, int D, long long ld, int heads_box, int tokens) {
     static const EncodeTiledFn enc = encode_tiled_fn();
     if (!enc) return false;
-    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)std::max(T, 1)};
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)T};
     const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)ld * 2};
     const cuuint32_t box[3] = {64, (cuuint32_t)heads_box, (cuuint32_t)tokens}, ones[3] = {1, 1, 1};
     return enc(map, type == CORAL_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims,
@@ -247,9 +247,10 @@ bool make_rows_map(CUtensorMap* map, int type, const void* base, int T, int head
 template <typename T, int DB>
 int launch_prompt(const coral_lmhead_prompt_args* a, const PaArgs& k, unsigned blocks, cudaStream_t st) {
     CUtensorMap q, kk, v;
-    if (!make_rows_map(&q, a->type, a->q_dev, a->T, a->n_q, a->D, a->ld_q, k.gp, 128 / k.gp) ||
-        !make_rows_map(&kk, a->type, a->k_dev, a->Tk, a->n_k, a->D, a->ld_k, 1, kPaKeys) ||
-        !make_rows_map(&v, a->type, a->v_dev, a->Tk, a->n_k, a->D, a->ld_v, 1, kPaKeys))
+    if (!make_rows_map(&q, a->type, a->q_dev, a->T, a->n_q, a->D, a->ld_q, k.gp, 128 / k.gp)) return CORAL_ERR_CUDA;
+    kk = v = q;                                    // without keys there are no loads of them
+    if (a->Tk && (!make_rows_map(&kk, a->type, a->k_dev, a->Tk, a->n_k, a->D, a->ld_k, 1, kPaKeys) ||
+                  !make_rows_map(&v, a->type, a->v_dev, a->Tk, a->n_k, a->D, a->ld_v, 1, kPaKeys)))
         return CORAL_ERR_CUDA;
     constexpr size_t smem = pa_smem_bytes<DB>();
     if (!allow_smem(prompt_attention_kernel<T, DB>, smem)) return CORAL_ERR_CUDA;

@@ -267,6 +267,25 @@ def test_what_a_row_does_not_see_has_no_influence(tree):
         assert out[np.flatnonzero(see)].isnan().all()
 
 
+@pytest.mark.parametrize("n,tree", [(1, False), (8, True), (40, True)])
+def test_pages_beyond_32_bit_offsets(n, tree):
+    """The same tokens on the last pages of a cache of 5 GB: the same bits, and read back from there."""
+    c = Case(16, [n + 90, 600], n, 4, 2, 128, 32, 64, torch.bfloat16, tree=tree)
+    want, pages = c.run(), 2 ** 18
+    big = lmhead.Kv4Cache(pages, 64, 2, 128, group=32, dtype=torch.bfloat16)
+    assert big.pages.numel() > 2 ** 32
+    c.table += pages - c.cache.cfg.n_pages
+    for s, x in enumerate(c.lens):
+        j = torch.arange(x)
+        slots = (c.table[s].long()[j // 64] * 64 + j % 64).cuda()
+        k, v = (torch.from_numpy(a[s]).bfloat16().cuda() for a in (c.k, c.v))
+        big.store(k, v, slots)
+        assert all(torch.equal(a, b) for a, b in zip(big.load(slots), (k, v)))
+    c.cache = big
+    got = c.run()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_steps_of_very_different_size():
     c = Case(7, [500], 1, 4, 2, 64, 32, 16, torch.bfloat16, spread=40)
     c.check(c.run())

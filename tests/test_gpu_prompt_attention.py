@@ -137,6 +137,27 @@ def test_scores_of_any_size(sign, t, power):
     assert some
 
 
+def test_no_keys_at_all():
+    d = _make(1, [3, 5], [0, 0], 4, 2, 64, torch.bfloat16)
+    out, lse = _run(d)
+    assert not out.any() and (lse == -INF).all()
+
+
+def test_rows_beyond_32_bit_offsets():
+    """Tokens 2^20 elements apart, the last of them 2^31 elements from the first: the same bits as side by side."""
+    d = _make(2, [1100, 1000], [1100, 1000], 4, 2, 64, torch.bfloat16)
+    want = _run(d)
+    room = torch.empty(2100, 2 ** 20, dtype=torch.bfloat16, device="cuda")
+    at = 0
+    for n in "qkv":
+        x = room[:, at:at + d[n].shape[1] * 64].view(2100, -1, 64)
+        x.copy_(d[n])
+        d[n], at = x, at + 512
+    out = room[:, at:at + 256].view(2100, 4, 64)
+    lmhead.coral_lmhead_prompt_attention(d["q"], d["k"], d["v"], _offsets(d["lens"]), out)
+    assert torch.equal(out, want[0])
+
+
 def test_scales():
     d = _make(6, [90], [90], 2, 1, 64, torch.bfloat16)
     for scale in (1e-30, 0.01, 3.0):

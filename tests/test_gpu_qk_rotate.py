@@ -204,3 +204,25 @@ def test_binding_refuses_wrong_tensors():
     with pytest.raises(ValueError):
         lmhead.coral_lmhead_qk_rotate_backward(d["q"], d["k"], d["positions"], d["freqs"], d["dq"], d["dk"], torch.empty_like(d["dq"]), torch.empty_like(d["dk"]),
                                                w_q=d["w_q"], w_k=d["w_k"], dw_q=torch.empty(64, device="cuda"), workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+
+
+def test_rows_beyond_32_bit_offsets():
+    """Tokens 2^20 elements apart, the last of them 2^31 elements from the first: the same bits as side by side, both ways."""
+    g = torch.Generator().manual_seed(5)
+    T, n_q, n_k, D, t = 2100, 3, 2, 64, torch.bfloat16
+    room = torch.empty(T, 2 ** 20, dtype=t, device="cuda")
+    near = {n: torch.randn(T, h, D, generator=g).to(t).cuda() for n, h in (("q", n_q), ("k", n_k), ("dq", n_q), ("dk", n_k))}
+    far = {}
+    for i, (n, x) in enumerate(near.items()):
+        far[n] = room[:, i * 256:i * 256 + x.shape[1] * D].view(x.shape)
+        far[n].copy_(x)
+    w = torch.randn(2, D, generator=g).to(t).cuda()
+    pos, freqs = torch.arange(T, dtype=torch.int32, device="cuda") * 50, (10000.0 ** (-torch.arange(D // 2) / (D // 2))).float().cuda()
+    ws = torch.empty(lmhead.coral_lmhead_qk_rotate_backward_bytes(T, n_q, n_k, D), dtype=torch.uint8, device="cuda")
+    got = []
+    for x in (near, far):
+        dw = [torch.empty(D, device="cuda") for _ in range(2)]
+        lmhead.coral_lmhead_qk_rotate_backward(x["q"], x["k"], pos, freqs, x["dq"], x["dk"], x["dq"], x["dk"], w[0], w[1], dw_q=dw[0], dw_k=dw[1], workspace=ws)
+        lmhead.coral_lmhead_qk_rotate(x["q"], x["k"], pos, freqs, x["q"], x["k"], w[0], w[1])
+        got.append(dw + list(x.values()))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
