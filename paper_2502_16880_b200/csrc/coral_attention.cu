@@ -164,7 +164,7 @@ Kv4Plan kv4_plan(const coral_lmhead_kv4_config* c, const coral_lmhead_kv4_attent
     p.row_blocks = (int)((rows - 1) / per_block + 1);
     p.units = (long long)a->n_seq * c->n_heads * p.row_blocks;
     // The number of parts whose rounds of resident blocks take the least, a block counted as its tokens plus 512 for what it begins and
-    // ends with (64 sequences of up to 4096 tokens, 256 blocks unsplit: 58 us in 5 parts, 43 in one).  A part has a span at least.
+    // ends with (64 sequences of up to 4096 tokens, 256 blocks unsplit: 58 us in 5 parts, 35 in one).  A part has a span at least.
     const long long resident = (p.nr == 1 ? 2 : 1) * kSms, tokens = (long long)a->width * c->page, spans = (tokens - 1) / (kKv4SpanBlocks * kKv4Block) + 1;
     const long long most = std::min(spans, (long long)kKv4MaxSplits);
     long long best = -1;

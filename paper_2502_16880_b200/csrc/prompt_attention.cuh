@@ -14,7 +14,11 @@
 // a row at most, by the softmax warps themselves, and nothing else touches it before the end.
 // Masked scores are -inf before anything is computed of them; but a value row with an infinity or a NaN would reach every row of
 // the tile through 0 * inf.  Rows whose result is not finite although their sum is are therefore computed again at the end
-// by a warp each, over the keys that they see.
+// by a warp each, over the keys that they see; so are those of scores beyond kPaFar.
+// 8192 tokens, 32 query and 8 key heads of 128, bf16: 470 to 490 us, 1.15 PFLOP/s or 69 % of the measured product rate, and less under the
+// power limit (550).  It was 626 with steps of 128 keys and one buffer, 504 with 64 and two, 470 with the longest pairs of tiles first on as
+// many blocks as there are SMs and the next pair's operands loaded ahead.  What bounds it: a step of both tiles takes 1640 cycles, in which the products read operands from shared
+// memory for 1300 and the exponentials issue for 1100; either alone would be faster.
 #pragma once
 #include <type_traits>
 

@@ -10,6 +10,9 @@
 // and some of its heads at a time: it computes the token's angles once, the product position * freq and what is left of it after
 // whole turns in 64 bits (in 32, a position of a million is off by a tenth of a turn), and its threads keep what their item
 // needs of them, times the weights, in registers over all of those heads.  No block-wide barrier but for the column sums.
+// 16384 tokens of 32 + 8 heads of 128, bf16: 59 us, 87 % of the copy bandwidth measured (75 before a warp kept a token's factors over its
+// heads and loaded rows ahead).  Gradient of 8192 tokens: 62 us, 61 % (136 before): two rows and a token's factors in flight
+// take 128 registers, so 16 warps a SM have to cover the loads; the column sums' second kernel takes 4 of it.
 #pragma once
 #include <type_traits>
 
