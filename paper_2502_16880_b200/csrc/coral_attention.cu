@@ -75,7 +75,10 @@ int qk_grid(const QkArgs& k) {
 
 template <typename T, bool HALVES, int N, int L>
 cudaError_t launch_qk_kernel(const QkArgs& k, bool backward, int grid, cudaStream_t st) {
-    return launch_pdl(backward ? qk_rotate_backward_kernel<T, HALVES, N, L> : qk_rotate_kernel<T, HALVES, N, L>, dim3(grid), dim3(kQkThreads), 0, st, k);
+    if (!backward) return launch_pdl(qk_rotate_kernel<T, HALVES, N, L>, dim3(grid), dim3(kQkThreads), 0, st, k);
+    constexpr size_t smem = (size_t)kQkSlots<T, N> * kQkStep<T, N>;
+    if (!allow_smem(qk_rotate_backward_kernel<T, HALVES, N, L>, smem)) return cudaErrorUnknown;
+    return launch_pdl(qk_rotate_backward_kernel<T, HALVES, N, L>, dim3(grid), dim3(kQkThreads), smem, st, k);
 }
 
 template <typename T>

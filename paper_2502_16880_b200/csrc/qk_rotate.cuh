@@ -16,6 +16,7 @@
 #pragma once
 #include <type_traits>
 
+#include "cp_async.cuh"
 #include "element.cuh"
 
 namespace coral {
@@ -272,11 +273,38 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_rotate_kernel(const __grid_c
 }
 
 // The column sums of a warp's rows stay in registers; they go through a fixed order (a thread's rows, the block's threads, the blocks'
-// partial rows), so the same call gives the same bits.
+// partial rows), so the same call gives the same bits.  What a thread reads of dy and x comes through a ring in shared memory of its own,
+// several rows ahead and across tokens: registers have room for one row ahead only.
+template <typename T, int N> constexpr int kQkStep = 4 * N * (int)sizeof(T) * kQkThreads;          // a row of each thread: two granules of dy and of x
+template <typename T, int N> constexpr int kQkSlots = 80 * 1024 / kQkStep<T, N>;
+template <typename T, int N>
+struct QkRing {
+    static constexpr int kBytes = N * (int)sizeof(T);
+    unsigned char* base;
+    __device__ __forceinline__ unsigned char* at(int slot, int granule) const { return base + ((slot * 4 + granule) * kQkThreads + (int)threadIdx.x) * kBytes; }
+    __device__ __forceinline__ void fill(int slot, int granule, const T* from) const {
+        if constexpr (kBytes == 8) {
+            cp_async8(at(slot, granule), from);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kBytes; i += 16) cp_async16(at(slot, granule) + i, reinterpret_cast<const unsigned char*>(from) + i);
+        }
+    }
+    __device__ __forceinline__ QkRaw<T, N> row(int slot, int granule, bool on) const {
+        QkRaw<T, N> r{};
+        if (on) r.load(reinterpret_cast<const T*>(at(slot, granule)));
+        return r;
+    }
+};
+
 template <typename T, bool HALVES, int N, int L>
 __global__ void __launch_bounds__(kQkThreads, 2) qk_rotate_backward_kernel(const __grid_constant__ QkArgs a) {
     __shared__ __align__(16) float s_cs[kQkWarps][kQkMaxD / 2], s_sn[kQkWarps][kQkMaxD / 2];
     __shared__ float s_sum[2 * N * kQkThreads];               // [column of an item][thread]
+    extern __shared__ __align__(16) unsigned char qk_ring[];
+    constexpr int SLOTS = kQkSlots<T, N>;
+    static_assert(SLOTS >= 2, "a row is read while the next is on its way");
+    const QkRing<T, N> ring{qk_ring};
     float *cs = s_cs[threadIdx.x >> 5], *sn = s_sn[threadIdx.x >> 5];
     const int lanes = L ? L : a.lanes, lane = threadIdx.x & 31, row = lane / lanes, rows = 32 / lanes;
     const QkItem<T, HALVES, N, L != 0> it(lane & (lanes - 1), a);
@@ -301,22 +329,67 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_rotate_backward_kernel(const
             wu = ru.cols();
             wv = rv.cols();
         }
-        for (long long unit = blockIdx.x * kQkWarps + (threadIdx.x >> 5); unit < units; unit += warps) {
-            const int t = a.shares == 1 ? (int)unit : (int)(unit / a.shares), h0 = (int)(unit - (long long)t * a.shares) * a.span[part];
-            const int heads = min(a.span[part], all_heads - h0);
+        const long long first = blockIdx.x * kQkWarps + (threadIdx.x >> 5);
+        auto token = [&](long long unit, int* h0, int* heads) {     // of a unit, with its heads
+            const int t = a.shares == 1 ? (int)unit : (int)(unit / a.shares);
+            *h0 = (int)(unit - (long long)t * a.shares) * a.span[part];
+            *heads = min(a.span[part], all_heads - *h0);
+            return t;
+        };
+        // the next row to be fetched
+        long long next = first;
+        int next_h = row, next_heads = 0;
+        const T *next_x = nullptr, *next_dy = nullptr;
+        auto open = [&]() {
+            for (; next < units; next += warps) {
+                int h0;
+                const int t = token(next, &h0, &next_heads);
+                if (next_heads <= 0) continue;
+                next_h = row;
+                next_x = x + t * ld_x + (h0 + row) * a.D;
+                next_dy = dy + t * ld_dy + (h0 + row) * a.D;
+                return;
+            }
+        };
+        auto fetch = [&](int slot) {
+            if (next < units) {
+                if (next_h < next_heads) {
+                    if (L || it.c0 >= 0) {
+                        ring.fill(slot, 0, next_dy + it.c0);
+                        if (w) ring.fill(slot, 2, next_x + it.c0);
+                    }
+                    if (L || it.c1 >= 0) {
+                        ring.fill(slot, 1, next_dy + it.c1);
+                        if (w) ring.fill(slot, 3, next_x + it.c1);
+                    }
+                }
+                next_h += rows;
+                next_x += rows * a.D;
+                next_dy += rows * a.D;
+                if (next_h - row >= next_heads) {
+                    next += warps;
+                    open();
+                }
+            }
+            cp_async_commit();
+        };
+        open();
+#pragma unroll 1
+        for (int i = 0; i < SLOTS - 1; ++i) fetch(i);
+        int slot = 0;
+        for (long long unit = first; unit < units; unit += warps) {
+            int h0, heads;
+            const int t = token(unit, &h0, &heads);
             if (heads <= 0) continue;
-            const T *from = x + t * ld_x + (h0 + row) * a.D, *from_dy = dy + t * ld_dy + (h0 + row) * a.D;
             T* to = dx + t * ld_dx + (h0 + row) * a.D;
-            QkRaw<T, N> u0, v0, u1, v1, p0, q0, p1, q1;
-            it.load(from_dy, row < heads, p0, q0);
-            it.load(from, row < heads && w, u0, v0);
             qk_angles(a, t, cs, sn);
             const QkTurn<N> f = qk_turn<HALVES, true>(it, cs, sn, one, one);
             for (int h = row; h - row < heads; h += rows) {
-                from += rows * a.D;
-                from_dy += rows * a.D;
-                it.load(from_dy, h + rows < heads, p1, q1);
-                it.load(from, h + rows < heads && w, u1, v1);
+                cp_async_wait<SLOTS - 2>();
+                const bool on = h < heads, on0 = on && (L || it.c0 >= 0), on1 = on && (L || it.c1 >= 0);
+                const QkRaw<T, N> p0 = ring.row(slot, 0, on0), q0 = ring.row(slot, 1, on1), u0 = ring.row(slot, 2, on0 && w), v0 = ring.row(slot, 3, on1 && w);
+                fetch(slot == 0 ? SLOTS - 1 : slot - 1);           // the row before: its values are in use
+                slot = slot + 1 == SLOTS ? 0 : slot + 1;
                 QkCols<N> du = p0.cols(), dv = q0.cols();
                 f.template operator()<HALVES>(du, dv);
                 if (w) {
@@ -340,10 +413,6 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_rotate_backward_kernel(const
                 }
                 if (h < heads) it.store(to, du, dv);
                 to += rows * a.D;
-                u0 = u1;
-                v0 = v1;
-                p0 = p1;
-                q0 = q1;
             }
         }
         if (!a.part) continue;

@@ -214,6 +214,21 @@ def test_ragged_rows():
     c.check((out, lse))
 
 
+@pytest.mark.parametrize("tree", [False, True])
+def test_max_q_above_the_rows(tree):
+    """A bound on the rows of a sequence larger than any has: other kernels and blocks without work, the same results up to rounding."""
+    c = Case(17, [40, 0, 300, 7], [3, 0, 9, 1], 6, 2, 64, 32, 32, torch.bfloat16, tree=tree)
+    for max_q in (9, 12, 64) + (() if tree else (1000, 100000)):
+        c.check(c.run(max_q=max_q))
+
+
+def test_many_sequences():
+    g = torch.Generator().manual_seed(18)
+    lens = [int(x) for x in torch.randint(0, 40, (3000,), generator=g)]
+    c = Case(18, lens, 1, 2, 1, 64, 64, 16, torch.float16)
+    c.check(c.run())
+
+
 def test_long_caches_are_split():
     for lens, n in (([20000, 3], 1), ([9000], 12), ([33000], 1)):
         c = Case(len(lens), lens, n, 8, 2, 64, 64, 64, torch.bfloat16)
