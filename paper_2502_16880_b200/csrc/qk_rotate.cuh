@@ -10,9 +10,10 @@
 // and some of its heads at a time: it computes the token's angles once, the product position * freq and what is left of it after
 // whole turns in 64 bits (in 32, a position of a million is off by a tenth of a turn), and its threads keep what their item
 // needs of them, times the weights, in registers over all of those heads.  No block-wide barrier but for the column sums.
-// 16384 tokens of 32 + 8 heads of 128, bf16: 59 us, 87 % of the copy bandwidth measured (75 before a warp kept a token's factors over its
-// heads and loaded rows ahead).  Gradient of 8192 tokens: 62 us, 61 % (136 before): two rows and a token's factors in flight
-// take 128 registers, so 16 warps a SM have to cover the loads; the column sums' second kernel takes 4 of it.
+// 16384 tokens of 32 + 8 heads of 128, bf16: 56 us, 91 % of the copy bandwidth measured (75 before a warp kept a token's factors over its
+// heads and loaded rows ahead, 58 with each position read where it is needed).  Gradient of 8192 tokens: 57 us, 68 % (136 before; 62 with one
+// row ahead in registers): 126 registers leave 16 warps a SM, each token's angles are computed for the queries and again for the keys, and the
+// column sums' second kernel takes 4 of it.
 #pragma once
 #include <type_traits>
 
@@ -197,9 +198,9 @@ __device__ __forceinline__ void add_products(QkCols<N>& acc, const QkCols<N>& a,
     for (int i = 0; i < N / 2; ++i) acc.p[i] = fma2(a.p[i], b.p[i], acc.p[i]);
 }
 
-// Cosines and sines of a token, by a warp: the product in 64 bits is exact to 2^-53, and so are the turns taken off it.
-__device__ __forceinline__ void qk_angles(const QkArgs& a, int t, float* cs, float* sn) {
-    const double p = (double)a.pos[t] * 0.15915494309189533577;
+// Cosines and sines of a token's position, by a warp: the product in 64 bits is exact to 2^-53, and so are the turns taken off it.
+__device__ __forceinline__ void qk_angles(const QkArgs& a, int pos, float* cs, float* sn) {
+    const double p = (double)pos * 0.15915494309189533577;
     __syncwarp();
     for (int i = threadIdx.x & 31; i < a.rot >> 1; i += 32) {
         const double turns = p * (double)a.freq[i];
@@ -227,9 +228,13 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_rotate_kernel(const __grid_c
     const float inv_d = 1.f / (float)a.D;
     const int warps = gridDim.x * kQkWarps, step = rows * a.D;
     const long long units = (long long)a.T * a.shares;
+    auto token = [&](long long unit) { return a.shares == 1 ? (int)unit : (int)(unit / a.shares); };
+    const long long first = blockIdx.x * kQkWarps + (threadIdx.x >> 5);
     pdl_wait();
-    for (long long unit = blockIdx.x * kQkWarps + (threadIdx.x >> 5); unit < units; unit += warps) {
-        const int t = a.shares == 1 ? (int)unit : (int)(unit / a.shares), share = (int)(unit - (long long)t * a.shares);
+    int pos_ahead = first < units ? a.pos[token(first)] : 0;
+    for (long long unit = first; unit < units; unit += warps) {
+        const int t = token(unit), share = (int)(unit - (long long)t * a.shares), pos = pos_ahead;
+        if (unit + warps < units) pos_ahead = a.pos[token(unit + warps)];
         bool known = false;                                    // the token's angles
 #pragma unroll 1
         for (int part = 0; part < 2; ++part) {
@@ -240,7 +245,7 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_rotate_kernel(const __grid_c
             QkRaw<T, N> u0[2], v0[2], u1[2], v1[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) it.load(from + i * step, row + i * rows < heads, u0[i], v0[i]);
-            if (!known) qk_angles(a, t, cs, sn);
+            if (!known) qk_angles(a, pos, cs, sn);
             known = true;
             it.load(w, w != nullptr, u1[0], v1[0]);            // from L1: kept in the turn's factors only
             QkCols<N> wu = u1[0].cols(), wv = v1[0].cols();
@@ -382,7 +387,7 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_rotate_backward_kernel(const
             const int t = token(unit, &h0, &heads);
             if (heads <= 0) continue;
             T* to = dx + t * ld_dx + (h0 + row) * a.D;
-            qk_angles(a, t, cs, sn);
+            qk_angles(a, a.pos[t], cs, sn);
             const QkTurn<N> f = qk_turn<HALVES, true>(it, cs, sn, one, one);
             for (int h = row; h - row < heads; h += rows) {
                 cp_async_wait<SLOTS - 2>();
