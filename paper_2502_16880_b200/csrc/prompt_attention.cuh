@@ -13,7 +13,7 @@
 // reference that moves only when a score passes it by 2^8 (P stays below 2^8, its sum is fp32), so O is scaled in place a few times
 // a row at most, by the softmax warps themselves, and nothing else touches it before the end.
 // Masked scores are -inf before anything is computed of them; but a value row with an infinity or a NaN would reach every row of
-// the tile through 0 * inf.  Rows whose result is not finite although their sum is are therefore computed again at the end
+// the tile through 0 * inf.  What stands behind a sequence is made zero in shared memory; for the sequence's own, rows whose result is not finite although their sum is are therefore computed again at the end
 // by a warp each, over the keys that they see; so are those of scores beyond kPaFar.
 // 8192 tokens, 32 query and 8 key heads of 128, bf16: 470 to 490 us, 1.15 PFLOP/s or 69 % of the measured product rate, and less under the
 // power limit (550).  It was 626 with steps of 128 keys and one buffer, 504 with 64 and two, 470 with the longest pairs of tiles first on as
@@ -441,7 +441,16 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
             for (int j = 0; j < n; ++j) {
                 full();
                 if (j < nt) {
-                    const int buf = (done + j) & 1;
+                    const int buf = (done + j) & 1, left = sh.Lk - j * kPaKeys;
+                    // Rows behind the sequence's values get zero (by both tiles' warps alike): what lies there may be anything, and a
+                    // weight of zero times it not zero.
+                    if (left < kPaKeys) {
+                        for (int i = left * 8 + lane; i < kPaKeys * 8; i += 32)
+#pragma unroll
+                            for (int d = 0; d < DB; ++d) *reinterpret_cast<uint4*>(s_kv + stage * kStep + d * kPaBlock + i * 16) = make_uint4(0, 0, 0, 0);
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
                     if (j == 0) pa_wait(smem_u32(&o_free[t]), (uint32_t)(outputs & 1) ^ 1u, &abort_flag, a.st);
                     pa_wait(smem_u32(&p_full[t * 2 + buf]), (uint32_t)((done + j) >> 1) & 1u, &abort_flag, a.st);
                     tc_fence_after();

@@ -158,6 +158,20 @@ def test_rows_beyond_32_bit_offsets():
     assert torch.equal(out, want[0])
 
 
+@pytest.mark.parametrize("D", [64, 72, 128])
+def test_what_stands_behind_a_sequence_does_not_matter(D):
+    """The same bits whatever the rows behind the last sequence, and the next sequence's, hold."""
+    d = _make(3, [300, 77, 130], [310, 77, 200], 4, 2, D, torch.bfloat16, extra_rows=40)
+    want = _run(d)
+    for bad in (NAN, INF):
+        d["k"][587:], d["v"][587:] = bad, bad
+        got = _run(d)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    d["v"][310 + 77:587] = NAN                                 # the third sequence's: the others stay
+    got = _run(d)
+    assert torch.equal(got[0][:377], want[0][:377]) and torch.equal(got[1], want[1]) and got[0][377:507].isnan().all()
+
+
 def test_scales():
     d = _make(6, [90], [90], 2, 1, 64, torch.bfloat16)
     for scale in (1e-30, 0.01, 3.0):
