@@ -7,7 +7,8 @@
 // and so does the output, with p the weights of the softmax:
 //   out = sum over tokens of (p step_g) code + sum of p low_g.
 // Codes go to the warp MMA as fp16 subnormals (two operations a pair, no arithmetic); what is rounded is p step_g, to fp16, as p
-// would be for 16-bit values.
+// would be for 16-bit values, times a power of two that follows the row's and the group's own largest p step_g: what a row does not
+// see, or gives next to no weight, or what other groups hold, takes no bits from it.
 //
 // Layout: tokens in blocks of 16, [page][head][block of 16]: keys, values, (step, low) pairs of keys [group][16], of values.
 //   keys:   [16][4 lanes] of D / 8 bytes: column c is nibble c % 8 of word c / 32 of lane (c / 8) % 4
@@ -232,9 +233,10 @@ __global__ void __launch_bounds__(kKv4RowThreads) kv4_load_kernel(const __grid_c
 // NR MMAs.  A stream has a ring of chunks, filled by its first warp with one bulk copy a block (whatever the page size).  The running
 // maximum is a reference, moved only when a score passes it by 2^8, so that most chunks need one vote and no shuffles.  Long
 // caches are split over blocks, and kv4_join_kernel adds the parts up.
-// 131072 tokens of 8 heads of 128, 4 rows each, bf16: 38 us with the join, 57 % of the copy bandwidth measured; 64 sequences of up to 4096
-// tokens, 4 heads, 7 rows: 35 us, 50 %.  What bounds it: the chain of unpacking, MMA, weights and MMA of a chunk, of which 126 registers leave
-// 16 warps a SM (48 % of the issue slots), and its start, end and join, 5 to 9 us.
+// 131072 tokens of 8 heads of 128, 4 rows each, bf16: 39 us with the join, 56 % of the copy bandwidth measured; 64 sequences of up to 4096
+// tokens, 4 heads, 7 rows: 36 us, 49 %.  (One power of two a warp, by the steps of all its tokens, took 38.9 and 35.2 against 39.1 and 35.9, but
+// left rows without their bits beside a token or group of much larger values.)  What bounds it: the chain of unpacking, MMA, weights and MMA of a
+// chunk, of which 128 registers leave 16 warps a SM (48 % of the issue slots), and its start, end and join, 5 to 9 us.
 constexpr int kKv4Warps = 8;
 constexpr int kKv4Threads = kKv4Warps * 32;
 constexpr int kKv4SpanBlocks = 16;                  // spans of a split are a multiple of so many blocks of 16 tokens
@@ -301,12 +303,15 @@ struct Kv4Rowset {
     // (0.0005 -> 0.0003 of the output; bf16 outputs, rounded to 0.0017, do not show it)
     static constexpr bool kCentre = std::is_same_v<T, __half>;
     using Pair = unsigned long long;
+    // A row moves when one of its p passes 2^8 or an operand 2^15 (fp16 ends below 2^16); its largest p step so far is then brought to
+    // 2^6..2^7, so that what fp16's subnormals lose of an operand is 2^-31 of that at most.
+    static constexpr int kMostPower = 126, kMoved = 6;
+    static constexpr float kMostP = 256.f, kMostOperand = 32768.f;
 
     float acc[NR][J][4];
     float m[NR][2];
     Pair l[NR], corr[NR][NG];
-    float limit;                                             // steps up to here fit the scale of p step, 2^(127 - f_exp)
-    int f_exp;
+    Pair power[NR][NG];                                      // powers of two: acc is in units of 2^-24 / power, operand B is p step power
     // operand B of the scores, sums of the scaled queries (times 2^-24), and what makes a raw score one in powers of two
     uint4 qf[NR][W];
     Pair low[NR][NG], back[NR];
@@ -354,6 +359,7 @@ struct Kv4Rowset {
                 sum[i] *= 0x1p-24f;
                 low[r][i] = pair_of(__shfl_sync(0xffffffffu, sum[i], 8 * c), __shfl_sync(0xffffffffu, sum[i], 8 * c + 4));
                 corr[r][i] = 0;
+                power[r][i] = both(exp2_int(kMostPower));
             }
             back[r] = pair_of(__shfl_sync(0xffffffffu, undo, 8 * c), __shfl_sync(0xffffffffu, undo, 8 * c + 4));
             l[r] = 0;
@@ -368,8 +374,6 @@ struct Kv4Rowset {
 #pragma unroll
                 for (int x = 0; x < 4; ++x) acc[r][j][x] = 0.f;
         }
-        limit = 0.f;
-        f_exp = 127;
     }
 
     // Raw scores of a block's tokens g and g + 8: s[row tile][token].
@@ -412,57 +416,77 @@ struct Kv4Rowset {
         }
     }
 
-    // The maximum's reference and the scale of p step follow what these scores (where seen, x > -inf) and steps ask for.
+    // The reference of the maximum and the powers of rows whose p or operands ask for it: p anew from the raw scores s of the tokens that are
+    // seen (bit ((u NR + r) 2 + h) 2 + e), vp their steps.  A row goes by its own tokens alone: the rest of the warp keeps its bits.
     template <int U>
-    __device__ __forceinline__ void move(const Pair (&s)[U][NR][2], Pair (&x)[U][NR][2], float step) {
+    __device__ __forceinline__ void move(const Pair (&s)[U][NR][2], Pair (&p)[U][NR][2], const uint32_t (&vp)[U][NG][2], uint32_t seen) {
+        const uint32_t mine = 0x11111111u << (threadIdx.x & 3);             // the lanes that have this one's rows
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
             float f[2];
+            bool moves[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float t = m[r][e];
+                float t = m[r][e], most = 0.f, operand = 0.f;
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const float2 now = halves(x[u][r][h]), raw = halves(mul2(s[u][r][h], back[r]));
-                        if ((e ? now.y : now.x) > kNegInf) t = fmaxf(t, e ? raw.y : raw.x);
+                        const float2 raw = halves(mul2(s[u][r][h], back[r])), now = halves(p[u][r][h]);
+                        if (seen >> (((u * NR + r) * 2 + h) * 2 + e) & 1u) t = fmaxf(t, e ? raw.y : raw.x);
+                        most = fmaxf(most, e ? now.y : now.x);
+#pragma unroll
+                        for (int i = 0; i < NG; ++i) {
+                            const float2 w = halves(mul2(mul2(p[u][r][h], both(kv4_pair<T>(vp[u][i][h]).x)), power[r][i]));
+                            operand = fmaxf(operand, e ? w.y : w.x);
+                        }
                     }
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
-                f[e] = m[r][e] == t ? 1.f : exp2_fast(m[r][e] - t);
-                m[r][e] = t;
+                moves[e] = (__ballot_sync(0xffffffffu, most > kMostP || operand > kMostOperand) & mine) != 0;
+                f[e] = !moves[e] || m[r][e] == t ? 1.f : exp2_fast(m[r][e] - t);
+                if (moves[e]) m[r][e] = t;
             }
             const Pair f2 = pair_of(f[0], f[1]);
             l[r] = mul2(l[r], f2);
-#pragma unroll
-            for (int i = 0; i < NG; ++i) corr[r][i] = mul2(corr[r][i], f2);
-#pragma unroll
-            for (int j = 0; j < J; ++j)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) acc[r][j][k] *= f[k & 1];
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     // (the product rounded as in the maximum: of scores beyond 2^24, one fused step would leave more than the 2^8 that p has room for)
-                    const float2 old = halves(x[u][r][h]), now = halves(add2(mul2(s[u][r][h], back[r]), pair_of(-m[r][0], -m[r][1])));
-                    x[u][r][h] = pair_of(old.x == kNegInf ? kNegInf : now.x, old.y == kNegInf ? kNegInf : now.y);
+                    const float2 old = halves(p[u][r][h]), x = halves(add2(mul2(s[u][r][h], back[r]), pair_of(-m[r][0], -m[r][1])));
+                    const uint32_t on = seen >> (((u * NR + r) * 2 + h) * 2);
+                    p[u][r][h] = pair_of(!moves[0] ? old.x : on & 1u ? exp2_fast(x.x) : 0.f, !moves[1] ? old.y : on & 2u ? exp2_fast(x.y) : 0.f);
                 }
-        }
-        const float top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(step)));
-        if (top > limit) {
-            // 2^(127 - f_exp) brings the largest step so far to at most 2^6, and p is at most 2^8: fp16 holds their product
-            const int e = max(1, min((int)(__float_as_uint(top) >> 23), 253));
-            const Q4Power f(f_exp - e);
-            f_exp = e;
-            limit = e + 6 < 254 ? __uint_as_float((uint32_t)(e + 6) << 23) : 3.4e38f;
 #pragma unroll
-            for (int r = 0; r < NR; ++r)
+            for (int i = 0; i < NG; ++i) {
+                corr[r][i] = mul2(corr[r][i], f2);
+                const float2 had = halves(power[r][i]);
+                float now[2];
 #pragma unroll
-                for (int j = 0; j < J; ++j)
+                for (int e = 0; e < 2; ++e) {
+                    // what had the old power's 2^kMoved (or more) counts with what it is now, 2^(kMoved - exponent) f
+                    const int old = (int)(__float_as_uint(e ? had.y : had.x) >> 23);
+                    float largest = exp2_int(kMoved + 127 - old) * f[e];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[r][j][k] = f(acc[r][j][k]);
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float2 w = halves(mul2(p[u][r][h], both(kv4_pair<T>(vp[u][i][h]).x)));     // p is at most 1 here: no overflow
+                            largest = fmaxf(largest, e ? w.y : w.x);
+                        }
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
+                    const int next = moves[e] ? min(max(2 * 127 + kMoved - (int)(__float_as_uint(largest) >> 23), 127 - kMostPower + kMoved), 127 + kMostPower) : old;
+                    now[e] = __uint_as_float((uint32_t)next << 23);
+                    const Q4Power by(next - old);
+#pragma unroll
+                    for (int j = i * J / NG; j < (i + 1) * J / NG; ++j)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) acc[r][j][2 * k + e] = by(acc[r][j][2 * k + e] * f[e]);
+                }
+                power[r][i] = pair_of(now[0], now[1]);
+            }
         }
     }
 
@@ -471,10 +495,11 @@ struct Kv4Rowset {
     template <int U, bool CUT>
     __device__ __forceinline__ void work(const Kv4Args& a, const unsigned char* blk, int token, int q0, int past, int len, uint32_t there) {
         const int lane = threadIdx.x & 31, g = lane >> 2;
-        Pair s[U][NR][2], x[U][NR][2];
+        Pair s[U][NR][2], p[U][NR][2];
 #pragma unroll
         for (int u = 0; u < U; ++u) scores(blk + u * kBytes, s[u]);
-        float above = kNegInf, step = 0.f;
+        float above = 0.f, operand = 0.f, step_top[NG] = {};  // (a NaN is passed over)
+        float2 p_top[NR] = {};
         uint32_t vp[U][NG][2], seen = ~0u;                    // bit ((u NR + r) 2 + h) 2 + e
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -486,12 +511,11 @@ struct Kv4Rowset {
 #pragma unroll
                 for (int i = 0; i < NG; ++i) {
                     vp[u][i][h] = pv[i * 16 + 8 * h];
-                    if (real) step = fmaxf(step, kv4_pair<T>(vp[u][i][h]).x);      // (a NaN is passed over)
+                    step_top[i] = fmaxf(step_top[i], kv4_pair<T>(vp[u][i][h]).x);
                 }
 #pragma unroll
                 for (int r = 0; r < NR; ++r) {
-                    x[u][r][h] = fma2(s[u][r][h], back[r], pair_of(-m[r][0], -m[r][1]));
-                    float2 v = halves(x[u][r][h]);
+                    float2 v = halves(fma2(s[u][r][h], back[r], pair_of(-m[r][0], -m[r][1])));
                     if constexpr (CUT) {
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
@@ -503,43 +527,48 @@ struct Kv4Rowset {
                                 (e ? v.y : v.x) = kNegInf;
                             }
                         }
-                        x[u][r][h] = pair_of(v.x, v.y);
                     }
-                    above = fmaxf(above, fmaxf(v.x, v.y));
+                    v = make_float2(exp2_fast(v.x), exp2_fast(v.y));
+                    p_top[r] = make_float2(fmaxf(p_top[r].x, v.x), fmaxf(p_top[r].y, v.y));
+                    p[u][r][h] = pair_of(v.x, v.y);
                 }
             }
         }
-        if (__any_sync(0xffffffffu, above > 8.f || step > limit)) move<U>(s, x, step);
-        const float f = __uint_as_float((uint32_t)(254 - f_exp) << 23);
+        // Operands are at most the largest p of a row times the largest step, whichever tokens have them (and see them): move() looks closer.
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            above = fmaxf(above, fmaxf(p_top[r].x, p_top[r].y));
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                const float2 w = halves(mul2(mul2(pair_of(p_top[r].x, p_top[r].y), both(step_top[i])), power[r][i]));
+                operand = fmaxf(operand, fmaxf(w.x, w.y));
+            }
+        }
+        if (__any_sync(0xffffffffu, above > kMostP || operand > kMostOperand)) move<U>(s, p, vp, seen);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             uint32_t b[NR][NG][2];
-            Pair p[NR][2];
 #pragma unroll
             for (int r = 0; r < NR; ++r)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float2 v = halves(x[u][r][h]);
-                    p[r][h] = pair_of(exp2_fast(v.x), exp2_fast(v.y));
-                    l[r] = add2(l[r], p[r][h]);
-                }
+                for (int h = 0; h < 2; ++h) l[r] = add2(l[r], p[u][r][h]);
 #pragma unroll
             for (int i = 0; i < NG; ++i)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float2 pr = kv4_pair<T>(vp[u][i][h]);
-                    const Pair by = both(pr.x * f), lowest = both(kCentre ? fmaf(8.f, pr.x, pr.y) : pr.y);
+                    const Pair step = both(pr.x), lowest = both(kCentre ? fmaf(8.f, pr.x, pr.y) : pr.y);
 #pragma unroll
                     for (int r = 0; r < NR; ++r) {
                         float2 w;
                         if constexpr (CUT) {                  // a step or lowest value that is not finite has no part in what is not seen
                             const uint32_t on = seen >> (((u * NR + r) * 2 + h) * 2);
-                            const float2 q = halves(mul2(p[r][h], by)), y = halves(mul2(p[r][h], lowest));
+                            const float2 q = halves(mul2(mul2(p[u][r][h], step), power[r][i])), y = halves(mul2(p[u][r][h], lowest));
                             w = make_float2(on & 1u ? q.x : 0.f, on & 2u ? q.y : 0.f);
                             corr[r][i] = add2(corr[r][i], pair_of(on & 1u ? y.x : 0.f, on & 2u ? y.y : 0.f));
                         } else {
-                            w = halves(mul2(p[r][h], by));
-                            corr[r][i] = fma2(p[r][h], lowest, corr[r][i]);
+                            w = halves(mul2(mul2(p[u][r][h], step), power[r][i]));
+                            corr[r][i] = fma2(p[u][r][h], lowest, corr[r][i]);
                         }
                         b[r][i][h] = tile_transpose(half_pair(w.x, w.y));
                     }
@@ -585,15 +614,18 @@ struct Kv4Rowset {
             }
             return f;
         };
-        const Q4Power undo(f_exp - 127 + 24);
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
             float fix[NG][2];
+            Q4Power undo[NG][2];
 #pragma unroll
             for (int i = 0; i < NG; ++i) {
                 const float2 v = over_lanes(corr[r][i]);
                 fix[i][0] = v.x;
                 fix[i][1] = v.y;
+                const float2 had = halves(power[r][i]);
+                undo[i][0] = Q4Power(127 + 24 - (int)(__float_as_uint(had.x) >> 23));
+                undo[i][1] = Q4Power(127 + 24 - (int)(__float_as_uint(had.y) >> 23));
             }
             const float2 sum = over_lanes(l[r]);
 #pragma unroll
@@ -602,8 +634,8 @@ struct Kv4Rowset {
                 if (g == 0) ml[row] = make_float2(m[r][h], h ? sum.y : sum.x);
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
-                    out[row * D + 16 * j + g] = undo(acc[r][j][h]) + fix[j * NG / J][h];
-                    out[row * D + 16 * j + 8 + g] = undo(acc[r][j][2 + h]) * 0.0625f + fix[j * NG / J][h];
+                    out[row * D + 16 * j + g] = undo[j * NG / J][h](acc[r][j][h]) + fix[j * NG / J][h];
+                    out[row * D + 16 * j + 8 + g] = undo[j * NG / J][h](acc[r][j][2 + h]) * 0.0625f + fix[j * NG / J][h];
                 }
             }
         }
