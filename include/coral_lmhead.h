@@ -649,8 +649,9 @@ int coral_lmhead_kv4_load(const coral_lmhead_kv4_config *cfg, const void *cache_
  *   out = sum_j softmax_j(scale q . k_j) v_j  over j <= lens - n + i (tree_mask NULL), or over the j < lens - n and those
  *   j = lens - n + b with bit b of the row's tree_mask word (a node sees its ancestors and itself);  lse = log-sum-exp of scale q . k_j.
  * Sums and softmax in fp32.  For the product with the values a weight times a value's step (next to the largest such product of the same row and
- * group of columns), or from 33 rows of a key head on (max_q n_q / n_heads) a value, is rounded to fp16 (a weight too, where outputs are bf16).  A
- * row that sees nothing has out 0 and lse -inf.
+ * group of columns), or from 33 rows of a key head on (max_q n_q / n_heads) a value, is rounded to fp16 (a weight too, where outputs are bf16).
+ * Queries enter as fp16 next to the largest element of their row: what is 2^-39 of it is lost.  From 33 rows on so is what is 2^-39 of the largest key
+ * of 64 tokens (but for tokens whose keys are all below 2^-17 of it).  A row that sees nothing has out 0 and lse -inf.
  * Tokens that a row does not see have no influence, infinities and NaN too; pages outside [0, n_pages) hold no tokens.
  *   q, out [n_rows x n_q x D] of the cache's type; out_lse fp32 [n_rows x n_q] or NULL; n_q a multiple of n_heads.  Rows outside the
  *   sequences, and a sequence's rows from max_q on, are left as they are.  lens is clamped to width * page, offsets to n_rows.

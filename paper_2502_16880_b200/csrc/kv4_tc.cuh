@@ -8,9 +8,9 @@
 //   * a thread of the softmax has a row: P = exp2(S c kf - m) in fp16 (for fp16 outputs in two parts), with the step's key power kf in the
 //     factor and its value power in the reference m, which so follows the largest score and the largest value; P stays below 2^15 whatever
 //     the values' size,
-//   * fp16 holds 40 powers of two: where a token's keys or values lie so far below a step's or a former step's largest ones (which a row may
-//     not even see) that bits of them would be lost, a warp computes each row that meets them again, in fp32 (kt_row_again); also scores
-//     beyond kPaFar.
+//   * fp16 holds 40 powers of two: where a token's key, or a group of its values, lies so far below a step's or a former step's largest ones (which
+//     a row may not even see) that bits of them would be lost, a warp computes each row that meets them again, in fp32 (kt_row_again);
+//     also scores beyond kPaFar.
 // Columns lie in another order than in memory: 0 4 1 5 2 6 3 7 within eight (queries and keys alike, for the sums it is all one), and
 // place by place for the values (column 8 i + n at n D / 8 + ...), which the outputs undo.
 // 8 sequences x 8 key heads, trees of 60 nodes x 4 heads, 3001 tokens, fp16: 68 us with the join (11 at the tensor cores' measured rate); 66 with
@@ -46,8 +46,8 @@ __device__ __forceinline__ float kt_largest(float top, uint32_t pair) {
     const float2 p = kv4_pair<T>(pair);
     return fmaxf(top, fmaxf(fabsf(p.y), fabsf(fmaf(15.f, p.x, p.y))));
 }
-// Whether a token whose largest value is `own` would lose bits next to `top`: fp16 holds 2^-25 of what `top` brings to 2^14 or more, which has to be
-// 2^-22 of a key and 2^-13 of a value.
+// Whether a token's key, or a group of its values (which has outputs of its own), whose largest is `own` would lose bits next to `top`: fp16 holds
+// 2^-25 of what `top` brings to 2^14 or more, which has to be 2^-22 of the key and 2^-13 of the group.
 __device__ __forceinline__ bool kt_lost(float own, float top, bool value) { return own > 0.f && own < top * (value ? 0x1p-26f : 0x1p-17f); }
 __device__ __forceinline__ float kt_power(float top) {
     const int e = min(max((int)(__float_as_uint(top) >> 23), 16), 254);
@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
                 const int slot = j % kKtRaw;
                 pa_wait(smem_u32(&raw_full[slot]), (uint32_t)(j / kKtRaw) & 1u, &abort_flag, a.st);
                 const uint32_t there = present[j % kKtPresent];
-                float top_k[2] = {0.f, 0.f}, top_v[2] = {0.f, 0.f};
+                float top_k[2] = {0.f, 0.f}, top_v[2] = {0.f, 0.f}, least_v = 3.4e38f;      // least_v: of groups, zeros aside
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int token = lane + 32 * i;
@@ -473,13 +473,15 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
                         top_k[i] = kt_largest<T>(top_k[i], pairs[g * 16]);
-                        top_v[i] = kt_largest<T>(top_v[i], pairs[(NG + g) * 16]);
+                        const float own = kt_largest<T>(0.f, pairs[(NG + g) * 16]);
+                        top_v[i] = fmaxf(top_v[i], own);
+                        if (own > 0.f) least_v = fminf(least_v, own);
                     }
                 }
                 const float all_k = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(top_k[0], top_k[1]))));
                 const float all_v = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(top_v[0], top_v[1]))));
                 const uint32_t lost = __ballot_sync(0xffffffffu, kt_lost(top_k[0], all_k, false) || kt_lost(top_k[1], all_k, false) ||
-                                                                     kt_lost(top_v[0], all_v, true) || kt_lost(top_v[1], all_v, true));
+                                                                     kt_lost(least_v, all_v, true));
                 if (all_v > 0.f) before = kt_power(all_v);
                 if (lane == 0) {
                     s_power[j % kKtPowers] = make_float2(kt_power(all_k), before);

@@ -4,13 +4,15 @@ no weight, or a group of columns, 2^8 to 2^100 times the rest.  Each row, and ea
 Values are ones that 4 bits hold exactly (a power of two times those of test_gpu_kv4).  Tolerances, u = 2^-24, e a score's error as there.
 Up to 32 rows of a key head: p step is rounded to fp16, 2^-11 relative next to codes of up to 15, and where it is subnormal 2^-25 absolute of a scale
 that brings the row's and group's own largest p step to 2^6 or more: 2^-31 of that one.  With w the weights, n of them:
-|out - want| <= (2 e + (4 n + 64) u) sum w (|low| + 15 step) + 2^-11 sum w 15 step + 2^-31 15 n max(w step), plus the output's rounding."""
+|out - want| <= (2 e + (4 n + 64) u) sum w (|low| + 15 step) + 2^-11 sum w 15 step + 2^-31 15 n max(w step), plus the output's rounding.
+More rows: the tolerances of test_gpu_kv4_many_rows, which go by a column's own values."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import attention_oracle as ao
 from tests.test_gpu_kv4 import Case, TYPES, U, _exact
+from tests.test_gpu_kv4_many_rows import Many
 
 pytestmark = pytest.mark.gpu
 # The largest power, and how many powers below 2^-3 the ordinary steps are (fp16: steps of 2^-11 and 2^9).
@@ -116,3 +118,16 @@ def test_rows_are_the_same_bits_whatever_they_do_not_see(n, n_q, n_k):
         got = c.run()
         assert torch.equal(got[0][:-1], want[0][:-1]) and torch.equal(got[1][:-1], want[1][:-1])
         assert not torch.equal(got[0][-1], want[0][-1])
+
+@pytest.mark.parametrize("n,n_q,n_k,lens", [(40, 4, 2, [100, 300]), (64, 2, 1, [4000])])
+@pytest.mark.parametrize("far", [30, -60, 100])
+def test_groups_of_columns_with_many_rows(far, n, n_q, n_k, lens):
+    """Values of one group of columns 2^far times those of the next; keys 2^20 apart, with queries that make up for it."""
+    def first(by, f):
+        by[:, :, 0] = f
+    c = Many(far + 200, lens, n, n_q, n_k, 64, 32, 16, torch.bfloat16, tree=True, values=_scaled(first, far))
+    c.check(c.run())
+    power = 20 if far > 0 else -20
+    c = Many(far + 201, lens, n, n_q, n_k, 64, 32, 16, torch.bfloat16, tree=True, values=_scaled(first, power, keys=True))
+    c.q[..., :32] = (c.q[..., :32].float() * 2.0 ** -power).to(c.t)
+    c.check(c.run())
