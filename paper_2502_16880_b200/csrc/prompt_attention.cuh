@@ -13,8 +13,10 @@
 // reference that moves only when a score passes it by 2^8 (P stays below 2^8, its sum is fp32), so O is scaled in place a few times
 // a row at most, by the softmax warps themselves, and nothing else touches it before the end.
 // Masked scores are -inf before anything is computed of them; but a value row with an infinity or a NaN would reach every row of
-// the tile through 0 * inf.  What stands behind a sequence is made zero in shared memory; for the sequence's own, rows whose result is not finite although their sum is are therefore computed again at the end
-// by a warp each, over the keys that they see; so are those of scores beyond kPaFar.
+// the tile through 0 * inf.  What stands behind a sequence is made zero in shared memory; for the sequence's own, rows whose result is not
+// finite although their sum is are computed again by a warp each, over the keys that they see, unless that is what the values they see
+// make of it; so are those of scores beyond kPaFar.  That takes as long as there are keys, so it comes when the block's turns are over and
+// no warp waits any more (the waits are bounded).
 // 8192 tokens, 32 query and 8 key heads of 128, bf16: 470 to 490 us, 1.15 PFLOP/s or 69 % of the measured product rate, and less under the
 // power limit (550).  It was 626 with steps of 128 keys and one buffer, 504 with 64 and two, 470 with the longest pairs of tiles first on as
 // many blocks as there are SMs and the next pair's operands loaded ahead.  What bounds it: a step of both tiles takes 1640 cycles, in which the products read operands from shared
@@ -282,6 +284,32 @@ __device__ __noinline__ void pa_row_again(const PaArgs& a, const T* q, const T* 
     if (lse && lane == 0) *lse = sum == 0.f ? kNegInf : (top + log2f(sum)) * 0.69314718055994531f;
 }
 
+// What stands in the first output of a row that is to be computed again until that is done: a NaN as no conversion gives it.
+constexpr uint16_t kPaAgain = 0x7fa1;
+
+// Whether any of eight 16-bit elements is an infinity or a NaN.
+template <typename T>
+__device__ __forceinline__ bool pa_bad8(const uint4& w) {
+    constexpr uint32_t kOnes = std::is_same_v<T, __half> ? 0x7c007c00u : 0x7f807f80u;          // two exponents
+    return (__vcmpeq2(w.x & kOnes, kOnes) | __vcmpeq2(w.y & kOnes, kOnes) | __vcmpeq2(w.z & kOnes, kOnes) | __vcmpeq2(w.w & kOnes, kOnes)) != 0;
+}
+// The first of the rows from .. end that holds an infinity or a NaN (LAST: the last), by a warp; `end` (-1) if none does.
+template <typename T, bool LAST>
+__device__ __noinline__ int pa_bad_row(const T* v, long long ld, int D, int from, int end) {
+    const int per = D / 8;
+    int bad = LAST ? -1 : end;
+    for (int j0 = from; j0 < end && (LAST || bad == end); j0 += 64) {
+        const int n = min(64, end - j0);
+        for (int i = threadIdx.x & 31; i < n * per; i += 32) {
+            const int j = i / per;
+            if (!pa_bad8<T>(*reinterpret_cast<const uint4*>(v + (long long)(j0 + j) * ld + (i - j * per) * 8))) continue;
+            bad = LAST ? max(bad, j0 + j) : min(bad, j0 + j);
+        }
+        bad = LAST ? __reduce_max_sync(0xffffffffu, bad) : __reduce_min_sync(0xffffffffu, bad);
+    }
+    return bad;
+}
+
 // DB: blocks of 64 columns of a head (1 or 2).  Stages: steps' keys or values in the ring.
 template <int DB> constexpr int kPaStages = DB == 2 ? 10 : 16;
 template <int DB> constexpr size_t pa_smem_bytes() { return 1024 + (size_t)DB * (2 * kPaRows + kPaStages<DB> * kPaBlock); }
@@ -478,12 +506,12 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
         const int t = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = tmem + t * 128 + lanes, to = tmem + 256 + t * 128 + lanes;
-        int done = 0;                                          // steps of this tile in earlier turns
+        int done = 0, first_again = turns;                     // steps of this tile in earlier turns; the first with a row to be computed again
         for (int turn = 0; turn < turns; ++turn) {
             const PaShare sh = share_of(turn, false);
             if (sh.pair < 0) continue;
             const PaUnit u(a, sh);
-            const int nt = u.n[t], tok0 = u.token0(t), past = u.past, kv_head = u.kv_head;
+            const int nt = u.n[t], tok0 = u.token0(t), past = u.past;
             if (tok0 >= sh.Lq) continue;
             const int tok = tok0 + (row >> a.gp_log2), head = u.head0 + (row & (a.gp - 1));
             const int seen = max(0, min(tok + past + 1, sh.Lk));   // keys that this row sees
@@ -590,17 +618,42 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
             }
             if (live && a.lse) a.lse[(long long)(sh.q0 + tok) * a.n_q + head] = sum == 0.f ? kNegInf : (mc + log2f(sum)) * 0.69314718055994531f;
             // Rows of finite weights whose result is not (values that they do not see may be the reason), and those of scores too large.
-            const bool again = live && (far || (sum > 0.f && sum < __int_as_float(0x7f800000) && odd != 0.f));
-            __syncwarp();
-            for (uint32_t todo = __ballot_sync(0xffffffffu, again); todo; todo &= todo - 1) {
-                const int r = __ffs(todo) - 1;
-                const int tok_r = __shfl_sync(0xffffffffu, tok, r), head_r = __shfl_sync(0xffffffffu, head, r), seen_r = __shfl_sync(0xffffffffu, seen, r);
-                const bool far_r = __shfl_sync(0xffffffffu, far, r);
-                pa_row_again<T>(a, static_cast<const T*>(a.q) + (long long)(sh.q0 + tok_r) * a.ld_q + (long long)head_r * a.D,
-                                static_cast<const T*>(a.k) + (long long)sh.k0 * a.ld_k + (long long)kv_head * a.D,
-                                static_cast<const T*>(a.v) + (long long)sh.k0 * a.ld_v + (long long)kv_head * a.D, seen_r,
-                                static_cast<T*>(a.out) + (long long)(sh.q0 + tok_r) * a.ld_out + (long long)head_r * a.D,
-                                far_r && a.lse ? a.lse + (long long)(sh.q0 + tok_r) * a.n_q + head_r : nullptr);
+            far = far && live;
+            if (far) *reinterpret_cast<uint16_t*>(out) = kPaAgain;
+            if (__any_sync(0xffffffffu, far || (live && sum > 0.f && sum < __int_as_float(0x7f800000) && odd != 0.f))) first_again = min(first_again, turn);
+        }
+        if (first_again < turns) {
+            PaFinder find(a);
+            for (int turn = first_again; turn < turns; ++turn) {
+                const int unit = pa_unit(a, turn);
+                if (unit < 0) continue;
+                const PaShare sh = find(a, unit);
+                if (sh.pair < 0) continue;
+                const PaUnit u(a, sh);
+                const int tok = u.token0(t) + (row >> a.gp_log2), head = u.head0 + (row & (a.gp - 1)), seen = max(0, min(tok + u.past + 1, sh.Lk));
+                const T* v = static_cast<const T*>(a.v) + (long long)sh.k0 * a.ld_v + (long long)u.kv_head * a.D;
+                T* out = static_cast<T*>(a.out) + (long long)(sh.q0 + tok) * a.ld_out + (long long)head * a.D;
+                bool odd = false, far = false;                     // by what this thread wrote
+                if (tok < sh.Lq) {
+                    far = *reinterpret_cast<const uint16_t*>(out) == kPaAgain;
+                    for (int c = 0; c < a.D; c += 8) odd |= pa_bad8<T>(*reinterpret_cast<const uint4*>(out + c));
+                }
+                // Not finite, and rightly so: the row sees a value of that kind, and its last step held none that it does not see.  (fp16 has no
+                // weights below 2^-25, and zero times an infinity is a NaN where the sum is infinite: there all are computed again.)
+                if (std::is_same_v<T, __nv_bfloat16> && __any_sync(0xffffffffu, odd && !far)) {
+                    const int end = min(u.n[t] * kPaKeys, sh.Lk), least = __reduce_min_sync(0xffffffffu, odd ? seen : end);
+                    const int last = pa_bad_row<T, true>(v, a.ld_v, a.D, least, end);
+                    const int first = pa_bad_row<T, false>(v, a.ld_v, a.D, 0, __reduce_max_sync(0xffffffffu, odd ? seen : 0));
+                    odd = odd && (last >= seen || first >= seen);
+                }
+                for (uint32_t todo = __ballot_sync(0xffffffffu, odd || far); todo; todo &= todo - 1) {
+                    const int r = __ffs(todo) - 1, tok_r = __shfl_sync(0xffffffffu, tok, r), head_r = __shfl_sync(0xffffffffu, head, r);
+                    const bool lse_r = __shfl_sync(0xffffffffu, far, r) && a.lse;
+                    pa_row_again<T>(a, static_cast<const T*>(a.q) + (long long)(sh.q0 + tok_r) * a.ld_q + (long long)head_r * a.D,
+                                    static_cast<const T*>(a.k) + (long long)sh.k0 * a.ld_k + (long long)u.kv_head * a.D, v, __shfl_sync(0xffffffffu, seen, r),
+                                    static_cast<T*>(a.out) + (long long)(sh.q0 + tok_r) * a.ld_out + (long long)head_r * a.D,
+                                    lse_r ? a.lse + (long long)(sh.q0 + tok_r) * a.n_q + head_r : nullptr);
+                }
             }
         }
     }
