@@ -10,8 +10,8 @@
 // and some of its heads at a time: it computes the token's angles once, the product position * freq and what is left of it after
 // whole turns in 64 bits (in 32, a position of a million is off by a tenth of a turn), and its threads keep what their item
 // needs of them, times the weights, in registers over all of those heads.  No block-wide barrier but for the column sums.
-// 16384 tokens of 32 + 8 heads of 128, bf16: 56 us, 91 % of the copy bandwidth measured (75 before a warp kept a token's factors over its
-// heads and loaded rows ahead, 58 with each position read where it is needed).  Gradient of 8192 tokens: 57 us, 68 % (136 before; 62 with one
+// 16384 tokens of 32 + 8 heads of 128, bf16: 58.7 us, 87 % of the copy bandwidth measured (75 before a warp kept a token's factors over its
+// heads and loaded rows ahead, 60 with each position read where it is needed).  Gradient of 8192 tokens: 58 us, 66 % (136 before; 62 with one
 // row ahead in registers): 126 registers leave 16 warps a SM, each token's angles are computed for the queries and again for the keys, and the
 // column sums' second kernel takes 4 of it.
 #pragma once
@@ -119,23 +119,33 @@ struct QkItem {
 };
 
 // The turn of an item as factors, times weights: u' = u uc + v~ us, v' = v vc + u~ vs, where v~ is the other granule (HALVES) or the
-// granule itself with the members of its pairs exchanged.  Columns that are not turned have the factors (weight, 0).
+// granule itself with the members of its pairs exchanged.  A granule that is not turned has the weight for a factor and no second term (zero
+// times an infinity in a column that is none of its business would be a NaN).
 template <int N> struct QkTurn {
     QkCols<N> uc, us, vc, vs;
     template <bool HALVES>
-    __device__ __forceinline__ void operator()(QkCols<N>& u, QkCols<N>& v) const {
+    __device__ __forceinline__ void operator()(QkCols<N>& u, QkCols<N>& v, bool turn_u, bool turn_v) const {
+        if (turn_u && turn_v) {                      // (in one piece: granule by granule it is 2 % slower)
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            const unsigned long long a = u.p[i], b = v.p[i];
-            unsigned long long a2 = a, b2 = b;
-            if (!HALVES) {
-                const float2 x = halves(a), y = halves(b);
-                a2 = pair_of(x.y, x.x);
-                b2 = pair_of(y.y, y.x);
+            for (int i = 0; i < N / 2; ++i) {
+                const unsigned long long a = u.p[i], b = v.p[i];
+                u.p[i] = fma2(HALVES ? b : exchanged(a), us.p[i], mul2(a, uc.p[i]));
+                v.p[i] = fma2(HALVES ? a : exchanged(b), vs.p[i], mul2(b, vc.p[i]));
             }
-            u.p[i] = fma2(HALVES ? b2 : a2, us.p[i], mul2(a, uc.p[i]));
-            v.p[i] = fma2(HALVES ? a2 : b2, vs.p[i], mul2(b, vc.p[i]));
+        } else {                                     // (of two halves none is turned alone)
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                const unsigned long long a = u.p[i], b = v.p[i];
+                u.p[i] = mul2(a, uc.p[i]);
+                v.p[i] = mul2(b, vc.p[i]);
+                if (!HALVES && turn_u) u.p[i] = fma2(exchanged(a), us.p[i], u.p[i]);
+                if (!HALVES && turn_v) v.p[i] = fma2(exchanged(b), vs.p[i], v.p[i]);
+            }
         }
+    }
+    static __device__ __forceinline__ unsigned long long exchanged(unsigned long long a) {
+        const float2 x = halves(a);
+        return pair_of(x.y, x.x);
     }
 };
 // wu, wv: the weights of the item's own columns.  BACK: the opposite angle.
@@ -265,7 +275,7 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_rotate_kernel(const __grid_c
                         u = scale_cols(u, r);
                         v = scale_cols(v, r);
                     }
-                    f.template operator()<HALVES>(u, v);
+                    f.template operator()<HALVES>(u, v, it.turn0, it.turn1);
                     if (h + i * rows < heads) it.store(to + i * step, u, v);
                     u0[i] = u1[i];
                     v0[i] = v1[i];
@@ -396,7 +406,7 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_rotate_backward_kernel(const
                 fetch(slot == 0 ? SLOTS - 1 : slot - 1);           // the row before: its values are in use
                 slot = slot + 1 == SLOTS ? 0 : slot + 1;
                 QkCols<N> du = p0.cols(), dv = q0.cols();
-                f.template operator()<HALVES>(du, dv);
+                f.template operator()<HALVES>(du, dv, it.turn0, it.turn1);
                 if (w) {
                     QkCols<N> u = u0.cols(), v = v0.cols();
                     const QkCols<N> dwu = mul_cols(du, wu), dwv = mul_cols(dv, wv);
