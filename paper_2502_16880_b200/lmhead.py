@@ -450,7 +450,7 @@ def _op_ptr(name, t, dtype, shape, dev):
 
 def _op_device(t, name) -> int:
     dev = t.get_device()
-    if dev < 0 or dev != torch._C._cuda_getDevice():
+    if dev < 0 or dev != torch.cuda.current_device():
         raise ValueError(f"{name} must be on the current CUDA device")
     return dev
 
