@@ -160,11 +160,9 @@ Kv4Plan kv4_plan(const coral_lmhead_kv4_config* c, const coral_lmhead_kv4_attent
     Kv4Plan p{};
     const long long rows = (long long)a->max_q * (a->n_q / c->n_heads);
     p.nr = rows <= 8 ? 1 : rows < kKv4ManyFrom ? 2 : 0;
-    p.row_groups = 1;
-    if (p.nr)
-        for (; p.row_groups < kKv4Warps && p.row_groups * 8 * p.nr < rows; p.row_groups *= 2) {}
-    const int per_block = p.nr ? p.row_groups * 8 * p.nr : 256;
-    p.row_blocks = (int)((rows - 1) / per_block + 1);
+    static_assert(kKv4ManyFrom <= 2 * 8 * 2 + 1, "two row groups of two tiles of eight rows are what kv4_attention_kernel takes");
+    p.row_groups = p.nr && rows > 8 * p.nr ? 2 : 1;
+    p.row_blocks = p.nr ? 1 : (int)((rows - 1) / 256 + 1);
     p.units = (long long)a->n_seq * c->n_heads * p.row_blocks;
     // The number of parts whose rounds of resident blocks take the least, a block counted as its tokens plus 512 for what it begins and
     // ends with (64 sequences of up to 4096 tokens, 256 blocks unsplit: 58 us in 5 parts, 35 in one).  A part has a span at least.

@@ -225,8 +225,8 @@ __global__ void __launch_bounds__(kKv4RowThreads) kv4_load_kernel(const __grid_c
 }
 
 // ---- attention -----------------------------------------------------------------------------------------------
-// A block takes up to 8 NR row_groups rows (query tokens of a sequence times the query heads of one key head) and a span of the
-// sequence's cache.  Its eight warps are row groups of `parts` warps; warp i of each group takes every parts-th chunk of U blocks
+// A block takes all rows of a key head (query tokens of a sequence times the query heads; 8 NR row_groups at most, with row_groups 1 or 2) and a
+// span of the sequence's cache.  Its eight warps are row groups of `parts` warps; warp i of each group takes every parts-th chunk of U blocks
 // of 16 tokens, so the warps of one number share a stream of chunks and the others do without them:
 //   scores  [16 tokens x 8 rows] = K (operand A, unpacked) Q^T,   out [D x 8 rows] += V^T (operand A, unpacked) P^T
 // with tokens and columns on the MMA's long side, so one sequence's few rows cost no more than 8 and an unpacked operand serves
@@ -246,7 +246,8 @@ constexpr int kKv4MaxTree = 64;                     // query tokens under a tree
 struct Kv4Args {
     Kv4Cache c;
     int n_seq, n_rows, max_q, n_q, G, width, n_pages;
-    int row_groups, row_blocks, splits, slots;      // slots: chunks of a stream's ring
+    int row_groups, splits, slots;                  // (up to 32 rows) row groups, and chunks of a stream's ring
+    int row_blocks;                                 // (more) blocks that share a key head's rows
     float scale2;                                   // scale log2(e)
     long long ld_table, ld_q, ld_out;
     const void* q;
@@ -672,13 +673,11 @@ __global__ void __launch_bounds__(kKv4Threads, NR == 1 ? 2 : 1) kv4_attention_ke
     unsigned unit = blockIdx.x;
     const int split = unit % a.splits;
     unit /= a.splits;
-    const int row_block = unit % a.row_blocks;
-    unit /= a.row_blocks;
     const int head = unit % a.c.n_k, seq = unit / a.c.n_k;
     int q0, n;
     kv4_rows_of(a, seq, &q0, &n);
-    const int rows = min(n, a.max_q) * a.G, row0 = row_block * 8 * NR * a.row_groups;
-    if (row0 >= rows) return;
+    const int rows = min(n, a.max_q) * a.G;
+    if (rows == 0) return;
     const int len = (int)max(0LL, min((long long)a.lens[seq], min((long long)a.width * a.c.page, 0x7fff0000LL)));
     const int spans = (len + kKv4SpanBlocks * kKv4Block - 1) / (kKv4SpanBlocks * kKv4Block), per = (spans + a.splits - 1) / a.splits;
     // chunks of this block, and those of this warp's stream: from + mine, from + mine + parts, ...
@@ -710,8 +709,8 @@ __global__ void __launch_bounds__(kKv4Threads, NR == 1 ? 2 : 1) kv4_attention_ke
     if (group == 0)
         for (int i = 0; i < min(a.slots, chunks); ++i) copy(i, i);
     Rowset set;
-    set.begin(a, q0, head, row0 + group * 8 * NR, rows);
-    const bool live = row0 + group * NR * 8 < rows;
+    set.begin(a, q0, head, group * 8 * NR, rows);
+    const bool live = group * NR * 8 < rows;
     const int past = len - n, open = past + (a.tree ? 0 : 1);          // every row sees the tokens before `open`
     int slot = 0;
     uint32_t phase = 0;
@@ -744,8 +743,8 @@ __global__ void __launch_bounds__(kKv4Threads, NR == 1 ? 2 : 1) kv4_attention_ke
     __syncthreads();
     // the warps of a row group, four columns a thread
     for (int i = threadIdx.x; i < a.row_groups * 8 * NR * (D / 4); i += kKv4Threads) {
-        const int local = i / (D / 4), col = (i - local * (D / 4)) * 4;
-        const int grp = local / (8 * NR), r = local - grp * 8 * NR, row = row0 + local;
+        const int row = i / (D / 4), col = (i - row * (D / 4)) * 4;
+        const int grp = row / (8 * NR), r = row - grp * 8 * NR;
         if (row >= rows) continue;
         float top = kNegInf;
         for (int w = 0; w < parts; ++w) top = fmaxf(top, s_ml[grp * parts + w][r].x);
