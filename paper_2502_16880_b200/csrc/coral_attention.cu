@@ -77,6 +77,7 @@ template <typename T, bool HALVES, int N, int L>
 cudaError_t launch_qk_kernel(const QkArgs& k, bool backward, int grid, cudaStream_t st) {
     if (!backward) return launch_pdl(qk_rotate_kernel<T, HALVES, N, L>, dim3(grid), dim3(kQkThreads), 0, st, k);
     constexpr size_t smem = (size_t)kQkSlots<T, N> * kQkStep<T, N>;
+    static_assert(kQkStatic<N> <= kMostStatic, "what allow_smem counts with");
     if (!allow_smem(qk_rotate_backward_kernel<T, HALVES, N, L>, smem)) return cudaErrorUnknown;
     return launch_pdl(qk_rotate_backward_kernel<T, HALVES, N, L>, dim3(grid), dim3(kQkThreads), smem, st, k);
 }

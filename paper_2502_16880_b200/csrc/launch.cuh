@@ -32,11 +32,12 @@ inline bool device_sms(int* sms) {
     return cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess;
 }
 
-// The attribute is per kernel and device; above 48 KB, static shared memory (at most 16 KB in kernels that have both) counted in, it has
+// The attribute is per kernel and device; above 48 KB, static shared memory (at most kMostStatic in kernels that have both) counted in, it has
 // to be raised before the launch.
+constexpr size_t kMostStatic = 24 * 1024;
 template <typename K>
 bool allow_smem(K kernel, size_t bytes) {
-    return bytes <= 32 * 1024 ||
+    return bytes <= 48 * 1024 - kMostStatic ||
            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
 }
 

@@ -292,6 +292,8 @@ __global__ void __launch_bounds__(kQkThreads, 2) qk_rotate_kernel(const __grid_c
 // several rows ahead and across tokens: registers have room for one row ahead only.
 template <typename T, int N> constexpr int kQkStep = 4 * N * (int)sizeof(T) * kQkThreads;          // a row of each thread: two granules of dy and of x
 template <typename T, int N> constexpr int kQkSlots = 80 * 1024 / kQkStep<T, N>;
+// Static shared memory of the kernel: angles of its warps, sums of its threads.
+template <int N> constexpr size_t kQkStatic = 2 * kQkWarps * (kQkMaxD / 2) * sizeof(float) + 2 * N * kQkThreads * sizeof(float);
 template <typename T, int N>
 struct QkRing {
     static constexpr int kBytes = N * (int)sizeof(T);
