@@ -10,11 +10,11 @@
 //     the values' size,
 //   * fp16 holds 40 powers of two: where a token's key, or a group of its values, lies so far below a step's or a former step's largest ones (which
 //     a row may not even see) that bits of them would be lost, a warp computes each row that meets them again, in fp32 (kt_row_again);
-//     also scores beyond kPaFar.
+//     also scores beyond kPaFar, and results that are not finite, unless values that the row sees are the only such ones in sight.
 // Columns lie in another order than in memory: 0 4 1 5 2 6 3 7 within eight (queries and keys alike, for the sums it is all one), and
 // place by place for the values (column 8 i + n at n D / 8 + ...), which the outputs undo.
-// 8 sequences x 8 key heads, trees of 60 nodes x 4 heads, 3001 tokens, fp16: 68 us with the join (11 at the tensor cores' measured rate); 66 with
-// one part of a weight, 60 with one tile of the keys too, whose log of sums was off by 5e-4 where few tokens are seen.  What bounds it: 64 tokens
+// 8 sequences x 8 key heads, trees of 60 nodes x 4 heads, 3001 tokens, fp16: 71 us with the join (11 at the tensor cores' measured rate), of which
+// the question why a row is not finite costs 0.6; when that took 70, 66 with one part of a weight, 60 with one tile of the keys too, whose log of sums was off by 5e-4 where few tokens are seen.  What bounds it: 64 tokens
 // take 3500 cycles, of which the products' operands read shared memory for 2500 (2.5 times those of prompt_attention.cuh, since keys count
 // twice), and an unpacking warp is busy all the time, keys 1700 and values 1000 (with one tile of rows it alone sets the 3100 cycles).
 #pragma once
@@ -90,20 +90,42 @@ __device__ __forceinline__ KtTwo kt_values_two(uint32_t w, unsigned long long st
 __device__ __forceinline__ uint32_t kt_chunk(int row, int chunk, int rows) { return (chunk >> 3) * rows * 128 + row * 128 + ((chunk ^ row) & 7) * 16; }
 
 // Tokens `from` to `len` of a row, by a warp in fp32, from the packed tokens that it sees: the reference m (a power of two), the sum of the weights
-// 2^(score - m), and the weighted sum of the values, D / 32 columns a lane.
+// 2^(score - m), and the weighted sum of the values, D / 32 columns a lane.  ASK: only if it is not values that the row sees, and no others, that
+// are not finite (false: what the row has is right).
 template <typename T, int D, int NG>
-__device__ __noinline__ void kt_row_again(const Kv4Args& a, const int32_t* table, int head, const T* q, int from, int len, int past, int node,
+__device__ __forceinline__ bool kt_row_again(const Kv4Args& a, bool ask, const int32_t* table, int head, const T* q, int from, int len, int past, int node,
                                           unsigned long long tree, float* m, float* sum, float* acc) {
     const int lane = threadIdx.x & 31;
     constexpr int N = D / 32;
-    // this lane's token j: where its block lies (-1: it is not seen) and its score
-    auto score = [&](int j, long long* block) {
+    // where the block of token j lies (-1: there is none, or it is not seen)
+    auto seen = [&](int j) {
         const int at = j - past;
-        *block = -1;
-        if (j >= len || !(at < 0 || (a.tree ? at < kKv4MaxTree && tree >> at & 1ull : at <= node))) return kNegInf;
+        return j < len && (at < 0 || (a.tree ? at < kKv4MaxTree && tree >> at & 1ull : at <= node));
+    };
+    auto block_of = [&](int j) -> long long {
         const int sub = j / kKv4Block, per = (int)a.c.subs.d, page_at = a.c.subs(sub), page = __ldg(table + page_at);
-        if (page < 0 || page >= a.n_pages) return kNegInf;
-        *block = (((long long)page * a.c.n_k + head) * per + sub - page_at * per) * (kKv4Block * D + 128 * NG);
+        if (page < 0 || page >= a.n_pages) return -1;
+        return (((long long)page * a.c.n_k + head) * per + sub - page_at * per) * (kKv4Block * D + 128 * NG);
+    };
+    if (ask) {
+        // 1: a value that the row sees is not finite, 2: one that it does not
+        auto bad = [&](int j) {
+            const long long block = j < len ? block_of(j) : -1;
+            if (block < 0) return 0;
+            float odd = 0.f;
+            for (int g = 0; g < NG; ++g) odd = fmaf(0.f, kv4_pair<T>(reinterpret_cast<const uint32_t*>(a.c.base + block + 16 * D)[(NG + g) * 16 + (j & 15)]).y, odd);
+            return odd == 0.f ? 0 : seen(j) ? 1 : 2;
+        };
+        int found = 0;
+        for (int j = max(from, past); j < len; j += 32) found |= bad(j + lane);
+        found = __reduce_or_sync(0xffffffffu, found);
+        for (int j = from; !found && j < min(past, len); j += 32) found = __any_sync(0xffffffffu, j + lane < past && bad(j + lane));
+        if (found == 1) return false;
+    }
+    // this lane's token j: its score
+    auto score = [&](int j, long long* block) {
+        *block = seen(j) ? block_of(j) : -1;
+        if (*block < 0) return kNegInf;
         const unsigned char* blk = a.c.base + *block;
         float s = 0.f;
         for (int c = 0; c < D; ++c) {
@@ -143,6 +165,33 @@ __device__ __noinline__ void kt_row_again(const Kv4Args& a, const int32_t* table
     for (int o = 16; o; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
     *m = top;
     *sum = all;
+    return true;
+}
+
+// The rows of a warp that are to be computed again: those of `todo`, without a question those of `lost`.  Tokens from .. to of this block's part.
+template <typename T, int D, int NG>
+__device__ __noinline__ void kt_rows_again(const Kv4Args& a, uint32_t todo, uint32_t lost, const int32_t* table, int head, int split, int q0, int tok, int q_head,
+                                           unsigned long long tree, int from, int to, int past) {
+    const int lane = threadIdx.x & 31;
+    const bool whole = a.splits == 1;
+    for (; todo; todo &= todo - 1) {
+        const int r = __ffs(todo) - 1, tok_r = __shfl_sync(0xffffffffu, tok, r), head_r = __shfl_sync(0xffffffffu, q_head, r);
+        const unsigned long long tree_r = __shfl_sync(0xffffffffu, tree, r);
+        float acc[D / 32], m, sum;
+        if (!kt_row_again<T, D, NG>(a, !(lost >> r & 1u), table, head, static_cast<const T*>(a.q) + (q0 + tok_r) * a.ld_q + (long long)head_r * D, from, to, past, tok_r,
+                                    tree_r, &m, &sum, acc))
+            continue;
+        const long long at = (long long)(q0 + tok_r) * a.n_q + head_r, part = (long long)split * a.n_rows * a.n_q + at;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) {
+            if (whole) static_cast<T*>(a.out)[(long long)(q0 + tok_r) * a.ld_out + (long long)head_r * D + lane * (D / 32) + e] = Elem<T>::down(sum == 0.f ? 0.f : acc[e] / sum);
+            else a.part_o[part * D + lane * (D / 32) + e] = acc[e];
+        }
+        if (lane == 0) {
+            if (!whole) a.part_ml[part] = make_float2(sum == 0.f ? kKv4NoMax : m, sum);
+            else if (a.lse) a.lse[at] = sum == 0.f ? kNegInf : (m + log2f(sum)) * 0.69314718055994531f;
+        }
+    }
 }
 
 template <typename T, int D, int NG>
@@ -416,23 +465,9 @@ __global__ void __launch_bounds__(kKtThreads, 1) kv4_many_kernel(const __grid_co
         // Rows of finite weights whose result is not (values that they do not see may be the reason), and those that met tokens far apart.
         const bool again = live && (lost || (sum > 0.f && sum < __int_as_float(0x7f800000) && odd != 0.f));
         __syncwarp();
-        for (uint32_t todo = __ballot_sync(0xffffffffu, again); todo; todo &= todo - 1) {
-            const int r = __ffs(todo) - 1, tok_r = __shfl_sync(0xffffffffu, tok, r), head_r = __shfl_sync(0xffffffffu, q_head, r);
-            const unsigned long long tree_r = __shfl_sync(0xffffffffu, tree, r);
-            float acc[D / 32], m_r, sum_r;
-            kt_row_again<T, D, NG>(a, table, head, static_cast<const T*>(a.q) + (q0 + tok_r) * a.ld_q + (long long)head_r * D, step0 * kPaKeys,
-                                   min(len, (step0 + n) * kPaKeys), past, tok_r, tree_r, &m_r, &sum_r, acc);
-            const long long at_r = (long long)(q0 + tok_r) * a.n_q + head_r, part_r = (long long)split * a.n_rows * a.n_q + at_r;
-#pragma unroll
-            for (int e = 0; e < D / 32; ++e) {
-                if (whole) static_cast<T*>(a.out)[(long long)(q0 + tok_r) * a.ld_out + (long long)head_r * D + lane * (D / 32) + e] = Elem<T>::down(sum_r == 0.f ? 0.f : acc[e] / sum_r);
-                else a.part_o[part_r * D + lane * (D / 32) + e] = acc[e];
-            }
-            if (lane == 0) {
-                if (!whole) a.part_ml[part_r] = make_float2(sum_r == 0.f ? kKv4NoMax : m_r, sum_r);
-                else if (a.lse) a.lse[at_r] = sum_r == 0.f ? kNegInf : (m_r + log2f(sum_r)) * 0.69314718055994531f;
-            }
-        }
+        if (__any_sync(0xffffffffu, again))
+            kt_rows_again<T, D, NG>(a, __ballot_sync(0xffffffffu, again), __ballot_sync(0xffffffffu, lost), table, head, split, q0, tok, q_head, tree, step0 * kPaKeys,
+                                    min(len, (step0 + n) * kPaKeys), past);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kKtRegsFew));
         if (warp == 10) {
