@@ -596,7 +596,7 @@ int coral_lmhead_qk_rotate_backward(const coral_lmhead_qk_args *args, void *work
  * no key (Lk < Lq), or whose scores are all -inf, has out 0 and lse -inf.  Keys and values that a row does not see have no influence on it,
  * infinities and NaN too.
  * Rows of scores beyond 2^22 / log2(e), and rows that a value which is not finite may have reached unseen (fp16: seen too), are computed again one
- * by one: slower, a few milliseconds for a row of 100000 keys, but not less exact.
+ * by one, by 8 warps a SM: not less exact, but 0.15 us for a key of a row (16384 tokens of 8 heads of which one late value is NaN: 77 ms, not 0.5).
  *   type CORAL_TYPE_BF16 or _F16.  q, out [T x n_q x D], k, v [Tk x n_k x D], tokens ld_* apart; D a multiple of 8, 8 to 128; n_q a
  *   multiple of n_k.  q_offsets, k_offsets int64 [n_seq + 1], not decreasing, clamped to T and Tk; k_offsets NULL: those of the
  *   queries (Tk = T).  out_lse fp32 [T x n_q] or NULL.  Rows outside the sequences are left as they are.  out may not overlap an input.

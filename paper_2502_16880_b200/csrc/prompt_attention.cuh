@@ -238,35 +238,60 @@ struct PaUnit {
 // sums have room for.
 constexpr float kPaFar = 0x1p22f;
 
-// One row again, by a warp in fp32: only keys that it sees take part.  Four columns a lane.
+// One row again, by a warp in fp32: only keys that it sees take part.  Scores: sixteen lanes a key, eight columns each; values: four columns a lane.
 template <typename T>
 __device__ __noinline__ void pa_row_again(const PaArgs& a, const T* q, const T* k, const T* v, int seen, T* out, float* lse) {
-    const int lane = threadIdx.x & 31;
-    auto score = [&](int j) {
-        float s = 0.f;
-        for (int c = 0; c < a.D; c += 8) {
-            float x[8], y[8];
-            Elem<T>::load8(q + c, x);
-            Elem<T>::load8(k + (long long)j * a.ld_k + c, y);
+    const int lane = threadIdx.x & 31, part = lane & 15;
+    const bool on = part * 8 < a.D;
+    float x[8] = {};
+    if (on) Elem<T>::load8(q + part * 8, x);
+    // of key j0 + lane; eight loads on their way at a time
+    auto score = [&](int j0) {
+        float mine = 0.f;
+        for (int i0 = 0; i0 < 16; i0 += 8) {
+            float y[8][8], s[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s = fmaf(x[i], y[i], s);
+            for (int i = 0; i < 8; ++i) Elem<T>::load8(k + (long long)min(j0 + i0 + i + (lane & 16), seen - 1) * a.ld_k + (on ? part * 8 : 0), y[i]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s[i] = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[i] = fmaf(x[e], y[i][e], s[i]);
+                if (!on) s[i] = 0.f;
+            }
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (part == i0 + i) mine = s[i];
         }
-        return __fmul_rn(s, a.c);                              // rounded once for the maximum and the weight, whatever its size
+        return __fmul_rn(mine, a.c);                           // rounded once for the maximum and the weight, whatever its size
     };
     float top = kNegInf, sum = 0.f, acc[4] = {};
-    for (int j = lane; j < seen; j += 32) top = fmaxf(top, score(j));
+    for (int j0 = 0; j0 < seen; j0 += 32) {
+        const float s = score(j0);
+        if (j0 + lane < seen) top = fmaxf(top, s);
+    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (top == kNegInf) top = 0.f;
     for (int j0 = 0; j0 < seen; j0 += 32) {
-        const float p = j0 + lane < seen ? pa_exp2(score(j0 + lane) - top) : 0.f;
+        const float s = score(j0), p = j0 + lane < seen ? pa_exp2(s - top) : 0.f;
         sum += p;
-        for (int i = 0; i < min(32, seen - j0); ++i) {
-            const float w = __shfl_sync(0xffffffffu, p, i);
-            if (lane * 4 < a.D) {
-                const uint2 r = *reinterpret_cast<const uint2*>(v + (long long)(j0 + i) * a.ld_v + lane * 4);
+        const int n = min(32, seen - j0);
+        for (int i0 = 0; i0 < n; i0 += 8) {                    // eight values on their way at a time
+            uint2 r[8];
+            if (lane * 4 < a.D)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) r[i] = *reinterpret_cast<const uint2*>(v + (long long)(j0 + min(i0 + i, n - 1)) * a.ld_v + lane * 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float w = __shfl_sync(0xffffffffu, p, i0 + i);
+                if (lane * 4 >= a.D || i0 + i >= n) continue;
                 T h[4];
-                *reinterpret_cast<uint2*>(h) = r;
+                *reinterpret_cast<uint2*>(h) = r[i];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, Elem<T>::up(h[e]), acc[e]);
             }
@@ -286,6 +311,13 @@ __device__ __noinline__ void pa_row_again(const PaArgs& a, const T* q, const T* 
 
 // What stands in the first output of a row that is to be computed again until that is done: a NaN as no conversion gives it.
 constexpr uint16_t kPaAgain = 0x7fa1;
+// (ordered with the outputs' other stores and loads, which have other types)
+__device__ __forceinline__ void pa_mark(void* out) { asm volatile("st.global.u16 [%0], %1;" ::"l"(out), "h"(kPaAgain) : "memory"); }
+__device__ __forceinline__ bool pa_marked(const void* out) {
+    uint16_t w;
+    asm volatile("ld.global.u16 %0, [%1];" : "=h"(w) : "l"(out) : "memory");
+    return w == kPaAgain;
+}
 
 // Whether any of eight 16-bit elements is an infinity or a NaN.
 template <typename T>
@@ -619,7 +651,7 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
             if (live && a.lse) a.lse[(long long)(sh.q0 + tok) * a.n_q + head] = sum == 0.f ? kNegInf : (mc + log2f(sum)) * 0.69314718055994531f;
             // Rows of finite weights whose result is not (values that they do not see may be the reason), and those of scores too large.
             far = far && live;
-            if (far) *reinterpret_cast<uint16_t*>(out) = kPaAgain;
+            if (far) pa_mark(out);
             if (__any_sync(0xffffffffu, far || (live && sum > 0.f && sum < __int_as_float(0x7f800000) && odd != 0.f))) first_again = min(first_again, turn);
         }
         if (first_again < turns) {
@@ -635,7 +667,7 @@ prompt_attention_kernel(const PaArgs a, const __grid_constant__ CUtensorMap map_
                 T* out = static_cast<T*>(a.out) + (long long)(sh.q0 + tok) * a.ld_out + (long long)head * a.D;
                 bool odd = false, far = false;                     // by what this thread wrote
                 if (tok < sh.Lq) {
-                    far = *reinterpret_cast<const uint16_t*>(out) == kPaAgain;
+                    far = pa_marked(out);
                     for (int c = 0; c < a.D; c += 8) odd |= pa_bad8<T>(*reinterpret_cast<const uint4*>(out + c));
                 }
                 // Not finite, and rightly so: the row sees a value of that kind, and its last step held none that it does not see.  (fp16 has no
