@@ -17,10 +17,13 @@
 // finite although their sum is are computed again by a warp each, over the keys that they see, unless that is what the values they see
 // make of it; so are those of scores beyond kPaFar.  That takes as long as there are keys, so it comes when the block's turns are over and
 // no warp waits any more (the waits are bounded).
-// 8192 tokens, 32 query and 8 key heads of 128, bf16: 470 to 490 us, 1.15 PFLOP/s or 69 % of the measured product rate, and less under the
-// power limit (550).  It was 626 with steps of 128 keys and one buffer, 504 with 64 and two, 470 with the longest pairs of tiles first on as
-// many blocks as there are SMs and the next pair's operands loaded ahead.  What bounds it: a step of both tiles takes 1640 cycles, in which the products read operands from shared
-// memory for 1300 and the exponentials issue for 1100; either alone would be faster.
+// Weights are rounded to the type for their product (operand A is 16 bits wide; a second part of what is left would be half as many products
+// again): outputs are off by 2.0e-3 of their norm in bf16 and 2.9e-4 in fp16, by 1.5e-3 and 2.1e-4 with fp32 weights, their own rounding.
+// 8192 tokens, 32 query and 8 key heads of 128, bf16: 536 to 556 us by the power limit, 1.0 PFLOP/s or 59 to 61 % of the measured product rate
+// (470 us on one box that held its clocks; there it was 626 with steps of 128 keys and one buffer, 504 with 64 and two, 470 with the longest
+// pairs of tiles first on as many blocks as there are SMs and the next pair's operands loaded ahead).  What bounds it: a step of both tiles
+// takes 1640 cycles, in which the products read operands from shared memory for 1300 and the exponentials issue for 1100; either alone would
+// be faster.
 #pragma once
 #include <type_traits>
 
