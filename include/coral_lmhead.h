@@ -592,7 +592,8 @@ int coral_lmhead_qk_rotate_backward(const coral_lmhead_qk_args *args, void *work
  * there before; coral_lmhead_kv4_load brings those out of the cache).  For query i of Lq, with Lk keys, and query head h, with the
  * keys and values of head h / (n_q / n_k):
  *   out = sum_j softmax_j(scale q . k_j) v_j  over j <= i + Lk - Lq;  lse = log-sum-exp of scale q . k_j over the same
- * Scores, softmax statistics and sums in fp32; the weights are rounded to `type` for the product with the values.  A row that sees
+ * Scores, softmax statistics and sums in fp32 (of weights of up to 2^8 times the values before their division: the number of keys times the largest
+ * value has to stay in fp32's range); the weights are rounded to `type` for the product with the values.  A row that sees
  * no key (Lk < Lq), or whose scores are all -inf, has out 0 and lse -inf.  Keys and values that a row does not see have no influence on it,
  * infinities and NaN too.
  * Rows of scores beyond 2^22 / log2(e), and rows that a value which is not finite may have reached unseen (fp16: seen too), are computed again one
@@ -650,7 +651,7 @@ int coral_lmhead_kv4_load(const coral_lmhead_kv4_config *cfg, const void *cache_
  * sequence and query head h, with the keys and values of head h / (n_q / n_heads) as the cache holds them:
  *   out = sum_j softmax_j(scale q . k_j) v_j  over j <= lens - n + i (tree_mask NULL), or over the j < lens - n and those
  *   j = lens - n + b with bit b of the row's tree_mask word (a node sees its ancestors and itself);  lse = log-sum-exp of scale q . k_j.
- * Sums and softmax in fp32.  For the product with the values a weight times a value's step (next to the largest such product of the same row and
+ * Sums and softmax in fp32, sums undivided as in prompts.  For the product with the values a weight times a value's step (next to the largest such product of the same row and
  * group of columns), or from 33 rows of a key head on (max_q n_q / n_heads) a value, is rounded to fp16 (a weight too, where outputs are bf16).
  * Queries enter as fp16 next to the largest element of their row: what is 2^-39 of it is lost.  From 33 rows on so is what is 2^-39 of the largest key
  * of 64 tokens (but for tokens whose keys are all below 2^-17 of it).  A row that sees nothing has out 0 and lse -inf.
